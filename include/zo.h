@@ -352,6 +352,48 @@ ZO_API zo_status zo_perturb_noalloc(void* W, int64_t m, int64_t n, int64_t ldw, 
                                     uint32_t matrix_index, uint32_t t, int32_t qa, float ca,
                                     int32_t qb, float cb, float eps, void* stream);
 
+/*
+ * Layer normalisation over the rows of a matrix: the norm of the layers around the
+ * perturbed weights, and -- for a model's tail that is trained by backpropagation while the
+ * subspace steps train what lies below it -- its gradients.  The paper has no counterpart.
+ *
+ * zo_layernorm_forward -- for every row of X (rows x cols, row stride ldx elements)
+ *   h = X, or with a residual R (may be NULL) h = rnd(X + R), written to H;
+ *   mean = (1/cols) sum h,  rstd = ((1/cols) sum (h - mean)^2 + eps)^(-1/2);
+ *   Y = rnd((h - mean) rstd weight + bias).
+ *   X, R, Y, H: dtype; weight and bias (cols values; NULL = 1 and 0): wdtype; mean and rstd:
+ *   fp32, one per row, NULL where the backward pass is not wanted.  H is needed exactly
+ *   where R is given.
+ * zo_layernorm_backward -- from the gradient dY of Y, and X = the h above with its mean and
+ *   rstd:  g = dY weight,  xh = (X - mean) rstd,
+ *   dX = rnd(rstd (g - (1/cols) sum g - xh (1/cols) sum g xh) + dR)   (dR: the gradient that
+ *     reaches h past the norm; NULL = none),
+ *   dweight = rnd(sum over rows of dY xh),  dbias = rnd(sum over rows of dY)  (NULL = not
+ *     wanted; no rows: zero).
+ *   workspace: caller-owned device memory of at least zo_layernorm_workspace(rows, cols)
+ *     bytes, 16-byte aligned, for the column sums' partial rows (unused without dweight and
+ *     dbias); calls whose work overlaps need one each.
+ * Sums and statistics are held in fp32; the variance is taken about the mean, so a mean that
+ * is large against the spread costs no digits.  Every output is rounded once.  No
+ * atomics: the same inputs give the same bits.  A row
+ * with an infinity or NaN gives NaN in its own row of Y and dX (and in the column sums).
+ * Any alignment and any strides >= cols are taken; rows whose pointers, strides and width
+ * allow 16-byte accesses run faster.  0 <= rows < 2^31, 1 <= cols < 2^31.  Outputs must not
+ * overlap inputs.  Asynchronous on `stream` (void* cudaStream_t) of the current device.
+ */
+ZO_API zo_status zo_layernorm_forward(const void* X, int64_t ldx, const void* R, int64_t ldr,
+                                      int64_t rows, int64_t cols, int32_t dtype,
+                                      const void* weight, const void* bias, int32_t wdtype,
+                                      float eps, void* Y, int64_t ldy, void* H, int64_t ldh,
+                                      float* mean, float* rstd, void* stream);
+ZO_API int64_t zo_layernorm_workspace(int64_t rows, int64_t cols);
+ZO_API zo_status zo_layernorm_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx,
+                                       const void* dR, int64_t lddr, int64_t rows, int64_t cols,
+                                       int32_t dtype, const void* weight, int32_t wdtype,
+                                       const float* mean, const float* rstd, void* dX,
+                                       int64_t lddx, void* dweight, void* dbias, void* workspace,
+                                       int64_t workspace_bytes, void* stream);
+
 /* zo_status_string -- static description of a status code. */
 ZO_API const char* zo_status_string(int32_t status);
 

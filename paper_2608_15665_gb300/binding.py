@@ -94,6 +94,17 @@ _SIGNATURES = {
                                         _c.c_uint64, _c.c_uint32, _c.c_uint32, _c.c_int32,
                                         _c.c_float, _c.c_int32, _c.c_float, _c.c_float,
                                         _c.c_void_p]),
+    "zo_layernorm_forward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                          _c.c_int64, _c.c_int64, _c.c_int32, _c.c_void_p,
+                                          _c.c_void_p, _c.c_int32, _c.c_float, _c.c_void_p,
+                                          _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p,
+                                          _c.c_void_p, _c.c_void_p]),
+    "zo_layernorm_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64]),
+    "zo_layernorm_backward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                           _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
+                                           _c.c_int32, _c.c_void_p, _c.c_int32, _c.c_void_p,
+                                           _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p,
+                                           _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p]),
     "zo_status_string": (_c.c_char_p, [_c.c_int32]),
     "zo_last_error": (_c.c_char_p, []),
 }
@@ -287,3 +298,96 @@ def zo_philox_fill(seed, x1, x2, x3, out, stream=None):
 def zo_normal_fill(seed, x1, x2, x3, out, stream=None):
     _check(LIB.zo_normal_fill(int(seed) & (2**64 - 1), int(x1), int(x2), int(x3), _ptr(out),
                               out.numel(), _stream_handle(stream)), "zo_normal_fill")
+
+
+def _dtype_code(t, where, name):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return ZO_BF16
+    if t.dtype == torch.float32:
+        return ZO_F32
+    raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {t.dtype}: bf16 or fp32")
+
+
+def _rows(t, where, name, shape, dtype, device):
+    """(pointer, row stride) of a rows x cols matrix with unit column stride (None -> NULL)."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ZoError(ZO_ERR_SHAPE, where, f"{name} has shape {tuple(t.shape)}, "
+                                           f"expected {'2-D' if shape is None else tuple(shape)}")
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ZoError(ZO_ERR_SHAPE, where, f"{name} needs unit column stride and separate rows")
+    if dtype is not None and t.dtype != dtype:
+        raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {t.dtype}, expected {dtype}")
+    if device is not None and t.device != device:
+        raise ZoError(ZO_ERR_INVALID_ARG, where, f"{name} is on {t.device}, expected {device}")
+    return t.data_ptr(), max(t.stride(0), cols) if rows > 1 else cols
+
+
+def _vector(t, where, name, n, dtype, device):
+    """Pointer of a contiguous vector of n values (None -> NULL)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ZoError(ZO_ERR_SHAPE, where, f"{name} must be a contiguous vector of {n} values")
+    if t.dtype != dtype:
+        raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {t.dtype}, expected {dtype}")
+    if t.device != device:
+        raise ZoError(ZO_ERR_INVALID_ARG, where, f"{name} is on {t.device}, expected {device}")
+    return t.data_ptr()
+
+
+def zo_layernorm_forward(X, R, weight, bias, eps, Y, H=None, mean=None, rstd=None, stream=None):
+    """Y = LayerNorm(X (+ R)) row by row (see include/zo.h); every tensor is checked here,
+    since the C ABI cannot see the sizes behind its pointers."""
+    import torch
+    at = "zo_layernorm_forward"
+    px, ldx = _rows(X, at, "X", None, None, None)
+    shape, dt, dev = X.shape, X.dtype, X.device
+    code, n = _dtype_code(X, at, "X"), X.shape[1]
+    w = weight if weight is not None else bias
+    wdt = torch.float32 if w is None else w.dtype
+    wcode = ZO_F32 if w is None else _dtype_code(w, at, "weight")
+    pr, ldr = _rows(R, at, "R", shape, dt, dev)
+    py, ldy = _rows(Y, at, "Y", shape, dt, dev)
+    ph, ldh = _rows(H, at, "H", shape, dt, dev)
+    _check(LIB.zo_layernorm_forward(
+        px, ldx, pr, ldr, shape[0], n, code, _vector(weight, at, "weight", n, wdt, dev),
+        _vector(bias, at, "bias", n, wdt, dev), wcode, float(eps), py, ldy, ph, ldh,
+        _vector(mean, at, "mean", shape[0], torch.float32, dev),
+        _vector(rstd, at, "rstd", shape[0], torch.float32, dev), _stream_handle(stream)), at)
+
+
+def zo_layernorm_workspace(rows, cols):
+    """Bytes of workspace that zo_layernorm_backward needs for its column sums."""
+    return int(LIB.zo_layernorm_workspace(int(rows), int(cols)))
+
+
+def zo_layernorm_backward(dY, X, dR, weight, mean, rstd, dX, dweight=None, dbias=None,
+                          workspace=None, stream=None):
+    """dX, dweight and dbias of zo_layernorm_forward (see include/zo.h).  workspace: a
+    contiguous uint8 tensor of zo_layernorm_workspace(rows, cols) bytes."""
+    import torch
+    at = "zo_layernorm_backward"
+    px, ldx = _rows(X, at, "X", None, None, None)
+    shape, dt, dev = X.shape, X.dtype, X.device
+    code, (rows, n) = _dtype_code(X, at, "X"), X.shape
+    w = weight if weight is not None else dweight if dweight is not None else dbias
+    wdt = torch.float32 if w is None else w.dtype
+    wcode = ZO_F32 if w is None else _dtype_code(w, at, "weight")
+    pdy, lddy = _rows(dY, at, "dY", shape, dt, dev)
+    pdr, lddr = _rows(dR, at, "dR", shape, dt, dev)
+    pdx, lddx = _rows(dX, at, "dX", shape, dt, dev)
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise ZoError(ZO_ERR_INVALID_ARG, at, "workspace must be contiguous uint8 beside X")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+    _check(LIB.zo_layernorm_backward(
+        pdy, lddy, px, ldx, pdr, lddr, rows, n, code, _vector(weight, at, "weight", n, wdt, dev),
+        wcode, _vector(mean, at, "mean", rows, torch.float32, dev),
+        _vector(rstd, at, "rstd", rows, torch.float32, dev), pdx, lddx,
+        _vector(dweight, at, "dweight", n, wdt, dev), _vector(dbias, at, "dbias", n, wdt, dev),
+        ws, ws_bytes, _stream_handle(stream)), at)

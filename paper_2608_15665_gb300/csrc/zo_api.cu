@@ -11,27 +11,15 @@
 #include <string>
 #include <vector>
 
-#include <cudaTypedefs.h>
-
 #include "../../include/zo.h"
+#include "zo_host.h"
 #include "zo_kernels.h"
 
 namespace {
 
+using namespace zo::host;
+
 thread_local std::string g_last_error;
-
-zo_status cuda_fail(cudaError_t e, const char* what) {
-  g_last_error = std::string(what) + ": " + cudaGetErrorString(e);
-  return ZO_ERR_CUDA;
-}
-
-#define ZO_CUDA(call, what)                                   \
-  do {                                                        \
-    cudaError_t _e = (call);                                  \
-    if (_e != cudaSuccess) return cuda_fail(_e, what);        \
-  } while (0)
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 bool supported_rank(int32_t r) {
   return r == 4 || r == 8 || r == 16 || r == 32 || r == 64 || r == 128;
@@ -53,21 +41,6 @@ namespace {
 int64_t s_flag_words(int64_t s_cap) {
   return (s_cap / 256 + 1) * zo::kLinearPairCounters + zo::kLinearFewFlags;
 }
-
-// Makes a context's device current for the length of a call and gives the caller's back:
-// every kernel of a context runs on the device it was created on, whatever device the
-// calling thread has selected since.
-struct DeviceGuard {
-  int prev = -1;
-  bool switched = false;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) == cudaSuccess && prev != dev && cudaSetDevice(dev) == cudaSuccess)
-      switched = true;
-  }
-  ~DeviceGuard() {
-    if (switched) cudaSetDevice(prev);
-  }
-};
 
 }  // namespace
 
@@ -368,45 +341,6 @@ zo_status run_weight_pass(zo_ctx* c) {
   }
   ++c->launches;
   return record_stop(c);
-}
-
-PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-  }
-  return fn;
-}
-
-// 2-D tensor map of 16-bit elements (bf16, or fp16 with f16 = true): `cols` contiguous
-// elements per row, `rows` rows `row_bytes` apart, boxes of box_cols x box_rows with the
-// 128-byte swizzle.
-bool encode_16b_2d(CUtensorMap* tm, void* base, uint64_t cols, uint64_t rows, uint64_t row_bytes,
-                   uint32_t box_cols, uint32_t box_rows, bool f16,
-                   CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
-  auto enc = tensor_map_encoder();
-  if (!enc) return false;
-  const cuuint64_t dims[2] = {cols, rows};
-  const cuuint64_t strides[1] = {row_bytes};
-  const cuuint32_t box[2] = {box_cols, box_rows};
-  const cuuint32_t estr[2] = {1, 1};
-  return enc(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base,
-             dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-bool encode_bf16_2d(CUtensorMap* tm, void* base, uint64_t cols, uint64_t rows, uint64_t row_bytes,
-                    uint32_t box_cols, uint32_t box_rows,
-                    CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
-  return encode_16b_2d(tm, base, cols, rows, row_bytes, box_cols, box_rows, false, swizzle);
-}
-bool encode_f16_2d(CUtensorMap* tm, void* base, uint64_t cols, uint64_t rows, uint64_t row_bytes,
-                   uint32_t box_cols, uint32_t box_rows) {
-  return encode_16b_2d(tm, base, cols, rows, row_bytes, box_cols, box_rows, true);
 }
 
 // Tile table of the narrow-tile FMA pass (r in {4, 8}).
