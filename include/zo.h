@@ -394,6 +394,71 @@ ZO_API zo_status zo_layernorm_backward(const void* dY, int64_t lddy, const void*
                                        int64_t lddx, void* dweight, void* dbias, void* workspace,
                                        int64_t workspace_bytes, void* stream);
 
+/*
+ * Orthogonalised updates by Newton-Schulz products, and the Muon optimiser's step on them.
+ * The paper's subspace Adam has this as its counterpart for matrices trained by
+ * backpropagation (a model's tail), and for the r x r moments themselves: U_i and V_i are
+ * column-orthonormal, so orthogonalising M_i orthogonalises U_i M_i V_i^T.
+ *
+ *   X_0 = U / (||U||_F + eps), transposed where m > n (p x c, p = min(m, n));
+ *   X_(k+1) = a_k X_k + (b_k A + c_k A A) X_k,  A = X_k X_k^T,  k = 0 .. steps - 1;
+ *   NS(U) = X_steps, transposed back.
+ * Each step acts on the singular values alone, as s -> a s + b s^3 + c s^5.
+ *
+ * zo_muon_create -- bind the caller's matrices: W (weights, or the result of
+ *   zo_orthogonalize), G (the gradient, or the matrix to orthogonalise) and M (fp32
+ *   momentum, contiguous m x n; NULL = none).  Any element alignment and any row strides >= n
+ *   are taken.  The pointers must stay valid until zo_muon_destroy; the contents of G are read by
+ *   each call.  workspace: caller-owned device memory of at least zo_muon_workspace(mats,
+ *   n_mats) bytes, 256-byte aligned, kept until zo_muon_destroy and used by this context
+ *   alone.  The tables are copied to it on `stream` (void* cudaStream_t), on which every
+ *   later call launches.  Nothing else is allocated on the device.
+ * zo_orthogonalize -- W_i <- rnd(NS(G_i)) for every matrix.
+ * zo_muon_step -- for every matrix
+ *     M_i <- momentum M_i + G_i,  U_i = nesterov ? G_i + momentum M_i : M_i  (no M: U_i = G_i)
+ *     W_i <- rnd((1 - lr weight_decay) W_i - lr s_i NS(U_i)),
+ *   s_i by `adjust`: ZO_MUON_ADJUST_NONE 1, _ASPECT sqrt(max(1, m / n)), _RMS 0.2 sqrt(max(m, n)).
+ * steps: 1 .. 32; coeffs: host array of 3 steps floats a_0 b_0 c_0 a_1 ..., or NULL for the
+ *   quintic (3.4445, -4.7750, 2.0315) in every step.  Coefficients under which the singular
+ *   values can leave the range the iterates are held in are refused
+ *   (ZO_ERR_INVALID_ARG): with the bounds u_0 = 1, u_(k+1) = max |a s + b s^3 + c s^5| over
+ *   0 <= s <= u_k, every u_k, u_k^2 and max |b s^2 + c s^4| has to stay below 2^12.
+ * eps >= 0 (1e-7 is usual); a zero matrix gives zero (with eps = 0 too).
+ * Precision: sums are fp32.  Iterates are held as power-of-two-scaled fp16 pairs (~22
+ *   significant bits).  Their products are of fp32 grade where W is fp32 or min(m, n) <= 128;
+ *   for larger bf16 matrices the products take single fp16 factors (11 bits), whose error in
+ *   the result is of the order of rounding it to bf16.  A U with ||U||_F far below eps loses digits: the
+ *   scaled iterate resolves 2^-38.  A NaN or infinity in U_i gives NaN in all of W_i.
+ * Captured into a graph, the calls may be replayed on other contents of G, M and W.
+ */
+enum { ZO_MUON_ADJUST_NONE = 0, ZO_MUON_ADJUST_ASPECT = 1, ZO_MUON_ADJUST_RMS = 2 };
+
+typedef struct zo_muon_matrix {
+  void* W;            /* device; m x n, row stride ldw elements, dtype below */
+  const void* G;      /* device; m x n, row stride ldg elements, grad_dtype below */
+  float* M;           /* device; m x n contiguous fp32 momentum, or NULL */
+  int64_t m, n;
+  int64_t ldw, ldg;
+  int32_t dtype;      /* ZO_F32 or ZO_BF16 */
+  int32_t grad_dtype; /* ZO_F32 or ZO_BF16 */
+} zo_muon_matrix;
+
+typedef struct zo_muon_ctx zo_muon_ctx;
+
+ZO_API int64_t zo_muon_workspace(const zo_muon_matrix* mats, int32_t n_mats);
+ZO_API zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t n_mats,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+/* zo_muon_destroy -- synchronise the stream and free the context.  NULL is a no-op. */
+ZO_API zo_status zo_muon_destroy(zo_muon_ctx* ctx);
+ZO_API zo_status zo_orthogonalize(zo_muon_ctx* ctx, int32_t steps, const float* coeffs, float eps);
+ZO_API zo_status zo_muon_step(zo_muon_ctx* ctx, float momentum, int32_t nesterov, float lr,
+                              float weight_decay, int32_t adjust, int32_t steps,
+                              const float* coeffs, float eps);
+/* zo_muon_sync_status -- synchronise the stream; return (and clear) the device status word. */
+ZO_API zo_status zo_muon_sync_status(zo_muon_ctx* ctx);
+/* zo_muon_launches -- number of kernels this context has launched since zo_muon_create. */
+ZO_API int64_t zo_muon_launches(const zo_muon_ctx* ctx);
+
 /* zo_status_string -- static description of a status code. */
 ZO_API const char* zo_status_string(int32_t status);
 

@@ -33,6 +33,10 @@ ZO_SCHEME_DIRECT = 2
 ZO_OPT_ADAM = 0
 ZO_OPT_SGD = 1
 
+ZO_MUON_ADJUST_NONE = 0
+ZO_MUON_ADJUST_ASPECT = 1
+ZO_MUON_ADJUST_RMS = 2
+
 ZO_OPTION_WPASS_PATH = 0
 ZO_OPTION_TIMING = 1
 ZO_OPTION_TEST_WAIT_TIMEOUT = 2
@@ -58,6 +62,20 @@ class zo_matrix(ctypes.Structure):
         ("V", ctypes.c_void_p),
         ("M", ctypes.c_void_p),
         ("Vm", ctypes.c_void_p),
+    ]
+
+
+class zo_muon_matrix(ctypes.Structure):
+    _fields_ = [
+        ("W", ctypes.c_void_p),
+        ("G", ctypes.c_void_p),
+        ("M", ctypes.c_void_p),
+        ("m", ctypes.c_int64),
+        ("n", ctypes.c_int64),
+        ("ldw", ctypes.c_int64),
+        ("ldg", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
     ]
 
 
@@ -105,6 +123,15 @@ _SIGNATURES = {
                                            _c.c_int32, _c.c_void_p, _c.c_int32, _c.c_void_p,
                                            _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p,
                                            _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "zo_muon_workspace": (_c.c_int64, [_c.c_void_p, _c.c_int32]),
+    "zo_muon_create": (_c.c_int32, [_c.POINTER(_c.c_void_p), _c.c_void_p, _c.c_int32, _c.c_void_p,
+                                    _c.c_int64, _c.c_void_p]),
+    "zo_muon_destroy": (_c.c_int32, [_c.c_void_p]),
+    "zo_orthogonalize": (_c.c_int32, [_c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_float]),
+    "zo_muon_step": (_c.c_int32, [_c.c_void_p, _c.c_float, _c.c_int32, _c.c_float, _c.c_float,
+                                  _c.c_int32, _c.c_int32, _c.c_void_p, _c.c_float]),
+    "zo_muon_sync_status": (_c.c_int32, [_c.c_void_p]),
+    "zo_muon_launches": (_c.c_int64, [_c.c_void_p]),
     "zo_status_string": (_c.c_char_p, [_c.c_int32]),
     "zo_last_error": (_c.c_char_p, []),
 }
@@ -326,6 +353,11 @@ def _rows(t, where, name, shape, dtype, device):
     return t.data_ptr(), max(t.stride(0), cols) if rows > 1 else cols
 
 
+def _on_device(t, where):
+    if not t.is_cuda:
+        raise ZoError(ZO_ERR_INVALID_ARG, where, f"the tensors are on {t.device}, not on a GPU")
+
+
 def _vector(t, where, name, n, dtype, device):
     """Pointer of a contiguous vector of n values (None -> NULL)."""
     if t is None:
@@ -353,6 +385,7 @@ def zo_layernorm_forward(X, R, weight, bias, eps, Y, H=None, mean=None, rstd=Non
     pr, ldr = _rows(R, at, "R", shape, dt, dev)
     py, ldy = _rows(Y, at, "Y", shape, dt, dev)
     ph, ldh = _rows(H, at, "H", shape, dt, dev)
+    _on_device(X, at)
     _check(LIB.zo_layernorm_forward(
         px, ldx, pr, ldr, shape[0], n, code, _vector(weight, at, "weight", n, wdt, dev),
         _vector(bias, at, "bias", n, wdt, dev), wcode, float(eps), py, ldy, ph, ldh,
@@ -385,9 +418,81 @@ def zo_layernorm_backward(dY, X, dR, weight, mean, rstd, dX, dweight=None, dbias
         if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
             raise ZoError(ZO_ERR_INVALID_ARG, at, "workspace must be contiguous uint8 beside X")
         ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+    _on_device(X, at)
     _check(LIB.zo_layernorm_backward(
         pdy, lddy, px, ldx, pdr, lddr, rows, n, code, _vector(weight, at, "weight", n, wdt, dev),
         wcode, _vector(mean, at, "mean", rows, torch.float32, dev),
         _vector(rstd, at, "rstd", rows, torch.float32, dev), pdx, lddx,
         _vector(dweight, at, "dweight", n, wdt, dev), _vector(dbias, at, "dbias", n, wdt, dev),
         ws, ws_bytes, _stream_handle(stream)), at)
+
+
+def make_muon_matrix(W, G, M=None):
+    """zo_muon_matrix for torch tensors: W and G m x n (bf16 or fp32, any row stride), M a
+    contiguous m x n fp32 momentum or None."""
+    import torch
+    at = "make_muon_matrix"
+    pw, ldw = _rows(W, at, "W", None, None, None)
+    pg, ldg = _rows(G, at, "G", W.shape, None, W.device)
+    if M is not None and (tuple(M.shape) != tuple(W.shape) or not M.is_contiguous()):
+        raise ZoError(ZO_ERR_SHAPE, at, "M must be contiguous with W's shape")
+    if M is not None and (M.dtype != torch.float32 or M.device != W.device):
+        raise ZoError(ZO_ERR_DTYPE, at, "M must be fp32 beside W")
+    _on_device(W, at)
+    return zo_muon_matrix(pw, pg, _ptr(M), W.shape[0], W.shape[1], ldw, ldg,
+                          _dtype_code(W, at, "W"), _dtype_code(G, at, "G"))
+
+
+def _coeffs(steps, coeffs, where):
+    """(steps, address, keep-alive) of a sequence of (a, b, c) per step, or of the default."""
+    import numpy as np
+    if coeffs is None:
+        return int(steps), None, None
+    arr = np.ascontiguousarray(np.asarray(coeffs, dtype=np.float32))
+    if arr.shape != (int(steps), 3):
+        raise ZoError(ZO_ERR_SHAPE, where, f"coeffs has shape {arr.shape}, expected {(steps, 3)}")
+    return int(steps), arr.ctypes.data, arr
+
+
+def zo_muon_workspace(mats):
+    """Bytes of device workspace for a context over `mats`."""
+    arr = (zo_muon_matrix * len(mats))(*mats)
+    n = int(LIB.zo_muon_workspace(arr, len(mats)))
+    if n <= 0:
+        raise ZoError(ZO_ERR_INVALID_ARG, "zo_muon_workspace", zo_last_error())
+    return n
+
+
+def zo_muon_create(mats, workspace, stream=None):
+    arr = (zo_muon_matrix * len(mats))(*mats)
+    ctx = ctypes.c_void_p()
+    _check(LIB.zo_muon_create(ctypes.byref(ctx), arr, len(mats), _ptr(workspace),
+                              workspace.numel() * workspace.element_size(),
+                              _stream_handle(stream)), "zo_muon_create")
+    return ctx
+
+
+def zo_muon_destroy(ctx):
+    _check(LIB.zo_muon_destroy(ctx), "zo_muon_destroy")
+
+
+def zo_orthogonalize(ctx, steps=5, coeffs=None, eps=1e-7):
+    n, ptr, keep = _coeffs(steps, coeffs, "zo_orthogonalize")
+    _check(LIB.zo_orthogonalize(ctx, n, ptr, float(eps)), "zo_orthogonalize")
+    del keep
+
+
+def zo_muon_step(ctx, momentum, nesterov, lr, weight_decay, adjust, steps=5, coeffs=None,
+                 eps=1e-7):
+    n, ptr, keep = _coeffs(steps, coeffs, "zo_muon_step")
+    _check(LIB.zo_muon_step(ctx, float(momentum), int(bool(nesterov)), float(lr),
+                            float(weight_decay), int(adjust), n, ptr, float(eps)), "zo_muon_step")
+    del keep
+
+
+def zo_muon_sync_status(ctx):
+    _check(LIB.zo_muon_sync_status(ctx), "zo_muon_sync_status")
+
+
+def zo_muon_launches(ctx):
+    return int(LIB.zo_muon_launches(ctx))

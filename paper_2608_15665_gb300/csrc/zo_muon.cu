@@ -1,0 +1,415 @@
+// Host runtime and C ABI of the orthogonalised updates (declared in include/zo.h): the
+// workspace's layout, the groups that share it, and the launches of a call.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <new>
+#include <vector>
+
+#include "../../include/zo.h"
+#include "zo_host.h"
+#include "zo_ops.h"
+
+namespace {
+
+using namespace zo::host;
+
+constexpr int32_t kMaxSteps = 32;
+constexpr double kMuonA = 3.4445, kMuonB = -4.7750, kMuonC = 2.0315;
+// Matrices are worked on in groups that share the iterates' buffers, of at most this many
+// bytes (or one matrix): enough work in every launch to fill the device, without a second
+// copy of a whole model's weights.
+constexpr int64_t kGroupBytes = int64_t(1) << 30;
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+struct Group {
+  int32_t unit0 = 0, n_units = 0;
+  int32_t sym0 = 0, n_sym = 0;          // tiles on or below the diagonals (p x p)
+  int32_t apply0 = 0, n_apply = 0;      // tiles of X' (p x c)
+};
+
+// Where everything lies in the workspace: the status word, the tables, the norm's partial
+// sums, then the buffers that the groups share.
+struct Layout {
+  std::vector<zo::OrthoMat> mats;       // buffer pointers hold byte offsets until placed
+  std::vector<int4> units, tiles;
+  std::vector<Group> groups;
+  int64_t mats_at = 0, units_at = 0, tiles_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
+  int64_t tables_end = 0;
+};
+
+zo_status check_matrix(const zo_muon_matrix& m) {
+  if (!m.W || !m.G) return refuse(ZO_ERR_INVALID_ARG, "null W or G in zo_muon_matrix");
+  if ((m.dtype != ZO_F32 && m.dtype != ZO_BF16) ||
+      (m.grad_dtype != ZO_F32 && m.grad_dtype != ZO_BF16))
+    return refuse(ZO_ERR_DTYPE, "unknown dtype in zo_muon_matrix");
+  if (m.m < 1 || m.n < 1 || m.m >= (int64_t(1) << 24) || m.n >= (int64_t(1) << 24) ||
+      m.ldw < m.n || m.ldg < m.n || m.ldw >= (int64_t(1) << 40) || m.ldg >= (int64_t(1) << 40) ||
+      std::min(m.m, m.n) > (int64_t(1) << 16))
+    return refuse(ZO_ERR_SHAPE, "zo_muon_matrix: need 1 <= m, n < 2^24, min(m, n) <= 2^16, "
+                                "n <= ldw, ldg < 2^40");
+  const auto aligned = [](const void* p, int32_t dtype) {
+    return reinterpret_cast<uintptr_t>(p) % (dtype == ZO_BF16 ? 2 : 4) == 0;
+  };
+  if (!aligned(m.W, m.dtype) || !aligned(m.G, m.grad_dtype) || !aligned(m.M, ZO_F32))
+    return refuse(ZO_ERR_ALIGN, "zo_muon_matrix: a buffer is not aligned to its elements");
+  return ZO_OK;
+}
+
+zo_status check_matrices(const zo_muon_matrix* mats, int32_t n_mats) {
+  if (!mats || n_mats <= 0) return refuse(ZO_ERR_INVALID_ARG, "need at least one matrix");
+  for (int32_t i = 0; i < n_mats; ++i) {
+    const zo_status st = check_matrix(mats[i]);
+    if (st != ZO_OK) return st;
+  }
+  return ZO_OK;
+}
+
+uint16_t* at_offset(int64_t off) { return reinterpret_cast<uint16_t*>(off); }
+
+zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
+  Layout& L = *out;
+  int64_t used = 0, most = 0, slots = 0;
+  for (int32_t i = 0; i < n_mats; ++i) {
+    const zo_muon_matrix& m = mats[i];
+    zo::OrthoMat d{};
+    d.G = m.G;
+    d.W = m.W;
+    d.M = m.M;
+    d.ldg = m.ldg;
+    d.ldw = m.ldw;
+    d.m = m.m;
+    d.n = m.n;
+    d.p = std::min(m.m, m.n);
+    d.c = std::max(m.m, m.n);
+    d.grad_bf16 = m.grad_dtype == ZO_BF16;
+    d.bf16 = m.dtype == ZO_BF16;
+    d.tall = m.m > m.n;
+    d.pairs = zo::ortho_pairs(d.bf16, d.p);
+    d.ldx = round_up(d.c, 64);
+    d.ldp = round_up(d.p, 64);
+    const int64_t x_bytes = d.p * d.ldx * 2, a_bytes = d.p * d.ldp * 2;
+    const int64_t bytes = (d.pairs ? 4 : 3) * x_bytes + (d.pairs ? 4 : 2) * a_bytes;
+    if (L.groups.empty() || used + bytes > kGroupBytes) {
+      L.groups.emplace_back();
+      L.groups.back().unit0 = (int32_t)L.units.size();
+      used = 0;
+    }
+    Group& g = L.groups.back();
+    int64_t off = used;
+    const auto take = [&](int64_t n) {
+      const int64_t at = off;
+      off += n;                                     // every size is a multiple of 128
+      return at_offset(at);
+    };
+    d.xh[0] = take(x_bytes);
+    d.xh[1] = take(x_bytes);
+    d.xl[0] = take(x_bytes);
+    d.xl[1] = d.pairs ? take(x_bytes) : d.xl[0];
+    d.ah = take(a_bytes);
+    d.bh = take(a_bytes);
+    if (d.pairs) {
+      d.al = take(a_bytes);
+      d.bl = take(a_bytes);
+    }
+    used = round_up(off, 256);
+    most = std::max(most, used);
+    d.unit0 = (int32_t)slots;
+    for (int64_t r = 0; r < d.m; r += zo::kOrthoUnitRows)
+      for (int64_t c = 0; c < d.n; c += zo::kOrthoUnitCols)
+        L.units.push_back(make_int4(i, (int)r, (int)c, (int)slots++));
+    d.n_units = (int32_t)(slots - d.unit0);
+    if (slots > (int64_t(1) << 30))
+      return refuse(ZO_ERR_SHAPE, "zo_muon: too many elements in one context");
+    g.n_units += d.n_units;
+    L.mats.push_back(d);
+  }
+  // tiles, group by group
+  size_t next = 0;
+  for (Group& g : L.groups) {
+    const size_t first = next;
+    int64_t units = 0;
+    while (next < L.mats.size() && units + L.mats[next].n_units <= g.n_units)
+      units += L.mats[next++].n_units;
+    g.sym0 = (int32_t)L.tiles.size();
+    for (size_t i = first; i < next; ++i)
+      for (int64_t r = 0; r < L.mats[i].p; r += zo::kOrthoTile)
+        for (int64_t c = 0; c <= r; c += zo::kOrthoTile)
+          L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
+    g.n_sym = (int32_t)L.tiles.size() - g.sym0;
+    g.apply0 = (int32_t)L.tiles.size();
+    for (size_t i = first; i < next; ++i)
+      for (int64_t r = 0; r < L.mats[i].p; r += zo::kOrthoTile)
+        for (int64_t c = 0; c < L.mats[i].c; c += zo::kOrthoTile)
+          L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
+    g.n_apply = (int32_t)L.tiles.size() - g.apply0;
+    if (L.tiles.size() > (size_t(1) << 28))
+      return refuse(ZO_ERR_SHAPE, "zo_muon: too many tiles in one context");
+  }
+  int64_t at = 256;                                 // the status word
+  const auto place = [&](int64_t bytes) {
+    const int64_t here = at;
+    at = round_up(at + bytes, 256);
+    return here;
+  };
+  L.mats_at = place(sizeof(zo::OrthoMat) * L.mats.size());
+  L.units_at = place(sizeof(int4) * L.units.size());
+  L.tiles_at = place(sizeof(int4) * L.tiles.size());
+  L.tables_end = at;
+  L.partial_at = place(sizeof(float) * slots);
+  L.buffers_at = at;
+  L.bytes = at + most;
+  return ZO_OK;
+}
+
+// The extreme values of a s + b s^3 + c s^5 over 0 <= s <= u, and of b t + c t^2 over
+// 0 <= t <= u^2.
+double most_of_step(double a, double b, double c, double u) {
+  double most = std::fabs(u * (a + u * u * (b + c * u * u)));
+  // stationary where a + 3 b t + 5 c t^2 = 0, t = s^2
+  double roots[2];
+  int n = 0;
+  if (c != 0.0) {
+    const double disc = 9 * b * b - 20 * a * c;
+    if (disc >= 0) {
+      roots[n++] = (-3 * b + std::sqrt(disc)) / (10 * c);
+      roots[n++] = (-3 * b - std::sqrt(disc)) / (10 * c);
+    }
+  } else if (b != 0.0) {
+    roots[n++] = -a / (3 * b);
+  }
+  for (int k = 0; k < n; ++k)
+    if (roots[k] > 0 && roots[k] < u * u) {
+      const double s = std::sqrt(roots[k]);
+      most = std::max(most, std::fabs(s * (a + roots[k] * (b + c * roots[k]))));
+    }
+  return most;
+}
+double most_of_poly(double b, double c, double u) {
+  const double t = u * u;
+  double most = std::fabs(t * (b + c * t));
+  if (c != 0.0) {
+    const double v = -b / (2 * c);
+    if (v > 0 && v < t) most = std::max(most, std::fabs(v * (b + c * v)));
+  }
+  return most;
+}
+
+// The exponent e with bound 2^e in (2^14, 2^15.5]: below fp16's 65504 with room for rounding.
+int32_t exponent_for(double bound) {
+  int e = 0;
+  std::frexp(std::max(bound, 1e-3) * 1.05, &e);     // bound 1.05 = f 2^e, 0.5 <= f < 1
+  return 15 - e;
+}
+
+// Steps with the exponents of their iterates.
+zo_status plan_steps(int32_t steps, const float* coeffs, std::vector<zo::OrthoStep>* out) {
+  if (steps < 1 || steps > kMaxSteps)
+    return refuse(ZO_ERR_INVALID_ARG, "zo_muon: need 1 <= steps <= 32");
+  double u = 1.0;
+  for (int32_t k = 0; k < steps; ++k) {
+    zo::OrthoStep s{};
+    s.a = coeffs ? coeffs[3 * k] : (float)kMuonA;
+    s.b = coeffs ? coeffs[3 * k + 1] : (float)kMuonB;
+    s.c = coeffs ? coeffs[3 * k + 2] : (float)kMuonC;
+    if (!std::isfinite(s.a) || !std::isfinite(s.b) || !std::isfinite(s.c))
+      return refuse(ZO_ERR_INVALID_ARG, "zo_muon: a coefficient is not finite");
+    const double poly = most_of_poly(s.b, s.c, u), next = most_of_step(s.a, s.b, s.c, u);
+    if (!(u * u < 4096.0) || !(poly < 4096.0) || !(next < 4096.0))
+      return refuse(ZO_ERR_INVALID_ARG,
+                    "zo_muon: with these coefficients the singular values can pass 2^12");
+    s.ex = exponent_for(u);
+    s.ea = exponent_for(u * u);
+    s.eb = exponent_for(poly);
+    s.ex_next = exponent_for(next);
+    s.k = k;
+    s.last = k + 1 == steps;
+    out->push_back(s);
+    u = next;
+  }
+  return ZO_OK;
+}
+
+}  // namespace
+
+struct zo_muon_ctx {
+  int device = 0;
+  cudaStream_t stream = nullptr;
+  Layout plan;
+  uint8_t* ws = nullptr;
+  int64_t launches = 0;
+};
+
+namespace {
+
+zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const float* coeffs) {
+  std::vector<zo::OrthoStep> st;
+  const zo_status ok = plan_steps(steps, coeffs, &st);
+  if (ok != ZO_OK) return ok;
+  const Layout& L = c->plan;
+  const auto* mats = reinterpret_cast<const zo::OrthoMat*>(c->ws + L.mats_at);
+  const auto* units = reinterpret_cast<const int4*>(c->ws + L.units_at);
+  const auto* tiles = reinterpret_cast<const int4*>(c->ws + L.tiles_at);
+  auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
+  for (const Group& g : L.groups) {
+    ZO_CUDA(zo::launch_ortho_momentum(mats, units + g.unit0, g.n_units, u, partial, c->stream),
+            "orthogonalisation: momentum kernel");
+    ZO_CUDA(zo::launch_ortho_scale(mats, units + g.unit0, g.n_units, u, st[0].ex, partial,
+                                   c->stream),
+            "orthogonalisation: scaling kernel");
+    c->launches += 2;
+    for (const zo::OrthoStep& s : st) {
+      ZO_CUDA(zo::launch_ortho_product(mats, tiles + g.sym0, g.n_sym, zo::kOrthoGram, s, u, c->stream),
+              "orthogonalisation: product kernel");
+      ZO_CUDA(zo::launch_ortho_product(mats, tiles + g.sym0, g.n_sym, zo::kOrthoPoly, s, u, c->stream),
+              "orthogonalisation: product kernel");
+      ZO_CUDA(zo::launch_ortho_product(mats, tiles + g.apply0, g.n_apply, zo::kOrthoApply, s, u,
+                                       c->stream),
+              "orthogonalisation: product kernel");
+      c->launches += 3;
+    }
+  }
+  return ZO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t zo_muon_workspace(const zo_muon_matrix* mats, int32_t n_mats) {
+  try {
+    Layout L;
+    if (check_matrices(mats, n_mats) != ZO_OK || plan(mats, n_mats, &L) != ZO_OK) return 0;
+    return L.bytes;
+  } catch (const std::bad_alloc&) {
+    refuse(ZO_ERR_NOMEM, "zo_muon_workspace: out of host memory");
+    return 0;
+  }
+}
+
+zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t n_mats,
+                         void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!out) return ZO_ERR_INVALID_ARG;
+  *out = nullptr;
+  try {
+    zo_status st = check_matrices(mats, n_mats);
+    if (st != ZO_OK) return st;
+    std::unique_ptr<zo_muon_ctx> c(new zo_muon_ctx());
+    st = plan(mats, n_mats, &c->plan);
+    if (st != ZO_OK) return st;
+    Layout& L = c->plan;
+    if (!workspace || workspace_bytes < L.bytes)
+      return refuse(ZO_ERR_INVALID_ARG,
+                    "zo_muon_create: the workspace is missing or smaller than zo_muon_workspace");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+      return refuse(ZO_ERR_ALIGN, "zo_muon_create: the workspace must be 256-byte aligned");
+    int dev = 0, major = 0, minor = 0;
+    ZO_CUDA(cudaGetDevice(&dev), "cudaGetDevice");
+    ZO_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev), "device");
+    ZO_CUDA(cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev), "device");
+    if (major != 10 || minor != 3)
+      return refuse(ZO_ERR_CUDA, "this library is built for sm_103a (GB300) only");
+    c->device = dev;
+    c->stream = reinterpret_cast<cudaStream_t>(stream);
+    c->ws = static_cast<uint8_t*>(workspace);
+    uint8_t* buffers = c->ws + L.buffers_at;
+    for (zo::OrthoMat& d : L.mats) {
+      const auto put = [&](uint16_t*& p) {
+        p = reinterpret_cast<uint16_t*>(buffers + reinterpret_cast<int64_t>(p));
+      };
+      put(d.xh[0]);
+      put(d.xh[1]);
+      put(d.xl[0]);
+      put(d.xl[1]);
+      put(d.ah);
+      put(d.bh);
+      if (d.pairs) {
+        put(d.al);
+        put(d.bl);
+      }
+    }
+    // one copy of the status word (0) and every table
+    std::vector<uint8_t> image((size_t)L.tables_end, 0);
+    std::memcpy(image.data() + L.mats_at, L.mats.data(), sizeof(zo::OrthoMat) * L.mats.size());
+    std::memcpy(image.data() + L.units_at, L.units.data(), sizeof(int4) * L.units.size());
+    std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(int4) * L.tiles.size());
+    ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),
+            "upload tables");
+    L.mats.clear();
+    L.units.clear();
+    L.tiles.clear();
+    *out = c.release();
+    return ZO_OK;
+  } catch (const std::bad_alloc&) {
+    return refuse(ZO_ERR_NOMEM, "zo_muon_create: out of host memory");
+  }
+}
+
+zo_status zo_muon_destroy(zo_muon_ctx* c) {
+  if (!c) return ZO_OK;
+  DeviceGuard guard(c->device);
+  const cudaError_t e = cudaStreamSynchronize(c->stream);
+  delete c;
+  if (e != cudaSuccess) return cuda_fail(e, "zo_muon_destroy");
+  return ZO_OK;
+}
+
+zo_status zo_orthogonalize(zo_muon_ctx* c, int32_t steps, const float* coeffs, float eps) {
+  if (!c) return ZO_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || !std::isfinite(eps))
+    return refuse(ZO_ERR_INVALID_ARG, "zo_orthogonalize: need a finite eps >= 0");
+  DeviceGuard guard(c->device);
+  zo::OrthoUpdate u{};
+  u.eps = eps;
+  try {
+    return run(c, u, steps, coeffs);
+  } catch (const std::bad_alloc&) {
+    return refuse(ZO_ERR_NOMEM, "zo_orthogonalize: out of host memory");
+  }
+}
+
+zo_status zo_muon_step(zo_muon_ctx* c, float momentum, int32_t nesterov, float lr,
+                       float weight_decay, int32_t adjust, int32_t steps, const float* coeffs,
+                       float eps) {
+  if (!c) return ZO_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || !std::isfinite(eps) || !std::isfinite(lr) || !std::isfinite(weight_decay) ||
+      !(momentum >= 0.0f && momentum < 1.0f))
+    return refuse(ZO_ERR_INVALID_ARG,
+                  "zo_muon_step: need finite scalars, eps >= 0 and momentum in [0, 1)");
+  if (adjust < ZO_MUON_ADJUST_NONE || adjust > ZO_MUON_ADJUST_RMS)
+    return refuse(ZO_ERR_INVALID_ARG, "zo_muon_step: unknown adjust");
+  DeviceGuard guard(c->device);
+  zo::OrthoUpdate u{};
+  u.momentum = momentum;
+  u.step = 1;
+  u.nesterov = nesterov != 0;
+  u.adjust = adjust;
+  u.keep = (float)(1.0 - (double)lr * (double)weight_decay);
+  u.lr = lr;
+  u.eps = eps;
+  try {
+    return run(c, u, steps, coeffs);
+  } catch (const std::bad_alloc&) {
+    return refuse(ZO_ERR_NOMEM, "zo_muon_step: out of host memory");
+  }
+}
+
+zo_status zo_muon_sync_status(zo_muon_ctx* c) {
+  if (!c) return ZO_ERR_INVALID_ARG;
+  DeviceGuard guard(c->device);
+  uint32_t s = 0;
+  ZO_CUDA(cudaMemcpyAsync(&s, c->ws, sizeof(s), cudaMemcpyDeviceToHost, c->stream), "read status");
+  ZO_CUDA(cudaStreamSynchronize(c->stream), "stream synchronize");
+  if (s != 0) {
+    ZO_CUDA(cudaMemsetAsync(c->ws, 0, sizeof(uint32_t), c->stream), "clear status");
+    ZO_CUDA(cudaStreamSynchronize(c->stream), "stream synchronize");
+    return refuse(ZO_ERR_TIMEOUT, "a device-side wait ran out");
+  }
+  return ZO_OK;
+}
+
+int64_t zo_muon_launches(const zo_muon_ctx* c) { return c ? c->launches : 0; }
+
+}  // extern "C"

@@ -30,4 +30,55 @@ cudaError_t launch_layernorm_forward(const LayerNormArgs& a, cudaStream_t s);
 int64_t layernorm_partial_rows(int64_t rows, int64_t cols, int32_t sms);
 cudaError_t launch_layernorm_backward(const LayerNormArgs& a, int32_t sms, cudaStream_t s);
 
+// ---- Newton-Schulz orthogonalisation and the Muon update (zo_ortho.cu) ----------------
+// One matrix: U (m x n) is worked on as X (p x c, p = min(m, n)), transposed where m > n.
+// Iterates are held as fp16 values of x 2^e, with e of the step (OrthoStep).
+struct OrthoMat {
+  const void* G;
+  void* W;
+  float* M;
+  int64_t ldg, ldw, m, n, p, c;
+  int32_t grad_bf16, bf16, tall;
+  int32_t pairs;                    // products of hi + lo pairs (ortho_pairs)
+  int32_t unit0, n_units;           // its slots of the norm's partial sums
+  int64_t ldx, ldp;                 // row strides of X, and of A and B (multiples of 64)
+  uint16_t *xh[2], *xl[2];          // X_k in xh[k & 1], xl[k & 1].  Without pairs no other
+                                    // tile reads an element's lo part: one buffer serves both
+  uint16_t *ah, *al, *bh, *bl;      // A and B = b A + c A A (lo parts only with pairs)
+};
+// kOrthoUnitRows x kOrthoUnitCols elements of U: (matrix, first row, first column, slot)
+constexpr int kOrthoUnitRows = 64, kOrthoUnitCols = 256;
+constexpr int kOrthoTile = 64;      // a tile of a product: (matrix, first row, first column)
+
+enum OrthoPhase : int32_t { kOrthoGram = 0, kOrthoPoly = 1, kOrthoApply = 2 };
+
+struct OrthoStep {
+  float a, b, c;
+  int32_t ex, ea, eb;               // exponents of X_k, A and B
+  int32_t ex_next;                  // of X_(k+1)
+  int32_t k;                        // index of the step: X_k is in xh[k & 1]
+  int32_t last;                     // the result goes to W instead of X_(k+1)
+};
+struct OrthoUpdate {
+  float momentum;
+  int32_t step;                     // 0: U = G, W <- NS(U); 1: the Muon update
+  int32_t nesterov, adjust;
+  float keep, lr;                   // W <- keep W - lr s NS(U)
+  float eps;
+};
+
+// fp32 results take products of fp32 grade.  So do bf16 results of at most 128 rows: their few
+// singular directions do not average rounding out (8 x 8: 4.1e-3 of the result's norm with
+// single factors, rounding the result 1.7e-3), and their time is latency, not products.
+inline bool ortho_pairs(bool bf16, int64_t p) { return !bf16 || p <= 128; }
+
+cudaError_t launch_ortho_momentum(const OrthoMat* mats, const int4* units, int32_t n_units,
+                                  const OrthoUpdate& u, float* partial, cudaStream_t s);
+cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t n_units,
+                               const OrthoUpdate& u, int32_t ex, const float* partial,
+                               cudaStream_t s);
+cudaError_t launch_ortho_product(const OrthoMat* mats, const int4* tiles, int32_t n_tiles,
+                                 OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
+                                 cudaStream_t s);
+
 }  // namespace zo

@@ -81,3 +81,74 @@ class LayerNorm(torch.autograd.Function):
         dx, dw, db = layer_norm_backward(dy.contiguous(), x, weight, mean, rstd,
                                          wdtype=ctx.wdtype, want_weight=need_w, want_bias=need_b)
         return dx, dw, db, None
+
+
+ADJUST = {"none": zb.ZO_MUON_ADJUST_NONE, "aspect": zb.ZO_MUON_ADJUST_ASPECT,
+          "rms": zb.ZO_MUON_ADJUST_RMS}
+
+
+class _MuonContext:
+    """A context over matrices and its workspace, on PyTorch's current stream (or `stream`)."""
+
+    def __init__(self, weights, grads, momenta, stream):
+        mats = [zb.make_muon_matrix(W, G, M) for W, G, M in zip(weights, grads, momenta)]
+        self.ctx = None
+        dev = weights[0].device
+        with torch.cuda.device(dev):
+            self.stream = torch.cuda.current_stream() if stream is None else stream
+            with torch.cuda.stream(self.stream):
+                self.workspace = torch.empty(zb.zo_muon_workspace(mats), dtype=torch.uint8,
+                                             device=dev)
+            self.ctx = zb.zo_muon_create(mats, self.workspace, self.stream)
+
+    def sync(self):
+        zb.zo_muon_sync_status(self.ctx)
+
+    def close(self):
+        if self.ctx is not None:
+            zb.zo_muon_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Orthogonalizer(_MuonContext):
+    """``op()`` orthogonalises every input by Newton-Schulz steps into its output (allocated
+    with the input's shape and type if not given).  All on one CUDA device."""
+
+    def __init__(self, inputs, outputs=None, stream=None):
+        self.inputs = list(inputs)
+        self.outputs = ([torch.empty(G.shape, dtype=G.dtype, device=G.device) for G in self.inputs]
+                        if outputs is None else list(outputs))
+        if len(self.outputs) != len(self.inputs):
+            raise ValueError("as many outputs as inputs are needed")
+        super().__init__(self.outputs, self.inputs, [None] * len(self.inputs), stream)
+
+    def __call__(self, steps=5, coeffs=None, eps=1e-7):
+        zb.zo_orthogonalize(self.ctx, steps, coeffs, eps)
+        return self.outputs
+
+
+class Muon(_MuonContext):
+    """The Muon optimiser over a list of weights (bf16 or fp32, on one CUDA device) whose
+    gradients live in ``grads`` (allocated beside the weights, zero, if not given) and whose
+    fp32 momenta in ``momenta``."""
+
+    def __init__(self, weights, grads=None, momenta=None, stream=None):
+        self.weights = list(weights)
+        self.grads = ([torch.zeros(W.shape, dtype=W.dtype, device=W.device) for W in self.weights]
+                      if grads is None else list(grads))
+        self.momenta = ([torch.zeros(W.shape, dtype=torch.float32, device=W.device)
+                         for W in self.weights] if momenta is None else list(momenta))
+        if not len(self.weights) == len(self.grads) == len(self.momenta):
+            raise ValueError("as many gradients and momenta as weights are needed")
+        super().__init__(self.weights, self.grads, self.momenta, stream)
+
+    def step(self, lr, momentum=0.95, nesterov=True, weight_decay=0.0, adjust="aspect", steps=5,
+             coeffs=None, eps=1e-7):
+        zb.zo_muon_step(self.ctx, momentum, nesterov, lr, weight_decay, ADJUST[adjust], steps,
+                        coeffs, eps)
