@@ -26,8 +26,8 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 struct Group {
   int32_t unit0 = 0, n_units = 0;
-  int32_t sym0 = 0, n_sym = 0;          // tiles on or below the diagonals (p x p)
-  int32_t apply0 = 0, n_apply = 0;      // tiles of X' (p x c)
+  // by single and by pair products: tiles on or below the diagonals (p x p), tiles of X' (p x c)
+  int32_t sym0[2] = {}, n_sym[2] = {}, apply0[2] = {}, n_apply[2] = {};
 };
 
 // Where everything lies in the workspace: the status word, the tables, the norm's partial
@@ -36,7 +36,7 @@ struct Layout {
   std::vector<zo::OrthoMat> mats;       // buffer pointers hold byte offsets until placed
   std::vector<int4> units, tiles;
   std::vector<Group> groups;
-  int64_t mats_at = 0, units_at = 0, tiles_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
+  int64_t mats_at = 0, maps_at = 0, units_at = 0, tiles_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
   int64_t tables_end = 0;
 };
 
@@ -88,6 +88,7 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     d.bf16 = m.dtype == ZO_BF16;
     d.tall = m.m > m.n;
     d.pairs = zo::ortho_pairs(d.bf16, d.p);
+    d.wide_rows = aligned16(m.W) && m.ldw * (d.bf16 ? 2 : 4) % 16 == 0;
     d.ldx = round_up(d.c, 64);
     d.ldp = round_up(d.p, 64);
     const int64_t x_bytes = d.p * d.ldx * 2, a_bytes = d.p * d.ldp * 2;
@@ -133,18 +134,21 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     int64_t units = 0;
     while (next < L.mats.size() && units + L.mats[next].n_units <= g.n_units)
       units += L.mats[next++].n_units;
-    g.sym0 = (int32_t)L.tiles.size();
-    for (size_t i = first; i < next; ++i)
-      for (int64_t r = 0; r < L.mats[i].p; r += zo::kOrthoTile)
-        for (int64_t c = 0; c <= r; c += zo::kOrthoTile)
-          L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
-    g.n_sym = (int32_t)L.tiles.size() - g.sym0;
-    g.apply0 = (int32_t)L.tiles.size();
-    for (size_t i = first; i < next; ++i)
-      for (int64_t r = 0; r < L.mats[i].p; r += zo::kOrthoTile)
-        for (int64_t c = 0; c < L.mats[i].c; c += zo::kOrthoTile)
-          L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
-    g.n_apply = (int32_t)L.tiles.size() - g.apply0;
+    for (int pr = 0; pr < 2; ++pr) {
+      const int cols = zo::ortho_tile_cols(pr != 0);
+      g.sym0[pr] = (int32_t)L.tiles.size();
+      for (size_t i = first; i < next; ++i)
+        for (int64_t r = 0; L.mats[i].pairs == pr && r < L.mats[i].p; r += zo::kOrthoTileRows)
+          for (int64_t c = 0; c < std::min(r + zo::kOrthoTileRows, L.mats[i].p); c += cols)
+            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
+      g.n_sym[pr] = (int32_t)L.tiles.size() - g.sym0[pr];
+      g.apply0[pr] = (int32_t)L.tiles.size();
+      for (size_t i = first; i < next; ++i)
+        for (int64_t r = 0; L.mats[i].pairs == pr && r < L.mats[i].p; r += zo::kOrthoTileRows)
+          for (int64_t c = 0; c < L.mats[i].c; c += cols)
+            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
+      g.n_apply[pr] = (int32_t)L.tiles.size() - g.apply0[pr];
+    }
     if (L.tiles.size() > (size_t(1) << 28))
       return refuse(ZO_ERR_SHAPE, "zo_muon: too many tiles in one context");
   }
@@ -155,6 +159,7 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     return here;
   };
   L.mats_at = place(sizeof(zo::OrthoMat) * L.mats.size());
+  L.maps_at = place((int64_t)sizeof(CUtensorMap) * zo::kOrthoMaps * L.mats.size());
   L.units_at = place(sizeof(int4) * L.units.size());
   L.tiles_at = place(sizeof(int4) * L.tiles.size());
   L.tables_end = at;
@@ -162,6 +167,20 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
   L.buffers_at = at;
   L.bytes = at + most;
   return ZO_OK;
+}
+
+// The tensor maps of one matrix (its buffers placed).
+bool encode_maps(const zo::OrthoMat& d, CUtensorMap* m) {
+  uint16_t* buf[8] = {d.xh[0], d.xh[1], d.xl[0], d.xl[1], d.ah, d.al, d.bh, d.bl};
+  for (int k = 0; k < 8; ++k) {
+    if (!buf[k]) continue;
+    const int64_t cols = k < 4 ? d.c : d.p, ld = k < 4 ? d.ldx : d.ldp;
+    if (!encode_f16_2d(m + k, buf[k], cols, d.p, ld * 2, 64, 64) ||
+        !encode_16b_2d(m + zo::kMapStoreX + k, buf[k], cols, d.p, ld * 2, 32, 32, true,
+                       CU_TENSOR_MAP_SWIZZLE_64B))
+      return false;
+  }
+  return true;
 }
 
 // The extreme values of a s + b s^3 + c s^5 over 0 <= s <= u, and of b t + c t^2 over
@@ -239,6 +258,7 @@ struct zo_muon_ctx {
   cudaStream_t stream = nullptr;
   Layout plan;
   uint8_t* ws = nullptr;
+  int32_t n_pairs = 0;
   int64_t launches = 0;
 };
 
@@ -252,6 +272,8 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   const auto* mats = reinterpret_cast<const zo::OrthoMat*>(c->ws + L.mats_at);
   const auto* units = reinterpret_cast<const int4*>(c->ws + L.units_at);
   const auto* tiles = reinterpret_cast<const int4*>(c->ws + L.tiles_at);
+  const auto* maps = reinterpret_cast<const CUtensorMap*>(c->ws + L.maps_at);
+  auto* status = reinterpret_cast<uint32_t*>(c->ws);
   auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
   for (const Group& g : L.groups) {
     ZO_CUDA(zo::launch_ortho_momentum(mats, units + g.unit0, g.n_units, u, partial, c->stream),
@@ -260,16 +282,17 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
                                    c->stream),
             "orthogonalisation: scaling kernel");
     c->launches += 2;
-    for (const zo::OrthoStep& s : st) {
-      ZO_CUDA(zo::launch_ortho_product(mats, tiles + g.sym0, g.n_sym, zo::kOrthoGram, s, u, c->stream),
-              "orthogonalisation: product kernel");
-      ZO_CUDA(zo::launch_ortho_product(mats, tiles + g.sym0, g.n_sym, zo::kOrthoPoly, s, u, c->stream),
-              "orthogonalisation: product kernel");
-      ZO_CUDA(zo::launch_ortho_product(mats, tiles + g.apply0, g.n_apply, zo::kOrthoApply, s, u,
-                                       c->stream),
-              "orthogonalisation: product kernel");
-      c->launches += 3;
-    }
+    for (const zo::OrthoStep& s : st)
+      for (const zo::OrthoPhase phase : {zo::kOrthoGram, zo::kOrthoPoly, zo::kOrthoApply})
+        for (int pr = 0; pr < 2; ++pr) {
+          const bool apply = phase == zo::kOrthoApply;
+          const int32_t n = apply ? g.n_apply[pr] : g.n_sym[pr];
+          if (n == 0) continue;
+          ZO_CUDA(zo::launch_ortho_product(mats, maps, tiles + (apply ? g.apply0[pr] : g.sym0[pr]), n,
+                                           pr != 0, c->n_pairs, phase, s, u, status, c->stream),
+                  "orthogonalisation: product kernel");
+          ++c->launches;
+        }
   }
   return ZO_OK;
 }
@@ -330,9 +353,17 @@ zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t 
         put(d.bl);
       }
     }
+    std::vector<CUtensorMap> maps(zo::kOrthoMaps * L.mats.size());
+    for (size_t i = 0; i < L.mats.size(); ++i)
+      if (!encode_maps(L.mats[i], &maps[zo::kOrthoMaps * i]))
+        return refuse(ZO_ERR_CUDA, "zo_muon_create: cuTensorMapEncodeTiled rejected a descriptor");
+    c->n_pairs = zo::ortho_max_pairs();
+    if (c->n_pairs <= 0)
+      return refuse(ZO_ERR_CUDA, "zo_muon_create: no cluster of the product kernel fits");
     // one copy of the status word (0) and every table
     std::vector<uint8_t> image((size_t)L.tables_end, 0);
     std::memcpy(image.data() + L.mats_at, L.mats.data(), sizeof(zo::OrthoMat) * L.mats.size());
+    std::memcpy(image.data() + L.maps_at, maps.data(), sizeof(CUtensorMap) * maps.size());
     std::memcpy(image.data() + L.units_at, L.units.data(), sizeof(int4) * L.units.size());
     std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(int4) * L.tiles.size());
     ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),

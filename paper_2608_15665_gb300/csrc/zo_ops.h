@@ -41,6 +41,7 @@ struct OrthoMat {
   int32_t grad_bf16, bf16, tall;
   int32_t pairs;                    // products of hi + lo pairs (ortho_pairs)
   int32_t unit0, n_units;           // its slots of the norm's partial sums
+  int32_t wide_rows;                // W's rows start on 16 bytes
   int64_t ldx, ldp;                 // row strides of X, and of A and B (multiples of 64)
   uint16_t *xh[2], *xl[2];          // X_k in xh[k & 1], xl[k & 1].  Without pairs no other
                                     // tile reads an element's lo part: one buffer serves both
@@ -48,7 +49,16 @@ struct OrthoMat {
 };
 // kOrthoUnitRows x kOrthoUnitCols elements of U: (matrix, first row, first column, slot)
 constexpr int kOrthoUnitRows = 64, kOrthoUnitCols = 256;
-constexpr int kOrthoTile = 64;      // a tile of a product: (matrix, first row, first column)
+// A tile of a product: (matrix, first row, first column, 0)
+constexpr int kOrthoTileRows = 256;
+__host__ __device__ constexpr int ortho_tile_cols(bool pairs) { return pairs ? 128 : 256; }
+
+// Tensor maps of one matrix: 64 x 64 loads of X_k (hi of even and odd k, lo of even and odd
+// k), of A and of B (hi, lo), and the 32 x 32 stores in the same order.
+enum OrthoMap : int32_t {
+  kMapX = 0, kMapA = 4, kMapB = 6, kMapStoreX = 8, kMapStoreA = 12, kMapStoreB = 14,
+  kOrthoMaps = 16
+};
 
 enum OrthoPhase : int32_t { kOrthoGram = 0, kOrthoPoly = 1, kOrthoApply = 2 };
 
@@ -77,8 +87,11 @@ cudaError_t launch_ortho_momentum(const OrthoMat* mats, const int4* units, int32
 cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t n_units,
                                const OrthoUpdate& u, int32_t ex, const float* partial,
                                cudaStream_t s);
-cudaError_t launch_ortho_product(const OrthoMat* mats, const int4* tiles, int32_t n_tiles,
-                                 OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
+// Clusters of the product kernels that fit on the device at once
+int32_t ortho_max_pairs();
+cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, const int4* tiles,
+                                 int32_t n_tiles, bool pairs, int32_t n_pairs, OrthoPhase phase,
+                                 const OrthoStep& st, const OrthoUpdate& u, uint32_t* status,
                                  cudaStream_t s);
 
 }  // namespace zo

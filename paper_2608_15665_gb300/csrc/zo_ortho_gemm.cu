@@ -1,0 +1,514 @@
+// The products of a Newton-Schulz step on SM pairs: M = 256 tcgen05.mma.cta_group::2 across
+// the two SMs of a cluster, fp16 operands, fp32 accumulators in Tensor Memory.
+//
+//   Gram:   A  = X X^T            both operands rows of X, K along them
+//   Poly:   B  = b A + c A A      both operands rows of A (A is symmetric)
+//   Apply:  X' = a X + B X        rows of B, and X itself as an MN-major operand: the
+//                                 descriptor's transpose bit reads X's columns, so no
+//                                 transposed copy of X is kept
+//
+// Pair tile = 256 x N of the result; CTA c of the cluster holds rows 128 c .. of the A
+// operand and N / 2 of the B operand's rows (columns of X).  A and B are symmetric: tiles that
+// meet or lie left of the diagonal blocks of 256 are computed, those left of them are stored a
+// second time transposed.  The accumulators are buffered: the epilogue of one runs under the
+// next one's products.
+//
+// kPairs = false: hi parts only, N = 256 (32 KB per 64 of K for 128 x 256 x 64 multiply-adds
+// of an SM), one accumulation per tile.
+// kPairs = true: hi + lo, the products hi.lo + lo.hi + hi.hi.  The tensor cores' fp32 sums
+// round towards zero, which over K = 5120 moved an 8 x 5120 result by 3.3e-5 of its norm; so
+// every 128 of K the accumulator is drained and added up in the epilogue's registers, rounded
+// to nearest, and the small products come first.  N = 128: 64 sums per thread.
+// b A, a X and the stored X_k are a pair's sum in both.
+//
+// Roles (320 threads per CTA, one CTA per SM):
+//   warp 0, lane 0: TMA producer of this CTA's halves; both halves of a stage complete their
+//                   bytes on the leader's full barrier, which the leader's producer arms.
+//   warp 1:         Tensor Memory; in the leader lane 0 issues the MMAs.
+//   warps 2..9:     epilogue: warp w reads TMEM lanes 32 (w % 4) .. + 31 and one half of the
+//                   columns, 32 at a time, and stores 32 x 32 boxes by TMA (64-byte swizzle).
+// Every wait is bounded; a give-up sets the abort flag of both CTAs and the status word.
+#include <algorithm>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "zo_cluster.cuh"
+#include "zo_launch.cuh"
+#include "zo_ops.h"
+#include "zo_sm100.cuh"
+#include "zo_tc_common.cuh"
+
+namespace zo {
+namespace {
+
+using namespace sm100;
+using namespace cta2;
+using tc::exp2i;
+
+constexpr int kTileRows = 256;
+constexpr int kBlockBytes = 64 * 128;                 // a TMA box: 64 rows x 64 fp16
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kBoxBytes = 32 * 32 * 2;
+constexpr int kOutBytes = kEpiWarps * 2 * kBoxBytes;  // a direct and a mirrored box per warp
+constexpr int kRing = 192 * 1024;
+constexpr int kTmemCols = 512;
+constexpr size_t kSmem = kRing + kOutBytes + 1024 /*barriers*/ + 1024 /*align*/;
+static_assert(kSmem <= 227 * 1024, "shared memory per CTA");
+constexpr long long kWait = 4000000000LL;             // ~2 s at 2 GHz
+
+struct Shared {
+  uint64_t full[8], empty[8];
+  uint64_t acc_full[4], acc_empty[4];
+  uint64_t drain;                // one commit after the leader's last MMA
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+__device__ __forceinline__ void give_up(Shared& sh, uint32_t* status) {
+  atomicOr(status, 1u);
+  *reinterpret_cast<volatile int*>(&sh.abort_flag) = 1;
+  store_peer(&sh.abort_flag, 1);
+}
+
+// Descriptor of an MN-major operand in 128-byte swizzled blocks of 64 columns x 64 K-rows:
+// K-rows 128 bytes apart, groups of eight 1024 bytes apart (stride offset), blocks of 64
+// columns 8192 bytes apart (leading offset).
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(8192u >> 4) << 16;
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;
+  d |= static_cast<uint64_t>(1u) << 46;
+  d |= static_cast<uint64_t>(2u) << 61;
+  return d;
+}
+constexpr uint32_t kMnMajorB = 1u << 16;               // instruction descriptor: B MN-major
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+struct Phase {
+  int phase;
+  OrthoStep st;
+  OrthoUpdate u;
+};
+
+__device__ __forceinline__ int64_t depth_of(const OrthoMat& mt, int phase) {
+  return phase == kOrthoGram ? mt.c : mt.p;
+}
+
+// W <- keep W - lr s v, or W <- v, of 32 values of one row of X.  `w` points at the first;
+// the next is `step` elements on, `n` are inside.
+template <typename T, bool kWide>
+__device__ __forceinline__ void write_weights(T* w, int64_t step, int n, const float (&v)[32],
+                                              const OrthoUpdate& u, float rate) {
+  if constexpr (kWide) {            // 32 neighbours of a 16-byte aligned row
+    constexpr int kE = 16 / sizeof(T);
+#pragma unroll
+    for (int q = 0; q < 32; q += kE) {
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (u.step) raw = *reinterpret_cast<const uint4*>(w + q);
+      uint32_t r[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) {
+          const float o = u.step ? fmaf(-rate, v[q + e], u.keep * __uint_as_float(r[e])) : v[q + e];
+          r[e] = __float_as_uint(o);
+        } else {
+          float a = v[q + 2 * e], b = v[q + 2 * e + 1];
+          if (u.step) {
+            a = fmaf(-rate, a, u.keep * __uint_as_float(r[e] << 16));
+            b = fmaf(-rate, b, u.keep * __uint_as_float(r[e] & 0xFFFF0000u));
+          }
+          const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+          r[e] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+      }
+      *reinterpret_cast<uint4*>(w + q) = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+  } else {
+    float old[32];
+    if (u.step) {
+#pragma unroll
+      for (int q = 0; q < 32; ++q)
+        if (q < n) old[q] = static_cast<float>(w[q * step]);
+    }
+#pragma unroll
+    for (int q = 0; q < 32; ++q)
+      if (q < n) w[q * step] = static_cast<T>(u.step ? fmaf(-rate, v[q], u.keep * old[q]) : v[q]);
+  }
+}
+
+template <bool kPairs>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restrict__ maps,
+                  const int4* __restrict__ tiles, int n_tiles, const Phase ph,
+                  uint32_t* __restrict__ status) {
+  constexpr int kCols = ortho_tile_cols(kPairs);
+  constexpr int kABytes = 2 * kBlockBytes, kBBytes = kCols / 128 * kBlockBytes;   // per CTA
+  constexpr int kStageBytes = (kPairs ? 2 : 1) * (kABytes + kBBytes);
+  constexpr int kStages = kRing / kStageBytes;
+  constexpr int kSeg = 2;                            // kPairs: stages of one accumulation
+  constexpr int kBufs = kTmemCols / kCols;
+  constexpr int kWarpCols = kCols / 2, kChunks = kWarpCols / 32;
+  static_assert(kStages <= 8 && kBufs <= 4 && sizeof(Shared) <= 1024);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  uint8_t* out_smem = smem + kRing;
+  Shared& sh = *reinterpret_cast<Shared*>(out_smem + kOutBytes);
+  const uint32_t rank = cluster_rank();
+  const bool leader = rank == 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const volatile int* abort = &sh.abort_flag;
+  const int phase = ph.phase;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&sh.full[s], 1);
+      mbar_init(&sh.empty[s], 1);
+    }
+    for (int s = 0; s < kBufs; ++s) {
+      mbar_init(&sh.acc_full[s], 1);
+      mbar_init(&sh.acc_empty[s], 2 * kEpiWarps);
+    }
+    mbar_init(&sh.drain, 1);
+    sh.abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc_pair(&sh.tmem_base, kTmemCols);
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem_base;
+  pdl_wait();
+  pdl_trigger();
+
+  if (warp == 0 && lane == 0) {
+    // ---------------------------------------------------------------- operands (this CTA)
+    int64_t it = 0;
+    bool ok = true;
+    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+      const int4 tl = tiles[t];
+      const int64_t steps = (depth_of(mats[tl.x], phase) + 63) / 64;
+      const CUtensorMap* m = maps + (int64_t)tl.x * kOrthoMaps;
+      const int cur = ph.st.k & 1;
+      const CUtensorMap* ah = m + (phase == kOrthoGram ? kMapX + cur
+                                   : phase == kOrthoPoly ? kMapA : kMapB);
+      const CUtensorMap* al = ah + (phase == kOrthoGram ? 2 : 1);
+      const CUtensorMap* bh = m + (phase == kOrthoPoly ? kMapA : kMapX + cur);
+      const CUtensorMap* bl = bh + (phase == kOrthoPoly ? 1 : 2);
+      const int i0 = tl.y + 128 * (int)rank, j0 = tl.z + kCols / 2 * (int)rank;
+      for (int64_t k = 0; k < steps; ++k, ++it) {
+        const int s = (int)(it % kStages);
+        if (!mbar_wait_bounded(&sh.empty[s], (uint32_t)(((it / kStages) & 1) ^ 1), abort, kWait)) {
+          ok = false;
+          break;
+        }
+        if (leader) mbar_arrive_expect_tx(&sh.full[s], 2 * kStageBytes);
+        const int k0 = (int)(64 * k);
+        // hi parts of A and B, then the lo parts
+        uint8_t* dst = smem + s * kStageBytes;
+#pragma unroll
+        for (int part = 0; part < (kPairs ? 2 : 1); ++part) {
+          const CUtensorMap* a = part ? al : ah;
+          const CUtensorMap* bm = part ? bl : bh;
+#pragma unroll
+          for (int q = 0; q < 2; ++q, dst += kBlockBytes)
+            tma_load_2d_to_leader(dst, a, k0, i0 + 64 * q, &sh.full[s]);
+#pragma unroll
+          for (int q = 0; q < kCols / 128; ++q, dst += kBlockBytes) {
+            if (phase == kOrthoApply) tma_load_2d_to_leader(dst, bm, j0 + 64 * q, k0, &sh.full[s]);
+            else tma_load_2d_to_leader(dst, bm, k0, j0 + 64 * q, &sh.full[s]);
+          }
+        }
+      }
+    }
+    if (!ok) give_up(sh, status);
+    // the leader's MMAs have released every stage this CTA filled
+    for (int s = 0; s < kStages; ++s) {
+      const int64_t last = tc::last_in_slot(it, s, kStages);
+      if (last >= 0)
+        mbar_wait_bounded(&sh.empty[s], (uint32_t)((last / kStages) & 1), nullptr, kWait);
+    }
+  } else if (warp == 1 && lane == 0 && leader) {
+    // ---------------------------------------------------------------- MMA issuer (leader)
+    const bool mn = phase == kOrthoApply;
+    const uint32_t idesc = idesc_f16_f32(kTileRows, kCols) | (mn ? kMnMajorB : 0u);
+    int64_t it = 0, n_acc = 0;
+    bool ok = true;
+    // the four MMAs of one stage and product: hi.lo (0), lo.hi (1), hi.hi (2)
+    const auto products = [&](uint32_t d, int64_t at, int prod, bool fresh) {
+      const uint32_t base = smem_u32(smem + (int)(at % kStages) * kStageBytes);
+      const uint32_t a = base + (prod == 1 ? kABytes + kBBytes : 0);
+      const uint32_t b = base + kABytes + (prod == 0 ? kABytes + kBBytes : 0);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const uint64_t bd = mn ? sdesc_mn_sw128(b + 2048 * kk) : sdesc_k_sw128(b + 32 * kk);
+        mma_pair_ss(d, sdesc_k_sw128(a + 32 * kk), bd, idesc, fresh && kk == 0 ? 0u : 1u);
+      }
+    };
+    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+      const int64_t steps = (depth_of(mats[tiles[t].x], phase) + 63) / 64;
+      const int64_t seg = kPairs ? kSeg : steps;
+      for (int64_t k0 = 0; k0 < steps && ok; k0 += seg, ++n_acc) {
+        const int64_t n = min(seg, steps - k0);
+        const int acc = (int)(n_acc % kBufs);
+        const uint32_t d = tmem + (uint32_t)(acc * kCols);
+        if (!mbar_wait_bounded(&sh.acc_empty[acc], (uint32_t)(((n_acc / kBufs) & 1) ^ 1), abort,
+                               kWait)) {
+          ok = false;
+          break;
+        }
+        for (int64_t k = 0; k < n; ++k) {
+          const int s = (int)((it + k) % kStages);
+          if (!mbar_wait_bounded(&sh.full[s], (uint32_t)(((it + k) / kStages) & 1), abort, kWait)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if constexpr (!kPairs) {
+            products(d, it + k, 2, k == 0);
+            commit_both(&sh.empty[s]);
+          }
+        }
+        if (!ok) break;
+        if constexpr (kPairs) {
+          for (int prod = 0; prod < 3; ++prod)
+            for (int64_t k = 0; k < n; ++k) products(d, it + k, prod, prod == 0 && k == 0);
+          for (int64_t k = 0; k < n; ++k) commit_both(&sh.empty[(it + k) % kStages]);
+        }
+        commit_both(&sh.acc_full[acc]);
+        it += n;
+      }
+    }
+    if (!ok) give_up(sh, status);
+    // every MMA has completed before Tensor Memory is freed
+    commit_both(&sh.drain);
+    mbar_wait_bounded(&sh.drain, 0u, nullptr, kWait);
+  } else if (warp >= 2) {
+    // ---------------------------------------------------------------- epilogue (each CTA)
+    const int g = warp & 3;                        // TMEM lane group
+    const int half = (warp - 2) >> 2;              // half of the columns
+    uint8_t* direct = out_smem + (warp - 2) * 2 * kBoxBytes;
+    uint8_t* mirror = direct + kBoxBytes;
+    int64_t n_acc = 0;
+    bool ok = true;
+    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+      const int4 tl = tiles[t];
+      const OrthoMat& mt = mats[tl.x];
+      const CUtensorMap* m = maps + (int64_t)tl.x * kOrthoMaps;
+      const int cur = ph.st.k & 1;
+      const int64_t i0 = tl.y + 128 * (int64_t)rank + 32 * g, i = i0 + lane;
+      const int64_t p = mt.p, cols = phase == kOrthoApply ? mt.c : mt.p;
+      const uint32_t col0 = ((uint32_t)(32 * g) << 16) + (uint32_t)(kWarpCols * half);
+      uint32_t raw[kPairs ? kChunks : 1][32];
+      int acc = 0;
+      if constexpr (kPairs) {
+        // the segments' sums, added up in fp32
+        const int64_t segs = (depth_of(mt, phase) + 64 * kSeg - 1) / (64 * kSeg);
+#pragma unroll
+        for (int q = 0; q < kChunks; ++q)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) raw[q][e] = 0u;
+        for (int64_t sg = 0; sg < segs; ++sg, ++n_acc) {
+          acc = (int)(n_acc % kBufs);
+          if (!mbar_wait_bounded(&sh.acc_full[acc], (uint32_t)((n_acc / kBufs) & 1), abort, kWait)) {
+            ok = false;
+            break;
+          }
+          __syncwarp();
+          tc_fence_after();
+#pragma unroll
+          for (int q = 0; q < kChunks; ++q) {
+            uint32_t part[32];
+            tmem_ld_32x32b_x32(tmem + col0 + (uint32_t)(acc * kCols + 32 * q), part);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              raw[q][e] = __float_as_uint(__uint_as_float(raw[q][e]) + __uint_as_float(part[e]));
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_leader(&sh.acc_empty[acc]);
+        }
+      } else {
+        acc = (int)(n_acc % kBufs);
+        ok = mbar_wait_bounded(&sh.acc_full[acc], (uint32_t)((n_acc / kBufs) & 1), abort, kWait);
+        ++n_acc;
+        __syncwarp();
+        tc_fence_after();
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int q = 0; q < kChunks; ++q) {
+        const int64_t j0 = tl.z + kWarpCols * half + 32 * q;
+        if (i0 >= p || j0 >= cols) continue;       // the same in every lane
+        if constexpr (!kPairs) {
+          tmem_ld_32x32b_x32(tmem + col0 + (uint32_t)(acc * kCols + 32 * q), raw[0]);
+          tmem_ld_wait();
+        }
+        const uint32_t (&sum)[32] = raw[kPairs ? q : 0];
+        float v[32];
+        if (phase == kOrthoGram) {
+          const float s = exp2i(ph.st.ea - 2 * ph.st.ex);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]) * s;
+        } else {
+          // b A + c A A, or a X + B X: the matrix itself is added to the product
+          const bool poly = phase == kOrthoPoly;
+          const uint16_t* hi = (poly ? mt.ah : mt.xh[cur]) + i * (poly ? mt.ldp : mt.ldx) + j0;
+          const uint16_t* lo = (poly ? mt.al : mt.xl[cur]) + i * (poly ? mt.ldp : mt.ldx) + j0;
+          const bool two = !poly || kPairs;
+          const float s0 = poly ? ph.st.b * exp2i(ph.st.eb - ph.st.ea)
+                                : ph.st.a * exp2i(ph.st.last ? -ph.st.ex : ph.st.ex_next - ph.st.ex);
+          const float s1 = poly ? ph.st.c * exp2i(ph.st.eb - 2 * ph.st.ea)
+                                : exp2i((ph.st.last ? 0 : ph.st.ex_next) - ph.st.ex - ph.st.eb);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint4 h = make_uint4(0, 0, 0, 0), l = h;
+            if (i < p) {
+              h = *reinterpret_cast<const uint4*>(hi + e);
+              if (two) l = *reinterpret_cast<const uint4*>(lo + e);
+            }
+            const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const float2 x = unpack2(hw[w]), y = unpack2(lw[w]);
+              v[e + 2 * w] = fmaf(s0, x.x + y.x, s1 * __uint_as_float(sum[e + 2 * w]));
+              v[e + 2 * w + 1] = fmaf(s0, x.y + y.y, s1 * __uint_as_float(sum[e + 2 * w + 1]));
+            }
+          }
+        }
+        if (phase == kOrthoApply && ph.st.last) {
+          const float fm = (float)mt.m, fn = (float)mt.n;
+          const float rate = ph.u.lr * (ph.u.adjust == 1 ? sqrtf(fmaxf(1.0f, fm / fn))
+                                        : ph.u.adjust == 2 ? 0.2f * sqrtf(fmaxf(fm, fn)) : 1.0f);
+          const int n = (int)min((int64_t)32, cols - j0);
+          const int64_t at = mt.tall ? j0 * mt.ldw + i : i * mt.ldw + j0;
+          const int64_t step = mt.tall ? mt.ldw : 1;
+          const bool wide = !mt.tall && n == 32 && mt.wide_rows;
+          if (i >= p) {
+            // a row past the matrix
+          } else if (mt.bf16) {
+            __nv_bfloat16* w = static_cast<__nv_bfloat16*>(mt.W) + at;
+            if (wide) write_weights<__nv_bfloat16, true>(w, step, n, v, ph.u, rate);
+            else write_weights<__nv_bfloat16, false>(w, step, n, v, ph.u, rate);
+          } else {
+            float* w = static_cast<float*>(mt.W) + at;
+            if (wide) write_weights<float, true>(w, step, n, v, ph.u, rate);
+            else write_weights<float, false>(w, step, n, v, ph.u, rate);
+          }
+          __syncwarp();
+          continue;
+        }
+        // hi, then (a pair, or X in any case) lo, as 32 x 32 boxes; below the diagonal of a
+        // symmetric result the box of the transposed place too
+        const bool both = phase != kOrthoApply && tl.z + kCols <= tl.y;
+        const int parts = phase == kOrthoApply || kPairs ? 2 : 1;
+        const CUtensorMap* to = m + (phase == kOrthoGram ? kMapStoreA
+                                     : phase == kOrthoPoly ? kMapStoreB : kMapStoreX + (cur ^ 1));
+        const int to_lo = phase == kOrthoApply ? 2 : 1;
+        for (int part = 0; part < parts; ++part) {
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            w[e] = pack2(v[2 * e], v[2 * e + 1]);
+            const float2 h = unpack2(w[e]);        // what is left for the lo part
+            v[2 * e] -= h.x;
+            v[2 * e + 1] -= h.y;
+          }
+          if (lane == 0) bulk_wait_read_all();     // the boxes' last stores have read them
+          __syncwarp();
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint4*>(direct + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) =
+                make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+          if (both) {
+            // two rows' values of one column to a word: neighbouring lanes trade halves
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const uint32_t o = __shfl_xor_sync(0xffffffffu, w[e], 1);
+              const uint32_t mine = (lane & 1) ? (o >> 16) | (w[e] & 0xFFFF0000u)
+                                               : (w[e] & 0xFFFFu) | (o << 16);
+              const int row = 2 * e + (lane & 1);  // column 2 e + (lane & 1) of the tile
+              *reinterpret_cast<uint32_t*>(mirror + row * 64 + (((lane >> 3) ^ ((row >> 1) & 3)) << 4) +
+                                           (lane & 6) * 2) = mine;
+            }
+          }
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(to + part * to_lo, (int)j0, (int)i0, direct);
+            if (both) tma_store_2d(to + part * to_lo, (int)i0, (int)j0, mirror);
+            bulk_commit();
+          }
+        }
+      }
+      if constexpr (!kPairs) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_leader(&sh.acc_empty[acc]);
+      }
+    }
+    if (!ok && lane == 0) give_up(sh, status);
+    if (lane == 0) bulk_wait_all();
+  }
+
+  tc_fence_before();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, kTmemCols);
+  }
+}
+
+template <bool kPairs>
+int32_t max_pairs() {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = kSmem;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 2;
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaFuncSetAttribute(ortho_gemm_kernel<kPairs>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           (int)kSmem) != cudaSuccess)
+    return 0;
+  int clusters = 0;
+  if (cudaOccupancyMaxActiveClusters(&clusters, ortho_gemm_kernel<kPairs>, &cfg) != cudaSuccess)
+    return 0;
+  return clusters;
+}
+
+}  // namespace
+
+int32_t ortho_max_pairs() { return std::min(max_pairs<false>(), max_pairs<true>()); }
+
+cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, const int4* tiles,
+                                 int32_t n_tiles, bool pairs, int32_t n_pairs, OrthoPhase phase,
+                                 const OrthoStep& st, const OrthoUpdate& u, uint32_t* status,
+                                 cudaStream_t s) {
+  if (n_tiles <= 0) return cudaSuccess;
+  if (n_pairs <= 0) return cudaErrorInvalidValue;
+  const Phase ph{(int)phase, st, u};
+  const unsigned grid = 2u * (unsigned)std::min(n_tiles, n_pairs);
+  return pairs ? launch_dependent(ortho_gemm_kernel<true>, grid, kThreads, kSmem, s, 1, true, mats,
+                                  maps, tiles, n_tiles, ph, status)
+               : launch_dependent(ortho_gemm_kernel<false>, grid, kThreads, kSmem, s, 1, true, mats,
+                                  maps, tiles, n_tiles, ph, status);
+}
+
+}  // namespace zo
