@@ -1,6 +1,7 @@
 // Host runtime and C ABI of the orthogonalised updates (declared in include/zo.h): the
 // workspace's layout, the groups that share it, and the launches of a call.
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <cstring>
 #include <memory>
@@ -15,7 +16,6 @@ namespace {
 
 using namespace zo::host;
 
-constexpr int32_t kMaxSteps = 32;
 constexpr double kMuonA = 3.4445, kMuonB = -4.7750, kMuonC = 2.0315;
 // Matrices are worked on in groups that share the iterates' buffers, of at most this many
 // bytes (or one matrix): enough work in every launch to fill the device, without a second
@@ -30,13 +30,22 @@ struct Group {
   int32_t sym0[2] = {}, n_sym[2] = {}, apply0[2] = {}, n_apply[2] = {};
 };
 
+// Matrices of at most 128 rows that one launch takes: one cluster size, and shared memories
+// within a factor of two (they decide how many CTAs share an SM).
+struct Small {
+  int32_t cluster = 0, smem = 0, first = 0, n = 0;
+};
+
 // Where everything lies in the workspace: the status word, the tables, the norm's partial
 // sums, then the buffers that the groups share.
 struct Layout {
   std::vector<zo::OrthoMat> mats;       // buffer pointers hold byte offsets until placed
   std::vector<int4> units, tiles;
   std::vector<Group> groups;
-  int64_t mats_at = 0, maps_at = 0, units_at = 0, tiles_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
+  std::vector<int32_t> small_list;
+  int32_t n_maps = 0;                   // matrices with tensor maps
+  std::vector<Small> small;
+  int64_t mats_at = 0, maps_at = 0, small_at = 0, units_at = 0, tiles_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
   int64_t tables_end = 0;
 };
 
@@ -89,6 +98,12 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     d.tall = m.m > m.n;
     d.pairs = zo::ortho_pairs(d.bf16, d.p);
     d.wide_rows = aligned16(m.W) && m.ldw * (d.bf16 ? 2 : 4) % 16 == 0;
+    if (const int32_t cl = zo::ortho_small_cluster(d.p, d.c)) {
+      d.small = cl;
+      L.mats.push_back(d);
+      continue;
+    }
+    d.maps = L.n_maps++;
     d.ldx = round_up(d.c, 64);
     d.ldp = round_up(d.p, 64);
     const int64_t x_bytes = d.p * d.ldx * 2, a_bytes = d.p * d.ldp * 2;
@@ -132,25 +147,42 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
   for (Group& g : L.groups) {
     const size_t first = next;
     int64_t units = 0;
-    while (next < L.mats.size() && units + L.mats[next].n_units <= g.n_units)
-      units += L.mats[next++].n_units;
+    for (; next < L.mats.size() && units + L.mats[next].n_units <= g.n_units; ++next)
+      units += L.mats[next].n_units;               // (a small matrix has none)
+    const auto of = [&](size_t i, int pr) { return !L.mats[i].small && L.mats[i].pairs == pr; };
     for (int pr = 0; pr < 2; ++pr) {
       const int cols = zo::ortho_tile_cols(pr != 0);
       g.sym0[pr] = (int32_t)L.tiles.size();
       for (size_t i = first; i < next; ++i)
-        for (int64_t r = 0; L.mats[i].pairs == pr && r < L.mats[i].p; r += zo::kOrthoTileRows)
+        for (int64_t r = 0; of(i, pr) && r < L.mats[i].p; r += zo::kOrthoTileRows)
           for (int64_t c = 0; c < std::min(r + zo::kOrthoTileRows, L.mats[i].p); c += cols)
-            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
+            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, L.mats[i].maps));
       g.n_sym[pr] = (int32_t)L.tiles.size() - g.sym0[pr];
       g.apply0[pr] = (int32_t)L.tiles.size();
       for (size_t i = first; i < next; ++i)
-        for (int64_t r = 0; L.mats[i].pairs == pr && r < L.mats[i].p; r += zo::kOrthoTileRows)
+        for (int64_t r = 0; of(i, pr) && r < L.mats[i].p; r += zo::kOrthoTileRows)
           for (int64_t c = 0; c < L.mats[i].c; c += cols)
-            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, 0));
+            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, L.mats[i].maps));
       g.n_apply[pr] = (int32_t)L.tiles.size() - g.apply0[pr];
     }
     if (L.tiles.size() > (size_t(1) << 28))
       return refuse(ZO_ERR_SHAPE, "zo_muon: too many tiles in one context");
+  }
+  // small matrices by cluster size, then by shared memory
+  std::vector<std::array<int32_t, 3>> order;
+  for (size_t i = 0; i < L.mats.size(); ++i)
+    if (const int32_t cl = L.mats[i].small)
+      order.push_back({cl, zo::ortho_small_smem(L.mats[i].p, L.mats[i].c, cl), (int32_t)i});
+  std::sort(order.begin(), order.end());
+  for (const auto& o : order) {
+    if (L.small.empty() || L.small.back().cluster != o[0] ||
+        o[1] > 2 * zo::ortho_small_smem(L.mats[L.small_list[L.small.back().first]].p,
+                                        L.mats[L.small_list[L.small.back().first]].c, o[0])) {
+      L.small.push_back({o[0], o[1], (int32_t)L.small_list.size(), 0});
+    }
+    L.small.back().smem = o[1];                    // the largest so far
+    ++L.small.back().n;
+    L.small_list.push_back(o[2]);
   }
   int64_t at = 256;                                 // the status word
   const auto place = [&](int64_t bytes) {
@@ -159,7 +191,8 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     return here;
   };
   L.mats_at = place(sizeof(zo::OrthoMat) * L.mats.size());
-  L.maps_at = place((int64_t)sizeof(CUtensorMap) * zo::kOrthoMaps * L.mats.size());
+  L.maps_at = place((int64_t)sizeof(CUtensorMap) * zo::kOrthoMaps * L.n_maps);
+  L.small_at = place(sizeof(int32_t) * L.small_list.size());
   L.units_at = place(sizeof(int4) * L.units.size());
   L.tiles_at = place(sizeof(int4) * L.tiles.size());
   L.tables_end = at;
@@ -225,7 +258,7 @@ int32_t exponent_for(double bound) {
 
 // Steps with the exponents of their iterates.
 zo_status plan_steps(int32_t steps, const float* coeffs, std::vector<zo::OrthoStep>* out) {
-  if (steps < 1 || steps > kMaxSteps)
+  if (steps < 1 || steps > zo::kOrthoMaxSteps)
     return refuse(ZO_ERR_INVALID_ARG, "zo_muon: need 1 <= steps <= 32");
   double u = 1.0;
   for (int32_t k = 0; k < steps; ++k) {
@@ -275,6 +308,13 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   const auto* maps = reinterpret_cast<const CUtensorMap*>(c->ws + L.maps_at);
   auto* status = reinterpret_cast<uint32_t*>(c->ws);
   auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
+  const auto* which = reinterpret_cast<const int32_t*>(c->ws + L.small_at);
+  for (const Small& g : L.small) {
+    ZO_CUDA(zo::launch_ortho_small(mats, which + g.first, g.n, g.cluster, g.smem, st.data(),
+                                   (int32_t)st.size(), u, status, c->stream),
+            "orthogonalisation: kernel of matrices of at most 128 rows");
+    ++c->launches;
+  }
   for (const Group& g : L.groups) {
     ZO_CUDA(zo::launch_ortho_momentum(mats, units + g.unit0, g.n_units, u, partial, c->stream),
             "orthogonalisation: momentum kernel");
@@ -339,6 +379,7 @@ zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t 
     c->ws = static_cast<uint8_t*>(workspace);
     uint8_t* buffers = c->ws + L.buffers_at;
     for (zo::OrthoMat& d : L.mats) {
+      if (d.small) continue;
       const auto put = [&](uint16_t*& p) {
         p = reinterpret_cast<uint16_t*>(buffers + reinterpret_cast<int64_t>(p));
       };
@@ -353,19 +394,22 @@ zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t 
         put(d.bl);
       }
     }
-    std::vector<CUtensorMap> maps(zo::kOrthoMaps * L.mats.size());
-    for (size_t i = 0; i < L.mats.size(); ++i)
-      if (!encode_maps(L.mats[i], &maps[zo::kOrthoMaps * i]))
+    std::vector<CUtensorMap> maps((size_t)zo::kOrthoMaps * L.n_maps);
+    for (const zo::OrthoMat& d : L.mats)
+      if (!d.small && !encode_maps(d, &maps[(size_t)zo::kOrthoMaps * d.maps]))
         return refuse(ZO_ERR_CUDA, "zo_muon_create: cuTensorMapEncodeTiled rejected a descriptor");
-    c->n_pairs = zo::ortho_max_pairs();
-    if (c->n_pairs <= 0)
+    c->n_pairs = L.groups.empty() ? 0 : zo::ortho_max_pairs();
+    if (!L.groups.empty() && c->n_pairs <= 0)
       return refuse(ZO_ERR_CUDA, "zo_muon_create: no cluster of the product kernel fits");
     // one copy of the status word (0) and every table
     std::vector<uint8_t> image((size_t)L.tables_end, 0);
     std::memcpy(image.data() + L.mats_at, L.mats.data(), sizeof(zo::OrthoMat) * L.mats.size());
-    std::memcpy(image.data() + L.maps_at, maps.data(), sizeof(CUtensorMap) * maps.size());
-    std::memcpy(image.data() + L.units_at, L.units.data(), sizeof(int4) * L.units.size());
-    std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(int4) * L.tiles.size());
+    if (!maps.empty())
+      std::memcpy(image.data() + L.maps_at, maps.data(), sizeof(CUtensorMap) * maps.size());
+    if (!L.small_list.empty())
+      std::memcpy(image.data() + L.small_at, L.small_list.data(), sizeof(int32_t) * L.small_list.size());
+    if (!L.units.empty()) std::memcpy(image.data() + L.units_at, L.units.data(), sizeof(int4) * L.units.size());
+    if (!L.tiles.empty()) std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(int4) * L.tiles.size());
     ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),
             "upload tables");
     L.mats.clear();

@@ -40,6 +40,9 @@ struct OrthoMat {
   int64_t ldg, ldw, m, n, p, c;
   int32_t grad_bf16, bf16, tall;
   int32_t pairs;                    // products of hi + lo pairs (ortho_pairs)
+  int32_t small;                    // its cluster's CTAs in the one-launch kernel, which uses
+                                    // none of the fields below; 0: the others'
+  int32_t maps;                     // index of its kOrthoMaps tensor maps
   int32_t unit0, n_units;           // its slots of the norm's partial sums
   int32_t wide_rows;                // W's rows start on 16 bytes
   int64_t ldx, ldp;                 // row strides of X, and of A and B (multiples of 64)
@@ -49,7 +52,7 @@ struct OrthoMat {
 };
 // kOrthoUnitRows x kOrthoUnitCols elements of U: (matrix, first row, first column, slot)
 constexpr int kOrthoUnitRows = 64, kOrthoUnitCols = 256;
-// A tile of a product: (matrix, first row, first column, 0)
+// A tile of a product: (matrix, first row, first column, index of its tensor maps)
 constexpr int kOrthoTileRows = 256;
 __host__ __device__ constexpr int ortho_tile_cols(bool pairs) { return pairs ? 128 : 256; }
 
@@ -69,6 +72,7 @@ struct OrthoStep {
   int32_t k;                        // index of the step: X_k is in xh[k & 1]
   int32_t last;                     // the result goes to W instead of X_(k+1)
 };
+constexpr int kOrthoMaxSteps = 32;
 struct OrthoUpdate {
   float momentum;
   int32_t step;                     // 0: U = G, W <- NS(U); 1: the Muon update
@@ -93,5 +97,14 @@ cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, 
                                  int32_t n_tiles, bool pairs, int32_t n_pairs, OrthoPhase phase,
                                  const OrthoStep& st, const OrthoUpdate& u, uint32_t* status,
                                  cudaStream_t s);
+
+// Matrices of at most 128 rows, in one launch (zo_ortho_small.cu): the CTAs of a matrix's
+// cluster (0: too wide for one), and a CTA's shared memory.  A launch takes the matrices
+// mats[which[0 .. n)], all of one cluster size, and the largest of their shared memories.
+int32_t ortho_small_cluster(int64_t p, int64_t c);
+int32_t ortho_small_smem(int64_t p, int64_t c, int32_t cluster);
+cudaError_t launch_ortho_small(const OrthoMat* mats, const int* which, int32_t n, int32_t cluster,
+                               int32_t smem, const OrthoStep* steps, int32_t n_steps,
+                               const OrthoUpdate& u, uint32_t* status, cudaStream_t s);
 
 }  // namespace zo

