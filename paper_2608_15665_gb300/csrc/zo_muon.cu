@@ -30,10 +30,11 @@ struct Group {
   int32_t sym0[2] = {}, n_sym[2] = {}, apply0[2] = {}, n_apply[2] = {};
 };
 
-// Matrices of at most 128 rows that one launch takes: one cluster size, and shared memories
-// within a factor of two (they decide how many CTAs share an SM).
+// Matrices that one launch of a one-launch kernel takes: one kernel (rows: the fp32 kernel's
+// instance, 0 the tensor cores'), one cluster size, and shared memories within a factor of two
+// (they decide how many CTAs share an SM).
 struct Small {
-  int32_t cluster = 0, smem = 0, first = 0, n = 0;
+  int32_t rows = 0, cluster = 0, smem = 0, least = 0, first = 0, n = 0;
 };
 
 // Where everything lies in the workspace: the status word, the tables, the norm's partial
@@ -98,8 +99,9 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     d.tall = m.m > m.n;
     d.pairs = zo::ortho_pairs(d.bf16, d.p);
     d.wide_rows = aligned16(m.W) && m.ldw * (d.bf16 ? 2 : 4) % 16 == 0;
-    if (const int32_t cl = zo::ortho_small_cluster(d.p, d.c)) {
-      d.small = cl;
+    d.small = zo::ortho_fma_cluster(d.p, d.c);
+    if (d.small == 0) d.small = zo::ortho_small_cluster(d.p, d.c);
+    if (d.small > 0) {
       L.mats.push_back(d);
       continue;
     }
@@ -168,21 +170,23 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     if (L.tiles.size() > (size_t(1) << 28))
       return refuse(ZO_ERR_SHAPE, "zo_muon: too many tiles in one context");
   }
-  // small matrices by cluster size, then by shared memory
-  std::vector<std::array<int32_t, 3>> order;
-  for (size_t i = 0; i < L.mats.size(); ++i)
-    if (const int32_t cl = L.mats[i].small)
-      order.push_back({cl, zo::ortho_small_smem(L.mats[i].p, L.mats[i].c, cl), (int32_t)i});
+  // the one-launch kernels' matrices by instance, cluster size and shared memory
+  std::vector<std::array<int32_t, 4>> order;
+  for (size_t i = 0; i < L.mats.size(); ++i) {
+    const zo::OrthoMat& d = L.mats[i];
+    if (d.small == 0) continue;
+    const int32_t rows = zo::ortho_fma_rows(d.p);
+    order.push_back({rows, d.small, rows ? zo::ortho_fma_smem(d.p, d.c, d.small)
+                                         : zo::ortho_small_smem(d.p, d.c, d.small), (int32_t)i});
+  }
   std::sort(order.begin(), order.end());
   for (const auto& o : order) {
-    if (L.small.empty() || L.small.back().cluster != o[0] ||
-        o[1] > 2 * zo::ortho_small_smem(L.mats[L.small_list[L.small.back().first]].p,
-                                        L.mats[L.small_list[L.small.back().first]].c, o[0])) {
-      L.small.push_back({o[0], o[1], (int32_t)L.small_list.size(), 0});
-    }
-    L.small.back().smem = o[1];                    // the largest so far
+    if (L.small.empty() || L.small.back().rows != o[0] || L.small.back().cluster != o[1] ||
+        o[2] > 2 * L.small.back().least)
+      L.small.push_back({o[0], o[1], o[2], o[2], (int32_t)L.small_list.size(), 0});
+    L.small.back().smem = o[2];                    // the largest so far
     ++L.small.back().n;
-    L.small_list.push_back(o[2]);
+    L.small_list.push_back(o[3]);
   }
   int64_t at = 256;                                 // the status word
   const auto place = [&](int64_t bytes) {
@@ -310,9 +314,11 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
   const auto* which = reinterpret_cast<const int32_t*>(c->ws + L.small_at);
   for (const Small& g : L.small) {
-    ZO_CUDA(zo::launch_ortho_small(mats, which + g.first, g.n, g.cluster, g.smem, st.data(),
-                                   (int32_t)st.size(), u, status, c->stream),
-            "orthogonalisation: kernel of matrices of at most 128 rows");
+    ZO_CUDA(g.rows ? zo::launch_ortho_fma(mats, which + g.first, g.n, g.rows, g.cluster, g.smem,
+                                          st.data(), (int32_t)st.size(), u, c->stream)
+                   : zo::launch_ortho_small(mats, which + g.first, g.n, g.cluster, g.smem,
+                                            st.data(), (int32_t)st.size(), u, status, c->stream),
+            "orthogonalisation: one-launch kernel");
     ++c->launches;
   }
   for (const Group& g : L.groups) {

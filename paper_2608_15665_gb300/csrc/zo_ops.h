@@ -40,7 +40,7 @@ struct OrthoMat {
   int64_t ldg, ldw, m, n, p, c;
   int32_t grad_bf16, bf16, tall;
   int32_t pairs;                    // products of hi + lo pairs (ortho_pairs)
-  int32_t small;                    // its cluster's CTAs in the one-launch kernel, which uses
+  int32_t small;                    // its cluster's CTAs in a one-launch kernel, which uses
                                     // none of the fields below; 0: the others'
   int32_t maps;                     // index of its kOrthoMaps tensor maps
   int32_t unit0, n_units;           // its slots of the norm's partial sums
@@ -98,9 +98,17 @@ cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, 
                                  const OrthoStep& st, const OrthoUpdate& u, uint32_t* status,
                                  cudaStream_t s);
 
-// Matrices of at most 128 rows, in one launch (zo_ortho_small.cu): the CTAs of a matrix's
-// cluster (0: too wide for one), and a CTA's shared memory.  A launch takes the matrices
-// mats[which[0 .. n)], all of one cluster size, and the largest of their shared memories.
+// Matrices of at most 32 rows (zo_ortho_fma.cu: fp32, `rows` = 8, 16 or 32) and of 33 to 128
+// (zo_ortho_small.cu: tensor cores), each kind in one launch: the CTAs of a matrix's cluster
+// (0: not one of these, or too wide), and a CTA's shared memory.  A launch takes the matrices
+// mats[which[0 .. n)], all of one cluster size (and rows), and the largest of their shared
+// memories.
+int32_t ortho_fma_rows(int64_t p);
+int32_t ortho_fma_cluster(int64_t p, int64_t c);
+int32_t ortho_fma_smem(int64_t p, int64_t c, int32_t cluster);
+cudaError_t launch_ortho_fma(const OrthoMat* mats, const int* which, int32_t n, int32_t rows,
+                             int32_t cluster, int32_t smem, const OrthoStep* steps,
+                             int32_t n_steps, const OrthoUpdate& u, cudaStream_t s);
 int32_t ortho_small_cluster(int64_t p, int64_t c);
 int32_t ortho_small_smem(int64_t p, int64_t c, int32_t cluster);
 cudaError_t launch_ortho_small(const OrthoMat* mats, const int* which, int32_t n, int32_t cluster,

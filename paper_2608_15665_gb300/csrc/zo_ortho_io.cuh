@@ -1,0 +1,181 @@
+// What the one-launch orthogonalisation kernels (zo_ortho_fma.cu, zo_ortho_small.cu) share: a
+// CTA's walk over its columns of the caller's matrices, and a cluster's sum of one value.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "zo_cluster.cuh"
+#include "zo_ops.h"
+
+namespace zo {
+namespace ortho {
+
+// (kThreads: threads of the CTA)
+
+// kV consecutive values of a bf16 or fp32 buffer
+template <int kV>
+__device__ __forceinline__ void load_values(const void* p, int bf16, int64_t at, float (&v)[kV]) {
+  if constexpr (kV == 4) {
+    if (bf16) {
+      const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + at);
+      v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xFFFF0000u);
+      v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+    } else {
+      const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+      v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    }
+  } else {
+    v[0] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at])
+                : static_cast<const float*>(p)[at];
+  }
+}
+template <int kV>
+__device__ __forceinline__ void store_values(void* p, int bf16, int64_t at, const float (&v)[kV]) {
+  if constexpr (kV == 4) {
+    if (bf16) {
+      const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p) + at) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    } else {
+      *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+  } else {
+    if (bf16) static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(v[0]);
+    else static_cast<float*>(p)[at] = v[0];
+  }
+}
+
+// whether rows of a buffer with `ld` elements between them can be read four at a time
+__device__ __forceinline__ bool by_fours(const void* p, int64_t ld, int bf16, int64_t n) {
+  return n % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (bf16 ? 8 : 16) == 0;
+}
+
+// This CTA's share of a matrix: X's columns c0 .. c0 + cols - 1, i.e. rows of the caller's
+// matrix where it is tall.  Calls f(x_row, x_col, row, col) for the first element of every run
+// of kV elements that are neighbours in the caller's rows, four runs of a thread at a time
+// through `batch`, which loads before it computes.
+template <int kThreads, int kV, typename F>
+__device__ __forceinline__ void for_runs(const OrthoMat& mt, int64_t c0, int cols, F batch) {
+  const int rows = mt.tall ? cols : (int)mt.p;              // of the caller's matrix
+  const int runs = (mt.tall ? (int)mt.p : cols) / kV;       // in each (kV divides it)
+  if (rows == 0 || runs == 0) return;
+  int r = (int)threadIdx.x / runs, q = (int)threadIdx.x - r * runs;
+  const int dr = kThreads / runs, dq = kThreads - dr * runs;
+  while (r < rows) {
+    int rr[4], qq[4], n = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      rr[k] = r;
+      qq[k] = q * kV;
+      if (r < rows) {
+        n = k + 1;
+        r += dr;
+        q += dq;
+        if (q >= runs) {
+          q -= runs;
+          ++r;
+        }
+      }
+    }
+    batch(rr, qq, n);
+  }
+}
+
+// M <- momentum M + G and U, of every run: f(x_row, x_col, values) stores them.  Returns this
+// thread's sum of U^2.
+template <int kThreads, int kV, typename F>
+__device__ __forceinline__ float load_update(const OrthoMat& mt, const OrthoUpdate& u, int64_t c0,
+                                             int cols, F f) {
+  const bool moving = u.step && mt.M != nullptr;
+  const int64_t r0 = mt.tall ? c0 : 0, k0 = mt.tall ? 0 : c0;
+  float sq = 0.0f;
+  for_runs<kThreads, kV>(mt, c0, cols, [&](const int (&r)[4], const int (&q)[4], int n) {
+    float g[4][kV], m[4][kV];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < n) load_values<kV>(mt.G, mt.grad_bf16, (r0 + r[k]) * mt.ldg + k0 + q[k], g[k]);
+    if (moving) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < n) load_values<kV>(mt.M, 0, (r0 + r[k]) * mt.n + k0 + q[k], m[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k >= n) continue;
+      if (moving) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) m[k][e] = fmaf(u.momentum, m[k][e], g[k][e]);
+        store_values<kV>(mt.M, 0, (r0 + r[k]) * mt.n + k0 + q[k], m[k]);
+#pragma unroll
+        for (int e = 0; e < kV; ++e)
+          g[k][e] = u.nesterov ? fmaf(u.momentum, m[k][e], g[k][e]) : m[k][e];
+      }
+#pragma unroll
+      for (int e = 0; e < kV; ++e) sq = fmaf(g[k][e], g[k][e], sq);
+      f(mt.tall ? q[k] : r[k], mt.tall ? r[k] : q[k], g[k]);
+    }
+  });
+  return sq;
+}
+
+// W <- keep W - lr s O, or W <- O: f(x_row, x_col, values) fetches O's run.
+template <int kThreads, int kV, typename F>
+__device__ __forceinline__ void store_result(const OrthoMat& mt, const OrthoUpdate& u, int64_t c0,
+                                             int cols, F f) {
+  const int64_t r0 = mt.tall ? c0 : 0, k0 = mt.tall ? 0 : c0;
+  const float fm = (float)mt.m, fn = (float)mt.n;
+  const float rate = u.lr * (u.adjust == 1 ? sqrtf(fmaxf(1.0f, fm / fn))
+                             : u.adjust == 2 ? 0.2f * sqrtf(fmaxf(fm, fn)) : 1.0f);
+  for_runs<kThreads, kV>(mt, c0, cols, [&](const int (&r)[4], const int (&q)[4], int n) {
+    float w[4][kV];
+    if (u.step) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < n) load_values<kV>(mt.W, mt.bf16, (r0 + r[k]) * mt.ldw + k0 + q[k], w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k >= n) continue;
+      float o[kV];
+      f(mt.tall ? q[k] : r[k], mt.tall ? r[k] : q[k], o);
+      if (u.step) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) o[e] = fmaf(-rate, o[e], u.keep * w[k][e]);
+      }
+      store_values<kV>(mt.W, mt.bf16, (r0 + r[k]) * mt.ldw + k0 + q[k], o);
+    }
+  });
+}
+
+struct SumShared {
+  float warp[32];
+  float cta;
+};
+// 1 / (||U|| + eps) from the threads' sums (in warp, then rank order); every CTA of the cluster
+// gets the same.  A barrier of the CTA's threads lies between earlier and later work.
+template <int kThreads>
+__device__ __forceinline__ float inverse_norm(float sq, float eps, int cluster, SumShared& sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+  if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = sq;
+  __syncthreads();
+  sq = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) sq += sh.warp[w];
+  if (cluster > 1) {
+    if (threadIdx.x == 0) sh.cta = sq;
+    cta2::cluster_sync_all();
+    sq = 0.0f;
+    for (int r = 0; r < cluster; ++r) {
+      float v;
+      asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                   : "=f"(v) : "r"(cta2::map_to(&sh.cta, (uint32_t)r)) : "memory");
+      sq += v;
+    }
+  }
+  const float norm = sqrtf(sq) + eps;
+  return norm == 0.0f ? 0.0f : 1.0f / norm;
+}
+
+}  // namespace ortho
+}  // namespace zo

@@ -1,23 +1,25 @@
-// Newton-Schulz orthogonalisation of matrices of at most 128 rows in one launch: momentum,
-// norm, every step and the update of W, with X in shared memory throughout.
+// Newton-Schulz orthogonalisation of matrices of 33 to 128 rows in one launch: momentum, norm,
+// every step and the update of W, with X in shared memory throughout.  (At most 32 rows:
+// zo_ortho_fma.cu.)
 //
 // A matrix is a cluster of C CTAs, each with X's columns [rank cs, rank cs + cs).  A step:
 //   Gram   each CTA's X X^T on its columns, summed over the cluster through distributed
-//          shared memory (CTA r sums the rows of its share and writes them into every CTA);
+//          shared memory (CTA r sums its share of the elements and writes them into every CTA);
 //   Poly   B = b A + c A A, by every CTA for itself;
-//   Apply  the columns' X' = a X + B X, computed as X'^T = X^T B (B is symmetric), so that the
-//          128 rows of an MMA are X's columns and no Tensor Memory lane idles at p = 8 or 16.
+//   Apply  the columns' X' = a X + B X.
 // All three are M = 128 tcgen05.mma on fp16 hi + lo pairs (hi.lo, lo.hi, then hi.hi), fp32
 // accumulators.  X lies in shared memory once, as 128-byte swizzled panels of 64 columns: the
 // Gram product reads them as a K-major operand, Apply as an MN-major one.  Rows are padded
 // with zeros to a multiple of 16; where an operand has fewer than an MMA's 128 rows, the
 // rest of it is whatever follows in shared memory, and those rows of the result are not read.
-// The Gram product's K is dealt to up to four accumulators, since the tensor cores' sums
-// round towards zero (zo_ortho_gemm.cu).
+// A product's K steps are dealt to up to four accumulators in turn: consecutive MMAs into one
+// wait for each other (~85 cycles a step of 16, whatever N), and the tensor cores' sums round
+// towards zero (zo_ortho_gemm.cu).
+// Between load and scaling, and between the last step and the update of W, the two fp16 planes
+// of X hold the upper and lower halves of fp32 values, so that the caller's matrices are read
+// and written once, in their own order.
 //
-// Latency-bound: three MMA round trips and their epilogues per step (~1 us each), whatever
-// the width, and everything else once.  The same matrices by the launches of the SM-pair
-// kernel cost 17 launches, each with little work.
+// Bound by latency and the epilogues: three MMA round trips per step.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -26,6 +28,7 @@
 #include "zo_cluster.cuh"
 #include "zo_launch.cuh"
 #include "zo_ops.h"
+#include "zo_ortho_io.cuh"
 #include "zo_sm100.cuh"
 #include "zo_tc_common.cuh"
 
@@ -35,7 +38,6 @@ namespace {
 using namespace sm100;
 using tc::exp2i;
 
-constexpr int kThreads = 256;
 constexpr int kMaxCluster = 8;
 constexpr long long kWait = 4000000000LL;               // ~2 s at 2 GHz
 constexpr int kSmemMax = 227 * 1024;
@@ -45,8 +47,7 @@ struct Geometry {
   int a_panels;                   // 64-column panels of A
   int x_bytes, a_bytes;           // of a hi (or lo) part
   int red_bytes;                  // the cluster's partial Gram sums
-  int splits, chunks;             // Gram accumulators; 128-column chunks of Apply
-  int tmem_cols;
+  int tmem_cols, n_sym, n_apply;  // Tensor Memory; accumulators of Gram and Poly, of Apply
   int smem;
 };
 __host__ __device__ inline Geometry geometry(int p, int64_t c, int cluster) {
@@ -59,17 +60,20 @@ __host__ __device__ inline Geometry geometry(int p, int64_t c, int cluster) {
   g.x_bytes = g.panels * g.p16 * 128;
   g.a_bytes = g.a_panels * g.p16 * 128;
   g.red_bytes = cluster > 1 ? g.p16 * g.p16 * 4 : 0;
-  // K steps of 16 to an accumulator: at least 4
-  g.splits = g.panels >= 4 ? 4 : g.panels >= 2 ? 2 : 1;
-  g.chunks = (g.cs + 127) / 128;
-  const int cols = (g.splits > g.chunks ? g.splits : g.chunks) * g.p16;
-  g.tmem_cols = 32;
-  while (g.tmem_cols < cols) g.tmem_cols *= 2;
-  // an operand's last rows: up to 128 of them from any 8-row group on; Apply reads a second
-  // panel where there is one only
+  // an operand's last rows: up to 128 of them from any 8-row group on
   const int over = 16 * 1024;
   const int need = 2 * g.x_bytes + 2 * g.a_bytes + (g.red_bytes > over ? g.red_bytes : over) +
                    1024 /*barrier, sums*/ + 1024 /*align*/;
+  // two accumulators of each product, or all the Tensor Memory that the CTAs which fit beside
+  // each other leave
+  const int widest = g.p16 > g.cs ? g.p16 : g.cs;
+  const int fit = 228 * 1024 / (need + 1024) > 0 ? 228 * 1024 / (need + 1024) : 1;
+  g.tmem_cols = 32;
+  while (g.tmem_cols < widest || (g.tmem_cols < 512 && (g.tmem_cols < 2 * widest ||
+                                                        2 * g.tmem_cols * fit <= 512)))
+    g.tmem_cols *= 2;
+  g.n_sym = g.tmem_cols / g.p16 < 4 ? g.tmem_cols / g.p16 : 4;
+  g.n_apply = g.tmem_cols / g.cs < 4 ? g.tmem_cols / g.cs : 4;
   // A CTA must never wait for another's Tensor Memory: clusters of two launches could then
   // wait for one another.  So each takes at least its columns' share of the SM's 228 KB (1 KB
   // of them the system's), and CTAs that fit together have their columns too.
@@ -81,8 +85,7 @@ __host__ __device__ inline Geometry geometry(int p, int64_t c, int cluster) {
 struct Shared {
   uint64_t done;
   uint32_t tmem_base;
-  float warp_sum[kThreads / 32];
-  float cta_sum;
+  ortho::SumShared sums;
 };
 
 // byte offset of element (row, col) in panels of `rows` rows, 128-byte swizzle
@@ -99,7 +102,7 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t leading) {
   d |= static_cast<uint64_t>(2u) << 61;
   return d;
 }
-constexpr uint32_t kMnMajorA = 1u << 15;
+constexpr uint32_t kMnMajorB = 1u << 16;
 
 __device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t (&v)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -107,18 +110,46 @@ __device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t (&v)[8]) {
                  "=r"(v[6]), "=r"(v[7])
                : "r"(taddr));
 }
-__device__ __forceinline__ float f16(const uint8_t* p) {
-  return __half2float(*reinterpret_cast<const __half*>(p));
+// eight columns of up to four accumulators `stride` columns apart, added up
+__device__ __forceinline__ void tmem_sum_x8(uint32_t taddr, int n, uint32_t stride, float (&v)[8]) {
+  uint32_t r[4][8];
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+    if (a < n) tmem_ld_x8(taddr + a * stride, r[a]);
+  tmem_ld_wait();
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[0][e]);
+#pragma unroll
+  for (int a = 1; a < 4; ++a)
+    if (a < n) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(r[a][e]);
+    }
 }
-__device__ __forceinline__ void split(float x, uint16_t& hi, uint16_t& lo) {
-  const __half h = __float2half_rn(x);
-  const __half l = __float2half_rn(x - __half2float(h));
-  hi = __half_as_ushort(h);
-  lo = __half_as_ushort(l);
+// hi + lo of eight neighbouring fp16 pairs
+__device__ __forceinline__ void pairs8(const uint8_t* hi, const uint8_t* lo, float (&v)[8]) {
+  const uint4 h = *reinterpret_cast<const uint4*>(hi), l = *reinterpret_cast<const uint4*>(lo);
+  const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&hw[k]));
+    const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&lw[k]));
+    v[2 * k] = x.x + y.x;
+    v[2 * k + 1] = x.y + y.y;
+  }
 }
-__device__ __forceinline__ float element(const void* p, int bf16, int64_t at) {
-  return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at])
-              : static_cast<const float*>(p)[at];
+// the upper and lower halves of fp32 values, in the two planes
+__device__ __forceinline__ uint32_t upper2(float a, float b) {
+  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+}
+__device__ __forceinline__ uint32_t lower2(float a, float b) {
+  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
+}
+__device__ __forceinline__ float first_of(uint32_t up, uint32_t low) {
+  return __uint_as_float(__byte_perm(low, up, 0x5410));
+}
+__device__ __forceinline__ float second_of(uint32_t up, uint32_t low) {
+  return __uint_as_float(__byte_perm(low, up, 0x7632));
 }
 
 struct Steps {
@@ -126,7 +157,8 @@ struct Steps {
   int n;
 };
 
-__global__ void __launch_bounds__(kThreads)
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, 512 / kThreads)
 ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ which, int cluster,
                    const __grid_constant__ Steps steps, const OrthoUpdate u,
                    uint32_t* __restrict__ status) {
@@ -136,17 +168,16 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   const OrthoMat mt = mats[which[blockIdx.x / cluster]];
   const int rank = (int)(blockIdx.x % cluster);
-  const int p = (int)mt.p;
-  const Geometry geo = geometry(p, mt.c, cluster);
-  const int p16 = geo.p16;
+  const Geometry geo = geometry((int)mt.p, mt.c, cluster);
+  const int p16 = geo.p16, cs = geo.cs;
   uint8_t* xh = smem + 1024;
   uint8_t* xl = xh + geo.x_bytes;
   uint8_t* ah = xl + geo.x_bytes;
   uint8_t* al = ah + geo.a_bytes;
   float* red = reinterpret_cast<float*>(al + geo.a_bytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int64_t c0 = (int64_t)rank * geo.cs;
-  const int cols = (int)max((int64_t)0, min((int64_t)geo.cs, mt.c - c0));   // of this CTA
+  const int64_t c0 = (int64_t)rank * cs;
+  const int cols = (int)max((int64_t)0, min((int64_t)cs, mt.c - c0));   // of this CTA
 
   if (tid == 0) {
     mbar_init(&sh.done, 1);
@@ -156,6 +187,9 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     tmem_alloc(&sh.tmem_base, (uint32_t)geo.tmem_cols);
     tmem_relinquish();
   }
+  // both parts of X: the padding rows and columns stay zero
+  for (int b = tid * 16; b < 2 * geo.x_bytes; b += kThreads * 16)
+    *reinterpret_cast<uint4*>(xh + b) = make_uint4(0, 0, 0, 0);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -163,70 +197,52 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
   pdl_wait();
   pdl_trigger();
 
-  // ---------------------------------------------------------------- U and its norm
-  // element e of this CTA's share: (row i, column j) with the caller's rows contiguous
-  const int n_el = p * cols;
-  const auto place = [&](int e, int& i, int& j) {
-    if (mt.tall) { j = e / p; i = e - j * p; }
-    else { i = e / cols; j = e - i * cols; }
-  };
-  const auto update_of = [&](int i, int j, bool write) {
-    const int64_t r = mt.tall ? c0 + j : i, c = mt.tall ? i : c0 + j;
-    const float g = element(mt.G, mt.grad_bf16, r * mt.ldg + c);
-    if (!u.step || mt.M == nullptr) return g;
-    float* m = mt.M + r * mt.n + c;
-    float mom = *m;
-    if (write) {
-      mom = fmaf(u.momentum, mom, g);
-      *m = mom;
-    }
-    return u.nesterov ? fmaf(u.momentum, mom, g) : mom;
-  };
-  float sq = 0.0f;
-#pragma unroll 4
-  for (int e = tid; e < n_el; e += kThreads) {
-    int i, j;
-    place(e, i, j);
-    const float v = update_of(i, j, true);
-    sq = fmaf(v, v, sq);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-  if (lane == 0) sh.warp_sum[warp] = sq;
-  // zero both parts of X: the padding rows and columns stay so
-  for (int b = tid * 16; b < 2 * geo.x_bytes; b += kThreads * 16)
-    *reinterpret_cast<uint4*>(xh + b) = make_uint4(0, 0, 0, 0);
-  __syncthreads();
-  sq = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) sq += sh.warp_sum[w];
-  double total = (double)sq;
-  if (cluster > 1) {
-    if (tid == 0) sh.cta_sum = sq;
-    cta2::cluster_sync_all();
-    total = 0.0;
-    for (int r = 0; r < cluster; ++r) {
-      float v;
-      asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                   : "=f"(v) : "r"(cta2::map_to(&sh.cta_sum, (uint32_t)r)) : "memory");
-      total += (double)v;
-    }
-  }
-  const float norm = (float)sqrt(total) + u.eps;
-  const float inv = norm == 0.0f ? 0.0f : exp2i(steps.s[0].ex) / norm;
-#pragma unroll 4
-  for (int e = tid; e < n_el; e += kThreads) {
-    int i, j;
-    place(e, i, j);
-    uint16_t hi, lo;
-    split(update_of(i, j, false) * inv, hi, lo);
+  // ---------------------------------------------------------------- U, scaled by its norm
+  const auto put = [&](int i, int j, float v) {
     const int at = swizzled(p16, i, j);
-    *reinterpret_cast<uint16_t*>(xh + at) = hi;
-    *reinterpret_cast<uint16_t*>(xl + at) = lo;
+    *reinterpret_cast<uint16_t*>(xh + at) = (uint16_t)(__float_as_uint(v) >> 16);
+    *reinterpret_cast<uint16_t*>(xl + at) = (uint16_t)__float_as_uint(v);
+  };
+  const auto get = [&](int i, int j) {
+    const int at = swizzled(p16, i, j);
+    return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(xh + at) << 16 |
+                           *reinterpret_cast<const uint16_t*>(xl + at));
+  };
+  const int64_t n = mt.tall ? mt.p : cols;
+  float sq;
+  if (ortho::by_fours(mt.G, mt.ldg, mt.grad_bf16, n) &&
+      (mt.M == nullptr || !u.step || ortho::by_fours(mt.M, mt.n, 0, n))) {
+    sq = ortho::load_update<kThreads, 4>(mt, u, c0, cols, [&](int i, int j, const float (&v)[4]) {
+      if (mt.tall) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put(i + e, j, v[e]);
+      } else {
+        const int at = swizzled(p16, i, j);
+        *reinterpret_cast<uint2*>(xh + at) = make_uint2(upper2(v[0], v[1]), upper2(v[2], v[3]));
+        *reinterpret_cast<uint2*>(xl + at) = make_uint2(lower2(v[0], v[1]), lower2(v[2], v[3]));
+      }
+    });
+  } else {
+    sq = ortho::load_update<kThreads, 1>(mt, u, c0, cols,
+                                         [&](int i, int j, const float (&v)[1]) { put(i, j, v[0]); });
+  }
+  const float inv = ortho::inverse_norm<kThreads>(sq, u.eps, cluster, sh.sums);
+  const float s_in = exp2i(steps.s[0].ex);
+  for (int b = tid * 16; b < geo.x_bytes; b += kThreads * 16) {
+    uint4* ph = reinterpret_cast<uint4*>(xh + b);
+    uint4* pl = reinterpret_cast<uint4*>(xl + b);
+    const uint4 h = *ph, l = *pl;
+    const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = first_of(hw[k], lw[k]) * inv;
+      v[2 * k + 1] = second_of(hw[k], lw[k]) * inv;
+    }
+    tc::split8_f16(v, s_in, *ph, *pl);
   }
 
   // ---------------------------------------------------------------- the steps
-  const uint32_t idesc = idesc_f16_f32(128, p16);
   uint32_t parity = 0;
   const auto before_mma = [&]() {              // every thread's shared-memory writes are done
     fence_async_smem();
@@ -240,89 +256,87 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     __syncwarp();
     tc_fence_after();
   };
-  const int g4 = warp & 3, half = warp >> 2;   // TMEM lane group; half of the columns
+  constexpr int kGroups = kThreads / 128;      // warps that share a TMEM lane group
+  const int g4 = warp & 3, group = warp >> 2;
   const uint32_t lanes = (uint32_t)(32 * g4) << 16;
   const int row = 32 * g4 + lane;
+  const bool active = 32 * g4 < p16;           // (a whole warp)
   const uint32_t xh_s = smem_u32(xh), xl_s = smem_u32(xl), ah_s = smem_u32(ah), al_s = smem_u32(al);
+  const uint32_t panel = (uint32_t)(p16 * 128);
+  // D += sum over K steps of A B^T: K step s of 16 lies at step(s) of either operand's bytes
+  const auto product = [&](int n_k, int n_acc, uint32_t stride, uint32_t idesc, uint32_t hi_a,
+                           uint32_t lo_a, uint32_t hi_b, uint32_t lo_b, auto step_a, auto step_b,
+                           uint32_t lead_b, uint32_t col) {
+    for (int prod = 0; prod < 3; ++prod) {
+      const uint32_t a = prod == 1 ? lo_a : hi_a, b = prod == 0 ? lo_b : hi_b;
+      int acc = 0;
+      for (int s = 0; s < n_k; ++s) {
+        mma_f16(tmem + col + (uint32_t)acc * stride, sdesc(a + step_a(s), 16),
+                sdesc(b + step_b(s), lead_b), idesc, prod > 0 || s >= n_acc ? 1u : 0u);
+        if (++acc == n_acc) acc = 0;
+      }
+    }
+  };
+  const auto k_major = [&](int s) { return (uint32_t)(s >> 2) * panel + 32u * (uint32_t)(s & 3); };
+  const auto mn_major = [&](int s) { return 2048u * (uint32_t)s; };
+  const uint32_t idesc_sym = idesc_f16_f32(128, p16);
 
   for (int k = 0; k < steps.n; ++k) {
     const OrthoStep st = steps.s[k];
     // ---- A = X X^T over this CTA's columns
     before_mma();
     if (tid == 0) {
-      const int per = (geo.panels + geo.splits - 1) / geo.splits;
-      for (int s = 0; s < geo.splits; ++s)
-        for (int prod = 0; prod < 3; ++prod) {
-          const uint32_t a = prod == 1 ? xl_s : xh_s, b = prod == 0 ? xl_s : xh_s;
-          for (int q = s * per; q < min(geo.panels, (s + 1) * per); ++q)
-            for (int kk = 0; kk < 4; ++kk) {
-              const uint32_t off = (uint32_t)(q * p16 * 128 + 32 * kk);
-              mma_f16(tmem + (uint32_t)(s * p16), sdesc(a + off, 16), sdesc(b + off, 16), idesc,
-                      (prod > 0 || q > s * per || kk > 0) ? 1u : 0u);
-            }
-        }
+      product(4 * geo.panels, geo.n_sym, (uint32_t)p16, idesc_sym, xh_s, xl_s, xh_s, xl_s, k_major,
+              k_major, 16, 0);
       mma_commit(&sh.done);
     }
     wait_mma();
     const float sa = exp2i(st.ea - 2 * st.ex);
-    if (32 * g4 < p16) {
-      for (int j = half * (p16 / 2); j < (half + 1) * (p16 / 2); j += 8) {
-        uint32_t r[8];
+    if (active) {
+      const int n_acc = min(geo.n_sym, 4 * geo.panels);
+      for (int j = 8 * group; j < p16; j += 8 * kGroups) {
         float v[8];
-        tmem_ld_x8(tmem + lanes + (uint32_t)j, r);
-        tmem_ld_wait();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[e]);
-        const int per = (geo.panels + geo.splits - 1) / geo.splits;
-        for (int s = 1; s < geo.splits && s * per < geo.panels; ++s) {
-          tmem_ld_x8(tmem + lanes + (uint32_t)(s * p16 + j), r);
-          tmem_ld_wait();
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(r[e]);
-        }
+        tmem_sum_x8(tmem + lanes + (uint32_t)j, n_acc, (uint32_t)p16, v);
         if (row < p16) {
           if (cluster > 1) {
             float* to = red + row * p16 + j;
             *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<float4*>(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
           } else {
-            uint4 hi, lo;
-            tc::split8_f16(v, sa, hi, lo);
             const int at = swizzled(p16, row, j);
-            *reinterpret_cast<uint4*>(ah + at) = hi;
-            *reinterpret_cast<uint4*>(al + at) = lo;
+            tc::split8_f16(v, sa, *reinterpret_cast<uint4*>(ah + at), *reinterpret_cast<uint4*>(al + at));
           }
         }
         __syncwarp();
       }
     }
     if (cluster > 1) {
-      // CTA r sums the 8-column pieces r, r + C, ... in rank order and writes them to all
+      // CTA r sums the 4-column pieces r, r + C, ... in rank order and writes them to all
       cta2::cluster_sync_all();
-      const int pieces = p16 * p16 / 8;
+      const int pieces = p16 * p16 / 4;
       for (int q = rank + cluster * tid; q < pieces; q += cluster * kThreads) {
-        const int i = q / (p16 / 8), j = q % (p16 / 8) * 8;
-        float v[8] = {};
-        for (int r = 0; r < cluster; ++r) {
-          const uint32_t from = cta2::map_to(red + i * p16 + j, (uint32_t)r);
+        const int i = q / (p16 / 4), j = q % (p16 / 4) * 4;
+        float4 f[kMaxCluster];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float4 f;
+        for (int r = 0; r < kMaxCluster; ++r)
+          if (r < cluster)
             asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                         : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(from + 16 * h) : "memory");
-            v[4 * h] += f.x; v[4 * h + 1] += f.y; v[4 * h + 2] += f.z; v[4 * h + 3] += f.w;
+                         : "=f"(f[r].x), "=f"(f[r].y), "=f"(f[r].z), "=f"(f[r].w)
+                         : "r"(cta2::map_to(red + i * p16 + j, (uint32_t)r)) : "memory");
+        float4 v = f[0];
+#pragma unroll
+        for (int r = 1; r < kMaxCluster; ++r)
+          if (r < cluster) {
+            v.x += f[r].x; v.y += f[r].y; v.z += f[r].z; v.w += f[r].w;
           }
-        }
-        uint4 hi, lo;
-        tc::split8_f16(v, sa, hi, lo);
+        uint2 hi, lo;
+        tc::split4_f16(v, sa, hi, lo);
         const int at = swizzled(p16, i, j);
         for (int r = 0; r < cluster; ++r) {
-          asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                           cta2::map_to(ah + at, (uint32_t)r)),
-                       "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w) : "memory");
-          asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                           cta2::map_to(al + at, (uint32_t)r)),
-                       "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w) : "memory");
+          asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(
+                           cta2::map_to(ah + at, (uint32_t)r)), "r"(hi.x), "r"(hi.y) : "memory");
+          asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(
+                           cta2::map_to(al + at, (uint32_t)r)), "r"(lo.x), "r"(lo.y) : "memory");
         }
       }
       asm volatile("fence.proxy.async;" ::: "memory");
@@ -331,95 +345,60 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     // ---- B = b A + c A A, in A's place
     before_mma();
     if (tid == 0) {
-      for (int prod = 0; prod < 3; ++prod) {
-        const uint32_t a = prod == 1 ? al_s : ah_s, b = prod == 0 ? al_s : ah_s;
-        for (int kk = 0; kk < p16 / 16; ++kk) {
-          const uint32_t off = (uint32_t)((kk / 4) * p16 * 128 + 32 * (kk % 4));
-          mma_f16(tmem, sdesc(a + off, 16), sdesc(b + off, 16), idesc, (prod > 0 || kk > 0) ? 1u : 0u);
-        }
-      }
+      product(p16 / 16, geo.n_sym, (uint32_t)p16, idesc_sym, ah_s, al_s, ah_s, al_s, k_major,
+              k_major, 16, 0);
       mma_commit(&sh.done);
     }
     wait_mma();
-    if (32 * g4 < p16) {
+    if (active) {
       const float s0 = st.b * exp2i(st.eb - st.ea), s1 = st.c * exp2i(st.eb - 2 * st.ea);
-      for (int j = half * (p16 / 2); j < (half + 1) * (p16 / 2); j += 8) {
-        uint32_t r[8];
-        tmem_ld_x8(tmem + lanes + (uint32_t)j, r);
-        tmem_ld_wait();
+      const int n_acc = min(geo.n_sym, p16 / 16);
+      for (int j = 8 * group; j < p16; j += 8 * kGroups) {
+        float v[8];
+        tmem_sum_x8(tmem + lanes + (uint32_t)j, n_acc, (uint32_t)p16, v);
         if (row < p16) {
           const int at = swizzled(p16, row, j);
-          float v[8];
+          float x[8];
+          pairs8(ah + at, al + at, x);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            v[e] = fmaf(s0, f16(ah + at + 2 * e) + f16(al + at + 2 * e), s1 * __uint_as_float(r[e]));
-          uint4 hi, lo;
-          tc::split8_f16(v, 1.0f, hi, lo);
-          *reinterpret_cast<uint4*>(ah + at) = hi;
-          *reinterpret_cast<uint4*>(al + at) = lo;
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(s0, x[e], s1 * v[e]);
+          tc::split8_f16(v, 1.0f, *reinterpret_cast<uint4*>(ah + at), *reinterpret_cast<uint4*>(al + at));
         }
         __syncwarp();
       }
     }
-    // ---- X'^T = a X^T + X^T B, 128 columns of X at a time
+    // ---- X' = a X + B X, at most 256 columns an MMA
     before_mma();
     if (tid == 0) {
-      const uint32_t panel = (uint32_t)(p16 * 128);
-      for (int q = 0; q < geo.chunks; ++q)
-        for (int prod = 0; prod < 3; ++prod) {
-          const uint32_t a = (prod == 1 ? xl_s : xh_s) + 2 * q * panel;
-          const uint32_t b = prod == 0 ? al_s : ah_s;
-          for (int kk = 0; kk < p16 / 16; ++kk) {
-            const uint32_t off = (uint32_t)((kk / 4) * p16 * 128 + 32 * (kk % 4));
-            mma_f16(tmem + (uint32_t)(q * p16), sdesc(a + 2048 * kk, panel), sdesc(b + off, 16),
-                    idesc | kMnMajorA, (prod > 0 || kk > 0) ? 1u : 0u);
-          }
-        }
+      for (int q = 0; q < geo.panels; q += 4) {
+        const int width = 64 * min(4, geo.panels - q);
+        product(p16 / 16, geo.n_apply, (uint32_t)cs, idesc_f16_f32(128, width) | kMnMajorB, ah_s,
+                al_s, xh_s + q * panel, xl_s + q * panel, k_major, mn_major, panel,
+                (uint32_t)(64 * q));
+      }
       mma_commit(&sh.done);
     }
     wait_mma();
-    const float s0 = st.a * exp2i(st.last ? -st.ex : st.ex_next - st.ex);
-    const float s1 = exp2i((st.last ? 0 : st.ex_next) - st.ex - st.eb);
-    const float fm = (float)mt.m, fn = (float)mt.n;
-    const float rate = u.lr * (u.adjust == 1 ? sqrtf(fmaxf(1.0f, fm / fn))
-                               : u.adjust == 2 ? 0.2f * sqrtf(fmaxf(fm, fn)) : 1.0f);
-    for (int q = 0; q < geo.chunks; ++q) {
-      const int j = 128 * q + row;             // this thread's column of X
-      for (int i0 = half * (p16 / 2); i0 < (half + 1) * (p16 / 2); i0 += 8) {
-        uint32_t r[8];
-        tmem_ld_x8(tmem + lanes + (uint32_t)(q * p16 + i0), r);
-        tmem_ld_wait();
-        if (j < cols) {
-          float v[8], old[8];
-          int64_t w[8];
+    if (active) {
+      const float s0 = st.a * exp2i(st.last ? -st.ex : st.ex_next - st.ex);
+      const float s1 = exp2i((st.last ? 0 : st.ex_next) - st.ex - st.eb);
+      const int n_acc = min(geo.n_apply, p16 / 16);
+      for (int j = 8 * group; j < cs; j += 8 * kGroups) {
+        float v[8];
+        tmem_sum_x8(tmem + lanes + (uint32_t)j, n_acc, (uint32_t)cs, v);
+        if (row < p16) {
+          const int at = swizzled(p16, row, j);
+          uint4* ph = reinterpret_cast<uint4*>(xh + at);
+          uint4* pl = reinterpret_cast<uint4*>(xl + at);
+          float x[8];
+          pairs8(xh + at, xl + at, x);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int at = swizzled(p16, i0 + e, j);
-            v[e] = fmaf(s0, f16(xh + at) + f16(xl + at), s1 * __uint_as_float(r[e]));
-          }
-          if (!st.last) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int at = swizzled(p16, i0 + e, j);
-              uint16_t hi, lo;
-              split(v[e], hi, lo);
-              *reinterpret_cast<uint16_t*>(xh + at) = hi;
-              *reinterpret_cast<uint16_t*>(xl + at) = lo;
-            }
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(s0, x[e], s1 * v[e]);
+          if (st.last) {
+            *ph = make_uint4(upper2(v[0], v[1]), upper2(v[2], v[3]), upper2(v[4], v[5]), upper2(v[6], v[7]));
+            *pl = make_uint4(lower2(v[0], v[1]), lower2(v[2], v[3]), lower2(v[4], v[5]), lower2(v[6], v[7]));
           } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int64_t i = i0 + e;
-              w[e] = mt.tall ? (c0 + j) * mt.ldw + i : i * mt.ldw + c0 + j;
-              old[e] = u.step && i < p ? element(mt.W, mt.bf16, w[e]) : 0.0f;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (i0 + e >= p) continue;
-              const float o = u.step ? fmaf(-rate, v[e], u.keep * old[e]) : v[e];
-              if (mt.bf16) static_cast<__nv_bfloat16*>(mt.W)[w[e]] = __float2bfloat16_rn(o);
-              else static_cast<float*>(mt.W)[w[e]] = o;
-            }
+            tc::split8_f16(v, 1.0f, *ph, *pl);
           }
         }
         __syncwarp();
@@ -427,24 +406,55 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     }
   }
 
+  // ---------------------------------------------------------------- the result
   tc_fence_before();
   __syncthreads();
   if (warp == 0) {
     tc_fence_after();
     tmem_dealloc(tmem, (uint32_t)geo.tmem_cols);
   }
+  if (ortho::by_fours(mt.W, mt.ldw, mt.bf16, n)) {
+    ortho::store_result<kThreads, 4>(mt, u, c0, cols, [&](int i, int j, float (&v)[4]) {
+      if (mt.tall) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = get(i + e, j);
+      } else {
+        const int at = swizzled(p16, i, j);
+        const uint2 h = *reinterpret_cast<const uint2*>(xh + at);
+        const uint2 l = *reinterpret_cast<const uint2*>(xl + at);
+        v[0] = first_of(h.x, l.x);
+        v[1] = second_of(h.x, l.x);
+        v[2] = first_of(h.y, l.y);
+        v[3] = second_of(h.y, l.y);
+      }
+    });
+  } else {
+    ortho::store_result<kThreads, 1>(mt, u, c0, cols,
+                                     [&](int i, int j, float (&v)[1]) { v[0] = get(i, j); });
+  }
+}
+
+template <int kThreads>
+cudaError_t launch(const OrthoMat* mats, const int* which, int32_t n, int32_t cluster, int32_t smem,
+                   const Steps& st, const OrthoUpdate& u, uint32_t* status, cudaStream_t s) {
+  const cudaError_t e = cudaFuncSetAttribute(ortho_small_kernel<kThreads>,
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(ortho_small_kernel<kThreads>, (unsigned)n * (unsigned)cluster, kThreads,
+                          (size_t)smem, s, (unsigned)cluster, true, mats, which, cluster, st, u,
+                          status);
 }
 
 }  // namespace
 
 int32_t ortho_small_cluster(int64_t p, int64_t c) {
-  if (p > 128) return 0;
+  if (p <= 32 || p > 128) return 0;
   for (int cl = 1; cl <= kMaxCluster; cl *= 2) {
     // a CTA's columns: at most 256 where the cluster can still grow
     if (cl < kMaxCluster && c > 256 * (int64_t)cl) continue;
-    if (c > (int64_t)cl * 8192) return 0;
+    if (c > 512 * (int64_t)cl) return 0;                 // a column of Tensor Memory each
     const Geometry g = geometry((int)p, c, cl);
-    if (g.smem <= kSmemMax && g.tmem_cols <= 512) return cl;
+    if (g.smem <= kSmemMax) return cl;
   }
   return 0;
 }
@@ -457,15 +467,12 @@ cudaError_t launch_ortho_small(const OrthoMat* mats, const int* which, int32_t n
                                const OrthoUpdate& u, uint32_t* status, cudaStream_t s) {
   if (n <= 0) return cudaSuccess;
   if (n_steps > kOrthoMaxSteps || smem > kSmemMax) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(ortho_small_kernel,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
-  if (e != cudaSuccess) return e;
   Steps st{};
   st.n = n_steps;
   std::copy(steps, steps + n_steps, st.s);
-  return launch_dependent(ortho_small_kernel, (unsigned)n * (unsigned)cluster, kThreads,
-                          (size_t)smem, s, (unsigned)cluster, true, mats, which, cluster, st, u,
-                          status);
+  // sixteen warps for the epilogues where a CTA has its SM to itself
+  return smem > 114 * 1024 ? launch<512>(mats, which, n, cluster, smem, st, u, status, s)
+                           : launch<256>(mats, which, n, cluster, smem, st, u, status, s);
 }
 
 }  // namespace zo
