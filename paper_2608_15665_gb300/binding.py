@@ -327,30 +327,36 @@ def zo_normal_fill(seed, x1, x2, x3, out, stream=None):
                               out.numel(), _stream_handle(stream)), "zo_normal_fill")
 
 
-def _dtype_code(t, where, name):
+def _code_of(dtype, where, name):
     import torch
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return ZO_BF16
-    if t.dtype == torch.float32:
+    if dtype == torch.float32:
         return ZO_F32
-    raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {t.dtype}: bf16 or fp32")
+    raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {dtype}: bf16 or fp32")
+
+
+def _dtype_code(t, where, name):
+    return _code_of(t.dtype, where, name)
 
 
 def _rows(t, where, name, shape, dtype, device):
     """(pointer, row stride) of a rows x cols matrix with unit column stride (None -> NULL)."""
     if t is None:
         return None, 0
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ZoError(ZO_ERR_SHAPE, where, f"{name} has shape {tuple(t.shape)}, "
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
+        raise ZoError(ZO_ERR_SHAPE, where, f"{name} has shape {tuple(size)}, "
                                            f"expected {'2-D' if shape is None else tuple(shape)}")
-    rows, cols = t.shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+    rows, cols = size
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         raise ZoError(ZO_ERR_SHAPE, where, f"{name} needs unit column stride and separate rows")
     if dtype is not None and t.dtype != dtype:
         raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {t.dtype}, expected {dtype}")
     if device is not None and t.device != device:
         raise ZoError(ZO_ERR_INVALID_ARG, where, f"{name} is on {t.device}, expected {device}")
-    return t.data_ptr(), max(t.stride(0), cols) if rows > 1 else cols
+    return t.data_ptr(), ld if rows > 1 else cols
 
 
 def _on_device(t, where):
@@ -362,7 +368,8 @@ def _vector(t, where, name, n, dtype, device):
     """Pointer of a contiguous vector of n values (None -> NULL)."""
     if t is None:
         return None
-    if tuple(t.shape) != (n,) or not t.is_contiguous():
+    size = t.shape
+    if len(size) != 1 or size[0] != n or not t.is_contiguous():
         raise ZoError(ZO_ERR_SHAPE, where, f"{name} must be a contiguous vector of {n} values")
     if t.dtype != dtype:
         raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {t.dtype}, expected {dtype}")

@@ -13,22 +13,25 @@
 // large against the spread.  Sums, statistics and gradients are held in fp32 and every
 // output is rounded once.
 //
-// A row belongs to a group of threads: a warp up to kWarpCols columns, else a whole CTA.
+// A row belongs to a group of threads: a warp where its lanes hold it, else a whole CTA.
 // Thread t of a group takes the chunks t, t + group, ... of VEC consecutive columns: 16
 // bytes of the activations' type where every pointer, stride and the width allow it, else
-// single elements.
-// Rows wider than a CTA's registers are swept from memory (kE = 0).
+// single elements.  Rows wider than a CTA's registers are swept from memory (kE = 0).
 //
-// The backward pass's column sums: its CTAs take the rows blockIdx, blockIdx + gridDim, ...
-// and keep dw and db of their own columns in registers over all of them, so that each CTA
+// Forward: 32 columns a thread and short CTAs, many rows in flight on an SM.
+//
+// Backward: the CTAs take the rows blockIdx, blockIdx + gridDim, ... and keep dw and db of
+// their own columns in registers over all of them (16 columns a thread), so that each CTA
 // writes one row of partial sums, which a second kernel adds up in a fixed order: no
-// atomics, the same bits on every run.
+// atomics, the same bits on every run.  As few CTAs are resident, what keeps HBM busy is a
+// ring of rows per group in shared memory, filled by bulk copies a few rows ahead.
 #include <algorithm>
 
 #include <cuda_bf16.h>
 
 #include "zo_launch.cuh"
 #include "zo_ops.h"
+#include "zo_sm100.cuh"
 
 namespace zo {
 namespace {
@@ -116,6 +119,9 @@ __device__ __forceinline__ float group_sum(float v, float* buf) {
 
 // threads of a CTA whose rows take `group` threads each
 __host__ __device__ constexpr int block_of(int group) { return group == 32 ? 128 : group; }
+
+constexpr int kForwardElems = 32;             // columns per thread and row, in registers
+constexpr int kBackwardElems = 16;
 
 // ---------------------------------------------------------------------------- forward
 template <typename T, typename TW, int kGroup, int kE, int V>
@@ -225,18 +231,45 @@ forward_kernel(const LayerNormArgs a) {
 }
 
 // --------------------------------------------------------------------------- backward
+// an untiled bulk copy of `bytes` (16-byte aligned, a multiple of 16) into shared memory
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+          sm100::smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(sm100::smem_u32(bar))
+      : "memory");
+}
+
 // Rows held in registers: each thread keeps its columns' weight, dw and db over all rows
-// of its group.
-template <typename T, typename TW, int kGroup, int kE, int V>
-__global__ void __launch_bounds__(block_of(kGroup))
-backward_kernel(const LayerNormArgs a) {
+// of its group.  kRing: the rows come through a ring of `stages` rows in shared memory
+// (16-byte chunks only), else straight from memory.
+constexpr int kMaxStages = 8;
+constexpr long long kWait = 4000000000LL;       // ~2 s at 2 GHz
+
+// CTAs of the backward kernel on an SM: as many as leave a thread the ~100 registers of its
+// columns
+__host__ __device__ constexpr int resident_of(int block) { return block <= 128 ? 4 : block <= 320 ? 2 : 1; }
+
+template <typename T, typename TW, int kGroup, int kE, int V, bool kRing>
+__global__ void __launch_bounds__(block_of(kGroup), resident_of(block_of(kGroup)))
+backward_kernel(const LayerNormArgs a, int stages, int row_bytes) {
   constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup;
   static_assert(kE > 0, "rows in registers");
   __shared__ float buf[2][2][32];
-  extern __shared__ float joined[];             // kGroups > 1: dw and db of each warp
+  __shared__ uint64_t full[kGroups][kMaxStages];
+  extern __shared__ __align__(128) uint8_t dyn[];   // the ring; then dw and db of each warp
   const int t = threadIdx.x % kGroup, grp = threadIdx.x / kGroup;
   const int64_t cols = a.cols;
   const float inv_n = 1.0f / (float)cols;
+  const int n_buf = a.r ? 3 : 2;
+  uint8_t* ring = dyn + (size_t)grp * stages * n_buf * row_bytes;
+  if constexpr (kRing) {
+    if (t == 0) {
+      for (int s = 0; s < stages; ++s) sm100::mbar_init(&full[grp][s], 1);
+      sm100::fence_mbar_init();
+    }
+    __syncthreads();
+  }
   pdl_wait();
   pdl_trigger();
   const TW* w = static_cast<const TW*>(a.weight);
@@ -249,13 +282,45 @@ backward_kernel(const LayerNormArgs a) {
     if (w && j < cols) load<TW, V>(w + j, wv[e]);
   }
   const int64_t stride = (int64_t)gridDim.x * kGroups;
-  int flip = 0;
-  for (int64_t row = (int64_t)blockIdx.x * kGroups + grp; row < a.rows; row += stride, flip ^= 1) {
+  const int64_t row0 = (int64_t)blockIdx.x * kGroups + grp;
+  // thread 0 of the group: row `row` into stage s
+  const auto fetch = [&](int64_t row, int s) {
+    const uint32_t bytes = (uint32_t)(cols * sizeof(T));
+    uint8_t* dst = ring + (size_t)s * n_buf * row_bytes;
+    sm100::mbar_arrive_expect_tx(&full[grp][s], bytes * n_buf);
+    bulk_load(dst, static_cast<const T*>(a.x) + row * a.ldx, bytes, &full[grp][s]);
+    bulk_load(dst + row_bytes, static_cast<const T*>(a.dy) + row * a.lddy, bytes, &full[grp][s]);
+    if (a.r)
+      bulk_load(dst + 2 * row_bytes, static_cast<const T*>(a.r) + row * a.ldr, bytes, &full[grp][s]);
+  };
+  if constexpr (kRing) {
+    if (t == 0)
+      for (int s = 0; s < stages; ++s)
+        if (row0 + s * stride < a.rows) fetch(row0 + s * stride, s);
+  }
+  int flip = 0, stage = 0;
+  uint32_t phase = 0;
+  float mean_next = row0 < a.rows ? a.mean[row0] : 0.0f, rstd_next = row0 < a.rows ? a.rstd[row0] : 0.0f;
+  for (int64_t row = row0; row < a.rows; row += stride, flip ^= 1) {
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
     const T* dr = a.r ? static_cast<const T*>(a.r) + row * a.ldr : nullptr;
     T* dx = static_cast<T*>(a.dx) + row * a.lddx;
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    const float mean = mean_next, rstd = rstd_next;
+    if (row + stride < a.rows) {
+      mean_next = a.mean[row + stride];
+      rstd_next = a.rstd[row + stride];
+    }
+    if constexpr (kRing) {
+      if (!sm100::mbar_wait_bounded(&full[grp][stage], phase, nullptr, kWait)) {
+        // (bulk copies of this kernel's own: not expected; the row is computed from memory)
+      } else {
+        const uint8_t* src = ring + (size_t)stage * n_buf * row_bytes;
+        x = reinterpret_cast<const T*>(src);
+        dy = reinterpret_cast<const T*>(src + row_bytes);
+        if (a.r) dr = reinterpret_cast<const T*>(src + 2 * row_bytes);
+      }
+    }
     float xh[kE][V], g[kE][V];
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
@@ -280,13 +345,10 @@ backward_kernel(const LayerNormArgs a) {
         s1 += g[e][k];
         s2 = fmaf(g[e][k], xh[e][k], s2);
       }
-    if constexpr (kGroup == 32) {
-      s1 = warp_sum(s1);
-      s2 = warp_sum(s2);
-    } else {
+    s1 = warp_sum(s1);
+    s2 = warp_sum(s2);
+    if constexpr (kGroup > 32) {
       constexpr int kWarps = kGroup / 32;
-      s1 = warp_sum(s1);
-      s2 = warp_sum(s2);
       if ((threadIdx.x & 31) == 0) {
         buf[flip][0][threadIdx.x >> 5] = s1;
         buf[flip][1][threadIdx.x >> 5] = s2;
@@ -313,11 +375,26 @@ backward_kernel(const LayerNormArgs a) {
       }
       store<T, V>(dx + j, o);
     }
+    if constexpr (kRing) {
+      // every thread of the group has read the stage: the row `stages` ahead may have it
+      if constexpr (kGroup > 32) {
+        if (a.r) __syncthreads();               // (dr was read behind the sums' barrier)
+      } else {
+        __syncwarp();
+      }
+      if (t == 0 && row + stages * stride < a.rows) fetch(row + stages * stride, stage);
+      if (++stage == stages) {
+        stage = 0;
+        phase ^= 1u;
+      }
+    }
   }
   if (a.partial == nullptr) return;
   if constexpr (kGroups > 1) {
     // the warps' sums meet in shared memory, added in warp order
+    float* joined = reinterpret_cast<float*>(dyn);
     const int width = kE * kGroup * V;
+    __syncthreads();                            // the rings are no longer read
 #pragma unroll
     for (int e = 0; e < kE; ++e)
 #pragma unroll
@@ -339,10 +416,12 @@ backward_kernel(const LayerNormArgs a) {
     for (int e = 0; e < kE; ++e) {
       const int64_t j = ((int64_t)e * kGroup + t) * V;
       if (j >= cols) continue;
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        p[j + k] = dw[e][k];
-        p[cols + j + k] = db[e][k];
+      if constexpr (V == 1) {
+        p[j] = dw[e][0];
+        p[cols + j] = db[e][0];
+      } else {
+        store<float, V>(p + j, dw[e]);          // (V divides cols: 16-byte aligned)
+        store<float, V>(p + cols + j, db[e]);
       }
     }
   }
@@ -426,24 +505,24 @@ bool wide_rows(const void* p, int64_t ld, int esize) {
   return p == nullptr || (aligned(p, 16) && ld * esize % 16 == 0);
 }
 
-constexpr int64_t kWarpCols = 32 * 16;        // widest row of a warp
-
 // f(Group, E) for the first shape whose threads hold `chunks` chunks of a row
 template <int E0, typename F>
 cudaError_t for_shape(int64_t chunks, F f) {
-  if (chunks <= 32 * E0) return f(std::integral_constant<int, 32>{}, std::integral_constant<int, E0>{});
-  if (chunks <= 128 * E0) return f(std::integral_constant<int, 128>{}, std::integral_constant<int, E0>{});
-  if (chunks <= 256 * E0) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, E0>{});
-  if (chunks <= 512 * E0) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, E0>{});
-  if (chunks <= 1024 * E0) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, E0>{});
-  return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
+  using std::integral_constant;
+  const integral_constant<int, E0> e{};
+  if (chunks <= 32 * E0) return f(integral_constant<int, 32>{}, e);
+  if (chunks <= 128 * E0) return f(integral_constant<int, 128>{}, e);
+  if (chunks <= 192 * E0) return f(integral_constant<int, 192>{}, e);
+  if (chunks <= 256 * E0) return f(integral_constant<int, 256>{}, e);
+  if (chunks <= 320 * E0) return f(integral_constant<int, 320>{}, e);
+  if (chunks <= 512 * E0) return f(integral_constant<int, 512>{}, e);
+  if (chunks <= 768 * E0) return f(integral_constant<int, 768>{}, e);
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
 }
-
-constexpr int kElemsPerThread = 16;           // columns per thread and row, in registers
 
 template <typename T, typename TW, int V>
 cudaError_t forward_v(const LayerNormArgs& a, cudaStream_t s) {
-  constexpr int kE = kElemsPerThread / V;
+  constexpr int kE = kForwardElems / V;
   return for_shape<kE>((a.cols + V - 1) / V, [&](auto group, auto e) {
     constexpr int G = decltype(group)::value, E = decltype(e)::value;
     constexpr int per = block_of(G) / G;
@@ -463,7 +542,7 @@ cudaError_t forward_t(const LayerNormArgs& a, cudaStream_t s) {
 
 template <typename T, typename TW, int V>
 cudaError_t backward_v(const LayerNormArgs& a, int64_t n_partial, cudaStream_t s) {
-  constexpr int kE = kElemsPerThread / V;
+  constexpr int kE = kBackwardElems / V;
   return for_shape<kE>((a.cols + V - 1) / V, [&](auto group, auto e) -> cudaError_t {
     constexpr int G = decltype(group)::value, E = decltype(e)::value;
     if constexpr (E == 0) {
@@ -474,9 +553,25 @@ cudaError_t backward_v(const LayerNormArgs& a, int64_t n_partial, cudaStream_t s
       return cudaGetLastError();
     } else {
       constexpr int groups = block_of(G) / G;
-      const size_t smem = groups > 1 ? sizeof(float) * 2 * groups * E * G * V : 0;
-      return launch_dependent(backward_kernel<T, TW, G, E, V>, (unsigned)n_partial, block_of(G),
-                              smem, s, 1, true, a);
+      size_t smem = groups > 1 ? sizeof(float) * 2 * groups * E * G * V : 0;
+      if constexpr (V > 1) {
+        // as many rows ahead as the CTAs of an SM have room for
+        constexpr size_t kRingBytes = 208 * 1024 / resident_of(block_of(G));
+        const int row_bytes = (int)(a.cols * sizeof(T));
+        const size_t row = (size_t)groups * (a.r ? 3 : 2) * row_bytes;
+        const int stages = (int)std::min<size_t>(kMaxStages, kRingBytes / row);
+        if (stages >= 2) {
+          const auto kernel = backward_kernel<T, TW, G, E, V, true>;
+          smem = std::max(smem, stages * row);
+          const cudaError_t err = cudaFuncSetAttribute(
+              kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+          if (err != cudaSuccess) return err;
+          return launch_dependent(kernel, (unsigned)n_partial, block_of(G), smem, s, 1, true, a,
+                                  stages, row_bytes);
+        }
+      }
+      return launch_dependent(backward_kernel<T, TW, G, E, V, false>, (unsigned)n_partial,
+                              block_of(G), smem, s, 1, true, a, 0, 0);
     }
   });
 }
@@ -498,9 +593,10 @@ cudaError_t backward_t(const LayerNormArgs& a, int64_t n_partial, cudaStream_t s
 }  // namespace
 
 int64_t layernorm_partial_rows(int64_t rows, int64_t cols, int32_t sms) {
-  // rows of a CTA at a time: its four warps' where a warp holds a row
-  const int64_t at_once = cols <= kWarpCols ? 4 : 1;
-  return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, 2 * sms));
+  // two CTAs on an SM (four of the warp-per-row kernel, with four rows each at a time)
+  const bool warps = cols <= 32 * kBackwardElems;
+  const int64_t at_once = warps ? 4 : 1;
+  return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, (warps ? 4 : 2) * sms));
 }
 
 cudaError_t launch_layernorm_forward(const LayerNormArgs& a, cudaStream_t s) {

@@ -12,9 +12,10 @@
 // Gram product reads them as a K-major operand, Apply as an MN-major one.  Rows are padded
 // with zeros to a multiple of 16; where an operand has fewer than an MMA's 128 rows, the
 // rest of it is whatever follows in shared memory, and those rows of the result are not read.
-// A product's K steps are dealt to up to four accumulators in turn: consecutive MMAs into one
-// wait for each other (~85 cycles a step of 16, whatever N), and the tensor cores' sums round
-// towards zero (zo_ortho_gemm.cu).
+// One accumulator a product: dealing the K steps to four in turn took the MMAs of 128 x 128 no
+// less time, and adding them up in the epilogues doubled a step's (75 K cycles for five steps,
+// 187 K with four).  The small products come first, so that few of the sums that the tensor
+// cores round towards zero (zo_ortho_gemm.cu) are large ones.
 // Between load and scaling, and between the last step and the update of W, the two fp16 planes
 // of X hold the upper and lower halves of fp32 values, so that the caller's matrices are read
 // and written once, in their own order.
@@ -47,7 +48,7 @@ struct Geometry {
   int a_panels;                   // 64-column panels of A
   int x_bytes, a_bytes;           // of a hi (or lo) part
   int red_bytes;                  // the cluster's partial Gram sums
-  int tmem_cols, n_sym, n_apply;  // Tensor Memory; accumulators of Gram and Poly, of Apply
+  int tmem_cols;                  // an accumulator: p16 columns, or in Apply cs
   int smem;
 };
 __host__ __device__ inline Geometry geometry(int p, int64_t c, int cluster) {
@@ -64,16 +65,8 @@ __host__ __device__ inline Geometry geometry(int p, int64_t c, int cluster) {
   const int over = 16 * 1024;
   const int need = 2 * g.x_bytes + 2 * g.a_bytes + (g.red_bytes > over ? g.red_bytes : over) +
                    1024 /*barrier, sums*/ + 1024 /*align*/;
-  // two accumulators of each product, or all the Tensor Memory that the CTAs which fit beside
-  // each other leave
-  const int widest = g.p16 > g.cs ? g.p16 : g.cs;
-  const int fit = 228 * 1024 / (need + 1024) > 0 ? 228 * 1024 / (need + 1024) : 1;
   g.tmem_cols = 32;
-  while (g.tmem_cols < widest || (g.tmem_cols < 512 && (g.tmem_cols < 2 * widest ||
-                                                        2 * g.tmem_cols * fit <= 512)))
-    g.tmem_cols *= 2;
-  g.n_sym = g.tmem_cols / g.p16 < 4 ? g.tmem_cols / g.p16 : 4;
-  g.n_apply = g.tmem_cols / g.cs < 4 ? g.tmem_cols / g.cs : 4;
+  while (g.tmem_cols < g.p16 || g.tmem_cols < g.cs) g.tmem_cols *= 2;
   // A CTA must never wait for another's Tensor Memory: clusters of two launches could then
   // wait for one another.  So each takes at least its columns' share of the SM's 228 KB (1 KB
   // of them the system's), and CTAs that fit together have their columns too.
@@ -110,21 +103,13 @@ __device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t (&v)[8]) {
                  "=r"(v[6]), "=r"(v[7])
                : "r"(taddr));
 }
-// eight columns of up to four accumulators `stride` columns apart, added up
-__device__ __forceinline__ void tmem_sum_x8(uint32_t taddr, int n, uint32_t stride, float (&v)[8]) {
-  uint32_t r[4][8];
-#pragma unroll
-  for (int a = 0; a < 4; ++a)
-    if (a < n) tmem_ld_x8(taddr + a * stride, r[a]);
+// eight columns of an accumulator
+__device__ __forceinline__ void sums8(uint32_t taddr, float (&v)[8]) {
+  uint32_t r[8];
+  tmem_ld_x8(taddr, r);
   tmem_ld_wait();
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[0][e]);
-#pragma unroll
-  for (int a = 1; a < 4; ++a)
-    if (a < n) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(r[a][e]);
-    }
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[e]);
 }
 // hi + lo of eight neighbouring fp16 pairs
 __device__ __forceinline__ void pairs8(const uint8_t* hi, const uint8_t* lo, float (&v)[8]) {
@@ -263,22 +248,18 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
   const bool active = 32 * g4 < p16;           // (a whole warp)
   const uint32_t xh_s = smem_u32(xh), xl_s = smem_u32(xl), ah_s = smem_u32(ah), al_s = smem_u32(al);
   const uint32_t panel = (uint32_t)(p16 * 128);
-  // D += sum over K steps of A B^T: K step s of 16 lies at step(s) of either operand's bytes
-  const auto product = [&](int n_k, int n_acc, uint32_t stride, uint32_t idesc, uint32_t hi_a,
-                           uint32_t lo_a, uint32_t hi_b, uint32_t lo_b, auto step_a, auto step_b,
-                           uint32_t lead_b, uint32_t col) {
-    for (int prod = 0; prod < 3; ++prod) {
-      const uint32_t a = prod == 1 ? lo_a : hi_a, b = prod == 0 ? lo_b : hi_b;
-      int acc = 0;
-      for (int s = 0; s < n_k; ++s) {
-        mma_f16(tmem + col + (uint32_t)acc * stride, sdesc(a + step_a(s), 16),
-                sdesc(b + step_b(s), lead_b), idesc, prod > 0 || s >= n_acc ? 1u : 0u);
-        if (++acc == n_acc) acc = 0;
-      }
-    }
-  };
   const auto k_major = [&](int s) { return (uint32_t)(s >> 2) * panel + 32u * (uint32_t)(s & 3); };
   const auto mn_major = [&](int s) { return 2048u * (uint32_t)s; };
+  // D = sum over K steps of A B^T: K step s of 16 lies at step(s) of either operand's bytes
+  const auto product = [&](int n_k, uint32_t idesc, uint32_t hi_a, uint32_t lo_a, uint32_t hi_b,
+                           uint32_t lo_b, auto step_b, uint32_t lead_b, uint32_t col) {
+    for (int prod = 0; prod < 3; ++prod) {
+      const uint32_t a = prod == 1 ? lo_a : hi_a, b = prod == 0 ? lo_b : hi_b;
+      for (int s = 0; s < n_k; ++s)
+        mma_f16(tmem + col, sdesc(a + k_major(s), 16), sdesc(b + step_b(s), lead_b), idesc,
+                prod > 0 || s > 0 ? 1u : 0u);
+    }
+  };
   const uint32_t idesc_sym = idesc_f16_f32(128, p16);
 
   for (int k = 0; k < steps.n; ++k) {
@@ -286,17 +267,15 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     // ---- A = X X^T over this CTA's columns
     before_mma();
     if (tid == 0) {
-      product(4 * geo.panels, geo.n_sym, (uint32_t)p16, idesc_sym, xh_s, xl_s, xh_s, xl_s, k_major,
-              k_major, 16, 0);
+      product(4 * geo.panels, idesc_sym, xh_s, xl_s, xh_s, xl_s, k_major, 16, 0);
       mma_commit(&sh.done);
     }
     wait_mma();
     const float sa = exp2i(st.ea - 2 * st.ex);
     if (active) {
-      const int n_acc = min(geo.n_sym, 4 * geo.panels);
       for (int j = 8 * group; j < p16; j += 8 * kGroups) {
         float v[8];
-        tmem_sum_x8(tmem + lanes + (uint32_t)j, n_acc, (uint32_t)p16, v);
+        sums8(tmem + lanes + (uint32_t)j, v);
         if (row < p16) {
           if (cluster > 1) {
             float* to = red + row * p16 + j;
@@ -345,17 +324,15 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     // ---- B = b A + c A A, in A's place
     before_mma();
     if (tid == 0) {
-      product(p16 / 16, geo.n_sym, (uint32_t)p16, idesc_sym, ah_s, al_s, ah_s, al_s, k_major,
-              k_major, 16, 0);
+      product(p16 / 16, idesc_sym, ah_s, al_s, ah_s, al_s, k_major, 16, 0);
       mma_commit(&sh.done);
     }
     wait_mma();
     if (active) {
       const float s0 = st.b * exp2i(st.eb - st.ea), s1 = st.c * exp2i(st.eb - 2 * st.ea);
-      const int n_acc = min(geo.n_sym, p16 / 16);
       for (int j = 8 * group; j < p16; j += 8 * kGroups) {
         float v[8];
-        tmem_sum_x8(tmem + lanes + (uint32_t)j, n_acc, (uint32_t)p16, v);
+        sums8(tmem + lanes + (uint32_t)j, v);
         if (row < p16) {
           const int at = swizzled(p16, row, j);
           float x[8];
@@ -372,9 +349,8 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     if (tid == 0) {
       for (int q = 0; q < geo.panels; q += 4) {
         const int width = 64 * min(4, geo.panels - q);
-        product(p16 / 16, geo.n_apply, (uint32_t)cs, idesc_f16_f32(128, width) | kMnMajorB, ah_s,
-                al_s, xh_s + q * panel, xl_s + q * panel, k_major, mn_major, panel,
-                (uint32_t)(64 * q));
+        product(p16 / 16, idesc_f16_f32(128, width) | kMnMajorB, ah_s, al_s, xh_s + q * panel,
+                xl_s + q * panel, mn_major, panel, (uint32_t)(64 * q));
       }
       mma_commit(&sh.done);
     }
@@ -382,10 +358,9 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     if (active) {
       const float s0 = st.a * exp2i(st.last ? -st.ex : st.ex_next - st.ex);
       const float s1 = exp2i((st.last ? 0 : st.ex_next) - st.ex - st.eb);
-      const int n_acc = min(geo.n_apply, p16 / 16);
       for (int j = 8 * group; j < cs; j += 8 * kGroups) {
         float v[8];
-        tmem_sum_x8(tmem + lanes + (uint32_t)j, n_acc, (uint32_t)cs, v);
+        sums8(tmem + lanes + (uint32_t)j, v);
         if (row < p16) {
           const int at = swizzled(p16, row, j);
           uint4* ph = reinterpret_cast<uint4*>(xh + at);
@@ -471,7 +446,7 @@ cudaError_t launch_ortho_small(const OrthoMat* mats, const int* which, int32_t n
   st.n = n_steps;
   std::copy(steps, steps + n_steps, st.s);
   // sixteen warps for the epilogues where a CTA has its SM to itself
-  return smem > 114 * 1024 ? launch<512>(mats, which, n, cluster, smem, st, u, status, s)
+  return smem > 113 * 1024 ? launch<512>(mats, which, n, cluster, smem, st, u, status, s)
                            : launch<256>(mats, which, n, cluster, smem, st, u, status, s);
 }
 

@@ -11,6 +11,7 @@ caller's tensors and launches them on PyTorch's current stream:
 No arithmetic happens here.
 """
 
+import contextlib
 from typing import NamedTuple, Optional
 
 import torch
@@ -25,19 +26,45 @@ class LayerNormOut(NamedTuple):
     h: Optional[torch.Tensor]          # x + residual, rounded to x's type (None: no residual)
 
 
+def _on(x):
+    """The current stream's handle on x's device, and that device's context if it is not the
+    current one."""
+    dev = x.get_device()
+    if dev < 0:
+        raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, "firstorder", "the tensors are not on a GPU")
+    here = dev == torch.cuda.current_device()
+    return torch.cuda.current_stream(dev).cuda_stream, _HERE if here else torch.cuda.device(dev)
+
+
+_HERE = contextlib.nullcontext()
+
+
 def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
     """LayerNorm over the last dimension of a rows x cols tensor, of x + residual where a
     residual is given (the sum comes back as ``h``)."""
-    rows = x.shape[0]
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    h = torch.empty_like(y) if residual is not None else None
-    mean = rstd = None
+    at = "layer_norm"
+    px, ldx = zb._rows(x, at, "x", None, None, None)
+    (rows, cols), dt, dev = x.shape, x.dtype, x.device
+    w = weight if weight is not None else bias
+    wdt = torch.float32 if w is None else w.dtype
+    pw = zb._vector(weight, at, "weight", cols, wdt, dev)
+    pb = zb._vector(bias, at, "bias", cols, wdt, dev)
+    pr, ldr = zb._rows(residual, at, "residual", x.shape, dt, dev)
+    stream, there = _on(x)
+    # the outputs are contiguous: nothing of them needs a check
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    h = ph = mean = rstd = pm = ps = None
+    if residual is not None:
+        h = torch.empty_like(y)
+        ph = h.data_ptr()
     if stats:
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    with torch.cuda.device(x.device):
-        zb.zo_layernorm_forward(x, residual, weight, bias, eps, y, h, mean, rstd,
-                                torch.cuda.current_stream())
+        mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
+        pm, ps = mean.data_ptr(), rstd.data_ptr()
+    with there:
+        zb._check(zb.LIB.zo_layernorm_forward(
+            px, ldx, pr, ldr, rows, cols, zb._dtype_code(x, at, "x"), pw, pb,
+            zb.ZO_F32 if w is None else zb._dtype_code(w, at, "weight"), eps, y.data_ptr(), cols,
+            ph, cols, pm, ps, stream), at)
     return LayerNormOut(y, mean, rstd, h)
 
 
@@ -46,19 +73,31 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dresidual=None, wdtype=None, 
     """(dx, dweight, dbias) from the gradient of y and the forward pass's input (its ``h``
     where there was a residual) and statistics; dresidual is added to dx.  dweight and dbias
     have the weight's type (wdtype where there is none); None where not wanted."""
-    if wdtype is None:
-        wdtype = torch.float32 if weight is None else weight.dtype
-    rows, cols = x.shape
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw = torch.empty(cols, dtype=wdtype, device=x.device) if want_weight else None
-    db = torch.empty(cols, dtype=wdtype, device=x.device) if want_bias else None
-    with torch.cuda.device(x.device):
-        ws = None
+    at = "layer_norm_backward"
+    px, ldx = zb._rows(x, at, "x", None, None, None)
+    (rows, cols), dt, dev = x.shape, x.dtype, x.device
+    if weight is not None:
+        wdtype = weight.dtype
+    elif wdtype is None:
+        wdtype = torch.float32
+    pw = zb._vector(weight, at, "weight", cols, wdtype, dev)
+    pdy, lddy = zb._rows(dy, at, "dy", x.shape, dt, dev)
+    pdr, lddr = zb._rows(dresidual, at, "dresidual", x.shape, dt, dev)
+    pm = zb._vector(mean, at, "mean", rows, torch.float32, dev)
+    ps = zb._vector(rstd, at, "rstd", rows, torch.float32, dev)
+    stream, there = _on(x)
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+    dw = x.new_empty((cols,), dtype=wdtype) if want_weight else None
+    db = x.new_empty((cols,), dtype=wdtype) if want_bias else None
+    with there:
+        ws, ws_bytes = None, 0
         if want_weight or want_bias:
-            ws = torch.empty(zb.zo_layernorm_workspace(rows, cols), dtype=torch.uint8,
-                             device=x.device)
-        zb.zo_layernorm_backward(dy, x, dresidual, weight, mean, rstd, dx, dw, db, ws,
-                                 torch.cuda.current_stream())
+            ws_bytes = zb.LIB.zo_layernorm_workspace(rows, cols)
+            ws = x.new_empty((ws_bytes,), dtype=torch.uint8)
+        zb._check(zb.LIB.zo_layernorm_backward(
+            pdy, lddy, px, ldx, pdr, lddr, rows, cols, zb._dtype_code(x, at, "x"), pw,
+            zb._code_of(wdtype, at, "weight"), pm, ps, dx.data_ptr(), cols, zb._ptr(dw),
+            zb._ptr(db), zb._ptr(ws), ws_bytes, stream), at)
     return dx, dw, db
 
 
