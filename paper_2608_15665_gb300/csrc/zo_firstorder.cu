@@ -78,7 +78,9 @@ zo_status zo_layernorm_forward(const void* X, int64_t ldx, const void* R, int64_
   a.dtype = dtype;
   a.wdtype = wdtype;
   a.eps = eps;
-  ZO_CUDA(zo::launch_layernorm_forward(a, reinterpret_cast<cudaStream_t>(stream)),
+  const int32_t sms = sm_count();
+  if (sms <= 0) return refuse(ZO_ERR_CUDA, "zo_layernorm_forward: no usable CUDA device");
+  ZO_CUDA(zo::launch_layernorm_forward(a, sms, reinterpret_cast<cudaStream_t>(stream)),
           "layer norm forward kernel");
   return ZO_OK;
 }

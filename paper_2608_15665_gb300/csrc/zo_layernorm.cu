@@ -18,13 +18,16 @@
 // bytes of the activations' type where every pointer, stride and the width allow it, else
 // single elements.  Rows wider than a CTA's registers are swept from memory (kE = 0).
 //
-// Forward: 32 columns a thread and short CTAs, many rows in flight on an SM.
+// Many rows: a few resident CTAs take the rows blockIdx, blockIdx + gridDim, ..., and what
+// keeps HBM busy is a ring of rows per group in shared memory, filled by bulk copies several
+// rows ahead.  A row that does not start or end on 16 bytes is copied with the rest of its
+// first and last 16 (never past an aligned 16 bytes that hold a part of the row).  At 16384 x
+// 5120 bf16 with a residual the backward pass took 271 us without the ring, 115 us with it.
+// Few rows, one per group: straight from memory, which has the shorter latency.
 //
-// Backward: the CTAs take the rows blockIdx, blockIdx + gridDim, ... and keep dw and db of
-// their own columns in registers over all of them (16 columns a thread), so that each CTA
-// writes one row of partial sums, which a second kernel adds up in a fixed order: no
-// atomics, the same bits on every run.  As few CTAs are resident, what keeps HBM busy is a
-// ring of rows per group in shared memory, filled by bulk copies a few rows ahead.
+// The backward pass keeps dw and db of a thread's own columns in registers over all its
+// rows, so that each CTA writes one row of partial sums, which a second kernel adds up in a
+// fixed order: no atomics, the same bits on every run.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -48,20 +51,25 @@ template <> struct Elem<__nv_bfloat16> {
   static __device__ __nv_bfloat16 from(float v) { return __float2bfloat16_rn(v); }
 };
 
-// V consecutive elements as floats
-template <typename T, int V>
+// V consecutive elements as floats.  kReadOnly: of buffers that no kernel writes meanwhile, so
+// that the loads can be issued ahead of stores.
+template <typename T, int V, bool kReadOnly = false>
 __device__ __forceinline__ void load(const T* p, float (&v)[V]) {
+  const auto get = [](const auto* q) {
+    if constexpr (kReadOnly) return __ldg(q);
+    else return *q;
+  };
   if constexpr (V == 1) {
-    v[0] = Elem<T>::to(*p);
+    v[0] = Elem<T>::to(get(p));
   } else if constexpr (sizeof(T) == 4) {
     static_assert(V % 4 == 0);
 #pragma unroll
     for (int k = 0; k < V / 4; ++k) {
-      const float4 q = reinterpret_cast<const float4*>(p)[k];
+      const float4 q = get(reinterpret_cast<const float4*>(p) + k);
       v[4 * k] = q.x; v[4 * k + 1] = q.y; v[4 * k + 2] = q.z; v[4 * k + 3] = q.w;
     }
   } else if constexpr (V == 8) {
-    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    const uint4 q = get(reinterpret_cast<const uint4*>(p));
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -70,7 +78,7 @@ __device__ __forceinline__ void load(const T* p, float (&v)[V]) {
     }
   } else {
     static_assert(V == 4);
-    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    const uint2 q = get(reinterpret_cast<const uint2*>(p));
     v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xFFFF0000u);
     v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xFFFF0000u);
   }
@@ -120,8 +128,75 @@ __device__ __forceinline__ float group_sum(float v, float* buf) {
 // threads of a CTA whose rows take `group` threads each
 __host__ __device__ constexpr int block_of(int group) { return group == 32 ? 128 : group; }
 
-constexpr int kForwardElems = 32;             // columns per thread and row, in registers
-constexpr int kBackwardElems = 16;
+// resident CTAs of the many-row kernels on an SM: as many as leave a thread its columns' registers
+__host__ __device__ constexpr int resident_of(int block) { return block <= 128 ? 3 : block <= 320 ? 2 : 1; }
+
+// columns per thread and row, in registers: of a warp's rows, of a CTA's
+constexpr int kWarpElems = 32, kCtaElems = 16;
+
+// ------------------------------------------------------------------------------- ring
+constexpr int kMaxStages = 8;
+constexpr long long kWait = 4000000000LL;     // ~2 s at 2 GHz
+
+// an untiled bulk copy of `bytes` (16-byte aligned, a multiple of 16) into shared memory
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+          sm100::smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(sm100::smem_u32(bar))
+      : "memory");
+}
+
+// The rows of one group, `stages` of them in flight; up to three matrices, row `row` of each
+// in one stage.  `slot` bytes hold a row and the rest of its first and last 16.
+template <typename T>
+struct Ring {
+  const T* base[3];
+  int64_t ld[3];
+  int n, stages;
+  uint32_t slot, bytes;
+  uint8_t* smem;
+  uint64_t* full;
+  int stage = 0;
+  uint32_t phase = 0;
+
+  __device__ const T* row_of(int m, int64_t row) const { return base[m] + row * ld[m]; }
+  static __device__ uint32_t lead(const T* p) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u); }
+  // by one thread of the group
+  __device__ void fetch(int64_t row, int s) const {
+    uint8_t* dst = smem + (size_t)s * n * slot;
+    uint32_t total = 0, part[3];
+#pragma unroll
+    for (int m = 0; m < 3; ++m) {
+      part[m] = m < n ? (lead(row_of(m, row)) + bytes + 15u) & ~15u : 0u;
+      total += part[m];
+    }
+    sm100::mbar_arrive_expect_tx(&full[s], total);
+#pragma unroll
+    for (int m = 0; m < 3; ++m)
+      if (m < n) {
+        const T* p = row_of(m, row);
+        bulk_load(dst + m * slot, reinterpret_cast<const uint8_t*>(p) - lead(p), part[m], &full[s]);
+      }
+  }
+  // the matrices' pointers to row `row`: in shared memory (or, should the copies not have
+  // come, in memory itself)
+  __device__ void take(int64_t row, const T* (&p)[3]) const {
+    const bool here = sm100::mbar_wait_bounded(&full[stage], phase, nullptr, kWait);
+    const uint8_t* src = smem + (size_t)stage * n * slot;
+#pragma unroll
+    for (int m = 0; m < 3; ++m) {
+      const T* q = m < n ? row_of(m, row) : nullptr;
+      p[m] = m < n && here ? reinterpret_cast<const T*>(src + m * slot + lead(q)) : q;
+    }
+  }
+  __device__ void advance() {
+    if (++stage == stages) {
+      stage = 0;
+      phase ^= 1u;
+    }
+  }
+};
 
 // ---------------------------------------------------------------------------- forward
 template <typename T, typename TW, int kGroup, int kE, int V>
@@ -144,10 +219,10 @@ forward_kernel(const LayerNormArgs a) {
   const float inv_n = 1.0f / (float)cols;
 
   auto fetch = [&](int64_t j, float (&v)[V]) {
-    load<T, V>(x + j, v);
+    load<T, V, true>(x + j, v);
     if (r) {
       float q[V];
-      load<T, V>(r + j, q);
+      load<T, V, true>(r + j, q);
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = Elem<T>::to(Elem<T>::from(v[k] + q[k]));
     }
@@ -156,8 +231,8 @@ forward_kernel(const LayerNormArgs a) {
     float wv[V], bv[V], o[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) { wv[k] = 1.0f; bv[k] = 0.0f; }
-    if (w) load<TW, V>(w + j, wv);
-    if (b) load<TW, V>(b + j, bv);
+    if (w) load<TW, V, true>(w + j, wv);
+    if (b) load<TW, V, true>(b + j, bv);
 #pragma unroll
     for (int k = 0; k < V; ++k) o[k] = fmaf((v[k] - mean) * rstd, wv[k], bv[k]);
     store<T, V>(y + j, o);
@@ -230,29 +305,104 @@ forward_kernel(const LayerNormArgs a) {
   }
 }
 
-// --------------------------------------------------------------------------- backward
-// an untiled bulk copy of `bytes` (16-byte aligned, a multiple of 16) into shared memory
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-          sm100::smem_u32(dst)),
-      "l"(src), "r"(bytes), "r"(sm100::smem_u32(bar))
-      : "memory");
+// Many rows: the group's rows by a ring; weight and bias stay in registers.
+template <typename T, typename TW, int kGroup, int kE, int V>
+__global__ void __launch_bounds__(block_of(kGroup), resident_of(block_of(kGroup)))
+forward_ring_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
+  constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup;
+  __shared__ float buf[2][2][32];
+  __shared__ uint64_t full[kGroups][kMaxStages];
+  extern __shared__ __align__(128) uint8_t dyn[];
+  const int t = threadIdx.x % kGroup, grp = threadIdx.x / kGroup;
+  const int64_t cols = a.cols;
+  const float inv_n = 1.0f / (float)cols;
+  Ring<T> ring{{static_cast<const T*>(a.x), static_cast<const T*>(a.r), nullptr},
+               {a.ldx, a.ldr, 0}, a.r ? 2 : 1, stages, slot, (uint32_t)(cols * sizeof(T)),
+               dyn + (size_t)grp * stages * (a.r ? 2 : 1) * slot, full[grp]};
+  if (t == 0) {
+    for (int s = 0; s < stages; ++s) sm100::mbar_init(&full[grp][s], 1);
+    sm100::fence_mbar_init();
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  const int64_t stride = (int64_t)gridDim.x * kGroups;
+  const int64_t row0 = (int64_t)blockIdx.x * kGroups + grp;
+  if (t == 0)
+    for (int s = 0; s < stages; ++s)
+      if (row0 + s * stride < a.rows) ring.fetch(row0 + s * stride, s);
+  const TW* w = static_cast<const TW*>(a.weight);
+  const TW* b = static_cast<const TW*>(a.bias);
+  float wv[kE][V], bv[kE][V];
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const int64_t j = ((int64_t)e * kGroup + t) * V;
+#pragma unroll
+    for (int k = 0; k < V; ++k) { wv[e][k] = 1.0f; bv[e][k] = 0.0f; }
+    if (w && j < cols) load<TW, V, true>(w + j, wv[e]);
+    if (b && j < cols) load<TW, V, true>(b + j, bv[e]);
+  }
+  int flip = 0;
+  for (int64_t row = row0; row < a.rows; row += stride, flip ^= 1) {
+    const T* src[3];
+    ring.take(row, src);
+    T* y = static_cast<T*>(a.y) + row * a.ldy;
+    float v[kE][V];
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const int64_t j = ((int64_t)e * kGroup + t) * V;
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[e][k] = 0.0f;
+      if (j < cols) {
+        load<T, V>(src[0] + j, v[e]);
+        if (a.r) {
+          float q[V];
+          load<T, V>(src[1] + j, q);
+#pragma unroll
+          for (int k = 0; k < V; ++k) v[e][k] = Elem<T>::to(Elem<T>::from(v[e][k] + q[k]));
+          store<T, V>(static_cast<T*>(a.h) + row * a.ldh + j, v[e]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < V; ++k) s += v[e][k];
+    }
+    const float mean = group_sum<kGroup>(s, buf[flip][0]) * inv_n;
+    // every thread of the group has read the stage
+    if (t == 0 && row + stages * stride < a.rows) ring.fetch(row + stages * stride, ring.stage);
+    ring.advance();
+    float q = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const int64_t j = ((int64_t)e * kGroup + t) * V;
+      if (j < cols) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) q = fmaf(v[e][k] - mean, v[e][k] - mean, q);
+      }
+    }
+    const float rstd = 1.0f / sqrtf(group_sum<kGroup>(q, buf[flip][1]) * inv_n + a.eps);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const int64_t j = ((int64_t)e * kGroup + t) * V;
+      if (j < cols) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[e][k] = fmaf((v[e][k] - mean) * rstd, wv[e][k], bv[e][k]);
+        store<T, V>(y + j, v[e]);
+      }
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+  }
 }
 
+// --------------------------------------------------------------------------- backward
 // Rows held in registers: each thread keeps its columns' weight, dw and db over all rows
-// of its group.  kRing: the rows come through a ring of `stages` rows in shared memory
-// (16-byte chunks only), else straight from memory.
-constexpr int kMaxStages = 8;
-constexpr long long kWait = 4000000000LL;       // ~2 s at 2 GHz
-
-// CTAs of the backward kernel on an SM: as many as leave a thread the ~100 registers of its
-// columns
-__host__ __device__ constexpr int resident_of(int block) { return block <= 128 ? 4 : block <= 320 ? 2 : 1; }
-
+// of its group.  kRing: the rows come through a ring, else straight from memory.
 template <typename T, typename TW, int kGroup, int kE, int V, bool kRing>
 __global__ void __launch_bounds__(block_of(kGroup), resident_of(block_of(kGroup)))
-backward_kernel(const LayerNormArgs a, int stages, int row_bytes) {
+backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup;
   static_assert(kE > 0, "rows in registers");
   __shared__ float buf[2][2][32];
@@ -261,8 +411,9 @@ backward_kernel(const LayerNormArgs a, int stages, int row_bytes) {
   const int t = threadIdx.x % kGroup, grp = threadIdx.x / kGroup;
   const int64_t cols = a.cols;
   const float inv_n = 1.0f / (float)cols;
-  const int n_buf = a.r ? 3 : 2;
-  uint8_t* ring = dyn + (size_t)grp * stages * n_buf * row_bytes;
+  Ring<T> ring{{static_cast<const T*>(a.x), static_cast<const T*>(a.dy), static_cast<const T*>(a.r)},
+               {a.ldx, a.lddy, a.ldr}, a.r ? 3 : 2, stages, slot, (uint32_t)(cols * sizeof(T)),
+               dyn + (size_t)grp * stages * (a.r ? 3 : 2) * slot, full[grp]};
   if constexpr (kRing) {
     if (t == 0) {
       for (int s = 0; s < stages; ++s) sm100::mbar_init(&full[grp][s], 1);
@@ -279,55 +430,33 @@ backward_kernel(const LayerNormArgs a, int stages, int row_bytes) {
     const int64_t j = ((int64_t)e * kGroup + t) * V;
 #pragma unroll
     for (int k = 0; k < V; ++k) { wv[e][k] = 1.0f; dw[e][k] = db[e][k] = 0.0f; }
-    if (w && j < cols) load<TW, V>(w + j, wv[e]);
+    if (w && j < cols) load<TW, V, true>(w + j, wv[e]);
   }
   const int64_t stride = (int64_t)gridDim.x * kGroups;
   const int64_t row0 = (int64_t)blockIdx.x * kGroups + grp;
-  // thread 0 of the group: row `row` into stage s
-  const auto fetch = [&](int64_t row, int s) {
-    const uint32_t bytes = (uint32_t)(cols * sizeof(T));
-    uint8_t* dst = ring + (size_t)s * n_buf * row_bytes;
-    sm100::mbar_arrive_expect_tx(&full[grp][s], bytes * n_buf);
-    bulk_load(dst, static_cast<const T*>(a.x) + row * a.ldx, bytes, &full[grp][s]);
-    bulk_load(dst + row_bytes, static_cast<const T*>(a.dy) + row * a.lddy, bytes, &full[grp][s]);
-    if (a.r)
-      bulk_load(dst + 2 * row_bytes, static_cast<const T*>(a.r) + row * a.ldr, bytes, &full[grp][s]);
-  };
   if constexpr (kRing) {
     if (t == 0)
       for (int s = 0; s < stages; ++s)
-        if (row0 + s * stride < a.rows) fetch(row0 + s * stride, s);
+        if (row0 + s * stride < a.rows) ring.fetch(row0 + s * stride, s);
   }
-  int flip = 0, stage = 0;
-  uint32_t phase = 0;
+  int flip = 0;
   float mean_next = row0 < a.rows ? a.mean[row0] : 0.0f, rstd_next = row0 < a.rows ? a.rstd[row0] : 0.0f;
   for (int64_t row = row0; row < a.rows; row += stride, flip ^= 1) {
-    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
-    const T* dr = a.r ? static_cast<const T*>(a.r) + row * a.ldr : nullptr;
+    const T* src[3] = {ring.row_of(0, row), ring.row_of(1, row), a.r ? ring.row_of(2, row) : nullptr};
     T* dx = static_cast<T*>(a.dx) + row * a.lddx;
     const float mean = mean_next, rstd = rstd_next;
     if (row + stride < a.rows) {
       mean_next = a.mean[row + stride];
       rstd_next = a.rstd[row + stride];
     }
-    if constexpr (kRing) {
-      if (!sm100::mbar_wait_bounded(&full[grp][stage], phase, nullptr, kWait)) {
-        // (bulk copies of this kernel's own: not expected; the row is computed from memory)
-      } else {
-        const uint8_t* src = ring + (size_t)stage * n_buf * row_bytes;
-        x = reinterpret_cast<const T*>(src);
-        dy = reinterpret_cast<const T*>(src + row_bytes);
-        if (a.r) dr = reinterpret_cast<const T*>(src + 2 * row_bytes);
-      }
-    }
+    if constexpr (kRing) ring.take(row, src);
     float xh[kE][V], g[kE][V];
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
       const int64_t j = ((int64_t)e * kGroup + t) * V;
       if (j < cols) {
-        load<T, V>(x + j, xh[e]);
-        load<T, V>(dy + j, g[e]);
+        load<T, V>(src[0] + j, xh[e]);
+        load<T, V>(src[1] + j, g[e]);
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) { xh[e][k] = mean; g[e][k] = 0.0f; }
@@ -367,9 +496,9 @@ backward_kernel(const LayerNormArgs a, int stages, int row_bytes) {
       float o[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) o[k] = rstd * (g[e][k] - s1 - xh[e][k] * s2);
-      if (dr) {
+      if (a.r) {
         float q[V];
-        load<T, V>(dr + j, q);
+        load<T, V>(src[2] + j, q);
 #pragma unroll
         for (int k = 0; k < V; ++k) o[k] += q[k];
       }
@@ -382,11 +511,8 @@ backward_kernel(const LayerNormArgs a, int stages, int row_bytes) {
       } else {
         __syncwarp();
       }
-      if (t == 0 && row + stages * stride < a.rows) fetch(row + stages * stride, stage);
-      if (++stage == stages) {
-        stage = 0;
-        phase ^= 1u;
-      }
+      if (t == 0 && row + stages * stride < a.rows) ring.fetch(row + stages * stride, ring.stage);
+      ring.advance();
     }
   }
   if (a.partial == nullptr) return;
@@ -505,45 +631,70 @@ bool wide_rows(const void* p, int64_t ld, int esize) {
   return p == nullptr || (aligned(p, 16) && ld * esize % 16 == 0);
 }
 
-// f(Group, E) for the first shape whose threads hold `chunks` chunks of a row
-template <int E0, typename F>
-cudaError_t for_shape(int64_t chunks, F f) {
+// f(Group, E) for the first shape whose threads hold a row's chunks of V columns
+template <int V, typename F>
+cudaError_t for_shape(int64_t cols, F f) {
   using std::integral_constant;
-  const integral_constant<int, E0> e{};
-  if (chunks <= 32 * E0) return f(integral_constant<int, 32>{}, e);
-  if (chunks <= 128 * E0) return f(integral_constant<int, 128>{}, e);
-  if (chunks <= 192 * E0) return f(integral_constant<int, 192>{}, e);
-  if (chunks <= 256 * E0) return f(integral_constant<int, 256>{}, e);
-  if (chunks <= 320 * E0) return f(integral_constant<int, 320>{}, e);
-  if (chunks <= 512 * E0) return f(integral_constant<int, 512>{}, e);
-  if (chunks <= 768 * E0) return f(integral_constant<int, 768>{}, e);
+  const int64_t chunks = (cols + V - 1) / V;
+  constexpr int EW = kWarpElems / V, E = kCtaElems / V;
+  if (chunks <= 32 * EW) return f(integral_constant<int, 32>{}, integral_constant<int, EW>{});
+  if (chunks <= 128 * E) return f(integral_constant<int, 128>{}, integral_constant<int, E>{});
+  if (chunks <= 192 * E) return f(integral_constant<int, 192>{}, integral_constant<int, E>{});
+  if (chunks <= 256 * E) return f(integral_constant<int, 256>{}, integral_constant<int, E>{});
+  if (chunks <= 320 * E) return f(integral_constant<int, 320>{}, integral_constant<int, E>{});
+  if (chunks <= 512 * E) return f(integral_constant<int, 512>{}, integral_constant<int, E>{});
+  if (chunks <= 768 * E) return f(integral_constant<int, 768>{}, integral_constant<int, E>{});
   return f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
 }
 
+// stages of a ring of n matrices' rows, as many as an SM's resident CTAs have room for
+template <int kGroup>
+int ring_stages(int n, uint32_t slot) {
+  constexpr int block = block_of(kGroup);
+  const size_t room = 208 * 1024 / resident_of(block);
+  return (int)std::min<size_t>(kMaxStages, room / ((size_t)(block / kGroup) * n * slot));
+}
+template <typename T>
+uint32_t ring_slot(int64_t cols) {
+  return (uint32_t)((cols * sizeof(T) + 15) / 16 * 16 + 16);
+}
+
 template <typename T, typename TW, int V>
-cudaError_t forward_v(const LayerNormArgs& a, cudaStream_t s) {
-  constexpr int kE = kForwardElems / V;
-  return for_shape<kE>((a.cols + V - 1) / V, [&](auto group, auto e) {
+cudaError_t forward_v(const LayerNormArgs& a, int32_t sms, cudaStream_t s) {
+  return for_shape<V>(a.cols, [&](auto group, auto e) -> cudaError_t {
     constexpr int G = decltype(group)::value, E = decltype(e)::value;
-    constexpr int per = block_of(G) / G;
+    constexpr int block = block_of(G), per = block / G;
+    if constexpr (E > 0) {
+      const int64_t grid = (int64_t)resident_of(block) * sms;
+      const uint32_t slot = ring_slot<T>(a.cols);
+      const int n = a.r ? 2 : 1, stages = ring_stages<G>(n, slot);
+      // more rows than the resident groups have at once
+      if (a.rows > grid * per && stages >= 2) {
+        const auto kernel = forward_ring_kernel<T, TW, G, E, V>;
+        const size_t smem = (size_t)per * stages * n * slot;
+        const cudaError_t err = cudaFuncSetAttribute(
+            kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err != cudaSuccess) return err;
+        return launch_dependent(kernel, (unsigned)grid, block, smem, s, 1, true, a, stages, slot);
+      }
+    }
     return launch_dependent(forward_kernel<T, TW, G, E, V>, (unsigned)((a.rows + per - 1) / per),
-                            block_of(G), 0, s, 1, true, a);
+                            block, 0, s, 1, true, a);
   });
 }
 template <typename T, typename TW>
-cudaError_t forward_t(const LayerNormArgs& a, cudaStream_t s) {
+cudaError_t forward_t(const LayerNormArgs& a, int32_t sms, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T);
   const bool wide = a.cols % V == 0 && wide_rows(a.x, a.ldx, sizeof(T)) &&
                     wide_rows(a.r, a.ldr, sizeof(T)) && wide_rows(a.y, a.ldy, sizeof(T)) &&
                     wide_rows(a.h, a.ldh, sizeof(T)) && aligned(a.weight, 16) &&
                     aligned(a.bias, 16);
-  return wide ? forward_v<T, TW, V>(a, s) : forward_v<T, TW, 1>(a, s);
+  return wide ? forward_v<T, TW, V>(a, sms, s) : forward_v<T, TW, 1>(a, sms, s);
 }
 
 template <typename T, typename TW, int V>
 cudaError_t backward_v(const LayerNormArgs& a, int64_t n_partial, cudaStream_t s) {
-  constexpr int kE = kBackwardElems / V;
-  return for_shape<kE>((a.cols + V - 1) / V, [&](auto group, auto e) -> cudaError_t {
+  return for_shape<V>(a.cols, [&](auto group, auto e) -> cudaError_t {
     constexpr int G = decltype(group)::value, E = decltype(e)::value;
     if constexpr (E == 0) {
       backward_wide_kernel<T, TW><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, s>>>(a);
@@ -552,26 +703,18 @@ cudaError_t backward_v(const LayerNormArgs& a, int64_t n_partial, cudaStream_t s
       wide_sums_kernel<T><<<dim3((unsigned)((a.cols + 255) / 256), (unsigned)n_partial), 256, 0, s>>>(a);
       return cudaGetLastError();
     } else {
-      constexpr int groups = block_of(G) / G;
+      constexpr int block = block_of(G), groups = block / G;
       size_t smem = groups > 1 ? sizeof(float) * 2 * groups * E * G * V : 0;
-      if constexpr (V > 1) {
-        // as many rows ahead as the CTAs of an SM have room for
-        constexpr size_t kRingBytes = 208 * 1024 / resident_of(block_of(G));
-        const int row_bytes = (int)(a.cols * sizeof(T));
-        const size_t row = (size_t)groups * (a.r ? 3 : 2) * row_bytes;
-        const int stages = (int)std::min<size_t>(kMaxStages, kRingBytes / row);
-        if (stages >= 2) {
-          const auto kernel = backward_kernel<T, TW, G, E, V, true>;
-          smem = std::max(smem, stages * row);
-          const cudaError_t err = cudaFuncSetAttribute(
-              kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-          if (err != cudaSuccess) return err;
-          return launch_dependent(kernel, (unsigned)n_partial, block_of(G), smem, s, 1, true, a,
-                                  stages, row_bytes);
-        }
-      }
-      return launch_dependent(backward_kernel<T, TW, G, E, V, false>, (unsigned)n_partial,
-                              block_of(G), smem, s, 1, true, a, 0, 0);
+      const uint32_t slot = ring_slot<T>(a.cols);
+      const int n = a.r ? 3 : 2, stages = ring_stages<G>(n, slot);
+      const bool ring = a.rows > n_partial * groups && stages >= 2;
+      const auto kernel = ring ? backward_kernel<T, TW, G, E, V, true>
+                               : backward_kernel<T, TW, G, E, V, false>;
+      if (ring) smem = std::max(smem, (size_t)groups * stages * n * slot);
+      const cudaError_t err = cudaFuncSetAttribute(
+          kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::max<size_t>(smem, 1024));
+      if (err != cudaSuccess) return err;
+      return launch_dependent(kernel, (unsigned)n_partial, block, smem, s, 1, true, a, stages, slot);
     }
   });
 }
@@ -593,18 +736,19 @@ cudaError_t backward_t(const LayerNormArgs& a, int64_t n_partial, cudaStream_t s
 }  // namespace
 
 int64_t layernorm_partial_rows(int64_t rows, int64_t cols, int32_t sms) {
-  // two CTAs on an SM (four of the warp-per-row kernel, with four rows each at a time)
-  const bool warps = cols <= 32 * kBackwardElems;
-  const int64_t at_once = warps ? 4 : 1;
-  return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, (warps ? 4 : 2) * sms));
+  // the resident CTAs, which hold four rows at a time where a row is a warp's
+  const bool warps = cols <= 32 * kWarpElems;
+  const int64_t at_once = warps ? 4 : 1, ctas = (int64_t)(warps ? resident_of(128) : 2) * sms;
+  return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, ctas));
 }
 
-cudaError_t launch_layernorm_forward(const LayerNormArgs& a, cudaStream_t s) {
+cudaError_t launch_layernorm_forward(const LayerNormArgs& a, int32_t sms, cudaStream_t s) {
   if (a.rows <= 0) return cudaSuccess;
   if (a.dtype == kF32)
-    return a.wdtype == kF32 ? forward_t<float, float>(a, s) : forward_t<float, __nv_bfloat16>(a, s);
-  return a.wdtype == kF32 ? forward_t<__nv_bfloat16, float>(a, s)
-                          : forward_t<__nv_bfloat16, __nv_bfloat16>(a, s);
+    return a.wdtype == kF32 ? forward_t<float, float>(a, sms, s)
+                            : forward_t<float, __nv_bfloat16>(a, sms, s);
+  return a.wdtype == kF32 ? forward_t<__nv_bfloat16, float>(a, sms, s)
+                          : forward_t<__nv_bfloat16, __nv_bfloat16>(a, sms, s);
 }
 
 cudaError_t launch_layernorm_backward(const LayerNormArgs& a, int32_t sms, cudaStream_t s) {

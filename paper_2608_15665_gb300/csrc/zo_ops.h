@@ -25,7 +25,7 @@ struct LayerNormArgs {
   float eps;
 };
 
-cudaError_t launch_layernorm_forward(const LayerNormArgs& a, cudaStream_t s);
+cudaError_t launch_layernorm_forward(const LayerNormArgs& a, int32_t sms, cudaStream_t s);
 // CTAs of the backward pass: rows of the partial sums of dweight and of dbias
 int64_t layernorm_partial_rows(int64_t rows, int64_t cols, int32_t sms);
 cudaError_t launch_layernorm_backward(const LayerNormArgs& a, int32_t sms, cudaStream_t s);

@@ -11,7 +11,6 @@ caller's tensors and launches them on PyTorch's current stream:
 No arithmetic happens here.
 """
 
-import contextlib
 from typing import NamedTuple, Optional
 
 import torch
@@ -26,17 +25,17 @@ class LayerNormOut(NamedTuple):
     h: Optional[torch.Tensor]          # x + residual, rounded to x's type (None: no residual)
 
 
-def _on(x):
-    """The current stream's handle on x's device, and that device's context if it is not the
-    current one."""
+def _call(fn, x, at, *args):
+    """A call of the C ABI on the current stream of x's device."""
     dev = x.get_device()
     if dev < 0:
-        raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, "firstorder", "the tensors are not on a GPU")
-    here = dev == torch.cuda.current_device()
-    return torch.cuda.current_stream(dev).cuda_stream, _HERE if here else torch.cuda.device(dev)
-
-
-_HERE = contextlib.nullcontext()
+        raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, f"the tensors are on {x.device}, not on a GPU")
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    if dev == torch.cuda.current_device():
+        zb._check(fn(*args, stream), at)
+    else:
+        with torch.cuda.device(dev):
+            zb._check(fn(*args, stream), at)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
@@ -50,7 +49,6 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
     pw = zb._vector(weight, at, "weight", cols, wdt, dev)
     pb = zb._vector(bias, at, "bias", cols, wdt, dev)
     pr, ldr = zb._rows(residual, at, "residual", x.shape, dt, dev)
-    stream, there = _on(x)
     # the outputs are contiguous: nothing of them needs a check
     y = torch.empty_like(x, memory_format=torch.contiguous_format)
     h = ph = mean = rstd = pm = ps = None
@@ -58,13 +56,13 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
         h = torch.empty_like(y)
         ph = h.data_ptr()
     if stats:
-        mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
+        mean = torch.empty(rows, dtype=torch.float32, device=dev)
+        rstd = torch.empty_like(mean)
         pm, ps = mean.data_ptr(), rstd.data_ptr()
-    with there:
-        zb._check(zb.LIB.zo_layernorm_forward(
-            px, ldx, pr, ldr, rows, cols, zb._dtype_code(x, at, "x"), pw, pb,
-            zb.ZO_F32 if w is None else zb._dtype_code(w, at, "weight"), eps, y.data_ptr(), cols,
-            ph, cols, pm, ps, stream), at)
+    _call(zb.LIB.zo_layernorm_forward, x, at, px, ldx, pr, ldr, rows, cols,
+          zb._dtype_code(x, at, "x"), pw, pb,
+          zb.ZO_F32 if w is None else zb._dtype_code(w, at, "weight"), eps, y.data_ptr(), cols, ph,
+          cols, pm, ps)
     return LayerNormOut(y, mean, rstd, h)
 
 
@@ -85,19 +83,22 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dresidual=None, wdtype=None, 
     pdr, lddr = zb._rows(dresidual, at, "dresidual", x.shape, dt, dev)
     pm = zb._vector(mean, at, "mean", rows, torch.float32, dev)
     ps = zb._vector(rstd, at, "rstd", rows, torch.float32, dev)
-    stream, there = _on(x)
     dx = torch.empty_like(x, memory_format=torch.contiguous_format)
-    dw = x.new_empty((cols,), dtype=wdtype) if want_weight else None
-    db = x.new_empty((cols,), dtype=wdtype) if want_bias else None
-    with there:
-        ws, ws_bytes = None, 0
-        if want_weight or want_bias:
-            ws_bytes = zb.LIB.zo_layernorm_workspace(rows, cols)
-            ws = x.new_empty((ws_bytes,), dtype=torch.uint8)
-        zb._check(zb.LIB.zo_layernorm_backward(
-            pdy, lddy, px, ldx, pdr, lddr, rows, cols, zb._dtype_code(x, at, "x"), pw,
-            zb._code_of(wdtype, at, "weight"), pm, ps, dx.data_ptr(), cols, zb._ptr(dw),
-            zb._ptr(db), zb._ptr(ws), ws_bytes, stream), at)
+    dw = db = pdw = pdb = pws = None
+    ws_bytes = 0
+    if want_weight:
+        dw = torch.empty(cols, dtype=wdtype, device=dev)
+        pdw = dw.data_ptr()
+    if want_bias:
+        db = torch.empty(cols, dtype=wdtype, device=dev)
+        pdb = db.data_ptr()
+    if want_weight or want_bias:
+        ws_bytes = zb.LIB.zo_layernorm_workspace(rows, cols)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+        pws = ws.data_ptr()
+    _call(zb.LIB.zo_layernorm_backward, x, at, pdy, lddy, px, ldx, pdr, lddr, rows, cols,
+          zb._dtype_code(x, at, "x"), pw, zb._code_of(wdtype, at, "weight"), pm, ps, dx.data_ptr(),
+          cols, pdw, pdb, pws, ws_bytes)
     return dx, dw, db
 
 

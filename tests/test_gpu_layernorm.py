@@ -247,3 +247,45 @@ def test_the_workspace_is_checked(lib, gpu):
         with pytest.raises(lib.ZoError) as e:
             lib.zo_layernorm_backward(x, x, None, v, st, st, torch.empty_like(x), v, v, ws)
         assert e.value.status == lib.ZO_ERR_INVALID_ARG
+
+
+# more rows than are in flight at once, on and off 16-byte boundaries
+MANY = [(2000, 77, 0), (1900, 1003, 1), (2500, 640, 0), (700, 2051, 0), (900, 2048, 8),
+        (330, 5121, 0), (400, 5120, 0), (340, 9001, 2), (320, 12288, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("rows,cols,pad", MANY, ids=[f"{s[0]}x{s[1]}" for s in MANY])
+def test_many_rows(lib, gpu, rows, cols, pad, residual, dtype):
+    from paper_2608_15665_gb300 import firstorder as fo
+    x, dy = rows_of(rows, cols, dtype, gpu, 1, pad), rows_of(rows, cols, dtype, gpu, 4, pad)
+    r = rows_of(rows, cols, dtype, gpu, 5, 0) if residual else None
+    dr = rows_of(rows, cols, dtype, gpu, 6, pad) if residual else None
+    w, b = vec(cols, "f32", gpu, 2, 1.0), vec(cols, "f32", gpu, 3, 0.0)
+    out = fo.layer_norm(x, w, b, 1e-5, residual=r)
+    h = out.h if residual else x
+    if residual:
+        assert torch.equal(out.h, (x.float() + r.float()).to(TYPES[dtype]))
+    check_forward(out, f64(h), w, b, 1e-5, dtype)
+    dx, dw, db = fo.layer_norm_backward(dy, h, w, out.mean, out.rstd, dresidual=dr)
+    check_backward(dx, dw, db, f64(dy), f64(h), w, f64(out.mean), f64(out.rstd),
+                   f64(dr) if residual else 0.0, dtype, "f32")
+
+
+@pytest.mark.parametrize("lead", [1, 3, 5])
+def test_rows_that_start_anywhere(lib, gpu, lead):
+    """Views whose first element lies at an odd place of its buffer: a row's first and last 16
+    bytes are shared with values that are not the row's (NaN here)."""
+    from paper_2608_15665_gb300 import firstorder as fo
+    rows, cols = 2100, 250
+    base = torch.full((rows * 260 + 16,), float("nan"), dtype=torch.bfloat16, device=gpu)
+    x = torch.as_strided(base, (rows, cols), (260, 1), lead)
+    x.copy_(rows_of(rows, cols, "bf16", gpu, 9))
+    w, b = vec(cols, "bf16", gpu, 2, 1.0), vec(cols, "bf16", gpu, 3, 0.0)
+    out = fo.layer_norm(x, w, b)
+    plain = fo.layer_norm(x.contiguous(), w, b)
+    assert torch.equal(out.y, plain.y) and torch.equal(out.mean, plain.mean)
+    dy = rows_of(rows, cols, "bf16", gpu, 4)
+    got = fo.layer_norm_backward(dy, x, w, out.mean, out.rstd)
+    check_backward(*got, f64(dy), f64(x), w, f64(out.mean), f64(out.rstd), 0.0, "bf16", "bf16")
