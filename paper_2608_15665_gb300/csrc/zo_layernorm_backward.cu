@@ -1,0 +1,309 @@
+// Layer normalisation, backward pass (zo_layernorm.cuh).
+#include "zo_layernorm.cuh"
+
+namespace zo {
+namespace {
+
+using namespace ln;
+
+// --------------------------------------------------------------------------- backward
+// Rows held in registers: each thread keeps its columns' weight, dw and db over all rows
+// of its group.  kRing: the rows come through a ring, else straight from memory.
+template <typename T, typename TW, int kGroup, int kElems, int V, bool kRing>
+__global__ void __launch_bounds__(block_of(kGroup), resident_of(kGroup, kElems, true))
+backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
+  constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup, kE = kElems / V;
+  static_assert(kE > 0, "rows in registers");
+  __shared__ float buf[2][2][32];
+  __shared__ uint64_t full[kGroups][kMaxStages];
+  extern __shared__ __align__(128) uint8_t dyn[];   // the ring; then dw and db of each warp
+  const int t = threadIdx.x % kGroup, grp = threadIdx.x / kGroup;
+  const int64_t cols = a.cols;
+  const float inv_n = 1.0f / (float)cols;
+  Ring<T> ring{{static_cast<const T*>(a.x), static_cast<const T*>(a.dy), static_cast<const T*>(a.r)},
+               {a.ldx, a.lddy, a.ldr}, a.r ? 3 : 2, stages, slot, (uint32_t)(cols * sizeof(T)),
+               dyn + (size_t)grp * stages * (a.r ? 3 : 2) * slot, full[grp]};
+  if constexpr (kRing) {
+    if (t == 0) {
+      for (int s = 0; s < stages; ++s) sm100::mbar_init(&full[grp][s], 1);
+      sm100::fence_mbar_init();
+    }
+    __syncthreads();
+  }
+  pdl_wait();
+  pdl_trigger();
+  const TW* w = static_cast<const TW*>(a.weight);
+  float wv[kE][V], dw[kE][V], db[kE][V];
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const int64_t j = ((int64_t)e * kGroup + t) * V;
+#pragma unroll
+    for (int k = 0; k < V; ++k) { wv[e][k] = 1.0f; dw[e][k] = db[e][k] = 0.0f; }
+    if (w && j < cols) load<TW, V, true>(w + j, wv[e]);
+  }
+  const int64_t stride = (int64_t)gridDim.x * kGroups;
+  const int64_t row0 = (int64_t)blockIdx.x * kGroups + grp;
+  if constexpr (kRing) {
+    if (t == 0)
+      for (int s = 0; s < stages; ++s)
+        if (row0 + s * stride < a.rows) ring.fetch(row0 + s * stride, s);
+  }
+  int flip = 0;
+  float mean_next = row0 < a.rows ? a.mean[row0] : 0.0f, rstd_next = row0 < a.rows ? a.rstd[row0] : 0.0f;
+  // the groups of a warp go on together
+  const int64_t first = kGroup < 32 ? row0 - (threadIdx.x % 32) / kGroup : row0;
+  for (int64_t step = 0; first + step < a.rows; step += stride, flip ^= 1) {
+    const bool live = kGroup >= 32 || row0 + step < a.rows;
+    const int64_t row = live ? row0 + step : a.rows - 1;
+    const T* src[3] = {ring.row_of(0, row), ring.row_of(1, row), a.r ? ring.row_of(2, row) : nullptr};
+    T* dx = static_cast<T*>(a.dx) + row * a.lddx;
+    const float mean = live ? mean_next : 0.0f, rstd = live ? rstd_next : 0.0f;
+    if (row0 + step + stride < a.rows) {
+      mean_next = a.mean[row0 + step + stride];
+      rstd_next = a.rstd[row0 + step + stride];
+    }
+    if constexpr (kRing) ring.take(row, src);
+    float xh[kE][V], g[kE][V];
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const int64_t j = ((int64_t)e * kGroup + t) * V;
+      if (live && j < cols) {
+        load<T, V>(src[0] + j, xh[e]);
+        load<T, V>(src[1] + j, g[e]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) { xh[e][k] = mean; g[e][k] = 0.0f; }
+      }
+    }
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        xh[e][k] = (xh[e][k] - mean) * rstd;
+        db[e][k] += g[e][k];
+        dw[e][k] = fmaf(g[e][k], xh[e][k], dw[e][k]);
+        g[e][k] *= wv[e][k];
+        s1 += g[e][k];
+        s2 = fmaf(g[e][k], xh[e][k], s2);
+      }
+#pragma unroll
+    for (int o = (kGroup < 32 ? kGroup : 32) / 2; o > 0; o >>= 1) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if constexpr (kGroup > 32) {
+      constexpr int kWarps = kGroup / 32;
+      if ((threadIdx.x & 31) == 0) {
+        buf[flip][0][threadIdx.x >> 5] = s1;
+        buf[flip][1][threadIdx.x >> 5] = s2;
+      }
+      __syncthreads();
+      const int lane = threadIdx.x & 31;
+      s1 = warp_sum(lane < kWarps ? buf[flip][0][lane] : 0.0f);
+      s2 = warp_sum(lane < kWarps ? buf[flip][1][lane] : 0.0f);
+    }
+    s1 *= inv_n;
+    s2 *= inv_n;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const int64_t j = ((int64_t)e * kGroup + t) * V;
+      if (!live || j >= cols) continue;
+      float o[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[k] = rstd * (g[e][k] - s1 - xh[e][k] * s2);
+      if (a.r) {
+        float q[V];
+        load<T, V>(src[2] + j, q);
+#pragma unroll
+        for (int k = 0; k < V; ++k) o[k] += q[k];
+      }
+      store<T, V>(dx + j, o);
+    }
+    if constexpr (kRing) {
+      // every thread of the group has read the stage: the row `stages` ahead may have it
+      if constexpr (kGroup > 32) {
+        if (a.r) __syncthreads();               // (dr was read behind the sums' barrier)
+      } else {
+        __syncwarp();
+      }
+      if (t == 0 && row + stages * stride < a.rows) ring.fetch(row + stages * stride, ring.stage);
+      ring.advance();
+    }
+  }
+  if (a.partial == nullptr) return;
+  if constexpr (kGroups > 1) {
+    // the warps' sums meet in shared memory, added in warp order
+    float* joined = reinterpret_cast<float*>(dyn);
+    const int width = kE * kGroup * V;
+    __syncthreads();                            // the rings are no longer read
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        joined[(grp * 2 + 0) * width + (e * kGroup + t) * V + k] = dw[e][k];
+        joined[(grp * 2 + 1) * width + (e * kGroup + t) * V + k] = db[e][k];
+      }
+    __syncthreads();
+    for (int j = threadIdx.x; j < 2 * width; j += kBlock) {
+      const int which = j / width, c = j % width;
+      if (c >= cols) continue;
+      float s = 0.0f;
+      for (int q = 0; q < kGroups; ++q) s += joined[(q * 2 + which) * width + c];
+      a.partial[((int64_t)blockIdx.x * 2 + which) * cols + c] = s;
+    }
+  } else {
+    float* p = a.partial + (int64_t)blockIdx.x * 2 * cols;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const int64_t j = ((int64_t)e * kGroup + t) * V;
+      if (j >= cols) continue;
+      if constexpr (V == 1) {
+        p[j] = dw[e][0];
+        p[cols + j] = db[e][0];
+      } else {
+        store<float, V>(p + j, dw[e]);          // (V divides cols: 16-byte aligned)
+        store<float, V>(p + cols + j, db[e]);
+      }
+    }
+  }
+}
+
+// Rows wider than the registers: one CTA per row at a time, each row swept twice from
+// memory; the column sums are the next kernel's.
+template <typename T, typename TW>
+__global__ void __launch_bounds__(1024) backward_wide_kernel(const LayerNormArgs a) {
+  __shared__ float buf[2][2][32];
+  const int64_t cols = a.cols;
+  const float inv_n = 1.0f / (float)cols;
+  const TW* w = static_cast<const TW*>(a.weight);
+  int flip = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
+    const T* dr = a.r ? static_cast<const T*>(a.r) + row * a.ldr : nullptr;
+    T* dx = static_cast<T*>(a.dx) + row * a.lddx;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int64_t j = threadIdx.x; j < cols; j += 1024) {
+      const float g = Elem<T>::to(dy[j]) * (w ? Elem<TW>::to(w[j]) : 1.0f);
+      s1 += g;
+      s2 = fmaf(g, (Elem<T>::to(x[j]) - mean) * rstd, s2);
+    }
+    s1 = group_sum<1024>(s1, buf[flip][0]) * inv_n;
+    s2 = group_sum<1024>(s2, buf[flip][1]) * inv_n;
+    for (int64_t j = threadIdx.x; j < cols; j += 1024) {
+      const float g = Elem<T>::to(dy[j]) * (w ? Elem<TW>::to(w[j]) : 1.0f);
+      float o = rstd * (g - s1 - (Elem<T>::to(x[j]) - mean) * rstd * s2);
+      if (dr) o += Elem<T>::to(dr[j]);
+      dx[j] = Elem<T>::from(o);
+    }
+  }
+}
+// dw and db of the rows blockIdx.y, blockIdx.y + gridDim.y, ...: one column per thread
+template <typename T>
+__global__ void __launch_bounds__(256) wide_sums_kernel(const LayerNormArgs a) {
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= a.cols) return;
+  float dw = 0.0f, db = 0.0f;
+  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    const float dy = Elem<T>::to(static_cast<const T*>(a.dy)[row * a.lddy + j]);
+    const float x = Elem<T>::to(static_cast<const T*>(a.x)[row * a.ldx + j]);
+    db += dy;
+    dw = fmaf(dy, (x - a.mean[row]) * a.rstd[row], dw);
+  }
+  a.partial[(int64_t)blockIdx.y * 2 * a.cols + j] = dw;
+  a.partial[((int64_t)blockIdx.y * 2 + 1) * a.cols + j] = db;
+}
+
+// Adds the partial rows: 32 columns of dw or db per CTA, its 32 warps the rows w, w + 32,
+// ..., then the 32 sums in warp order.
+template <typename TW>
+__global__ void __launch_bounds__(1024) column_sums_kernel(const float* __restrict__ partial,
+                                                           int64_t n_partial, int64_t cols,
+                                                           TW* dweight, TW* dbias) {
+  __shared__ float part[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t j = (int64_t)blockIdx.x * 32 + lane;
+  const int which = blockIdx.y;
+  pdl_wait();
+  pdl_trigger();
+  float s = 0.0f;
+  if (j < cols)
+#pragma unroll 8
+    for (int64_t p = warp; p < n_partial; p += 32) s += partial[(p * 2 + which) * cols + j];
+  part[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || j >= cols) return;
+  s = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 32; ++w) s += part[w][lane];
+  TW* out = which == 0 ? dweight : dbias;
+  if (out) out[j] = Elem<TW>::from(s);
+}
+
+template <typename T, typename TW, int V>
+cudaError_t backward_v(const LayerNormArgs& a, int32_t sms, int64_t n_partial, cudaStream_t s) {
+  const Shape sh = shape_for(a.rows, a.cols, sms, true);
+  return with_shape(sh, [&](auto group, auto elems) -> cudaError_t {
+    constexpr int G = decltype(group)::value, E = decltype(elems)::value;
+    if constexpr (E == 0) {
+      backward_wide_kernel<T, TW><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, s>>>(a);
+      cudaError_t err = cudaGetLastError();
+      if (err != cudaSuccess || a.partial == nullptr) return err;
+      wide_sums_kernel<T><<<dim3((unsigned)((a.cols + 255) / 256), (unsigned)n_partial), 256, 0, s>>>(a);
+      return cudaGetLastError();
+    } else {
+      constexpr int block = block_of(G), groups = block / G;
+      size_t smem = groups > 1 ? sizeof(float) * 2 * groups * E * G : 0;
+      if constexpr (ring_of(G, E)) {
+        const uint32_t slot = ring_slot<T>(a.cols);
+        const int n = a.r ? 3 : 2, stages = ring_stages<G, E, true>(n, slot);
+        if (a.rows > groups_at_once(sh, sms, true) && stages >= 2) {
+          const auto kernel = backward_kernel<T, TW, G, E, V, true>;
+          smem = std::max(smem, (size_t)groups * stages * n * slot);
+          const cudaError_t err = cudaFuncSetAttribute(
+              kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+          if (err != cudaSuccess) return err;
+          return launch_dependent(kernel, (unsigned)n_partial, block, smem, s, 1, true, a, stages, slot);
+        }
+      }
+      return launch_dependent(backward_kernel<T, TW, G, E, V, false>, (unsigned)n_partial, block,
+                              smem, s, 1, true, a, 0, 0u);
+    }
+  });
+}
+template <typename T, typename TW>
+cudaError_t backward_t(const LayerNormArgs& a, int32_t sms, int64_t n_partial, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  const bool wide = a.cols % V == 0 && wide_rows(a.x, a.ldx, sizeof(T)) &&
+                    wide_rows(a.dy, a.lddy, sizeof(T)) && wide_rows(a.r, a.ldr, sizeof(T)) &&
+                    wide_rows(a.dx, a.lddx, sizeof(T)) && aligned(a.weight, 16);
+  cudaError_t e = cudaSuccess;
+  if (a.rows > 0)
+    e = wide ? backward_v<T, TW, V>(a, sms, n_partial, s) : backward_v<T, TW, 1>(a, sms, n_partial, s);
+  if (e != cudaSuccess || (a.dweight == nullptr && a.dbias == nullptr)) return e;
+  return launch_dependent(column_sums_kernel<TW>, dim3((unsigned)((a.cols + 31) / 32), 2), 1024, 0,
+                          s, 1, true, a.partial, a.rows > 0 ? n_partial : 0, a.cols,
+                          static_cast<TW*>(a.dweight), static_cast<TW*>(a.dbias));
+}
+
+}  // namespace
+
+int64_t layernorm_partial_rows(int64_t rows, int64_t cols, int32_t sms) {
+  const Shape sh = shape_for(rows, cols, sms, true);
+  if (sh.elems == 0) return std::min<int64_t>(rows, 2 * sms);   // slabs of the sums' own kernel
+  const int64_t at_once = block_of(sh.group) / sh.group;
+  return std::min<int64_t>((rows + at_once - 1) / at_once, (int64_t)resident_of(sh.group, sh.elems, true) * sms);
+}
+
+cudaError_t launch_layernorm_backward(const LayerNormArgs& a, int32_t sms, cudaStream_t s) {
+  const int64_t n = layernorm_partial_rows(a.rows, a.cols, sms);
+  if (a.dtype == kF32)
+    return a.wdtype == kF32 ? backward_t<float, float>(a, sms, n, s)
+                            : backward_t<float, __nv_bfloat16>(a, sms, n, s);
+  return a.wdtype == kF32 ? backward_t<__nv_bfloat16, float>(a, sms, n, s)
+                          : backward_t<__nv_bfloat16, __nv_bfloat16>(a, sms, n, s);
+}
+
+}  // namespace zo

@@ -4,8 +4,11 @@
 #include <array>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <memory>
 #include <new>
+#include <queue>
+#include <utility>
 #include <vector>
 
 #include "../../include/zo.h"
@@ -24,10 +27,13 @@ constexpr int64_t kGroupBytes = int64_t(1) << 30;
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
+// The tiles of one launch, dealt to the SM pairs: pair q's are tiles[first[q] .. first[q + 1]).
+struct TileList {
+  int32_t tile0 = 0, n = 0, pairs = 0, first0 = 0;
+};
 struct Group {
   int32_t unit0 = 0, n_units = 0;
-  // by single and by pair products: tiles on or below the diagonals (p x p), tiles of X' (p x c)
-  int32_t sym0[2] = {}, n_sym[2] = {}, apply0[2] = {}, n_apply[2] = {};
+  int32_t list[2][3] = {{-1, -1, -1}, {-1, -1, -1}};   // tile lists by [pairs][OrthoPhase]
 };
 
 // Matrices that one launch of a one-launch kernel takes: one kernel (rows: the fp32 kernel's
@@ -43,10 +49,12 @@ struct Layout {
   std::vector<zo::OrthoMat> mats;       // buffer pointers hold byte offsets until placed
   std::vector<int4> units, tiles;
   std::vector<Group> groups;
+  std::vector<TileList> lists;
+  std::vector<int32_t> first;           // kOrthoMaxPairs + 1 of every list
   std::vector<int32_t> small_list;
   int32_t n_maps = 0;                   // matrices with tensor maps
   std::vector<Small> small;
-  int64_t mats_at = 0, maps_at = 0, small_at = 0, units_at = 0, tiles_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
+  int64_t mats_at = 0, maps_at = 0, small_at = 0, units_at = 0, tiles_at = 0, first_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
   int64_t tables_end = 0;
 };
 
@@ -75,6 +83,41 @@ zo_status check_matrices(const zo_muon_matrix* mats, int32_t n_mats) {
     if (st != ZO_OK) return st;
   }
   return ZO_OK;
+}
+
+int64_t depth(const zo::OrthoMat& d, int phase) { return phase == zo::kOrthoGram ? d.c : d.p; }
+
+// Deals the tiles of every list, longest first, to n_pairs SM pairs, each to the pair with the
+// least to do so far; a pair's tiles keep their order.  A tile costs its depth in stages of 64,
+// and about six more for what the next tile's products do not hide.
+void deal_tiles(Layout& L, int32_t n_pairs) {
+  L.first.assign(L.lists.size() * (zo::kOrthoMaxPairs + 1), 0);
+  for (size_t l = 0; l < L.lists.size(); ++l) {
+    const TileList& list = L.lists[l];
+    int phase = 0;
+    for (const Group& g : L.groups)
+      for (int pr = 0; pr < 2; ++pr)
+        for (int k = 0; k < 3; ++k)
+          if (g.list[pr][k] == (int32_t)l) phase = k;
+    using Load = std::pair<int64_t, int32_t>;                // work so far, pair
+    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+    for (int32_t q = 0; q < n_pairs; ++q) least.push({0, q});
+    std::vector<std::vector<int4>> dealt(n_pairs);
+    for (int32_t t = 0; t < list.n; ++t) {
+      const int4 tile = L.tiles[list.tile0 + t];
+      Load to = least.top();
+      least.pop();
+      dealt[to.second].push_back(tile);
+      to.first += (depth(L.mats[tile.x], phase) + 63) / 64 + 6;
+      least.push(to);
+    }
+    int32_t at = list.tile0;
+    for (int32_t q = 0; q <= zo::kOrthoMaxPairs; ++q) {
+      L.first[list.first0 + q] = at - list.tile0;
+      if (q < n_pairs)
+        for (const int4& tile : dealt[q]) L.tiles[at++] = tile;
+    }
+  }
 }
 
 uint16_t* at_offset(int64_t off) { return reinterpret_cast<uint16_t*>(off); }
@@ -151,22 +194,28 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     int64_t units = 0;
     for (; next < L.mats.size() && units + L.mats[next].n_units <= g.n_units; ++next)
       units += L.mats[next].n_units;               // (a small matrix has none)
-    const auto of = [&](size_t i, int pr) { return !L.mats[i].small && L.mats[i].pairs == pr; };
-    for (int pr = 0; pr < 2; ++pr) {
-      const int cols = zo::ortho_tile_cols(pr != 0);
-      g.sym0[pr] = (int32_t)L.tiles.size();
-      for (size_t i = first; i < next; ++i)
-        for (int64_t r = 0; of(i, pr) && r < L.mats[i].p; r += zo::kOrthoTileRows)
-          for (int64_t c = 0; c < std::min(r + zo::kOrthoTileRows, L.mats[i].p); c += cols)
-            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, L.mats[i].maps));
-      g.n_sym[pr] = (int32_t)L.tiles.size() - g.sym0[pr];
-      g.apply0[pr] = (int32_t)L.tiles.size();
-      for (size_t i = first; i < next; ++i)
-        for (int64_t r = 0; of(i, pr) && r < L.mats[i].p; r += zo::kOrthoTileRows)
-          for (int64_t c = 0; c < L.mats[i].c; c += cols)
-            L.tiles.push_back(make_int4((int)i, (int)r, (int)c, L.mats[i].maps));
-      g.n_apply[pr] = (int32_t)L.tiles.size() - g.apply0[pr];
-    }
+    // X X^T and b A + c A A: tiles that meet or lie left of the diagonal's blocks of rows
+    for (int pr = 0; pr < 2; ++pr)
+      for (const int phase : {zo::kOrthoGram, zo::kOrthoPoly, zo::kOrthoApply}) {
+        TileList list{(int32_t)L.tiles.size(), 0, pr, (int32_t)(L.lists.size() * (zo::kOrthoMaxPairs + 1))};
+        for (size_t i = first; i < next; ++i) {
+          const zo::OrthoMat& d = L.mats[i];
+          if (d.small || d.pairs != pr) continue;
+          for (int64_t r = 0; r < d.p; r += zo::kOrthoTileRows) {
+            const int64_t end = phase == zo::kOrthoApply ? d.c : std::min(r + zo::kOrthoTileRows, d.p);
+            for (int64_t c = 0; c < end; c += zo::ortho_tile_cols(pr != 0))
+              L.tiles.push_back(make_int4((int)i, (int)r, (int)c, d.maps));
+          }
+        }
+        list.n = (int32_t)L.tiles.size() - list.tile0;
+        if (list.n == 0) continue;
+        // the longest products first (deal_tiles)
+        std::stable_sort(L.tiles.begin() + list.tile0, L.tiles.end(), [&](const int4& a, const int4& b) {
+          return depth(L.mats[a.x], phase) > depth(L.mats[b.x], phase);
+        });
+        g.list[pr][phase] = (int32_t)L.lists.size();
+        L.lists.push_back(list);
+      }
     if (L.tiles.size() > (size_t(1) << 28))
       return refuse(ZO_ERR_SHAPE, "zo_muon: too many tiles in one context");
   }
@@ -199,6 +248,7 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
   L.small_at = place(sizeof(int32_t) * L.small_list.size());
   L.units_at = place(sizeof(int4) * L.units.size());
   L.tiles_at = place(sizeof(int4) * L.tiles.size());
+  L.first_at = place((int64_t)sizeof(int32_t) * L.lists.size() * (zo::kOrthoMaxPairs + 1));
   L.tables_end = at;
   L.partial_at = place(sizeof(float) * slots);
   L.buffers_at = at;
@@ -309,6 +359,7 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   const auto* mats = reinterpret_cast<const zo::OrthoMat*>(c->ws + L.mats_at);
   const auto* units = reinterpret_cast<const int4*>(c->ws + L.units_at);
   const auto* tiles = reinterpret_cast<const int4*>(c->ws + L.tiles_at);
+  const auto* firsts = reinterpret_cast<const int32_t*>(c->ws + L.first_at);
   const auto* maps = reinterpret_cast<const CUtensorMap*>(c->ws + L.maps_at);
   auto* status = reinterpret_cast<uint32_t*>(c->ws);
   auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
@@ -331,11 +382,11 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
     for (const zo::OrthoStep& s : st)
       for (const zo::OrthoPhase phase : {zo::kOrthoGram, zo::kOrthoPoly, zo::kOrthoApply})
         for (int pr = 0; pr < 2; ++pr) {
-          const bool apply = phase == zo::kOrthoApply;
-          const int32_t n = apply ? g.n_apply[pr] : g.n_sym[pr];
-          if (n == 0) continue;
-          ZO_CUDA(zo::launch_ortho_product(mats, maps, tiles + (apply ? g.apply0[pr] : g.sym0[pr]), n,
-                                           pr != 0, c->n_pairs, phase, s, u, status, c->stream),
+          if (g.list[pr][phase] < 0) continue;
+          const TileList& list = L.lists[g.list[pr][phase]];
+          ZO_CUDA(zo::launch_ortho_product(mats, maps, tiles + list.tile0, firsts + list.first0,
+                                           pr != 0, std::min(list.n, c->n_pairs), phase, s, u,
+                                           status, c->stream),
                   "orthogonalisation: product kernel");
           ++c->launches;
         }
@@ -407,6 +458,8 @@ zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t 
     c->n_pairs = L.groups.empty() ? 0 : zo::ortho_max_pairs();
     if (!L.groups.empty() && c->n_pairs <= 0)
       return refuse(ZO_ERR_CUDA, "zo_muon_create: no cluster of the product kernel fits");
+    c->n_pairs = std::min(c->n_pairs, zo::kOrthoMaxPairs);
+    if (c->n_pairs > 0) deal_tiles(L, c->n_pairs);
     // one copy of the status word (0) and every table
     std::vector<uint8_t> image((size_t)L.tables_end, 0);
     std::memcpy(image.data() + L.mats_at, L.mats.data(), sizeof(zo::OrthoMat) * L.mats.size());
@@ -415,6 +468,8 @@ zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t 
     if (!L.small_list.empty())
       std::memcpy(image.data() + L.small_at, L.small_list.data(), sizeof(int32_t) * L.small_list.size());
     if (!L.units.empty()) std::memcpy(image.data() + L.units_at, L.units.data(), sizeof(int4) * L.units.size());
+    if (!L.first.empty())
+      std::memcpy(image.data() + L.first_at, L.first.data(), sizeof(int32_t) * L.first.size());
     if (!L.tiles.empty()) std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(int4) * L.tiles.size());
     ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),
             "upload tables");

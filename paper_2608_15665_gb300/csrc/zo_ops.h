@@ -93,10 +93,12 @@ cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t 
                                cudaStream_t s);
 // Clusters of the product kernels that fit on the device at once
 int32_t ortho_max_pairs();
+constexpr int kOrthoMaxPairs = 128;
+// pair q of n_pairs takes the tiles first[q] .. first[q + 1] - 1
 cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, const int4* tiles,
-                                 int32_t n_tiles, bool pairs, int32_t n_pairs, OrthoPhase phase,
-                                 const OrthoStep& st, const OrthoUpdate& u, uint32_t* status,
-                                 cudaStream_t s);
+                                 const int32_t* first, bool pairs, int32_t n_pairs,
+                                 OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
+                                 uint32_t* status, cudaStream_t s);
 
 // Matrices of at most 32 rows (zo_ortho_fma.cu: fp32, `rows` = 8, 16 or 32) and of 33 to 128
 // (zo_ortho_small.cu: tensor cores), each kind in one launch: the CTAs of a matrix's cluster

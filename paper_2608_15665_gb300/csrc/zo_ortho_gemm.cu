@@ -149,7 +149,7 @@ __device__ __forceinline__ void write_weights(T* w, int64_t step, int n, const f
 template <bool kPairs>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restrict__ maps,
-                  const int4* __restrict__ tiles, int n_tiles, const Phase ph,
+                  const int4* __restrict__ tiles, const int32_t* __restrict__ first, const Phase ph,
                   uint32_t* __restrict__ status) {
   constexpr int kCols = ortho_tile_cols(kPairs);
   constexpr int kABytes = 2 * kBlockBytes, kBBytes = kCols / 128 * kBlockBytes;   // per CTA
@@ -167,7 +167,8 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int pair = blockIdx.x >> 1;
+  const int t_begin = first[pair], t_end = first[pair + 1];
   const volatile int* abort = &sh.abort_flag;
   const int phase = ph.phase;
 
@@ -196,7 +197,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     // ---------------------------------------------------------------- operands (this CTA)
     int64_t it = 0;
     bool ok = true;
-    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+    for (int t = t_begin; t < t_end && ok; ++t) {
       const int4 tl = tiles[t];
       const int64_t steps = (depth_of(mats[tl.x], phase) + 63) / 64;
       const CUtensorMap* m = maps + (int64_t)tl.w * kOrthoMaps;
@@ -256,7 +257,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         mma_pair_ss(d, sdesc_k_sw128(a + 32 * kk), bd, idesc, fresh && kk == 0 ? 0u : 1u);
       }
     };
-    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+    for (int t = t_begin; t < t_end && ok; ++t) {
       const int64_t steps = (depth_of(mats[tiles[t].x], phase) + 63) / 64;
       const int64_t seg = kPairs ? kSeg : steps;
       for (int64_t k0 = 0; k0 < steps && ok; k0 += seg, ++n_acc) {
@@ -302,7 +303,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     uint8_t* mirror = direct + kBoxBytes;
     int64_t n_acc = 0;
     bool ok = true;
-    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+    for (int t = t_begin; t < t_end && ok; ++t) {
       const int4 tl = tiles[t];
       const OrthoMat& mt = mats[tl.x];
       const CUtensorMap* m = maps + (int64_t)tl.w * kOrthoMaps;
@@ -498,17 +499,16 @@ int32_t max_pairs() {
 int32_t ortho_max_pairs() { return std::min(max_pairs<false>(), max_pairs<true>()); }
 
 cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, const int4* tiles,
-                                 int32_t n_tiles, bool pairs, int32_t n_pairs, OrthoPhase phase,
-                                 const OrthoStep& st, const OrthoUpdate& u, uint32_t* status,
-                                 cudaStream_t s) {
-  if (n_tiles <= 0) return cudaSuccess;
+                                 const int32_t* first, bool pairs, int32_t n_pairs,
+                                 OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
+                                 uint32_t* status, cudaStream_t s) {
   if (n_pairs <= 0) return cudaErrorInvalidValue;
   const Phase ph{(int)phase, st, u};
-  const unsigned grid = 2u * (unsigned)std::min(n_tiles, n_pairs);
+  const unsigned grid = 2u * (unsigned)n_pairs;
   return pairs ? launch_dependent(ortho_gemm_kernel<true>, grid, kThreads, kSmem, s, 1, true, mats,
-                                  maps, tiles, n_tiles, ph, status)
+                                  maps, tiles, first, ph, status)
                : launch_dependent(ortho_gemm_kernel<false>, grid, kThreads, kSmem, s, 1, true, mats,
-                                  maps, tiles, n_tiles, ph, status);
+                                  maps, tiles, first, ph, status);
 }
 
 }  // namespace zo
