@@ -95,7 +95,6 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
 }
 
 struct Phase {
-  int phase;
   OrthoStep st;
   OrthoUpdate u;
 };
@@ -146,7 +145,8 @@ __device__ __forceinline__ void write_weights(T* w, int64_t step, int n, const f
   }
 }
 
-template <bool kPairs>
+// kLast: Apply of the last step, which writes W.
+template <bool kPairs, int phase, bool kLast>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restrict__ maps,
                   const int4* __restrict__ tiles, const int32_t* __restrict__ first, const Phase ph,
@@ -170,7 +170,6 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   const int pair = blockIdx.x >> 1;
   const int t_begin = first[pair], t_end = first[pair + 1];
   const volatile int* abort = &sh.abort_flag;
-  const int phase = ph.phase;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -195,11 +194,13 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 
   if (warp == 0 && lane == 0) {
     // ---------------------------------------------------------------- operands (this CTA)
-    int64_t it = 0;
+    int stage = 0;
+    uint32_t free_parity = 1;                  // of empty[stage]: the first round needs no wait
+    int64_t filled = 0;
     bool ok = true;
     for (int t = t_begin; t < t_end && ok; ++t) {
       const int4 tl = tiles[t];
-      const int64_t steps = (depth_of(mats[tl.x], phase) + 63) / 64;
+      const int steps = (int)((depth_of(mats[tl.x], phase) + 63) / 64);
       const CUtensorMap* m = maps + (int64_t)tl.w * kOrthoMaps;
       const int cur = ph.st.k & 1;
       const CUtensorMap* ah = m + (phase == kOrthoGram ? kMapX + cur
@@ -208,87 +209,127 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       const CUtensorMap* bh = m + (phase == kOrthoPoly ? kMapA : kMapX + cur);
       const CUtensorMap* bl = bh + (phase == kOrthoPoly ? 1 : 2);
       const int i0 = tl.y + 128 * (int)rank, j0 = tl.z + kCols / 2 * (int)rank;
-      for (int64_t k = 0; k < steps; ++k, ++it) {
-        const int s = (int)(it % kStages);
-        if (!mbar_wait_bounded(&sh.empty[s], (uint32_t)(((it / kStages) & 1) ^ 1), abort, kWait)) {
+      for (int k0 = 0; k0 < 64 * steps; k0 += 64) {
+        if (!mbar_wait_bounded(&sh.empty[stage], free_parity, abort, kWait)) {
           ok = false;
           break;
         }
-        if (leader) mbar_arrive_expect_tx(&sh.full[s], 2 * kStageBytes);
-        const int k0 = (int)(64 * k);
+        uint64_t* full = &sh.full[stage];
+        if (leader) mbar_arrive_expect_tx(full, 2 * kStageBytes);
         // hi parts of A and B, then the lo parts
-        uint8_t* dst = smem + s * kStageBytes;
+        uint8_t* dst = smem + stage * kStageBytes;
 #pragma unroll
         for (int part = 0; part < (kPairs ? 2 : 1); ++part) {
           const CUtensorMap* a = part ? al : ah;
           const CUtensorMap* bm = part ? bl : bh;
 #pragma unroll
           for (int q = 0; q < 2; ++q, dst += kBlockBytes)
-            tma_load_2d_to_leader(dst, a, k0, i0 + 64 * q, &sh.full[s]);
+            tma_load_2d_to_leader(dst, a, k0, i0 + 64 * q, full);
 #pragma unroll
           for (int q = 0; q < kCols / 128; ++q, dst += kBlockBytes) {
-            if (phase == kOrthoApply) tma_load_2d_to_leader(dst, bm, j0 + 64 * q, k0, &sh.full[s]);
-            else tma_load_2d_to_leader(dst, bm, k0, j0 + 64 * q, &sh.full[s]);
+            if (phase == kOrthoApply) tma_load_2d_to_leader(dst, bm, j0 + 64 * q, k0, full);
+            else tma_load_2d_to_leader(dst, bm, k0, j0 + 64 * q, full);
           }
+        }
+        ++filled;
+        if (++stage == kStages) {
+          stage = 0;
+          free_parity ^= 1u;
         }
       }
     }
     if (!ok) give_up(sh, status);
     // the leader's MMAs have released every stage this CTA filled
     for (int s = 0; s < kStages; ++s) {
-      const int64_t last = tc::last_in_slot(it, s, kStages);
+      const int64_t last = tc::last_in_slot(filled, s, kStages);
       if (last >= 0)
         mbar_wait_bounded(&sh.empty[s], (uint32_t)((last / kStages) & 1), nullptr, kWait);
     }
   } else if (warp == 1 && lane == 0 && leader) {
     // ---------------------------------------------------------------- MMA issuer (leader)
+    // One thread feeds the tensor cores of two SMs, an MMA every ~140 cycles, and every
+    // instruction between two MMAs is time they may lose: descriptors and barriers move by
+    // additions (with 64-bit remainders in this loop a stage of 64 took 715 to 906 cycles),
+    // and the next stage's barrier is looked at between this one's MMAs.
     const bool mn = phase == kOrthoApply;
     const uint32_t idesc = idesc_f16_f32(kTileRows, kCols) | (mn ? kMnMajorB : 0u);
-    int64_t it = 0, n_acc = 0;
-    bool ok = true;
-    // the four MMAs of one stage and product: hi.lo (0), lo.hi (1), hi.hi (2)
-    const auto products = [&](uint32_t d, int64_t at, int prod, bool fresh) {
-      const uint32_t base = smem_u32(smem + (int)(at % kStages) * kStageBytes);
-      const uint32_t a = base + (prod == 1 ? kABytes + kBBytes : 0);
-      const uint32_t b = base + kABytes + (prod == 0 ? kABytes + kBBytes : 0);
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        const uint64_t bd = mn ? sdesc_mn_sw128(b + 2048 * kk) : sdesc_k_sw128(b + 32 * kk);
-        mma_pair_ss(d, sdesc_k_sw128(a + 32 * kk), bd, idesc, fresh && kk == 0 ? 0u : 1u);
-      }
-    };
+    const uint32_t ring = smem_u32(smem);
+    constexpr uint64_t kStageStep = kStageBytes >> 4, kLoStep = (kABytes + kBBytes) >> 4;
+    const uint64_t a_first = sdesc_k_sw128(ring);
+    const uint64_t b_first = mn ? sdesc_mn_sw128(ring + kABytes) : sdesc_k_sw128(ring + kABytes);
+    const uint64_t b_step = (mn ? 2048 : 32) >> 4;
+    int stage = 0, acc = 0;
+    uint32_t parity = 0, acc_parity = 1;
+    bool ok = true, seen = false;              // seen: full[stage] has been found complete
     for (int t = t_begin; t < t_end && ok; ++t) {
-      const int64_t steps = (depth_of(mats[tiles[t].x], phase) + 63) / 64;
-      const int64_t seg = kPairs ? kSeg : steps;
-      for (int64_t k0 = 0; k0 < steps && ok; k0 += seg, ++n_acc) {
-        const int64_t n = min(seg, steps - k0);
-        const int acc = (int)(n_acc % kBufs);
-        const uint32_t d = tmem + (uint32_t)(acc * kCols);
-        if (!mbar_wait_bounded(&sh.acc_empty[acc], (uint32_t)(((n_acc / kBufs) & 1) ^ 1), abort,
-                               kWait)) {
+      int left = (int)((depth_of(mats[tiles[t].x], phase) + 63) / 64);
+      while (left > 0) {
+        const int n = kPairs ? min(kSeg, left) : left;
+        if (!mbar_wait_bounded(&sh.acc_empty[acc], acc_parity, abort, kWait)) {
           ok = false;
           break;
         }
-        for (int64_t k = 0; k < n; ++k) {
-          const int s = (int)((it + k) % kStages);
-          if (!mbar_wait_bounded(&sh.full[s], (uint32_t)(((it + k) / kStages) & 1), abort, kWait)) {
-            ok = false;
-            break;
+        tc_fence_after();
+        const uint32_t d = tmem + (uint32_t)(acc * kCols);
+        if constexpr (!kPairs) {
+          uint32_t add = 0;
+          for (int k = 0; k < n; ++k) {
+            if (!seen && !mbar_wait_bounded(&sh.full[stage], parity, abort, kWait)) {
+              ok = false;
+              break;
+            }
+            const uint64_t ad = a_first + (uint64_t)stage * kStageStep;
+            const uint64_t bd = b_first + (uint64_t)stage * kStageStep;
+            mma_pair_ss(d, ad, bd, idesc, add);
+            add = 1;
+            mma_pair_ss(d, ad + 2, bd + b_step, idesc, 1);
+            uint64_t* done = &sh.empty[stage];
+            if (++stage == kStages) {
+              stage = 0;
+              parity ^= 1u;
+            }
+            seen = mbar_try_wait(&sh.full[stage], parity);
+            mma_pair_ss(d, ad + 4, bd + 2 * b_step, idesc, 1);
+            mma_pair_ss(d, ad + 6, bd + 3 * b_step, idesc, 1);
+            commit_both(done);
           }
-          tc_fence_after();
-          if constexpr (!kPairs) {
-            products(d, it + k, 2, k == 0);
-            commit_both(&sh.empty[s]);
+        } else {
+          // the segment's stages, then hi.lo, lo.hi and hi.hi of them
+          int at[kSeg];
+#pragma unroll
+          for (int k = 0; k < kSeg; ++k) {
+            at[k] = stage;
+            if (k >= n || !ok) continue;
+            ok = mbar_wait_bounded(&sh.full[stage], parity, abort, kWait);
+            if (++stage == kStages) {
+              stage = 0;
+              parity ^= 1u;
+            }
+          }
+          if (ok) {
+#pragma unroll
+            for (int prod = 0; prod < 3; ++prod)
+#pragma unroll
+              for (int k = 0; k < kSeg; ++k) {
+                if (k >= n) continue;
+                const uint64_t ad = a_first + (uint64_t)at[k] * kStageStep + (prod == 1 ? kLoStep : 0);
+                const uint64_t bd = b_first + (uint64_t)at[k] * kStageStep + (prod == 0 ? kLoStep : 0);
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                  mma_pair_ss(d, ad + 2 * kk, bd + b_step * kk, idesc, (prod | k | kk) != 0 ? 1u : 0u);
+              }
+#pragma unroll
+            for (int k = 0; k < kSeg; ++k)
+              if (k < n) commit_both(&sh.empty[at[k]]);
           }
         }
         if (!ok) break;
-        if constexpr (kPairs) {
-          for (int prod = 0; prod < 3; ++prod)
-            for (int64_t k = 0; k < n; ++k) products(d, it + k, prod, prod == 0 && k == 0);
-          for (int64_t k = 0; k < n; ++k) commit_both(&sh.empty[(it + k) % kStages]);
-        }
         commit_both(&sh.acc_full[acc]);
-        it += n;
+        if (++acc == kBufs) {
+          acc = 0;
+          acc_parity ^= 1u;
+        }
+        left -= n;
       }
     }
     if (!ok) give_up(sh, status);
@@ -311,6 +352,25 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       const int64_t i0 = tl.y + 128 * (int64_t)rank + 32 * g, i = i0 + lane;
       const int64_t p = mt.p, cols = phase == kOrthoApply ? mt.c : mt.p;
       const uint32_t col0 = ((uint32_t)(32 * g) << 16) + (uint32_t)(kWarpCols * half);
+      // the matrix that is added to the product (A in Poly, X in Apply): this thread's row, 32
+      // columns of hi and lo, a chunk ahead of its use
+      const bool poly = phase == kOrthoPoly, two = !poly || kPairs;
+      const int64_t ld = poly ? mt.ldp : mt.ldx;
+      const uint16_t* own_hi = (poly ? mt.ah : mt.xh[cur]) + i * ld + tl.z + kWarpCols * half;
+      const uint16_t* own_lo = (poly ? mt.al : mt.xl[cur]) + i * ld + tl.z + kWarpCols * half;
+      uint4 own[2][4];
+      const auto fetch = [&](int q) {
+        const bool in = phase != kOrthoGram && i < p && tl.z + kWarpCols * half + 32 * q < cols;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          own[0][e] = own[1][e] = make_uint4(0, 0, 0, 0);
+          if (in) {
+            own[0][e] = *reinterpret_cast<const uint4*>(own_hi + 32 * q + 8 * e);
+            if (two) own[1][e] = *reinterpret_cast<const uint4*>(own_lo + 32 * q + 8 * e);
+          }
+        }
+      };
+      fetch(0);
       uint32_t raw[kPairs ? kChunks : 1][32];
       int acc = 0;
       if constexpr (kPairs) {
@@ -364,22 +424,13 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]) * s;
         } else {
-          // b A + c A A, or a X + B X: the matrix itself is added to the product
-          const bool poly = phase == kOrthoPoly;
-          const uint16_t* hi = (poly ? mt.ah : mt.xh[cur]) + i * (poly ? mt.ldp : mt.ldx) + j0;
-          const uint16_t* lo = (poly ? mt.al : mt.xl[cur]) + i * (poly ? mt.ldp : mt.ldx) + j0;
-          const bool two = !poly || kPairs;
           const float s0 = poly ? ph.st.b * exp2i(ph.st.eb - ph.st.ea)
-                                : ph.st.a * exp2i(ph.st.last ? -ph.st.ex : ph.st.ex_next - ph.st.ex);
+                                : ph.st.a * exp2i(kLast ? -ph.st.ex : ph.st.ex_next - ph.st.ex);
           const float s1 = poly ? ph.st.c * exp2i(ph.st.eb - 2 * ph.st.ea)
-                                : exp2i((ph.st.last ? 0 : ph.st.ex_next) - ph.st.ex - ph.st.eb);
+                                : exp2i((kLast ? 0 : ph.st.ex_next) - ph.st.ex - ph.st.eb);
 #pragma unroll
           for (int e = 0; e < 32; e += 8) {
-            uint4 h = make_uint4(0, 0, 0, 0), l = h;
-            if (i < p) {
-              h = *reinterpret_cast<const uint4*>(hi + e);
-              if (two) l = *reinterpret_cast<const uint4*>(lo + e);
-            }
+            const uint4 h = own[0][e / 8], l = own[1][e / 8];
             const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -389,7 +440,8 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             }
           }
         }
-        if (phase == kOrthoApply && ph.st.last) {
+        if (q + 1 < kChunks) fetch(q + 1);
+        if constexpr (kLast) {
           const float fm = (float)mt.m, fn = (float)mt.n;
           const float rate = ph.u.lr * (ph.u.adjust == 1 ? sqrtf(fmaxf(1.0f, fm / fn))
                                         : ph.u.adjust == 2 ? 0.2f * sqrtf(fmaxf(fm, fn)) : 1.0f);
@@ -427,11 +479,16 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             v[2 * e] -= h.x;
             v[2 * e + 1] -= h.y;
           }
-          if (lane == 0) bulk_wait_read_all();     // the boxes' last stores have read them
+          // the box's last store has read it: Apply's parts take the two boxes in turn
+          uint8_t* box = phase == kOrthoApply && part == 1 ? mirror : direct;
+          if (lane == 0) {
+            if (phase == kOrthoApply) bulk_wait_read_1();
+            else bulk_wait_read_all();
+          }
           __syncwarp();
 #pragma unroll
           for (int c = 0; c < 4; ++c)
-            *reinterpret_cast<uint4*>(direct + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) =
+            *reinterpret_cast<uint4*>(box + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) =
                 make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
           if (both) {
             // two rows' values of one column to a word: neighbouring lanes trade halves
@@ -448,7 +505,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
           fence_async_smem();
           __syncwarp();
           if (lane == 0) {
-            tma_store_2d(to + part * to_lo, (int)j0, (int)i0, direct);
+            tma_store_2d(to + part * to_lo, (int)j0, (int)i0, box);
             if (both) tma_store_2d(to + part * to_lo, (int)i0, (int)j0, mirror);
             bulk_commit();
           }
@@ -472,43 +529,55 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   }
 }
 
-template <bool kPairs>
-int32_t max_pairs() {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2, 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = kSmem;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = 2;
-  attr.val.clusterDim.y = 1;
-  attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaFuncSetAttribute(ortho_gemm_kernel<kPairs>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)kSmem) != cudaSuccess)
-    return 0;
-  int clusters = 0;
-  if (cudaOccupancyMaxActiveClusters(&clusters, ortho_gemm_kernel<kPairs>, &cfg) != cudaSuccess)
-    return 0;
-  return clusters;
+// f(kernel) with the instance of a launch
+template <typename F>
+auto with_kernel(bool pairs, int phase, bool last, F f) {
+#define ZO_PHASE(P)                                                                           \
+  phase == kOrthoGram ? f(ortho_gemm_kernel<P, kOrthoGram, false>)                            \
+  : phase == kOrthoPoly ? f(ortho_gemm_kernel<P, kOrthoPoly, false>)                          \
+  : last ? f(ortho_gemm_kernel<P, kOrthoApply, true>) : f(ortho_gemm_kernel<P, kOrthoApply, false>)
+  if (pairs) return ZO_PHASE(true);
+  return ZO_PHASE(false);
+#undef ZO_PHASE
 }
 
 }  // namespace
 
-int32_t ortho_max_pairs() { return std::min(max_pairs<false>(), max_pairs<true>()); }
+int32_t ortho_max_pairs() {
+  // (every instance has the same launch shape and shared memory)
+  return with_kernel(true, kOrthoApply, true, [](auto kernel) -> int32_t {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = kSmem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) !=
+            cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess)
+      return 0;
+    return clusters;
+  });
+}
 
 cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, const int4* tiles,
                                  const int32_t* first, bool pairs, int32_t n_pairs,
                                  OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
                                  uint32_t* status, cudaStream_t s) {
   if (n_pairs <= 0) return cudaErrorInvalidValue;
-  const Phase ph{(int)phase, st, u};
-  const unsigned grid = 2u * (unsigned)n_pairs;
-  return pairs ? launch_dependent(ortho_gemm_kernel<true>, grid, kThreads, kSmem, s, 1, true, mats,
-                                  maps, tiles, first, ph, status)
-               : launch_dependent(ortho_gemm_kernel<false>, grid, kThreads, kSmem, s, 1, true, mats,
-                                  maps, tiles, first, ph, status);
+  return with_kernel(pairs, (int)phase, st.last != 0, [&](auto kernel) -> cudaError_t {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(kernel, 2u * (unsigned)n_pairs, kThreads, kSmem, s, 1, true, mats, maps,
+                            tiles, first, Phase{st, u}, status);
+  });
 }
 
 }  // namespace zo
