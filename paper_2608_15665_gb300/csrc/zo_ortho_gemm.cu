@@ -62,6 +62,7 @@ struct Shared {
   uint64_t full[8], empty[8];
   uint64_t acc_full[4], acc_empty[4];
   uint64_t drain;                // one commit after the leader's last MMA
+  uint64_t in_full[kEpiWarps];   // an epilogue warp's boxes of A or X have arrived
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -181,6 +182,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       mbar_init(&sh.acc_empty[s], 2 * kEpiWarps);
     }
     mbar_init(&sh.drain, 1);
+    for (int w = 0; w < kEpiWarps; ++w) mbar_init(&sh.in_full[w], 1);
     sh.abort_flag = 0;
     fence_mbar_init();
   }
@@ -342,6 +344,10 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     const int half = (warp - 2) >> 2;              // half of the columns
     uint8_t* direct = out_smem + (warp - 2) * 2 * kBoxBytes;
     uint8_t* mirror = direct + kBoxBytes;
+    uint64_t* in_full = &sh.in_full[warp - 2];
+    constexpr bool kTwo = phase == kOrthoApply || kPairs;
+    uint32_t in_parity = 0;
+    bool pending = false;                          // lane 0: boxes requested and not yet taken
     int64_t n_acc = 0;
     bool ok = true;
     for (int t = t_begin; t < t_end && ok; ++t) {
@@ -352,25 +358,22 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       const int64_t i0 = tl.y + 128 * (int64_t)rank + 32 * g, i = i0 + lane;
       const int64_t p = mt.p, cols = phase == kOrthoApply ? mt.c : mt.p;
       const uint32_t col0 = ((uint32_t)(32 * g) << 16) + (uint32_t)(kWarpCols * half);
-      // the matrix that is added to the product (A in Poly, X in Apply): this thread's row, 32
-      // columns of hi and lo, a chunk ahead of its use
-      const bool poly = phase == kOrthoPoly, two = !poly || kPairs;
-      const int64_t ld = poly ? mt.ldp : mt.ldx;
-      const uint16_t* own_hi = (poly ? mt.ah : mt.xh[cur]) + i * ld + tl.z + kWarpCols * half;
-      const uint16_t* own_lo = (poly ? mt.al : mt.xl[cur]) + i * ld + tl.z + kWarpCols * half;
-      uint4 own[2][4];
-      const auto fetch = [&](int q) {
-        const bool in = phase != kOrthoGram && i < p && tl.z + kWarpCols * half + 32 * q < cols;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          own[0][e] = own[1][e] = make_uint4(0, 0, 0, 0);
-          if (in) {
-            own[0][e] = *reinterpret_cast<const uint4*>(own_hi + 32 * q + 8 * e);
-            if (two) own[1][e] = *reinterpret_cast<const uint4*>(own_lo + 32 * q + 8 * e);
-          }
-        }
+      const auto outside = [&](int q) {            // the same in every lane
+        return i0 >= p || tl.z + kWarpCols * half + 32 * q >= cols;
       };
-      fetch(0);
+      // lane 0: what is added to the product (A in Poly, X in Apply), 32 x 32 of hi and of lo,
+      // into the warp's boxes once their last stores have read them
+      const auto request = [&](int q) {
+        if (phase == kOrthoGram || outside(q)) return;
+        const CUtensorMap* from = m + (phase == kOrthoPoly ? kMapStoreA : kMapStoreX + cur);
+        const int j = tl.z + kWarpCols * half + 32 * q;
+        bulk_wait_read_all();
+        pending = true;
+        mbar_arrive_expect_tx(in_full, (kTwo ? 2 : 1) * kBoxBytes);
+        tma_load_2d(direct, from, j, (int)i0, in_full);
+        if (kTwo) tma_load_2d(mirror, from + (phase == kOrthoPoly ? 1 : 2), j, (int)i0, in_full);
+      };
+      if (lane == 0) request(0);
       uint32_t raw[kPairs ? kChunks : 1][32];
       int acc = 0;
       if constexpr (kPairs) {
@@ -412,7 +415,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 #pragma unroll
       for (int q = 0; q < kChunks; ++q) {
         const int64_t j0 = tl.z + kWarpCols * half + 32 * q;
-        if (i0 >= p || j0 >= cols) continue;       // the same in every lane
+        if (outside(q)) continue;
         if constexpr (!kPairs) {
           tmem_ld_32x32b_x32(tmem + col0 + (uint32_t)(acc * kCols + 32 * q), raw[0]);
           tmem_ld_wait();
@@ -424,23 +427,30 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]) * s;
         } else {
-          const float s0 = poly ? ph.st.b * exp2i(ph.st.eb - ph.st.ea)
-                                : ph.st.a * exp2i(kLast ? -ph.st.ex : ph.st.ex_next - ph.st.ex);
-          const float s1 = poly ? ph.st.c * exp2i(ph.st.eb - 2 * ph.st.ea)
-                                : exp2i((kLast ? 0 : ph.st.ex_next) - ph.st.ex - ph.st.eb);
+          if (!mbar_wait_bounded(in_full, in_parity, abort, kWait)) ok = false;
+          in_parity ^= 1u;
+          pending = false;
+          constexpr bool kPoly = phase == kOrthoPoly;
+          const float s0 = kPoly ? ph.st.b * exp2i(ph.st.eb - ph.st.ea)
+                                 : ph.st.a * exp2i(kLast ? -ph.st.ex : ph.st.ex_next - ph.st.ex);
+          const float s1 = kPoly ? ph.st.c * exp2i(ph.st.eb - 2 * ph.st.ea)
+                                 : exp2i((kLast ? 0 : ph.st.ex_next) - ph.st.ex - ph.st.eb);
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            const uint4 h = own[0][e / 8], l = own[1][e / 8];
+          for (int c = 0; c < 4; ++c) {
+            const int at = lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4);
+            const uint4 h = *reinterpret_cast<const uint4*>(direct + at);
+            const uint4 l = kTwo ? *reinterpret_cast<const uint4*>(mirror + at) : make_uint4(0, 0, 0, 0);
             const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
               const float2 x = unpack2(hw[w]), y = unpack2(lw[w]);
-              v[e + 2 * w] = fmaf(s0, x.x + y.x, s1 * __uint_as_float(sum[e + 2 * w]));
-              v[e + 2 * w + 1] = fmaf(s0, x.y + y.y, s1 * __uint_as_float(sum[e + 2 * w + 1]));
+              const int e = 8 * c + 2 * w;
+              v[e] = fmaf(s0, x.x + y.x, s1 * __uint_as_float(sum[e]));
+              v[e + 1] = fmaf(s0, x.y + y.y, s1 * __uint_as_float(sum[e + 1]));
             }
           }
+          __syncwarp();                            // every lane has read the boxes
         }
-        if (q + 1 < kChunks) fetch(q + 1);
         if constexpr (kLast) {
           const float fm = (float)mt.m, fn = (float)mt.n;
           const float rate = ph.u.lr * (ph.u.adjust == 1 ? sqrtf(fmaxf(1.0f, fm / fn))
@@ -460,6 +470,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             if (wide) write_weights<float, true>(w, step, n, v, ph.u, rate);
             else write_weights<float, false>(w, step, n, v, ph.u, rate);
           }
+          if (lane == 0 && q + 1 < kChunks) request(q + 1);
           __syncwarp();
           continue;
         }
@@ -479,13 +490,12 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             v[2 * e] -= h.x;
             v[2 * e + 1] -= h.y;
           }
-          // the box's last store has read it: Apply's parts take the two boxes in turn
+          // the box's last store has read it: Apply's parts take the boxes that held X's
           uint8_t* box = phase == kOrthoApply && part == 1 ? mirror : direct;
-          if (lane == 0) {
-            if (phase == kOrthoApply) bulk_wait_read_1();
-            else bulk_wait_read_all();
+          if (phase != kOrthoApply) {
+            if (lane == 0) bulk_wait_read_all();
+            __syncwarp();
           }
-          __syncwarp();
 #pragma unroll
           for (int c = 0; c < 4; ++c)
             *reinterpret_cast<uint4*>(box + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) =
@@ -510,6 +520,8 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             bulk_commit();
           }
         }
+        if (lane == 0 && q + 1 < kChunks) request(q + 1);
+        __syncwarp();
       }
       if constexpr (!kPairs) {
         tc_fence_before();
@@ -518,6 +530,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       }
     }
     if (!ok && lane == 0) give_up(sh, status);
+    if (lane == 0 && pending) mbar_wait_bounded(in_full, in_parity, nullptr, kWait);
     if (lane == 0) bulk_wait_all();
   }
 
