@@ -36,8 +36,8 @@ struct Group {
   int32_t list[2][3] = {{-1, -1, -1}, {-1, -1, -1}};   // tile lists by [pairs][OrthoPhase]
 };
 
-// Matrices that one launch of a one-launch kernel takes: one kernel (rows: the fp32 kernel's
-// instance, 0 the tensor cores'), one cluster size, and shared memories within a factor of two
+// Matrices that one launch of a one-launch kernel takes: one kernel (rows: zo_ortho_mma.cu's
+// instance, 0 zo_ortho_small.cu's), one cluster size, and shared memories within a factor of two
 // (they decide how many CTAs share an SM).
 struct Small {
   int32_t rows = 0, cluster = 0, smem = 0, least = 0, first = 0, n = 0;
@@ -142,7 +142,7 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     d.tall = m.m > m.n;
     d.pairs = zo::ortho_pairs(d.bf16, d.p);
     d.wide_rows = aligned16(m.W) && m.ldw * (d.bf16 ? 2 : 4) % 16 == 0;
-    d.small = zo::ortho_fma_cluster(d.p, d.c);
+    d.small = zo::ortho_mma_cluster(d.p, d.c);
     if (d.small == 0) d.small = zo::ortho_small_cluster(d.p, d.c);
     if (d.small > 0) {
       L.mats.push_back(d);
@@ -224,8 +224,8 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
   for (size_t i = 0; i < L.mats.size(); ++i) {
     const zo::OrthoMat& d = L.mats[i];
     if (d.small == 0) continue;
-    const int32_t rows = zo::ortho_fma_rows(d.p);
-    order.push_back({rows, d.small, rows ? zo::ortho_fma_smem(d.p, d.c, d.small)
+    const int32_t rows = zo::ortho_mma_rows(d.p);
+    order.push_back({rows, d.small, rows ? zo::ortho_mma_smem(d.p, d.c, d.small)
                                          : zo::ortho_small_smem(d.p, d.c, d.small), (int32_t)i});
   }
   std::sort(order.begin(), order.end());
@@ -365,7 +365,7 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
   const auto* which = reinterpret_cast<const int32_t*>(c->ws + L.small_at);
   for (const Small& g : L.small) {
-    ZO_CUDA(g.rows ? zo::launch_ortho_fma(mats, which + g.first, g.n, g.rows, g.cluster, g.smem,
+    ZO_CUDA(g.rows ? zo::launch_ortho_mma(mats, which + g.first, g.n, g.rows, g.cluster, g.smem,
                                           st.data(), (int32_t)st.size(), u, c->stream)
                    : zo::launch_ortho_small(mats, which + g.first, g.n, g.cluster, g.smem,
                                             st.data(), (int32_t)st.size(), u, status, c->stream),

@@ -100,15 +100,15 @@ cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, 
                                  OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
                                  uint32_t* status, cudaStream_t s);
 
-// Matrices of at most 32 rows (zo_ortho_fma.cu: fp32, `rows` = 8, 16 or 32) and of 33 to 128
-// (zo_ortho_small.cu: tensor cores), each kind in one launch: the CTAs of a matrix's cluster
+// Matrices of at most 64 rows (zo_ortho_mma.cu, `rows` = 16, 32 or 64) and of 65 to 128
+// (zo_ortho_small.cu), each kind in one launch: the CTAs of a matrix's cluster
 // (0: not one of these, or too wide), and a CTA's shared memory.  A launch takes the matrices
 // mats[which[0 .. n)], all of one cluster size (and rows), and the largest of their shared
 // memories.
-int32_t ortho_fma_rows(int64_t p);
-int32_t ortho_fma_cluster(int64_t p, int64_t c);
-int32_t ortho_fma_smem(int64_t p, int64_t c, int32_t cluster);
-cudaError_t launch_ortho_fma(const OrthoMat* mats, const int* which, int32_t n, int32_t rows,
+int32_t ortho_mma_rows(int64_t p);
+int32_t ortho_mma_cluster(int64_t p, int64_t c);
+int32_t ortho_mma_smem(int64_t p, int64_t c, int32_t cluster);
+cudaError_t launch_ortho_mma(const OrthoMat* mats, const int* which, int32_t n, int32_t rows,
                              int32_t cluster, int32_t smem, const OrthoStep* steps,
                              int32_t n_steps, const OrthoUpdate& u, cudaStream_t s);
 int32_t ortho_small_cluster(int64_t p, int64_t c);

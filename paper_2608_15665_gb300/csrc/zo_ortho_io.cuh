@@ -1,4 +1,4 @@
-// What the one-launch orthogonalisation kernels (zo_ortho_fma.cu, zo_ortho_small.cu) share: a
+// What the one-launch orthogonalisation kernels (zo_ortho_mma.cu, zo_ortho_small.cu) share: a
 // CTA's walk over its columns of the caller's matrices, and a cluster's sum of one value.
 #pragma once
 

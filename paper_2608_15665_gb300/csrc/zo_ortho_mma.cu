@@ -1,0 +1,431 @@
+// Newton-Schulz orthogonalisation of matrices of at most 64 rows in one launch: momentum, norm,
+// every step and the update of W, with X in shared memory throughout.
+//
+// A matrix is a cluster of C CTAs, each with its share of X's columns as a hi and a lo plane of
+// fp16 values of x 2^e.  A step:
+//   Gram   the CTA's X X^T: 16 rows of the result per warp, K dealt to the warps that are left;
+//          their fp32 sums are added up in warp order, then over the cluster in rank order (every
+//          CTA reads all the partial sums through distributed shared memory, so one cluster
+//          barrier a step is enough);
+//   Poly   B = b A + c A A, by every CTA for itself;
+//   Apply  X' = a X + B X in place: a warp takes all rows of eight or sixteen columns.
+// Products are hi.lo + lo.hi + hi.hi with fp32 sums, by warp-wide m16n8k16 MMAs on registers:
+// at these sizes a step is a chain of short latencies, and the round trip of a tcgen05.mma
+// (issue, commit, wait, Tensor Memory to registers: ~2.5 K cycles a product at 64 x 64, against
+// ~1 K here) would be most of it; from 65 rows on the larger MMAs win (zo_ortho_small.cu).
+// Between load and scaling, and between the last step and the update of W, the planes hold the
+// upper and lower halves of fp32 values, so that the caller's matrices are read and written
+// once, in their own order.
+#include <algorithm>
+
+#include <cuda_fp16.h>
+
+#include "zo_launch.cuh"
+#include "zo_ops.h"
+#include "zo_ortho_io.cuh"
+#include "zo_sm100.cuh"
+#include "zo_tc_common.cuh"
+
+namespace zo {
+namespace {
+
+using namespace ortho;
+using sm100::smem_u32;
+using tc::exp2i;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kSmemMax = 227 * 1024 - 1024;
+
+__host__ __device__ constexpr int mma_rows(int64_t p) { return p <= 16 ? 16 : p <= 32 ? 32 : 64; }
+// columns of a CTA, a multiple of 16, and the planes' row pitch in halves: 16 bytes past a
+// multiple of 128, so that eight rows' 16 bytes lie in different banks
+__host__ __device__ inline int mma_cols(int64_t c, int cluster) {
+  return (int)(((c + cluster - 1) / cluster + 15) / 16 * 16);
+}
+__host__ __device__ constexpr int pitch_of(int cs) { return (cs + 63) / 64 * 64 + 8; }
+
+template <int P>
+struct Shape {
+  static constexpr int kM = P / 16;                    // tiles of 16 rows
+  static constexpr int kSplits = P == 16 ? 8 : P == 32 ? 4 : 1;   // of Gram's K
+  static constexpr int kN = P == 64 ? P / 16 : P / 8;  // Gram: tiles of 8 columns per warp
+  static constexpr int kPitch = P + 8;                 // of A, B (halves) and of sums (floats)
+  static constexpr int kSumFloats = P * kPitch;
+  static_assert(kM * kSplits * (P / 8 / kN) == kWarps, "a Gram task per warp");
+  static __host__ __device__ int smem(int cs, int cluster) {
+    return 2 * 2 * P * pitch_of(cs) + 4 * 2 * P * kPitch +
+           4 * (kSplits + (cluster > 1 ? 2 : 0)) * kSumFloats;
+  }
+};
+
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+// D += A B, m16n8k16, fp16 operands, fp32 sums
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float2 pair2(const __half* hi, const __half* lo) {
+  const float2 h = __half22float2(*reinterpret_cast<const __half2*>(hi));
+  const float2 l = __half22float2(*reinterpret_cast<const __half2*>(lo));
+  return make_float2(h.x + l.x, h.y + l.y);
+}
+__device__ __forceinline__ void split2(float a, float b, __half* hi, __half* lo) {
+  const __half2 h = __floats2half2_rn(a, b);
+  const float2 f = __half22float2(h);
+  *reinterpret_cast<__half2*>(hi) = h;
+  *reinterpret_cast<__half2*>(lo) = __floats2half2_rn(a - f.x, b - f.y);
+}
+// the upper and lower halves of fp32 values in the two planes
+__device__ __forceinline__ uint32_t upper2(float a, float b) {
+  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+}
+__device__ __forceinline__ uint32_t lower2(float a, float b) {
+  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
+}
+__device__ __forceinline__ float first_of(uint32_t up, uint32_t low) {
+  return __uint_as_float(__byte_perm(low, up, 0x5410));
+}
+__device__ __forceinline__ float second_of(uint32_t up, uint32_t low) {
+  return __uint_as_float(__byte_perm(low, up, 0x7632));
+}
+
+struct Steps {
+  OrthoStep s[kOrthoMaxSteps];
+  int n;
+};
+
+// X' = a X + B X in kNb x 8 columns from j0 on, by one warp: X's columns are in registers
+// before any of them is written.
+template <int P, int kNb>
+__device__ __forceinline__ void apply(__half* xh, __half* xl, const __half* bh, const __half* bl,
+                                      int pitch, int j0, float s0, float s1, bool last) {
+  constexpr int kK = P / 16, kBp = Shape<P>::kPitch;
+  const int lane = threadIdx.x & 31;
+  uint32_t x[2][kK][4];                                // hi, lo; 16 rows x 16 columns each
+#pragma unroll
+  for (int k = 0; k < kK; ++k) {
+    // matrices: rows 16 k + 0..7 and + 8..15 of columns j0.. and j0 + 8..
+    const int at = (16 * k + (lane & 15)) * pitch + j0 + (kNb == 2 ? (lane >> 4) * 8 : 0);
+    ldmatrix_x4_trans(x[0][k], smem_u32(xh + at));
+    ldmatrix_x4_trans(x[1][k], smem_u32(xl + at));
+  }
+  __syncwarp();
+#pragma unroll
+  for (int m = 0; m < kK; ++m) {
+    float d[kNb][4] = {};
+#pragma unroll
+    for (int k = 0; k < kK; ++k) {
+      uint32_t b[2][4];
+      const int at = (16 * m + (lane & 15)) * kBp + 16 * k + (lane >> 4) * 8;
+      ldmatrix_x4(b[0], smem_u32(bh + at));
+      ldmatrix_x4(b[1], smem_u32(bl + at));
+#pragma unroll
+      for (int n = 0; n < kNb; ++n) {
+        mma(d[n], b[0], x[1][k][2 * n], x[1][k][2 * n + 1]);
+        mma(d[n], b[1], x[0][k][2 * n], x[0][k][2 * n + 1]);
+        mma(d[n], b[0], x[0][k][2 * n], x[0][k][2 * n + 1]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kNb; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = (16 * m + (lane >> 2) + 8 * h) * pitch + j0 + 8 * n + (lane & 3) * 2;
+        const float2 v = pair2(xh + at, xl + at);
+        const float a = fmaf(s0, v.x, s1 * d[n][2 * h]), b = fmaf(s0, v.y, s1 * d[n][2 * h + 1]);
+        if (last) {
+          *reinterpret_cast<uint32_t*>(xh + at) = upper2(a, b);
+          *reinterpret_cast<uint32_t*>(xl + at) = lower2(a, b);
+        } else {
+          split2(a, b, xh + at, xl + at);
+        }
+      }
+  }
+}
+
+template <int P>
+__global__ void __launch_bounds__(kThreads)
+ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ which, int cluster,
+                 const __grid_constant__ Steps steps, const OrthoUpdate u) {
+  using S = Shape<P>;
+  constexpr int kPitch = S::kPitch;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ SumShared sums;
+  const OrthoMat mt = mats[which[blockIdx.x / cluster]];
+  const int rank = (int)(blockIdx.x % cluster);
+  const int cs = mma_cols(mt.c, cluster), pitch = pitch_of(cs);
+  __half* xh = reinterpret_cast<__half*>(smem);
+  __half* xl = xh + P * pitch;
+  __half* ah = xl + P * pitch;
+  __half* al = ah + P * kPitch;
+  __half* bh = al + P * kPitch;
+  __half* bl = bh + P * kPitch;
+  float* part = reinterpret_cast<float*>(bl + P * kPitch);
+  float* red = part + S::kSplits * S::kSumFloats;      // two of them, for a cluster's sums
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int64_t c0 = (int64_t)rank * cs;
+  const int cols = (int)max((int64_t)0, min((int64_t)cs, mt.c - c0));
+
+  // both planes: the padding rows and columns stay zero
+  for (int e = tid; e < 2 * P * pitch / 8; e += kThreads)
+    reinterpret_cast<uint4*>(xh)[e] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+
+  // ---------------------------------------------------------------- U, scaled by its norm
+  const auto put = [&](int i, int j, float v) {
+    reinterpret_cast<uint16_t*>(xh)[i * pitch + j] = (uint16_t)(__float_as_uint(v) >> 16);
+    reinterpret_cast<uint16_t*>(xl)[i * pitch + j] = (uint16_t)__float_as_uint(v);
+  };
+  const auto get = [&](int i, int j) {
+    return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(xh)[i * pitch + j] << 16 |
+                           reinterpret_cast<const uint16_t*>(xl)[i * pitch + j]);
+  };
+  const int64_t n = mt.tall ? mt.p : cols;
+  float sq;
+  if (by_fours(mt.G, mt.ldg, mt.grad_bf16, n) &&
+      (mt.M == nullptr || !u.step || by_fours(mt.M, mt.n, 0, n))) {
+    sq = load_update<kThreads, 4>(mt, u, c0, cols, [&](int i, int j, const float (&v)[4]) {
+      if (mt.tall) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put(i + e, j, v[e]);
+      } else {
+        *reinterpret_cast<uint2*>(xh + i * pitch + j) = make_uint2(upper2(v[0], v[1]), upper2(v[2], v[3]));
+        *reinterpret_cast<uint2*>(xl + i * pitch + j) = make_uint2(lower2(v[0], v[1]), lower2(v[2], v[3]));
+      }
+    });
+  } else {
+    sq = load_update<kThreads, 1>(mt, u, c0, cols,
+                                  [&](int i, int j, const float (&v)[1]) { put(i, j, v[0]); });
+  }
+  const float inv = inverse_norm<kThreads>(sq, u.eps, cluster, sums);
+  const float s_in = exp2i(steps.s[0].ex);
+  for (int e = tid; e < P * pitch / 8; e += kThreads) {
+    uint4* ph = reinterpret_cast<uint4*>(xh) + e;
+    uint4* pl = reinterpret_cast<uint4*>(xl) + e;
+    const uint4 h = *ph, l = *pl;
+    const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = first_of(hw[k], lw[k]) * inv;
+      v[2 * k + 1] = second_of(hw[k], lw[k]) * inv;
+    }
+    tc::split8_f16(v, s_in, *ph, *pl);
+  }
+  __syncthreads();
+
+  // ---------------------------------------------------------------- the steps
+  const int row = lane >> 2, col = (lane & 3) * 2;     // of a sum's first two values
+  for (int k = 0; k < steps.n; ++k) {
+    const OrthoStep st = steps.s[k];
+    {
+      // ---- X X^T: rows 16 m, columns 8 (kN n0 ..), K tiles split, split + kSplits, ...
+      const int m = warp % S::kM, split = warp / S::kM % S::kSplits, n0 = warp / (S::kM * S::kSplits) * S::kN;
+      float d[S::kN][4] = {};
+      for (int kt = split; kt < cs / 16; kt += S::kSplits) {
+        uint32_t a[2][4];
+        const int at = (16 * m + (lane & 15)) * pitch + 16 * kt + (lane >> 4) * 8;
+        ldmatrix_x4(a[0], smem_u32(xh + at));
+        ldmatrix_x4(a[1], smem_u32(xl + at));
+#pragma unroll
+        for (int q = 0; q < S::kN; q += 2) {           // two tiles of 8 columns: 16 rows of X
+          uint32_t b[2][4];
+          const int bt = (8 * (n0 + q) + (lane & 15)) * pitch + 16 * kt + (lane >> 4) * 8;
+          ldmatrix_x4(b[0], smem_u32(xh + bt));
+          ldmatrix_x4(b[1], smem_u32(xl + bt));
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            mma(d[q + h], a[0], b[1][h], b[1][h + 2]);
+            mma(d[q + h], a[1], b[0][h], b[0][h + 2]);
+            mma(d[q + h], a[0], b[0][h], b[0][h + 2]);
+          }
+        }
+      }
+      float* to = part + split * S::kSumFloats;
+#pragma unroll
+      for (int q = 0; q < S::kN; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<float2*>(to + (16 * m + row + 8 * h) * kPitch + 8 * (n0 + q) + col) =
+              make_float2(d[q][2 * h], d[q][2 * h + 1]);
+    }
+    __syncthreads();
+    // the partial sums alternate between two buffers: those of the step before the last have
+    // been read by every CTA once the last step's barrier is passed
+    float* mine = red + (k & 1) * S::kSumFloats;
+    const float sa = exp2i(st.ea - 2 * st.ex);
+    const auto summed = [&](int at) {
+      float4 s = *reinterpret_cast<const float4*>(part + at);
+#pragma unroll
+      for (int w = 1; w < S::kSplits; ++w) {
+        const float4 q = *reinterpret_cast<const float4*>(part + w * S::kSumFloats + at);
+        s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+      }
+      return s;
+    };
+    const auto write_a = [&](int at, float4 s) {
+      split2(s.x * sa, s.y * sa, ah + at, al + at);
+      split2(s.z * sa, s.w * sa, ah + at + 2, al + at + 2);
+    };
+    if (cluster > 1) {
+      for (int e = tid; e < P * P / 4; e += kThreads) {
+        const int at = e / (P / 4) * kPitch + e % (P / 4) * 4;
+        *reinterpret_cast<float4*>(mine + at) = summed(at);
+      }
+      cta2::cluster_sync_all();
+      for (int e = tid; e < P * P / 4; e += kThreads) {
+        const int at = e / (P / 4) * kPitch + e % (P / 4) * 4;
+        float4 v[kMaxCluster];
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r)
+          if (r < cluster)
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(v[r].x), "=f"(v[r].y), "=f"(v[r].z), "=f"(v[r].w)
+                         : "r"(cta2::map_to(mine + at, (uint32_t)r)) : "memory");
+        float4 s = v[0];
+#pragma unroll
+        for (int r = 1; r < kMaxCluster; ++r)
+          if (r < cluster) {
+            s.x += v[r].x; s.y += v[r].y; s.z += v[r].z; s.w += v[r].w;
+          }
+        write_a(at, s);
+      }
+    } else {
+      for (int e = tid; e < P * P / 4; e += kThreads) {
+        const int at = e / (P / 4) * kPitch + e % (P / 4) * 4;
+        write_a(at, summed(at));
+      }
+    }
+    __syncthreads();
+    {
+      // ---- B = b A + c A A: rows 16 m, two tiles of 8 columns at a time
+      const float s0 = st.b * exp2i(st.eb - st.ea), s1 = st.c * exp2i(st.eb - 2 * st.ea);
+      for (int task = warp; task < S::kM * S::kM; task += kWarps) {
+        const int m = task % S::kM, q = task / S::kM;
+        float d[2][4] = {};
+#pragma unroll
+        for (int kt = 0; kt < S::kM; ++kt) {
+          uint32_t a[2][4], b[2][4];
+          const int at = (16 * m + (lane & 15)) * kPitch + 16 * kt + (lane >> 4) * 8;
+          const int bt = (16 * q + (lane & 15)) * kPitch + 16 * kt + (lane >> 4) * 8;
+          ldmatrix_x4(a[0], smem_u32(ah + at));
+          ldmatrix_x4(a[1], smem_u32(al + at));
+          ldmatrix_x4(b[0], smem_u32(ah + bt));
+          ldmatrix_x4(b[1], smem_u32(al + bt));
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            mma(d[h], a[0], b[1][h], b[1][h + 2]);
+            mma(d[h], a[1], b[0][h], b[0][h + 2]);
+            mma(d[h], a[0], b[0][h], b[0][h + 2]);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int at = (16 * m + row + 8 * h) * kPitch + 16 * q + 8 * t + col;
+            const float2 v = pair2(ah + at, al + at);
+            split2(fmaf(s0, v.x, s1 * d[t][2 * h]), fmaf(s0, v.y, s1 * d[t][2 * h + 1]), bh + at, bl + at);
+          }
+      }
+    }
+    __syncthreads();
+    {
+      // ---- X' = a X + B X: sixteen columns a warp, or eight where that leaves warps idle
+      const float s0 = st.a * exp2i(st.last ? -st.ex : st.ex_next - st.ex);
+      const float s1 = exp2i((st.last ? 0 : st.ex_next) - st.ex - st.eb);
+      if (cs <= 8 * kWarps) {
+        if (8 * warp < cs) apply<P, 1>(xh, xl, bh, bl, pitch, 8 * warp, s0, s1, st.last != 0);
+      } else {
+        for (int j = 16 * warp; j < cs; j += 16 * kWarps)
+          apply<P, 2>(xh, xl, bh, bl, pitch, j, s0, s1, st.last != 0);
+      }
+    }
+    __syncthreads();
+  }
+
+  // ---------------------------------------------------------------- the result
+  if (by_fours(mt.W, mt.ldw, mt.bf16, n)) {
+    store_result<kThreads, 4>(mt, u, c0, cols, [&](int i, int j, float (&v)[4]) {
+      if (mt.tall) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = get(i + e, j);
+      } else {
+        const uint2 h = *reinterpret_cast<const uint2*>(xh + i * pitch + j);
+        const uint2 l = *reinterpret_cast<const uint2*>(xl + i * pitch + j);
+        v[0] = first_of(h.x, l.x);
+        v[1] = second_of(h.x, l.x);
+        v[2] = first_of(h.y, l.y);
+        v[3] = second_of(h.y, l.y);
+      }
+    });
+  } else {
+    store_result<kThreads, 1>(mt, u, c0, cols, [&](int i, int j, float (&v)[1]) { v[0] = get(i, j); });
+  }
+  if (cluster > 1) cta2::cluster_sync_all();     // the peers have read this CTA's sums
+}
+
+int smem_of(int P, int cs, int cluster) {
+  return P == 16 ? Shape<16>::smem(cs, cluster)
+         : P == 32 ? Shape<32>::smem(cs, cluster) : Shape<64>::smem(cs, cluster);
+}
+
+template <int P>
+cudaError_t launch(const OrthoMat* mats, const int* which, int32_t n, int32_t cluster, int32_t smem,
+                   const Steps& st, const OrthoUpdate& u, cudaStream_t s) {
+  const cudaError_t e = cudaFuncSetAttribute(
+      ortho_mma_kernel<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(ortho_mma_kernel<P>, (unsigned)n * (unsigned)cluster, kThreads,
+                          (size_t)smem, s, (unsigned)cluster, true, mats, which, cluster, st, u);
+}
+
+}  // namespace
+
+int32_t ortho_mma_rows(int64_t p) { return p <= 64 ? mma_rows(p) : 0; }
+int32_t ortho_mma_cluster(int64_t p, int64_t c) {
+  if (p > 64) return 0;
+  const int P = mma_rows(p);
+  for (int cl = 1; cl <= kMaxCluster; cl *= 2) {
+    if (c > (int64_t)cl << 16) continue;
+    const int cs = mma_cols(c, cl);
+    // a CTA takes 10240 elements while the cluster can still grow
+    if (cl < kMaxCluster && P * cs > 10240) continue;
+    if (smem_of(P, cs, cl) <= kSmemMax) return cl;
+  }
+  return 0;
+}
+int32_t ortho_mma_smem(int64_t p, int64_t c, int32_t cluster) {
+  return smem_of(mma_rows(p), mma_cols(c, cluster), cluster);
+}
+
+cudaError_t launch_ortho_mma(const OrthoMat* mats, const int* which, int32_t n, int32_t rows,
+                             int32_t cluster, int32_t smem, const OrthoStep* steps,
+                             int32_t n_steps, const OrthoUpdate& u, cudaStream_t s) {
+  if (n <= 0) return cudaSuccess;
+  if (n_steps > kOrthoMaxSteps || smem > kSmemMax) return cudaErrorInvalidValue;
+  Steps st{};
+  st.n = n_steps;
+  std::copy(steps, steps + n_steps, st.s);
+  switch (rows) {
+    case 16: return launch<16>(mats, which, n, cluster, smem, st, u, s);
+    case 32: return launch<32>(mats, which, n, cluster, smem, st, u, s);
+    case 64: return launch<64>(mats, which, n, cluster, smem, st, u, s);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace zo

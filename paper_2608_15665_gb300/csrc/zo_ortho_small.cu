@@ -1,6 +1,6 @@
-// Newton-Schulz orthogonalisation of matrices of 33 to 128 rows in one launch: momentum, norm,
-// every step and the update of W, with X in shared memory throughout.  (At most 32 rows:
-// zo_ortho_fma.cu.)
+// Newton-Schulz orthogonalisation of matrices of 65 to 128 rows in one launch: momentum, norm,
+// every step and the update of W, with X in shared memory throughout.  (At most 64 rows:
+// zo_ortho_mma.cu.)
 //
 // A matrix is a cluster of C CTAs, each with X's columns [rank cs, rank cs + cs).  A step:
 //   Gram   each CTA's X X^T on its columns, summed over the cluster through distributed
@@ -423,7 +423,7 @@ cudaError_t launch(const OrthoMat* mats, const int* which, int32_t n, int32_t cl
 }  // namespace
 
 int32_t ortho_small_cluster(int64_t p, int64_t c) {
-  if (p <= 32 || p > 128) return 0;
+  if (p <= 64 || p > 128) return 0;
   for (int cl = 1; cl <= kMaxCluster; cl *= 2) {
     // a CTA's columns: at most 256 where the cluster can still grow
     if (cl < kMaxCluster && c > 256 * (int64_t)cl) continue;
