@@ -106,44 +106,63 @@ struct Steps {
 };
 
 // X' = a X + B X in kNb x 8 columns from j0 on, by one warp: X's columns are in registers
-// before any of them is written.
+// before any of them is written, and the sums of all rows and columns run side by side (an MMA
+// waits for the one before it on the same sums).
 template <int P, int kNb>
 __device__ __forceinline__ void apply(__half* xh, __half* xl, const __half* bh, const __half* bl,
                                       int pitch, int j0, float s0, float s1, bool last) {
-  constexpr int kK = P / 16, kBp = Shape<P>::kPitch;
+  constexpr int kK = P / 16, kBp = Shape<P>::kPitch, kX = (kNb + 1) / 2;
   const int lane = threadIdx.x & 31;
-  uint32_t x[2][kK][4];                                // hi, lo; 16 rows x 16 columns each
+  uint32_t x[2][kK][kX][4];                            // hi, lo; 16 rows x 16 columns each
 #pragma unroll
-  for (int k = 0; k < kK; ++k) {
-    // matrices: rows 16 k + 0..7 and + 8..15 of columns j0.. and j0 + 8..
-    const int at = (16 * k + (lane & 15)) * pitch + j0 + (kNb == 2 ? (lane >> 4) * 8 : 0);
-    ldmatrix_x4_trans(x[0][k], smem_u32(xh + at));
-    ldmatrix_x4_trans(x[1][k], smem_u32(xl + at));
-  }
-  __syncwarp();
+  for (int k = 0; k < kK; ++k)
 #pragma unroll
-  for (int m = 0; m < kK; ++m) {
-    float d[kNb][4] = {};
+    for (int q = 0; q < kX; ++q) {
+      // matrices: rows 16 k + 0..7 and + 8..15 of columns j.. and (kNb > 1) j + 8..
+      const int at = (16 * k + (lane & 15)) * pitch + j0 + 16 * q + (kNb > 1 ? (lane >> 4) * 8 : 0);
+      ldmatrix_x4_trans(x[0][k][q], smem_u32(xh + at));
+      ldmatrix_x4_trans(x[1][k][q], smem_u32(xl + at));
+    }
+  const int own = (lane >> 2) * pitch + j0 + (lane & 3) * 2;     // of a sum's first two values
+  float2 v[kK][kNb][2];
 #pragma unroll
-    for (int k = 0; k < kK; ++k) {
+  for (int m = 0; m < kK; ++m)
+#pragma unroll
+    for (int n = 0; n < kNb; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = own + (16 * m + 8 * h) * pitch + 8 * n;
+        v[m][n][h] = pair2(xh + at, xl + at);
+      }
+  float d[kK][kNb][4] = {};
+#pragma unroll
+  for (int k = 0; k < kK; ++k)
+#pragma unroll
+    for (int m = 0; m < kK; ++m) {
       uint32_t b[2][4];
       const int at = (16 * m + (lane & 15)) * kBp + 16 * k + (lane >> 4) * 8;
       ldmatrix_x4(b[0], smem_u32(bh + at));
       ldmatrix_x4(b[1], smem_u32(bl + at));
 #pragma unroll
-      for (int n = 0; n < kNb; ++n) {
-        mma(d[n], b[0], x[1][k][2 * n], x[1][k][2 * n + 1]);
-        mma(d[n], b[1], x[0][k][2 * n], x[0][k][2 * n + 1]);
-        mma(d[n], b[0], x[0][k][2 * n], x[0][k][2 * n + 1]);
-      }
+      for (int n = 0; n < kNb; ++n)
+        mma(d[m][n], b[0], x[1][k][n / 2][n % 2 * 2], x[1][k][n / 2][n % 2 * 2 + 1]);
+#pragma unroll
+      for (int n = 0; n < kNb; ++n)
+        mma(d[m][n], b[1], x[0][k][n / 2][n % 2 * 2], x[0][k][n / 2][n % 2 * 2 + 1]);
+#pragma unroll
+      for (int n = 0; n < kNb; ++n)
+        mma(d[m][n], b[0], x[0][k][n / 2][n % 2 * 2], x[0][k][n / 2][n % 2 * 2 + 1]);
     }
+  __syncwarp();
+#pragma unroll
+  for (int m = 0; m < kK; ++m)
 #pragma unroll
     for (int n = 0; n < kNb; ++n)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int at = (16 * m + (lane >> 2) + 8 * h) * pitch + j0 + 8 * n + (lane & 3) * 2;
-        const float2 v = pair2(xh + at, xl + at);
-        const float a = fmaf(s0, v.x, s1 * d[n][2 * h]), b = fmaf(s0, v.y, s1 * d[n][2 * h + 1]);
+        const int at = own + (16 * m + 8 * h) * pitch + 8 * n;
+        const float a = fmaf(s0, v[m][n][h].x, s1 * d[m][n][2 * h]);
+        const float b = fmaf(s0, v[m][n][h].y, s1 * d[m][n][2 * h + 1]);
         if (last) {
           *reinterpret_cast<uint32_t*>(xh + at) = upper2(a, b);
           *reinterpret_cast<uint32_t*>(xl + at) = lower2(a, b);
@@ -151,11 +170,10 @@ __device__ __forceinline__ void apply(__half* xh, __half* xl, const __half* bh, 
           split2(a, b, xh + at, xl + at);
         }
       }
-  }
 }
 
 template <int P>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, P == 16 ? 3 : 2)
 ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ which, int cluster,
                  const __grid_constant__ Steps steps, const OrthoUpdate u) {
   using S = Shape<P>;
@@ -311,47 +329,63 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
     }
     __syncthreads();
     {
-      // ---- B = b A + c A A: rows 16 m, two tiles of 8 columns at a time
+      // ---- B = b A + c A A: rows 16 m, kQ x 16 columns from 16 q on
+      constexpr int kQ = P == 64 ? 2 : 1;
       const float s0 = st.b * exp2i(st.eb - st.ea), s1 = st.c * exp2i(st.eb - 2 * st.ea);
-      for (int task = warp; task < S::kM * S::kM; task += kWarps) {
-        const int m = task % S::kM, q = task / S::kM;
-        float d[2][4] = {};
+      if (warp < S::kM * S::kM / kQ) {
+        const int m = warp % S::kM, q = warp / S::kM * kQ;
+        float2 v[2 * kQ][2];
 #pragma unroll
-        for (int kt = 0; kt < S::kM; ++kt) {
-          uint32_t a[2][4], b[2][4];
-          const int at = (16 * m + (lane & 15)) * kPitch + 16 * kt + (lane >> 4) * 8;
-          const int bt = (16 * q + (lane & 15)) * kPitch + 16 * kt + (lane >> 4) * 8;
-          ldmatrix_x4(a[0], smem_u32(ah + at));
-          ldmatrix_x4(a[1], smem_u32(al + at));
-          ldmatrix_x4(b[0], smem_u32(ah + bt));
-          ldmatrix_x4(b[1], smem_u32(al + bt));
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            mma(d[h], a[0], b[1][h], b[1][h + 2]);
-            mma(d[h], a[1], b[0][h], b[0][h + 2]);
-            mma(d[h], a[0], b[0][h], b[0][h + 2]);
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2 * kQ; ++t)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int at = (16 * m + row + 8 * h) * kPitch + 16 * q + 8 * t + col;
-            const float2 v = pair2(ah + at, al + at);
-            split2(fmaf(s0, v.x, s1 * d[t][2 * h]), fmaf(s0, v.y, s1 * d[t][2 * h + 1]), bh + at, bl + at);
+            v[t][h] = pair2(ah + at, al + at);
+          }
+        float d[2 * kQ][4] = {};
+#pragma unroll
+        for (int kt = 0; kt < S::kM; ++kt) {
+          uint32_t a[2][4], b[kQ][2][4];
+          const int at = (16 * m + (lane & 15)) * kPitch + 16 * kt + (lane >> 4) * 8;
+          ldmatrix_x4(a[0], smem_u32(ah + at));
+          ldmatrix_x4(a[1], smem_u32(al + at));
+#pragma unroll
+          for (int t = 0; t < kQ; ++t) {
+            const int bt = (16 * (q + t) + (lane & 15)) * kPitch + 16 * kt + (lane >> 4) * 8;
+            ldmatrix_x4(b[t][0], smem_u32(ah + bt));
+            ldmatrix_x4(b[t][1], smem_u32(al + bt));
+          }
+#pragma unroll
+          for (int h = 0; h < 2 * kQ; ++h) mma(d[h], a[0], b[h / 2][1][h % 2], b[h / 2][1][h % 2 + 2]);
+#pragma unroll
+          for (int h = 0; h < 2 * kQ; ++h) mma(d[h], a[1], b[h / 2][0][h % 2], b[h / 2][0][h % 2 + 2]);
+#pragma unroll
+          for (int h = 0; h < 2 * kQ; ++h) mma(d[h], a[0], b[h / 2][0][h % 2], b[h / 2][0][h % 2 + 2]);
+        }
+#pragma unroll
+        for (int t = 0; t < 2 * kQ; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int at = (16 * m + row + 8 * h) * kPitch + 16 * q + 8 * t + col;
+            split2(fmaf(s0, v[t][h].x, s1 * d[t][2 * h]), fmaf(s0, v[t][h].y, s1 * d[t][2 * h + 1]),
+                   bh + at, bl + at);
           }
       }
     }
     __syncthreads();
     {
-      // ---- X' = a X + B X: sixteen columns a warp, or eight where that leaves warps idle
+      // ---- X' = a X + B X: as many columns a warp as its registers hold, or eight where that
+      // leaves warps idle (at 64 rows B's tiles are most of what is read: sixteen at least)
+      constexpr int kNb = P == 64 ? 2 : 4;
       const float s0 = st.a * exp2i(st.last ? -st.ex : st.ex_next - st.ex);
       const float s1 = exp2i((st.last ? 0 : st.ex_next) - st.ex - st.eb);
-      if (cs <= 8 * kWarps) {
-        if (8 * warp < cs) apply<P, 1>(xh, xl, bh, bl, pitch, 8 * warp, s0, s1, st.last != 0);
+      const bool last = st.last != 0;
+      if (P < 64 && cs <= 8 * kWarps) {
+        if (8 * warp < cs) apply<P, 1>(xh, xl, bh, bl, pitch, 8 * warp, s0, s1, last);
       } else {
-        for (int j = 16 * warp; j < cs; j += 16 * kWarps)
-          apply<P, 2>(xh, xl, bh, bl, pitch, j, s0, s1, st.last != 0);
+        // (a multiple of 16 columns is left over at most, inside the row's padding)
+        for (int j = 8 * kNb * warp; j < cs; j += 8 * kNb * kWarps)
+          apply<P, kNb>(xh, xl, bh, bl, pitch, j, s0, s1, last);
       }
     }
     __syncthreads();
