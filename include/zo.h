@@ -87,7 +87,8 @@ enum {
 /* Optimizer applied in the subspace by zo_step. */
 enum {
   ZO_OPT_ADAM = 0,        /* subspace Adam, Eqs. (7)-(10) */
-  ZO_OPT_SGD = 1          /* SubZero's subspace SGD (Sec. 3): D = Zbar, moments untouched */
+  ZO_OPT_SGD = 1,         /* SubZero's subspace SGD (Sec. 3): D = Zbar, moments untouched */
+  ZO_OPT_MUON = 2         /* subspace Muon: the orthogonalised first moment, D = NS(M) */
 };
 
 /* Options for zo_set_option. */
@@ -219,6 +220,9 @@ ZO_API zo_status zo_perturb(zo_ctx* ctx, uint32_t t, int32_t qa, float ca, int32
  *     bias corrections 1 - beta^adam_t (Eq. (9), adam_t >= 1 counts Adam updates
  *     since the moments were zeroed), D_i = Mhat / (sqrt(Vhat) + eps_adam);
  *   ZO_OPT_SGD: D_i = G_i (moments untouched; adam_t, betas ignored);
+ *   ZO_OPT_MUON: M_i <- beta1 M_i + (1 - beta1) G_i (Eq. (7)), D_i = NS(M_i), the five
+ *     Newton-Schulz steps of zo_orthogonalize with eps = eps_adam, so that U_i D_i V_i^T
+ *     orthogonalises U_i M_i V_i^T (Vm_i untouched; adam_t, beta2 ignored);
  *   W_i <- rnd(W_i + U_i (-lr D_i + restore_coef * eps * Z_i^(restore_query)) V_i^T)
  *     (Eq. (10) plus the restore; restore_query = -1 drops the restore term).
  * losses: n_losses fp32 values (2q central, q+1 forward, q direct); device memory

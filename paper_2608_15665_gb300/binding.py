@@ -32,6 +32,7 @@ ZO_SCHEME_DIRECT = 2
 
 ZO_OPT_ADAM = 0
 ZO_OPT_SGD = 1
+ZO_OPT_MUON = 2
 
 ZO_MUON_ADJUST_NONE = 0
 ZO_MUON_ADJUST_ASPECT = 1

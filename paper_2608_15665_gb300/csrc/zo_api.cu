@@ -14,6 +14,7 @@
 #include "../../include/zo.h"
 #include "zo_host.h"
 #include "zo_kernels.h"
+#include "zo_ops.h"
 
 namespace {
 
@@ -83,6 +84,9 @@ struct zo_ctx {
   int32_t n_short = 0;
   int32_t n_small[4] = {0, 0, 0, 0};
   std::vector<int64_t> up_off, up_cnt, down_off, down_cnt;   // per level, into d_qr_blocks
+  // the moments as matrices to orthogonalise (ZO_OPT_MUON): M_i -> C_i
+  zo::OrthoMat* d_moments = nullptr;
+  int32_t* d_moment_list = nullptr;      // 0 .. n_mats - 1
   uint32_t* d_status = nullptr;
   int path_option = 0;
   int last_path = 0;
@@ -168,6 +172,8 @@ void free_ctx(zo_ctx* c) {
   cudaFree(c->d_cq_chunks);
   cudaFree(c->d_cq_partial);
   cudaFree(c->d_cq_linv);
+  cudaFree(c->d_moments);
+  cudaFree(c->d_moment_list);
   cudaFree(c->d_status);
   cudaFree(c->d_u_op);
   cudaFree(c->d_p_hl);
@@ -702,6 +708,8 @@ zo_status zo_create(zo_ctx** out, const zo_matrix* mats, int32_t n_mats, int32_t
   if (e == cudaSuccess) e = cudaMalloc(&c->d_proj_units, sizeof(int2) * std::max<size_t>(units.size(), 1));
   if (e == cudaSuccess) e = cudaMalloc(&c->d_qr_blocks, sizeof(zo::QrBlock) * std::max<size_t>(all_blocks.size(), 1));
   if (e == cudaSuccess) e = cudaMalloc(&c->d_status, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMalloc(&c->d_moments, sizeof(zo::OrthoMat) * n_mats);
+  if (e == cudaSuccess) e = cudaMalloc(&c->d_moment_list, sizeof(int32_t) * n_mats);
   if (e == cudaSuccess && !small_panels.empty())
     e = cudaMalloc(&c->d_small, sizeof(zo::CqPanel) * small_panels.size());
   if (e == cudaSuccess && c->n_cq_panels > 0) {
@@ -716,7 +724,20 @@ zo_status zo_create(zo_ctx** out, const zo_matrix* mats, int32_t n_mats, int32_t
     cuda_fail(e, "cudaMalloc(context tables)");
     return fail(ZO_ERR_NOMEM);
   }
-  e = cudaMemcpy(c->d_mats, c->h_mats.data(), sizeof(zo::MatDesc) * n_mats, cudaMemcpyHostToDevice);
+  std::vector<zo::OrthoMat> moments(n_mats);
+  std::vector<int32_t> moment_list(n_mats);
+  for (int32_t i = 0; i < n_mats; ++i) {
+    zo::OrthoMat& d = moments[i];
+    d.G = mats[i].M;
+    d.W = c->h_mats[i].C;
+    d.ldg = d.ldw = d.m = d.n = d.p = d.c = r;
+    moment_list[i] = i;
+  }
+  e = cudaMemcpy(c->d_moments, moments.data(), sizeof(zo::OrthoMat) * n_mats, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess)
+    e = cudaMemcpy(c->d_moment_list, moment_list.data(), sizeof(int32_t) * n_mats, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess)
+    e = cudaMemcpy(c->d_mats, c->h_mats.data(), sizeof(zo::MatDesc) * n_mats, cudaMemcpyHostToDevice);
   if (e == cudaSuccess)
     e = cudaMemcpy(c->d_tile_prefix, prefix.data(), sizeof(int64_t) * (n_mats + 1), cudaMemcpyHostToDevice);
   if (e == cudaSuccess)
@@ -891,7 +912,7 @@ zo_status zo_step(zo_ctx* c, uint32_t t, int32_t adam_t, const float* losses, in
     g_last_error = "zo_step: unknown scheme or wrong number of losses";
     return ZO_ERR_INVALID_ARG;
   }
-  if (optimizer != ZO_OPT_ADAM && optimizer != ZO_OPT_SGD) {
+  if (optimizer != ZO_OPT_ADAM && optimizer != ZO_OPT_SGD && optimizer != ZO_OPT_MUON) {
     g_last_error = "zo_step: unknown optimizer";
     return ZO_ERR_INVALID_ARG;
   }
@@ -909,6 +930,11 @@ zo_status zo_step(zo_ctx* c, uint32_t t, int32_t adam_t, const float* losses, in
     }
     inv_bc1 = 1.0 / (1.0 - std::pow((double)beta1, (double)adam_t));
     inv_bc2 = 1.0 / (1.0 - std::pow((double)beta2, (double)adam_t));
+  }
+  if (optimizer == ZO_OPT_MUON && (!(beta1 >= 0.0f && beta1 < 1.0f) || !(eps_adam >= 0.0f) ||
+                                   !std::isfinite(eps_adam))) {
+    g_last_error = "zo_step: need beta1 in [0, 1) and a finite eps_adam >= 0";
+    return ZO_ERR_INVALID_ARG;
   }
   if (tc_refused(c)) return refuse_tc(c);
   const float* d_losses = losses;
@@ -938,6 +964,25 @@ zo_status zo_step(zo_ctx* c, uint32_t t, int32_t adam_t, const float* losses, in
   p.restore_query = restore_query;
   p.restore_coef = restore_coef;
   p.gamma_out = gamma_out;
+  if (optimizer == ZO_OPT_MUON) {
+    // the moments, their directions D_i = NS(M_i) in C_i's place, then C_i from them
+    ZO_CUDA(zo::launch_coeff(c->d_mats, c->n_mats, p, /*dependent=*/true, c->stream), "coefficient kernel");
+    zo::OrthoStep steps[zo::kOrthoMaxSteps];
+    constexpr int32_t kSteps = 5;
+    if (!zo::plan_ortho_steps(kSteps, nullptr, steps)) return ZO_ERR_INVALID_ARG;
+    zo::OrthoUpdate u{};
+    u.eps = eps_adam;
+    const int32_t r = c->r, rows = zo::ortho_mma_rows(r);
+    ZO_CUDA(rows ? zo::launch_ortho_mma(c->d_moments, c->d_moment_list, c->n_mats, rows, 1,
+                                        zo::ortho_mma_smem(r, r, 1), steps, kSteps, u, c->stream)
+                 : zo::launch_ortho_small(c->d_moments, c->d_moment_list, c->n_mats, 1,
+                                          zo::ortho_small_smem(r, r, 1), steps, kSteps, u,
+                                          c->d_status, c->stream),
+            "orthogonalisation of the moments");
+    c->launches += 2;
+    p.mode = zo::kCoeffFromDirection;
+    p.gamma_out = nullptr;
+  }
   if (tc_path(c)) {
     p.c_hl = c->d_c_hl;
     p.pinv = c->d_pinv;

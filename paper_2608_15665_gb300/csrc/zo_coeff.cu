@@ -9,6 +9,8 @@
 //            Adam: M <- b1 M + (1-b1) G, Vm <- b2 Vm + (1-b2) G.G  (Eqs. (7), (8))
 //                  D = (M / (1-b1^t)) / (sqrt(Vm / (1-b2^t)) + eps_adam)  (Eqs. (9), (10))
 //            SGD:  D = G                                              (Sec. 3)
+//            Muon: M <- b1 M + (1-b1) G, nothing else: D = NS(M) is another kernel's, after
+//                  which mode kCoeffFromDirection takes D from C_i
 //            C_i = -lr D + restore_coef eps Z_i^(restore_query)
 // P_i = C_i V_i^T (r x n) then feeds the weight pass.  For the tensor-core path the kernel
 // also writes C_i as the projection's operand, rows [hi | lo] of the fp16 pair of
@@ -21,6 +23,7 @@
 #include "zo_cluster.cuh"
 #include "zo_kernels.h"
 #include "zo_launch.cuh"
+#include "zo_ops.h"
 #include "zo_tc_common.cuh"
 
 namespace zo {
@@ -112,10 +115,31 @@ coeff_kernel(const MatDesc* __restrict__ mats, const CoeffParams p) {
         d.y = (m.y * p.inv_bc1) / (sqrtf(v.y * p.inv_bc2) + p.eps_adam);
         d.z = (m.z * p.inv_bc1) / (sqrtf(v.z * p.inv_bc2) + p.eps_adam);
         d.w = (m.w * p.inv_bc1) / (sqrtf(v.w * p.inv_bc2) + p.eps_adam);
-      } else {
+      } else if (p.optimizer == 1) {
         d = g;
+      } else {
+        float4* M4 = reinterpret_cast<float4*>(md.M);
+        const float4 m = M4[c];
+        const float b1 = p.beta1, a1 = 1.0f - b1;
+        d = make_float4(b1 * m.x + a1 * g.x, b1 * m.y + a1 * g.y, b1 * m.z + a1 * g.z,
+                        b1 * m.w + a1 * g.w);
+        M4[c] = d;
       }
       out[it] = f4_scale(-p.lr, d);
+      if (p.restore_query >= 0) {
+        const float4 z = normal4(p.seed, (uint32_t)c, md.gidx, p.t,
+                                 query_word(kTagZ, (uint32_t)p.restore_query));
+        out[it] = f4_axpy(p.restore_coef * p.eps, z, out[it]);
+      }
+    }
+  }
+
+  if (p.mode == kCoeffFromDirection) {
+#pragma unroll
+    for (int it = 0; it < kCoeffIters; ++it) {
+      if (tid + it * kCoeffThreads >= per) break;
+      const int c = c0 + tid + it * kCoeffThreads;
+      out[it] = f4_scale(-p.lr, reinterpret_cast<const float4*>(md.C)[c]);
       if (p.restore_query >= 0) {
         const float4 z = normal4(p.seed, (uint32_t)c, md.gidx, p.t,
                                  query_word(kTagZ, (uint32_t)p.restore_query));

@@ -310,35 +310,36 @@ int32_t exponent_for(double bound) {
   return 15 - e;
 }
 
-// Steps with the exponents of their iterates.
-zo_status plan_steps(int32_t steps, const float* coeffs, std::vector<zo::OrthoStep>* out) {
-  if (steps < 1 || steps > zo::kOrthoMaxSteps)
-    return refuse(ZO_ERR_INVALID_ARG, "zo_muon: need 1 <= steps <= 32");
+}  // namespace
+
+bool zo::plan_ortho_steps(int32_t steps, const float* coeffs, OrthoStep* out) {
+  const auto refused = [](const char* why) {
+    set_last_error(why);
+    return false;
+  };
+  if (steps < 1 || steps > kOrthoMaxSteps) return refused("zo_muon: need 1 <= steps <= 32");
   double u = 1.0;
   for (int32_t k = 0; k < steps; ++k) {
-    zo::OrthoStep s{};
+    OrthoStep s{};
     s.a = coeffs ? coeffs[3 * k] : (float)kMuonA;
     s.b = coeffs ? coeffs[3 * k + 1] : (float)kMuonB;
     s.c = coeffs ? coeffs[3 * k + 2] : (float)kMuonC;
     if (!std::isfinite(s.a) || !std::isfinite(s.b) || !std::isfinite(s.c))
-      return refuse(ZO_ERR_INVALID_ARG, "zo_muon: a coefficient is not finite");
+      return refused("zo_muon: a coefficient is not finite");
     const double poly = most_of_poly(s.b, s.c, u), next = most_of_step(s.a, s.b, s.c, u);
     if (!(u * u < 4096.0) || !(poly < 4096.0) || !(next < 4096.0))
-      return refuse(ZO_ERR_INVALID_ARG,
-                    "zo_muon: with these coefficients the singular values can pass 2^12");
+      return refused("zo_muon: with these coefficients the singular values can pass 2^12");
     s.ex = exponent_for(u);
     s.ea = exponent_for(u * u);
     s.eb = exponent_for(poly);
     s.ex_next = exponent_for(next);
     s.k = k;
     s.last = k + 1 == steps;
-    out->push_back(s);
+    out[k] = s;
     u = next;
   }
-  return ZO_OK;
+  return true;
 }
-
-}  // namespace
 
 struct zo_muon_ctx {
   int device = 0;
@@ -352,9 +353,8 @@ struct zo_muon_ctx {
 namespace {
 
 zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const float* coeffs) {
-  std::vector<zo::OrthoStep> st;
-  const zo_status ok = plan_steps(steps, coeffs, &st);
-  if (ok != ZO_OK) return ok;
+  zo::OrthoStep st[zo::kOrthoMaxSteps];
+  if (!zo::plan_ortho_steps(steps, coeffs, st)) return ZO_ERR_INVALID_ARG;
   const Layout& L = c->plan;
   const auto* mats = reinterpret_cast<const zo::OrthoMat*>(c->ws + L.mats_at);
   const auto* units = reinterpret_cast<const int4*>(c->ws + L.units_at);
@@ -366,9 +366,9 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   const auto* which = reinterpret_cast<const int32_t*>(c->ws + L.small_at);
   for (const Small& g : L.small) {
     ZO_CUDA(g.rows ? zo::launch_ortho_mma(mats, which + g.first, g.n, g.rows, g.cluster, g.smem,
-                                          st.data(), (int32_t)st.size(), u, c->stream)
+                                          st, steps, u, c->stream)
                    : zo::launch_ortho_small(mats, which + g.first, g.n, g.cluster, g.smem,
-                                            st.data(), (int32_t)st.size(), u, status, c->stream),
+                                            st, steps, u, status, c->stream),
             "orthogonalisation: one-launch kernel");
     ++c->launches;
   }
@@ -379,13 +379,13 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
                                    c->stream),
             "orthogonalisation: scaling kernel");
     c->launches += 2;
-    for (const zo::OrthoStep& s : st)
+    for (int32_t k = 0; k < steps; ++k)
       for (const zo::OrthoPhase phase : {zo::kOrthoGram, zo::kOrthoPoly, zo::kOrthoApply})
         for (int pr = 0; pr < 2; ++pr) {
           if (g.list[pr][phase] < 0) continue;
           const TileList& list = L.lists[g.list[pr][phase]];
           ZO_CUDA(zo::launch_ortho_product(mats, maps, tiles + list.tile0, firsts + list.first0,
-                                           pr != 0, std::min(list.n, c->n_pairs), phase, s, u,
+                                           pr != 0, std::min(list.n, c->n_pairs), phase, st[k], u,
                                            status, c->stream),
                   "orthogonalisation: product kernel");
           ++c->launches;

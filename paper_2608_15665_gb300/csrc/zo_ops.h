@@ -73,6 +73,15 @@ struct OrthoStep {
   int32_t last;                     // the result goes to W instead of X_(k+1)
 };
 constexpr int kOrthoMaxSteps = 32;
+// The steps of a call with the exponents of their iterates (zo_muon.cu); coeffs: 3 per step, or
+// null for the quintic.  False, with zo_last_error set: steps out of range, or coefficients
+// under which the iterates can leave the range they are held in.
+bool plan_ortho_steps(int32_t steps, const float* coeffs, OrthoStep* out);
+
+// A mode of the coefficient kernel beside CoeffMode: C_i holds D_i, and becomes
+// -lr D_i + restore_coef eps Z_i^(restore_query).
+constexpr int32_t kCoeffFromDirection = 2;
+
 struct OrthoUpdate {
   float momentum;
   int32_t step;                     // 0: U = G, W <- NS(U); 1: the Muon update
