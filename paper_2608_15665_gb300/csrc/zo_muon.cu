@@ -54,7 +54,7 @@ struct Layout {
   std::vector<int32_t> small_list;
   int32_t n_maps = 0;                   // matrices with tensor maps
   std::vector<Small> small;
-  int64_t mats_at = 0, maps_at = 0, small_at = 0, units_at = 0, tiles_at = 0, first_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
+  int64_t mats_at = 0, maps_at = 0, small_at = 0, units_at = 0, tiles_at = 0, first_at = 0, counter_at = 0, inverse_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
   int64_t tables_end = 0;
 };
 
@@ -249,7 +249,9 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
   L.units_at = place(sizeof(int4) * L.units.size());
   L.tiles_at = place(sizeof(int4) * L.tiles.size());
   L.first_at = place((int64_t)sizeof(int32_t) * L.lists.size() * (zo::kOrthoMaxPairs + 1));
+  L.counter_at = place(sizeof(uint32_t) * L.mats.size());       // zeros, uploaded too
   L.tables_end = at;
+  L.inverse_at = place(sizeof(float) * L.mats.size());
   L.partial_at = place(sizeof(float) * slots);
   L.buffers_at = at;
   L.bytes = at + most;
@@ -363,6 +365,8 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   const auto* maps = reinterpret_cast<const CUtensorMap*>(c->ws + L.maps_at);
   auto* status = reinterpret_cast<uint32_t*>(c->ws);
   auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
+  auto* counter = reinterpret_cast<uint32_t*>(c->ws + L.counter_at);
+  auto* inverse = reinterpret_cast<float*>(c->ws + L.inverse_at);
   const auto* which = reinterpret_cast<const int32_t*>(c->ws + L.small_at);
   for (const Small& g : L.small) {
     ZO_CUDA(g.rows ? zo::launch_ortho_mma(mats, which + g.first, g.n, g.rows, g.cluster, g.smem,
@@ -373,9 +377,10 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
     ++c->launches;
   }
   for (const Group& g : L.groups) {
-    ZO_CUDA(zo::launch_ortho_momentum(mats, units + g.unit0, g.n_units, u, partial, c->stream),
+    ZO_CUDA(zo::launch_ortho_momentum(mats, units + g.unit0, g.n_units, u, partial, counter,
+                                      inverse, c->stream),
             "orthogonalisation: momentum kernel");
-    ZO_CUDA(zo::launch_ortho_scale(mats, units + g.unit0, g.n_units, u, st[0].ex, partial,
+    ZO_CUDA(zo::launch_ortho_scale(mats, units + g.unit0, g.n_units, u, st[0].ex, inverse,
                                    c->stream),
             "orthogonalisation: scaling kernel");
     c->launches += 2;

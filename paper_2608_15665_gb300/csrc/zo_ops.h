@@ -51,7 +51,7 @@ struct OrthoMat {
   uint16_t *ah, *al, *bh, *bl;      // A and B = b A + c A A (lo parts only with pairs)
 };
 // kOrthoUnitRows x kOrthoUnitCols elements of U: (matrix, first row, first column, slot)
-constexpr int kOrthoUnitRows = 64, kOrthoUnitCols = 256;
+constexpr int kOrthoUnitRows = 32, kOrthoUnitCols = 256;
 // A tile of a product: (matrix, first row, first column, index of its tensor maps)
 constexpr int kOrthoTileRows = 256;
 __host__ __device__ constexpr int ortho_tile_cols(bool pairs) { return pairs ? 128 : 256; }
@@ -95,10 +95,12 @@ struct OrthoUpdate {
 // single factors, rounding the result 1.7e-3), and their time is latency, not products.
 inline bool ortho_pairs(bool bf16, int64_t p) { return !bf16 || p <= 128; }
 
+// partial: a float per unit; counter (zero before the first call) and inverse: one per matrix
 cudaError_t launch_ortho_momentum(const OrthoMat* mats, const int4* units, int32_t n_units,
-                                  const OrthoUpdate& u, float* partial, cudaStream_t s);
+                                  const OrthoUpdate& u, float* partial, uint32_t* counter,
+                                  float* inverse, cudaStream_t s);
 cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t n_units,
-                               const OrthoUpdate& u, int32_t ex, const float* partial,
+                               const OrthoUpdate& u, int32_t ex, const float* inverse,
                                cudaStream_t s);
 // Clusters of the product kernels that fit on the device at once
 int32_t ortho_max_pairs();

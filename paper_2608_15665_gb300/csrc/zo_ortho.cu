@@ -4,13 +4,20 @@
 // Iterates are held as fp16 values of x 2^e: every entry of X_k, A and B is bounded by its
 // spectral norm, which the host follows through the steps, so e puts the bound just below
 // fp16's 65504 and 2^-29 of it is still a normal number.
+//
+// Bound by HBM: the first kernel reads G and M and writes M, the second, which needs the norm,
+// reads both again and writes X's hi and lo parts.  A unit of 32 x 256 elements per CTA, all
+// of a thread's loads under way at once, four elements at a time where the caller's rows allow
+// it; X is written from shared memory, by rows or, where U is taller than wide, by columns.
+// The norm: each unit's sum of squares, and the last of a matrix's units to finish adds them
+// up, in their order.
 #include <algorithm>
 
-#include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "zo_launch.cuh"
 #include "zo_ops.h"
+#include "zo_ortho_io.cuh"
 #include "zo_tc_common.cuh"
 
 namespace zo {
@@ -18,114 +25,168 @@ namespace {
 
 using tc::exp2i;
 
-__device__ __forceinline__ float element(const void* p, int bf16, int64_t at) {
-  return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at])
-              : static_cast<const float*>(p)[at];
-}
-// x = hi + lo in fp16
-__device__ __forceinline__ void split(float x, uint16_t& hi, uint16_t& lo) {
-  const __half h = __float2half_rn(x);
-  const __half l = __float2half_rn(x - __half2float(h));
-  hi = *reinterpret_cast<const uint16_t*>(&h);
-  lo = *reinterpret_cast<const uint16_t*>(&l);
-}
+constexpr int kRows = kOrthoUnitRows, kCols = kOrthoUnitCols;
+constexpr int kThreads = 256;
+constexpr int kPitch = kCols + 4;             // of a tile in shared memory, in floats
+static_assert(kCols == kThreads && kRows % 8 == 0, "a column per thread, or four rows of fours");
 
-constexpr int kUnitThreads = 256;
-static_assert(kOrthoUnitCols == kUnitThreads, "a column per thread");
-
-// U of one element, and with `write` the new momentum
-template <bool kWrite>
-__device__ __forceinline__ float update_of(const OrthoMat& mt, const OrthoUpdate& u, int64_t i,
-                                           int64_t j) {
-  const float g = element(mt.G, mt.grad_bf16, i * mt.ldg + j);
-  if (!u.step || mt.M == nullptr) return g;
-  float* m = mt.M + i * mt.n + j;
-  float mom = *m;
-  if constexpr (kWrite) {
-    mom = fmaf(u.momentum, mom, g);
-    *m = mom;
-  }
-  return u.nesterov ? fmaf(u.momentum, mom, g) : mom;
-}
-
-// M <- momentum M + G, and the sum of U^2 over each unit
-__global__ void __launch_bounds__(kUnitThreads)
-momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
-                const OrthoUpdate u, float* __restrict__ partial) {
-  __shared__ float sums[kUnitThreads / 32];
-  const int4 un = units[blockIdx.x];
-  const OrthoMat mt = mats[un.x];
-  pdl_wait();
-  pdl_trigger();
-  const int64_t j = (int64_t)un.z + threadIdx.x;
-  const int64_t end = min((int64_t)un.y + kOrthoUnitRows, mt.m);
-  float s = 0.0f;
-  if (j < mt.n)
-    for (int64_t i = un.y; i < end; ++i) {
-      const float v = update_of<true>(mt, u, i, j);
-      s = fmaf(v, v, s);
+// U of this thread's elements: f(row of the unit, column, kV values).  With kWrite the new
+// momentum is stored.
+template <bool kWrite, int kV, typename F>
+__device__ __forceinline__ void for_unit(const OrthoMat& mt, const OrthoUpdate& u, const int4& un, F f) {
+  constexpr int kPass = kThreads * kV / kCols;                  // rows at a time: 1 or 4
+  constexpr int kBatch = 8;
+  const int r0 = (int)threadIdx.x / (kCols / kV), c = (int)threadIdx.x % (kCols / kV) * kV;
+  const int64_t j = (int64_t)un.z + c;
+  const bool moving = u.step && mt.M != nullptr;
+  if (j >= mt.n) return;
+  for (int b = 0; b < kRows; b += kPass * kBatch) {
+    float g[kBatch][kV], m[kBatch][kV];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int64_t i = (int64_t)un.y + b + k * kPass + r0;
+      if (i < mt.m) ortho::load_values<kV>(mt.G, mt.grad_bf16, i * mt.ldg + j, g[k]);
+    }
+    if (moving) {
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int64_t i = (int64_t)un.y + b + k * kPass + r0;
+        if (i < mt.m) ortho::load_values<kV>(mt.M, 0, i * mt.n + j, m[k]);
+      }
     }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s = 0.0f;
-    for (int w = 0; w < kUnitThreads / 32; ++w) s += sums[w];
-    partial[un.w] = s;
+    for (int k = 0; k < kBatch; ++k) {
+      const int64_t i = (int64_t)un.y + b + k * kPass + r0;
+      if (i >= mt.m) continue;
+      if (moving) {
+        if constexpr (kWrite) {
+#pragma unroll
+          for (int e = 0; e < kV; ++e) m[k][e] = fmaf(u.momentum, m[k][e], g[k][e]);
+          ortho::store_values<kV>(mt.M, 0, i * mt.n + j, m[k]);
+        }
+#pragma unroll
+        for (int e = 0; e < kV; ++e)
+          g[k][e] = u.nesterov ? fmaf(u.momentum, m[k][e], g[k][e]) : m[k][e];
+      }
+      f(b + k * kPass + r0, c, g[k]);
+    }
   }
 }
+template <bool kWrite, typename F>
+__device__ __forceinline__ void for_unit(const OrthoMat& mt, const OrthoUpdate& u, const int4& un, F f) {
+  if (ortho::by_fours(mt.G, mt.ldg, mt.grad_bf16, mt.n) &&
+      (mt.M == nullptr || !u.step || ortho::by_fours(mt.M, mt.n, 0, mt.n)))
+    for_unit<kWrite, 4>(mt, u, un, f);
+  else
+    for_unit<kWrite, 1>(mt, u, un, f);
+}
 
-// X_0 = U / (||U|| + eps)
-__global__ void __launch_bounds__(kUnitThreads)
-scale_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
-             const OrthoUpdate u, int ex, const float* __restrict__ partial) {
-  __shared__ float tile[64][65];
-  __shared__ double sums[kUnitThreads / 32];
-  const int4 un = units[blockIdx.x];
-  const OrthoMat mt = mats[un.x];
-  pdl_wait();
-  pdl_trigger();
-  double s = 0.0;
-  for (int k = threadIdx.x; k < mt.n_units; k += kUnitThreads) s += (double)partial[mt.unit0 + k];
+__device__ __forceinline__ double block_sum(double s, double* sums) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
   __syncthreads();
   s = 0.0;
-  for (int w = 0; w < kUnitThreads / 32; ++w) s += sums[w];
-  const float norm = (float)sqrt(s) + u.eps;
-  const float inv = norm == 0.0f ? 0.0f : exp2i(ex) / norm;
-  const int64_t i0 = un.y;
-  for (int64_t j0 = un.z; j0 < min((int64_t)un.z + kOrthoUnitCols, mt.n); j0 += 64) {
-    __syncthreads();
-    for (int e = threadIdx.x; e < 64 * 64; e += kUnitThreads) {
-      const int64_t i = i0 + e / 64, j = j0 + e % 64;
-      if (i < mt.m && j < mt.n) tile[e / 64][e % 64] = update_of<false>(mt, u, i, j) * inv;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) s += sums[w];
+  __syncthreads();
+  return s;
+}
+
+// M <- momentum M + G, the sum of U^2 over each unit, and 1 / (||U|| + eps) of each matrix
+__global__ void __launch_bounds__(kThreads)
+momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
+                const OrthoUpdate u, float* __restrict__ partial, uint32_t* __restrict__ counter,
+                float* __restrict__ inverse) {
+  __shared__ double sums[kThreads / 32];
+  __shared__ bool last;
+  const int4 un = units[blockIdx.x];
+  const OrthoMat mt = mats[un.x];
+  pdl_wait();
+  pdl_trigger();
+  float s = 0.0f;
+  for_unit<true>(mt, u, un, [&](int, int, const auto& v) {
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(v) / sizeof(float)); ++e) s = fmaf(v[e], v[e], s);
+  });
+  const double total = block_sum((double)s, sums);
+  if (threadIdx.x == 0) {
+    partial[un.w] = (float)total;
+    __threadfence();
+    last = atomicAdd(&counter[un.x], 1u) == (uint32_t)mt.n_units - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double all = 0.0;
+  for (int k = threadIdx.x; k < mt.n_units; k += kThreads)
+    all += (double)__ldcg(&partial[mt.unit0 + k]);
+  all = block_sum(all, sums);
+  if (threadIdx.x == 0) {
+    const float norm = (float)sqrt(all) + u.eps;
+    inverse[un.x] = norm == 0.0f ? 0.0f : 1.0f / norm;
+    counter[un.x] = 0;                                          // for the next call
+  }
+}
+
+// X_0 = U / (||U|| + eps)
+__global__ void __launch_bounds__(kThreads)
+scale_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
+             const OrthoUpdate u, int ex, const float* __restrict__ inverse) {
+  __shared__ __align__(16) float tile[kRows * kPitch];
+  const int4 un = units[blockIdx.x];
+  const OrthoMat mt = mats[un.x];
+  // TMA moves whole 16-byte chunks, so a row of X ends in zeros up to a multiple of eight: what
+  // lies outside U is zero here
+  for (int e = threadIdx.x; e < kRows * kPitch / 4; e += kThreads)
+    reinterpret_cast<float4*>(tile)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  const float inv = inverse[un.x], scale = exp2i(ex);
+  for_unit<false>(mt, u, un, [&](int r, int c, const auto& v) {
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(v) / sizeof(float)); ++e) tile[r * kPitch + c + e] = v[e] * inv;
+  });
+  __syncthreads();
+  const int64_t width = (mt.c + 7) / 8 * 8;
+  for (int e = threadIdx.x; e < kRows * kCols / 4; e += kThreads) {
+    // four neighbours of a row of X
+    float4 v;
+    int64_t row, col;
+    if (mt.tall) {
+      const int c = e / (kRows / 4), r = e % (kRows / 4) * 4;
+      const float* t = tile + r * kPitch + c;
+      v = make_float4(t[0], t[kPitch], t[2 * kPitch], t[3 * kPitch]);
+      row = (int64_t)un.z + c;
+      col = (int64_t)un.y + r;
+    } else {
+      const int r = e / (kCols / 4), c = e % (kCols / 4) * 4;
+      v = *reinterpret_cast<const float4*>(tile + r * kPitch + c);
+      row = (int64_t)un.y + r;
+      col = (int64_t)un.z + c;
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < 64 * 64; e += kUnitThreads) {
-      // X's row and column; TMA moves whole 16-byte chunks, so a row's last one ends in zeros
-      const int64_t row = (mt.tall ? j0 : i0) + e / 64, col = (mt.tall ? i0 : j0) + e % 64;
-      if (row >= mt.p || col >= (mt.c + 7) / 8 * 8) continue;
-      const float x = col >= mt.c ? 0.0f : mt.tall ? tile[e % 64][e / 64] : tile[e / 64][e % 64];
-      split(x, mt.xh[0][row * mt.ldx + col], mt.xl[0][row * mt.ldx + col]);
-    }
+    if (row >= mt.p || col >= width) continue;
+    uint2 hi, lo;
+    tc::split4_f16(v, scale, hi, lo);
+    *reinterpret_cast<uint2*>(mt.xh[0] + row * mt.ldx + col) = hi;
+    *reinterpret_cast<uint2*>(mt.xl[0] + row * mt.ldx + col) = lo;
   }
 }
 
 }  // namespace
 
 cudaError_t launch_ortho_momentum(const OrthoMat* mats, const int4* units, int32_t n_units,
-                                  const OrthoUpdate& u, float* partial, cudaStream_t s) {
-  return launch_dependent(momentum_kernel, (unsigned)n_units, kUnitThreads, 0, s, 1, true, mats,
-                          units, u, partial);
+                                  const OrthoUpdate& u, float* partial, uint32_t* counter,
+                                  float* inverse, cudaStream_t s) {
+  return launch_dependent(momentum_kernel, (unsigned)n_units, kThreads, 0, s, 1, true, mats, units,
+                          u, partial, counter, inverse);
 }
 cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t n_units,
-                               const OrthoUpdate& u, int32_t ex, const float* partial,
+                               const OrthoUpdate& u, int32_t ex, const float* inverse,
                                cudaStream_t s) {
-  return launch_dependent(scale_kernel, (unsigned)n_units, kUnitThreads, 0, s, 1, true, mats, units,
-                          u, ex, partial);
+  return launch_dependent(scale_kernel, (unsigned)n_units, kThreads, 0, s, 1, true, mats, units, u,
+                          ex, inverse);
 }
 
 }  // namespace zo
