@@ -17,7 +17,7 @@
 // of an SM), one accumulation per tile.
 // kPairs = true: hi + lo, the products hi.lo + lo.hi + hi.hi.  The tensor cores' fp32 sums
 // round towards zero, which over K = 5120 moved an 8 x 5120 result by 3.3e-5 of its norm; so
-// every 128 of K the accumulator is drained and added up in the epilogue's registers, rounded
+// every 64 of K the accumulator is drained and added up in the epilogue's registers, rounded
 // to nearest, and the small products come first.  N = 128: 64 sums per thread.
 // b A, a X and the stored X_k are a pair's sum in both.
 //
@@ -156,7 +156,6 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   constexpr int kABytes = 2 * kBlockBytes, kBBytes = kCols / 128 * kBlockBytes;   // per CTA
   constexpr int kStageBytes = (kPairs ? 2 : 1) * (kABytes + kBBytes);
   constexpr int kStages = kRing / kStageBytes;
-  constexpr int kSeg = 2;                            // kPairs: stages of one accumulation
   constexpr int kBufs = kTmemCols / kCols;
   constexpr int kWarpCols = kCols / 2, kChunks = kWarpCols / 32;
   static_assert(kStages <= 8 && kBufs <= 4 && sizeof(Shared) <= 1024);
@@ -266,7 +265,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     for (int t = t_begin; t < t_end && ok; ++t) {
       int left = (int)((depth_of(mats[tiles[t].x], phase) + 63) / 64);
       while (left > 0) {
-        const int n = kPairs ? min(kSeg, left) : left;
+        const int n = kPairs ? 1 : left;
         if (!mbar_wait_bounded(&sh.acc_empty[acc], acc_parity, abort, kWait)) {
           ok = false;
           break;
@@ -296,34 +295,28 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             commit_both(done);
           }
         } else {
-          // the segment's stages, then hi.lo, lo.hi and hi.hi of them
-          int at[kSeg];
-#pragma unroll
-          for (int k = 0; k < kSeg; ++k) {
-            at[k] = stage;
-            if (k >= n || !ok) continue;
-            ok = mbar_wait_bounded(&sh.full[stage], parity, abort, kWait);
-            if (++stage == kStages) {
-              stage = 0;
-              parity ^= 1u;
-            }
+          // one stage: hi.lo, lo.hi, hi.hi
+          if (!seen && !mbar_wait_bounded(&sh.full[stage], parity, abort, kWait)) {
+            ok = false;
+            break;
           }
-          if (ok) {
+          const uint64_t ad = a_first + (uint64_t)stage * kStageStep;
+          const uint64_t bd = b_first + (uint64_t)stage * kStageStep;
+          uint64_t* done = &sh.empty[stage];
 #pragma unroll
-            for (int prod = 0; prod < 3; ++prod)
+          for (int kk = 0; kk < 4; ++kk)
+            mma_pair_ss(d, ad + 2 * kk, bd + kLoStep + b_step * kk, idesc, kk != 0 ? 1u : 0u);
 #pragma unroll
-              for (int k = 0; k < kSeg; ++k) {
-                if (k >= n) continue;
-                const uint64_t ad = a_first + (uint64_t)at[k] * kStageStep + (prod == 1 ? kLoStep : 0);
-                const uint64_t bd = b_first + (uint64_t)at[k] * kStageStep + (prod == 0 ? kLoStep : 0);
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                  mma_pair_ss(d, ad + 2 * kk, bd + b_step * kk, idesc, (prod | k | kk) != 0 ? 1u : 0u);
-              }
-#pragma unroll
-            for (int k = 0; k < kSeg; ++k)
-              if (k < n) commit_both(&sh.empty[at[k]]);
+          for (int kk = 0; kk < 4; ++kk)
+            mma_pair_ss(d, ad + kLoStep + 2 * kk, bd + b_step * kk, idesc, 1);
+          if (++stage == kStages) {
+            stage = 0;
+            parity ^= 1u;
           }
+          seen = mbar_try_wait(&sh.full[stage], parity);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) mma_pair_ss(d, ad + 2 * kk, bd + b_step * kk, idesc, 1);
+          commit_both(done);
         }
         if (!ok) break;
         commit_both(&sh.acc_full[acc]);
@@ -377,8 +370,8 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       uint32_t raw[kPairs ? kChunks : 1][32];
       int acc = 0;
       if constexpr (kPairs) {
-        // the segments' sums, added up in fp32
-        const int64_t segs = (depth_of(mt, phase) + 64 * kSeg - 1) / (64 * kSeg);
+        // the stages' sums, added up in fp32
+        const int64_t segs = (depth_of(mt, phase) + 63) / 64;
 #pragma unroll
         for (int q = 0; q < kChunks; ++q)
 #pragma unroll
