@@ -349,15 +349,18 @@ def _rows(t, where, name, shape, dtype, device):
     if len(size) != 2 or (shape is not None and size != shape):
         raise ZoError(ZO_ERR_SHAPE, where, f"{name} has shape {tuple(size)}, "
                                            f"expected {'2-D' if shape is None else tuple(shape)}")
-    rows, cols = size
-    ld, step = t.stride()
-    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
-        raise ZoError(ZO_ERR_SHAPE, where, f"{name} needs unit column stride and separate rows")
+    if not t.is_contiguous():
+        rows, cols = size
+        ld, step = t.stride()
+        if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+            raise ZoError(ZO_ERR_SHAPE, where, f"{name} needs unit column stride and separate rows")
+    else:
+        rows, ld = 2, size[1]
     if dtype is not None and t.dtype != dtype:
         raise ZoError(ZO_ERR_DTYPE, where, f"{name} is {t.dtype}, expected {dtype}")
     if device is not None and t.device != device:
         raise ZoError(ZO_ERR_INVALID_ARG, where, f"{name} is on {t.device}, expected {device}")
-    return t.data_ptr(), ld if rows > 1 else cols
+    return t.data_ptr(), ld if rows > 1 else size[1]
 
 
 def _on_device(t, where):

@@ -29,7 +29,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // The tiles of one launch, dealt to the SM pairs: pair q's are tiles[first[q] .. first[q + 1]).
 struct TileList {
-  int32_t tile0 = 0, n = 0, pairs = 0, first0 = 0;
+  int32_t tile0 = 0, n = 0, pairs = 0, narrow = 0, first0 = 0;
 };
 struct Group {
   int32_t unit0 = 0, n_units = 0;
@@ -47,14 +47,15 @@ struct Small {
 // sums, then the buffers that the groups share.
 struct Layout {
   std::vector<zo::OrthoMat> mats;       // buffer pointers hold byte offsets until placed
-  std::vector<int4> units, tiles;
+  std::vector<int4> units;
+  std::vector<zo::OrthoTile> tiles;
   std::vector<Group> groups;
   std::vector<TileList> lists;
   std::vector<int32_t> first;           // kOrthoMaxPairs + 1 of every list
   std::vector<int32_t> small_list;
   int32_t n_maps = 0;                   // matrices with tensor maps
   std::vector<Small> small;
-  int64_t mats_at = 0, maps_at = 0, small_at = 0, units_at = 0, tiles_at = 0, first_at = 0, counter_at = 0, inverse_at = 0, partial_at = 0, buffers_at = 0, bytes = 0;
+  int64_t mats_at = 0, maps_at = 0, small_at = 0, units_at = 0, tiles_at = 0, first_at = 0, counter_at = 0, slot_counter_at = 0, inverse_at = 0, partial_at = 0, sums_at = 0, buffers_at = 0, bytes = 0;
   int64_t tables_end = 0;
 };
 
@@ -87,35 +88,100 @@ zo_status check_matrices(const zo_muon_matrix* mats, int32_t n_mats) {
 
 int64_t depth(const zo::OrthoMat& d, int phase) { return phase == zo::kOrthoGram ? d.c : d.p; }
 
-// Deals the tiles of every list, longest first, to n_pairs SM pairs, each to the pair with the
-// least to do so far; a pair's tiles keep their order.  A tile costs its depth in stages of 64,
-// and about six more for what the next tile's products do not hide.
+// What a tile costs, in SM cycles: its stages of 64 of K, and in a launch's time once more the
+// epilogue behind the last one (measured at 2048 x 2048 and 1001 x 333).
+struct TileCost {
+  int64_t stage, tail;
+};
+TileCost tile_cost(bool pairs, bool narrow) {
+  if (pairs) return narrow ? TileCost{600, 5500} : TileCost{950, 8000};
+  return narrow ? TileCost{400, 6500} : TileCost{600, 11000};
+}
+
+// Parts of Gram's K for one matrix: where its own tiles are few, as many as make them about half
+// of a GPU's SM pairs, each at least eight stages deep.  It goes by the matrix alone, so that its
+// bits do not depend on what else the context holds.  (48 x 7680: one tile of 120 stages, 83 us
+// of a 100 us step in one part.)
+int32_t gram_parts(const zo::OrthoMat& d) {
+  const int64_t blocks = (d.p + zo::kOrthoTileRows - 1) / zo::kOrthoTileRows;
+  const int64_t tiles = blocks * (blocks + 1) / 2, stages = (d.c + 63) / 64;
+  int32_t parts = 1;
+  while (2 * parts <= zo::kOrthoMaxParts && 2 * parts * tiles <= 38 && 16 * parts <= stages) parts *= 2;
+  return parts;
+}
+
+// Deals tiles, the deepest first, to n SM pairs, each to the pair with the least to do so far (a
+// pair's tiles keep their order); returns the longest pair's cycles.
+int64_t deal(const std::vector<zo::OrthoTile>& tiles, int32_t n, TileCost cost,
+             std::vector<std::vector<zo::OrthoTile>>* dealt) {
+  using Load = std::pair<int64_t, int32_t>;   // work so far, pair
+  std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+  for (int32_t q = 0; q < n; ++q) least.push({0, q});
+  int64_t most = 0;
+  for (const zo::OrthoTile& t : tiles) {
+    Load to = least.top();
+    least.pop();
+    if (dealt) (*dealt)[to.second].push_back(t);
+    to.first += (int64_t)(t.k1 - t.k0) * cost.stage + cost.tail / 4;
+    most = std::max(most, to.first);
+    least.push(to);
+  }
+  return most + cost.tail;
+}
+
+// The tiles of one product over the matrices [first, next) of a group: those of X X^T and
+// b A + c A A that meet or lie left of the diagonal's blocks of rows, or all of X'.
+std::vector<zo::OrthoTile> make_tiles(const Layout& L, size_t first, size_t next, int pr, int phase,
+                                      bool narrow) {
+  std::vector<zo::OrthoTile> tiles;
+  int32_t slots = 0;
+  for (size_t i = first; i < next; ++i) {
+    const zo::OrthoMat& d = L.mats[i];
+    if (d.small || d.pairs != pr) continue;
+    const int32_t stages = (int32_t)((depth(d, phase) + 63) / 64);
+    const int32_t of = phase == zo::kOrthoGram ? gram_parts(d) : 1;
+    for (int64_t r = 0; r < d.p; r += zo::kOrthoTileRows) {
+      const int64_t end = phase == zo::kOrthoApply ? d.c : std::min(r + zo::kOrthoTileRows, d.p);
+      for (int64_t c = 0; c < end; c += zo::ortho_tile_cols(pr != 0, narrow)) {
+        for (int32_t k = 0; k < of; ++k)
+          tiles.push_back({(int32_t)i, (int32_t)r, (int32_t)c, d.maps, stages * k / of,
+                           stages * (k + 1) / of, of > 1 ? slots : -1, k, of});
+        slots += of > 1;
+      }
+    }
+  }
+  std::stable_sort(tiles.begin(), tiles.end(), [](const zo::OrthoTile& a, const zo::OrthoTile& b) {
+    return a.k1 - a.k0 > b.k1 - b.k0;
+  });
+  return tiles;
+}
+
+// The tiling with the least estimated time on the SM pairs of a whole GPU: wide or narrow
+// tiles, which give the same bits.
+std::vector<zo::OrthoTile> best_tiles(const Layout& L, size_t first, size_t next, int pr, int phase,
+                                      int32_t* narrow) {
+  constexpr int32_t kPairsOfGpu = 76;
+  std::vector<zo::OrthoTile> wide = make_tiles(L, first, next, pr, phase, false);
+  if (wide.empty()) return wide;
+  std::vector<zo::OrthoTile> thin = make_tiles(L, first, next, pr, phase, true);
+  *narrow = deal(thin, kPairsOfGpu, tile_cost(pr != 0, true), nullptr) <
+            deal(wide, kPairsOfGpu, tile_cost(pr != 0, false), nullptr);
+  return *narrow ? thin : wide;
+}
+
+// Every list's tiles in the order of the n_pairs SM pairs that take them.
 void deal_tiles(Layout& L, int32_t n_pairs) {
   L.first.assign(L.lists.size() * (zo::kOrthoMaxPairs + 1), 0);
-  for (size_t l = 0; l < L.lists.size(); ++l) {
-    const TileList& list = L.lists[l];
-    int phase = 0;
-    for (const Group& g : L.groups)
-      for (int pr = 0; pr < 2; ++pr)
-        for (int k = 0; k < 3; ++k)
-          if (g.list[pr][k] == (int32_t)l) phase = k;
-    using Load = std::pair<int64_t, int32_t>;                // work so far, pair
-    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
-    for (int32_t q = 0; q < n_pairs; ++q) least.push({0, q});
-    std::vector<std::vector<int4>> dealt(n_pairs);
-    for (int32_t t = 0; t < list.n; ++t) {
-      const int4 tile = L.tiles[list.tile0 + t];
-      Load to = least.top();
-      least.pop();
-      dealt[to.second].push_back(tile);
-      to.first += (depth(L.mats[tile.x], phase) + 63) / 64 + 6;
-      least.push(to);
-    }
-    int32_t at = list.tile0;
+  for (const TileList& list : L.lists) {
+    const auto begin = L.tiles.begin() + list.tile0;
+    const std::vector<zo::OrthoTile> tiles(begin, begin + list.n);
+    std::vector<std::vector<zo::OrthoTile>> dealt(n_pairs);
+    deal(tiles, n_pairs, tile_cost(list.pairs != 0, list.narrow != 0), &dealt);
+    int32_t at = 0;
     for (int32_t q = 0; q <= zo::kOrthoMaxPairs; ++q) {
-      L.first[list.first0 + q] = at - list.tile0;
+      L.first[list.first0 + q] = at;
       if (q < n_pairs)
-        for (const int4& tile : dealt[q]) L.tiles[at++] = tile;
+        for (const zo::OrthoTile& t : dealt[q]) L.tiles[list.tile0 + at++] = t;
     }
   }
 }
@@ -188,31 +254,27 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     L.mats.push_back(d);
   }
   // tiles, group by group
+  int32_t slots_used = 0;
+  int64_t sums_floats = 0;
   size_t next = 0;
   for (Group& g : L.groups) {
     const size_t first = next;
     int64_t units = 0;
     for (; next < L.mats.size() && units + L.mats[next].n_units <= g.n_units; ++next)
       units += L.mats[next].n_units;               // (a small matrix has none)
-    // X X^T and b A + c A A: tiles that meet or lie left of the diagonal's blocks of rows
     for (int pr = 0; pr < 2; ++pr)
       for (const int phase : {zo::kOrthoGram, zo::kOrthoPoly, zo::kOrthoApply}) {
-        TileList list{(int32_t)L.tiles.size(), 0, pr, (int32_t)(L.lists.size() * (zo::kOrthoMaxPairs + 1))};
-        for (size_t i = first; i < next; ++i) {
-          const zo::OrthoMat& d = L.mats[i];
-          if (d.small || d.pairs != pr) continue;
-          for (int64_t r = 0; r < d.p; r += zo::kOrthoTileRows) {
-            const int64_t end = phase == zo::kOrthoApply ? d.c : std::min(r + zo::kOrthoTileRows, d.p);
-            for (int64_t c = 0; c < end; c += zo::ortho_tile_cols(pr != 0))
-              L.tiles.push_back(make_int4((int)i, (int)r, (int)c, d.maps));
+        TileList list{(int32_t)L.tiles.size(), 0, pr, 0, (int32_t)(L.lists.size() * (zo::kOrthoMaxPairs + 1))};
+        const std::vector<zo::OrthoTile> tiles = best_tiles(L, first, next, pr, phase, &list.narrow);
+        if (tiles.empty()) continue;
+        L.tiles.insert(L.tiles.end(), tiles.begin(), tiles.end());
+        list.n = (int32_t)tiles.size();
+        for (const zo::OrthoTile& t : tiles)
+          if (t.parts > 1) {
+            slots_used = std::max(slots_used, t.slot + 1);
+            sums_floats = std::max(sums_floats, (int64_t)(t.slot + 1) * zo::kOrthoMaxParts *
+                                                    zo::ortho_part_floats(pr != 0, list.narrow != 0));
           }
-        }
-        list.n = (int32_t)L.tiles.size() - list.tile0;
-        if (list.n == 0) continue;
-        // the longest products first (deal_tiles)
-        std::stable_sort(L.tiles.begin() + list.tile0, L.tiles.end(), [&](const int4& a, const int4& b) {
-          return depth(L.mats[a.x], phase) > depth(L.mats[b.x], phase);
-        });
         g.list[pr][phase] = (int32_t)L.lists.size();
         L.lists.push_back(list);
       }
@@ -247,11 +309,13 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
   L.maps_at = place((int64_t)sizeof(CUtensorMap) * zo::kOrthoMaps * L.n_maps);
   L.small_at = place(sizeof(int32_t) * L.small_list.size());
   L.units_at = place(sizeof(int4) * L.units.size());
-  L.tiles_at = place(sizeof(int4) * L.tiles.size());
+  L.tiles_at = place(sizeof(zo::OrthoTile) * L.tiles.size());
   L.first_at = place((int64_t)sizeof(int32_t) * L.lists.size() * (zo::kOrthoMaxPairs + 1));
   L.counter_at = place(sizeof(uint32_t) * L.mats.size());       // zeros, uploaded too
+  L.slot_counter_at = place((int64_t)sizeof(uint32_t) * zo::kOrthoSlotCounters * slots_used);
   L.tables_end = at;
   L.inverse_at = place(sizeof(float) * L.mats.size());
+  L.sums_at = place((int64_t)sizeof(float) * sums_floats);
   L.partial_at = place(sizeof(float) * slots);
   L.buffers_at = at;
   L.bytes = at + most;
@@ -360,7 +424,9 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   const Layout& L = c->plan;
   const auto* mats = reinterpret_cast<const zo::OrthoMat*>(c->ws + L.mats_at);
   const auto* units = reinterpret_cast<const int4*>(c->ws + L.units_at);
-  const auto* tiles = reinterpret_cast<const int4*>(c->ws + L.tiles_at);
+  const auto* tiles = reinterpret_cast<const zo::OrthoTile*>(c->ws + L.tiles_at);
+  auto* sums = reinterpret_cast<float*>(c->ws + L.sums_at);
+  auto* slot_counters = reinterpret_cast<uint32_t*>(c->ws + L.slot_counter_at);
   const auto* firsts = reinterpret_cast<const int32_t*>(c->ws + L.first_at);
   const auto* maps = reinterpret_cast<const CUtensorMap*>(c->ws + L.maps_at);
   auto* status = reinterpret_cast<uint32_t*>(c->ws);
@@ -390,8 +456,9 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
           if (g.list[pr][phase] < 0) continue;
           const TileList& list = L.lists[g.list[pr][phase]];
           ZO_CUDA(zo::launch_ortho_product(mats, maps, tiles + list.tile0, firsts + list.first0,
-                                           pr != 0, std::min(list.n, c->n_pairs), phase, st[k], u,
-                                           status, c->stream),
+                                           sums, slot_counters, pr != 0, list.narrow != 0,
+                                           std::min(list.n, c->n_pairs), phase, st[k], u, status,
+                                           c->stream),
                   "orthogonalisation: product kernel");
           ++c->launches;
         }
@@ -475,7 +542,7 @@ zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t 
     if (!L.units.empty()) std::memcpy(image.data() + L.units_at, L.units.data(), sizeof(int4) * L.units.size());
     if (!L.first.empty())
       std::memcpy(image.data() + L.first_at, L.first.data(), sizeof(int32_t) * L.first.size());
-    if (!L.tiles.empty()) std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(int4) * L.tiles.size());
+    if (!L.tiles.empty()) std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(zo::OrthoTile) * L.tiles.size());
     ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),
             "upload tables");
     L.mats.clear();

@@ -52,9 +52,23 @@ struct OrthoMat {
 };
 // kOrthoUnitRows x kOrthoUnitCols elements of U: (matrix, first row, first column, slot)
 constexpr int kOrthoUnitRows = 32, kOrthoUnitCols = 256;
-// A tile of a product: (matrix, first row, first column, index of its tensor maps)
-constexpr int kOrthoTileRows = 256;
-__host__ __device__ constexpr int ortho_tile_cols(bool pairs) { return pairs ? 128 : 256; }
+// A tile of a product, kOrthoTileRows x ortho_tile_cols(): stages [k0, k1) of 64 of K.  Where few
+// deep tiles would leave SM pairs idle, a tile's K is split: its parts share the slot of the
+// buffer for their sums, and the last one to finish adds them up.
+struct OrthoTile {
+  int32_t mat, i0, j0, maps;        // matrix, first row and column, index of its tensor maps
+  int32_t k0, k1;
+  int32_t slot, part, parts;        // parts > 1: one of a split tile's
+};
+constexpr int kOrthoTileRows = 256, kOrthoMaxParts = 8;
+__host__ __device__ constexpr int ortho_tile_cols(bool pairs, bool narrow) {
+  return (pairs ? 128 : 256) / (narrow ? 2 : 1);
+}
+// floats of one part of a slot, and its counters (one for each of 8 epilogue warps of two CTAs)
+__host__ __device__ constexpr int64_t ortho_part_floats(bool pairs, bool narrow) {
+  return (int64_t)kOrthoTileRows * ortho_tile_cols(pairs, narrow);
+}
+constexpr int kOrthoSlotCounters = 16;
 
 // Tensor maps of one matrix: 64 x 64 loads of X_k (hi of even and odd k, lo of even and odd
 // k), of A and of B (hi, lo), and the 32 x 32 stores in the same order.
@@ -106,8 +120,10 @@ cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t 
 int32_t ortho_max_pairs();
 constexpr int kOrthoMaxPairs = 128;
 // pair q of n_pairs takes the tiles first[q] .. first[q + 1] - 1
-cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, const int4* tiles,
-                                 const int32_t* first, bool pairs, int32_t n_pairs,
+// sums, counters: of the split tiles' slots (counters are zero between launches)
+cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps,
+                                 const OrthoTile* tiles, const int32_t* first, float* sums,
+                                 uint32_t* counters, bool pairs, bool narrow, int32_t n_pairs,
                                  OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
                                  uint32_t* status, cudaStream_t s);
 

@@ -14,11 +14,15 @@
 // next one's products.
 //
 // kPairs = false: hi parts only, N = 256 (32 KB per 64 of K for 128 x 256 x 64 multiply-adds
-// of an SM), one accumulation per tile.
+// of an SM) or 128, one accumulation per tile.
 // kPairs = true: hi + lo, the products hi.lo + lo.hi + hi.hi.  The tensor cores' fp32 sums
 // round towards zero, which over K = 5120 moved an 8 x 5120 result by 3.3e-5 of its norm; so
 // every 64 of K the accumulator is drained and added up in the epilogue's registers, rounded
-// to nearest, and the small products come first.  N = 128: 64 sums per thread.
+// to nearest, and the small products come first.  N = 128 (64 sums per thread) or 64.
+// The narrow tiles are for launches that do not fill the device: their epilogue, the larger part
+// of a short launch, is half as long.  Gram's K is split over several SM pairs where few tiles
+// are deep (zo_muon.cu): a part's epilogue warps leave their fp32 sums in memory, and the last
+// part's add them up, in the parts' order.
 // b A, a X and the stored X_k are a pair's sum in both.
 //
 // Roles (320 threads per CTA, one CTA per SM):
@@ -100,10 +104,6 @@ struct Phase {
   OrthoUpdate u;
 };
 
-__device__ __forceinline__ int64_t depth_of(const OrthoMat& mt, int phase) {
-  return phase == kOrthoGram ? mt.c : mt.p;
-}
-
 // W <- keep W - lr s v, or W <- v, of 32 values of one row of X.  `w` points at the first;
 // the next is `step` elements on, `n` are inside.
 template <typename T, bool kWide>
@@ -147,16 +147,19 @@ __device__ __forceinline__ void write_weights(T* w, int64_t step, int n, const f
 }
 
 // kLast: Apply of the last step, which writes W.
-template <bool kPairs, int phase, bool kLast>
+template <bool kPairs, bool kNarrow, int phase, bool kLast>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restrict__ maps,
-                  const int4* __restrict__ tiles, const int32_t* __restrict__ first, const Phase ph,
+                  const OrthoTile* __restrict__ tiles, const int32_t* __restrict__ first,
+                  float* __restrict__ sums, uint32_t* __restrict__ counters, const Phase ph,
                   uint32_t* __restrict__ status) {
-  constexpr int kCols = ortho_tile_cols(kPairs);
-  constexpr int kABytes = 2 * kBlockBytes, kBBytes = kCols / 128 * kBlockBytes;   // per CTA
+  constexpr int kCols = ortho_tile_cols(kPairs, kNarrow);
+  // boxes of B per CTA: kCols / 2 rows (at 64 columns a box's other half is not read)
+  constexpr int kBBoxes = kCols >= 128 ? kCols / 128 : 1;
+  constexpr int kABytes = 2 * kBlockBytes, kBBytes = kBBoxes * kBlockBytes;   // per CTA
   constexpr int kStageBytes = (kPairs ? 2 : 1) * (kABytes + kBBytes);
-  constexpr int kStages = kRing / kStageBytes;
-  constexpr int kBufs = kTmemCols / kCols;
+  constexpr int kStages = kRing / kStageBytes < 8 ? kRing / kStageBytes : 8;
+  constexpr int kBufs = kTmemCols / kCols < 4 ? kTmemCols / kCols : 4;
   constexpr int kWarpCols = kCols / 2, kChunks = kWarpCols / 32;
   static_assert(kStages <= 8 && kBufs <= 4 && sizeof(Shared) <= 1024);
   extern __shared__ uint8_t smem_raw[];
@@ -200,17 +203,16 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     int64_t filled = 0;
     bool ok = true;
     for (int t = t_begin; t < t_end && ok; ++t) {
-      const int4 tl = tiles[t];
-      const int steps = (int)((depth_of(mats[tl.x], phase) + 63) / 64);
-      const CUtensorMap* m = maps + (int64_t)tl.w * kOrthoMaps;
+      const OrthoTile tl = tiles[t];
+      const CUtensorMap* m = maps + (int64_t)tl.maps * kOrthoMaps;
       const int cur = ph.st.k & 1;
       const CUtensorMap* ah = m + (phase == kOrthoGram ? kMapX + cur
                                    : phase == kOrthoPoly ? kMapA : kMapB);
       const CUtensorMap* al = ah + (phase == kOrthoGram ? 2 : 1);
       const CUtensorMap* bh = m + (phase == kOrthoPoly ? kMapA : kMapX + cur);
       const CUtensorMap* bl = bh + (phase == kOrthoPoly ? 1 : 2);
-      const int i0 = tl.y + 128 * (int)rank, j0 = tl.z + kCols / 2 * (int)rank;
-      for (int k0 = 0; k0 < 64 * steps; k0 += 64) {
+      const int i0 = tl.i0 + 128 * (int)rank, j0 = tl.j0 + kCols / 2 * (int)rank;
+      for (int k0 = 64 * tl.k0; k0 < 64 * tl.k1; k0 += 64) {
         if (!mbar_wait_bounded(&sh.empty[stage], free_parity, abort, kWait)) {
           ok = false;
           break;
@@ -227,7 +229,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
           for (int q = 0; q < 2; ++q, dst += kBlockBytes)
             tma_load_2d_to_leader(dst, a, k0, i0 + 64 * q, full);
 #pragma unroll
-          for (int q = 0; q < kCols / 128; ++q, dst += kBlockBytes) {
+          for (int q = 0; q < kBBoxes; ++q, dst += kBlockBytes) {
             if (phase == kOrthoApply) tma_load_2d_to_leader(dst, bm, j0 + 64 * q, k0, full);
             else tma_load_2d_to_leader(dst, bm, k0, j0 + 64 * q, full);
           }
@@ -263,7 +265,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     uint32_t parity = 0, acc_parity = 1;
     bool ok = true, seen = false;              // seen: full[stage] has been found complete
     for (int t = t_begin; t < t_end && ok; ++t) {
-      int left = (int)((depth_of(mats[tiles[t].x], phase) + 63) / 64);
+      int left = tiles[t].k1 - tiles[t].k0;
       while (left > 0) {
         const int n = kPairs ? 1 : left;
         if (!mbar_wait_bounded(&sh.acc_empty[acc], acc_parity, abort, kWait)) {
@@ -344,22 +346,22 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     int64_t n_acc = 0;
     bool ok = true;
     for (int t = t_begin; t < t_end && ok; ++t) {
-      const int4 tl = tiles[t];
-      const OrthoMat& mt = mats[tl.x];
-      const CUtensorMap* m = maps + (int64_t)tl.w * kOrthoMaps;
+      const OrthoTile tl = tiles[t];
+      const OrthoMat& mt = mats[tl.mat];
+      const CUtensorMap* m = maps + (int64_t)tl.maps * kOrthoMaps;
       const int cur = ph.st.k & 1;
-      const int64_t i0 = tl.y + 128 * (int64_t)rank + 32 * g, i = i0 + lane;
+      const int64_t i0 = tl.i0 + 128 * (int64_t)rank + 32 * g, i = i0 + lane;
       const int64_t p = mt.p, cols = phase == kOrthoApply ? mt.c : mt.p;
       const uint32_t col0 = ((uint32_t)(32 * g) << 16) + (uint32_t)(kWarpCols * half);
       const auto outside = [&](int q) {            // the same in every lane
-        return i0 >= p || tl.z + kWarpCols * half + 32 * q >= cols;
+        return i0 >= p || tl.j0 + kWarpCols * half + 32 * q >= cols;
       };
       // lane 0: what is added to the product (A in Poly, X in Apply), 32 x 32 of hi and of lo,
       // into the warp's boxes once their last stores have read them
       const auto request = [&](int q) {
         if (phase == kOrthoGram || outside(q)) return;
         const CUtensorMap* from = m + (phase == kOrthoPoly ? kMapStoreA : kMapStoreX + cur);
-        const int j = tl.z + kWarpCols * half + 32 * q;
+        const int j = tl.j0 + kWarpCols * half + 32 * q;
         bulk_wait_read_all();
         pending = true;
         mbar_arrive_expect_tx(in_full, (kTwo ? 2 : 1) * kBoxBytes);
@@ -371,12 +373,12 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       int acc = 0;
       if constexpr (kPairs) {
         // the stages' sums, added up in fp32
-        const int64_t segs = (depth_of(mt, phase) + 63) / 64;
+        const int segs = tl.k1 - tl.k0;
 #pragma unroll
         for (int q = 0; q < kChunks; ++q)
 #pragma unroll
           for (int e = 0; e < 32; ++e) raw[q][e] = 0u;
-        for (int64_t sg = 0; sg < segs; ++sg, ++n_acc) {
+        for (int sg = 0; sg < segs; ++sg, ++n_acc) {
           acc = (int)(n_acc % kBufs);
           if (!mbar_wait_bounded(&sh.acc_full[acc], (uint32_t)((n_acc / kBufs) & 1), abort, kWait)) {
             ok = false;
@@ -405,11 +407,53 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         tc_fence_after();
       }
       if (!ok) break;
+      bool finish = true, shared = false;
+      if (phase == kOrthoGram && tl.parts > 1 && !outside(0)) {
+        // this warp's sums of every part lie together: 32 lanes apart for coalescing
+        shared = true;
+        constexpr int kOwn = 32 * 32 * kChunks;
+        float* mine = sums + ((int64_t)tl.slot * kOrthoMaxParts + tl.part) * ortho_part_floats(kPairs, kNarrow) +
+                      ((int)rank * kEpiWarps + warp - 2) * kOwn + lane;
+#pragma unroll
+        for (int q = 0; q < kChunks; ++q) {
+          if constexpr (!kPairs) {
+            tmem_ld_32x32b_x32(tmem + col0 + (uint32_t)(acc * kCols + 32 * q), raw[0]);
+            tmem_ld_wait();
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            mine[(q * 32 + e) * 32] = __uint_as_float(raw[kPairs ? q : 0][e]);
+        }
+        __threadfence();
+        __syncwarp();
+        uint32_t* counter = counters + tl.slot * kOrthoSlotCounters + (int)rank * kEpiWarps + warp - 2;
+        uint32_t seen = 0;
+        if (lane == 0) {
+          seen = atomicAdd(counter, 1u);
+          if (seen == (uint32_t)tl.parts - 1) *counter = 0;    // for the next launch
+        }
+        finish = __shfl_sync(0xffffffffu, seen, 0) == (uint32_t)tl.parts - 1;
+        __threadfence();
+      }
 #pragma unroll
       for (int q = 0; q < kChunks; ++q) {
-        const int64_t j0 = tl.z + kWarpCols * half + 32 * q;
-        if (outside(q)) continue;
-        if constexpr (!kPairs) {
+        const int64_t j0 = tl.j0 + kWarpCols * half + 32 * q;
+        if (outside(q) || !finish) continue;
+        if (phase == kOrthoGram && shared) {
+          constexpr int kOwn = 32 * 32 * kChunks;
+          const float* from = sums + (int64_t)tl.slot * kOrthoMaxParts * ortho_part_floats(kPairs, kNarrow) +
+                              ((int)rank * kEpiWarps + warp - 2) * kOwn + lane;
+          float total[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) total[e] = __ldcg(from + (q * 32 + e) * 32);
+          for (int s = 1; s < tl.parts; ++s) {
+            from += ortho_part_floats(kPairs, kNarrow);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) total[e] += __ldcg(from + (q * 32 + e) * 32);
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) raw[kPairs ? q : 0][e] = __float_as_uint(total[e]);
+        } else if constexpr (!kPairs) {
           tmem_ld_32x32b_x32(tmem + col0 + (uint32_t)(acc * kCols + 32 * q), raw[0]);
           tmem_ld_wait();
         }
@@ -469,7 +513,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         }
         // hi, then (a pair, or X in any case) lo, as 32 x 32 boxes; below the diagonal of a
         // symmetric result the box of the transposed place too
-        const bool both = phase != kOrthoApply && tl.z + kCols <= tl.y;
+        const bool both = phase != kOrthoApply && tl.j0 + kCols <= tl.i0;
         const int parts = phase == kOrthoApply || kPairs ? 2 : 1;
         const CUtensorMap* to = m + (phase == kOrthoGram ? kMapStoreA
                                      : phase == kOrthoPoly ? kMapStoreB : kMapStoreX + (cur ^ 1));
@@ -537,13 +581,14 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 
 // f(kernel) with the instance of a launch
 template <typename F>
-auto with_kernel(bool pairs, int phase, bool last, F f) {
-#define ZO_PHASE(P)                                                                           \
-  phase == kOrthoGram ? f(ortho_gemm_kernel<P, kOrthoGram, false>)                            \
-  : phase == kOrthoPoly ? f(ortho_gemm_kernel<P, kOrthoPoly, false>)                          \
-  : last ? f(ortho_gemm_kernel<P, kOrthoApply, true>) : f(ortho_gemm_kernel<P, kOrthoApply, false>)
-  if (pairs) return ZO_PHASE(true);
-  return ZO_PHASE(false);
+auto with_kernel(bool pairs, bool narrow, int phase, bool last, F f) {
+#define ZO_PHASE(P, N)                                                    \
+  phase == kOrthoGram ? f(ortho_gemm_kernel<P, N, kOrthoGram, false>)     \
+  : phase == kOrthoPoly ? f(ortho_gemm_kernel<P, N, kOrthoPoly, false>)   \
+  : last ? f(ortho_gemm_kernel<P, N, kOrthoApply, true>)                  \
+         : f(ortho_gemm_kernel<P, N, kOrthoApply, false>)
+  if (pairs) return narrow ? ZO_PHASE(true, true) : ZO_PHASE(true, false);
+  return narrow ? ZO_PHASE(false, true) : ZO_PHASE(false, false);
 #undef ZO_PHASE
 }
 
@@ -551,7 +596,7 @@ auto with_kernel(bool pairs, int phase, bool last, F f) {
 
 int32_t ortho_max_pairs() {
   // (every instance has the same launch shape and shared memory)
-  return with_kernel(true, kOrthoApply, true, [](auto kernel) -> int32_t {
+  return with_kernel(true, false, kOrthoApply, true, [](auto kernel) -> int32_t {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -572,17 +617,18 @@ int32_t ortho_max_pairs() {
   });
 }
 
-cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps, const int4* tiles,
-                                 const int32_t* first, bool pairs, int32_t n_pairs,
+cudaError_t launch_ortho_product(const OrthoMat* mats, const CUtensorMap* maps,
+                                 const OrthoTile* tiles, const int32_t* first, float* sums,
+                                 uint32_t* counters, bool pairs, bool narrow, int32_t n_pairs,
                                  OrthoPhase phase, const OrthoStep& st, const OrthoUpdate& u,
                                  uint32_t* status, cudaStream_t s) {
   if (n_pairs <= 0) return cudaErrorInvalidValue;
-  return with_kernel(pairs, (int)phase, st.last != 0, [&](auto kernel) -> cudaError_t {
+  return with_kernel(pairs, narrow, (int)phase, st.last != 0, [&](auto kernel) -> cudaError_t {
     const cudaError_t e =
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     if (e != cudaSuccess) return e;
     return launch_dependent(kernel, 2u * (unsigned)n_pairs, kThreads, kSmem, s, 1, true, mats, maps,
-                            tiles, first, Phase{st, u}, status);
+                            tiles, first, sums, counters, Phase{st, u}, status);
   });
 }
 

@@ -25,17 +25,37 @@ class LayerNormOut(NamedTuple):
     h: Optional[torch.Tensor]          # x + residual, rounded to x's type (None: no residual)
 
 
-def _call(fn, x, at, *args):
-    """A call of the C ABI on the current stream of x's device."""
+# The handle of a device's current stream, without a Stream object around it where PyTorch
+# has that (about 1 us of a call that takes ten).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+_empty, _empty_like = torch.empty, torch.empty_like
+_contiguous = torch.contiguous_format
+_F32 = torch.float32
+_CODES = {torch.bfloat16: zb.ZO_BF16, torch.float32: zb.ZO_F32}
+
+
+def _code(dtype, at, name):
+    code = _CODES.get(dtype)
+    return zb._code_of(dtype, at, name) if code is None else code     # (refuses)
+
+
+def _call(fn, dev, at, *args):
+    """A call of the C ABI on the current stream of device number `dev`."""
+    if dev == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _raw_stream(dev))
+    if status:
+        zb._check(status, at)
+
+
+def _device_of(x, at):
     dev = x.get_device()
     if dev < 0:
         raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, f"the tensors are on {x.device}, not on a GPU")
-    stream = torch.cuda.current_stream(dev).cuda_stream
-    if dev == torch.cuda.current_device():
-        zb._check(fn(*args, stream), at)
-    else:
-        with torch.cuda.device(dev):
-            zb._check(fn(*args, stream), at)
+    return dev
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
@@ -43,26 +63,30 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
     residual is given (the sum comes back as ``h``)."""
     at = "layer_norm"
     px, ldx = zb._rows(x, at, "x", None, None, None)
-    (rows, cols), dt, dev = x.shape, x.dtype, x.device
-    w = weight if weight is not None else bias
-    wdt = torch.float32 if w is None else w.dtype
-    pw = zb._vector(weight, at, "weight", cols, wdt, dev)
-    pb = zb._vector(bias, at, "bias", cols, wdt, dev)
-    pr, ldr = zb._rows(residual, at, "residual", x.shape, dt, dev)
+    shape, dt, device = x.shape, x.dtype, x.device
+    rows, cols = shape
+    dev = _device_of(x, at)
+    pw = pb = pr = ph = pm = ps = h = mean = rstd = None
+    wdt, ldr = _F32, 0
+    if weight is not None:
+        wdt = weight.dtype
+        pw = zb._vector(weight, at, "weight", cols, wdt, device)
+    elif bias is not None:
+        wdt = bias.dtype
+    if bias is not None:
+        pb = zb._vector(bias, at, "bias", cols, wdt, device)
     # the outputs are contiguous: nothing of them needs a check
-    y = torch.empty_like(x, memory_format=torch.contiguous_format)
-    h = ph = mean = rstd = pm = ps = None
+    y = _empty_like(x, memory_format=_contiguous)
     if residual is not None:
-        h = torch.empty_like(y)
+        pr, ldr = zb._rows(residual, at, "residual", shape, dt, device)
+        h = _empty_like(y)
         ph = h.data_ptr()
     if stats:
-        mean = torch.empty(rows, dtype=torch.float32, device=dev)
-        rstd = torch.empty_like(mean)
+        mean = _empty(rows, dtype=_F32, device=device)
+        rstd = _empty_like(mean)
         pm, ps = mean.data_ptr(), rstd.data_ptr()
-    _call(zb.LIB.zo_layernorm_forward, x, at, px, ldx, pr, ldr, rows, cols,
-          zb._dtype_code(x, at, "x"), pw, pb,
-          zb.ZO_F32 if w is None else zb._dtype_code(w, at, "weight"), eps, y.data_ptr(), cols, ph,
-          cols, pm, ps)
+    _call(zb.LIB.zo_layernorm_forward, dev, at, px, ldx, pr, ldr, rows, cols, _code(dt, at, "x"),
+          pw, pb, _code(wdt, at, "weight"), eps, y.data_ptr(), cols, ph, cols, pm, ps)
     return LayerNormOut(y, mean, rstd, h)
 
 
@@ -73,32 +97,35 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dresidual=None, wdtype=None, 
     have the weight's type (wdtype where there is none); None where not wanted."""
     at = "layer_norm_backward"
     px, ldx = zb._rows(x, at, "x", None, None, None)
-    (rows, cols), dt, dev = x.shape, x.dtype, x.device
+    shape, dt, device = x.shape, x.dtype, x.device
+    rows, cols = shape
+    dev = _device_of(x, at)
+    pw = pdr = dw = db = pdw = pdb = pws = None
+    lddr = ws_bytes = 0
     if weight is not None:
         wdtype = weight.dtype
+        pw = zb._vector(weight, at, "weight", cols, wdtype, device)
     elif wdtype is None:
-        wdtype = torch.float32
-    pw = zb._vector(weight, at, "weight", cols, wdtype, dev)
-    pdy, lddy = zb._rows(dy, at, "dy", x.shape, dt, dev)
-    pdr, lddr = zb._rows(dresidual, at, "dresidual", x.shape, dt, dev)
-    pm = zb._vector(mean, at, "mean", rows, torch.float32, dev)
-    ps = zb._vector(rstd, at, "rstd", rows, torch.float32, dev)
-    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
-    dw = db = pdw = pdb = pws = None
-    ws_bytes = 0
+        wdtype = _F32
+    pdy, lddy = zb._rows(dy, at, "dy", shape, dt, device)
+    if dresidual is not None:
+        pdr, lddr = zb._rows(dresidual, at, "dresidual", shape, dt, device)
+    pm = zb._vector(mean, at, "mean", rows, _F32, device)
+    ps = zb._vector(rstd, at, "rstd", rows, _F32, device)
+    dx = _empty_like(x, memory_format=_contiguous)
     if want_weight:
-        dw = torch.empty(cols, dtype=wdtype, device=dev)
+        dw = _empty(cols, dtype=wdtype, device=device)
         pdw = dw.data_ptr()
     if want_bias:
-        db = torch.empty(cols, dtype=wdtype, device=dev)
+        db = _empty(cols, dtype=wdtype, device=device) if dw is None else _empty_like(dw)
         pdb = db.data_ptr()
     if want_weight or want_bias:
         ws_bytes = zb.LIB.zo_layernorm_workspace(rows, cols)
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+        ws = _empty(ws_bytes, dtype=torch.uint8, device=device)
         pws = ws.data_ptr()
-    _call(zb.LIB.zo_layernorm_backward, x, at, pdy, lddy, px, ldx, pdr, lddr, rows, cols,
-          zb._dtype_code(x, at, "x"), pw, zb._code_of(wdtype, at, "weight"), pm, ps, dx.data_ptr(),
-          cols, pdw, pdb, pws, ws_bytes)
+    _call(zb.LIB.zo_layernorm_backward, dev, at, pdy, lddy, px, ldx, pdr, lddr, rows, cols,
+          _code(dt, at, "x"), pw, _code(wdtype, at, "weight"), pm, ps, dx.data_ptr(), cols, pdw,
+          pdb, pws, ws_bytes)
     return dx, dw, db
 
 
