@@ -11,7 +11,7 @@ using namespace ln;
 template <typename T, typename TW, int kGroup, int kElems, int V>
 __global__ void __launch_bounds__(block_of(kGroup))
 forward_kernel(const LayerNormArgs a) {
-  constexpr int kBlock = block_of(kGroup), kRows = kBlock / kGroup, kE = kElems / V;
+  constexpr int kBlock = block_of(kGroup), kRows = kBlock / kGroup;
   __shared__ float buf[2][32];
   const int t = threadIdx.x % kGroup;
   const int64_t wanted = (int64_t)blockIdx.x * kRows + threadIdx.x / kGroup;
@@ -29,60 +29,48 @@ forward_kernel(const LayerNormArgs a) {
   const float inv_n = 1.0f / (float)cols;
 
   float mean, rstd;
-  if constexpr (kE > 0) {
+  if constexpr (kElems > 0) {
     // every load is under way before anything is computed
-    float v[kE][V], wv[kE][V], bv[kE][V];
-    const auto column = [&](int e) { return ((int64_t)e * kGroup + t) * V; };
+    const int col = t * V;
+    const auto inside = [&](int e) { return e * kGroup * V + col < (int)cols; };
+    const auto written = [&](int e) { return live && inside(e); };
+    float2 v[kElems / 2], wv[kElems / 2], bv[kElems / 2];
 #pragma unroll
-    for (int e = 0; e < kE; ++e)
-#pragma unroll
-      for (int k = 0; k < V; ++k) { v[e][k] = bv[e][k] = 0.0f; wv[e][k] = 1.0f; }
-#pragma unroll
-    for (int e = 0; e < kE; ++e)
-      if (column(e) < cols) load<T, V, true>(x + column(e), v[e]);
-    if (w) {
-#pragma unroll
-      for (int e = 0; e < kE; ++e)
-        if (column(e) < cols) load<TW, V, true>(w + column(e), wv[e]);
+    for (int i = 0; i < kElems / 2; ++i) {
+      wv[i] = both(1.0f);
+      bv[i] = both(0.0f);
     }
-    if (b) {
-#pragma unroll
-      for (int e = 0; e < kE; ++e)
-        if (column(e) < cols) load<TW, V, true>(b + column(e), bv[e]);
-    }
+    load_columns<T, kElems, kGroup, V, true>(x + col, inside, 0.0f, v);
+    if (w) load_columns<TW, kElems, kGroup, V, true>(w + col, inside, 0.0f, wv);
+    if (b) load_columns<TW, kElems, kGroup, V, true>(b + col, inside, 0.0f, bv);
     if (r) {
-      float q[kE][V];
+      float2 o[kElems / 2];
+      load_columns<T, kElems, kGroup, V, true>(r + col, inside, 0.0f, o);
 #pragma unroll
-      for (int e = 0; e < kE; ++e)
-        if (column(e) < cols) load<T, V, true>(r + column(e), q[e]);
-#pragma unroll
-      for (int e = 0; e < kE; ++e)
-        if (column(e) < cols) {
-#pragma unroll
-          for (int k = 0; k < V; ++k) v[e][k] = Elem<T>::to(Elem<T>::from(v[e][k] + q[e][k]));
-          if (live) store<T, V>(h + column(e), v[e]);
-        }
+      for (int i = 0; i < kElems / 2; ++i) v[i] = rounded<T>(add2(v[i], o[i]));
+      store_columns<T, kElems, kGroup, V>(h + col, written, v);
     }
-    float s = 0.0f, q = 0.0f;
+    float2 s = both(0.0f), q = both(0.0f);
 #pragma unroll
-    for (int e = 0; e < kE; ++e)
+    for (int i = 0; i < kElems / 2; ++i) s = add2(s, v[i]);
+    mean = group_sum<kGroup>(s.x + s.y, buf[0]) * inv_n;
+    const float2 minus = both(-mean);
 #pragma unroll
-      for (int k = 0; k < V; ++k) s += v[e][k];
-    mean = group_sum<kGroup>(s, buf[0]) * inv_n;
-#pragma unroll
-    for (int e = 0; e < kE; ++e)
-      if (column(e) < cols) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) q = fmaf(v[e][k] - mean, v[e][k] - mean, q);
+    for (int i = 0; i < kElems / 2; ++i) {
+      v[i] = add2(v[i], minus);
+      if constexpr (V == 1) {
+        if (!inside(2 * i)) v[i].x = 0.0f;
+        if (!inside(2 * i + 1)) v[i].y = 0.0f;
+      } else if (!inside(2 * i / V)) {
+        v[i] = both(0.0f);
       }
-    rstd = 1.0f / sqrtf(group_sum<kGroup>(q, buf[1]) * inv_n + a.eps);
+      q = fma2(v[i], v[i], q);
+    }
+    rstd = 1.0f / sqrtf(group_sum<kGroup>(q.x + q.y, buf[1]) * inv_n + a.eps);
+    const float2 scale = both(rstd);
 #pragma unroll
-    for (int e = 0; e < kE; ++e)
-      if (live && column(e) < cols) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[e][k] = fmaf((v[e][k] - mean) * rstd, wv[e][k], bv[e][k]);
-        store<T, V>(y + column(e), v[e]);
-      }
+    for (int i = 0; i < kElems / 2; ++i) v[i] = fma2(mul2(v[i], scale), wv[i], bv[i]);
+    store_columns<T, kElems, kGroup, V>(y + col, written, v);
   } else {
     float v[V], s = 0.0f, q = 0.0f;
     const auto fetch = [&](int64_t j) {
@@ -129,7 +117,7 @@ forward_kernel(const LayerNormArgs a) {
 template <typename T, typename TW, int kGroup, int kElems, int V>
 __global__ void __launch_bounds__(block_of(kGroup), resident_of(kGroup, kElems, false))
 forward_ring_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
-  constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup, kE = kElems / V;
+  constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup;
   __shared__ float buf[2][2][32];
   __shared__ uint64_t full[kGroups][kMaxStages];
   extern __shared__ __align__(128) uint8_t dyn[];
@@ -151,65 +139,55 @@ forward_ring_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   if (t == 0)
     for (int s = 0; s < stages; ++s)
       if (row0 + s * stride < a.rows) ring.fetch(row0 + s * stride, s);
-  const TW* w = static_cast<const TW*>(a.weight);
-  const TW* b = static_cast<const TW*>(a.bias);
-  float wv[kE][V], bv[kE][V];
+  const int col = t * V;                       // this thread's chunks: every kGroup V columns
+  const auto inside = [&](int e) { return e * kGroup * V + col < (int)cols; };
+  float2 wv[kElems / 2], bv[kElems / 2];
 #pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    const int64_t j = ((int64_t)e * kGroup + t) * V;
-#pragma unroll
-    for (int k = 0; k < V; ++k) { wv[e][k] = 1.0f; bv[e][k] = 0.0f; }
-    if (w && j < cols) load<TW, V, true>(w + j, wv[e]);
-    if (b && j < cols) load<TW, V, true>(b + j, bv[e]);
+  for (int i = 0; i < kElems / 2; ++i) {
+    wv[i] = both(1.0f);
+    bv[i] = both(0.0f);
   }
+  if (a.weight)
+    load_columns<TW, kElems, kGroup, V, true>(static_cast<const TW*>(a.weight) + col, inside, 0.0f, wv);
+  if (a.bias)
+    load_columns<TW, kElems, kGroup, V, true>(static_cast<const TW*>(a.bias) + col, inside, 0.0f, bv);
   int flip = 0;
   for (int64_t row = row0; row < a.rows; row += stride, flip ^= 1) {
-    const T* src[3];
-    ring.take(row, src);
-    T* y = static_cast<T*>(a.y) + row * a.ldy;
-    float v[kE][V];
-    float s = 0.0f;
+    const bool came = ring.ready();
+    float2 v[kElems / 2];
+    load_columns<T, kElems, kGroup, V, false>(ring.at(0, row) + col, inside, 0.0f, v);
+    if (a.r) {
+      float2 q[kElems / 2];
+      load_columns<T, kElems, kGroup, V, false>(ring.at(1, row) + col, inside, 0.0f, q);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int64_t j = ((int64_t)e * kGroup + t) * V;
-#pragma unroll
-      for (int k = 0; k < V; ++k) v[e][k] = 0.0f;
-      if (j < cols) {
-        load<T, V>(src[0] + j, v[e]);
-        if (a.r) {
-          float q[V];
-          load<T, V>(src[1] + j, q);
-#pragma unroll
-          for (int k = 0; k < V; ++k) v[e][k] = Elem<T>::to(Elem<T>::from(v[e][k] + q[k]));
-          store<T, V>(static_cast<T*>(a.h) + row * a.ldh + j, v[e]);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < V; ++k) s += v[e][k];
+      for (int i = 0; i < kElems / 2; ++i) v[i] = rounded<T>(add2(v[i], q[i]));
+      store_columns<T, kElems, kGroup, V>(static_cast<T*>(a.h) + row * a.ldh + col, inside, v);
     }
-    const float mean = group_sum<kGroup>(s, buf[flip][0]) * inv_n;
+    float2 s = both(0.0f), q = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < kElems / 2; ++i) s = add2(s, v[i]);
+    float mean = group_sum<kGroup>(s.x + s.y, buf[flip][0]) * inv_n;
     // every thread of the group has read the stage
     if (t == 0 && row + stages * stride < a.rows) ring.fetch(row + stages * stride, ring.stage);
     ring.advance();
-    float q = 0.0f;
+    if (!came) mean = __int_as_float(0x7FC00000);
+    const float2 minus = both(-mean);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int64_t j = ((int64_t)e * kGroup + t) * V;
-      if (j < cols) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) q = fmaf(v[e][k] - mean, v[e][k] - mean, q);
+    for (int i = 0; i < kElems / 2; ++i) {
+      v[i] = add2(v[i], minus);
+      if constexpr (V == 1) {
+        if (!inside(2 * i)) v[i].x = 0.0f;
+        if (!inside(2 * i + 1)) v[i].y = 0.0f;
+      } else if (!inside(2 * i / V)) {
+        v[i] = both(0.0f);
       }
+      q = fma2(v[i], v[i], q);
     }
-    const float rstd = 1.0f / sqrtf(group_sum<kGroup>(q, buf[flip][1]) * inv_n + a.eps);
+    const float rstd = 1.0f / sqrtf(group_sum<kGroup>(q.x + q.y, buf[flip][1]) * inv_n + a.eps);
+    const float2 scale = both(rstd);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int64_t j = ((int64_t)e * kGroup + t) * V;
-      if (j < cols) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[e][k] = fmaf((v[e][k] - mean) * rstd, wv[e][k], bv[e][k]);
-        store<T, V>(y + j, v[e]);
-      }
-    }
+    for (int i = 0; i < kElems / 2; ++i) v[i] = fma2(mul2(v[i], scale), wv[i], bv[i]);
+    store_columns<T, kElems, kGroup, V>(static_cast<T*>(a.y) + row * a.ldy + col, inside, v);
     if (t == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;

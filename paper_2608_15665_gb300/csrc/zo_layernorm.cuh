@@ -109,6 +109,70 @@ __device__ __forceinline__ void store(T* p, const float (&v)[V]) {
   }
 }
 
+// Two columns at a time: packed fp32 arithmetic (each half an IEEE operation, round to nearest).
+// At 24 instructions a column, and not by memory, a row's arithmetic bounded the passes.
+union Pair {
+  float2 f;
+  uint64_t u;
+};
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  Pair x{a}, y{b}, r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(x.u), "l"(y.u));
+  return r.f;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  Pair x{a}, y{b}, r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(x.u), "l"(y.u));
+  return r.f;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  Pair x{a}, y{b}, z{c}, r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(x.u), "l"(y.u), "l"(z.u));
+  return r.f;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// A thread's columns of a row as pairs: chunks of V columns, chunk e at column (e kGroup + t) V.
+// f(e) says whether chunk e lies inside the row; the values of the others are `rest`.
+template <typename T, int kElems, int kGroup, int V, bool kReadOnly, typename F>
+__device__ __forceinline__ void load_columns(const T* p, F inside, float rest, float2 (&v)[kElems / 2]) {
+#pragma unroll
+  for (int e = 0; e < kElems / V; ++e) {
+    float c[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) c[k] = rest;
+    if (inside(e)) load<T, V, kReadOnly>(p + e * kGroup * V, c);
+    if constexpr (V == 1) {
+      if (e % 2 == 0) v[e / 2].x = c[0];
+      else v[e / 2].y = c[0];
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; k += 2) v[(e * V + k) / 2] = make_float2(c[k], c[k + 1]);
+    }
+  }
+}
+template <typename T, int kElems, int kGroup, int V, typename F>
+__device__ __forceinline__ void store_columns(T* p, F inside, const float2 (&v)[kElems / 2]) {
+#pragma unroll
+  for (int e = 0; e < kElems / V; ++e) {
+    float c[V];
+    if constexpr (V == 1) {
+      c[0] = e % 2 == 0 ? v[e / 2].x : v[e / 2].y;
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; k += 2) {
+        c[k] = v[(e * V + k) / 2].x;
+        c[k + 1] = v[(e * V + k) / 2].y;
+      }
+    }
+    if (inside(e)) store<T, V>(p + e * kGroup * V, c);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float2 rounded(float2 v) {
+  return make_float2(Elem<T>::to(Elem<T>::from(v.x)), Elem<T>::to(Elem<T>::from(v.y)));
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -219,16 +283,11 @@ struct Ring {
         bulk_load(dst + m * slot, reinterpret_cast<const uint8_t*>(p) - lead(p), part[m], &full[s]);
       }
   }
-  // the matrices' pointers to row `row`: in shared memory (or, should the copies not have
-  // come, in memory itself)
-  __device__ void take(int64_t row, const T* (&p)[3]) const {
-    const bool here = sm100::mbar_wait_bounded(&full[stage], phase, nullptr, kWait);
-    const uint8_t* src = smem + (size_t)stage * n * slot;
-#pragma unroll
-    for (int m = 0; m < 3; ++m) {
-      const T* q = m < n ? row_of(m, row) : nullptr;
-      p[m] = m < n && here ? reinterpret_cast<const T*>(src + m * slot + lead(q)) : q;
-    }
+  // Waits for the stage of row `row`; the matrices' places in it are then at(m, row).  False: the
+  // copies have not come within the limit, and the row's results are NaN.
+  __device__ bool ready() const { return sm100::mbar_wait_bounded(&full[stage], phase, nullptr, kWait); }
+  __device__ const T* at(int m, int64_t row) const {
+    return reinterpret_cast<const T*>(smem + (size_t)(stage * n + m) * slot + lead(row_of(m, row)));
   }
   __device__ void advance() {
     if (++stage == stages) {

@@ -12,8 +12,8 @@ using namespace ln;
 template <typename T, typename TW, int kGroup, int kElems, int V, bool kRing>
 __global__ void __launch_bounds__(block_of(kGroup), resident_of(kGroup, kElems, true))
 backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
-  constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup, kE = kElems / V;
-  static_assert(kE > 0, "rows in registers");
+  constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup;
+  static_assert(kElems > 0, "rows in registers");
   __shared__ float buf[2][2][32];
   __shared__ uint64_t full[kGroups][kMaxStages];
   extern __shared__ __align__(128) uint8_t dyn[];   // the ring; then dw and db of each warp
@@ -32,15 +32,17 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   }
   pdl_wait();
   pdl_trigger();
-  const TW* w = static_cast<const TW*>(a.weight);
-  float wv[kE][V], dw[kE][V], db[kE][V];
+  const int col = t * V;                       // this thread's chunks: every kGroup V columns
+  const auto inside = [&](int e) { return e * kGroup * V + col < (int)cols; };
+  constexpr int kPairs = kElems / 2;
+  float2 wv[kPairs], dw[kPairs], db[kPairs];
 #pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    const int64_t j = ((int64_t)e * kGroup + t) * V;
-#pragma unroll
-    for (int k = 0; k < V; ++k) { wv[e][k] = 1.0f; dw[e][k] = db[e][k] = 0.0f; }
-    if (w && j < cols) load<TW, V, true>(w + j, wv[e]);
+  for (int i = 0; i < kPairs; ++i) {
+    wv[i] = both(1.0f);
+    dw[i] = db[i] = both(0.0f);
   }
+  if (a.weight)
+    load_columns<TW, kElems, kGroup, V, true>(static_cast<const TW*>(a.weight) + col, inside, 0.0f, wv);
   const int64_t stride = (int64_t)gridDim.x * kGroups;
   const int64_t row0 = (int64_t)blockIdx.x * kGroups + grp;
   if constexpr (kRing) {
@@ -55,38 +57,35 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   for (int64_t step = 0; first + step < a.rows; step += stride, flip ^= 1) {
     const bool live = kGroup >= 32 || row0 + step < a.rows;
     const int64_t row = live ? row0 + step : a.rows - 1;
-    const T* src[3] = {ring.row_of(0, row), ring.row_of(1, row), a.r ? ring.row_of(2, row) : nullptr};
-    T* dx = static_cast<T*>(a.dx) + row * a.lddx;
-    const float mean = live ? mean_next : 0.0f, rstd = live ? rstd_next : 0.0f;
+    T* dx = static_cast<T*>(a.dx) + row * a.lddx + col;
+    float mean = live ? mean_next : 0.0f;
+    const float rstd = live ? rstd_next : 0.0f;
     if (row0 + step + stride < a.rows) {
       mean_next = a.mean[row0 + step + stride];
       rstd_next = a.rstd[row0 + step + stride];
     }
-    if constexpr (kRing) ring.take(row, src);
-    float xh[kE][V], g[kE][V];
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int64_t j = ((int64_t)e * kGroup + t) * V;
-      if (live && j < cols) {
-        load<T, V>(src[0] + j, xh[e]);
-        load<T, V>(src[1] + j, g[e]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) { xh[e][k] = mean; g[e][k] = 0.0f; }
-      }
+    const auto here = [&](int e) { return live && inside(e); };
+    float2 xh[kPairs], g[kPairs];
+    if constexpr (kRing) {
+      if (!ring.ready()) mean = __int_as_float(0x7FC00000);
+      load_columns<T, kElems, kGroup, V, false>(ring.at(0, row) + col, here, mean, xh);
+      load_columns<T, kElems, kGroup, V, false>(ring.at(1, row) + col, here, 0.0f, g);
+    } else {
+      load_columns<T, kElems, kGroup, V, true>(ring.row_of(0, row) + col, here, mean, xh);
+      load_columns<T, kElems, kGroup, V, true>(ring.row_of(1, row) + col, here, 0.0f, g);
     }
-    float s1 = 0.0f, s2 = 0.0f;
+    float2 p1 = both(0.0f), p2 = both(0.0f);
+    const float2 minus = both(-mean), scale = both(rstd);
 #pragma unroll
-    for (int e = 0; e < kE; ++e)
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        xh[e][k] = (xh[e][k] - mean) * rstd;
-        db[e][k] += g[e][k];
-        dw[e][k] = fmaf(g[e][k], xh[e][k], dw[e][k]);
-        g[e][k] *= wv[e][k];
-        s1 += g[e][k];
-        s2 = fmaf(g[e][k], xh[e][k], s2);
-      }
+    for (int i = 0; i < kPairs; ++i) {
+      xh[i] = mul2(add2(xh[i], minus), scale);
+      db[i] = add2(db[i], g[i]);
+      dw[i] = fma2(g[i], xh[i], dw[i]);
+      g[i] = mul2(g[i], wv[i]);
+      p1 = add2(p1, g[i]);
+      p2 = fma2(g[i], xh[i], p2);
+    }
+    float s1 = p1.x + p1.y, s2 = p2.x + p2.y;
 #pragma unroll
     for (int o = (kGroup < 32 ? kGroup : 32) / 2; o > 0; o >>= 1) {
       s1 += __shfl_xor_sync(0xffffffffu, s1, o);
@@ -103,23 +102,16 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
       s1 = warp_sum(lane < kWarps ? buf[flip][0][lane] : 0.0f);
       s2 = warp_sum(lane < kWarps ? buf[flip][1][lane] : 0.0f);
     }
-    s1 *= inv_n;
-    s2 *= inv_n;
+    const float2 m1 = both(-s1 * inv_n), m2 = both(-s2 * inv_n);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int64_t j = ((int64_t)e * kGroup + t) * V;
-      if (!live || j >= cols) continue;
-      float o[V];
+    for (int i = 0; i < kPairs; ++i) g[i] = mul2(scale, fma2(xh[i], m2, add2(g[i], m1)));
+    if (a.r) {
+      if constexpr (kRing) load_columns<T, kElems, kGroup, V, false>(ring.at(2, row) + col, here, 0.0f, xh);
+      else load_columns<T, kElems, kGroup, V, true>(ring.row_of(2, row) + col, here, 0.0f, xh);
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = rstd * (g[e][k] - s1 - xh[e][k] * s2);
-      if (a.r) {
-        float q[V];
-        load<T, V>(src[2] + j, q);
-#pragma unroll
-        for (int k = 0; k < V; ++k) o[k] += q[k];
-      }
-      store<T, V>(dx + j, o);
+      for (int i = 0; i < kPairs; ++i) g[i] = add2(g[i], xh[i]);
     }
+    store_columns<T, kElems, kGroup, V>(dx, here, g);
     if constexpr (kRing) {
       // every thread of the group has read the stage: the row `stages` ahead may have it
       if constexpr (kGroup > 32) {
@@ -135,37 +127,24 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   if constexpr (kGroups > 1) {
     // the warps' sums meet in shared memory, added in warp order
     float* joined = reinterpret_cast<float*>(dyn);
-    const int width = kE * kGroup * V;
+    constexpr int kWidth = kElems * kGroup;
+    const auto all = [](int) { return true; };
     __syncthreads();                            // the rings are no longer read
-#pragma unroll
-    for (int e = 0; e < kE; ++e)
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        joined[(grp * 2 + 0) * width + (e * kGroup + t) * V + k] = dw[e][k];
-        joined[(grp * 2 + 1) * width + (e * kGroup + t) * V + k] = db[e][k];
-      }
+    store_columns<float, kElems, kGroup, V>(joined + (grp * 2 + 0) * kWidth + col, all, dw);
+    store_columns<float, kElems, kGroup, V>(joined + (grp * 2 + 1) * kWidth + col, all, db);
     __syncthreads();
-    for (int j = threadIdx.x; j < 2 * width; j += kBlock) {
-      const int which = j / width, c = j % width;
+    for (int j = threadIdx.x; j < 2 * kWidth; j += kBlock) {
+      const int which = j / kWidth, c = j % kWidth;
       if (c >= cols) continue;
       float s = 0.0f;
-      for (int q = 0; q < kGroups; ++q) s += joined[(q * 2 + which) * width + c];
+      for (int q = 0; q < kGroups; ++q) s += joined[(q * 2 + which) * kWidth + c];
       a.partial[((int64_t)blockIdx.x * 2 + which) * cols + c] = s;
     }
   } else {
-    float* p = a.partial + (int64_t)blockIdx.x * 2 * cols;
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int64_t j = ((int64_t)e * kGroup + t) * V;
-      if (j >= cols) continue;
-      if constexpr (V == 1) {
-        p[j] = dw[e][0];
-        p[cols + j] = db[e][0];
-      } else {
-        store<float, V>(p + j, dw[e]);          // (V divides cols: 16-byte aligned)
-        store<float, V>(p + cols + j, db[e]);
-      }
-    }
+    // (V divides cols: 16-byte aligned)
+    float* p = a.partial + (int64_t)blockIdx.x * 2 * cols + col;
+    store_columns<float, kElems, kGroup, V>(p, inside, dw);
+    store_columns<float, kElems, kGroup, V>(p + cols, inside, db);
   }
 }
 
