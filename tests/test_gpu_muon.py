@@ -85,6 +85,24 @@ def test_orthogonalize_matches_the_definition(lib, gpu, m, n, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,pad", [(48, 7680, 0), (7681, 33, 3), (130, 8192, 0), (200, 6001, 1),
+                                     (4097, 257, 0)])
+def test_few_rows_of_great_length(lib, gpu, m, n, pad, dtype):
+    """Gram's K in several parts, whose sums are added in one order whoever finishes last."""
+    from paper_2608_15665_gb300 import firstorder as fo
+    G = gauss(m, n, dtype, gpu, 13, pad, spread=0.5)
+    op = fo.Orthogonalizer([G, G])
+    first = [o.clone() for o in op()]
+    for _ in range(8):
+        again = op()
+    op.sync()
+    check(first[0], ns(f64(G)), dtype)
+    for t in (first[1], again[0], again[1]):
+        assert torch.equal(first[0], t)
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ill_conditioned_matrices(lib, gpu, dtype):
     """Singular values falling as 1 / k, and a few strong directions over a noise floor: the
     small ones end far from 1, and are those that rounding noise meets first."""
