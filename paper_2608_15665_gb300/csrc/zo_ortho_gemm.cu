@@ -77,6 +77,19 @@ __device__ __forceinline__ void give_up(Shared& sh, uint32_t* status) {
   store_peer(&sh.abort_flag, 1);
 }
 
+// Whether the barrier's phase is over, without the wait that try_wait may make of it.
+__device__ __forceinline__ bool mbar_done(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Descriptor of an MN-major operand in 128-byte swizzled blocks of 64 columns x 64 K-rows:
 // K-rows 128 bytes apart, groups of eight 1024 bytes apart (stride offset), blocks of 64
 // columns 8192 bytes apart (leading offset).
@@ -161,7 +174,9 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   constexpr int kStages = kRing / kStageBytes < 8 ? kRing / kStageBytes : 8;
   constexpr int kBufs = kTmemCols / kCols < 4 ? kTmemCols / kCols : 4;
   constexpr int kWarpCols = kCols / 2, kChunks = kWarpCols / 32;
-  static_assert(kStages <= 8 && kBufs <= 4 && sizeof(Shared) <= 1024);
+  // a pair's stage is one accumulation: the barrier that tells the epilogue that it is done
+  // tells the producer that the stage is free
+  static_assert(kStages <= 8 && kBufs <= 4 && sizeof(Shared) <= 1024 && (!kPairs || kStages == kBufs));
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -173,6 +188,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   const int pair = blockIdx.x >> 1;
   const int t_begin = first[pair], t_end = first[pair + 1];
   const volatile int* abort = &sh.abort_flag;
+  uint64_t* const released = kPairs ? sh.acc_full : sh.empty;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -213,7 +229,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       const CUtensorMap* bl = bh + (phase == kOrthoPoly ? 1 : 2);
       const int i0 = tl.i0 + 128 * (int)rank, j0 = tl.j0 + kCols / 2 * (int)rank;
       for (int k0 = 64 * tl.k0; k0 < 64 * tl.k1; k0 += 64) {
-        if (!mbar_wait_bounded(&sh.empty[stage], free_parity, abort, kWait)) {
+        if (!mbar_wait_bounded(&released[stage], free_parity, abort, kWait)) {
           ok = false;
           break;
         }
@@ -246,7 +262,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     for (int s = 0; s < kStages; ++s) {
       const int64_t last = tc::last_in_slot(filled, s, kStages);
       if (last >= 0)
-        mbar_wait_bounded(&sh.empty[s], (uint32_t)((last / kStages) & 1), nullptr, kWait);
+        mbar_wait_bounded(&released[s], (uint32_t)((last / kStages) & 1), nullptr, kWait);
     }
   } else if (warp == 1 && lane == 0 && leader) {
     // ---------------------------------------------------------------- MMA issuer (leader)
@@ -265,59 +281,33 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     uint32_t parity = 0, acc_parity = 1;
     bool ok = true, seen = false;              // seen: full[stage] has been found complete
     for (int t = t_begin; t < t_end && ok; ++t) {
-      int left = tiles[t].k1 - tiles[t].k0;
-      while (left > 0) {
-        const int n = kPairs ? 1 : left;
+      const int n = tiles[t].k1 - tiles[t].k0;
+      if constexpr (!kPairs) {
         if (!mbar_wait_bounded(&sh.acc_empty[acc], acc_parity, abort, kWait)) {
           ok = false;
           break;
         }
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(acc * kCols);
-        if constexpr (!kPairs) {
-          uint32_t add = 0;
-          for (int k = 0; k < n; ++k) {
-            if (!seen && !mbar_wait_bounded(&sh.full[stage], parity, abort, kWait)) {
-              ok = false;
-              break;
-            }
-            const uint64_t ad = a_first + (uint64_t)stage * kStageStep;
-            const uint64_t bd = b_first + (uint64_t)stage * kStageStep;
-            mma_pair_ss(d, ad, bd, idesc, add);
-            add = 1;
-            mma_pair_ss(d, ad + 2, bd + b_step, idesc, 1);
-            uint64_t* done = &sh.empty[stage];
-            if (++stage == kStages) {
-              stage = 0;
-              parity ^= 1u;
-            }
-            seen = mbar_try_wait(&sh.full[stage], parity);
-            mma_pair_ss(d, ad + 4, bd + 2 * b_step, idesc, 1);
-            mma_pair_ss(d, ad + 6, bd + 3 * b_step, idesc, 1);
-            commit_both(done);
-          }
-        } else {
-          // one stage: hi.lo, lo.hi, hi.hi
+        uint32_t add = 0;
+        for (int k = 0; k < n; ++k) {
           if (!seen && !mbar_wait_bounded(&sh.full[stage], parity, abort, kWait)) {
             ok = false;
             break;
           }
           const uint64_t ad = a_first + (uint64_t)stage * kStageStep;
           const uint64_t bd = b_first + (uint64_t)stage * kStageStep;
+          mma_pair_ss(d, ad, bd, idesc, add);
+          add = 1;
+          mma_pair_ss(d, ad + 2, bd + b_step, idesc, 1);
           uint64_t* done = &sh.empty[stage];
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            mma_pair_ss(d, ad + 2 * kk, bd + kLoStep + b_step * kk, idesc, kk != 0 ? 1u : 0u);
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            mma_pair_ss(d, ad + kLoStep + 2 * kk, bd + b_step * kk, idesc, 1);
           if (++stage == kStages) {
             stage = 0;
             parity ^= 1u;
           }
-          seen = mbar_try_wait(&sh.full[stage], parity);
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) mma_pair_ss(d, ad + 2 * kk, bd + b_step * kk, idesc, 1);
+          seen = mbar_done(&sh.full[stage], parity);
+          mma_pair_ss(d, ad + 4, bd + 2 * b_step, idesc, 1);
+          mma_pair_ss(d, ad + 6, bd + 3 * b_step, idesc, 1);
           commit_both(done);
         }
         if (!ok) break;
@@ -326,7 +316,38 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
           acc = 0;
           acc_parity ^= 1u;
         }
-        left -= n;
+      } else {
+        // two stages at a time, each hi.lo + lo.hi + hi.hi: an MMA that adds to the last one's
+        // sums waits for them, so the two accumulators take turns
+        const auto ready = [&](int at, uint32_t par) {
+          return mbar_wait_bounded(&sh.acc_empty[at], par ^ 1u, abort, kWait) &&
+                 mbar_wait_bounded(&sh.full[at], par, abort, kWait);
+        };
+        for (int k = 0; k < n; k += 2) {
+          const int s0 = stage;
+          const int s1 = s0 + 1 == kStages ? 0 : s0 + 1;
+          const bool two = k + 1 < n;
+          const uint32_t parity1 = s1 ? parity : parity ^ 1u;
+          if (!ready(s0, parity) || (two && !ready(s1, parity1))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint64_t ad[2] = {a_first + (uint64_t)s0 * kStageStep, a_first + (uint64_t)s1 * kStageStep};
+          const uint64_t bd[2] = {b_first + (uint64_t)s0 * kStageStep, b_first + (uint64_t)s1 * kStageStep};
+          const uint32_t d[2] = {tmem + (uint32_t)(s0 * kCols), tmem + (uint32_t)(s1 * kCols)};
+#pragma unroll
+          for (int e = 0; e < 12; ++e) {
+            const uint64_t a_at = 2 * (e % 4) + (e / 4 == 1 ? kLoStep : 0);
+            const uint64_t b_at = b_step * (e % 4) + (e / 4 == 0 ? kLoStep : 0);
+            mma_pair_ss(d[0], ad[0] + a_at, bd[0] + b_at, idesc, e != 0 ? 1u : 0u);
+            if (two) mma_pair_ss(d[1], ad[1] + a_at, bd[1] + b_at, idesc, e != 0 ? 1u : 0u);
+          }
+          commit_both(&sh.acc_full[s0]);
+          if (two) commit_both(&sh.acc_full[s1]);
+          stage = two ? (s1 + 1 == kStages ? 0 : s1 + 1) : s1;
+          parity = two ? (stage ? parity1 : parity1 ^ 1u) : parity1;
+        }
       }
     }
     if (!ok) give_up(sh, status);
