@@ -75,6 +75,20 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// the same, m16n8k8
+__device__ __forceinline__ void mma_k8(float (&d)[4], const uint32_t (&a)[2], uint32_t b) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(b));
+}
+// an 8 x 8 matrix of halves, a row's pair per lane, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
 __device__ __forceinline__ float2 pair2(const __half* hi, const __half* lo) {
   const float2 h = __half22float2(*reinterpret_cast<const __half2*>(hi));
   const float2 l = __half22float2(*reinterpret_cast<const __half2*>(lo));
@@ -172,6 +186,83 @@ __device__ __forceinline__ void apply(__half* xh, __half* xl, const __half* bh, 
       }
 }
 
+// X of at most eight rows in registers: a warp's kTiles x 16 columns (tile warp + 8 i), as the A
+// operand of X'^T = a X^T + X^T B: lane (g, t) holds rows 2 t, 2 t + 1 of columns g and g + 8.
+// That is also how the product's sums lie, so Apply reads nothing but B; Gram's operands are the
+// same 8 x 8 blocks transposed.  (Sixteen rows would take twice the registers: three CTAs an SM,
+// 80 registers a thread, spilled and were slower than shared memory.)
+constexpr int kTiles = 5;
+struct Columns {
+  uint32_t hi[kTiles][2], lo[kTiles][2];
+};
+__device__ __forceinline__ int tile_col(int i) { return 16 * ((int)(threadIdx.x >> 5) + kWarps * i); }
+// from the planes' fp32 values
+__device__ __forceinline__ void take(Columns& x, const __half* xh, const __half* xl, int pitch, int cs,
+                                     float inv, float scale) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    if (tile_col(i) >= cs) break;
+    uint32_t up[4], low[4];                           // (rows 8 .. 15 are not used)
+    const int at = (lane & 15) * pitch + tile_col(i) + (lane >> 4) * 8;
+    ldmatrix_x4_trans(up, smem_u32(xh + at));
+    ldmatrix_x4_trans(low, smem_u32(xl + at));
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      split2(first_of(up[2 * q], low[2 * q]) * inv * scale, second_of(up[2 * q], low[2 * q]) * inv * scale,
+             reinterpret_cast<__half*>(&x.hi[i][q]), reinterpret_cast<__half*>(&x.lo[i][q]));
+  }
+}
+// the warp's share of X X^T
+__device__ __forceinline__ void gram(const Columns& x, int cs, float* to) {
+  constexpr int kPitch = Shape<16>::kPitch;
+  const int lane = threadIdx.x & 31;
+  float small[4] = {}, large[4] = {};                 // hi.lo + lo.hi, and hi.hi
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    if (tile_col(i) >= cs) break;
+    const uint32_t h[4] = {transposed(x.hi[i][0]), 0, transposed(x.hi[i][1]), 0};
+    const uint32_t l[4] = {transposed(x.lo[i][0]), 0, transposed(x.lo[i][1]), 0};
+    mma(small, h, l[0], l[2]);
+    mma(large, h, h[0], h[2]);
+    mma(small, l, h[0], h[2]);
+  }
+  const float2 v = make_float2(small[0] + large[0], small[1] + large[1]);
+  float* at = to + (lane >> 2) * kPitch + (lane & 3) * 2;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)                         // the rest of 16 x 16 is zero
+    *reinterpret_cast<float2*>(at + (q & 1) * 8 + (q >> 1) * 8 * kPitch) = q == 0 ? v : make_float2(0.f, 0.f);
+}
+// X' = a X + B X; the last step's fp32 values go to the planes
+__device__ __forceinline__ void apply(Columns& x, int cs, const __half* bh, const __half* bl, __half* xh,
+                                      __half* xl, int pitch, float s0, float s1, bool last) {
+  const int lane = threadIdx.x & 31;
+  const int own = (lane >> 2) * Shape<16>::kPitch + (lane & 3) * 2;
+  const uint32_t b_hi = *reinterpret_cast<const uint32_t*>(bh + own);
+  const uint32_t b_lo = *reinterpret_cast<const uint32_t*>(bl + own);
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    if (tile_col(i) >= cs) break;
+    float d[4] = {};
+    mma_k8(d, x.hi[i], b_lo);
+    mma_k8(d, x.lo[i], b_hi);
+    mma_k8(d, x.hi[i], b_hi);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float2 o = pair2(reinterpret_cast<const __half*>(&x.hi[i][q]),
+                             reinterpret_cast<const __half*>(&x.lo[i][q]));
+      const float v0 = fmaf(s0, o.x, s1 * d[2 * q]), v1 = fmaf(s0, o.y, s1 * d[2 * q + 1]);
+      if (last) {
+        const int at = (lane >> 2) * pitch + tile_col(i) + 8 * q + (lane & 3) * 2;
+        *reinterpret_cast<uint32_t*>(xh + at) = transposed(upper2(v0, v1));
+        *reinterpret_cast<uint32_t*>(xl + at) = transposed(lower2(v0, v1));
+      } else {
+        split2(v0, v1, reinterpret_cast<__half*>(&x.hi[i][q]), reinterpret_cast<__half*>(&x.lo[i][q]));
+      }
+    }
+  }
+}
+
 template <int P>
 __global__ void __launch_bounds__(kThreads, P == 16 ? 3 : 2)
 ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ which, int cluster,
@@ -230,26 +321,34 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
   }
   const float inv = inverse_norm<kThreads>(sq, u.eps, cluster, sums);
   const float s_in = exp2i(steps.s[0].ex);
-  for (int e = tid; e < P * pitch / 8; e += kThreads) {
-    uint4* ph = reinterpret_cast<uint4*>(xh) + e;
-    uint4* pl = reinterpret_cast<uint4*>(xl) + e;
-    const uint4 h = *ph, l = *pl;
-    const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
-    float v[8];
+  const bool in_registers = P == 16 && mt.p <= 8 && cs <= 16 * kTiles * kWarps;
+  Columns x;
+  if (in_registers) {
+    take(x, xh, xl, pitch, cs, inv, s_in);
+  } else {
+    for (int e = tid; e < P * pitch / 8; e += kThreads) {
+      uint4* ph = reinterpret_cast<uint4*>(xh) + e;
+      uint4* pl = reinterpret_cast<uint4*>(xl) + e;
+      const uint4 h = *ph, l = *pl;
+      const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+      float v[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[2 * k] = first_of(hw[k], lw[k]) * inv;
-      v[2 * k + 1] = second_of(hw[k], lw[k]) * inv;
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = first_of(hw[k], lw[k]) * inv;
+        v[2 * k + 1] = second_of(hw[k], lw[k]) * inv;
+      }
+      tc::split8_f16(v, s_in, *ph, *pl);
     }
-    tc::split8_f16(v, s_in, *ph, *pl);
+    __syncthreads();
   }
-  __syncthreads();
 
   // ---------------------------------------------------------------- the steps
   const int row = lane >> 2, col = (lane & 3) * 2;     // of a sum's first two values
   for (int k = 0; k < steps.n; ++k) {
     const OrthoStep st = steps.s[k];
-    {
+    if (in_registers) {
+      gram(x, cs, part + warp * S::kSumFloats);
+    } else {
       // ---- X X^T: rows 16 m, columns 8 (kN n0 ..), K tiles split, split + kSplits, ...
       const int m = warp % S::kM, split = warp / S::kM % S::kSplits, n0 = warp / (S::kM * S::kSplits) * S::kN;
       float d[S::kN][4] = {};
@@ -380,7 +479,9 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
       const float s0 = st.a * exp2i(st.last ? -st.ex : st.ex_next - st.ex);
       const float s1 = exp2i((st.last ? 0 : st.ex_next) - st.ex - st.eb);
       const bool last = st.last != 0;
-      if (P < 64 && cs <= 8 * kWarps) {
+      if (in_registers) {
+        apply(x, cs, bh, bl, xh, xl, pitch, s0, s1, last);
+      } else if (P < 64 && cs <= 8 * kWarps) {
         if (8 * warp < cs) apply<P, 1>(xh, xl, bh, bl, pitch, 8 * warp, s0, s1, last);
       } else {
         // (a multiple of 16 columns is left over at most, inside the row's padding)
