@@ -40,6 +40,7 @@
 #include "zo_cluster.cuh"
 #include "zo_launch.cuh"
 #include "zo_ops.h"
+#include "zo_ortho_io.cuh"
 #include "zo_sm100.cuh"
 #include "zo_tc_common.cuh"
 
@@ -48,6 +49,7 @@ namespace {
 
 using namespace sm100;
 using namespace cta2;
+using ortho::elected;
 using tc::exp2i;
 
 constexpr int kTileRows = 256;
@@ -77,17 +79,9 @@ __device__ __forceinline__ void give_up(Shared& sh, uint32_t* status) {
   store_peer(&sh.abort_flag, 1);
 }
 
-// Whether the barrier's phase is over, without the wait that try_wait may make of it.
-__device__ __forceinline__ bool mbar_done(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
+// a wait by a whole warp, the same for every lane
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort, kWait)) != 0;
 }
 
 // Descriptor of an MN-major operand in 128-byte swizzled blocks of 64 columns x 64 K-rows:
@@ -212,7 +206,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   pdl_wait();
   pdl_trigger();
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0) {
     // ---------------------------------------------------------------- operands (this CTA)
     int stage = 0;
     uint32_t free_parity = 1;                  // of empty[stage]: the first round needs no wait
@@ -229,27 +223,30 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       const CUtensorMap* bl = bh + (phase == kOrthoPoly ? 1 : 2);
       const int i0 = tl.i0 + 128 * (int)rank, j0 = tl.j0 + kCols / 2 * (int)rank;
       for (int k0 = 64 * tl.k0; k0 < 64 * tl.k1; k0 += 64) {
-        if (!mbar_wait_bounded(&released[stage], free_parity, abort, kWait)) {
+        if (!warp_wait(&released[stage], free_parity, abort)) {
           ok = false;
           break;
         }
-        uint64_t* full = &sh.full[stage];
-        if (leader) mbar_arrive_expect_tx(full, 2 * kStageBytes);
-        // hi parts of A and B, then the lo parts
-        uint8_t* dst = smem + stage * kStageBytes;
+        if (elected()) {
+          uint64_t* full = &sh.full[stage];
+          if (leader) mbar_arrive_expect_tx(full, 2 * kStageBytes);
+          // hi parts of A and B, then the lo parts
+          uint8_t* dst = smem + stage * kStageBytes;
 #pragma unroll
-        for (int part = 0; part < (kPairs ? 2 : 1); ++part) {
-          const CUtensorMap* a = part ? al : ah;
-          const CUtensorMap* bm = part ? bl : bh;
+          for (int part = 0; part < (kPairs ? 2 : 1); ++part) {
+            const CUtensorMap* a = part ? al : ah;
+            const CUtensorMap* bm = part ? bl : bh;
 #pragma unroll
-          for (int q = 0; q < 2; ++q, dst += kBlockBytes)
-            tma_load_2d_to_leader(dst, a, k0, i0 + 64 * q, full);
+            for (int q = 0; q < 2; ++q, dst += kBlockBytes)
+              tma_load_2d_to_leader(dst, a, k0, i0 + 64 * q, full);
 #pragma unroll
-          for (int q = 0; q < kBBoxes; ++q, dst += kBlockBytes) {
-            if (phase == kOrthoApply) tma_load_2d_to_leader(dst, bm, j0 + 64 * q, k0, full);
-            else tma_load_2d_to_leader(dst, bm, k0, j0 + 64 * q, full);
+            for (int q = 0; q < kBBoxes; ++q, dst += kBlockBytes) {
+              if (phase == kOrthoApply) tma_load_2d_to_leader(dst, bm, j0 + 64 * q, k0, full);
+              else tma_load_2d_to_leader(dst, bm, k0, j0 + 64 * q, full);
+            }
           }
         }
+        __syncwarp();
         ++filled;
         if (++stage == kStages) {
           stage = 0;
@@ -257,19 +254,18 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         }
       }
     }
-    if (!ok) give_up(sh, status);
+    if (!ok && lane == 0) give_up(sh, status);
     // the leader's MMAs have released every stage this CTA filled
     for (int s = 0; s < kStages; ++s) {
       const int64_t last = tc::last_in_slot(filled, s, kStages);
       if (last >= 0)
         mbar_wait_bounded(&released[s], (uint32_t)((last / kStages) & 1), nullptr, kWait);
     }
-  } else if (warp == 1 && lane == 0 && leader) {
+  } else if (warp == 1 && leader) {
     // ---------------------------------------------------------------- MMA issuer (leader)
-    // One thread feeds the tensor cores of two SMs, an MMA every ~140 cycles, and every
-    // instruction between two MMAs is time they may lose: descriptors and barriers move by
-    // additions (with 64-bit remainders in this loop a stage of 64 took 715 to 906 cycles),
-    // and the next stage's barrier is looked at between this one's MMAs.
+    // One lane feeds the tensor cores of two SMs, an MMA every 64 (pairs) or 128 cycles, and
+    // every instruction between two MMAs is time they may lose: descriptors and barriers move
+    // by additions (with 64-bit remainders in this loop a stage of 64 took 715 to 906 cycles).
     const bool mn = phase == kOrthoApply;
     const uint32_t idesc = idesc_f16_f32(kTileRows, kCols) | (mn ? kMnMajorB : 0u);
     const uint32_t ring = smem_u32(smem);
@@ -279,80 +275,59 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     const uint64_t b_step = (mn ? 2048 : 32) >> 4;
     int stage = 0, acc = 0;
     uint32_t parity = 0, acc_parity = 1;
-    bool ok = true, seen = false;              // seen: full[stage] has been found complete
+    bool ok = true;
     for (int t = t_begin; t < t_end && ok; ++t) {
       const int n = tiles[t].k1 - tiles[t].k0;
       if constexpr (!kPairs) {
-        if (!mbar_wait_bounded(&sh.acc_empty[acc], acc_parity, abort, kWait)) {
+        if (!warp_wait(&sh.acc_empty[acc], acc_parity, abort)) {
+          ok = false;
+          break;
+        }
+      }
+      for (int k = 0; k < n; ++k) {
+        // a pair's stage is an accumulation of its own
+        if (kPairs && !warp_wait(&sh.acc_empty[stage], parity ^ 1u, abort)) ok = false;
+        if (!ok || !warp_wait(&sh.full[stage], parity, abort)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        const uint32_t d = tmem + (uint32_t)(acc * kCols);
-        uint32_t add = 0;
-        for (int k = 0; k < n; ++k) {
-          if (!seen && !mbar_wait_bounded(&sh.full[stage], parity, abort, kWait)) {
-            ok = false;
-            break;
+        const uint64_t ad = a_first + (uint64_t)stage * kStageStep;
+        const uint64_t bd = b_first + (uint64_t)stage * kStageStep;
+        const uint32_t d = tmem + (uint32_t)((kPairs ? stage : acc) * kCols);
+        if (elected()) {
+          if constexpr (kPairs) {
+            // hi.lo, lo.hi, hi.hi
+#pragma unroll
+            for (int e = 0; e < 12; ++e)
+              mma_pair_ss(d, ad + 2 * (e % 4) + (e / 4 == 1 ? kLoStep : 0),
+                          bd + b_step * (e % 4) + (e / 4 == 0 ? kLoStep : 0), idesc, e != 0 ? 1u : 0u);
+            commit_both(&sh.acc_full[stage]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              mma_pair_ss(d, ad + 2 * e, bd + b_step * e, idesc, e != 0 || k != 0 ? 1u : 0u);
+            commit_both(&sh.empty[stage]);
+            if (k + 1 == n) commit_both(&sh.acc_full[acc]);
           }
-          const uint64_t ad = a_first + (uint64_t)stage * kStageStep;
-          const uint64_t bd = b_first + (uint64_t)stage * kStageStep;
-          mma_pair_ss(d, ad, bd, idesc, add);
-          add = 1;
-          mma_pair_ss(d, ad + 2, bd + b_step, idesc, 1);
-          uint64_t* done = &sh.empty[stage];
-          if (++stage == kStages) {
-            stage = 0;
-            parity ^= 1u;
-          }
-          seen = mbar_done(&sh.full[stage], parity);
-          mma_pair_ss(d, ad + 4, bd + 2 * b_step, idesc, 1);
-          mma_pair_ss(d, ad + 6, bd + 3 * b_step, idesc, 1);
-          commit_both(done);
         }
-        if (!ok) break;
-        commit_both(&sh.acc_full[acc]);
+        __syncwarp();
+        if (++stage == kStages) {
+          stage = 0;
+          parity ^= 1u;
+        }
+      }
+      if constexpr (!kPairs) {
         if (++acc == kBufs) {
           acc = 0;
           acc_parity ^= 1u;
         }
-      } else {
-        // two stages at a time, each hi.lo + lo.hi + hi.hi: an MMA that adds to the last one's
-        // sums waits for them, so the two accumulators take turns
-        const auto ready = [&](int at, uint32_t par) {
-          return mbar_wait_bounded(&sh.acc_empty[at], par ^ 1u, abort, kWait) &&
-                 mbar_wait_bounded(&sh.full[at], par, abort, kWait);
-        };
-        for (int k = 0; k < n; k += 2) {
-          const int s0 = stage;
-          const int s1 = s0 + 1 == kStages ? 0 : s0 + 1;
-          const bool two = k + 1 < n;
-          const uint32_t parity1 = s1 ? parity : parity ^ 1u;
-          if (!ready(s0, parity) || (two && !ready(s1, parity1))) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint64_t ad[2] = {a_first + (uint64_t)s0 * kStageStep, a_first + (uint64_t)s1 * kStageStep};
-          const uint64_t bd[2] = {b_first + (uint64_t)s0 * kStageStep, b_first + (uint64_t)s1 * kStageStep};
-          const uint32_t d[2] = {tmem + (uint32_t)(s0 * kCols), tmem + (uint32_t)(s1 * kCols)};
-#pragma unroll
-          for (int e = 0; e < 12; ++e) {
-            const uint64_t a_at = 2 * (e % 4) + (e / 4 == 1 ? kLoStep : 0);
-            const uint64_t b_at = b_step * (e % 4) + (e / 4 == 0 ? kLoStep : 0);
-            mma_pair_ss(d[0], ad[0] + a_at, bd[0] + b_at, idesc, e != 0 ? 1u : 0u);
-            if (two) mma_pair_ss(d[1], ad[1] + a_at, bd[1] + b_at, idesc, e != 0 ? 1u : 0u);
-          }
-          commit_both(&sh.acc_full[s0]);
-          if (two) commit_both(&sh.acc_full[s1]);
-          stage = two ? (s1 + 1 == kStages ? 0 : s1 + 1) : s1;
-          parity = two ? (stage ? parity1 : parity1 ^ 1u) : parity1;
-        }
       }
     }
-    if (!ok) give_up(sh, status);
+    if (!ok && lane == 0) give_up(sh, status);
     // every MMA has completed before Tensor Memory is freed
-    commit_both(&sh.drain);
+    if (elected()) commit_both(&sh.drain);
+    __syncwarp();
     mbar_wait_bounded(&sh.drain, 0u, nullptr, kWait);
   } else if (warp >= 2) {
     // ---------------------------------------------------------------- epilogue (each CTA)

@@ -237,6 +237,7 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     tc_fence_after();
   };
   const auto wait_mma = [&]() {
+    __syncwarp();
     if (!mbar_wait_bounded(&sh.done, parity, nullptr, kWait) && lane == 0) atomicOr(status, 1u);
     parity ^= 1u;
     __syncwarp();
@@ -267,7 +268,7 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     const OrthoStep st = steps.s[k];
     // ---- A = X X^T over this CTA's columns
     before_mma();
-    if (tid == 0) {
+    if (warp == 0 && ortho::elected()) {
       product(4 * geo.panels, idesc_sym, xh_s, xl_s, xh_s, xl_s, k_major, 16, 0);
       mma_commit(&sh.done);
     }
@@ -333,7 +334,7 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     }
     // ---- B = b A + c A A, in A's place
     before_mma();
-    if (tid == 0) {
+    if (warp == 0 && ortho::elected()) {
       product(p16 / 16, idesc_sym, ah_s, al_s, ah_s, al_s, k_major, 16, 0);
       mma_commit(&sh.done);
     }
@@ -356,7 +357,7 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     }
     // ---- X' = a X + B X, at most 256 columns an MMA
     before_mma();
-    if (tid == 0) {
+    if (warp == 0 && ortho::elected()) {
       for (int q = 0; q < geo.panels; q += 4) {
         const int width = 64 * min(4, geo.panels - q);
         product(p16 / 16, idesc_f16_f32(128, width) | kMnMajorB, ah_s, al_s, xh_s + q * panel,
