@@ -26,11 +26,11 @@
 // b A, a X and the stored X_k are a pair's sum in both.
 //
 // Roles (320 threads per CTA, one CTA per SM):
-//   warp 0, lane 0: TMA producer of this CTA's halves; both halves of a stage complete their
-//                   bytes on the leader's full barrier, which the leader's producer arms.
-//   warp 1:         Tensor Memory; in the leader lane 0 issues the MMAs.
-//   warps 2..9:     epilogue: warp w reads TMEM lanes 32 (w % 4) .. + 31 and one half of the
-//                   columns, 32 at a time, and stores 32 x 32 boxes by TMA (64-byte swizzle).
+//   warp 0:     an elected lane is the TMA producer of this CTA's halves; both halves of a stage
+//               complete their bytes on the leader's full barrier, which its producer arms.
+//   warp 1:     Tensor Memory; in the leader an elected lane issues the MMAs.
+//   warps 2..9: epilogue: warp w reads TMEM lanes 32 (w % 4) .. + 31 and one half of the
+//               columns, 32 at a time, and stores 32 x 32 boxes by TMA (64-byte swizzle).
 // Every wait is bounded; a give-up sets the abort flag of both CTAs and the status word.
 #include <algorithm>
 
@@ -150,6 +150,22 @@ __device__ __forceinline__ void write_weights(T* w, int64_t step, int n, const f
 #pragma unroll
     for (int q = 0; q < 32; ++q)
       if (q < n) w[q * step] = static_cast<T>(u.step ? fmaf(-rate, v[q], u.keep * old[q]) : v[q]);
+  }
+}
+
+// Rows i0 .. + 31 of X, columns j0 .. + n - 1, in the caller's matrix.
+__device__ __forceinline__ void prefetch_weights(const OrthoMat& mt, int64_t j0, int n, int64_t i0) {
+  const int lane = threadIdx.x & 31, size = mt.bf16 ? 2 : 4;
+  const uint8_t* w = static_cast<const uint8_t*>(mt.W);
+  const int64_t i = i0 + lane;
+  if (mt.tall) {
+    for (int q = lane; q < n; q += 32)
+      if (i0 < mt.p && j0 + q < mt.c)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(w + ((j0 + q) * mt.ldw + i0) * size));
+  } else {
+    for (int q = 0; q < n; q += 128 / size)
+      if (i < mt.p && j0 + q < mt.c)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(w + (i * mt.ldw + j0 + q) * size));
   }
 }
 
@@ -365,6 +381,10 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         if (kTwo) tma_load_2d(mirror, from + (phase == kOrthoPoly ? 1 : 2), j, (int)i0, in_full);
       };
       if (lane == 0) request(0);
+      if constexpr (kLast) {
+        // the weights that this warp will update, on their way to L2 while the MMAs run
+        if (ph.u.step) prefetch_weights(mt, tl.j0 + kWarpCols * half, kWarpCols, i0);
+      }
       uint32_t raw[kPairs ? kChunks : 1][32];
       int acc = 0;
       if constexpr (kPairs) {
