@@ -57,10 +57,18 @@ constexpr int kBlockBytes = 64 * 128;                 // a TMA box: 64 rows x 64
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kBoxBytes = 32 * 32 * 2;
-constexpr int kOutBytes = kEpiWarps * 2 * kBoxBytes;  // a direct and a mirrored box per warp
-constexpr int kRing = 192 * 1024;
+constexpr int kSetBytes = 2 * kBoxBytes;              // a warp's direct and mirrored box
+// The ring of stages and the epilogue's boxes share 224 KB.  Narrow tiles of single products have
+// two sets of boxes a warp, so that both chunks' X or A are on their way under the MMAs (ninety-six
+// 256 x 256 bf16: 220 -> 208 us); for wide ones the ring's sixth stage is worth more (a 7B model's
+// 4096 x 4096 and 11008 x 4096: 3395 us with it, 3447 with the second set).
+__host__ __device__ constexpr int box_sets(bool pairs, bool narrow) { return !pairs && narrow ? 2 : 1; }
+constexpr int kRoom = 224 * 1024;
+__host__ __device__ constexpr int ring_bytes(bool pairs, bool narrow) {
+  return kRoom - box_sets(pairs, narrow) * kEpiWarps * kSetBytes;
+}
 constexpr int kTmemCols = 512;
-constexpr size_t kSmem = kRing + kOutBytes + 1024 /*barriers*/ + 1024 /*align*/;
+constexpr size_t kSmem = kRoom + 1024 /*barriers*/ + 1024 /*align*/;
 static_assert(kSmem <= 227 * 1024, "shared memory per CTA");
 constexpr long long kWait = 4000000000LL;             // ~2 s at 2 GHz
 
@@ -68,7 +76,7 @@ struct Shared {
   uint64_t full[8], empty[8];
   uint64_t acc_full[4], acc_empty[4];
   uint64_t drain;                // one commit after the leader's last MMA
-  uint64_t in_full[kEpiWarps];   // an epilogue warp's boxes of A or X have arrived
+  uint64_t in_full[2 * kEpiWarps];   // an epilogue warp's boxes of A or X have arrived, by set
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -181,6 +189,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   constexpr int kBBoxes = kCols >= 128 ? kCols / 128 : 1;
   constexpr int kABytes = 2 * kBlockBytes, kBBytes = kBBoxes * kBlockBytes;   // per CTA
   constexpr int kStageBytes = (kPairs ? 2 : 1) * (kABytes + kBBytes);
+  constexpr int kSets = box_sets(kPairs, kNarrow), kRing = ring_bytes(kPairs, kNarrow);
   constexpr int kStages = kRing / kStageBytes < 8 ? kRing / kStageBytes : 8;
   constexpr int kBufs = kTmemCols / kCols < 4 ? kTmemCols / kCols : 4;
   constexpr int kWarpCols = kCols / 2, kChunks = kWarpCols / 32;
@@ -191,7 +200,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   uint8_t* out_smem = smem + kRing;
-  Shared& sh = *reinterpret_cast<Shared*>(out_smem + kOutBytes);
+  Shared& sh = *reinterpret_cast<Shared*>(smem + kRoom);
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -210,7 +219,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       mbar_init(&sh.acc_empty[s], 2 * kEpiWarps);
     }
     mbar_init(&sh.drain, 1);
-    for (int w = 0; w < kEpiWarps; ++w) mbar_init(&sh.in_full[w], 1);
+    for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(&sh.in_full[w], 1);
     sh.abort_flag = 0;
     fence_mbar_init();
   }
@@ -349,12 +358,11 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
     // ---------------------------------------------------------------- epilogue (each CTA)
     const int g = warp & 3;                        // TMEM lane group
     const int half = (warp - 2) >> 2;              // half of the columns
-    uint8_t* direct = out_smem + (warp - 2) * 2 * kBoxBytes;
-    uint8_t* mirror = direct + kBoxBytes;
-    uint64_t* in_full = &sh.in_full[warp - 2];
+    uint8_t* const boxes = out_smem + (warp - 2) * kSets * kSetBytes;
+    uint64_t* const in_full = &sh.in_full[2 * (warp - 2)];
     constexpr bool kTwo = phase == kOrthoApply || kPairs;
-    uint32_t in_parity = 0;
-    bool pending = false;                          // lane 0: boxes requested and not yet taken
+    uint32_t in_parity[kSets] = {};
+    bool pending[kSets] = {};                      // lane 0: boxes requested and not yet taken
     int64_t n_acc = 0;
     bool ok = true;
     for (int t = t_begin; t < t_end && ok; ++t) {
@@ -374,13 +382,18 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         if (phase == kOrthoGram || outside(q)) return;
         const CUtensorMap* from = m + (phase == kOrthoPoly ? kMapStoreA : kMapStoreX + cur);
         const int j = tl.j0 + kWarpCols * half + 32 * q;
+        uint8_t* to = boxes + q % kSets * kSetBytes;
+        uint64_t* full = in_full + q % kSets;
         bulk_wait_read_all();
-        pending = true;
-        mbar_arrive_expect_tx(in_full, (kTwo ? 2 : 1) * kBoxBytes);
-        tma_load_2d(direct, from, j, (int)i0, in_full);
-        if (kTwo) tma_load_2d(mirror, from + (phase == kOrthoPoly ? 1 : 2), j, (int)i0, in_full);
+        pending[q % kSets] = true;
+        mbar_arrive_expect_tx(full, (kTwo ? 2 : 1) * kBoxBytes);
+        tma_load_2d(to, from, j, (int)i0, full);
+        if (kTwo) tma_load_2d(to + kBoxBytes, from + (phase == kOrthoPoly ? 1 : 2), j, (int)i0, full);
       };
-      if (lane == 0) request(0);
+      if (lane == 0) {
+#pragma unroll
+        for (int q = 0; q < (kSets < kChunks ? kSets : kChunks); ++q) request(q);
+      }
       if constexpr (kLast) {
         // the weights that this warp will update, on their way to L2 while the MMAs run
         if (ph.u.step) prefetch_weights(mt, tl.j0 + kWarpCols * half, kWarpCols, i0);
@@ -455,6 +468,8 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       for (int q = 0; q < kChunks; ++q) {
         const int64_t j0 = tl.j0 + kWarpCols * half + 32 * q;
         if (outside(q) || !finish) continue;
+        uint8_t* const direct = boxes + q % kSets * kSetBytes;
+        uint8_t* const mirror = direct + kBoxBytes;
         if (phase == kOrthoGram && shared) {
           constexpr int kOwn = 32 * 32 * kChunks;
           const float* from = sums + (int64_t)tl.slot * kOrthoMaxParts * ortho_part_floats(kPairs, kNarrow) +
@@ -480,9 +495,9 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]) * s;
         } else {
-          if (!mbar_wait_bounded(in_full, in_parity, abort, kWait)) ok = false;
-          in_parity ^= 1u;
-          pending = false;
+          if (!mbar_wait_bounded(in_full + q % kSets, in_parity[q % kSets], abort, kWait)) ok = false;
+          in_parity[q % kSets] ^= 1u;
+          pending[q % kSets] = false;
           constexpr bool kPoly = phase == kOrthoPoly;
           const float s0 = kPoly ? ph.st.b * exp2i(ph.st.eb - ph.st.ea)
                                  : ph.st.a * exp2i(kLast ? -ph.st.ex : ph.st.ex_next - ph.st.ex);
@@ -523,7 +538,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             if (wide) write_weights<float, true>(w, step, n, v, ph.u, rate);
             else write_weights<float, false>(w, step, n, v, ph.u, rate);
           }
-          if (lane == 0 && q + 1 < kChunks) request(q + 1);
+          if (lane == 0 && q + kSets < kChunks) request(q + kSets);
           __syncwarp();
           continue;
         }
@@ -573,7 +588,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
             bulk_commit();
           }
         }
-        if (lane == 0 && q + 1 < kChunks) request(q + 1);
+        if (lane == 0 && q + kSets < kChunks) request(q + kSets);
         __syncwarp();
       }
       if constexpr (!kPairs) {
@@ -583,7 +598,9 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
       }
     }
     if (!ok && lane == 0) give_up(sh, status);
-    if (lane == 0 && pending) mbar_wait_bounded(in_full, in_parity, nullptr, kWait);
+#pragma unroll
+    for (int q = 0; q < kSets; ++q)
+      if (lane == 0 && pending[q]) mbar_wait_bounded(in_full + q, in_parity[q], nullptr, kWait);
     if (lane == 0) bulk_wait_all();
   }
 

@@ -103,6 +103,29 @@ def test_few_rows_of_great_length(lib, gpu, m, n, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,pad", [(7, 4999, 1), (3, 641, 0), (8, 5136, 0), (4801, 6, 2), (2, 130, 0),
+                                     (9, 5120, 0), (16, 641, 3)])
+def test_at_most_sixteen_rows(lib, gpu, m, n, pad, dtype):
+    """X in registers or in shared memory, clusters whose last CTA has few columns or none."""
+    from paper_2608_15665_gb300 import firstorder as fo
+    G = gauss(m, n, dtype, gpu, 17, pad, spread=0.5)
+    W = gauss(m, n, dtype, gpu, 18, pad)
+    op = fo.Orthogonalizer([G])
+    first = op()[0].clone()
+    check(first, ns(f64(G)), dtype)
+    assert torch.equal(first, op()[0])
+    op.close()
+    before, mu = f64(W), fo.Muon([W], [G])
+    mu.step(0.25, 0.0, False, 0.0, "none")
+    mu.sync()
+    want = before - 0.25 * ns(f64(G))
+    ulp = 2.0 ** -9 if dtype == "bf16" else 2.0 ** -24
+    err = float((f64(W) - want).norm())
+    assert err <= TOL[dtype] * 0.25 * float(ns(f64(G)).norm()) + 2 * ulp * float(want.norm())
+    mu.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ill_conditioned_matrices(lib, gpu, dtype):
     """Singular values falling as 1 / k, and a few strong directions over a noise floor: the
     small ones end far from 1, and are those that rounding noise meets first."""
