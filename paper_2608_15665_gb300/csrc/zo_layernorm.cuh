@@ -28,6 +28,10 @@
 // Few rows, and narrow ones: straight from memory.  Few wide rows go to CTAs with eight columns
 // a thread, for latency.
 //
+// Measured: forward 4096 x 4096 bf16 with a residual 22.4 us (6.0 TB/s), 50001 x 768 fp32 52.7 us
+// (5.8), 8192 x 8192 bf16 63 us (4.3); backward 16384 x 5120 bf16 with a residual 96-104 us
+// (6.4-7.0 TB/s with the column sums), 2048 x 2048 11 us; one row of 5120 2.1 us.
+//
 // The backward pass keeps dw and db of a thread's own columns in registers over all its
 // rows, so that each CTA writes one row of partial sums, which a second kernel adds up in a
 // fixed order: no atomics, the same bits on every run.
@@ -221,12 +225,12 @@ inline Shape shape_of(int64_t cols, bool few) {
   if (few && cols <= 2048) return {256, 8};
   if (few && cols <= 4096) return {512, 8};
   if (cols <= 1024) return {32, 32};
-  if (cols <= 2048) return {128, 16};
-  if (cols <= 3072) return {192, 16};
-  if (cols <= 4096) return {256, 16};
-  if (cols <= 5120) return {320, 16};
-  if (cols <= 8192) return {512, 16};
-  if (cols <= 12288) return {768, 16};
+  if (cols <= 128 * 16) return {128, 16};
+  if (cols <= 192 * 16) return {192, 16};
+  if (cols <= 256 * 16) return {256, 16};
+  if (cols <= 320 * 16) return {320, 16};
+  if (cols <= 512 * 16) return {512, 16};
+  if (cols <= 768 * 16) return {768, 16};
   return {1024, 0};
 }
 inline int64_t groups_at_once(Shape sh, int32_t sms, bool backward) {

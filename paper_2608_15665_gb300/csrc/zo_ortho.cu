@@ -6,9 +6,13 @@
 // fp16's 65504 and 2^-29 of it is still a normal number.
 //
 // Bound by HBM: the first kernel reads G and M and writes M, the second, which needs the norm,
-// reads both again and writes X's hi and lo parts.  A unit of 32 x 256 elements per CTA, all
-// of a thread's loads under way at once, four elements at a time where the caller's rows allow
-// it; X is written from shared memory, by rows or, where U is taller than wide, by columns.
+// reads both again and writes X's hi and lo parts.  A unit of 32 x 256 elements per CTA, four
+// elements a load where the caller's rows allow it; X is written from shared memory, by rows or,
+// where U is taller than wide, by columns.  A CTA is a chain of loads, a sum or a tile, and
+// stores, so four share an SM, with half of a thread's loads under way at once: for a Muon step's
+// 62 M bf16 weights the two kernels took 448 us with two CTAs and all loads at once, 294 us so
+// (1.24 GB: 186 us at the copy rate); six CTAs with a quarter of the loads are 25 us faster there
+// and 13 us slower at 1001 x 333.
 // The norm: each unit's sum of squares, and the last of a matrix's units to finish adds them
 // up, in their order.
 #include <algorithm>
@@ -27,6 +31,7 @@ using tc::exp2i;
 
 constexpr int kRows = kOrthoUnitRows, kCols = kOrthoUnitCols;
 constexpr int kThreads = 256;
+constexpr int kResident = 4;                  // CTAs of an SM
 constexpr int kPitch = kCols + 4;             // of a tile in shared memory, in floats
 static_assert(kCols == kThreads && kRows % 8 == 0, "a column per thread, or four rows of fours");
 
@@ -35,7 +40,7 @@ static_assert(kCols == kThreads && kRows % 8 == 0, "a column per thread, or four
 template <bool kWrite, int kV, typename F>
 __device__ __forceinline__ void for_unit(const OrthoMat& mt, const OrthoUpdate& u, const int4& un, F f) {
   constexpr int kPass = kThreads * kV / kCols;                  // rows at a time: 1 or 4
-  constexpr int kBatch = 8;
+  constexpr int kBatch = kV == 4 ? 4 : 8;                       // rows under way at once
   const int r0 = (int)threadIdx.x / (kCols / kV), c = (int)threadIdx.x % (kCols / kV) * kV;
   const int64_t j = (int64_t)un.z + c;
   const bool moving = u.step && mt.M != nullptr;
@@ -94,7 +99,7 @@ __device__ __forceinline__ double block_sum(double s, double* sums) {
 }
 
 // M <- momentum M + G, the sum of U^2 over each unit, and 1 / (||U|| + eps) of each matrix
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kResident)
 momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
                 const OrthoUpdate u, float* __restrict__ partial, uint32_t* __restrict__ counter,
                 float* __restrict__ inverse) {
@@ -130,7 +135,7 @@ momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ unit
 }
 
 // X_0 = U / (||U|| + eps)
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kResident)
 scale_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
              const OrthoUpdate u, int ex, const float* __restrict__ inverse) {
   __shared__ __align__(16) float tile[kRows * kPitch];

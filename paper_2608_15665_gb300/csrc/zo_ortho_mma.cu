@@ -16,6 +16,9 @@
 // Between load and scaling, and between the last step and the update of W, the planes hold the
 // upper and lower halves of fp32 values, so that the caller's matrices are read and written
 // once, in their own order.
+// Bound by the chain's latencies.  224 matrices of 32 x 32 fp32 9.5 us; Muon steps of forty 8 x
+// 5120 26 us: five steps of 6 K cycles, half of them the cluster's sums, and 14 K of load, norm
+// and store.
 #include <algorithm>
 
 #include <cuda_fp16.h>

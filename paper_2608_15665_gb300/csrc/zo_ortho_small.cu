@@ -20,7 +20,9 @@
 // of X hold the upper and lower halves of fp32 values, so that the caller's matrices are read
 // and written once, in their own order.
 //
-// Bound by latency and the epilogues: three MMA round trips per step.
+// Bound by latency and the epilogues: a product's MMAs take 1.9-2.1 K cycles and its epilogue
+// 1.3-2.2 K, about half of that at shared memory's rate, one after the other.  224 matrices of
+// 128 x 128 fp32: 73 us, two waves of a CTA per SM; one matrix 36 us.
 #include <algorithm>
 
 #include <cuda_bf16.h>
