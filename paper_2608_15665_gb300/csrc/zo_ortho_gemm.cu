@@ -93,6 +93,9 @@ __device__ __forceinline__ void give_up(Shared& sh, uint32_t* status) {
   store_peer(&sh.abort_flag, 1);
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
+}
 // a wait by a whole warp, the same for every lane
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const volatile int* abort) {
   return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort, kWait)) != 0;
@@ -234,6 +237,25 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
+  // the context's tables are older than the launches before this one: the first tile's entry
+  // and tensor maps are fetched under their tail
+  if (t_begin < t_end && (warp == 0 || warp == 2) && lane == 0) {
+    const CUtensorMap* m = maps + (int64_t)tiles[t_begin].maps * kOrthoMaps;
+    const int cur = ph.st.k & 1;
+    constexpr int kSide = phase == kOrthoGram ? kMapX : phase == kOrthoPoly ? kMapA : kMapB;
+    if (warp == 0) {
+      prefetch_map(m + kSide + (phase == kOrthoGram ? cur : 0));
+      if (phase == kOrthoApply) prefetch_map(m + kMapX + cur);
+      if (kPairs) prefetch_map(m + kSide + (phase == kOrthoGram ? 2 + cur : 1));
+      if (kPairs && phase == kOrthoApply) prefetch_map(m + kMapX + 2 + cur);
+    } else {
+      if (phase != kOrthoGram) prefetch_map(m + (phase == kOrthoPoly ? kMapStoreA : kMapStoreX + cur));
+      if (!kLast)
+        prefetch_map(m + (phase == kOrthoGram ? kMapStoreA
+                          : phase == kOrthoPoly ? kMapStoreB : kMapStoreX + (cur ^ 1)));
+    }
+  }
+  __syncwarp();
   pdl_wait();
   pdl_trigger();
 
