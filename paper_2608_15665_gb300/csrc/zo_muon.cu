@@ -612,6 +612,10 @@ zo_status zo_muon_sync_status(zo_muon_ctx* c) {
   ZO_CUDA(cudaStreamSynchronize(c->stream), "stream synchronize");
   if (s != 0) {
     ZO_CUDA(cudaMemsetAsync(c->ws, 0, sizeof(uint32_t), c->stream), "clear status");
+    // launches that gave up may have left counters of finished units and parts behind
+    ZO_CUDA(cudaMemsetAsync(c->ws + c->plan.counter_at, 0,
+                            (size_t)(c->plan.tables_end - c->plan.counter_at), c->stream),
+            "clear counters");
     ZO_CUDA(cudaStreamSynchronize(c->stream), "stream synchronize");
     return refuse(ZO_ERR_TIMEOUT, "a device-side wait ran out");
   }
