@@ -354,7 +354,12 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
     } else {
       // ---- X X^T: rows 16 m, columns 8 (kN n0 ..), K tiles split, split + kSplits, ...
       const int m = warp % S::kM, split = warp / S::kM % S::kSplits, n0 = warp / (S::kM * S::kSplits) * S::kN;
-      float d[S::kN][4] = {};
+      // An MMA's fp32 sum rounds towards zero.  At 64 rows, where one warp goes over all of a CTA's
+      // K, hi.hi of 16 columns at a time is added up here, to nearest (48 x 3008: 2.8e-6 of the
+      // result instead of 4.2e-6); with K dealt to four or eight warps it made no difference and
+      // took 5 to 20% of the call.
+      constexpr bool kNearest = P == 64;
+      float d[S::kN][4] = {}, small[kNearest ? S::kN : 1][4] = {};
       for (int kt = split; kt < cs / 16; kt += S::kSplits) {
         uint32_t a[2][4];
         const int at = (16 * m + (lane & 15)) * pitch + 16 * kt + (lane >> 4) * 8;
@@ -368,11 +373,26 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
           ldmatrix_x4(b[1], smem_u32(xl + bt));
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            mma(d[q + h], a[0], b[1][h], b[1][h + 2]);
-            mma(d[q + h], a[1], b[0][h], b[0][h + 2]);
-            mma(d[q + h], a[0], b[0][h], b[0][h + 2]);
+            if constexpr (kNearest) {
+              float large[4] = {};
+              mma(small[q + h], a[0], b[1][h], b[1][h + 2]);
+              mma(large, a[0], b[0][h], b[0][h + 2]);
+              mma(small[q + h], a[1], b[0][h], b[0][h + 2]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) d[q + h][e] += large[e];
+            } else {
+              mma(d[q + h], a[0], b[1][h], b[1][h + 2]);
+              mma(d[q + h], a[1], b[0][h], b[0][h + 2]);
+              mma(d[q + h], a[0], b[0][h], b[0][h + 2]);
+            }
           }
         }
+      }
+      if constexpr (kNearest) {
+#pragma unroll
+        for (int q = 0; q < S::kN; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[q][e] += small[q][e];
       }
       float* to = part + split * S::kSumFloats;
 #pragma unroll
