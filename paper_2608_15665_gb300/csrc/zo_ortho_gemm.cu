@@ -96,7 +96,8 @@ __device__ __forceinline__ void give_up(Shared& sh, uint32_t* status) {
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
 }
-// a wait by a whole warp, the same for every lane
+// A wait by a whole warp, the same for every lane.  (A lane's own wait may run out where another's
+// does not; the warp-wide instructions behind a wait need all lanes, and lane 0 to report it.)
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const volatile int* abort) {
   return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort, kWait)) != 0;
 }
@@ -422,6 +423,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 #pragma unroll
         for (int q = 0; q < (kSets < kChunks ? kSets : kChunks); ++q) request(q);
       }
+      __syncwarp();
       if constexpr (kLast) {
         // the weights that this warp will update, on their way to L2 while the MMAs run
         if (ph.u.step) prefetch_weights(mt, tl.j0 + kWarpCols * half, kWarpCols, i0);
@@ -437,11 +439,10 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
           for (int e = 0; e < 32; ++e) raw[q][e] = 0u;
         for (int sg = 0; sg < segs; ++sg, ++n_acc) {
           acc = (int)(n_acc % kBufs);
-          if (!mbar_wait_bounded(&sh.acc_full[acc], (uint32_t)((n_acc / kBufs) & 1), abort, kWait)) {
+          if (!warp_wait(&sh.acc_full[acc], (uint32_t)((n_acc / kBufs) & 1), abort)) {
             ok = false;
             break;
           }
-          __syncwarp();
           tc_fence_after();
 #pragma unroll
           for (int q = 0; q < kChunks; ++q) {
@@ -458,9 +459,8 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         }
       } else {
         acc = (int)(n_acc % kBufs);
-        ok = mbar_wait_bounded(&sh.acc_full[acc], (uint32_t)((n_acc / kBufs) & 1), abort, kWait);
+        ok = warp_wait(&sh.acc_full[acc], (uint32_t)((n_acc / kBufs) & 1), abort);
         ++n_acc;
-        __syncwarp();
         tc_fence_after();
       }
       if (!ok) break;
@@ -523,7 +523,10 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]) * s;
         } else {
-          if (!mbar_wait_bounded(in_full + q % kSets, in_parity[q % kSets], abort, kWait)) ok = false;
+          if (!warp_wait(in_full + q % kSets, in_parity[q % kSets], abort)) {
+            ok = false;
+            break;
+          }
           in_parity[q % kSets] ^= 1u;
           pending[q % kSets] = false;
           constexpr bool kPoly = phase == kOrthoPoly;
