@@ -162,7 +162,10 @@ class _MuonContext:
         self.ctx = None
         dev = weights[0].device
         with torch.cuda.device(dev):
-            self.stream = torch.cuda.current_stream() if stream is None else stream
+            current = torch.cuda.current_stream()
+            self.stream = current if stream is None else stream
+            if self.stream != current:      # what was filled for this context until now
+                self.stream.wait_stream(current)
             with torch.cuda.stream(self.stream):
                 self.workspace = torch.empty(zb.zo_muon_workspace(mats), dtype=torch.uint8,
                                              device=dev)
