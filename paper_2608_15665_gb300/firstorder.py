@@ -3,10 +3,11 @@
 A model whose body is trained by subspace steps can train its tail by backpropagation,
 which costs one backward pass through the tail alone and no activations of what lies
 below it.  This module allocates the outputs and workspaces of those operators next to the
-caller's tensors and launches them on PyTorch's current stream:
+caller's tensors and launches them in the order of PyTorch's current stream:
 
 * ``layer_norm`` / ``layer_norm_backward`` -- the norm's forward and backward pass, and
-  ``LayerNorm``, the two as one ``torch.autograd.Function``.
+  ``LayerNorm``, the two as one ``torch.autograd.Function``;
+* ``Orthogonalizer`` / ``Muon`` -- handles over matrices, bound to one stream.
 
 No arithmetic happens here.
 """
@@ -155,7 +156,11 @@ ADJUST = {"none": zb.ZO_MUON_ADJUST_NONE, "aspect": zb.ZO_MUON_ADJUST_ASPECT,
 
 
 class _MuonContext:
-    """A context over matrices and its workspace, on PyTorch's current stream (or `stream`)."""
+    """A context over matrices and its workspace, on the stream that is PyTorch's current one
+    when it is made (or `stream`).  A call under another current stream runs on the context's
+    own all the same, after what that stream holds so far, and that stream goes on after it.
+    (In a graph's capture too, where the context's own is not the legacy default stream, which
+    CUDA keeps out of captures.)"""
 
     def __init__(self, weights, grads, momenta, stream):
         mats = [zb.make_muon_matrix(W, G, M) for W, G, M in zip(weights, grads, momenta)]
@@ -170,6 +175,16 @@ class _MuonContext:
                 self.workspace = torch.empty(zb.zo_muon_workspace(mats), dtype=torch.uint8,
                                              device=dev)
             self.ctx = zb.zo_muon_create(mats, self.workspace, self.stream)
+        self.device = dev
+
+    def _call(self, fn, *args):
+        if _raw_stream(self.device.index) == self.stream.cuda_stream:
+            fn(self.ctx, *args)
+            return
+        current = torch.cuda.current_stream(self.device)
+        self.stream.wait_stream(current)
+        fn(self.ctx, *args)
+        current.wait_stream(self.stream)
 
     def sync(self):
         zb.zo_muon_sync_status(self.ctx)
@@ -199,7 +214,7 @@ class Orthogonalizer(_MuonContext):
         super().__init__(self.outputs, self.inputs, [None] * len(self.inputs), stream)
 
     def __call__(self, steps=5, coeffs=None, eps=1e-7):
-        zb.zo_orthogonalize(self.ctx, steps, coeffs, eps)
+        self._call(zb.zo_orthogonalize, steps, coeffs, eps)
         return self.outputs
 
 
@@ -220,5 +235,5 @@ class Muon(_MuonContext):
 
     def step(self, lr, momentum=0.95, nesterov=True, weight_decay=0.0, adjust="aspect", steps=5,
              coeffs=None, eps=1e-7):
-        zb.zo_muon_step(self.ctx, momentum, nesterov, lr, weight_decay, ADJUST[adjust], steps,
-                        coeffs, eps)
+        self._call(zb.zo_muon_step, momentum, nesterov, lr, weight_decay, ADJUST[adjust], steps,
+                   coeffs, eps)

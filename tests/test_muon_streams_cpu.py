@@ -69,3 +69,21 @@ def test_the_current_stream_waits_for_nothing(cuda, which):
     assert op.stream is cuda.current
     assert cuda.log == ["zo_muon_create"]
     op.close()
+
+
+def _call(op):
+    op.step(0.1) if hasattr(op, "step") else op()
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_a_call_under_another_stream_lies_between_its_work(cuda, which):
+    from paper_2608_15665_gb300 import firstorder as fo
+    op, s = _handles(fo, None)[which](), cuda.stream("s")
+    del cuda.log[:]
+    name = ("zo_muon_step", "zo_orthogonalize")[which]
+    with torch.cuda.stream(s):
+        _call(op)
+    assert cuda.log == [("default", "waits for", "s"), name, ("s", "waits for", "default")]
+    del cuda.log[:]
+    _call(op)                                                # and under its own
+    assert cuda.log == [name]
