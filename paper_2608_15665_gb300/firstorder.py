@@ -145,7 +145,7 @@ class LayerNorm(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
-        _, need_w, need_b, _ = ctx.needs_input_grad
+        need_w, need_b = ctx.needs_input_grad[1:3]       # (there is no fourth without an eps)
         dx, dw, db = layer_norm_backward(dy.contiguous(), x, weight, mean, rstd,
                                          wdtype=ctx.wdtype, want_weight=need_w, want_bias=need_b)
         return dx, dw, db, None
