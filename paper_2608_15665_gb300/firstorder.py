@@ -15,6 +15,7 @@ No arithmetic happens here.
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as zb
 
@@ -131,7 +132,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dresidual=None, wdtype=None, 
 
 
 class LayerNorm(torch.autograd.Function):
-    """``LayerNorm.apply(x, weight, bias, eps)`` on a rows x cols tensor."""
+    """``LayerNorm.apply(x, weight, bias, eps)`` on a rows x cols tensor.  Differentiable once:
+    the gradients are the kernels', and asking for theirs is an error."""
 
     @staticmethod
     def forward(ctx, x, weight, bias, eps=1e-5):
@@ -143,6 +145,7 @@ class LayerNorm(torch.autograd.Function):
         return out.y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         need_w, need_b = ctx.needs_input_grad[1:3]       # (there is no fourth without an eps)

@@ -58,3 +58,12 @@ def test_gradients_with_and_without_an_eps(fo, extra, eps, needs):
         assert (t.grad is None) == (want is None)
         if want is not None:
             assert torch.allclose(t.grad, want, rtol=1e-9, atol=1e-12)
+
+
+def test_a_second_derivative_is_refused(fo):
+    """A penalty on the gradient is not silently taken for a constant."""
+    x, w, b = _inputs()
+    y = fo.LayerNorm.apply(x, w, b, 1e-5)
+    dx, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (y.sum() + dx.square().sum()).backward()
