@@ -60,10 +60,20 @@ def _device_of(x, at):
     return dev
 
 
+def _refuse_grad(at, *tensors):
+    """Outputs made through raw pointers have no history: where one would be recorded, an error."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, "an input requires a gradient, which is not "
+                             "recorded here: call LayerNorm.apply, or this under torch.no_grad()")
+
+
 def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
     """LayerNorm over the last dimension of a rows x cols tensor, of x + residual where a
-    residual is given (the sum comes back as ``h``)."""
+    residual is given (the sum comes back as ``h``).  Its outputs have no history for autograd
+    (``LayerNorm`` does that): inputs that require gradients are refused where they are recorded."""
     at = "layer_norm"
+    _refuse_grad(at, x, weight, bias, residual)
     px, ldx = zb._rows(x, at, "x", None, None, None)
     shape, dt, device = x.shape, x.dtype, x.device
     rows, cols = shape
@@ -96,8 +106,10 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dresidual=None, wdtype=None, 
                         want_bias=True):
     """(dx, dweight, dbias) from the gradient of y and the forward pass's input (its ``h``
     where there was a residual) and statistics; dresidual is added to dx.  dweight and dbias
-    have the weight's type (wdtype where there is none); None where not wanted."""
+    have the weight's type (wdtype where there is none); None where not wanted.  Like
+    ``layer_norm``, without a history for autograd."""
     at = "layer_norm_backward"
+    _refuse_grad(at, dy, x, weight, mean, rstd, dresidual)
     px, ldx = zb._rows(x, at, "x", None, None, None)
     shape, dt, device = x.shape, x.dtype, x.device
     rows, cols = shape
