@@ -178,9 +178,16 @@ class _MuonContext:
     CUDA keeps out of captures.)"""
 
     def __init__(self, weights, grads, momenta, stream):
-        mats = [zb.make_muon_matrix(W, G, M) for W, G, M in zip(weights, grads, momenta)]
         self.ctx = None
+        at = type(self).__name__
+        if not weights:
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, "need at least one matrix")
         dev = weights[0].device
+        # (make_muon_matrix compares a matrix's own tensors)
+        if any(W.device != dev for W in weights) or getattr(stream, "device", dev) != dev:
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at,
+                             "the matrices and the stream have to be on one CUDA device")
+        mats = [zb.make_muon_matrix(W, G, M) for W, G, M in zip(weights, grads, momenta)]
         with torch.cuda.device(dev):
             current = torch.cuda.current_stream()
             self.stream = current if stream is None else stream
