@@ -207,8 +207,7 @@ cudaError_t forward_v(const LayerNormArgs& a, int32_t sms, cudaStream_t s) {
       if (a.rows > groups_at_once(sh, sms, false) && stages >= 2) {
         const auto kernel = forward_ring_kernel<T, TW, G, E, V>;
         const size_t smem = (size_t)per * stages * n * slot;
-        const cudaError_t err = cudaFuncSetAttribute(
-            kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t err = allow_smem(kernel, kRingRoom<G, E, false>);
         if (err != cudaSuccess) return err;
         return launch_dependent(kernel, (unsigned)(resident_of(G, E, false) * sms), block, smem, s, 1,
                                 true, a, stages, slot);

@@ -321,11 +321,20 @@ cudaError_t with_shape(Shape sh, F f) {
   return cudaErrorInvalidValue;
 }
 
-// stages of a ring of n matrices' rows, as many as an SM's resident CTAs have room for
+// a CTA's room for its rings: what an SM's resident CTAs share
+template <int kGroup, int kElems, bool kBackward>
+constexpr size_t kRingRoom = 208 * 1024 / resident_of(kGroup, kElems, kBackward);
+// stages of a ring of n matrices' rows, as many as there is room for
 template <int kGroup, int kElems, bool kBackward>
 int ring_stages(int n, uint32_t slot) {
-  const size_t room = 208 * 1024 / resident_of(kGroup, kElems, kBackward);
-  return (int)std::min<size_t>(kMaxStages, room / ((size_t)(block_of(kGroup) / kGroup) * n * slot));
+  return (int)std::min<size_t>(kMaxStages, kRingRoom<kGroup, kElems, kBackward> /
+                                               ((size_t)(block_of(kGroup) / kGroup) * n * slot));
+}
+// Lets a kernel take up to `most` bytes of dynamic shared memory.  `most` is the instance's own and
+// not one call's: the limit belongs to the kernel, and calls of several threads share it.
+template <typename K>
+cudaError_t allow_smem(K kernel, size_t most) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
 }
 template <typename T>
 uint32_t ring_slot(int64_t cols) {

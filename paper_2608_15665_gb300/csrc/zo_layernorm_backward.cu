@@ -234,21 +234,21 @@ cudaError_t backward_v(const LayerNormArgs& a, int32_t sms, int64_t n_partial, c
       return cudaGetLastError();
     } else {
       constexpr int block = block_of(G), groups = block / G;
-      size_t smem = groups > 1 ? sizeof(float) * 2 * groups * E * G : 0;
+      constexpr size_t joined = groups > 1 ? sizeof(float) * 2 * groups * E * G : 0;
+      static_assert(joined <= 48 * 1024, "the sums fit without a limit of their own");
       if constexpr (ring_of(G, E)) {
         const uint32_t slot = ring_slot<T>(a.cols);
         const int n = a.r ? 3 : 2, stages = ring_stages<G, E, true>(n, slot);
         if (a.rows > groups_at_once(sh, sms, true) && stages >= 2) {
           const auto kernel = backward_kernel<T, TW, G, E, V, true>;
-          smem = std::max(smem, (size_t)groups * stages * n * slot);
-          const cudaError_t err = cudaFuncSetAttribute(
-              kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+          const size_t smem = std::max(joined, (size_t)groups * stages * n * slot);
+          const cudaError_t err = allow_smem(kernel, std::max(joined, kRingRoom<G, E, true>));
           if (err != cudaSuccess) return err;
           return launch_dependent(kernel, (unsigned)n_partial, block, smem, s, 1, true, a, stages, slot);
         }
       }
       return launch_dependent(backward_kernel<T, TW, G, E, V, false>, (unsigned)n_partial, block,
-                              smem, s, 1, true, a, 0, 0u);
+                              joined, s, 1, true, a, 0, 0u);
     }
   });
 }
