@@ -427,7 +427,8 @@ ZO_API zo_status zo_layernorm_backward(const void* dY, int64_t lddy, const void*
  *   values can leave the range the iterates are held in are refused
  *   (ZO_ERR_INVALID_ARG): with the bounds u_0 = 1, u_(k+1) = max |a s + b s^3 + c s^5| over
  *   0 <= s <= u_k, every u_k, u_k^2 and max |b s^2 + c s^4| has to stay below 2^12.
- * eps >= 0 (1e-7 is usual); a zero matrix gives zero (with eps = 0 too).
+ * eps >= 0 (1e-7 is usual); a zero matrix gives zero (with eps = 0 too).  U may have any finite
+ *   scale: where its squares leave fp32's range it is scaled by a power of two before its norm.
  * Precision: sums are fp32.  Iterates are held as power-of-two-scaled fp16 pairs (~22
  *   significant bits).  Their products are of fp32 grade where W is fp32 or min(m, n) <= 128;
  *   for larger bf16 matrices the products take single fp16 factors (11 bits), whose error in

@@ -314,9 +314,9 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
   L.counter_at = place(sizeof(uint32_t) * L.mats.size());       // zeros, uploaded too
   L.slot_counter_at = place((int64_t)sizeof(uint32_t) * zo::kOrthoSlotCounters * slots_used);
   L.tables_end = at;
-  L.inverse_at = place(sizeof(float) * L.mats.size());
+  L.inverse_at = place(sizeof(float2) * L.mats.size());
   L.sums_at = place((int64_t)sizeof(float) * sums_floats);
-  L.partial_at = place(sizeof(float) * slots);
+  L.partial_at = place(sizeof(double) * slots);
   L.buffers_at = at;
   L.bytes = at + most;
   return ZO_OK;
@@ -430,9 +430,9 @@ zo_status run(zo_muon_ctx* c, const zo::OrthoUpdate& u, int32_t steps, const flo
   const auto* firsts = reinterpret_cast<const int32_t*>(c->ws + L.first_at);
   const auto* maps = reinterpret_cast<const CUtensorMap*>(c->ws + L.maps_at);
   auto* status = reinterpret_cast<uint32_t*>(c->ws);
-  auto* partial = reinterpret_cast<float*>(c->ws + L.partial_at);
+  auto* partial = reinterpret_cast<double*>(c->ws + L.partial_at);
   auto* counter = reinterpret_cast<uint32_t*>(c->ws + L.counter_at);
-  auto* inverse = reinterpret_cast<float*>(c->ws + L.inverse_at);
+  auto* inverse = reinterpret_cast<float2*>(c->ws + L.inverse_at);
   const auto* which = reinterpret_cast<const int32_t*>(c->ws + L.small_at);
   for (const Small& g : L.small) {
     ZO_CUDA(g.rows ? zo::launch_ortho_mma(mats, which + g.first, g.n, g.rows, g.cluster, g.smem,

@@ -109,12 +109,13 @@ struct OrthoUpdate {
 // single factors, rounding the result 1.7e-3), and their time is latency, not products.
 inline bool ortho_pairs(bool bf16, int64_t p) { return !bf16 || p <= 128; }
 
-// partial: a float per unit; counter (zero before the first call) and inverse: one per matrix
+// partial: one per unit; counter (zero before the first call) and inverse (a power of two, and
+// what U is multiplied by after it): one per matrix
 cudaError_t launch_ortho_momentum(const OrthoMat* mats, const int4* units, int32_t n_units,
-                                  const OrthoUpdate& u, float* partial, uint32_t* counter,
-                                  float* inverse, cudaStream_t s);
+                                  const OrthoUpdate& u, double* partial, uint32_t* counter,
+                                  float2* inverse, cudaStream_t s);
 cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t n_units,
-                               const OrthoUpdate& u, int32_t ex, const float* inverse,
+                               const OrthoUpdate& u, int32_t ex, const float2* inverse,
                                cudaStream_t s);
 // Clusters of the product kernels that fit on the device at once
 int32_t ortho_max_pairs();

@@ -14,7 +14,8 @@
 // (1.24 GB: 186 us at the copy rate); six CTAs with a quarter of the loads are 25 us faster there
 // and 13 us slower at 1001 x 333.
 // The norm: each unit's sum of squares, and the last of a matrix's units to finish adds them
-// up, in their order.
+// up, in their order.  Where a unit's squares leave fp32, the unit is read again and scaled by a
+// power of two; where the norm does, U is scaled before it is divided by it.
 #include <algorithm>
 
 #include <cuda_fp16.h>
@@ -98,12 +99,40 @@ __device__ __forceinline__ double block_sum(double s, double* sums) {
   return s;
 }
 
-// M <- momentum M + G, the sum of U^2 over each unit, and 1 / (||U|| + eps) of each matrix
+// the sum of U^2 over a unit whose squares are beyond fp32, where its values are not
+__device__ __noinline__ double scaled_squares(const OrthoMat* mats, const OrthoUpdate& u, int4 un,
+                                              double total, double* sums, uint32_t* mosts) {
+  const OrthoMat mt = mats[un.x];
+  uint32_t most = 0;
+  for_unit<false>(mt, u, un, [&](int, int, const auto& v) {
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(v) / sizeof(float)); ++e)
+      most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  });
+  most = __reduce_max_sync(0xffffffffu, most);
+  if ((threadIdx.x & 31) == 0) mosts[threadIdx.x >> 5] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) most = max(most, mosts[w]);
+  if (!ortho::plain_value(most)) return total;                  // zero, or not finite: as it is
+  const int e = ortho::square_exponent(most);
+  const float scale = exp2i(-e);
+  float s = 0.0f;
+  for_unit<false>(mt, u, un, [&](int, int, const auto& v) {
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(v) / sizeof(float)); ++k) s = fmaf(v[k] * scale, v[k] * scale, s);
+  });
+  return block_sum((double)s, sums) * __hiloint2double((1023 + 2 * e) << 20, 0);     // 4^e
+}
+
+// M <- momentum M + G, the sum of U^2 over each unit, and of each matrix 2^-e and
+// 2^e / (||U|| + eps), e = 0 unless the norm is far from 1
 __global__ void __launch_bounds__(kThreads, kResident)
 momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
-                const OrthoUpdate u, float* __restrict__ partial, uint32_t* __restrict__ counter,
-                float* __restrict__ inverse) {
+                const OrthoUpdate u, double* __restrict__ partial, uint32_t* __restrict__ counter,
+                float2* __restrict__ inverse) {
   __shared__ double sums[kThreads / 32];
+  __shared__ uint32_t mosts[kThreads / 32];
   __shared__ bool last;
   const int4 un = units[blockIdx.x];
   const OrthoMat mt = mats[un.x];
@@ -114,9 +143,11 @@ momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ unit
 #pragma unroll
     for (int e = 0; e < (int)(sizeof(v) / sizeof(float)); ++e) s = fmaf(v[e], v[e], s);
   });
-  const double total = block_sum((double)s, sums);
+  double total = block_sum((double)s, sums);
+  total = ortho::squares_hold(total) ? (double)(float)total
+                                     : scaled_squares(mats, u, un, total, sums, mosts);
   if (threadIdx.x == 0) {
-    partial[un.w] = (float)total;
+    partial[un.w] = total;
     __threadfence();
     last = atomicAdd(&counter[un.x], 1u) == (uint32_t)mt.n_units - 1;
   }
@@ -125,11 +156,15 @@ momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ unit
   __threadfence();
   double all = 0.0;
   for (int k = threadIdx.x; k < mt.n_units; k += kThreads)
-    all += (double)__ldcg(&partial[mt.unit0 + k]);
+    all += __ldcg(&partial[mt.unit0 + k]);
   all = block_sum(all, sums);
   if (threadIdx.x == 0) {
-    const float norm = (float)sqrt(all) + u.eps;
-    inverse[un.x] = norm == 0.0f ? 0.0f : 1.0f / norm;
+    const double root = sqrt(all);
+    float scale = 1.0f;
+    if (root > 0.0 && root < 0x1p-50) scale = 0x1p126f;
+    else if (root > 0x1p60 && root < 0x1p200) scale = 0x1p-126f;  // (more is an infinity)
+    const float norm = (float)(root * (double)scale) + u.eps * scale;
+    inverse[un.x] = make_float2(scale, norm == 0.0f ? 0.0f : 1.0f / norm);
     counter[un.x] = 0;                                          // for the next call
   }
 }
@@ -137,7 +172,7 @@ momentum_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ unit
 // X_0 = U / (||U|| + eps)
 __global__ void __launch_bounds__(kThreads, kResident)
 scale_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
-             const OrthoUpdate u, int ex, const float* __restrict__ inverse) {
+             const OrthoUpdate u, int ex, const float2* __restrict__ inverse) {
   __shared__ __align__(16) float tile[kRows * kPitch];
   const int4 un = units[blockIdx.x];
   const OrthoMat mt = mats[un.x];
@@ -148,10 +183,11 @@ scale_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const float inv = inverse[un.x], scale = exp2i(ex);
+  const float2 inv = inverse[un.x];
+  const float scale = exp2i(ex);
   for_unit<false>(mt, u, un, [&](int r, int c, const auto& v) {
 #pragma unroll
-    for (int e = 0; e < (int)(sizeof(v) / sizeof(float)); ++e) tile[r * kPitch + c + e] = v[e] * inv;
+    for (int e = 0; e < (int)(sizeof(v) / sizeof(float)); ++e) tile[r * kPitch + c + e] = v[e] * inv.x * inv.y;
   });
   __syncthreads();
   const int64_t width = (mt.c + 7) / 8 * 8;
@@ -182,13 +218,13 @@ scale_kernel(const OrthoMat* __restrict__ mats, const int4* __restrict__ units,
 }  // namespace
 
 cudaError_t launch_ortho_momentum(const OrthoMat* mats, const int4* units, int32_t n_units,
-                                  const OrthoUpdate& u, float* partial, uint32_t* counter,
-                                  float* inverse, cudaStream_t s) {
+                                  const OrthoUpdate& u, double* partial, uint32_t* counter,
+                                  float2* inverse, cudaStream_t s) {
   return launch_dependent(momentum_kernel, (unsigned)n_units, kThreads, 0, s, 1, true, mats, units,
                           u, partial, counter, inverse);
 }
 cudaError_t launch_ortho_scale(const OrthoMat* mats, const int4* units, int32_t n_units,
-                               const OrthoUpdate& u, int32_t ex, const float* inverse,
+                               const OrthoUpdate& u, int32_t ex, const float2* inverse,
                                cudaStream_t s) {
   return launch_dependent(scale_kernel, (unsigned)n_units, kThreads, 0, s, 1, true, mats, units, u,
                           ex, inverse);

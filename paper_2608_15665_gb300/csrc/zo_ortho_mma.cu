@@ -103,20 +103,6 @@ __device__ __forceinline__ void split2(float a, float b, __half* hi, __half* lo)
   *reinterpret_cast<__half2*>(hi) = h;
   *reinterpret_cast<__half2*>(lo) = __floats2half2_rn(a - f.x, b - f.y);
 }
-// the upper and lower halves of fp32 values in the two planes
-__device__ __forceinline__ uint32_t upper2(float a, float b) {
-  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-}
-__device__ __forceinline__ uint32_t lower2(float a, float b) {
-  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
-}
-__device__ __forceinline__ float first_of(uint32_t up, uint32_t low) {
-  return __uint_as_float(__byte_perm(low, up, 0x5410));
-}
-__device__ __forceinline__ float second_of(uint32_t up, uint32_t low) {
-  return __uint_as_float(__byte_perm(low, up, 0x7632));
-}
-
 struct Steps {
   OrthoStep s[kOrthoMaxSteps];
   int n;
@@ -322,7 +308,8 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
     sq = load_update<kThreads, 1>(mt, u, c0, cols,
                                   [&](int i, int j, const float (&v)[1]) { put(i, j, v[0]); });
   }
-  const float inv = inverse_norm<kThreads>(sq, u.eps, cluster, sums);
+  const Planes planes{reinterpret_cast<uint4*>(xh), reinterpret_cast<uint4*>(xl), P * pitch / 8};
+  const float inv = inverse_norm<kThreads>(sq, u.eps, cluster, sums, planes);
   const float s_in = exp2i(steps.s[0].ex);
   const bool in_registers = P == 16 && mt.p <= 8 && cs <= 16 * kTiles * kWarps;
   Columns x;

@@ -39,6 +39,10 @@ namespace zo {
 namespace {
 
 using namespace sm100;
+using ortho::first_of;
+using ortho::lower2;
+using ortho::second_of;
+using ortho::upper2;
 using tc::exp2i;
 
 constexpr int kMaxCluster = 8;
@@ -126,20 +130,6 @@ __device__ __forceinline__ void pairs8(const uint8_t* hi, const uint8_t* lo, flo
     v[2 * k + 1] = x.y + y.y;
   }
 }
-// the upper and lower halves of fp32 values, in the two planes
-__device__ __forceinline__ uint32_t upper2(float a, float b) {
-  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-}
-__device__ __forceinline__ uint32_t lower2(float a, float b) {
-  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
-}
-__device__ __forceinline__ float first_of(uint32_t up, uint32_t low) {
-  return __uint_as_float(__byte_perm(low, up, 0x5410));
-}
-__device__ __forceinline__ float second_of(uint32_t up, uint32_t low) {
-  return __uint_as_float(__byte_perm(low, up, 0x7632));
-}
-
 struct Steps {
   OrthoStep s[kOrthoMaxSteps];
   int n;
@@ -214,7 +204,8 @@ ortho_small_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ wh
     sq = ortho::load_update<kThreads, 1>(mt, u, c0, cols,
                                          [&](int i, int j, const float (&v)[1]) { put(i, j, v[0]); });
   }
-  const float inv = ortho::inverse_norm<kThreads>(sq, u.eps, cluster, sh.sums);
+  const ortho::Planes planes{reinterpret_cast<uint4*>(xh), reinterpret_cast<uint4*>(xl), geo.x_bytes / 16};
+  const float inv = ortho::inverse_norm<kThreads>(sq, u.eps, cluster, sh.sums, planes);
   const float s_in = exp2i(steps.s[0].ex);
   for (int b = tid * 16; b < geo.x_bytes; b += kThreads * 16) {
     uint4* ph = reinterpret_cast<uint4*>(xh + b);
