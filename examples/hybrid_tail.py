@@ -101,6 +101,7 @@ def train(steps=40, lr_body=0.02, lr_norm=0.5, lr_head=0.02, device="cuda"):
     losses.append(float(model.tail_step(0.0, 0.0)))
     model.zo.sync()
     model.muon.sync()
+    fo.layer_norm_sync()
     model.close()
     return losses
 

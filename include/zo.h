@@ -381,6 +381,9 @@ ZO_API zo_status zo_perturb_noalloc(void* W, int64_t m, int64_t n, int64_t ldw, 
  * is large against the spread costs no digits.  Every output is rounded once.  No
  * atomics: the same inputs give the same bits.  A row
  * with an infinity or NaN gives NaN in its own row of Y and dX (and in the column sums).
+ * zo_layernorm_sync_status -- synchronise the stream; ZO_ERR_TIMEOUT, once, where a wait of a
+ *   layer norm kernel on the current device has run out since it was last asked (its row, and
+ *   later rows of the same threads, are NaN then); ZO_OK otherwise.
  * Any alignment and any strides >= cols are taken; rows whose pointers, strides and width
  * allow 16-byte accesses run faster.  0 <= rows < 2^31, 1 <= cols < 2^31.  Outputs must not
  * overlap inputs.  Asynchronous on `stream` (void* cudaStream_t) of the current device.
@@ -397,6 +400,7 @@ ZO_API zo_status zo_layernorm_backward(const void* dY, int64_t lddy, const void*
                                        const float* mean, const float* rstd, void* dX,
                                        int64_t lddx, void* dweight, void* dbias, void* workspace,
                                        int64_t workspace_bytes, void* stream);
+ZO_API zo_status zo_layernorm_sync_status(void* stream);
 
 /*
  * Orthogonalised updates by Newton-Schulz products, and the Muon optimiser's step on them.

@@ -124,6 +124,7 @@ _SIGNATURES = {
                                            _c.c_int32, _c.c_void_p, _c.c_int32, _c.c_void_p,
                                            _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p,
                                            _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "zo_layernorm_sync_status": (_c.c_int32, [_c.c_void_p]),
     "zo_muon_workspace": (_c.c_int64, [_c.c_void_p, _c.c_int32]),
     "zo_muon_create": (_c.c_int32, [_c.POINTER(_c.c_void_p), _c.c_void_p, _c.c_int32, _c.c_void_p,
                                     _c.c_int64, _c.c_void_p]),
@@ -436,6 +437,10 @@ def zo_layernorm_backward(dY, X, dR, weight, mean, rstd, dX, dweight=None, dbias
         _vector(rstd, at, "rstd", rows, torch.float32, dev), pdx, lddx,
         _vector(dweight, at, "dweight", n, wdt, dev), _vector(dbias, at, "dbias", n, wdt, dev),
         ws, ws_bytes, _stream_handle(stream)), at)
+
+
+def zo_layernorm_sync_status(stream=None):
+    _check(LIB.zo_layernorm_sync_status(_stream_handle(stream)), "zo_layernorm_sync_status")
 
 
 def make_muon_matrix(W, G, M=None):

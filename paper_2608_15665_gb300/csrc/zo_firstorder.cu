@@ -9,6 +9,9 @@ namespace {
 
 using namespace zo::host;
 
+// Set by a layer norm kernel whose wait for its rows has run out; one per device.
+__device__ uint32_t g_layernorm_status;
+
 bool known_dtype(int32_t d) { return d == ZO_F32 || d == ZO_BF16; }
 int32_t elem_bytes(int32_t d) { return d == ZO_BF16 ? 2 : 4; }
 
@@ -30,6 +33,19 @@ int32_t sm_count() {
     count[dev] = n;
   }
   return count[dev];
+}
+
+// the current device's status word, or null
+uint32_t* status_word() {
+  static uint32_t* word[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  if (word[dev] == nullptr) {
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_layernorm_status) != cudaSuccess) return nullptr;
+    word[dev] = static_cast<uint32_t*>(p);
+  }
+  return word[dev];
 }
 
 zo_status check_rows(int64_t rows, int64_t cols, int32_t dtype, int32_t wdtype) {
@@ -79,7 +95,8 @@ zo_status zo_layernorm_forward(const void* X, int64_t ldx, const void* R, int64_
   a.wdtype = wdtype;
   a.eps = eps;
   const int32_t sms = sm_count();
-  if (sms <= 0) return refuse(ZO_ERR_CUDA, "zo_layernorm_forward: no usable CUDA device");
+  a.status = status_word();
+  if (sms <= 0 || !a.status) return refuse(ZO_ERR_CUDA, "zo_layernorm_forward: no usable CUDA device");
   ZO_CUDA(zo::launch_layernorm_forward(a, sms, reinterpret_cast<cudaStream_t>(stream)),
           "layer norm forward kernel");
   return ZO_OK;
@@ -120,6 +137,8 @@ zo_status zo_layernorm_backward(const void* dY, int64_t lddy, const void* X, int
                   "zo_layernorm_backward: the workspace is missing or smaller than "
                   "zo_layernorm_workspace(rows, cols)");
   zo::LayerNormArgs a{};
+  a.status = status_word();
+  if (!a.status) return refuse(ZO_ERR_CUDA, "zo_layernorm_backward: no usable CUDA device");
   a.dy = dY;
   a.x = X;
   a.r = dR;
@@ -140,6 +159,21 @@ zo_status zo_layernorm_backward(const void* dY, int64_t lddy, const void* X, int
   a.wdtype = wdtype;
   ZO_CUDA(zo::launch_layernorm_backward(a, sms, reinterpret_cast<cudaStream_t>(stream)),
           "layer norm backward kernels");
+  return ZO_OK;
+}
+
+zo_status zo_layernorm_sync_status(void* stream) {
+  const auto s = reinterpret_cast<cudaStream_t>(stream);
+  uint32_t* word = status_word();
+  if (!word) return refuse(ZO_ERR_CUDA, "zo_layernorm_sync_status: no usable CUDA device");
+  uint32_t status = 0;
+  ZO_CUDA(cudaMemcpyAsync(&status, word, sizeof(status), cudaMemcpyDeviceToHost, s), "read status");
+  ZO_CUDA(cudaStreamSynchronize(s), "stream synchronize");
+  if (status != 0) {
+    ZO_CUDA(cudaMemsetAsync(word, 0, sizeof(status), s), "clear status");
+    ZO_CUDA(cudaStreamSynchronize(s), "stream synchronize");
+    return refuse(ZO_ERR_TIMEOUT, "layer norm: a device-side wait ran out");
+  }
   return ZO_OK;
 }
 

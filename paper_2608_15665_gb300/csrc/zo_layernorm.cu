@@ -120,6 +120,7 @@ forward_ring_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   constexpr int kBlock = block_of(kGroup), kGroups = kBlock / kGroup;
   __shared__ float buf[2][2][32];
   __shared__ uint64_t full[kGroups][kMaxStages];
+  __shared__ Lost lost[kGroups];
   extern __shared__ __align__(128) uint8_t dyn[];
   const int t = threadIdx.x % kGroup, grp = threadIdx.x / kGroup;
   const int64_t cols = a.cols;
@@ -129,6 +130,7 @@ forward_ring_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
                dyn + (size_t)grp * stages * (a.r ? 2 : 1) * slot, full[grp]};
   if (t == 0) {
     for (int s = 0; s < stages; ++s) sm100::mbar_init(&full[grp][s], 1);
+    lost[grp].yes = 0;
     sm100::fence_mbar_init();
   }
   __syncthreads();
@@ -152,25 +154,32 @@ forward_ring_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   if (a.bias)
     load_columns<TW, kElems, kGroup, V, true>(static_cast<const TW*>(a.bias) + col, inside, 0.0f, bv);
   int flip = 0;
+  bool gone = false;
   for (int64_t row = row0; row < a.rows; row += stride, flip ^= 1) {
-    const bool came = ring.ready();
+    float2 s = both(0.0f), q = both(0.0f);
+    const bool came = ring.ready(lost[grp], gone);
+    if (!came) {
+      s = both(nan_value());                   // the row's sum, and with it all of the row, is NaN
+      ring.lose(lost[grp], row);
+    }
     float2 v[kElems / 2];
     load_columns<T, kElems, kGroup, V, false>(ring.at(0, row) + col, inside, 0.0f, v);
     if (a.r) {
-      float2 q[kElems / 2];
-      load_columns<T, kElems, kGroup, V, false>(ring.at(1, row) + col, inside, 0.0f, q);
+      float2 o[kElems / 2];
+      load_columns<T, kElems, kGroup, V, false>(ring.at(1, row) + col, inside, 0.0f, o);
 #pragma unroll
-      for (int i = 0; i < kElems / 2; ++i) v[i] = rounded<T>(add2(v[i], q[i]));
+      for (int i = 0; i < kElems / 2; ++i) v[i] = rounded<T>(add2(v[i], o[i]));
+      if (!came) to_nan(v);
       store_columns<T, kElems, kGroup, V>(static_cast<T*>(a.h) + row * a.ldh + col, inside, v);
     }
-    float2 s = both(0.0f), q = both(0.0f);
 #pragma unroll
     for (int i = 0; i < kElems / 2; ++i) s = add2(s, v[i]);
-    float mean = group_sum<kGroup>(s.x + s.y, buf[flip][0]) * inv_n;
+    const float mean = group_sum<kGroup>(s.x + s.y, buf[flip][0]) * inv_n;
     // every thread of the group has read the stage
-    if (t == 0 && row + stages * stride < a.rows) ring.fetch(row + stages * stride, ring.stage);
+    gone = lost[grp].yes;
+    if (t == 0 && row + stages * stride < a.rows && !gone)
+      ring.fetch(row + stages * stride, ring.stage);
     ring.advance();
-    if (!came) mean = __int_as_float(0x7FC00000);
     const float2 minus = both(-mean);
 #pragma unroll
     for (int i = 0; i < kElems / 2; ++i) {
@@ -193,6 +202,7 @@ forward_ring_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
       if (a.rstd) a.rstd[row] = rstd;
     }
   }
+  if (t == 0) ring.finish(lost[grp], row0, stride, a.rows, a.status);
 }
 
 template <typename T, typename TW, int V>

@@ -135,6 +135,12 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return r.f;
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float nan_value() { return __int_as_float(0x7FC00000); }
+template <int kPairs>
+__device__ __forceinline__ void to_nan(float2 (&v)[kPairs]) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) v[i] = both(nan_value());
+}
 
 // A thread's columns of a row as pairs: chunks of V columns, chunk e at column (e kGroup + t) V.
 // f(e) says whether chunk e lies inside the row; the values of the others are `rest`.
@@ -255,6 +261,12 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       : "memory");
 }
 
+// the first row of a group whose copies did not come in time
+struct Lost {
+  volatile int yes;
+  volatile int64_t row;
+};
+
 // The rows of one group, `stages` of them in flight; up to three matrices, row `row` of each
 // in one stage.  `slot` bytes hold a row and the rest of its first and last 16.
 template <typename T>
@@ -287,9 +299,29 @@ struct Ring {
         bulk_load(dst + m * slot, reinterpret_cast<const uint8_t*>(p) - lead(p), part[m], &full[s]);
       }
   }
-  // Waits for the stage of row `row`; the matrices' places in it are then at(m, row).  False: the
-  // copies have not come within the limit, and the row's results are NaN.
-  __device__ bool ready() const { return sm100::mbar_wait_bounded(&full[stage], phase, nullptr, kWait); }
+  // Waits for the present stage, whose row's places in it are then at(m, row).  False: the copies have
+  // not come within the limit, or a row before was lost (`gone`, read of lost.yes behind a barrier of
+  // the group); the row's results are NaN, and the thread calls lose().  (The barrier alone does
+  // not tell a stage that was not fetched again: two rounds on, its parity is the last copies'.)
+  __device__ bool ready(const Lost& lost, bool gone) const {
+    return !gone && (sm100::mbar_try_wait(&full[stage], phase) ||
+                     sm100::mbar_wait_bounded(&full[stage], phase, &lost.yes, kWait));
+  }
+  static __device__ void lose(Lost& lost, int64_t row) {
+    if (lost.yes) return;
+    lost.row = row;
+    lost.yes = 1;
+  }
+  // By the fetching thread after the last row: where one was lost (after which nothing is fetched: a
+  // stage whose bytes may be still to come is not armed again), the call's status is set, and the
+  // copies that were in flight come to rest.
+  __device__ void finish(const Lost& lost, int64_t row0, int64_t stride, int64_t rows, uint32_t* status) const {
+    if (!lost.yes) return;
+    atomicOr(status, 1u);
+    int64_t k = (lost.row - row0) / stride;
+    for (int s = 0; s < stages && row0 + k * stride < rows; ++s, ++k)
+      sm100::mbar_wait_bounded(&full[k % stages], (uint32_t)(k / stages & 1), nullptr, kWait);
+  }
   __device__ const T* at(int m, int64_t row) const {
     return reinterpret_cast<const T*>(smem + (size_t)(stage * n + m) * slot + lead(row_of(m, row)));
   }

@@ -16,6 +16,7 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   static_assert(kElems > 0, "rows in registers");
   __shared__ float buf[2][2][32];
   __shared__ uint64_t full[kGroups][kMaxStages];
+  __shared__ Lost lost[kGroups];
   extern __shared__ __align__(128) uint8_t dyn[];   // the ring; then dw and db of each warp
   const int t = threadIdx.x % kGroup, grp = threadIdx.x / kGroup;
   const int64_t cols = a.cols;
@@ -26,6 +27,7 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
   if constexpr (kRing) {
     if (t == 0) {
       for (int s = 0; s < stages; ++s) sm100::mbar_init(&full[grp][s], 1);
+      lost[grp].yes = 0;
       sm100::fence_mbar_init();
     }
     __syncthreads();
@@ -51,6 +53,7 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
         if (row0 + s * stride < a.rows) ring.fetch(row0 + s * stride, s);
   }
   int flip = 0;
+  bool gone = false;
   float mean_next = row0 < a.rows ? a.mean[row0] : 0.0f, rstd_next = row0 < a.rows ? a.rstd[row0] : 0.0f;
   // the groups of a warp go on together
   const int64_t first = kGroup < 32 ? row0 - (threadIdx.x % 32) / kGroup : row0;
@@ -67,7 +70,12 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
     const auto here = [&](int e) { return live && inside(e); };
     float2 xh[kPairs], g[kPairs];
     if constexpr (kRing) {
-      if (!ring.ready()) mean = __int_as_float(0x7FC00000);
+      if (!ring.ready(lost[grp], gone)) {
+        // NaN in the row's sums, and with them in all of its dx, and in this thread's dw and db
+        mean = nan_value();
+        to_nan(db);
+        ring.lose(lost[grp], row);
+      }
       load_columns<T, kElems, kGroup, V, false>(ring.at(0, row) + col, here, mean, xh);
       load_columns<T, kElems, kGroup, V, false>(ring.at(1, row) + col, here, 0.0f, g);
     } else {
@@ -119,9 +127,14 @@ backward_kernel(const LayerNormArgs a, int stages, uint32_t slot) {
       } else {
         __syncwarp();
       }
-      if (t == 0 && row + stages * stride < a.rows) ring.fetch(row + stages * stride, ring.stage);
+      gone = lost[grp].yes;
+      if (t == 0 && row + stages * stride < a.rows && !gone)
+        ring.fetch(row + stages * stride, ring.stage);
       ring.advance();
     }
+  }
+  if constexpr (kRing) {
+    if (t == 0) ring.finish(lost[grp], row0, stride, a.rows, a.status);
   }
   if (a.partial == nullptr) return;
   if constexpr (kGroups > 1) {

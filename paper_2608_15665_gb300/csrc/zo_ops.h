@@ -23,6 +23,7 @@ struct LayerNormArgs {
   int64_t ldx, ldr, lddy, ldy, ldh, lddx;
   int32_t dtype, wdtype;          // of x, r, y, h, dy, dx, dr; of weight, bias, dweight, dbias
   float eps;
+  uint32_t* status;               // set where a wait has run out
 };
 
 cudaError_t launch_layernorm_forward(const LayerNormArgs& a, int32_t sms, cudaStream_t s);

@@ -6,7 +6,8 @@ below it.  This module allocates the outputs and workspaces of those operators n
 caller's tensors and launches them in the order of PyTorch's current stream:
 
 * ``layer_norm`` / ``layer_norm_backward`` -- the norm's forward and backward pass, and
-  ``LayerNorm``, the two as one ``torch.autograd.Function``;
+  ``LayerNorm``, the two as one ``torch.autograd.Function``; ``layer_norm_sync`` asks
+  whether all of them went well;
 * ``Orthogonalizer`` / ``Muon`` -- handles over matrices, bound to one stream.
 
 No arithmetic happens here.
@@ -141,6 +142,13 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dresidual=None, wdtype=None, 
           _code(dt, at, "x"), pw, _code(wdtype, at, "weight"), pm, ps, dx.data_ptr(), cols, pdw,
           pdb, pws, ws_bytes)
     return dx, dw, db
+
+
+def layer_norm_sync(device=None):
+    """Waits for the current stream, and raises where a wait inside a layer norm's kernel has run
+    out on this device since it was last asked (rows of that call are NaN then)."""
+    with torch.cuda.device(device):
+        zb.zo_layernorm_sync_status(torch.cuda.current_stream())
 
 
 class LayerNorm(torch.autograd.Function):
