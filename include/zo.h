@@ -434,13 +434,16 @@ ZO_API zo_status zo_layernorm_sync_status(void* stream);
  * eps >= 0 (1e-7 is usual); a zero matrix gives zero (with eps = 0 too).  U may have any finite
  *   scale: where its squares leave fp32's range it is scaled by a power of two before its norm.
  * Precision: sums are fp32.  Iterates are held as power-of-two-scaled fp16 pairs (~22
- *   significant bits).  Their products are of fp32 grade where W is fp32 or min(m, n) <= 128;
- *   for larger bf16 matrices the products take single fp16 factors (11 bits), whose error in
- *   the result is of the order of rounding it to bf16.  A U with ||U||_F far below eps loses digits: the
+ *   significant bits).  Their products are of fp32 grade where W is fp32, where min(m, n) <= 128
+ *   and where the matrix's grade asks for it; for larger bf16 matrices the products take single
+ *   fp16 factors (11 bits) otherwise, and the result is up to 1.25 times as far from the
+ *   definition as its rounding to bf16 alone puts it.  Their products take about a third of the
+ *   time of the fp32 grade's.  A U with ||U||_F far below eps loses digits: the
  *   scaled iterate resolves 2^-38.  A NaN or infinity in U_i gives NaN in all of W_i.
  * Captured into a graph, the calls may be replayed on other contents of G, M and W.
  */
 enum { ZO_MUON_ADJUST_NONE = 0, ZO_MUON_ADJUST_ASPECT = 1, ZO_MUON_ADJUST_RMS = 2 };
+enum { ZO_MUON_GRADE_DTYPE = 0, ZO_MUON_GRADE_F32 = 1 };
 
 typedef struct zo_muon_matrix {
   void* W;            /* device; m x n, row stride ldw elements, dtype below */
@@ -450,6 +453,7 @@ typedef struct zo_muon_matrix {
   int64_t ldw, ldg;
   int32_t dtype;      /* ZO_F32 or ZO_BF16 */
   int32_t grad_dtype; /* ZO_F32 or ZO_BF16 */
+  int32_t grade;      /* of the products: by dtype and size, or fp32's in any case */
 } zo_muon_matrix;
 
 typedef struct zo_muon_ctx zo_muon_ctx;

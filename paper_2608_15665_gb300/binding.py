@@ -37,6 +37,8 @@ ZO_OPT_MUON = 2
 ZO_MUON_ADJUST_NONE = 0
 ZO_MUON_ADJUST_ASPECT = 1
 ZO_MUON_ADJUST_RMS = 2
+ZO_MUON_GRADE_DTYPE = 0
+ZO_MUON_GRADE_F32 = 1
 
 ZO_OPTION_WPASS_PATH = 0
 ZO_OPTION_TIMING = 1
@@ -77,6 +79,7 @@ class zo_muon_matrix(ctypes.Structure):
         ("ldg", ctypes.c_int64),
         ("dtype", ctypes.c_int32),
         ("grad_dtype", ctypes.c_int32),
+        ("grade", ctypes.c_int32),
     ]
 
 

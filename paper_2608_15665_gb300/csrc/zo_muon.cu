@@ -64,6 +64,8 @@ zo_status check_matrix(const zo_muon_matrix& m) {
   if ((m.dtype != ZO_F32 && m.dtype != ZO_BF16) ||
       (m.grad_dtype != ZO_F32 && m.grad_dtype != ZO_BF16))
     return refuse(ZO_ERR_DTYPE, "unknown dtype in zo_muon_matrix");
+  if (m.grade != ZO_MUON_GRADE_DTYPE && m.grade != ZO_MUON_GRADE_F32)
+    return refuse(ZO_ERR_INVALID_ARG, "unknown grade in zo_muon_matrix");
   if (m.m < 1 || m.n < 1 || m.m >= (int64_t(1) << 24) || m.n >= (int64_t(1) << 24) ||
       m.ldw < m.n || m.ldg < m.n || m.ldw >= (int64_t(1) << 40) || m.ldg >= (int64_t(1) << 40) ||
       std::min(m.m, m.n) > (int64_t(1) << 16))
@@ -206,7 +208,7 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
     d.grad_bf16 = m.grad_dtype == ZO_BF16;
     d.bf16 = m.dtype == ZO_BF16;
     d.tall = m.m > m.n;
-    d.pairs = zo::ortho_pairs(d.bf16, d.p);
+    d.pairs = m.grade == ZO_MUON_GRADE_F32 || zo::ortho_pairs(d.bf16, d.p);
     d.wide_rows = aligned16(m.W) && m.ldw * (d.bf16 ? 2 : 4) % 16 == 0;
     d.small = zo::ortho_mma_cluster(d.p, d.c);
     if (d.small == 0) d.small = zo::ortho_small_cluster(d.p, d.c);

@@ -185,7 +185,7 @@ class _MuonContext:
     (In a graph's capture too, where the context's own is not the legacy default stream, which
     CUDA keeps out of captures.)"""
 
-    def __init__(self, weights, grads, momenta, stream):
+    def __init__(self, weights, grads, momenta, stream, precise):
         self.ctx = None
         at = type(self).__name__
         if not weights:
@@ -196,6 +196,9 @@ class _MuonContext:
             raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at,
                              "the matrices and the stream have to be on one CUDA device")
         mats = [zb.make_muon_matrix(W, G, M) for W, G, M in zip(weights, grads, momenta)]
+        if precise:
+            for mat in mats:
+                mat.grade = zb.ZO_MUON_GRADE_F32
         with torch.cuda.device(dev):
             current = torch.cuda.current_stream()
             self.stream = current if stream is None else stream
@@ -233,15 +236,16 @@ class _MuonContext:
 
 class Orthogonalizer(_MuonContext):
     """``op()`` orthogonalises every input by Newton-Schulz steps into its output (allocated
-    with the input's shape and type if not given).  All on one CUDA device."""
+    with the input's shape and type if not given).  All on one CUDA device.  precise: products of
+    fp32 grade for bf16 matrices of more than 128 rows (and columns) too."""
 
-    def __init__(self, inputs, outputs=None, stream=None):
+    def __init__(self, inputs, outputs=None, stream=None, precise=False):
         self.inputs = list(inputs)
         self.outputs = ([torch.empty(G.shape, dtype=G.dtype, device=G.device) for G in self.inputs]
                         if outputs is None else list(outputs))
         if len(self.outputs) != len(self.inputs):
             raise ValueError("as many outputs as inputs are needed")
-        super().__init__(self.outputs, self.inputs, [None] * len(self.inputs), stream)
+        super().__init__(self.outputs, self.inputs, [None] * len(self.inputs), stream, precise)
 
     def __call__(self, steps=5, coeffs=None, eps=1e-7):
         self._call(zb.zo_orthogonalize, steps, coeffs, eps)
@@ -251,9 +255,9 @@ class Orthogonalizer(_MuonContext):
 class Muon(_MuonContext):
     """The Muon optimiser over a list of weights (bf16 or fp32, on one CUDA device) whose
     gradients live in ``grads`` (allocated beside the weights, zero, if not given) and whose
-    fp32 momenta in ``momenta``."""
+    fp32 momenta in ``momenta``.  precise: as for ``Orthogonalizer``."""
 
-    def __init__(self, weights, grads=None, momenta=None, stream=None):
+    def __init__(self, weights, grads=None, momenta=None, stream=None, precise=False):
         self.weights = list(weights)
         self.grads = ([torch.zeros(W.shape, dtype=W.dtype, device=W.device) for W in self.weights]
                       if grads is None else list(grads))
@@ -261,7 +265,7 @@ class Muon(_MuonContext):
                          for W in self.weights] if momenta is None else list(momenta))
         if not len(self.weights) == len(self.grads) == len(self.momenta):
             raise ValueError("as many gradients and momenta as weights are needed")
-        super().__init__(self.weights, self.grads, self.momenta, stream)
+        super().__init__(self.weights, self.grads, self.momenta, stream, precise)
 
     def step(self, lr, momentum=0.95, nesterov=True, weight_decay=0.0, adjust="aspect", steps=5,
              coeffs=None, eps=1e-7):
