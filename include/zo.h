@@ -420,7 +420,8 @@ ZO_API zo_status zo_layernorm_sync_status(void* stream);
  *   each call.  workspace: caller-owned device memory of at least zo_muon_workspace(mats,
  *   n_mats) bytes, 256-byte aligned, kept until zo_muon_destroy and used by this context
  *   alone.  The tables are copied to it on `stream` (void* cudaStream_t), on which every
- *   later call launches.  Nothing else is allocated on the device.
+ *   later call launches; the call returns when they are there.  Nothing else is allocated on
+ *   the device.
  * zo_orthogonalize -- W_i <- rnd(NS(G_i)) for every matrix.
  * zo_muon_step -- for every matrix
  *     M_i <- momentum M_i + G_i,  U_i = nesterov ? G_i + momentum M_i : M_i  (no M: U_i = G_i)

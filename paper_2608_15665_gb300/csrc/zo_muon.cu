@@ -547,6 +547,8 @@ zo_status zo_muon_create(zo_muon_ctx** out, const zo_muon_matrix* mats, int32_t 
     if (!L.tiles.empty()) std::memcpy(image.data() + L.tiles_at, L.tiles.data(), sizeof(zo::OrthoTile) * L.tiles.size());
     ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),
             "upload tables");
+    // (a copy from pageable memory may be asynchronous where the GPU reads the host's page tables)
+    ZO_CUDA(cudaStreamSynchronize(c->stream), "stream synchronize");
     L.mats.clear();
     L.units.clear();
     L.tiles.clear();
