@@ -9,14 +9,22 @@
 //          barrier a step is enough);
 //   Poly   B = b A + c A A, by every CTA for itself;
 //   Apply  X' = a X + B X in place: a warp takes all rows of eight or sixteen columns.
-// Products are hi.lo + lo.hi + hi.hi with fp32 sums, by warp-wide m16n8k16 MMAs on registers:
-// at these sizes a step is a chain of short latencies, and the round trip of a tcgen05.mma
-// (issue, commit, wait, Tensor Memory to registers: ~2.5 K cycles a product at 64 x 64, against
-// ~1 K here) would be most of it; from 65 rows on the larger MMAs win (zo_ortho_small.cu).
+// Products are hi.lo + lo.hi + hi.hi with fp32 sums (to 32 rows lo.lo too in Poly and Apply), by
+// warp-wide m16n8k16 MMAs on registers: at these sizes a step is a chain of short latencies, and
+// the round trip of a tcgen05.mma (issue, commit, wait, Tensor Memory to registers: ~2.5 K cycles
+// a product at 64 x 64, against ~1 K here) would be most of it; from 65 rows on the larger MMAs
+// win (zo_ortho_small.cu).
+// An MMA's fp32 sum rounds towards zero, which few singular directions do not average out.  At 64
+// rows hi.hi is therefore summed apart from the small products, 16 of K at a time, to nearest;
+// at 16 rows so is X X^T, whose K is long.  Mean errors of sets so, and in one sum without lo.lo
+// (fp32 evaluation): 112 of 64 x 64 7.2e-7, 1.31e-6 (1.19e-6); 30 of 64 x 256 1.32e-6, 2.56e-6
+// (1.49e-6); 100 of 32 x 64 1.35e-6, 1.65e-6 (1.13e-6); 448 of 8 x 8 6.9e-7, 8.6e-7 (7.5e-7); 20 of
+// 8 x 8000 7.5e-7, 1.43e-6 (8.3e-7).  It takes 8 to 11% of the time at 64 rows, 4% at 32, 1 to 4% at
+// 16, and none where X is in registers.
 // Between load and scaling, and between the last step and the update of W, the planes hold the
 // upper and lower halves of fp32 values, so that the caller's matrices are read and written
 // once, in their own order.
-// Bound by the chain's latencies.  224 matrices of 32 x 32 fp32 9.5 us; Muon steps of forty 8 x
+// Bound by the chain's latencies.  224 matrices of 32 x 32 fp32 9.8 us; Muon steps of forty 8 x
 // 5120 26 us: five steps of 6 K cycles, half of them the cluster's sums, and 14 K of load, norm
 // and store.
 #include <algorithm>
@@ -78,14 +86,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// the same, m16n8k8
-__device__ __forceinline__ void mma_k8(float (&d)[4], const uint32_t (&a)[2], uint32_t b) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(b));
-}
 // an 8 x 8 matrix of halves, a row's pair per lane, transposed
 __device__ __forceinline__ uint32_t transposed(uint32_t a) {
   uint32_t d;
@@ -110,7 +110,8 @@ struct Steps {
 
 // X' = a X + B X in kNb x 8 columns from j0 on, by one warp: X's columns are in registers
 // before any of them is written, and the sums of all rows and columns run side by side (an MMA
-// waits for the one before it on the same sums).
+// waits for the one before it on the same sums).  At 64 rows hi.hi comes after all the others, for
+// which B_hi is read twice: its sums beside theirs would not fit the registers.
 template <int P, int kNb>
 __device__ __forceinline__ void apply(__half* xh, __half* xl, const __half* bh, const __half* bl,
                                       int pitch, int j0, float s0, float s1, bool last) {
@@ -146,16 +147,39 @@ __device__ __forceinline__ void apply(__half* xh, __half* xl, const __half* bh, 
       const int at = (16 * m + (lane & 15)) * kBp + 16 * k + (lane >> 4) * 8;
       ldmatrix_x4(b[0], smem_u32(bh + at));
       ldmatrix_x4(b[1], smem_u32(bl + at));
+      if constexpr (P <= 32) {
+#pragma unroll
+        for (int n = 0; n < kNb; ++n)
+          mma(d[m][n], b[1], x[1][k][n / 2][n % 2 * 2], x[1][k][n / 2][n % 2 * 2 + 1]);
+      }
 #pragma unroll
       for (int n = 0; n < kNb; ++n)
         mma(d[m][n], b[0], x[1][k][n / 2][n % 2 * 2], x[1][k][n / 2][n % 2 * 2 + 1]);
 #pragma unroll
       for (int n = 0; n < kNb; ++n)
         mma(d[m][n], b[1], x[0][k][n / 2][n % 2 * 2], x[0][k][n / 2][n % 2 * 2 + 1]);
+      if constexpr (P != 64) {
 #pragma unroll
-      for (int n = 0; n < kNb; ++n)
-        mma(d[m][n], b[0], x[0][k][n / 2][n % 2 * 2], x[0][k][n / 2][n % 2 * 2 + 1]);
+        for (int n = 0; n < kNb; ++n)
+          mma(d[m][n], b[0], x[0][k][n / 2][n % 2 * 2], x[0][k][n / 2][n % 2 * 2 + 1]);
+      }
     }
+  if constexpr (P == 64) {
+#pragma unroll
+    for (int m = 0; m < kK; ++m)
+#pragma unroll
+      for (int k = 0; k < kK; ++k) {
+        uint32_t b[4];
+        ldmatrix_x4(b, smem_u32(bh + (16 * m + (lane & 15)) * kBp + 16 * k + (lane >> 4) * 8));
+#pragma unroll
+        for (int n = 0; n < kNb; ++n) {
+          float g[4] = {};
+          mma(g, b, x[0][k][n / 2][n % 2 * 2], x[0][k][n / 2][n % 2 * 2 + 1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[m][n][e] += g[e];
+        }
+      }
+  }
   __syncwarp();
 #pragma unroll
   for (int m = 0; m < kK; ++m)
@@ -179,7 +203,10 @@ __device__ __forceinline__ void apply(__half* xh, __half* xl, const __half* bh, 
 // operand of X'^T = a X^T + X^T B: lane (g, t) holds rows 2 t, 2 t + 1 of columns g and g + 8.
 // That is also how the product's sums lie, so Apply reads nothing but B; Gram's operands are the
 // same 8 x 8 blocks transposed.  (Sixteen rows would take twice the registers: three CTAs an SM,
-// 80 registers a thread, spilled and were slower than shared memory.)
+// 80 registers a thread, spilled and were slower than shared memory.  Five tiles, 5120 columns of
+// a cluster of eight, are what the registers hold beside the rest: with eight, spills take 7% of
+// 224 of 8 x 8 and 3% of forty 8 x 5120, 26.4 -> 27.3 us; forty 8 x 5136 would take 28 us there,
+// 39 from shared memory.)
 constexpr int kTiles = 5;
 struct Columns {
   uint32_t hi[kTiles][2], lo[kTiles][2];
@@ -202,21 +229,27 @@ __device__ __forceinline__ void take(Columns& x, const __half* xh, const __half*
              reinterpret_cast<__half*>(&x.hi[i][q]), reinterpret_cast<__half*>(&x.lo[i][q]));
   }
 }
-// the warp's share of X X^T
+// the warp's share of X X^T: hi above lo, eight rows each, so that an MMA is two products, and every
+// 16 columns added up to nearest
 __device__ __forceinline__ void gram(const Columns& x, int cs, float* to) {
   constexpr int kPitch = Shape<16>::kPitch;
   const int lane = threadIdx.x & 31;
-  float small[4] = {}, large[4] = {};                 // hi.lo + lo.hi, and hi.hi
+  float2 small = make_float2(0.f, 0.f), large = small;
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     if (tile_col(i) >= cs) break;
-    const uint32_t h[4] = {transposed(x.hi[i][0]), 0, transposed(x.hi[i][1]), 0};
-    const uint32_t l[4] = {transposed(x.lo[i][0]), 0, transposed(x.lo[i][1]), 0};
-    mma(small, h, l[0], l[2]);
-    mma(large, h, h[0], h[2]);
-    mma(small, l, h[0], h[2]);
+    const uint32_t h0 = transposed(x.hi[i][0]), h1 = transposed(x.hi[i][1]);
+    const uint32_t l0 = transposed(x.lo[i][0]), l1 = transposed(x.lo[i][1]);
+    const uint32_t both[4] = {h0, l0, h1, l1};
+    float p[4] = {}, q[4] = {};                       // hi.hi over lo.hi, hi.lo over lo.lo
+    mma(p, both, h0, h1);
+    mma(q, both, l0, l1);
+    large.x += p[0];
+    large.y += p[1];
+    small.x += p[2] + (q[0] + q[2]);
+    small.y += p[3] + (q[1] + q[3]);
   }
-  const float2 v = make_float2(small[0] + large[0], small[1] + large[1]);
+  const float2 v = make_float2(small.x + large.x, small.y + large.y);
   float* at = to + (lane >> 2) * kPitch + (lane & 3) * 2;
 #pragma unroll
   for (int q = 0; q < 4; ++q)                         // the rest of 16 x 16 is zero
@@ -232,10 +265,11 @@ __device__ __forceinline__ void apply(Columns& x, int cs, const __half* bh, cons
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     if (tile_col(i) >= cs) break;
+    // hi beside lo: one MMA is (hi + lo) B_lo, the other (hi + lo) B_hi
+    const uint32_t both[4] = {x.hi[i][0], x.hi[i][1], x.lo[i][0], x.lo[i][1]};
     float d[4] = {};
-    mma_k8(d, x.hi[i], b_lo);
-    mma_k8(d, x.lo[i], b_hi);
-    mma_k8(d, x.hi[i], b_hi);
+    mma(d, both, b_lo, b_lo);
+    mma(d, both, b_hi, b_hi);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const float2 o = pair2(reinterpret_cast<const __half*>(&x.hi[i][q]),
@@ -341,11 +375,10 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
     } else {
       // ---- X X^T: rows 16 m, columns 8 (kN n0 ..), K tiles split, split + kSplits, ...
       const int m = warp % S::kM, split = warp / S::kM % S::kSplits, n0 = warp / (S::kM * S::kSplits) * S::kN;
-      // An MMA's fp32 sum rounds towards zero.  At 64 rows, where one warp goes over all of a CTA's
-      // K, hi.hi of 16 columns at a time is added up here, to nearest (48 x 3008: 2.8e-6 of the
-      // result instead of 4.2e-6); with K dealt to four or eight warps it made no difference and
-      // took 5 to 20% of the call.
-      constexpr bool kNearest = P == 64;
+      // hi.hi of 16 columns at a time is added up here, to nearest; not at 32 rows, where K is dealt
+      // to four warps and that took 6% of the time for a tenth of the error.  (lo.lo made no
+      // difference to the error.)
+      constexpr bool kNearest = P != 32;
       float d[S::kN][4] = {}, small[kNearest ? S::kN : 1][4] = {};
       for (int kt = split; kt < cs / 16; kt += S::kSplits) {
         uint32_t a[2][4];
@@ -451,7 +484,7 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
             const int at = (16 * m + row + 8 * h) * kPitch + 16 * q + 8 * t + col;
             v[t][h] = pair2(ah + at, al + at);
           }
-        float d[2 * kQ][4] = {};
+        float d[2 * kQ][4] = {}, large[P == 64 ? 2 * kQ : 1][4] = {};    // (large: hi.hi)
 #pragma unroll
         for (int kt = 0; kt < S::kM; ++kt) {
           uint32_t a[2][4], b[kQ][2][4];
@@ -464,12 +497,31 @@ ortho_mma_kernel(const OrthoMat* __restrict__ mats, const int* __restrict__ whic
             ldmatrix_x4(b[t][0], smem_u32(ah + bt));
             ldmatrix_x4(b[t][1], smem_u32(al + bt));
           }
+          if constexpr (P <= 32) {
+#pragma unroll
+            for (int h = 0; h < 2 * kQ; ++h) mma(d[h], a[1], b[h / 2][1][h % 2], b[h / 2][1][h % 2 + 2]);
+          }
 #pragma unroll
           for (int h = 0; h < 2 * kQ; ++h) mma(d[h], a[0], b[h / 2][1][h % 2], b[h / 2][1][h % 2 + 2]);
 #pragma unroll
           for (int h = 0; h < 2 * kQ; ++h) mma(d[h], a[1], b[h / 2][0][h % 2], b[h / 2][0][h % 2 + 2]);
 #pragma unroll
-          for (int h = 0; h < 2 * kQ; ++h) mma(d[h], a[0], b[h / 2][0][h % 2], b[h / 2][0][h % 2 + 2]);
+          for (int h = 0; h < 2 * kQ; ++h) {
+            if constexpr (P == 64) {
+              float g[4] = {};
+              mma(g, a[0], b[h / 2][0][h % 2], b[h / 2][0][h % 2 + 2]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) large[h][e] += g[e];
+            } else {
+              mma(d[h], a[0], b[h / 2][0][h % 2], b[h / 2][0][h % 2 + 2]);
+            }
+          }
+        }
+        if constexpr (P == 64) {
+#pragma unroll
+          for (int h = 0; h < 2 * kQ; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[h][e] += large[h][e];
         }
 #pragma unroll
         for (int t = 0; t < 2 * kQ; ++t)
