@@ -377,8 +377,8 @@ ZO_API zo_status zo_perturb_noalloc(void* W, int64_t m, int64_t n, int64_t ldw, 
  *   workspace: caller-owned device memory of at least zo_layernorm_workspace(rows, cols)
  *     bytes, 16-byte aligned, for the column sums' partial rows (unused without dweight and
  *     dbias); calls whose work overlaps need one each.
- * Sums and statistics are held in fp32; the variance is taken about the mean, so a mean that
- * is large against the spread costs no digits.  Every output is rounded once.  No
+ * Sums and statistics are held in fp32 (squared distances from the mean overflow past 1.8e19);
+ * the variance is taken about the mean, so a mean that is large against the spread costs no digits.  Every output is rounded once.  No
  * atomics: the same inputs give the same bits.  A row
  * with an infinity or NaN gives NaN in its own row of Y and dX (and in the column sums).
  * zo_layernorm_sync_status -- synchronise the stream; ZO_ERR_TIMEOUT, once, where a wait of a

@@ -28,9 +28,12 @@
 // Few rows, and narrow ones: straight from memory.  Few wide rows go to CTAs with eight columns
 // a thread, for latency.
 //
-// Measured: forward 4096 x 4096 bf16 with a residual 22.4 us (6.0 TB/s), 50001 x 768 fp32 52.7 us
-// (5.8), 8192 x 8192 bf16 63 us (4.3); backward 16384 x 5120 bf16 with a residual 96-104 us
-// (6.4-7.0 TB/s with the column sums), 2048 x 2048 11 us; one row of 5120 2.1 us.
+// Measured, in graphs of calls over inputs larger than L2: forward 4096 x 4096 bf16 with a residual
+// 22.7 us (5.9 TB/s), 50001 x 768 fp32 52.7 us (5.8), 8192 x 8192 bf16 61 us (4.4); backward 16384 x
+// 5120 bf16 with a residual 104 us (6.5 TB/s with the column sums), 2048 x 2048 12.0 us (10.8 us
+// its first kernel alone; the sums' launch lies under it); one row of 5120 2.1 us.  Rows that
+// are swept: 2048 x 16384 bf16 57 us forward (2.3 TB/s), 160 us backward (1.3), against 24 and 54 us
+// at 12288 columns.
 //
 // The backward pass keeps dw and db of a thread's own columns in registers over all its
 // rows, so that each CTA writes one row of partial sums, which a second kernel adds up in a
