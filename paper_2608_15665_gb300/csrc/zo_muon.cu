@@ -136,7 +136,7 @@ int64_t deal(const std::vector<zo::OrthoTile>& tiles, int32_t n, TileCost cost,
 std::vector<zo::OrthoTile> make_tiles(const Layout& L, size_t first, size_t next, int pr, int phase,
                                       bool narrow) {
   std::vector<zo::OrthoTile> tiles;
-  int32_t slots = 0;
+  int32_t slots = 0, sums = 0;
   for (size_t i = first; i < next; ++i) {
     const zo::OrthoMat& d = L.mats[i];
     if (d.small || d.pairs != pr) continue;
@@ -147,8 +147,9 @@ std::vector<zo::OrthoTile> make_tiles(const Layout& L, size_t first, size_t next
       for (int64_t c = 0; c < end; c += zo::ortho_tile_cols(pr != 0, narrow)) {
         for (int32_t k = 0; k < of; ++k)
           tiles.push_back({(int32_t)i, (int32_t)r, (int32_t)c, d.maps, stages * k / of,
-                           stages * (k + 1) / of, of > 1 ? slots : -1, k, of});
+                           stages * (k + 1) / of, of > 1 ? slots : -1, k, of, sums});
         slots += of > 1;
+        sums += of > 1 ? of : 0;
       }
     }
   }
@@ -274,7 +275,7 @@ zo_status plan(const zo_muon_matrix* mats, int32_t n_mats, Layout* out) {
         for (const zo::OrthoTile& t : tiles)
           if (t.parts > 1) {
             slots_used = std::max(slots_used, t.slot + 1);
-            sums_floats = std::max(sums_floats, (int64_t)(t.slot + 1) * zo::kOrthoMaxParts *
+            sums_floats = std::max(sums_floats, (int64_t)(t.sum0 + t.parts) *
                                                     zo::ortho_part_floats(pr != 0, list.narrow != 0));
           }
         g.list[pr][phase] = (int32_t)L.lists.size();

@@ -54,18 +54,19 @@ struct OrthoMat {
 // kOrthoUnitRows x kOrthoUnitCols elements of U: (matrix, first row, first column, slot)
 constexpr int kOrthoUnitRows = 32, kOrthoUnitCols = 256;
 // A tile of a product, kOrthoTileRows x ortho_tile_cols(): stages [k0, k1) of 64 of K.  Where few
-// deep tiles would leave SM pairs idle, a tile's K is split: its parts share the slot of the
-// buffer for their sums, and the last one to finish adds them up.
+// deep tiles would leave SM pairs idle, a tile's K is split: its parts share a slot of counters,
+// their sums lie side by side, and the last one to finish adds them up.
 struct OrthoTile {
   int32_t mat, i0, j0, maps;        // matrix, first row and column, index of its tensor maps
   int32_t k0, k1;
   int32_t slot, part, parts;        // parts > 1: one of a split tile's
+  int32_t sum0;                     // the first of its parts' sums, in ortho_part_floats()
 };
 constexpr int kOrthoTileRows = 256, kOrthoMaxParts = 8;
 __host__ __device__ constexpr int ortho_tile_cols(bool pairs, bool narrow) {
   return (pairs ? 128 : 256) / (narrow ? 2 : 1);
 }
-// floats of one part of a slot, and its counters (one for each of 8 epilogue warps of two CTAs)
+// floats of one part's sums, and a slot's counters (one for each of 8 epilogue warps of two CTAs)
 __host__ __device__ constexpr int64_t ortho_part_floats(bool pairs, bool narrow) {
   return (int64_t)kOrthoTileRows * ortho_tile_cols(pairs, narrow);
 }

@@ -469,7 +469,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         // this warp's sums of every part lie together: 32 lanes apart for coalescing
         shared = true;
         constexpr int kOwn = 32 * 32 * kChunks;
-        float* mine = sums + ((int64_t)tl.slot * kOrthoMaxParts + tl.part) * ortho_part_floats(kPairs, kNarrow) +
+        float* mine = sums + (int64_t)(tl.sum0 + tl.part) * ortho_part_floats(kPairs, kNarrow) +
                       ((int)rank * kEpiWarps + warp - 2) * kOwn + lane;
 #pragma unroll
         for (int q = 0; q < kChunks; ++q) {
@@ -500,7 +500,7 @@ ortho_gemm_kernel(const OrthoMat* __restrict__ mats, const CUtensorMap* __restri
         uint8_t* const mirror = direct + kBoxBytes;
         if (phase == kOrthoGram && shared) {
           constexpr int kOwn = 32 * 32 * kChunks;
-          const float* from = sums + (int64_t)tl.slot * kOrthoMaxParts * ortho_part_floats(kPairs, kNarrow) +
+          const float* from = sums + (int64_t)tl.sum0 * ortho_part_floats(kPairs, kNarrow) +
                               ((int)rank * kEpiWarps + warp - 2) * kOwn + lane;
           float total[32];
 #pragma unroll
