@@ -437,9 +437,9 @@ ZO_API zo_status zo_layernorm_sync_status(void* stream);
  * Precision: sums are fp32.  Iterates are held as power-of-two-scaled fp16 pairs (~22
  *   significant bits).  Their products are of fp32 grade where W is fp32, where min(m, n) <= 128
  *   and where the matrix's grade asks for it; for larger bf16 matrices the products take single
- *   fp16 factors (11 bits) otherwise, and the result is up to 1.25 times as far from the
- *   definition as its rounding to bf16 alone puts it.  Their products take about a third of the
- *   time of the fp32 grade's.  A U with ||U||_F far below eps loses digits: the
+ *   fp16 factors (11 bits) otherwise, and the result is 1.1 to 1.5 times as far from the
+ *   definition as its rounding to bf16 alone puts it (the flatter its spectrum, the further).
+ *   Their products take about a third of the time of the fp32 grade's.  A U with ||U||_F far below eps loses digits: the
  *   scaled iterate resolves 2^-38.  A NaN or infinity in U_i gives NaN in all of W_i.
  * Captured into a graph, the calls may be replayed on other contents of G, M and W.
  */

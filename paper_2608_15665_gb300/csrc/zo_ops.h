@@ -109,8 +109,9 @@ struct OrthoUpdate {
 // fp32 results take products of fp32 grade.  So do bf16 results of at most 128 rows: their few
 // singular directions do not average rounding out (8 x 8: 4.1e-3 of the result's norm with
 // single factors, rounding the result 1.7e-3), and their time is latency, not products.  Larger
-// bf16 matrices take single factors (2.0e-3 to 2.1e-3, against 1.7e-3) unless their caller asks
-// for pairs (4096 x 4096: 2.81 ms instead of 0.96).
+// bf16 matrices take single factors (1.1 to 1.3 times the rounding's error for gradients, 1.2 to 1.5
+// times for Gaussian matrices, whose spectra are flat) unless their caller asks for pairs (4096 x
+// 4096: 2.81 ms instead of 0.96; 96 of 256 x 256 327 us instead of 196, eight 103 instead of 95).
 inline bool ortho_pairs(bool bf16, int64_t p) { return !bf16 || p <= 128; }
 
 // partial: one per unit; counter (zero before the first call) and inverse (a power of two, and
