@@ -45,7 +45,8 @@
  *   counter = (e / 4, matrix index, t or refresh index j, tag << 24 | query k),
  *   lane e % 4 for element e of a row-major buffer; u = ((x >> 8) + 1) * 2^-24;
  *   Box-Muller on lane pairs (0,1), (2,3): z_a = sqrt(-2 ln u_a) cos(2 pi u_b),
- *   z_b = sqrt(-2 ln u_a) sin(2 pi u_b).  Tags: 1 = Z, 2 = Omega_U, 3 = Omega_V.
+ *   z_b = sqrt(-2 ln u_a) sin(2 pi u_b).  Tags: 1 = Z, 2 = Omega_U, 3 = Omega_V,
+ *   5 = zo_mezo_perturb, 6 = zo_adamw_step.
  */
 #ifndef SUBZERO_GB300_ZO_H
 #define SUBZERO_GB300_ZO_H
@@ -472,6 +473,64 @@ ZO_API zo_status zo_muon_step(zo_muon_ctx* ctx, float momentum, int32_t nesterov
 ZO_API zo_status zo_muon_sync_status(zo_muon_ctx* ctx);
 /* zo_muon_launches -- number of kernels this context has launched since zo_muon_create. */
 ZO_API int64_t zo_muon_launches(const zo_muon_ctx* ctx);
+
+/*
+ * The AdamW step over many tensors at once, for what a model's tail has beside the matrices
+ * that zo_muon_step takes: norms' weights, biases, embeddings, the head.
+ *
+ *   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g^2
+ *   W <- rnd((1 - lr weight_decay) W - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps))
+ *
+ * zo_adamw_create -- bind the caller's tensors, each m x n (a vector: m = 1) of W and its
+ *   gradient G with any element alignment and row strides >= n, and its states.  The pointers
+ *   must stay valid until zo_adamw_destroy; the contents of G are read by each step.  A buffer
+ *   that a step writes may be given once.  Tensors may be empty.  workspace: caller-owned device
+ *   memory of at least zo_adamw_workspace(tensors, n_tensors, bits) bytes, 256-byte aligned, kept
+ *   until zo_adamw_destroy and used by this context alone; the tables are copied to it on
+ *   `stream` (void* cudaStream_t), on which every later call launches, and the call returns when
+ *   they are there.
+ * States, m n elements each in the order of W's rows without gaps, zero before the first step:
+ *   bits = 32: M and V hold m and v in fp32.
+ *   bits = 8:  M holds m, and V holds r = sqrt(v), as e4m3 codes (4 exponent bits of bias 7, 3
+ *     mantissa bits, 0x7F = NaN) of which each stands for itself times 2^(max(E, 40) - 134) with
+ *     the byte E of its block of 256 elements in Em (Ev), ceil(m n / 256) bytes each.  E is the
+ *     biased fp32 exponent of the block's largest finite |m| (r).  A step computes in fp32, as
+ *     above, and W takes the m and v from before their rounding.  That is up or down at random,
+ *     by 16 bits of the counter contract's integer stream an element (a mean that moves by a
+ *     thousandth a step would never leave a code if it went to the nearest): of the words of
+ *     Philox4x32-10(counter = (e / 8, index of the tensor, t, 6 << 24), key = seed), element e
+ *     takes the low (e even) or high half of word (e % 8) / 2, u, and becomes floor(x + u 2^-16)
+ *     with x in steps of the codes around it.  r > 0 keeps a code above 0.  Infinity becomes NaN.
+ * zo_adamw_step -- one step of every tensor: its number t >= 1 (count NULL), or t = 0 and a
+ *   device count that the step raises by one and goes by, so that a captured step may be
+ *   replayed.  The states' sums are formed from products that are each rounded to fp32.  A NaN
+ *   or infinity in G gives NaN in its own element of W and m, no others.
+ */
+typedef struct zo_adamw_tensor {
+  void* W;            /* device; m x n, row stride ldw elements, dtype below */
+  const void* G;      /* device; m x n, row stride ldg elements, grad_dtype below */
+  void* M;            /* device; m n states: fp32, or codes */
+  void* V;
+  uint8_t* Em;        /* device; ceil(m n / 256) exponents (bits = 8; else NULL) */
+  uint8_t* Ev;
+  int64_t m, n;
+  int64_t ldw, ldg;
+  int32_t dtype;      /* ZO_F32 or ZO_BF16 */
+  int32_t grad_dtype; /* ZO_F32 or ZO_BF16 */
+} zo_adamw_tensor;
+
+typedef struct zo_adamw_ctx zo_adamw_ctx;
+
+ZO_API int64_t zo_adamw_workspace(const zo_adamw_tensor* tensors, int32_t n_tensors, int32_t bits);
+ZO_API zo_status zo_adamw_create(zo_adamw_ctx** out, const zo_adamw_tensor* tensors,
+                                 int32_t n_tensors, int32_t bits, uint64_t seed, void* workspace,
+                                 int64_t workspace_bytes, void* stream);
+/* zo_adamw_destroy -- synchronise the stream and free the context.  NULL is a no-op. */
+ZO_API zo_status zo_adamw_destroy(zo_adamw_ctx* ctx);
+ZO_API zo_status zo_adamw_step(zo_adamw_ctx* ctx, int64_t t, int64_t* count, double lr,
+                               double beta1, double beta2, double eps, double weight_decay);
+/* zo_adamw_launches -- number of kernels this context has launched since zo_adamw_create. */
+ZO_API int64_t zo_adamw_launches(const zo_adamw_ctx* ctx);
 
 /* zo_status_string -- static description of a status code. */
 ZO_API const char* zo_status_string(int32_t status);

@@ -83,6 +83,23 @@ class zo_muon_matrix(ctypes.Structure):
     ]
 
 
+class zo_adamw_tensor(ctypes.Structure):
+    _fields_ = [
+        ("W", ctypes.c_void_p),
+        ("G", ctypes.c_void_p),
+        ("M", ctypes.c_void_p),
+        ("V", ctypes.c_void_p),
+        ("Em", ctypes.c_void_p),
+        ("Ev", ctypes.c_void_p),
+        ("m", ctypes.c_int64),
+        ("n", ctypes.c_int64),
+        ("ldw", ctypes.c_int64),
+        ("ldg", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+    ]
+
+
 _c = ctypes
 _SIGNATURES = {
     "zo_create": (_c.c_int32, [_c.POINTER(_c.c_void_p), _c.POINTER(zo_matrix), _c.c_int32,
@@ -137,6 +154,13 @@ _SIGNATURES = {
                                   _c.c_int32, _c.c_int32, _c.c_void_p, _c.c_float]),
     "zo_muon_sync_status": (_c.c_int32, [_c.c_void_p]),
     "zo_muon_launches": (_c.c_int64, [_c.c_void_p]),
+    "zo_adamw_workspace": (_c.c_int64, [_c.c_void_p, _c.c_int32, _c.c_int32]),
+    "zo_adamw_create": (_c.c_int32, [_c.POINTER(_c.c_void_p), _c.c_void_p, _c.c_int32, _c.c_int32,
+                                     _c.c_uint64, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "zo_adamw_destroy": (_c.c_int32, [_c.c_void_p]),
+    "zo_adamw_step": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_double, _c.c_double,
+                                   _c.c_double, _c.c_double, _c.c_double]),
+    "zo_adamw_launches": (_c.c_int64, [_c.c_void_p]),
     "zo_status_string": (_c.c_char_p, [_c.c_int32]),
     "zo_last_error": (_c.c_char_p, []),
 }
@@ -515,3 +539,76 @@ def zo_muon_sync_status(ctx):
 
 def zo_muon_launches(ctx):
     return int(LIB.zo_muon_launches(ctx))
+
+
+ADAMW_BLOCK = 256                    # elements of an 8-bit state with one exponent
+
+
+def make_adamw_tensor(W, G, M, V, Em=None, Ev=None):
+    """zo_adamw_tensor for torch tensors: W and G of one shape (bf16 or fp32), both contiguous or
+    matrices with unit column stride; M and V contiguous, one value an element: fp32, or bytes
+    (float8_e4m3fn or uint8) with their blocks' exponents Em and Ev (uint8)."""
+    import torch
+    at = "make_adamw_tensor"
+    if tuple(G.shape) != tuple(W.shape):
+        raise ZoError(ZO_ERR_SHAPE, at, f"G has shape {tuple(G.shape)}, expected {tuple(W.shape)}")
+    if G.device != W.device:
+        raise ZoError(ZO_ERR_INVALID_ARG, at, f"G is on {G.device}, expected {W.device}")
+    count = W.numel()
+    if W.is_contiguous() and G.is_contiguous():
+        m, n, pw, pg = 1, count, W.data_ptr(), G.data_ptr()
+        ldw = ldg = count
+    else:
+        pw, ldw = _rows(W, at, "W", None, None, None)
+        pg, ldg = _rows(G, at, "G", W.shape, None, None)
+        m, n = W.shape
+    if (Em is None) != (Ev is None):
+        raise ZoError(ZO_ERR_INVALID_ARG, at, "need both exponents, or none")
+    codes = (torch.float32,) if Em is None else (torch.float8_e4m3fn, torch.uint8)
+    for name, t, size, types in (("M", M, count, codes), ("V", V, count, codes),
+                                 ("Em", Em, -(-count // ADAMW_BLOCK), (torch.uint8,)),
+                                 ("Ev", Ev, -(-count // ADAMW_BLOCK), (torch.uint8,))):
+        if t is None and name in ("Em", "Ev"):
+            continue
+        if t.numel() != size or not t.is_contiguous():
+            raise ZoError(ZO_ERR_SHAPE, at, f"{name} must be contiguous, of {size} values")
+        if t.dtype not in types:
+            raise ZoError(ZO_ERR_DTYPE, at, f"{name} is {t.dtype}, expected {types[0]}")
+        if t.device != W.device:
+            raise ZoError(ZO_ERR_INVALID_ARG, at, f"{name} is on {t.device}, expected {W.device}")
+    _on_device(W, at)
+    return zo_adamw_tensor(pw, pg, _ptr(M), _ptr(V), _ptr(Em), _ptr(Ev), m, n, ldw, ldg,
+                           _dtype_code(W, at, "W"), _dtype_code(G, at, "G"))
+
+
+def zo_adamw_workspace(tensors, bits):
+    """Bytes of device workspace for a context over `tensors`."""
+    arr = (zo_adamw_tensor * len(tensors))(*tensors)
+    n = int(LIB.zo_adamw_workspace(arr, len(tensors), int(bits)))
+    if n <= 0:
+        raise ZoError(ZO_ERR_INVALID_ARG, "zo_adamw_workspace", zo_last_error())
+    return n
+
+
+def zo_adamw_create(tensors, bits, seed, workspace, stream=None):
+    arr = (zo_adamw_tensor * len(tensors))(*tensors)
+    ctx = ctypes.c_void_p()
+    _check(LIB.zo_adamw_create(ctypes.byref(ctx), arr, len(tensors), int(bits),
+                               int(seed) & (2**64 - 1), _ptr(workspace),
+                               workspace.numel() * workspace.element_size(),
+                               _stream_handle(stream)), "zo_adamw_create")
+    return ctx
+
+
+def zo_adamw_destroy(ctx):
+    _check(LIB.zo_adamw_destroy(ctx), "zo_adamw_destroy")
+
+
+def zo_adamw_step(ctx, t, count, lr, beta1, beta2, eps, weight_decay):
+    """count: None, or a one-element int64 tensor on the context's device (then t is 0)."""
+    _check(LIB.zo_adamw_step(ctx, int(t), _ptr(count), float(lr), float(beta1), float(beta2),
+                             float(eps), float(weight_decay)), "zo_adamw_step")
+
+
+def zo_adamw_launches(ctx):
+    return int(LIB.zo_adamw_launches(ctx))

@@ -1,0 +1,576 @@
+// The AdamW step over many tensors at once: host runtime, C ABI (declared in include/zo.h) and
+// the kernel, one launch for all tensors (two where the device counts the steps).
+//
+//   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g^2
+//   W <- rnd((1 - lr wd) W - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps))
+//
+// Bound by HBM: W is read and written, g read, the states read and written, once each.  A warp
+// works on blocks of 256 neighbouring elements, eight to a lane; a CTA on kChunk elements of one
+// tensor, found in a table of the chunks, its loads in flight together.
+//
+// States in 8 bits: m and r = sqrt(v) as e4m3 codes times 2^(E - 134), E = the biased fp32
+// exponent of the largest |m| (r) of the block of 256, in one byte; so the block's largest is in
+// [128, 256], and values down to 2^-17 of it keep a code.  r and not v: the codes reach over 17
+// binades, v's spread is twice that of r.  Codes are rounded up or down at random, by 16 bits of
+// the Philox stream an element, as v moves by a thousandth of itself a step and the codes are an
+// eighth apart: to nearest, a running mean would never move.  The expectation is the running
+// mean's; its noise is (1 - b2) / 2 x 1/8 of r^2 a step in variance, ~9% of r where the gradients'
+// squares vary by about their mean.  m and r take the same bits: the two errors are not used
+// together.  A root above zero keeps a code above zero, or m / eps would be taken as the update.
+// The moments' sums are products and sums each rounded on its own: the exponents are then the
+// same as those of any other fp32 evaluation in this order.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <new>
+#include <type_traits>
+#include <unordered_set>
+#include <vector>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "../../include/zo.h"
+#include "zo_device.cuh"
+#include "zo_host.h"
+#include "zo_launch.cuh"
+
+namespace {
+
+using namespace zo::host;
+
+constexpr uint32_t kTagAdamW = 6;
+constexpr int kThreads = 256, kLane = 8;
+constexpr int kBlock = 32 * kLane;               // elements of a power of two
+constexpr int kUnits = 2;                        // blocks a warp holds at once
+constexpr int kChunk = kThreads * kLane * kUnits;
+static_assert(kBlock == 256 && kChunk % kBlock == 0, "a chunk is whole blocks");
+
+struct Tensor {
+  void* W;
+  const void* G;
+  void *M, *V;                                   // fp32, or codes
+  uint8_t *Em, *Ev;                              // exponents (8 bits)
+  int64_t n, cols, ldw, ldg;                     // elements; of a row, and the rows' strides
+  int32_t kind;                                  // bit 0: W is bf16; bit 1: G is bf16
+  int32_t wide;                                  // contiguous, and aligned to a lane's accesses
+};
+
+// What a step is made of; c1 and c2 are 1 - b1^t and 1 - b2^t.
+struct Step {
+  float b1, one_b1, b2, one_b2, keep, lr, eps;
+  float c1, c2;
+  uint32_t t;
+  uint32_t key0, key1;
+};
+struct Counted {                                 // c1, c2 and t where the device counts
+  float c1, c2;
+  uint32_t t;
+};
+
+// One more step: its number and bias corrections.
+__global__ void adamw_count_kernel(int64_t* count, double b1, double b2, Counted* out) {
+  zo::pdl_wait();
+  int64_t t = *count;
+  t = t < 0 ? 1 : t + 1;
+  *count = t;
+  *out = Counted{(float)-expm1((double)t * log(b1)), (float)-expm1((double)t * log(b2)),
+                 (uint32_t)t};
+}
+
+template <typename T>
+__device__ __forceinline__ float to_float(T x) { return static_cast<float>(x); }
+
+// Eight values of a lane as they lie in memory.
+template <typename T>
+struct Raw {
+  static constexpr int kWords = 2 * (int)sizeof(T);
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (sizeof(T) == 1) {
+      const uint2 a = __ldcs(reinterpret_cast<const uint2*>(p));
+      w[0] = a.x;
+      w[1] = a.y;
+    } else {
+#pragma unroll
+      for (int q = 0; q < kWords; q += 4) {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p) + q / 4);
+        w[q] = a.x;
+        w[q + 1] = a.y;
+        w[q + 2] = a.z;
+        w[q + 3] = a.w;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (sizeof(T) == 1) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < kWords; q += 4)
+        reinterpret_cast<uint4*>(p)[q / 4] = make_uint4(w[q], w[q + 1], w[q + 2], w[q + 3]);
+    }
+  }
+  // element by element, `n` of them from place e0 on, in rows of `cols` elements `ld` apart
+  __device__ __forceinline__ void gather(const T* p, int64_t e0, int n, int64_t cols, int64_t ld) {
+#pragma unroll
+    for (int q = 0; q < kWords; ++q) w[q] = 0u;
+    if (n == 0) return;
+    int64_t row = cols == ld ? 0 : e0 / cols, col = e0 - row * cols;
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) {
+      if (e < n) {
+        const T x = p[row * ld + col];
+        uint32_t bits;
+        if constexpr (sizeof(T) == 4) bits = __float_as_uint(x);
+        else if constexpr (sizeof(T) == 2) bits = __bfloat16_as_ushort(x);
+        else bits = x;
+        w[e / kPer] |= bits << (kBits * (e % kPer));
+      }
+      step(row, col, cols, ld);
+    }
+  }
+  __device__ __forceinline__ void scatter(T* p, int64_t e0, int n, int64_t cols, int64_t ld) const {
+    if (n == 0) return;
+    int64_t row = cols == ld ? 0 : e0 / cols, col = e0 - row * cols;
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) {
+      if (e < n) {
+        const uint32_t bits = w[e / kPer] >> (kBits * (e % kPer));
+        if constexpr (sizeof(T) == 4) p[row * ld + col] = __uint_as_float(bits);
+        else if constexpr (sizeof(T) == 2)
+          p[row * ld + col] = __ushort_as_bfloat16((unsigned short)bits);
+        else p[row * ld + col] = (T)bits;
+      }
+      step(row, col, cols, ld);
+    }
+  }
+
+ private:
+  static constexpr int kBits = 8 * (int)sizeof(T), kPer = 32 / kBits;
+  static __device__ __forceinline__ void step(int64_t& row, int64_t& col, int64_t cols, int64_t ld) {
+    if (++col == cols && cols != ld) {
+      col = 0;
+      ++row;
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw<T>& r, float (&x)[kLane]) {
+#pragma unroll
+  for (int e = 0; e < kLane; ++e) {
+    if constexpr (sizeof(T) == 4) x[e] = __uint_as_float(r.w[e]);
+    else x[e] = __uint_as_float(e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void pack(const float (&x)[kLane], Raw<T>& r) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) r.w[e] = __float_as_uint(x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kLane; e += 2) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[e], x[e + 1]);
+      r.w[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+}
+
+// ---- 8-bit states ------------------------------------------------------------------------
+__device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
+
+// Eight e4m3 codes times 2^(E - 134).
+__device__ __forceinline__ void decode(const Raw<uint8_t>& r, uint32_t E, float (&x)[kLane]) {
+  const float s = power((int)max(E, 40u) - 134);
+#pragma unroll
+  for (int q = 0; q < kLane / 2; ++q) {
+    const __half2 h = __nv_cvt_fp8x2_to_halfraw2(
+        (__nv_fp8x2_storage_t)(r.w[q / 2] >> (16 * (q & 1))), __NV_E4M3);
+    const float2 f = __half22float2(h);
+    x[2 * q] = f.x * s;
+    x[2 * q + 1] = f.y * s;
+  }
+}
+
+// Codes of nonnegative (kSigned: any) x of a block whose largest has the biased exponent E.
+// x 2^(134 - E) 2^-120 is laid out like the code: its exponent field, and its subnormal numbers,
+// begin where e4m3's do.  So the code is the fp32 bits without the last 20, rounded up where
+// these and the random bits carry.  Infinity and NaN become NaN.  (Two products: one power of two
+// of both may leave fp32's range.  The second rounds subnormals at 2^-20 of a code's step.)
+template <bool kSigned>
+__device__ __forceinline__ void encode(const float (&x)[kLane], uint32_t E, const uint4& random,
+                                       Raw<uint8_t>& r) {
+  const float s = power(134 - (int)max(E, 40u));
+  const uint32_t rw[4] = {random.x, random.y, random.z, random.w};
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = 4 * q + i;
+      const uint32_t add = e & 1 ? (rw[e / 2] >> 12) & 0xFFFF0u : (rw[e / 2] << 4) & 0xFFFF0u;
+      const uint32_t bits = __float_as_uint((kSigned ? fabsf(x[e]) : x[e]) * s * 0x1p-120f);
+      uint32_t code = min((bits + add) >> 20, 0x7Fu);
+      if constexpr (kSigned) code |= (__float_as_uint(x[e]) >> 24) & 0x80u;
+      else code = max(code, min(__float_as_uint(x[e]), 1u));
+      word |= code << (8 * i);
+    }
+    r.w[q] = word;
+  }
+}
+
+// The largest finite |x| of the warp's block, as bits.
+__device__ __forceinline__ uint32_t largest(const float (&x)[kLane]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < kLane; ++e) top = max(top, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (top >= 0x7F800000u) {
+    top = 0;
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) {
+      const uint32_t b = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+      if (b < 0x7F800000u) top = max(top, b);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+  }
+  return top;
+}
+
+__device__ __forceinline__ float root_of(float v) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// A lane's eight elements, from e0 on, of which the first `count` are the tensor's.
+template <bool kEight, typename W, typename G>
+struct Unit {
+  using S = std::conditional_t<kEight, uint8_t, float>;
+  Raw<W> w;
+  Raw<G> g;
+  Raw<S> m, v;
+  uint32_t em, ev;
+  int64_t e0;
+  int count;
+
+  __device__ __forceinline__ void load(const Tensor& t, int64_t first) {
+    e0 = first;
+    count = (int)max((int64_t)0, min((int64_t)kLane, t.n - e0));
+    const W* pw = static_cast<const W*>(t.W);
+    const G* pg = static_cast<const G*>(t.G);
+    const S *pm = static_cast<const S*>(t.M), *pv = static_cast<const S*>(t.V);
+    if (t.wide && count == kLane) {
+      w.load(pw + e0);
+      g.load(pg + e0);
+      m.load(pm + e0);
+      v.load(pv + e0);
+    } else {
+      w.gather(pw, e0, count, t.cols, t.ldw);
+      g.gather(pg, e0, count, t.cols, t.ldg);
+      m.gather(pm, e0, count, t.cols, t.cols);
+      v.gather(pv, e0, count, t.cols, t.cols);
+    }
+    if constexpr (kEight) {
+      const bool any = __shfl_sync(0xffffffffu, count, 0) > 0;
+      em = any ? t.Em[e0 / kBlock] : 0u;
+      ev = any ? t.Ev[e0 / kBlock] : 0u;
+    }
+  }
+
+  __device__ __forceinline__ void finish(const Tensor& t, uint32_t index, const Step& st) {
+    float x[kLane], y[kLane], a[kLane], b[kLane];
+    unpack(g, y);
+    if constexpr (kEight) {
+      decode(m, em, a);
+      decode(v, ev, b);
+    } else {
+      unpack(m, a);
+      unpack(v, b);
+    }
+    const float rate = st.lr / st.c1, spread = rsqrtf(st.c2);
+    unpack(w, x);
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) {
+      const float gg = __fmul_rn(y[e], y[e]);
+      if constexpr (kEight) b[e] = __fmul_rn(b[e], b[e]);
+      a[e] = __fadd_rn(__fmul_rn(st.b1, a[e]), __fmul_rn(st.one_b1, y[e]));
+      b[e] = __fadd_rn(__fmul_rn(st.b2, b[e]), __fmul_rn(st.one_b2, gg));
+      y[e] = root_of(b[e]);
+      x[e] = fmaf(st.keep, x[e], -__fdividef(rate * a[e], fmaf(y[e], spread, st.eps)));
+    }
+    pack(x, w);
+    if constexpr (kEight) {
+      const uint32_t first = __shfl_sync(0xffffffffu, (uint32_t)(count > 0), 0);
+      const uint32_t tm = largest(a), tv = largest(b);
+      // 2^k <= r < 2^(k + 1) where 2^2k <= v < 2^(2k + 2)
+      em = tm >> 23;
+      ev = tv >> 23 ? (uint32_t)((((int)(tv >> 23) - 127) >> 1) + 127) : 0u;
+      const uint4 random = zo::philox4x32_10(
+          make_uint4((uint32_t)(e0 / kLane), index, st.t, kTagAdamW << 24), st.key0, st.key1);
+      encode<true>(a, em, random, m);
+      encode<false>(y, ev, random, v);
+      if (first && (threadIdx.x & 31) == 0) {
+        t.Em[e0 / kBlock] = (uint8_t)em;
+        t.Ev[e0 / kBlock] = (uint8_t)ev;
+      }
+    } else {
+      pack(a, m);
+      pack(b, v);
+    }
+    W* pw = static_cast<W*>(t.W);
+    S *pm = static_cast<S*>(t.M), *pv = static_cast<S*>(t.V);
+    if (t.wide && count == kLane) {
+      w.store(pw + e0);
+      m.store(pm + e0);
+      v.store(pv + e0);
+    } else {
+      w.scatter(pw, e0, count, t.cols, t.ldw);
+      m.scatter(pm, e0, count, t.cols, t.cols);
+      v.scatter(pv, e0, count, t.cols, t.cols);
+    }
+  }
+};
+
+template <bool kEight, typename W, typename G>
+__device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, uint32_t index,
+                                          const Step& st) {
+  Unit<kEight, W, G> u[kUnits];
+  const int64_t e0 = first + (int64_t)threadIdx.x * kLane;
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) u[k].load(t, e0 + (int64_t)k * kThreads * kLane);
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) u[k].finish(t, index, st);
+}
+
+// chunks: (tensor, number of the chunk in it)
+template <bool kEight>
+__global__ void __launch_bounds__(kThreads)
+adamw_kernel(const Tensor* __restrict__ tensors, const int2* __restrict__ chunks, Step st,
+             const Counted* __restrict__ counted) {
+  const int2 at = chunks[blockIdx.x];
+  const Tensor t = tensors[at.x];
+  zo::pdl_wait();
+  zo::pdl_trigger();
+  if (counted) {
+    const Counted c = *counted;
+    st.c1 = c.c1;
+    st.c2 = c.c2;
+    st.t = c.t;
+  }
+  const int64_t first = (int64_t)at.y * kChunk;
+  using B = __nv_bfloat16;
+  switch (t.kind) {
+    case 0: run_chunk<kEight, float, float>(t, first, (uint32_t)at.x, st); break;
+    case 1: run_chunk<kEight, B, float>(t, first, (uint32_t)at.x, st); break;
+    case 2: run_chunk<kEight, float, B>(t, first, (uint32_t)at.x, st); break;
+    default: run_chunk<kEight, B, B>(t, first, (uint32_t)at.x, st); break;
+  }
+}
+
+// ---- host ----------------------------------------------------------------------------------
+
+zo_status check_tensor(const zo_adamw_tensor& t, int32_t bits) {
+  if ((t.dtype != ZO_F32 && t.dtype != ZO_BF16) || (t.grad_dtype != ZO_F32 && t.grad_dtype != ZO_BF16))
+    return refuse(ZO_ERR_DTYPE, "unknown dtype in zo_adamw_tensor");
+  if (t.m < 0 || t.n < 0 || t.m >= (int64_t(1) << 34) || t.n >= (int64_t(1) << 34) ||
+      (t.n > 0 && t.m > (int64_t(1) << 34) / t.n) || t.ldw < t.n || t.ldg < t.n ||
+      t.ldw >= (int64_t(1) << 40) || t.ldg >= (int64_t(1) << 40))
+    return refuse(ZO_ERR_SHAPE, "zo_adamw_tensor: need 0 <= m, n; m n <= 2^34; n <= ldw, ldg < 2^40");
+  if (t.m * t.n == 0) return ZO_OK;
+  if (!t.W || !t.G || !t.M || !t.V || (bits == 8 && (!t.Em || !t.Ev)))
+    return refuse(ZO_ERR_INVALID_ARG, "null W, G, M or V (with 8 bits: Em or Ev) in zo_adamw_tensor");
+  const auto aligned = [](const void* p, int bytes) {
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0;
+  };
+  if (!aligned(t.W, t.dtype == ZO_BF16 ? 2 : 4) || !aligned(t.G, t.grad_dtype == ZO_BF16 ? 2 : 4) ||
+      (bits == 32 && (!aligned(t.M, 4) || !aligned(t.V, 4))))
+    return refuse(ZO_ERR_ALIGN, "zo_adamw_tensor: a buffer is not aligned to its elements");
+  return ZO_OK;
+}
+
+zo_status check_tensors(const zo_adamw_tensor* ts, int32_t n, int32_t bits) {
+  if (!ts || n <= 0) return refuse(ZO_ERR_INVALID_ARG, "zo_adamw: need at least one tensor");
+  if (bits != 8 && bits != 32)
+    return refuse(ZO_ERR_UNSUPPORTED, "zo_adamw: states are held in 8 or in 32 bits");
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const zo_status st = check_tensor(ts[i], bits);
+    if (st != ZO_OK) return st;
+    chunks += (ts[i].m * ts[i].n + kChunk - 1) / kChunk;
+  }
+  if (chunks > INT_MAX) return refuse(ZO_ERR_SHAPE, "zo_adamw: too many elements for one context");
+  return ZO_OK;
+}
+
+// Whatever a step writes is written by one tensor alone.
+zo_status check_distinct(const zo_adamw_tensor* ts, int32_t n, int32_t bits) {
+  std::unordered_set<const void*> seen;
+  for (int32_t i = 0; i < n; ++i) {
+    if (ts[i].m * ts[i].n == 0) continue;
+    const void* own[5] = {ts[i].W, ts[i].M, ts[i].V, ts[i].Em, ts[i].Ev};
+    for (int k = 0; k < (bits == 8 ? 5 : 3); ++k)
+      if (!seen.insert(own[k]).second)
+        return refuse(ZO_ERR_INVALID_ARG, "zo_adamw_create: a buffer that a step writes is given twice");
+  }
+  return ZO_OK;
+}
+
+struct Layout {
+  int64_t tensors_at = 0, chunks_at = 0, bytes = 0, chunks = 0;
+};
+int64_t round_up(int64_t v) { return (v + 255) / 256 * 256; }
+Layout layout(const zo_adamw_tensor* ts, int32_t n) {
+  Layout L;
+  for (int32_t i = 0; i < n; ++i) L.chunks += (ts[i].m * ts[i].n + kChunk - 1) / kChunk;
+  L.tensors_at = 256;                                      // Counted
+  L.chunks_at = round_up(L.tensors_at + (int64_t)sizeof(Tensor) * n);
+  L.bytes = round_up(L.chunks_at + (int64_t)sizeof(int2) * L.chunks);
+  return L;
+}
+
+}  // namespace
+
+struct zo_adamw_ctx {
+  int device = 0;
+  cudaStream_t stream = nullptr;
+  Layout plan;
+  uint8_t* ws = nullptr;
+  int32_t bits = 32;
+  uint64_t seed = 0;
+  int64_t launches = 0;
+};
+
+extern "C" {
+
+int64_t zo_adamw_workspace(const zo_adamw_tensor* tensors, int32_t n_tensors, int32_t bits) {
+  return check_tensors(tensors, n_tensors, bits) == ZO_OK ? layout(tensors, n_tensors).bytes : 0;
+}
+
+zo_status zo_adamw_create(zo_adamw_ctx** out, const zo_adamw_tensor* tensors, int32_t n_tensors,
+                          int32_t bits, uint64_t seed, void* workspace, int64_t workspace_bytes,
+                          void* stream) {
+  if (!out) return ZO_ERR_INVALID_ARG;
+  *out = nullptr;
+  try {
+    zo_status st = check_tensors(tensors, n_tensors, bits);
+    if (st == ZO_OK) st = check_distinct(tensors, n_tensors, bits);
+    if (st != ZO_OK) return st;
+    const Layout L = layout(tensors, n_tensors);
+    if (!workspace || workspace_bytes < L.bytes)
+      return refuse(ZO_ERR_INVALID_ARG,
+                    "zo_adamw_create: the workspace is missing or smaller than zo_adamw_workspace");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+      return refuse(ZO_ERR_ALIGN, "zo_adamw_create: the workspace must be 256-byte aligned");
+    int dev = 0, major = 0, minor = 0;
+    ZO_CUDA(cudaGetDevice(&dev), "cudaGetDevice");
+    ZO_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev), "device");
+    ZO_CUDA(cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev), "device");
+    if (major != 10 || minor != 3)
+      return refuse(ZO_ERR_CUDA, "this library is built for sm_103a (GB300) only");
+    std::unique_ptr<zo_adamw_ctx> c(new zo_adamw_ctx());
+    c->device = dev;
+    c->stream = reinterpret_cast<cudaStream_t>(stream);
+    c->plan = L;
+    c->ws = static_cast<uint8_t*>(workspace);
+    c->bits = bits;
+    c->seed = seed;
+    std::vector<uint8_t> image((size_t)L.bytes, 0);
+    auto* ts = reinterpret_cast<Tensor*>(image.data() + L.tensors_at);
+    auto* chunks = reinterpret_cast<int2*>(image.data() + L.chunks_at);
+    for (int32_t i = 0; i < n_tensors; ++i) {
+      const zo_adamw_tensor& s = tensors[i];
+      Tensor& d = ts[i];
+      d.W = s.W;
+      d.G = s.G;
+      d.M = s.M;
+      d.V = s.V;
+      d.Em = s.Em;
+      d.Ev = s.Ev;
+      d.n = s.m * s.n;
+      // one row is contiguous, and so are rows without a gap
+      const bool flat_w = s.m <= 1 || s.ldw == s.n, flat_g = s.m <= 1 || s.ldg == s.n;
+      d.cols = flat_w && flat_g ? d.n : s.n;
+      d.ldw = flat_w ? d.cols : s.ldw;
+      d.ldg = flat_g ? d.cols : s.ldg;
+      d.kind = (s.dtype == ZO_BF16 ? 1 : 0) | (s.grad_dtype == ZO_BF16 ? 2 : 0);
+      const auto to16 = [](const void* p) { return aligned16(p); };
+      const auto to8 = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 8 == 0; };
+      d.wide = flat_w && flat_g && to16(s.W) && to16(s.G) &&
+               (bits == 8 ? to8(s.M) && to8(s.V) : to16(s.M) && to16(s.V));
+      for (int64_t k = 0; k * kChunk < d.n; ++k) *chunks++ = make_int2(i, (int)k);
+    }
+    ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),
+            "upload tables");
+    // (a copy from pageable memory may be asynchronous where the GPU reads the host's page tables)
+    ZO_CUDA(cudaStreamSynchronize(c->stream), "stream synchronize");
+    *out = c.release();
+    return ZO_OK;
+  } catch (const std::bad_alloc&) {
+    return refuse(ZO_ERR_NOMEM, "zo_adamw_create: out of host memory");
+  }
+}
+
+zo_status zo_adamw_destroy(zo_adamw_ctx* c) {
+  if (!c) return ZO_OK;
+  DeviceGuard guard(c->device);
+  const cudaError_t e = cudaStreamSynchronize(c->stream);
+  delete c;
+  if (e != cudaSuccess) return cuda_fail(e, "zo_adamw_destroy");
+  return ZO_OK;
+}
+
+zo_status zo_adamw_step(zo_adamw_ctx* c, int64_t t, int64_t* count, double lr, double beta1,
+                        double beta2, double eps, double weight_decay) {
+  if (!c) return ZO_ERR_INVALID_ARG;
+  if ((count == nullptr) != (t >= 1) || t < 0)
+    return refuse(ZO_ERR_INVALID_ARG, "zo_adamw_step: need t >= 1, or t = 0 and a count");
+  if (reinterpret_cast<uintptr_t>(count) % 8 != 0)
+    return refuse(ZO_ERR_ALIGN, "zo_adamw_step: the count is not aligned to its type");
+  // (past half a million steps 1 - 0.99999^t is 1 - 0.0067; its logarithm is what is held)
+  if (!std::isfinite(lr) || !std::isfinite(weight_decay) || !(eps >= 0.0) || !std::isfinite(eps) ||
+      !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
+    return refuse(ZO_ERR_INVALID_ARG,
+                  "zo_adamw_step: need finite scalars, eps >= 0 and betas in [0, 1)");
+  if (c->plan.chunks == 0 && !count) return ZO_OK;
+  DeviceGuard guard(c->device);
+  Step st{};
+  st.b1 = (float)beta1;
+  st.one_b1 = (float)(1.0 - beta1);
+  st.b2 = (float)beta2;
+  st.one_b2 = (float)(1.0 - beta2);
+  st.keep = (float)(1.0 - lr * weight_decay);
+  st.lr = (float)lr;
+  st.eps = (float)eps;
+  st.key0 = (uint32_t)c->seed;
+  st.key1 = (uint32_t)(c->seed >> 32);
+  auto* counted = reinterpret_cast<Counted*>(c->ws);
+  if (count) {
+    ZO_CUDA(zo::launch_dependent(adamw_count_kernel, 1u, 1, 0, c->stream, 1, true, count, beta1,
+                                 beta2, counted),
+            "AdamW count kernel");
+    ++c->launches;
+  } else {
+    st.c1 = (float)-std::expm1((double)t * std::log(beta1));
+    st.c2 = (float)-std::expm1((double)t * std::log(beta2));
+    st.t = (uint32_t)t;
+  }
+  if (c->plan.chunks == 0) return ZO_OK;
+  const auto* ts = reinterpret_cast<const Tensor*>(c->ws + c->plan.tensors_at);
+  const auto* chunks = reinterpret_cast<const int2*>(c->ws + c->plan.chunks_at);
+  ZO_CUDA(zo::launch_dependent(c->bits == 8 ? adamw_kernel<true> : adamw_kernel<false>,
+                               (unsigned)c->plan.chunks, kThreads, 0, c->stream, 1, true, ts,
+                               chunks, st, count ? counted : nullptr),
+          "AdamW kernel");
+  ++c->launches;
+  return ZO_OK;
+}
+
+int64_t zo_adamw_launches(const zo_adamw_ctx* c) { return c ? c->launches : 0; }
+
+}  // extern "C"

@@ -8,7 +8,8 @@ caller's tensors and launches them in the order of PyTorch's current stream:
 * ``layer_norm`` / ``layer_norm_backward`` -- the norm's forward and backward pass, and
   ``LayerNorm``, the two as one ``torch.autograd.Function``; ``layer_norm_sync`` asks
   whether all of them went well;
-* ``Orthogonalizer`` / ``Muon`` -- handles over matrices, bound to one stream.
+* ``Orthogonalizer`` / ``Muon`` / ``AdamW`` -- handles over matrices (tensors of any shape for
+  AdamW, whose states take 32 or 8 bits), bound to one stream.
 
 No arithmetic happens here.
 """
@@ -178,15 +179,55 @@ ADJUST = {"none": zb.ZO_MUON_ADJUST_NONE, "aspect": zb.ZO_MUON_ADJUST_ASPECT,
           "rms": zb.ZO_MUON_ADJUST_RMS}
 
 
-class _MuonContext:
-    """A context over matrices and its workspace, on the stream that is PyTorch's current one
+class _Handle:
+    """A context of the library and its workspace, on the stream that is PyTorch's current one
     when it is made (or `stream`).  A call under another current stream runs on the context's
     own all the same, after what that stream holds so far, and that stream goes on after it.
     (In a graph's capture too, where the context's own is not the legacy default stream, which
     CUDA keeps out of captures.)"""
 
+    ctx = None
+
+    def _open(self, dev, stream, workspace_bytes, create):
+        """Allocates workspace_bytes() and binds create(workspace, stream) on device `dev`."""
+        with torch.cuda.device(dev):
+            current = torch.cuda.current_stream()
+            self.stream = current if stream is None else stream
+            if self.stream != current:      # what was filled for this context until now
+                self.stream.wait_stream(current)
+            with torch.cuda.stream(self.stream):
+                self.workspace = torch.empty(workspace_bytes(), dtype=torch.uint8, device=dev)
+            self.ctx = create(self.workspace, self.stream)
+        self.device = dev
+
+    def _call(self, fn, *args):
+        if _raw_stream(self.device.index) == self.stream.cuda_stream:
+            fn(self.ctx, *args)
+            return
+        current = torch.cuda.current_stream(self.device)
+        self.stream.wait_stream(current)
+        fn(self.ctx, *args)
+        current.wait_stream(self.stream)
+
+    def _destroy(self, ctx):
+        raise NotImplementedError
+
+    def close(self):
+        if self.ctx is not None:
+            self._destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class _MuonContext(_Handle):
+    """A handle over matrices."""
+
     def __init__(self, weights, grads, momenta, stream, precise):
-        self.ctx = None
         at = type(self).__name__
         if not weights:
             raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, "need at least one matrix")
@@ -199,39 +240,14 @@ class _MuonContext:
         if precise:
             for mat in mats:
                 mat.grade = zb.ZO_MUON_GRADE_F32
-        with torch.cuda.device(dev):
-            current = torch.cuda.current_stream()
-            self.stream = current if stream is None else stream
-            if self.stream != current:      # what was filled for this context until now
-                self.stream.wait_stream(current)
-            with torch.cuda.stream(self.stream):
-                self.workspace = torch.empty(zb.zo_muon_workspace(mats), dtype=torch.uint8,
-                                             device=dev)
-            self.ctx = zb.zo_muon_create(mats, self.workspace, self.stream)
-        self.device = dev
+        self._open(dev, stream, lambda: zb.zo_muon_workspace(mats),
+                   lambda workspace, on: zb.zo_muon_create(mats, workspace, on))
 
-    def _call(self, fn, *args):
-        if _raw_stream(self.device.index) == self.stream.cuda_stream:
-            fn(self.ctx, *args)
-            return
-        current = torch.cuda.current_stream(self.device)
-        self.stream.wait_stream(current)
-        fn(self.ctx, *args)
-        current.wait_stream(self.stream)
+    def _destroy(self, ctx):
+        zb.zo_muon_destroy(ctx)
 
     def sync(self):
         zb.zo_muon_sync_status(self.ctx)
-
-    def close(self):
-        if self.ctx is not None:
-            zb.zo_muon_destroy(self.ctx)
-            self.ctx = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
 
 
 class Orthogonalizer(_MuonContext):
@@ -271,3 +287,77 @@ class Muon(_MuonContext):
              coeffs=None, eps=1e-7):
         self._call(zb.zo_muon_step, momentum, nesterov, lr, weight_decay, ADJUST[adjust], steps,
                    coeffs, eps)
+
+
+class AdamWState(NamedTuple):
+    """States of one tensor, an element each in the order of its rows: m and v in fp32, or m and
+    sqrt(v) as float8_e4m3fn values of which each stands for itself times 2^(max(E, 40) - 134)
+    with the exponent E of its 256 elements in m_exp and v_exp (uint8)."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_exp: Optional[torch.Tensor] = None
+    v_exp: Optional[torch.Tensor] = None
+
+
+def adamw_state(weight, bits=32):
+    """The states of a tensor before its first step: zero."""
+    n, dev = weight.numel(), weight.device
+    if bits == 32:
+        return AdamWState(torch.zeros(n, device=dev), torch.zeros(n, device=dev))
+    m, v = (torch.zeros(n, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+            for _ in range(2))
+    return AdamWState(m, v, *(torch.zeros(-(-n // zb.ADAMW_BLOCK), dtype=torch.uint8, device=dev)
+                              for _ in range(2)))
+
+
+class AdamW(_Handle):
+    """The AdamW optimiser over a list of tensors (bf16 or fp32, on one CUDA device) whose
+    gradients live in ``grads`` (allocated beside the weights, zero, if not given) and whose
+    states, in 32 or 8 bits, in ``states``.  ``seed``: of the 8-bit states' random rounding.
+    ``steps``: the number of steps taken, kept on the host; a step is told its number by it.
+    ``count``: a one-element int64 tensor on the device, which takes its place: then a step that
+    was captured into a graph may be replayed."""
+
+    def __init__(self, weights, grads=None, states=None, bits=32, seed=0, count=None, stream=None):
+        at = "AdamW"
+        self.weights = list(weights)
+        if not self.weights:
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, "need at least one tensor")
+        if bits not in (8, 32):
+            raise zb.ZoError(zb.ZO_ERR_UNSUPPORTED, at, "states are held in 8 or in 32 bits")
+        dev = self.weights[0].device
+        if any(W.device != dev for W in self.weights) or getattr(stream, "device", dev) != dev:
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at,
+                             "the tensors and the stream have to be on one CUDA device")
+        if count is not None and (count.dtype != torch.int64 or count.numel() != 1
+                                  or count.device != dev):
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at,
+                             "count must be one int64 value beside the tensors")
+        self.grads = ([torch.zeros(W.shape, dtype=W.dtype, device=W.device) for W in self.weights]
+                      if grads is None else list(grads))
+        self.states = ([adamw_state(W, bits) for W in self.weights] if states is None
+                       else list(states))
+        if not len(self.weights) == len(self.grads) == len(self.states):
+            raise ValueError("as many gradients and states as weights are needed")
+        if any((s.m_exp is None) != (bits == 32) for s in self.states):
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, "states have exponents exactly with 8 bits")
+        self.bits, self.count, self.steps = bits, count, 0
+        tensors = [zb.make_adamw_tensor(W, G, *s)
+                   for W, G, s in zip(self.weights, self.grads, self.states)]
+        self._open(dev, stream, lambda: zb.zo_adamw_workspace(tensors, bits),
+                   lambda workspace, on: zb.zo_adamw_create(tensors, bits, seed, workspace, on))
+
+    def _destroy(self, ctx):
+        zb.zo_adamw_destroy(ctx)
+
+    def step(self, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, t=None):
+        """One step.  t: its number, where it is not to be the one after the last."""
+        if self.count is not None:
+            if t is not None:
+                raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, "AdamW.step",
+                                 "the count on the device gives the step its number")
+            self._call(zb.zo_adamw_step, 0, self.count, lr, betas[0], betas[1], eps, weight_decay)
+            return
+        t = self.steps + 1 if t is None else int(t)
+        self._call(zb.zo_adamw_step, t, None, lr, betas[0], betas[1], eps, weight_decay)
+        self.steps = t
