@@ -532,6 +532,53 @@ ZO_API zo_status zo_adamw_step(zo_adamw_ctx* ctx, int64_t t, int64_t* count, dou
 /* zo_adamw_launches -- number of kernels this context has launched since zo_adamw_create. */
 ZO_API int64_t zo_adamw_launches(const zo_adamw_ctx* ctx);
 
+/*
+ * A preference loss over pairs of answers (chosen, rejected): the loss above the tail, whose
+ * forward pass alone is a loss evaluation for zo_step (`loss` may be a place in its device
+ * array), and the gradient of its logits.
+ *
+ * zo_preference_forward -- logits: rows x vocab, row stride ldl; labels: one index per row, < 0
+ *   = the row does not count (a prompt, padding).  offsets: 2 pairs + 1 ascending row numbers;
+ *   sequence q has the rows offsets[q] .. offsets[q + 1] - 1, the chosen answers' first (0 ..
+ *   pairs - 1), then the rejected ones' in the same order.  With
+ *     lse_r = log sum_j exp l_rj,  logp_r = l_r[labels[r]] - lse_r,
+ *     s_q = the sum (average != 0: the mean) of logp_r over the counted rows of q (none: 0),
+ *     D = (s_c - ref_c) - (s_r - ref_r),  z = beta D - margin   (ref_logps: 2 pairs; NULL = 0),
+ *   the loss of a pair is, by `kind`,
+ *     ZO_PREFERENCE_SIGMOID: -(1 - smoothing) log sig(z) - smoothing log sig(-z),
+ *     ZO_PREFERENCE_HINGE:   max(0, 1 - z),
+ *     ZO_PREFERENCE_SQUARE:  (D - 1 / (2 beta))^2,
+ *   and `loss` the mean of `losses`.  logps: the 2 pairs s_q.  For the backward pass, NULL where
+ *   it is not wanted: lse (per row) and dlogp, d loss / d logp_r; both are 0 for rows that do
+ *   not count or are in no sequence.
+ *   workspace: caller-owned device memory of at least zo_preference_workspace(rows, vocab)
+ *   bytes, 16-byte aligned; calls whose work overlaps need one each.
+ * zo_preference_backward -- dlogits_rj = rnd(dloss dlogp_r ([j = labels[r]] - exp(l_rj - lse_r)))
+ *   (dloss: one fp32 value, NULL = 1); rows whose dlogp is 0 are not read and get zeros.  dlogits
+ *   may be logits itself, with the same stride.  It fits any loss of the rows' log-probabilities
+ *   whose derivatives are given as dlogp.
+ * Row sums are fp32 and sequence sums 64-bit; no order of sums depends on timing.  -inf and the
+ * type's lowest value count as exp(...) = 0 beside larger logits; a row of nothing but -inf gives
+ * NaN, and so does a label >= vocab.  Offsets out of order or range give wrong values and no
+ * access outside the buffers.  Rows that do not count may hold anything.  Any alignment and
+ * strides are taken; 16-byte accesses run faster (dlogits: with the logits' position within 16
+ * bytes).  Asynchronous on `stream` (void* cudaStream_t) of the current device.
+ */
+enum { ZO_PREFERENCE_SIGMOID = 0, ZO_PREFERENCE_HINGE = 1, ZO_PREFERENCE_SQUARE = 2 };
+
+ZO_API int64_t zo_preference_workspace(int64_t rows, int64_t vocab);
+ZO_API zo_status zo_preference_forward(const void* logits, int64_t ldl, int64_t rows, int64_t vocab,
+                                       int32_t dtype, const int64_t* labels,
+                                       const int64_t* offsets, int64_t pairs,
+                                       const float* ref_logps, int32_t kind, float beta,
+                                       float smoothing, float margin, int32_t average, float* loss,
+                                       float* losses, float* logps, float* lse, float* dlogp,
+                                       void* workspace, int64_t workspace_bytes, void* stream);
+ZO_API zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t rows,
+                                        int64_t vocab, int32_t dtype, const int64_t* labels,
+                                        const float* lse, const float* dlogp, const float* dloss,
+                                        void* dlogits, int64_t ldd, void* stream);
+
 /* zo_status_string -- static description of a status code. */
 ZO_API const char* zo_status_string(int32_t status);
 

@@ -40,6 +40,10 @@ ZO_MUON_ADJUST_RMS = 2
 ZO_MUON_GRADE_DTYPE = 0
 ZO_MUON_GRADE_F32 = 1
 
+ZO_PREFERENCE_SIGMOID = 0
+ZO_PREFERENCE_HINGE = 1
+ZO_PREFERENCE_SQUARE = 2
+
 ZO_OPTION_WPASS_PATH = 0
 ZO_OPTION_TIMING = 1
 ZO_OPTION_TEST_WAIT_TIMEOUT = 2
@@ -161,6 +165,16 @@ _SIGNATURES = {
     "zo_adamw_step": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_double, _c.c_double,
                                    _c.c_double, _c.c_double, _c.c_double]),
     "zo_adamw_launches": (_c.c_int64, [_c.c_void_p]),
+    "zo_preference_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64]),
+    "zo_preference_forward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
+                                           _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_int64,
+                                           _c.c_void_p, _c.c_int32, _c.c_float, _c.c_float,
+                                           _c.c_float, _c.c_int32, _c.c_void_p, _c.c_void_p,
+                                           _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p,
+                                           _c.c_int64, _c.c_void_p]),
+    "zo_preference_backward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
+                                            _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p,
+                                            _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p]),
     "zo_status_string": (_c.c_char_p, [_c.c_int32]),
     "zo_last_error": (_c.c_char_p, []),
 }
@@ -612,3 +626,63 @@ def zo_adamw_step(ctx, t, count, lr, beta1, beta2, eps, weight_decay):
 
 def zo_adamw_launches(ctx):
     return int(LIB.zo_adamw_launches(ctx))
+
+
+def zo_preference_workspace(rows, vocab):
+    """Bytes of workspace that zo_preference_forward needs."""
+    return int(LIB.zo_preference_workspace(int(rows), int(vocab)))
+
+
+def _one_value(t, where, name, device):
+    """Pointer of a one-element fp32 tensor (None -> NULL)."""
+    import torch
+    if t is None:
+        return None
+    if t.numel() != 1 or t.dtype != torch.float32 or t.device != device:
+        raise ZoError(ZO_ERR_INVALID_ARG, where, f"{name} must be one fp32 value beside the logits")
+    return t.data_ptr()
+
+
+def zo_preference_forward(logits, labels, offsets, ref_logps, kind, beta, smoothing, margin,
+                          average, loss, losses, logps, lse=None, dlogp=None, workspace=None,
+                          stream=None):
+    """The preference loss of pairs of answers (see include/zo.h); every tensor is checked here,
+    since the C ABI cannot see the sizes behind its pointers."""
+    import torch
+    at = "zo_preference_forward"
+    px, ldl = _rows(logits, at, "logits", None, None, None)
+    (rows, vocab), dev, f32 = logits.shape, logits.device, torch.float32
+    code = _dtype_code(logits, at, "logits")
+    if offsets.dim() != 1 or offsets.shape[0] < 3 or offsets.shape[0] % 2 == 0:
+        raise ZoError(ZO_ERR_SHAPE, at, "offsets must hold 2 pairs + 1 row numbers")
+    pairs = offsets.shape[0] // 2
+    if workspace is None or workspace.dtype != torch.uint8 or not workspace.is_contiguous() \
+            or workspace.device != dev:
+        raise ZoError(ZO_ERR_INVALID_ARG, at, "workspace must be contiguous uint8 beside the logits")
+    plabels = _vector(labels, at, "labels", rows, torch.int64, dev)
+    poffsets = _vector(offsets, at, "offsets", 2 * pairs + 1, torch.int64, dev)
+    pref = _vector(ref_logps, at, "ref_logps", 2 * pairs, f32, dev)
+    _on_device(logits, at)
+    _check(LIB.zo_preference_forward(
+        px, ldl, rows, vocab, code, plabels, poffsets, pairs, pref, int(kind), float(beta),
+        float(smoothing), float(margin), int(bool(average)), _one_value(loss, at, "loss", dev),
+        _vector(losses, at, "losses", pairs, f32, dev),
+        _vector(logps, at, "logps", 2 * pairs, f32, dev), _vector(lse, at, "lse", rows, f32, dev),
+        _vector(dlogp, at, "dlogp", rows, f32, dev), workspace.data_ptr(), workspace.numel(),
+        _stream_handle(stream)), at)
+
+
+def zo_preference_backward(logits, labels, lse, dlogp, dloss, dlogits, stream=None):
+    """The logits' gradient of zo_preference_forward (see include/zo.h)."""
+    import torch
+    at = "zo_preference_backward"
+    px, ldl = _rows(logits, at, "logits", None, None, None)
+    (rows, vocab), dev, f32 = logits.shape, logits.device, torch.float32
+    code = _dtype_code(logits, at, "logits")
+    pd, ldd = _rows(dlogits, at, "dlogits", logits.shape, logits.dtype, dev)
+    plabels = _vector(labels, at, "labels", rows, torch.int64, dev)
+    plse, pdlogp = _vector(lse, at, "lse", rows, f32, dev), _vector(dlogp, at, "dlogp", rows, f32, dev)
+    pdloss = _one_value(dloss, at, "dloss", dev)
+    _on_device(logits, at)
+    _check(LIB.zo_preference_backward(px, ldl, rows, vocab, code, plabels, plse, pdlogp, pdloss, pd,
+                                      ldd, _stream_handle(stream)), at)

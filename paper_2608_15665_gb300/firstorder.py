@@ -9,7 +9,10 @@ caller's tensors and launches them in the order of PyTorch's current stream:
   ``LayerNorm``, the two as one ``torch.autograd.Function``; ``layer_norm_sync`` asks
   whether all of them went well;
 * ``Orthogonalizer`` / ``Muon`` / ``AdamW`` -- handles over matrices (tensors of any shape for
-  AdamW, whose states take 32 or 8 bits), bound to one stream.
+  AdamW, whose states take 32 or 8 bits), bound to one stream;
+* ``preference_loss`` / ``preference_loss_backward`` -- a loss over pairs of answers from their
+  logits, and the logits' gradient; ``PreferenceLoss``, the two as one
+  ``torch.autograd.Function``.
 
 No arithmetic happens here.
 """
@@ -62,12 +65,12 @@ def _device_of(x, at):
     return dev
 
 
-def _refuse_grad(at, *tensors):
+def _refuse_grad(at, *tensors, function="LayerNorm"):
     """Outputs made through raw pointers have no history: where one would be recorded, an error."""
     for t in tensors:
         if t is not None and t.requires_grad and torch.is_grad_enabled():
             raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, "an input requires a gradient, which is not "
-                             "recorded here: call LayerNorm.apply, or this under torch.no_grad()")
+                             f"recorded here: call {function}.apply, or this under torch.no_grad()")
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, residual=None, stats=True):
@@ -361,3 +364,101 @@ class AdamW(_Handle):
         t = self.steps + 1 if t is None else int(t)
         self._call(zb.zo_adamw_step, t, None, lr, betas[0], betas[1], eps, weight_decay)
         self.steps = t
+
+
+class PreferenceOut(NamedTuple):
+    loss: torch.Tensor                 # the pairs' mean, one fp32 value
+    losses: torch.Tensor               # of every pair
+    logps: torch.Tensor                # of every sequence, the chosen ones first
+    lse: Optional[torch.Tensor]        # for the backward pass, per row (None: not asked for)
+    dlogp: Optional[torch.Tensor]
+
+
+PREFERENCES = {"sigmoid": zb.ZO_PREFERENCE_SIGMOID, "hinge": zb.ZO_PREFERENCE_HINGE,
+               "square": zb.ZO_PREFERENCE_SQUARE}
+
+
+def preference_loss(logits, labels, offsets, ref_logps=None, beta=0.1, kind="sigmoid",
+                    smoothing=0.0, margin=0.0, average=False, grad=True, out=None):
+    """The preference loss of pairs of answers from rows x vocab logits (bf16 or fp32) and the
+    rows' labels (int64; below zero: the row does not count).  offsets (int64, 2 pairs + 1): the
+    sequences' first rows, the chosen ones' and then the rejected ones', and the end.  ref_logps:
+    the reference model's sums per sequence (fp32; none: zero).  average: means instead of sums.
+    grad: also what the backward pass takes.  out: a one-element fp32 tensor for the loss, as a
+    place in the losses of a subspace step.  Its outputs have no history for autograd
+    (``PreferenceLoss`` does that)."""
+    at = "preference_loss"
+    _refuse_grad(at, logits, ref_logps, function="PreferenceLoss")
+    if kind not in PREFERENCES:
+        raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, f"unknown kind {kind!r}")
+    dev = _device_of(logits, at)
+    px, ldl = zb._rows(logits, at, "logits", None, None, None)
+    (rows, vocab), device = logits.shape, logits.device
+    if offsets.dim() != 1 or offsets.shape[0] < 3 or offsets.shape[0] % 2 == 0:
+        raise zb.ZoError(zb.ZO_ERR_SHAPE, at, "offsets must hold 2 pairs + 1 row numbers")
+    pairs = offsets.shape[0] // 2
+    plabels = zb._vector(labels, at, "labels", rows, torch.int64, device)
+    poffsets = zb._vector(offsets, at, "offsets", 2 * pairs + 1, torch.int64, device)
+    pref = zb._vector(ref_logps, at, "ref_logps", 2 * pairs, _F32, device)
+    loss = _empty((), dtype=_F32, device=device) if out is None else out
+    ploss = zb._one_value(loss, at, "out", device)
+    losses = _empty(pairs, dtype=_F32, device=device)
+    logps = _empty(2 * pairs, dtype=_F32, device=device)
+    lse = dlogp = plse = pdlogp = None
+    if grad:
+        lse = _empty(rows, dtype=_F32, device=device)
+        dlogp = _empty_like(lse)
+        plse, pdlogp = lse.data_ptr(), dlogp.data_ptr()
+    ws_bytes = zb.LIB.zo_preference_workspace(rows, vocab)
+    ws = _empty(ws_bytes, dtype=torch.uint8, device=device)
+    _call(zb.LIB.zo_preference_forward, dev, at, px, ldl, rows, vocab,
+          _code(logits.dtype, at, "logits"), plabels, poffsets, pairs, pref, PREFERENCES[kind],
+          beta, smoothing, margin, int(bool(average)), ploss, losses.data_ptr(), logps.data_ptr(),
+          plse, pdlogp, ws.data_ptr(), ws_bytes)
+    return PreferenceOut(loss, losses, logps, lse, dlogp)
+
+
+def preference_loss_backward(logits, labels, lse, dlogp, dloss=None, out=None):
+    """The logits' gradient from the forward pass's lse and dlogp (or any other loss's derivatives
+    by the rows' log-probabilities) and the loss's own gradient (one fp32 value; none: 1).  out:
+    where it goes, which may be the logits themselves.  Without a history for autograd."""
+    at = "preference_loss_backward"
+    _refuse_grad(at, logits, lse, dlogp, dloss, function="PreferenceLoss")
+    dev = _device_of(logits, at)
+    px, ldl = zb._rows(logits, at, "logits", None, None, None)
+    (rows, vocab), device = logits.shape, logits.device
+    plabels = zb._vector(labels, at, "labels", rows, torch.int64, device)
+    plse = zb._vector(lse, at, "lse", rows, _F32, device)
+    pdlogp = zb._vector(dlogp, at, "dlogp", rows, _F32, device)
+    pdloss = zb._one_value(dloss, at, "dloss", device)
+    if out is None:
+        # rows as far apart as the logits', for accesses of the same alignment
+        out = (_empty_like(logits, memory_format=_contiguous) if ldl == vocab else
+               _empty((rows, ldl), dtype=logits.dtype, device=device)[:, :vocab])
+    pd, ldd = zb._rows(out, at, "out", logits.shape, logits.dtype, device)
+    _call(zb.LIB.zo_preference_backward, dev, at, px, ldl, rows, vocab,
+          _code(logits.dtype, at, "logits"), plabels, plse, pdlogp, pdloss, pd, ldd)
+    return out
+
+
+class PreferenceLoss(torch.autograd.Function):
+    """``PreferenceLoss.apply(logits, labels, offsets, ref_logps, beta, kind, smoothing, margin,
+    average)``: the loss, differentiable once by the logits."""
+
+    @staticmethod
+    def forward(ctx, logits, labels, offsets, ref_logps=None, beta=0.1, kind="sigmoid",
+                smoothing=0.0, margin=0.0, average=False):
+        if ref_logps is not None and ref_logps.requires_grad:
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, "PreferenceLoss",
+                             "the reference's log-probabilities get no gradient: detach them")
+        out = preference_loss(logits, labels, offsets, ref_logps, beta, kind, smoothing, margin,
+                              average, grad=ctx.needs_input_grad[0])
+        ctx.save_for_backward(logits, labels, out.lse, out.dlogp)
+        return out.loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        logits, labels, lse, dlogp = ctx.saved_tensors
+        d = preference_loss_backward(logits, labels, lse, dlogp, dloss)
+        return (d,) + (None,) * (len(ctx.needs_input_grad) - 1)

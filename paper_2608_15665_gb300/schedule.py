@@ -76,6 +76,18 @@ class SubZeroPlus:
 
     def step(self, t, adam_t, losses, scheme, eps, lr, beta1, beta2, eps_adam, restore_query,
              restore_coef, optimizer=zb.ZO_OPT_ADAM, gamma_out=None):
+        """losses: as for zo_step; a list of one-element CUDA tensors (``preference_loss``) is
+        gathered on the device, so that the step waits for none of them on the host."""
+        if isinstance(losses, (list, tuple)) and losses and all(
+                isinstance(x, torch.Tensor) and x.is_cuda for x in losses):
+            losses = torch.stack([x.detach().reshape(()).float() for x in losses])
+            own = (torch.cuda.default_stream(losses.device) if self.stream is None else self.stream
+                   if isinstance(self.stream, torch.cuda.Stream)
+                   else torch.cuda.ExternalStream(int(self.stream), device=losses.device))
+            current = torch.cuda.current_stream(losses.device)
+            if own != current:
+                own.wait_stream(current)
+                losses.record_stream(own)
         zb.zo_step(self.ctx, t, adam_t, losses, SCHEMES[scheme], eps, lr, beta1, beta2, eps_adam,
                    restore_query, restore_coef, optimizer, gamma_out)
 
