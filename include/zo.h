@@ -579,6 +579,45 @@ ZO_API zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t
                                         const float* lse, const float* dlogp, const float* dloss,
                                         void* dlogits, int64_t ldd, void* stream);
 
+/*
+ * The gated linear block of a feed-forward layer, for a tail that reaches into the model's last
+ * block.  All matrices are bf16, row-major; products and activations are fp32 and every result is
+ * rounded once.
+ *
+ * zo_gated_forward -- G = X Wg^T, U = X Wu^T, H = act(G) U (element by element), from the fp32 G
+ *   and U.  X: T x D; Wg, Wu: F x D; H: T x F; G and U (T x F) are kept for the backward pass, or
+ *   both NULL.
+ * zo_gated_backward -- from dH (T x F) and the kept G and U:
+ *     dG = rnd(dH U act'(G)),  dU = rnd(dH act(G)),
+ *     dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X.
+ *   NULL = not wanted: dX (then Wg and Wu are not read), or both of dWg and dWu (then X is not).
+ *   workspace: caller-owned device memory of at least zo_gated_workspace(T, F) bytes, 16-byte
+ *   aligned, for dG and dU; calls whose work overlaps need one each.
+ * act: ZO_GATED_SILU g sig(g), or ZO_GATED_GELU_TANH g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))).
+ * Every matrix is 16-byte aligned and its row stride (ldx, ... in elements) a multiple of 8; D and
+ * F are multiples of 8, T is any number from 0 on (no tokens: dWg and dWu are zero).  Outputs must
+ * not overlap inputs.  No atomics: the same inputs give the same bits.  Asynchronous on `stream`
+ * (void* cudaStream_t) of the current device.
+ * zo_gated_sync_status -- synchronise the stream; ZO_ERR_TIMEOUT, once, where a wait of one of
+ *   these kernels on the current device has run out since it was last asked (its results are
+ *   incomplete then); ZO_OK otherwise.
+ */
+enum { ZO_GATED_SILU = 0, ZO_GATED_GELU_TANH = 1 };
+
+ZO_API zo_status zo_gated_forward(const void* X, int64_t ldx, int64_t T, int64_t D, const void* Wg,
+                                  int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F,
+                                  int32_t act, void* H, int64_t ldh, void* G, int64_t ldg, void* U,
+                                  int64_t ldu, void* stream);
+ZO_API int64_t zo_gated_workspace(int64_t T, int64_t F);
+ZO_API zo_status zo_gated_backward(const void* dH, int64_t lddh, const void* X, int64_t ldx,
+                                   int64_t T, int64_t D, const void* Wg, int64_t ldwg,
+                                   const void* Wu, int64_t ldwu, int64_t F, int32_t act,
+                                   const void* G, int64_t ldg, const void* U, int64_t ldu, void* dX,
+                                   int64_t lddx, void* dWg, int64_t lddwg, void* dWu,
+                                   int64_t lddwu, void* workspace, int64_t workspace_bytes,
+                                   void* stream);
+ZO_API zo_status zo_gated_sync_status(void* stream);
+
 /* zo_status_string -- static description of a status code. */
 ZO_API const char* zo_status_string(int32_t status);
 

@@ -44,6 +44,9 @@ ZO_PREFERENCE_SIGMOID = 0
 ZO_PREFERENCE_HINGE = 1
 ZO_PREFERENCE_SQUARE = 2
 
+ZO_GATED_SILU = 0
+ZO_GATED_GELU_TANH = 1
+
 ZO_OPTION_WPASS_PATH = 0
 ZO_OPTION_TIMING = 1
 ZO_OPTION_TEST_WAIT_TIMEOUT = 2
@@ -175,6 +178,18 @@ _SIGNATURES = {
     "zo_preference_backward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
                                             _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p,
                                             _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "zo_gated_forward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_void_p,
+                                      _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int32,
+                                      _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                      _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "zo_gated_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64]),
+    "zo_gated_backward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64,
+                                       _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                       _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_int64, _c.c_void_p,
+                                       _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                       _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                       _c.c_void_p]),
+    "zo_gated_sync_status": (_c.c_int32, [_c.c_void_p]),
     "zo_status_string": (_c.c_char_p, [_c.c_int32]),
     "zo_last_error": (_c.c_char_p, []),
 }
@@ -686,3 +701,62 @@ def zo_preference_backward(logits, labels, lse, dlogp, dloss, dlogits, stream=No
     _on_device(logits, at)
     _check(LIB.zo_preference_backward(px, ldl, rows, vocab, code, plabels, plse, pdlogp, pdloss, pd,
                                       ldd, _stream_handle(stream)), at)
+
+
+def _gated_matrix(t, where, name, shape, device):
+    """(pointer, row stride) of a bf16 matrix (None -> NULL)."""
+    import torch
+    return _rows(t, where, name, shape, torch.bfloat16, device)
+
+
+def zo_gated_forward(X, Wg, Wu, act, H, G=None, U=None, stream=None):
+    """H = act(X Wg^T) (X Wu^T), and the two products where G and U are given (see include/zo.h);
+    every tensor is checked here, since the C ABI cannot see the sizes behind its pointers."""
+    at = "zo_gated_forward"
+    px, ldx = _gated_matrix(X, at, "X", None, None)
+    dev, (T, D) = X.device, X.shape
+    pg, ldg = _gated_matrix(Wg, at, "Wg", None, dev)
+    F = Wg.shape[0]
+    pu, ldu = _gated_matrix(Wu, at, "Wu", Wg.shape, dev)
+    if Wg.shape[1] != D:
+        raise ZoError(ZO_ERR_SHAPE, at, f"Wg has shape {tuple(Wg.shape)}, expected (F, {D})")
+    outs = [_gated_matrix(t, at, name, (T, F), dev) for name, t in (("H", H), ("G", G), ("U", U))]
+    _on_device(X, at)
+    _check(LIB.zo_gated_forward(px, ldx, T, D, pg, ldg, pu, ldu, F, int(act), *outs[0], *outs[1],
+                                *outs[2], _stream_handle(stream)), at)
+
+
+def zo_gated_workspace(T, F):
+    """Bytes of workspace that zo_gated_backward needs."""
+    return int(LIB.zo_gated_workspace(int(T), int(F)))
+
+
+def zo_gated_backward(dH, X, Wg, Wu, act, G, U, dX=None, dWg=None, dWu=None, workspace=None,
+                      stream=None):
+    """dX, dWg and dWu of zo_gated_forward (see include/zo.h).  workspace: a contiguous uint8
+    tensor of zo_gated_workspace(T, F) bytes."""
+    import torch
+    at = "zo_gated_backward"
+    px, ldx = _gated_matrix(X, at, "X", None, None)
+    dev, (T, D) = X.device, X.shape
+    pg, ldg = _gated_matrix(Wg, at, "Wg", None, dev)
+    F = Wg.shape[0]
+    pu, ldu = _gated_matrix(Wu, at, "Wu", Wg.shape, dev)
+    if Wg.shape[1] != D:
+        raise ZoError(ZO_ERR_SHAPE, at, f"Wg has shape {tuple(Wg.shape)}, expected (F, {D})")
+    ins = [_gated_matrix(t, at, name, (T, F), dev) for name, t in (("dH", dH), ("G", G), ("U", U))]
+    outs = [_gated_matrix(t, at, name, shape, dev) for name, t, shape in
+            (("dX", dX, (T, D)), ("dWg", dWg, (F, D)), ("dWu", dWu, (F, D)))]
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise ZoError(ZO_ERR_INVALID_ARG, at, "workspace must be contiguous uint8 beside X")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+    _on_device(X, at)
+    _check(LIB.zo_gated_backward(*ins[0], px, ldx, T, D, pg, ldg, pu, ldu, F, int(act), *ins[1],
+                                 *ins[2], *outs[0], *outs[1], *outs[2], ws, ws_bytes,
+                                 _stream_handle(stream)), at)
+
+
+def zo_gated_sync_status(stream=None):
+    _check(LIB.zo_gated_sync_status(_stream_handle(stream)), "zo_gated_sync_status")

@@ -22,19 +22,6 @@ bool elem_aligned(const void* p, int32_t dtype) {
 
 constexpr int64_t kMaxExtent = int64_t(1) << 31;
 
-// SM count of the current device (cached per device), or 0
-int32_t sm_count() {
-  static int32_t count[64] = {};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (count[dev] == 0) {
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    count[dev] = n;
-  }
-  return count[dev];
-}
-
 // the current device's status word, or null
 uint32_t* status_word() {
   static uint32_t* word[64] = {};

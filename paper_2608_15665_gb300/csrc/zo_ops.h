@@ -1,5 +1,6 @@
 // Host-side launchers of the first-order operators (internal to the library): layer
-// normalisation, and Newton-Schulz orthogonalisation with the Muon update.
+// normalisation, Newton-Schulz orthogonalisation with the Muon update, and the products of the
+// gated linear block.
 #pragma once
 
 #include <cstdint>
@@ -149,5 +150,43 @@ int32_t ortho_small_smem(int64_t p, int64_t c, int32_t cluster);
 cudaError_t launch_ortho_small(const OrthoMat* mats, const int* which, int32_t n, int32_t cluster,
                                int32_t smem, const OrthoStep* steps, int32_t n_steps,
                                const OrthoUpdate& u, uint32_t* status, cudaStream_t s);
+
+// ---- gated linear block (zo_gated.cu; its products in zo_gated_gemm.cu) ----------------
+// All bf16.  Forward: G = X Wg^T, U = X Wu^T, H = act(G) U.  Backward, from dG and dU:
+// dX = dG Wg + dU Wu, dWg = dG^T X, dWu = dU^T X.
+constexpr int kGatedMaxPairs = 128;
+enum GatedAct : int32_t { kGatedSilu = 0, kGatedGelu = 1 };
+
+// act(g) = g s with s = sig(g) (SiLU) or sig(2 sqrt(2 / pi) (g + 0.044715 g^3)) (GELU by tanh: half of
+// 1 + tanh(y) is sig(2 y), without the cancellation at negative y).  The exponential's argument:
+#ifdef __CUDACC__
+__device__ __forceinline__ float gated_gate(float g, int32_t act) {
+  const float y = act == kGatedSilu ? g : 1.5957691216057308f * g * fmaf(0.044715f * g, g, 1.0f);
+  return __fdividef(1.0f, 1.0f + __expf(-y));
+}
+#endif
+
+struct GatedForward {
+  CUtensorMap x, w[2], out[3];      // X; Wg and Wu; H, G and U
+  int32_t T, D, F, act, save;
+  int32_t side;                     // columns of Wg (and of Wu) to a tile
+};
+struct GatedBackward {
+  CUtensorMap d_rows[2], w_cols[2], dx;           // dX: dG, dU along F; Wg, Wu by rows of F
+  CUtensorMap d_cols[2], x_cols, dw[2];           // dW: dG, dU and X by rows of T
+  int32_t T, D, F;
+  int32_t n_dx, n_dw;               // tiles of dX and of both dW (0: not wanted)
+  int32_t first[kGatedMaxPairs + 1];   // pair q takes dW's tiles first[q] .. first[q + 1] - 1
+};
+// rows of a box of X, and of Wg (Wu); columns and rows of a box of a result
+constexpr int kGatedRows = 128, kGatedOutCols = 16, kGatedOutRows = 32;
+// columns of a tile's two halves for this call
+int32_t gated_side(int64_t T, int64_t D, int64_t F, int32_t pairs);
+// SM pairs that run at once, or 0
+int32_t gated_max_pairs();
+// fills n_dx, n_dw and first
+void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs);
+cudaError_t launch_gated_forward(const GatedForward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
+cudaError_t launch_gated_backward(const GatedBackward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
 
 }  // namespace zo

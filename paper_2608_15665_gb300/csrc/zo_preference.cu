@@ -359,18 +359,6 @@ gradient_kernel(const Rows a, const float* __restrict__ lse, const float* __rest
 
 // ---- host ----------------------------------------------------------------------------------
 
-int32_t sm_count() {
-  static int32_t count[64] = {};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (count[dev] == 0) {
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    count[dev] = n;
-  }
-  return count[dev];
-}
-
 // Parts of a row: as many as give every SM two CTAs, none narrower than kPartCols.
 int32_t parts_of(int64_t rows, int64_t vocab, int32_t sms) {
   int32_t parts = 1;

@@ -12,7 +12,10 @@ caller's tensors and launches them in the order of PyTorch's current stream:
   AdamW, whose states take 32 or 8 bits), bound to one stream;
 * ``preference_loss`` / ``preference_loss_backward`` -- a loss over pairs of answers from their
   logits, and the logits' gradient; ``PreferenceLoss``, the two as one
-  ``torch.autograd.Function``.
+  ``torch.autograd.Function``;
+* ``gated_linear`` / ``gated_linear_backward`` -- the gated linear block of a feed-forward layer and
+  its gradients, and ``GatedLinear``, the two as one ``torch.autograd.Function``;
+  ``gated_linear_sync`` asks whether all of them went well.
 
 No arithmetic happens here.
 """
@@ -462,3 +465,99 @@ class PreferenceLoss(torch.autograd.Function):
         logits, labels, lse, dlogp = ctx.saved_tensors
         d = preference_loss_backward(logits, labels, lse, dlogp, dloss)
         return (d,) + (None,) * (len(ctx.needs_input_grad) - 1)
+
+
+class GatedOut(NamedTuple):
+    h: torch.Tensor
+    gate: Optional[torch.Tensor]       # X Wg^T and X Wu^T for the backward pass (None: not kept)
+    up: Optional[torch.Tensor]
+
+
+ACTIVATIONS = {"silu": zb.ZO_GATED_SILU, "gelu": zb.ZO_GATED_GELU_TANH}
+_BF16 = torch.bfloat16
+
+
+def _activation(act, at):
+    if act not in ACTIVATIONS:
+        raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, at, f"unknown activation {act!r}")
+    return ACTIVATIONS[act]
+
+
+def _gated_inputs(x, w_gate, w_up, at):
+    dev = _device_of(x, at)
+    px = zb._rows(x, at, "x", None, _BF16, None)
+    pg = zb._rows(w_gate, at, "w_gate", None, _BF16, x.device)
+    if w_gate.shape[1] != x.shape[1]:
+        raise zb.ZoError(zb.ZO_ERR_SHAPE, at, f"w_gate has shape {tuple(w_gate.shape)}, expected "
+                                              f"(F, {x.shape[1]})")
+    return dev, px, pg, zb._rows(w_up, at, "w_up", w_gate.shape, _BF16, x.device)
+
+
+def gated_linear(x, w_gate, w_up, act="silu", save=False):
+    """h = act(x w_gate^T) (x w_up^T) of a tokens x D matrix and F x D weights (bf16; D and F
+    multiples of 8), with act "silu" or "gelu" (by tanh).  save: both products too, for the
+    backward pass.  Its outputs have no history for autograd (``GatedLinear`` does that)."""
+    at = "gated_linear"
+    _refuse_grad(at, x, w_gate, w_up, function="GatedLinear")
+    code = _activation(act, at)
+    dev, px, pg, pu = _gated_inputs(x, w_gate, w_up, at)
+    (T, D), F = x.shape, w_gate.shape[0]
+    h = _empty((T, F), dtype=_BF16, device=x.device)
+    gate = up = pgate = pup = None
+    if save:
+        gate, up = _empty_like(h), _empty_like(h)
+        pgate, pup = gate.data_ptr(), up.data_ptr()
+    _call(zb.LIB.zo_gated_forward, dev, at, *px, T, D, *pg, *pu, F, code, h.data_ptr(), F, pgate, F,
+          pup, F)
+    return GatedOut(h, gate, up)
+
+
+def gated_linear_backward(dh, x, w_gate, w_up, gate, up, act="silu", want_x=True, want_weights=True):
+    """(dx, dw_gate, dw_up) from the gradient of h and the forward pass's inputs and products; None
+    where not wanted.  Like ``gated_linear``, without a history for autograd."""
+    at = "gated_linear_backward"
+    _refuse_grad(at, dh, x, w_gate, w_up, gate, up, function="GatedLinear")
+    code = _activation(act, at)
+    dev, px, pg, pu = _gated_inputs(x, w_gate, w_up, at)
+    (T, D), F, device = x.shape, w_gate.shape[0], x.device
+    ins = [zb._rows(t, at, name, (T, F), _BF16, device)
+           for name, t in (("dh", dh), ("gate", gate), ("up", up))]
+    dx = dwg = dwu = pdx = pdwg = pdwu = None
+    if want_x:
+        dx = _empty((T, D), dtype=_BF16, device=device)
+        pdx = dx.data_ptr()
+    if want_weights:
+        dwg, dwu = (_empty((F, D), dtype=_BF16, device=device) for _ in range(2))
+        pdwg, pdwu = dwg.data_ptr(), dwu.data_ptr()
+    ws_bytes = zb.LIB.zo_gated_workspace(T, F)
+    ws = _empty(ws_bytes, dtype=torch.uint8, device=device)
+    _call(zb.LIB.zo_gated_backward, dev, at, *ins[0], *px, T, D, *pg, *pu, F, code, *ins[1], *ins[2],
+          pdx, D, pdwg, D, pdwu, D, ws.data_ptr(), ws_bytes)
+    return dx, dwg, dwu
+
+
+def gated_linear_sync(device=None):
+    """Waits for the current stream, and raises where a wait inside a gated linear block's kernel has
+    run out on this device since it was last asked (results of that call are incomplete then)."""
+    with torch.cuda.device(device):
+        zb.zo_gated_sync_status(torch.cuda.current_stream())
+
+
+class GatedLinear(torch.autograd.Function):
+    """``GatedLinear.apply(x, w_gate, w_up, act)`` on a tokens x D matrix.  Differentiable once."""
+
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, act="silu"):
+        out = gated_linear(x, w_gate, w_up, act, save=any(ctx.needs_input_grad[:3]))
+        ctx.save_for_backward(x, w_gate, w_up, out.gate, out.up)
+        ctx.act = act
+        return out.h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh):
+        x, w_gate, w_up, gate, up = ctx.saved_tensors
+        need_x, need_g, need_u = ctx.needs_input_grad[:3]
+        dx, dwg, dwu = gated_linear_backward(dh.contiguous(), x, w_gate, w_up, gate, up, ctx.act,
+                                             want_x=need_x, want_weights=need_g or need_u)
+        return dx, dwg if need_g else None, dwu if need_u else None, None
