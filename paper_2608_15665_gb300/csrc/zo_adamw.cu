@@ -5,8 +5,8 @@
 //   W <- rnd((1 - lr wd) W - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps))
 //
 // Bound by HBM: W is read and written, g read, the states read and written, once each.  A warp
-// works on blocks of 256 neighbouring elements, eight to a lane; a CTA on kChunk elements of one
-// tensor, found in a table of the chunks, its loads in flight together.
+// works on blocks of 256 neighbouring elements, eight to a lane; a CTA on a chunk of one tensor,
+// found in a table of the chunks.
 //
 // States in 8 bits: m and r = sqrt(v) as e4m3 codes times 2^(E - 134), E = the biased fp32
 // exponent of the largest |m| (r) of the block of 256, in one byte; so the block's largest is in
@@ -45,9 +45,14 @@ using namespace zo::host;
 constexpr uint32_t kTagAdamW = 6;
 constexpr int kThreads = 256, kLane = 8;
 constexpr int kBlock = 32 * kLane;               // elements of a power of two
-constexpr int kUnits = 2;                        // blocks a warp holds at once
-constexpr int kChunk = kThreads * kLane * kUnits;
-static_assert(kBlock == 256 && kChunk % kBlock == 0, "a chunk is whole blocks");
+constexpr int kRow = kThreads * kLane;           // a block of every warp
+constexpr int kMaxUnits = 8;                    // such rows of a chunk, at most
+constexpr int kCtas = 3;                         // of an SM
+// 8 bits: a warp's ring of blocks in shared memory (W and G in fp32 at most)
+constexpr int kStages = 3, kStageBytes = kBlock * 10;
+constexpr int kRingBytes = kThreads / 32 * kStages * kStageBytes;
+static_assert(kCtas * kRingBytes <= 227 * 1024, "shared memory per SM");
+static_assert(kBlock == 256 && kRow % kBlock == 0 && kMaxUnits <= 32, "a chunk is whole blocks");
 
 struct Tensor {
   void* W;
@@ -59,30 +64,34 @@ struct Tensor {
   int32_t wide;                                  // contiguous, and aligned to a lane's accesses
 };
 
-// What a step is made of; c1 and c2 are 1 - b1^t and 1 - b2^t.
-struct Step {
-  float b1, one_b1, b2, one_b2, keep, lr, eps;
-  float c1, c2;
+// What a step is made of: the update is rate m / (sqrt(v) spread + eps).
+struct Now {                                     // what goes by the step's number
+  float rate, spread;                            // -lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   uint32_t t;
+};
+struct Step {
+  float b1, one_b1, b2, one_b2, keep, eps;
+  float none;                                    // -0: what a product is added to
+  Now now;
   uint32_t key0, key1;
 };
-struct Counted {                                 // c1, c2 and t where the device counts
-  float c1, c2;
-  uint32_t t;
-};
+__host__ __device__ inline Now now_of(int64_t t, double lr, double b1, double b2) {
+  return Now{(float)(lr / expm1((double)t * log(b1))),
+             (float)(1.0 / sqrt(-expm1((double)t * log(b2)))), (uint32_t)t};
+}
 
 // One more step: its number and bias corrections.
-__global__ void adamw_count_kernel(int64_t* count, double b1, double b2, Counted* out) {
+__global__ void adamw_count_kernel(int64_t* count, double lr, double b1, double b2, Now* out) {
   zo::pdl_wait();
   int64_t t = *count;
   t = t < 0 ? 1 : t + 1;
   *count = t;
-  *out = Counted{(float)-expm1((double)t * log(b1)), (float)-expm1((double)t * log(b2)),
-                 (uint32_t)t};
+  *out = now_of(t, lr, b1, b2);
 }
 
-template <typename T>
-__device__ __forceinline__ float to_float(T x) { return static_cast<float>(x); }
+__device__ __forceinline__ uint32_t smem_u32(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
 
 // Eight values of a lane as they lie in memory.
 template <typename T>
@@ -98,6 +107,34 @@ struct Raw {
 #pragma unroll
       for (int q = 0; q < kWords; q += 4) {
         const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p) + q / 4);
+        w[q] = a.x;
+        w[q + 1] = a.y;
+        w[q + 2] = a.z;
+        w[q + 3] = a.w;
+      }
+    }
+  }
+  // to shared memory, asynchronously, and from there
+  static __device__ __forceinline__ void fetch(uint8_t* to, const T* p) {
+    if constexpr (sizeof(T) == 1) {
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(to)), "l"(p) : "memory");
+    } else {
+#pragma unroll
+      for (int q = 0; q < kWords / 4; ++q)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + 512 * q)),
+                     "l"(p + q * (16 / sizeof(T)))
+                     : "memory");
+    }
+  }
+  __device__ __forceinline__ void take(const uint8_t* from) {
+    if constexpr (sizeof(T) == 1) {
+      const uint2 a = *reinterpret_cast<const uint2*>(from);
+      w[0] = a.x;
+      w[1] = a.y;
+    } else {
+#pragma unroll
+      for (int q = 0; q < kWords; q += 4) {
+        const uint4 a = *reinterpret_cast<const uint4*>(from + 128 * q);
         w[q] = a.x;
         w[q + 1] = a.y;
         w[q + 2] = a.z;
@@ -181,56 +218,93 @@ __device__ __forceinline__ void pack(const float (&x)[kLane], Raw<T>& r) {
   }
 }
 
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // ---- 8-bit states ------------------------------------------------------------------------
+// The kernel's instructions are what this path has to save: at HBM's rate an SM has 55 issue slots
+// an element.  So products and sums go two to an instruction, random bits and codes move by byte
+// permutations, and what is rare (a number that is not finite, a root whose code is 0) is found by a
+// maximum over the block and mended apart.
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 
 // Eight e4m3 codes times 2^(E - 134).
 __device__ __forceinline__ void decode(const Raw<uint8_t>& r, uint32_t E, float (&x)[kLane]) {
-  const float s = power((int)max(E, 40u) - 134);
+  const float2 s = both(power((int)max(E, 40u) - 134));
 #pragma unroll
   for (int q = 0; q < kLane / 2; ++q) {
     const __half2 h = __nv_cvt_fp8x2_to_halfraw2(
         (__nv_fp8x2_storage_t)(r.w[q / 2] >> (16 * (q & 1))), __NV_E4M3);
-    const float2 f = __half22float2(h);
-    x[2 * q] = f.x * s;
-    x[2 * q + 1] = f.y * s;
+    const float2 f = zo::mul2(__half22float2(h), s);
+    x[2 * q] = f.x;
+    x[2 * q + 1] = f.y;
   }
 }
 
-// Codes of nonnegative (kSigned: any) x of a block whose largest has the biased exponent E.
+// Codes of x of a block whose largest finite |x| is `top` (bits, 2^(E - 127) its power of two).
 // x 2^(134 - E) 2^-120 is laid out like the code: its exponent field, and its subnormal numbers,
 // begin where e4m3's do.  So the code is the fp32 bits without the last 20, rounded up where
-// these and the random bits carry.  Infinity and NaN become NaN.  (Two products: one power of two
-// of both may leave fp32's range.  The second rounds subnormals at 2^-20 of a code's step.)
+// these and the random bits carry; all of it is formed four bits further left, where the code is
+// the topmost byte below the sign.  (The product rounds subnormals at 2^-20 of a code's step.)
+// odd: the block holds something not finite, which becomes NaN.
 template <bool kSigned>
-__device__ __forceinline__ void encode(const float (&x)[kLane], uint32_t E, const uint4& random,
-                                       Raw<uint8_t>& r) {
-  const float s = power(134 - (int)max(E, 40u));
+__device__ __forceinline__ void encode(const float (&x)[kLane], uint32_t E, bool odd,
+                                       const uint4& random, Raw<uint8_t>& r) {
+  const int e40 = max((int)E, 40);
+  const float2 s = both(power(14 - min(e40, 140)));
   const uint32_t rw[4] = {random.x, random.y, random.z, random.w};
+  uint32_t c[kLane];
+  float y[kLane];
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    uint32_t word = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = 4 * q + i;
-      const uint32_t add = e & 1 ? (rw[e / 2] >> 12) & 0xFFFF0u : (rw[e / 2] << 4) & 0xFFFF0u;
-      const uint32_t bits = __float_as_uint((kSigned ? fabsf(x[e]) : x[e]) * s * 0x1p-120f);
-      uint32_t code = min((bits + add) >> 20, 0x7Fu);
-      if constexpr (kSigned) code |= (__float_as_uint(x[e]) >> 24) & 0x80u;
-      else code = max(code, min(__float_as_uint(x[e]), 1u));
-      word |= code << (8 * i);
-    }
-    r.w[q] = word;
+  for (int e = 0; e < kLane; e += 2) {
+    float2 v = make_float2(x[e], x[e + 1]);
+    if (e40 > 140) v = zo::mul2(v, both(power(140 - e40)));     // (their power leaves fp32's range)
+    v = zo::mul2(v, s);
+    y[e] = v.x;
+    y[e + 1] = v.y;
   }
+#pragma unroll
+  for (int e = 0; e < kLane; ++e) {
+    const uint32_t add = __byte_perm(rw[e / 2], 0, e & 1 ? 0x4324 : 0x4104);
+    const uint32_t bits = (__float_as_uint(y[e]) << 4) + add;
+    if constexpr (kSigned) c[e] = (bits & 0x7FFFFFFFu) | (__float_as_uint(x[e]) & 0x80000000u);
+    else c[e] = bits;
+  }
+  if constexpr (!kSigned) {
+    uint32_t least = c[0];
+#pragma unroll
+    for (int e = 1; e < kLane; ++e) least = min(least, c[e]);
+    if (least < 0x01000000u) {                       // above zero stays above zero
+#pragma unroll
+      for (int e = 0; e < kLane; ++e)
+        if (x[e] > 0.0f) c[e] = max(c[e], 0x01000000u);
+    }
+  }
+  if (odd) {
+#pragma unroll
+    for (int e = 0; e < kLane; ++e)
+      if (!(fabsf(x[e]) < __int_as_float(0x7F800000)))
+        c[e] = 0x7F000000u | (__float_as_uint(x[e]) & 0x80000000u);
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    r.w[q] = __byte_perm(__byte_perm(c[4 * q], c[4 * q + 1], 0x0073),
+                         __byte_perm(c[4 * q + 2], c[4 * q + 3], 0x0073), 0x5410);
 }
 
-// The largest finite |x| of the warp's block, as bits.
-__device__ __forceinline__ uint32_t largest(const float (&x)[kLane]) {
-  uint32_t top = 0;
+// The largest finite |x| of the warp's block, as bits; odd: there are others.
+__device__ __forceinline__ uint32_t largest(const float (&x)[kLane], bool* odd) {
+  // (a NaN is no maximum, but it and infinity spoil a sum of zeros)
+  float most = 0.0f;
+  float2 zeros = both(0.0f);
 #pragma unroll
-  for (int e = 0; e < kLane; ++e) top = max(top, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-  top = __reduce_max_sync(0xffffffffu, top);
-  if (top >= 0x7F800000u) {
+  for (int e = 0; e < kLane; e += 2) {
+    most = fmaxf(fmaxf(most, fabsf(x[e])), fabsf(x[e + 1]));
+    zeros = zo::fma2(make_float2(x[e], x[e + 1]), both(0.0f), zeros);
+  }
+  *odd = __any_sync(0xffffffffu, zeros.x + zeros.y != 0.0f);
+  uint32_t top;
+  top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
+  if (*odd) {
     top = 0;
 #pragma unroll
     for (int e = 0; e < kLane; ++e) {
@@ -244,7 +318,12 @@ __device__ __forceinline__ uint32_t largest(const float (&x)[kLane]) {
 
 __device__ __forceinline__ float root_of(float v) {
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
 
@@ -259,9 +338,12 @@ struct Unit {
   int64_t e0;
   int count;
 
-  __device__ __forceinline__ void load(const Tensor& t, int64_t first) {
+  __device__ __forceinline__ void at(const Tensor& t, int64_t first) {
     e0 = first;
     count = (int)max((int64_t)0, min((int64_t)kLane, t.n - e0));
+  }
+  __device__ __forceinline__ void load(const Tensor& t, int64_t first) {
+    at(t, first);
     const W* pw = static_cast<const W*>(t.W);
     const G* pg = static_cast<const G*>(t.G);
     const S *pm = static_cast<const S*>(t.M), *pv = static_cast<const S*>(t.V);
@@ -282,6 +364,28 @@ struct Unit {
       ev = any ? t.Ev[e0 / kBlock] : 0u;
     }
   }
+  // Through a warp's stage of shared memory: a lane takes what it has fetched itself.
+  static constexpr int g_at() { return 32 * kLane * (int)sizeof(W); }
+  static constexpr int m_at() { return g_at() + 32 * kLane * (int)sizeof(G); }
+  static __device__ __forceinline__ void fetch(const Tensor& t, int64_t e0, uint8_t* stage) {
+    const int lane = threadIdx.x & 31;
+    Raw<W>::fetch(stage + 16 * lane, static_cast<const W*>(t.W) + e0);
+    Raw<G>::fetch(stage + g_at() + 16 * lane, static_cast<const G*>(t.G) + e0);
+    Raw<S>::fetch(stage + m_at() + 8 * lane, static_cast<const S*>(t.M) + e0);
+    Raw<S>::fetch(stage + m_at() + 256 + 8 * lane, static_cast<const S*>(t.V) + e0);
+  }
+  __device__ __forceinline__ void take(const Tensor& t, int64_t first, const uint8_t* stage,
+                                       uint32_t e_m, uint32_t e_v) {
+    const int lane = threadIdx.x & 31;
+    e0 = first;
+    count = kLane;
+    w.take(stage + 16 * lane);
+    g.take(stage + g_at() + 16 * lane);
+    m.take(stage + m_at() + 8 * lane);
+    v.take(stage + m_at() + 256 + 8 * lane);
+    em = e_m;
+    ev = e_v;
+  }
 
   __device__ __forceinline__ void finish(const Tensor& t, uint32_t index, const Step& st) {
     float x[kLane], y[kLane], a[kLane], b[kLane];
@@ -293,28 +397,40 @@ struct Unit {
       unpack(m, a);
       unpack(v, b);
     }
-    const float rate = st.lr / st.c1, spread = rsqrtf(st.c2);
     unpack(w, x);
+    const float2 rate = both(st.now.rate), spread = both(st.now.spread), keep = both(st.keep);
+    const float2 b1 = both(st.b1), c1 = both(st.one_b1), b2 = both(st.b2), c2 = both(st.one_b2);
+    const float2 none = both(st.none);
 #pragma unroll
-    for (int e = 0; e < kLane; ++e) {
-      const float gg = __fmul_rn(y[e], y[e]);
-      if constexpr (kEight) b[e] = __fmul_rn(b[e], b[e]);
-      a[e] = __fadd_rn(__fmul_rn(st.b1, a[e]), __fmul_rn(st.one_b1, y[e]));
-      b[e] = __fadd_rn(__fmul_rn(st.b2, b[e]), __fmul_rn(st.one_b2, gg));
-      y[e] = root_of(b[e]);
-      x[e] = fmaf(st.keep, x[e], -__fdividef(rate * a[e], fmaf(y[e], spread, st.eps)));
+    for (int e = 0; e < kLane; e += 2) {
+      const float2 gr = make_float2(y[e], y[e + 1]);
+      float2 m2 = make_float2(a[e], a[e + 1]), v2 = make_float2(b[e], b[e + 1]);
+      if constexpr (kEight) v2 = zo::mul2(v2, v2);
+      // (products that a sum follows: as fused operations with a zero that the compiler does not
+      // know, or it would fuse the sum instead)
+      m2 = zo::add2(zo::fma2(b1, m2, none), zo::fma2(c1, gr, none));
+      v2 = zo::add2(zo::fma2(b2, v2, none), zo::fma2(c2, zo::mul2(gr, gr), none));
+      const float2 root = make_float2(root_of(v2.x), root_of(v2.y));
+      const float2 den = zo::fma2(root, spread, both(st.eps));
+      const float2 move = zo::mul2(zo::mul2(rate, m2), make_float2(reciprocal(den.x), reciprocal(den.y)));
+      const float2 to = zo::fma2(keep, make_float2(x[e], x[e + 1]), move);
+      x[e] = to.x, x[e + 1] = to.y;
+      y[e] = root.x, y[e + 1] = root.y;
+      a[e] = m2.x, a[e + 1] = m2.y;
+      b[e] = v2.x, b[e + 1] = v2.y;
     }
     pack(x, w);
     if constexpr (kEight) {
       const uint32_t first = __shfl_sync(0xffffffffu, (uint32_t)(count > 0), 0);
-      const uint32_t tm = largest(a), tv = largest(b);
+      bool odd_m, odd_v;
+      const uint32_t tm = largest(a, &odd_m), tv = largest(b, &odd_v);
       // 2^k <= r < 2^(k + 1) where 2^2k <= v < 2^(2k + 2)
       em = tm >> 23;
       ev = tv >> 23 ? (uint32_t)((((int)(tv >> 23) - 127) >> 1) + 127) : 0u;
       const uint4 random = zo::philox4x32_10(
-          make_uint4((uint32_t)(e0 / kLane), index, st.t, kTagAdamW << 24), st.key0, st.key1);
-      encode<true>(a, em, random, m);
-      encode<false>(y, ev, random, v);
+          make_uint4((uint32_t)(e0 / kLane), index, st.now.t, kTagAdamW << 24), st.key0, st.key1);
+      encode<true>(a, em, odd_m, random, m);
+      encode<false>(y, ev, odd_v, random, v);
       if (first && (threadIdx.x & 31) == 0) {
         t.Em[e0 / kBlock] = (uint8_t)em;
         t.Ev[e0 / kBlock] = (uint8_t)ev;
@@ -337,39 +453,69 @@ struct Unit {
   }
 };
 
+// `units` blocks of every warp, kRow elements apart.  In 8 bits, where a block's arithmetic takes
+// as long as its loads, whole blocks of aligned tensors come through shared memory, kStages of
+// them ahead of the arithmetic: with loads into registers 24 warps an SM waited half of their time
+// (131M elements, bf16: 386 us).
 template <bool kEight, typename W, typename G>
-__device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, uint32_t index,
+__device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int units, uint32_t index,
                                           const Step& st) {
-  Unit<kEight, W, G> u[kUnits];
-  const int64_t e0 = first + (int64_t)threadIdx.x * kLane;
+  int64_t e0 = first + (int64_t)threadIdx.x * kLane;
+  int k = 0;
+  Unit<kEight, W, G> u;
+  if constexpr (kEight) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* const mine = ring + warp * kStages * kStageBytes;
+    const int64_t begin = first + (int64_t)warp * kBlock;
+    // this warp's whole blocks
+    const int whole = !t.wide || t.n < begin + kBlock ? 0
+                      : (int)min((int64_t)units, (t.n - begin - kBlock) / kRow + 1);
+    uint32_t em = 0, ev = 0;                     // lane l: of block l
+    if (lane < whole) {
+      const int64_t block = begin / kBlock + (int64_t)lane * (kRow / kBlock);
+      em = t.Em[block];
+      ev = t.Ev[block];
+    }
 #pragma unroll
-  for (int k = 0; k < kUnits; ++k) u[k].load(t, e0 + (int64_t)k * kThreads * kLane);
-#pragma unroll
-  for (int k = 0; k < kUnits; ++k) u[k].finish(t, index, st);
+    for (int q = 0; q < kStages - 1; ++q) {
+      if (q < whole) Unit<kEight, W, G>::fetch(t, e0 + (int64_t)q * kRow, mine + q * kStageBytes);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    for (; k < whole; ++k) {
+      if (k + kStages - 1 < whole)
+        Unit<kEight, W, G>::fetch(t, e0 + (int64_t)(k + kStages - 1) * kRow,
+                                  mine + (k + kStages - 1) % kStages * kStageBytes);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      u.take(t, e0 + (int64_t)k * kRow, mine + k % kStages * kStageBytes,
+             __shfl_sync(0xffffffffu, em, k), __shfl_sync(0xffffffffu, ev, k));
+      u.finish(t, index, st);
+    }
+  }
+  for (; k < units; ++k) {
+    u.load(t, e0 + (int64_t)k * kRow);
+    u.finish(t, index, st);
+  }
 }
 
 // chunks: (tensor, number of the chunk in it)
 template <bool kEight>
-__global__ void __launch_bounds__(kThreads)
-adamw_kernel(const Tensor* __restrict__ tensors, const int2* __restrict__ chunks, Step st,
-             const Counted* __restrict__ counted) {
+__global__ void __launch_bounds__(kThreads, kEight ? kCtas : 4)
+adamw_kernel(const Tensor* __restrict__ tensors, const int2* __restrict__ chunks, int units, Step st,
+             const Now* __restrict__ counted) {
   const int2 at = chunks[blockIdx.x];
   const Tensor t = tensors[at.x];
   zo::pdl_wait();
   zo::pdl_trigger();
-  if (counted) {
-    const Counted c = *counted;
-    st.c1 = c.c1;
-    st.c2 = c.c2;
-    st.t = c.t;
-  }
-  const int64_t first = (int64_t)at.y * kChunk;
+  if (counted) st.now = *counted;
+  const int64_t first = (int64_t)at.y * units * kRow;
   using B = __nv_bfloat16;
   switch (t.kind) {
-    case 0: run_chunk<kEight, float, float>(t, first, (uint32_t)at.x, st); break;
-    case 1: run_chunk<kEight, B, float>(t, first, (uint32_t)at.x, st); break;
-    case 2: run_chunk<kEight, float, B>(t, first, (uint32_t)at.x, st); break;
-    default: run_chunk<kEight, B, B>(t, first, (uint32_t)at.x, st); break;
+    case 0: run_chunk<kEight, float, float>(t, first, units, (uint32_t)at.x, st); break;
+    case 1: run_chunk<kEight, B, float>(t, first, units, (uint32_t)at.x, st); break;
+    case 2: run_chunk<kEight, float, B>(t, first, units, (uint32_t)at.x, st); break;
+    default: run_chunk<kEight, B, B>(t, first, units, (uint32_t)at.x, st); break;
   }
 }
 
@@ -402,7 +548,7 @@ zo_status check_tensors(const zo_adamw_tensor* ts, int32_t n, int32_t bits) {
   for (int32_t i = 0; i < n; ++i) {
     const zo_status st = check_tensor(ts[i], bits);
     if (st != ZO_OK) return st;
-    chunks += (ts[i].m * ts[i].n + kChunk - 1) / kChunk;
+    chunks += (ts[i].m * ts[i].n + kRow - 1) / kRow;
   }
   if (chunks > INT_MAX) return refuse(ZO_ERR_SHAPE, "zo_adamw: too many elements for one context");
   return ZO_OK;
@@ -423,12 +569,20 @@ zo_status check_distinct(const zo_adamw_tensor* ts, int32_t n, int32_t bits) {
 
 struct Layout {
   int64_t tensors_at = 0, chunks_at = 0, bytes = 0, chunks = 0;
+  int32_t units = 1;
 };
 int64_t round_up(int64_t v) { return (v + 255) / 256 * 256; }
-Layout layout(const zo_adamw_tensor* ts, int32_t n) {
+int64_t chunks_of(const zo_adamw_tensor* ts, int32_t n, int64_t units) {
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < n; ++i) chunks += (ts[i].m * ts[i].n + units * kRow - 1) / (units * kRow);
+  return chunks;
+}
+// 8 bits: chunks as long as leave some of them to every CTA that a GPU of 152 SMs holds.
+Layout layout(const zo_adamw_tensor* ts, int32_t n, int32_t bits) {
   Layout L;
-  for (int32_t i = 0; i < n; ++i) L.chunks += (ts[i].m * ts[i].n + kChunk - 1) / kChunk;
-  L.tensors_at = 256;                                      // Counted
+  while (bits == 8 && L.units < kMaxUnits && chunks_of(ts, n, 2 * L.units) >= 4 * 152 * kCtas) L.units *= 2;
+  L.chunks = chunks_of(ts, n, L.units);
+  L.tensors_at = 256;                                      // Now
   L.chunks_at = round_up(L.tensors_at + (int64_t)sizeof(Tensor) * n);
   L.bytes = round_up(L.chunks_at + (int64_t)sizeof(int2) * L.chunks);
   return L;
@@ -449,7 +603,7 @@ struct zo_adamw_ctx {
 extern "C" {
 
 int64_t zo_adamw_workspace(const zo_adamw_tensor* tensors, int32_t n_tensors, int32_t bits) {
-  return check_tensors(tensors, n_tensors, bits) == ZO_OK ? layout(tensors, n_tensors).bytes : 0;
+  return check_tensors(tensors, n_tensors, bits) == ZO_OK ? layout(tensors, n_tensors, bits).bytes : 0;
 }
 
 zo_status zo_adamw_create(zo_adamw_ctx** out, const zo_adamw_tensor* tensors, int32_t n_tensors,
@@ -461,7 +615,7 @@ zo_status zo_adamw_create(zo_adamw_ctx** out, const zo_adamw_tensor* tensors, in
     zo_status st = check_tensors(tensors, n_tensors, bits);
     if (st == ZO_OK) st = check_distinct(tensors, n_tensors, bits);
     if (st != ZO_OK) return st;
-    const Layout L = layout(tensors, n_tensors);
+    const Layout L = layout(tensors, n_tensors, bits);
     if (!workspace || workspace_bytes < L.bytes)
       return refuse(ZO_ERR_INVALID_ARG,
                     "zo_adamw_create: the workspace is missing or smaller than zo_adamw_workspace");
@@ -500,10 +654,8 @@ zo_status zo_adamw_create(zo_adamw_ctx** out, const zo_adamw_tensor* tensors, in
       d.ldg = flat_g ? d.cols : s.ldg;
       d.kind = (s.dtype == ZO_BF16 ? 1 : 0) | (s.grad_dtype == ZO_BF16 ? 2 : 0);
       const auto to16 = [](const void* p) { return aligned16(p); };
-      const auto to8 = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 8 == 0; };
-      d.wide = flat_w && flat_g && to16(s.W) && to16(s.G) &&
-               (bits == 8 ? to8(s.M) && to8(s.V) : to16(s.M) && to16(s.V));
-      for (int64_t k = 0; k * kChunk < d.n; ++k) *chunks++ = make_int2(i, (int)k);
+      d.wide = flat_w && flat_g && to16(s.W) && to16(s.G) && to16(s.M) && to16(s.V);
+      for (int64_t k = 0; k * L.units * kRow < d.n; ++k) *chunks++ = make_int2(i, (int)k);
     }
     ZO_CUDA(cudaMemcpyAsync(c->ws, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream),
             "upload tables");
@@ -532,7 +684,6 @@ zo_status zo_adamw_step(zo_adamw_ctx* c, int64_t t, int64_t* count, double lr, d
     return refuse(ZO_ERR_INVALID_ARG, "zo_adamw_step: need t >= 1, or t = 0 and a count");
   if (reinterpret_cast<uintptr_t>(count) % 8 != 0)
     return refuse(ZO_ERR_ALIGN, "zo_adamw_step: the count is not aligned to its type");
-  // (past half a million steps 1 - 0.99999^t is 1 - 0.0067; its logarithm is what is held)
   if (!std::isfinite(lr) || !std::isfinite(weight_decay) || !(eps >= 0.0) || !std::isfinite(eps) ||
       !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
     return refuse(ZO_ERR_INVALID_ARG,
@@ -545,27 +696,29 @@ zo_status zo_adamw_step(zo_adamw_ctx* c, int64_t t, int64_t* count, double lr, d
   st.b2 = (float)beta2;
   st.one_b2 = (float)(1.0 - beta2);
   st.keep = (float)(1.0 - lr * weight_decay);
-  st.lr = (float)lr;
   st.eps = (float)eps;
+  st.none = -0.0f;
   st.key0 = (uint32_t)c->seed;
   st.key1 = (uint32_t)(c->seed >> 32);
-  auto* counted = reinterpret_cast<Counted*>(c->ws);
+  auto* counted = reinterpret_cast<Now*>(c->ws);
   if (count) {
-    ZO_CUDA(zo::launch_dependent(adamw_count_kernel, 1u, 1, 0, c->stream, 1, true, count, beta1,
-                                 beta2, counted),
+    ZO_CUDA(zo::launch_dependent(adamw_count_kernel, 1u, 1, 0, c->stream, 1, true, count, lr,
+                                 beta1, beta2, counted),
             "AdamW count kernel");
     ++c->launches;
   } else {
-    st.c1 = (float)-std::expm1((double)t * std::log(beta1));
-    st.c2 = (float)-std::expm1((double)t * std::log(beta2));
-    st.t = (uint32_t)t;
+    st.now = now_of(t, lr, beta1, beta2);
   }
   if (c->plan.chunks == 0) return ZO_OK;
   const auto* ts = reinterpret_cast<const Tensor*>(c->ws + c->plan.tensors_at);
   const auto* chunks = reinterpret_cast<const int2*>(c->ws + c->plan.chunks_at);
+  if (c->bits == 8)
+    ZO_CUDA(cudaFuncSetAttribute(adamw_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kRingBytes),
+            "AdamW kernel's shared memory");
   ZO_CUDA(zo::launch_dependent(c->bits == 8 ? adamw_kernel<true> : adamw_kernel<false>,
-                               (unsigned)c->plan.chunks, kThreads, 0, c->stream, 1, true, ts,
-                               chunks, st, count ? counted : nullptr),
+                               (unsigned)c->plan.chunks, kThreads, c->bits == 8 ? kRingBytes : 0,
+                               c->stream, 1, true, ts, chunks, c->plan.units, st, count ? counted : nullptr),
           "AdamW kernel");
   ++c->launches;
   return ZO_OK;

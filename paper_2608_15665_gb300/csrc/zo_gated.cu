@@ -152,7 +152,8 @@ zo_status zo_gated_forward(const void* X, int64_t ldx, int64_t T, int64_t D, con
   a.act = act == ZO_GATED_SILU ? zo::kGatedSilu : zo::kGatedGelu;
   a.save = G != nullptr;
   a.side = zo::gated_side(T, D, F, pairs);
-  if (!map_of(&a.x, X, D, T, ldx, 64, zo::kGatedRows) || !map_of(&a.w[0], Wg, D, F, ldwg, 64, a.side) ||
+  a.box_rows = zo::gated_box_rows(T);
+  if (!map_of(&a.x, X, D, T, ldx, 64, a.box_rows) || !map_of(&a.w[0], Wg, D, F, ldwg, 64, a.side) ||
       !map_of(&a.w[1], Wu, D, F, ldwu, 64, a.side) || !out_map(&a.out[0], H, F, T, ldh) ||
       (G && (!out_map(&a.out[1], G, F, T, ldg) || !out_map(&a.out[2], U, F, T, ldu))))
     return refuse(ZO_ERR_CUDA, "zo_gated_forward: cuTensorMapEncodeTiled rejected a descriptor");
@@ -218,13 +219,14 @@ zo_status zo_gated_backward(const void* dH, int64_t lddh, const void* X, int64_t
   a.T = (int32_t)T;
   a.D = (int32_t)D;
   a.F = (int32_t)F;
+  a.box_rows = zo::gated_box_rows(T);
   const uint16_t* d[2] = {e.dg, e.du};
   const void* w[2] = {Wg, Wu};
   const int64_t ldw[2] = {ldwg, ldwu};
   bool ok = true;
   for (int k = 0; k < 2; ++k) {
     if (dX)
-      ok = ok && map_of(&a.d_rows[k], d[k], F, T, F, 64, zo::kGatedRows) &&
+      ok = ok && map_of(&a.d_rows[k], d[k], F, T, F, 64, a.box_rows) &&
            map_of(&a.w_cols[k], w[k], D, F, ldw[k], 64, 64);
     if (dWg)
       ok = ok && map_of(&a.d_cols[k], d[k], F, T, F, 64, 64) &&

@@ -11,7 +11,11 @@
 //   dWg, dWu: tile = 256 rows of F x 256 columns of D, K = the tokens: both operands MN-major.
 //
 // dX's tiles are the deepest and few: they are dealt to the pairs first, round by round, and dW's
-// tiles in runs of neighbours whose lengths even the pairs' work out (gated_deal), in one launch.
+// behind them in the same launch, the pairs that have no tile in dX's last round beginning as many
+// rounds of dW's earlier as a tile of dX takes.  Neighbouring pairs take neighbouring tiles of
+// one block of F's rows: few panels of dG are in use at a time.  (In runs of neighbours per pair the
+// panels in use, 160 MB at 4096 tokens, came from HBM once for every tile: dWg and dWu of the 7B
+// shapes 525 us.)
 //
 // Bound by the operands' way from L2 to the SMs and the power cap's clock; few tokens by the
 // weights' way from HBM.  Accumulators are fp32 (the tensor cores' sums round towards zero: 2^-23
@@ -125,33 +129,44 @@ __device__ __forceinline__ bool tile_at(const GatedBackward& a, int pair, int pa
     t->dw = -1;
     return true;
   }
-  const int at = a.first[pair] + k - mine;
-  if (at >= a.first[pair + 1]) return false;
+  // dW's rounds: the pairs without a last tile of dX begin `skip` rounds earlier
+  const int late = a.n_dx % pairs, early = pairs - late;
+  const int round = k - mine + (pair < late ? a.skip : 0);
+  const int64_t at = round < a.skip ? (int64_t)round * early + pair - late
+                                    : (int64_t)a.skip * early + (int64_t)(round - a.skip) * pairs + pair;
+  if (at >= a.n_dw) return false;
   const int half = a.n_dw / 2;
   t->dw = at >= half;
-  const int in = at - t->dw * half;
+  const int in = (int)at - t->dw * half;
   t->i0 = in / cols * kTileRows;
   t->j0 = in % cols * kTileCols;
   t->n0 = t->n = (a.T + 63) / 64;
   return true;
 }
 
-// One stage of a tile's operands for CTA `rank`.
+// One stage of a tile's operands for CTA `rank`.  Tokens past the last are not loaded where they
+// fill a CTA's half, or where there are fewer than a box's: what shared memory holds in their place
+// ends in accumulator lanes that nothing reads.
 __device__ __forceinline__ void load_stage(const GatedForward& a, const Tile& t, int k, uint32_t rank,
                                            uint8_t* dst, uint64_t* full, bool leader) {
-  if (leader) mbar_arrive_expect_tx(full, 2u * (kHalfBytes + (uint32_t)a.side * 128u));
-  tma_load_2d_to_leader(dst, &a.x, 64 * k, t.i0 + 128 * (int)rank, full);
+  const bool second = t.i0 + 128 < a.T;
+  if (leader)
+    mbar_arrive_expect_tx(full, ((second ? 2u : 1u) * (uint32_t)a.box_rows + 2u * (uint32_t)a.side) * 128u);
+  if (rank == 0 || second) tma_load_2d_to_leader(dst, &a.x, 64 * k, t.i0 + 128 * (int)rank, full);
   tma_load_2d_to_leader(dst + kHalfBytes, &a.w[rank], 64 * k, t.j0, full);
 }
 __device__ __forceinline__ void load_stage(const GatedBackward& a, const Tile& t, int k, uint32_t rank,
                                            uint8_t* dst, uint64_t* full, bool leader) {
-  if (leader) mbar_arrive_expect_tx(full, 2u * kStageBytes);
+  const bool second = t.dw >= 0 || t.i0 + 128 < a.T;
+  if (leader)
+    mbar_arrive_expect_tx(full, t.dw >= 0 ? 2u * kStageBytes
+                                          : 2u * kHalfBytes + (second ? 2u : 1u) * (uint32_t)a.box_rows * 128u);
   const int i0 = t.i0 + 128 * (int)rank, j0 = t.j0 + 128 * (int)rank;
   const CUtensorMap* b;
   if (t.dw < 0) {
     const int which = k >= t.n0 ? 1 : 0;
     k -= which * t.n0;
-    tma_load_2d_to_leader(dst, &a.d_rows[which], 64 * k, i0, full);
+    if (rank == 0 || second) tma_load_2d_to_leader(dst, &a.d_rows[which], 64 * k, i0, full);
     b = &a.w_cols[which];
   } else {
     tma_load_2d_to_leader(dst, &a.d_cols[t.dw], i0, 64 * k, full);
@@ -445,6 +460,8 @@ int32_t gated_max_pairs() {
   return pairs[dev] = least;
 }
 
+int32_t gated_box_rows(int64_t T) { return (int32_t)std::min<int64_t>(128, (T + 7) / 8 * 8); }
+
 // The busiest pair's cycles: rounds of tiles, each D / 64 stages that take the longer of their
 // MMAs (128 cycles for 16 of K and N = 256) and their operands' way from L2 (~54 bytes a cycle),
 // and one epilogue behind the last.
@@ -469,25 +486,8 @@ void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs) {
   a->n_dw = want_w ? (int32_t)(2 * ceil_div(a->F, kTileRows) * cols) : 0;
   // stages of a tile, with what its beginning costs
   const int64_t deep = 2 * ceil_div(a->F, 64) + 4, flat = ceil_div(a->T, 64) + 4;
-  // the level that the pairs' work fills to: the least one whose room holds all tiles
-  const auto has = [&](int32_t q) { return (int64_t)(a->n_dx > q ? (a->n_dx - q + pairs - 1) / pairs : 0) * deep; };
-  const auto room = [&](int64_t level) {
-    int64_t n = 0;
-    for (int32_t q = 0; q < pairs; ++q) n += std::max<int64_t>(0, (level - has(q)) / flat);
-    return n;
-  };
-  int64_t lo = 0, hi = has(0) + flat * (a->n_dw + 1);
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (room(mid) >= a->n_dw) hi = mid;
-    else lo = mid + 1;
-  }
-  int64_t at = 0;
-  for (int32_t q = 0; q < pairs; ++q) {
-    a->first[q] = (int32_t)at;
-    at = std::min<int64_t>(a->n_dw, at + std::max<int64_t>(0, (lo - has(q)) / flat));
-  }
-  a->first[pairs] = (int32_t)at;
+  const int64_t late = a->n_dx % pairs;
+  a->skip = late == 0 ? 0 : (int32_t)std::min<int64_t>((deep + flat / 2) / flat, ceil_div(a->n_dw, pairs - late));
 }
 
 cudaError_t launch_gated_forward(const GatedForward& a, int32_t pairs, uint32_t* status, cudaStream_t s) {

@@ -170,21 +170,24 @@ struct GatedForward {
   CUtensorMap x, w[2], out[3];      // X; Wg and Wu; H, G and U
   int32_t T, D, F, act, save;
   int32_t side;                     // columns of Wg (and of Wu) to a tile
+  int32_t box_rows;                 // tokens in a box of X
 };
 struct GatedBackward {
   CUtensorMap d_rows[2], w_cols[2], dx;           // dX: dG, dU along F; Wg, Wu by rows of F
   CUtensorMap d_cols[2], x_cols, dw[2];           // dW: dG, dU and X by rows of T
   int32_t T, D, F;
+  int32_t box_rows;                 // tokens in a box of dG's and dU's rows
   int32_t n_dx, n_dw;               // tiles of dX and of both dW (0: not wanted)
-  int32_t first[kGatedMaxPairs + 1];   // pair q takes dW's tiles first[q] .. first[q + 1] - 1
+  int32_t skip;                     // rounds of dW's tiles that take as long as a tile of dX
 };
-// rows of a box of X, and of Wg (Wu); columns and rows of a box of a result
-constexpr int kGatedRows = 128, kGatedOutCols = 16, kGatedOutRows = 32;
+// columns and rows of a box of a result; tokens in a box of an operand: at most a CTA's 128
+constexpr int kGatedOutCols = 16, kGatedOutRows = 32;
+int32_t gated_box_rows(int64_t T);
 // columns of a tile's two halves for this call
 int32_t gated_side(int64_t T, int64_t D, int64_t F, int32_t pairs);
 // SM pairs that run at once, or 0
 int32_t gated_max_pairs();
-// fills n_dx, n_dw and first
+// fills n_dx, n_dw and skip
 void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs);
 cudaError_t launch_gated_forward(const GatedForward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
 cudaError_t launch_gated_backward(const GatedBackward& a, int32_t pairs, uint32_t* status, cudaStream_t s);

@@ -13,11 +13,13 @@
 //
 // The pairs' kernel is launched behind it: a CTA per pair sums its two sequences, in 64 bits,
 // and the one that finishes last adds the losses up, in their order.
+#include <algorithm>
 #include <cmath>
 
 #include <cuda_bf16.h>
 
 #include "../../include/zo.h"
+#include "zo_device.cuh"
 #include "zo_host.h"
 #include "zo_launch.cuh"
 
@@ -25,9 +27,14 @@ namespace {
 
 using namespace zo::host;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+// Small CTAs: one's first loads and last sums lie under the others' (16 pairs, 32000 wide: forward
+// 139 us with 128 threads, 148 with 256, 209 with 512).
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kUnroll = 4;                       // vectors of 16 bytes a thread has on their way
 constexpr int kMaxParts = 32, kPartCols = 4096;  // parts of a row, none narrower than this
+// columns of a CTA's part in the backward pass (812 rows of 50257 fp32: 52 us; in whole rows 58, as 5.3
+// rows an SM are 6 for some)
+constexpr int kGradCols = 8192;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Rows {
@@ -89,10 +96,17 @@ __device__ __forceinline__ void add(Sum& a, const Vec<T> (&v)[kUnroll]) {
   const float c = fmaxf(a.c, top);
   a.s *= exp_of(a.c - c);
   a.c = c;
+  // (two values an instruction, but for the exponentials)
+  const float2 less = make_float2(-c, -c), scale = make_float2(kLog2e, kLog2e);
+  float2 s = make_float2(a.s, 0.0f);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-    for (int i = 0; i < Vec<T>::kN; ++i) a.s += exp_of(v[u].get(i) - c);
+    for (int i = 0; i < Vec<T>::kN; i += 2) {
+      const float2 d = zo::mul2(zo::add2(make_float2(v[u].get(i), v[u].get(i + 1)), less), scale);
+      s = zo::add2(s, make_float2(exp2_approx(d.x), exp2_approx(d.y)));
+    }
+  a.s = s.x + s.y;
 }
 __device__ __forceinline__ void add(Sum& a, float x) {
   const float c = fmaxf(a.c, x);
@@ -107,7 +121,8 @@ __device__ __forceinline__ int head_of(const T* p, int n) {
 }
 
 // The rows' sums.  parts > 1: every part's to partial; else lse and logp.  Rows that do not count
-// get zeros.
+// get zeros.  A CTA per row (part): rows that do not count lie together, and with a fixed number of
+// rows to a CTA the busiest had a third more to read than the others (16 pairs: 190 us).
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 rows_kernel(const Rows a, Sum* __restrict__ partial, float* __restrict__ logp,
@@ -121,15 +136,12 @@ rows_kernel(const Rows a, Sum* __restrict__ partial, float* __restrict__ logp,
   if (row >= a.rows) return;
   const int64_t label = a.labels[row];
   const bool counted = label >= 0 && row >= a.offsets[0] && row < a.offsets[2 * a.pairs];
-  if (!counted) {
-    if (threadIdx.x == 0 && part == 0) {
-      logp[row] = 0.0f;
-      if (lse) lse[row] = 0.0f;
-      if (dlogp) dlogp[row] = 0.0f;
-    }
-    return;
+  if (threadIdx.x == 0 && part == 0) {
+    if (!counted) logp[row] = 0.0f;
+    if (!counted && lse) lse[row] = 0.0f;
+    if (dlogp) dlogp[row] = 0.0f;                // (of counted rows: until the pairs' kernel)
   }
-  if (dlogp && threadIdx.x == 0 && part == 0) dlogp[row] = 0.0f;   // until the pairs' kernel
+  if (!counted) return;
   const int j0 = part * a.part_cols, n = min(a.part_cols, a.vocab - j0);
   const T* x = static_cast<const T*>(a.x) + row * a.ld + j0;
   Sum sum{kLowest, 0.0f};
@@ -479,8 +491,10 @@ zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t rows, 
   a.vocab = (int32_t)vocab;
   a.rows = rows;
   a.labels = labels;
-  set_parts(&a, parts_of(rows, vocab, sms < 256 ? sms : 256));
+  set_parts(&a, (int32_t)std::max<int64_t>(parts_of(rows, vocab, sms), vocab / kGradCols));
   const auto s = reinterpret_cast<cudaStream_t>(stream);
+  if (rows * a.parts > INT32_MAX)
+    return refuse(ZO_ERR_SHAPE, "zo_preference_backward: too many logits for one call");
   const unsigned grid = (unsigned)(rows * a.parts);
   if (dtype == ZO_BF16)
     ZO_CUDA(zo::launch_dependent(gradient_kernel<__nv_bfloat16>, grid, kThreads, 0, s, 1, true, a, lse,

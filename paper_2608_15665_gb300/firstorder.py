@@ -403,8 +403,11 @@ def preference_loss(logits, labels, offsets, ref_logps=None, beta=0.1, kind="sig
     plabels = zb._vector(labels, at, "labels", rows, torch.int64, device)
     poffsets = zb._vector(offsets, at, "offsets", 2 * pairs + 1, torch.int64, device)
     pref = zb._vector(ref_logps, at, "ref_logps", 2 * pairs, _F32, device)
-    loss = _empty((), dtype=_F32, device=device) if out is None else out
-    ploss = zb._one_value(loss, at, "out", device)
+    if out is None:
+        loss = _empty((), dtype=_F32, device=device)
+        ploss = loss.data_ptr()
+    else:
+        loss, ploss = out, zb._one_value(out, at, "out", device)
     losses = _empty(pairs, dtype=_F32, device=device)
     logps = _empty(2 * pairs, dtype=_F32, device=device)
     lse = dlogp = plse = pdlogp = None

@@ -320,3 +320,35 @@ def test_refusals_of_a_step(lib, gpu):
         fo.AdamW([W, W], [G, G])
     torch.cuda.synchronize()
     assert torch.equal(W, before) and opt.steps == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_exponents_are_those_of_sums_of_rounded_products(lib, gpu, dtype):
+    """Codes and bf16 gradients have few digits: the sums often meet a power of two, and then a fused
+    product's other rounding shows in the block's exponent.  Bit for bit against fp32 arithmetic."""
+    from paper_2608_15665_gb300 import firstorder as fo
+    f = np.float32
+    n = 1 << 21
+    g = torch.Generator().manual_seed(3)
+    W = torch.zeros(n, dtype=TYPES[dtype], device=gpu)
+    G = (torch.randn(n, generator=g) * 2.0 ** torch.randint(-12, 12, (n,), generator=g).float())
+    G = G.to(torch.bfloat16).to(TYPES[dtype]).to(gpu)
+    state = fo.adamw_state(W, 8)
+    codes = torch.randint(0, 0x7F, (n,), generator=g, dtype=torch.uint8)
+    state.m.view(torch.uint8).copy_(codes)
+    state.v.view(torch.uint8).copy_(codes.flip(0))
+    for e in (state.m_exp, state.v_exp):
+        e.copy_(torch.randint(115, 140, e.shape, generator=g).to(torch.uint8))
+    m = values(state.m, state.m_exp, (n,)).astype(f)
+    r = values(state.v, state.v_exp, (n,)).astype(f)
+    x = f64(G).astype(f)
+    opt = fo.AdamW([W], [G], [state], bits=8)
+    opt.step(LR, (B1, B2), EPS, WD, t=7)
+    torch.cuda.synchronize()
+    m1 = f(B1) * m + f(1.0 - B1) * x
+    v1 = f(B2) * (r * r) + f(1.0 - B2) * (x * x)
+    top = np.abs(m1).reshape(-1, 256).max(1)
+    em = np.where(top > 0, np.frexp(top)[1] + 126, 0)
+    ev = np.frexp(v1.reshape(-1, 256).max(1))[1] - 1
+    assert np.array_equal(state.m_exp.cpu().numpy(), em)
+    assert np.array_equal(state.v_exp.cpu().numpy(), (ev >> 1) + 127)
