@@ -591,8 +591,8 @@ ZO_API zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t
  *     dG = rnd(dH U act'(G)),  dU = rnd(dH act(G)),
  *     dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X.
  *   NULL = not wanted: dX (then Wg and Wu are not read), or both of dWg and dWu (then X is not).
- *   workspace: caller-owned device memory of at least zo_gated_workspace(T, F) bytes, 16-byte
- *   aligned, for dG and dU; calls whose work overlaps need one each.
+ *   workspace: caller-owned device memory of at least zo_gated_workspace(T, D, F) bytes,
+ *   16-byte aligned, for dG, dU and parts of sums; calls whose work overlaps need one each.
  * act: ZO_GATED_SILU g sig(g), or ZO_GATED_GELU_TANH g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))).
  * Every matrix is 16-byte aligned and its row stride (ldx, ... in elements) a multiple of 8; D and
  * F are multiples of 8, T is any number from 0 on (no tokens: dWg and dWu are zero).  Outputs must
@@ -608,7 +608,7 @@ ZO_API zo_status zo_gated_forward(const void* X, int64_t ldx, int64_t T, int64_t
                                   int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F,
                                   int32_t act, void* H, int64_t ldh, void* G, int64_t ldg, void* U,
                                   int64_t ldu, void* stream);
-ZO_API int64_t zo_gated_workspace(int64_t T, int64_t F);
+ZO_API int64_t zo_gated_workspace(int64_t T, int64_t D, int64_t F);
 ZO_API zo_status zo_gated_backward(const void* dH, int64_t lddh, const void* X, int64_t ldx,
                                    int64_t T, int64_t D, const void* Wg, int64_t ldwg,
                                    const void* Wu, int64_t ldwu, int64_t F, int32_t act,

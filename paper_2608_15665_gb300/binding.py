@@ -182,7 +182,7 @@ _SIGNATURES = {
                                       _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int32,
                                       _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
                                       _c.c_void_p, _c.c_int64, _c.c_void_p]),
-    "zo_gated_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64]),
+    "zo_gated_workspace": (_c.c_int64, [_c.c_int64, _c.c_int64, _c.c_int64]),
     "zo_gated_backward": (_c.c_int32, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64,
                                        _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
                                        _c.c_int64, _c.c_int32, _c.c_void_p, _c.c_int64, _c.c_void_p,
@@ -726,15 +726,15 @@ def zo_gated_forward(X, Wg, Wu, act, H, G=None, U=None, stream=None):
                                 *outs[2], _stream_handle(stream)), at)
 
 
-def zo_gated_workspace(T, F):
+def zo_gated_workspace(T, D, F):
     """Bytes of workspace that zo_gated_backward needs."""
-    return int(LIB.zo_gated_workspace(int(T), int(F)))
+    return int(LIB.zo_gated_workspace(int(T), int(D), int(F)))
 
 
 def zo_gated_backward(dH, X, Wg, Wu, act, G, U, dX=None, dWg=None, dWu=None, workspace=None,
                       stream=None):
     """dX, dWg and dWu of zo_gated_forward (see include/zo.h).  workspace: a contiguous uint8
-    tensor of zo_gated_workspace(T, F) bytes."""
+    tensor of zo_gated_workspace(T, D, F) bytes."""
     import torch
     at = "zo_gated_backward"
     px, ldx = _gated_matrix(X, at, "X", None, None)

@@ -14,8 +14,8 @@
 // binades, v's spread is twice that of r.  Codes are rounded up or down at random, by 16 bits of
 // the Philox stream an element, as v moves by a thousandth of itself a step and the codes are an
 // eighth apart: to nearest, a running mean would never move.  The expectation is the running
-// mean's; its noise is (1 - b2) / 2 x 1/8 of r^2 a step in variance, ~9% of r where the gradients'
-// squares vary by about their mean.  m and r take the same bits: the two errors are not used
+// mean's; its noise settles where what a step adds, |dr| times a code's distance, is what the mean
+// forgets: about 15% of r for Gaussian gradients and b2 = 0.999.  m and r take the same bits: the two errors are not used
 // together.  A root above zero keeps a code above zero, or m / eps would be taken as the update.
 // The moments' sums are products and sums each rounded on its own: the exponents are then the
 // same as those of any other fp32 evaluation in this order.
@@ -43,13 +43,13 @@ namespace {
 using namespace zo::host;
 
 constexpr uint32_t kTagAdamW = 6;
-constexpr int kThreads = 256, kLane = 8;
+constexpr int kThreads = 128, kLane = 8;
 constexpr int kBlock = 32 * kLane;               // elements of a power of two
 constexpr int kRow = kThreads * kLane;           // a block of every warp
-constexpr int kMaxUnits = 8;                    // such rows of a chunk, at most
-constexpr int kCtas = 3;                         // of an SM
+constexpr int kMaxUnits = 8;                     // such rows of a chunk, at most
+constexpr int kCtas = 7;                         // of an SM
 // 8 bits: a warp's ring of blocks in shared memory (W and G in fp32 at most)
-constexpr int kStages = 3, kStageBytes = kBlock * 10;
+constexpr int kStages = 2, kStageBytes = kBlock * 10;
 constexpr int kRingBytes = kThreads / 32 * kStages * kStageBytes;
 static_assert(kCtas * kRingBytes <= 227 * 1024, "shared memory per SM");
 static_assert(kBlock == 256 && kRow % kBlock == 0 && kMaxUnits <= 32, "a chunk is whole blocks");
@@ -72,12 +72,22 @@ struct Now {                                     // what goes by the step's numb
 struct Step {
   float b1, one_b1, b2, one_b2, keep, eps;
   float none;                                    // -0: what a product is added to
-  Now now;
-  uint32_t key0, key1;
+  uint32_t key[20];                              // of Philox's rounds
 };
 __host__ __device__ inline Now now_of(int64_t t, double lr, double b1, double b2) {
   return Now{(float)(lr / expm1((double)t * log(b1))),
              (float)(1.0 / sqrt(-expm1((double)t * log(b2)))), (uint32_t)t};
+}
+
+// Philox4x32-10 of zo_device.cuh with the rounds' keys given: they are the same for all threads.
+__device__ __forceinline__ uint4 random_words(uint4 c, const uint32_t (&key)[20]) {
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t a = (uint64_t)0xD2511F53u * c.x, b = (uint64_t)0xCD9E8D57u * c.z;
+    c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ key[2 * r], (uint32_t)b,
+                   (uint32_t)(a >> 32) ^ c.w ^ key[2 * r + 1], (uint32_t)a);
+  }
+  return c;
 }
 
 // One more step: its number and bias corrections.
@@ -387,7 +397,7 @@ struct Unit {
     ev = e_v;
   }
 
-  __device__ __forceinline__ void finish(const Tensor& t, uint32_t index, const Step& st) {
+  __device__ __forceinline__ void finish(const Tensor& t, uint32_t index, const Step& st, const Now& now) {
     float x[kLane], y[kLane], a[kLane], b[kLane];
     unpack(g, y);
     if constexpr (kEight) {
@@ -398,7 +408,7 @@ struct Unit {
       unpack(v, b);
     }
     unpack(w, x);
-    const float2 rate = both(st.now.rate), spread = both(st.now.spread), keep = both(st.keep);
+    const float2 rate = both(now.rate), spread = both(now.spread), keep = both(st.keep);
     const float2 b1 = both(st.b1), c1 = both(st.one_b1), b2 = both(st.b2), c2 = both(st.one_b2);
     const float2 none = both(st.none);
 #pragma unroll
@@ -427,8 +437,8 @@ struct Unit {
       // 2^k <= r < 2^(k + 1) where 2^2k <= v < 2^(2k + 2)
       em = tm >> 23;
       ev = tv >> 23 ? (uint32_t)((((int)(tv >> 23) - 127) >> 1) + 127) : 0u;
-      const uint4 random = zo::philox4x32_10(
-          make_uint4((uint32_t)(e0 / kLane), index, st.now.t, kTagAdamW << 24), st.key0, st.key1);
+      const uint4 random = random_words(
+          make_uint4((uint32_t)(e0 / kLane), index, now.t, kTagAdamW << 24), st.key);
       encode<true>(a, em, odd_m, random, m);
       encode<false>(y, ev, odd_v, random, v);
       if (first && (threadIdx.x & 31) == 0) {
@@ -454,12 +464,13 @@ struct Unit {
 };
 
 // `units` blocks of every warp, kRow elements apart.  In 8 bits, where a block's arithmetic takes
-// as long as its loads, whole blocks of aligned tensors come through shared memory, kStages of
-// them ahead of the arithmetic: with loads into registers 24 warps an SM waited half of their time
-// (131M elements, bf16: 386 us).
+// as long as its loads, whole blocks of aligned tensors come through shared memory, the next one's
+// loads under this one's arithmetic: with loads into registers 24 warps an SM waited half of their
+// time (131M elements, bf16: 386 us; through shared memory 247 with three blocks ahead and 24 warps,
+// 229 with two and 28).
 template <bool kEight, typename W, typename G>
 __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int units, uint32_t index,
-                                          const Step& st) {
+                                          const Step& st, const Now& now) {
   int64_t e0 = first + (int64_t)threadIdx.x * kLane;
   int k = 0;
   Unit<kEight, W, G> u;
@@ -490,32 +501,32 @@ __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int un
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       u.take(t, e0 + (int64_t)k * kRow, mine + k % kStages * kStageBytes,
              __shfl_sync(0xffffffffu, em, k), __shfl_sync(0xffffffffu, ev, k));
-      u.finish(t, index, st);
+      u.finish(t, index, st, now);
     }
   }
   for (; k < units; ++k) {
     u.load(t, e0 + (int64_t)k * kRow);
-    u.finish(t, index, st);
+    u.finish(t, index, st, now);
   }
 }
 
 // chunks: (tensor, number of the chunk in it)
 template <bool kEight>
-__global__ void __launch_bounds__(kThreads, kEight ? kCtas : 4)
-adamw_kernel(const Tensor* __restrict__ tensors, const int2* __restrict__ chunks, int units, Step st,
-             const Now* __restrict__ counted) {
+__global__ void __launch_bounds__(kThreads, kEight ? kCtas : 8)
+adamw_kernel(const Tensor* __restrict__ tensors, const int2* __restrict__ chunks, int units,
+             const __grid_constant__ Step st, Now now, const Now* __restrict__ counted) {
   const int2 at = chunks[blockIdx.x];
   const Tensor t = tensors[at.x];
   zo::pdl_wait();
   zo::pdl_trigger();
-  if (counted) st.now = *counted;
+  if (counted) now = *counted;
   const int64_t first = (int64_t)at.y * units * kRow;
   using B = __nv_bfloat16;
   switch (t.kind) {
-    case 0: run_chunk<kEight, float, float>(t, first, units, (uint32_t)at.x, st); break;
-    case 1: run_chunk<kEight, B, float>(t, first, units, (uint32_t)at.x, st); break;
-    case 2: run_chunk<kEight, float, B>(t, first, units, (uint32_t)at.x, st); break;
-    default: run_chunk<kEight, B, B>(t, first, units, (uint32_t)at.x, st); break;
+    case 0: run_chunk<kEight, float, float>(t, first, units, (uint32_t)at.x, st, now); break;
+    case 1: run_chunk<kEight, B, float>(t, first, units, (uint32_t)at.x, st, now); break;
+    case 2: run_chunk<kEight, float, B>(t, first, units, (uint32_t)at.x, st, now); break;
+    default: run_chunk<kEight, B, B>(t, first, units, (uint32_t)at.x, st, now); break;
   }
 }
 
@@ -698,16 +709,19 @@ zo_status zo_adamw_step(zo_adamw_ctx* c, int64_t t, int64_t* count, double lr, d
   st.keep = (float)(1.0 - lr * weight_decay);
   st.eps = (float)eps;
   st.none = -0.0f;
-  st.key0 = (uint32_t)c->seed;
-  st.key1 = (uint32_t)(c->seed >> 32);
+  for (uint32_t r = 0; r < 10; ++r) {
+    st.key[2 * r] = (uint32_t)c->seed + r * 0x9E3779B9u;
+    st.key[2 * r + 1] = (uint32_t)(c->seed >> 32) + r * 0xBB67AE85u;
+  }
   auto* counted = reinterpret_cast<Now*>(c->ws);
+  Now now{};
   if (count) {
     ZO_CUDA(zo::launch_dependent(adamw_count_kernel, 1u, 1, 0, c->stream, 1, true, count, lr,
                                  beta1, beta2, counted),
             "AdamW count kernel");
     ++c->launches;
   } else {
-    st.now = now_of(t, lr, beta1, beta2);
+    now = now_of(t, lr, beta1, beta2);
   }
   if (c->plan.chunks == 0) return ZO_OK;
   const auto* ts = reinterpret_cast<const Tensor*>(c->ws + c->plan.tensors_at);
@@ -718,7 +732,7 @@ zo_status zo_adamw_step(zo_adamw_ctx* c, int64_t t, int64_t* count, double lr, d
             "AdamW kernel's shared memory");
   ZO_CUDA(zo::launch_dependent(c->bits == 8 ? adamw_kernel<true> : adamw_kernel<false>,
                                (unsigned)c->plan.chunks, kThreads, c->bits == 8 ? kRingBytes : 0,
-                               c->stream, 1, true, ts, chunks, c->plan.units, st, count ? counted : nullptr),
+                               c->stream, 1, true, ts, chunks, c->plan.units, st, now, count ? counted : nullptr),
           "AdamW kernel");
   ++c->launches;
   return ZO_OK;

@@ -44,6 +44,8 @@ struct Gradients {
   int64_t lddh, ldg, ldu;
   uint32_t vectors, per_row;          // of 8 elements
   int32_t act;
+  uint32_t* counters;                 // of the products' split tiles: zero before them
+  uint32_t n_counters;
 };
 
 __device__ __forceinline__ float value(const uint4& v, int i) {
@@ -65,6 +67,7 @@ __global__ void __launch_bounds__(kThreads) gated_gradients_kernel(const Gradien
   const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
   zo::pdl_wait();
   zo::pdl_trigger();
+  for (uint32_t i = at; i < a.n_counters; i += gridDim.x * kThreads) a.counters[i] = 0;
   if (at >= a.vectors) return;
   const int64_t row = at / a.per_row, col = 8 * (int64_t)(at % a.per_row);
   const uint4 dh = __ldcs(reinterpret_cast<const uint4*>(a.dh + row * a.lddh + col));
@@ -124,7 +127,22 @@ bool out_map(CUtensorMap* m, void* p, int64_t cols, int64_t rows, int64_t ld) {
   return map_of(m, p, cols, rows, ld, zo::kGatedOutCols, zo::kGatedOutRows, CU_TENSOR_MAP_SWIZZLE_32B);
 }
 
-int64_t gradient_bytes(int64_t T, int64_t F) { return (T * F * 2 + 255) / 256 * 256; }
+int64_t round_up(int64_t v) { return (v + 255) / 256 * 256; }
+int64_t gradient_bytes(int64_t T, int64_t F) { return round_up(T * F * 2); }
+
+// The workspace: dG, dU, then what the split tiles of dX take.
+struct Layout {
+  int64_t sums_at, counters_at, counters, bytes;
+};
+Layout layout(int64_t T, int64_t D, int64_t F) {
+  const int64_t parts = zo::gated_parts(T, D, F), tiles = parts > 1 ? zo::gated_dx_tiles(T, D) : 0;
+  Layout L;
+  L.sums_at = 2 * gradient_bytes(T, F);
+  L.counters_at = L.sums_at + tiles * parts * zo::kGatedPartFloats * (int64_t)sizeof(float);
+  L.counters = tiles * zo::kGatedCounters;
+  L.bytes = L.counters_at + round_up(L.counters * (int64_t)sizeof(uint32_t));
+  return L;
+}
 
 }  // namespace
 
@@ -162,8 +180,8 @@ zo_status zo_gated_forward(const void* X, int64_t ldx, int64_t T, int64_t D, con
   return ZO_OK;
 }
 
-int64_t zo_gated_workspace(int64_t T, int64_t F) {
-  return check_sizes(T, 8, F, ZO_GATED_SILU) == ZO_OK ? 2 * gradient_bytes(T, F) : 0;
+int64_t zo_gated_workspace(int64_t T, int64_t D, int64_t F) {
+  return check_sizes(T, D, F, ZO_GATED_SILU) == ZO_OK && T > 0 ? layout(T, D, F).bytes : 0;
 }
 
 zo_status zo_gated_backward(const void* dH, int64_t lddh, const void* X, int64_t ldx, int64_t T,
@@ -195,9 +213,10 @@ zo_status zo_gated_backward(const void* dH, int64_t lddh, const void* X, int64_t
   if (st == ZO_OK && dWg) st = check_buffers(x, 1);
   if (st == ZO_OK && dX) st = check_buffers(x + 1, 1);
   if (st != ZO_OK) return st;
-  if (!workspace || workspace_bytes < zo_gated_workspace(T, F))
+  const Layout L = layout(T, D, F);
+  if (!workspace || workspace_bytes < L.bytes)
     return refuse(ZO_ERR_INVALID_ARG, "zo_gated_backward: the workspace is missing or smaller than "
-                                      "zo_gated_workspace(T, F)");
+                                      "zo_gated_workspace(T, D, F)");
   if (!aligned16(workspace))
     return refuse(ZO_ERR_ALIGN, "zo_gated_backward: the workspace must be 16-byte aligned");
   const int32_t pairs = zo::gated_max_pairs();
@@ -215,7 +234,12 @@ zo_status zo_gated_backward(const void* dH, int64_t lddh, const void* X, int64_t
   e.per_row = (uint32_t)(F / 8);
   e.vectors = (uint32_t)(T * (F / 8));
   e.act = act == ZO_GATED_SILU ? zo::kGatedSilu : zo::kGatedGelu;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  e.counters = reinterpret_cast<uint32_t*>(ws + L.counters_at);
+  e.n_counters = (uint32_t)L.counters;
   zo::GatedBackward a{};
+  a.sums = reinterpret_cast<float*>(ws + L.sums_at);
+  a.counters = e.counters;
   a.T = (int32_t)T;
   a.D = (int32_t)D;
   a.F = (int32_t)F;

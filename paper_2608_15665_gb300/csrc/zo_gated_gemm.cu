@@ -10,7 +10,7 @@
 //             instruction descriptor's transpose bit), so no transposed copy is kept.
 //   dWg, dWu: tile = 256 rows of F x 256 columns of D, K = the tokens: both operands MN-major.
 //
-// dX's tiles are the deepest and few: they are dealt to the pairs first, round by round, and dW's
+// dX's tiles are the deepest and few (where very few, K is split: gated_parts): they are dealt to the pairs first, round by round, and dW's
 // behind them in the same launch, the pairs that have no tile in dX's last round beginning as many
 // rounds of dW's earlier as a tile of dX takes.  Neighbouring pairs take neighbouring tiles of
 // one block of F's rows: few panels of dG are in use at a time.  (In runs of neighbours per pair the
@@ -98,8 +98,10 @@ constexpr uint32_t kMnMajorA = 1u << 15, kMnMajorB = 1u << 16;
 // A pair's tiles in their order, the same for every role.
 struct Tile {
   int i0, j0;                    // first row and column of the result
-  int n0, n;                     // stages of 64 of K: of the first operands, and all
+  int k0, n;                     // its stages of 64 of K: the first, and their number
+  int n0;                        // stages of the first operands (dX)
   int dw;                        // -1: forward or dX; 0, 1: dWg, dWu
+  int at, part;                  // dX's tile, and which part of its K
 };
 __device__ __forceinline__ bool tile_at(const GatedForward& a, int pair, int pairs, int k, Tile* t) {
   // groups of 16 blocks of tokens; within one, the tokens first: the pairs at work share few
@@ -111,6 +113,7 @@ __device__ __forceinline__ bool tile_at(const GatedForward& a, int pair, int pai
   const int height = min(16, rows - 16 * group);
   t->i0 = (16 * group + in % height) * kTileRows;
   t->j0 = in / height * a.side;
+  t->k0 = 0;
   t->n0 = t->n = (a.D + 63) / 64;
   t->dw = -1;
   return true;
@@ -119,13 +122,17 @@ __device__ __forceinline__ bool tile_at(const GatedBackward& a, int pair, int pa
   const int cols = (a.D + kTileCols - 1) / kTileCols;
   const int mine = a.n_dx > pair ? (a.n_dx - pair + pairs - 1) / pairs : 0;
   if (k < mine) {
-    const int at = pair + k * pairs, rows = (a.T + kTileRows - 1) / kTileRows;
+    const int item = pair + k * pairs, rows = (a.T + kTileRows - 1) / kTileRows;
+    const int at = item / a.parts;
     const int group = at / (16 * cols), in = at - group * 16 * cols;
     const int height = min(16, rows - 16 * group);
     t->i0 = (16 * group + in % height) * kTileRows;
     t->j0 = in / height * kTileCols;
     t->n0 = (a.F + 63) / 64;
-    t->n = 2 * t->n0;
+    t->at = at;
+    t->part = item - at * a.parts;
+    t->k0 = 2 * t->n0 * t->part / a.parts;
+    t->n = 2 * t->n0 * (t->part + 1) / a.parts - t->k0;
     t->dw = -1;
     return true;
   }
@@ -140,6 +147,7 @@ __device__ __forceinline__ bool tile_at(const GatedBackward& a, int pair, int pa
   const int in = (int)at - t->dw * half;
   t->i0 = in / cols * kTileRows;
   t->j0 = in % cols * kTileCols;
+  t->k0 = 0;
   t->n0 = t->n = (a.T + 63) / 64;
   return true;
 }
@@ -223,7 +231,7 @@ __device__ __forceinline__ void to_floats(const uint32_t (&r)[16], float (&v)[16
 
 // The accumulator at `tmem` (this warp's lanes) to the results: 32 rows from row0 on.
 __device__ __forceinline__ void finish(const GatedForward& a, const Tile& t, uint32_t tmem, int half,
-                                       int row0, Boxes& boxes) {
+                                       int row0, int, Boxes& boxes) {
   for (int c = half; c < a.side / 16; c += 2) {
     const int col = t.j0 + 16 * c;
     if (row0 >= a.T || col >= a.F) break;
@@ -248,24 +256,55 @@ __device__ __forceinline__ void finish(const GatedForward& a, const Tile& t, uin
     }
   }
 }
+// warp: of the pair's sixteen.  Of a tile whose K is split, each warp leaves its part's sums in
+// memory (32 lanes apart for coalescing), and the last part's adds them up in the parts' order.
 __device__ __forceinline__ void finish(const GatedBackward& a, const Tile& t, uint32_t tmem, int half,
-                                       int row0, Boxes& boxes) {
+                                       int row0, int warp, Boxes& boxes) {
+  constexpr int kChunks = kTileCols / 32;             // of a warp
   const CUtensorMap* to = t.dw < 0 ? &a.dx : &a.dw[t.dw];
-  const int rows = t.dw < 0 ? a.T : a.F;
+  const int rows = t.dw < 0 ? a.T : a.F, lane = threadIdx.x & 31;
+  if (row0 >= rows) return;
+  const bool split = t.dw < 0 && a.parts > 1;
+  const float* from = nullptr;
+  if (split) {
+    constexpr int kOwn = 32 * 16 * kChunks;
+    float* first = a.sums + (int64_t)t.at * a.parts * kGatedPartFloats + warp * kOwn + lane;
+    float* mine = first + t.part * kGatedPartFloats;
 #pragma unroll 1
-  for (int c = half; c < kTileCols / 16; c += 4) {
-    if (row0 >= rows || t.j0 + 16 * c >= a.D) break;
-    uint32_t r[2][16];
-    tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * c), r[0]);
-    tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * c + 32), r[1]);
-    tmem_ld_wait();
-    float v[16];
-    to_floats(r[0], v);
-    boxes.store(v, to, t.j0 + 16 * c, row0);
-    if (t.j0 + 16 * c + 32 < a.D) {
-      to_floats(r[1], v);
-      boxes.store(v, to, t.j0 + 16 * c + 32, row0);
+    for (int i = 0; i < kChunks; ++i) {
+      if (t.j0 + 16 * (half + 2 * i) >= a.D) break;
+      uint32_t r[16];
+      tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * (half + 2 * i)), r);
+      tmem_ld_wait();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mine[(i * 16 + e) * 32] = __uint_as_float(r[e]);
     }
+    __threadfence();
+    __syncwarp();
+    uint32_t seen = 0;
+    if (lane == 0) seen = atomicAdd(a.counters + t.at * kGatedCounters + warp, 1u);
+    if (__shfl_sync(0xffffffffu, seen, 0) != (uint32_t)a.parts - 1) return;
+    __threadfence();
+    from = first;
+  }
+#pragma unroll 1
+  for (int i = 0; i < kChunks; ++i) {
+    const int c = half + 2 * i;
+    if (t.j0 + 16 * c >= a.D) break;
+    float v[16];
+    if (split) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = __ldcg(from + (i * 16 + e) * 32);
+      for (int p = 1; p < a.parts; ++p)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] += __ldcg(from + p * kGatedPartFloats + (i * 16 + e) * 32);
+    } else {
+      uint32_t r[16];
+      tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * c), r);
+      tmem_ld_wait();
+      to_floats(r, v);
+    }
+    boxes.store(v, to, t.j0 + 16 * c, row0);
   }
 }
 
@@ -315,7 +354,7 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
           ok = false;
           break;
         }
-        if (elected()) load_stage(a, t, q, rank, smem + stage * kStageBytes, &sh.full[stage], leader);
+        if (elected()) load_stage(a, t, t.k0 + q, rank, smem + stage * kStageBytes, &sh.full[stage], leader);
         __syncwarp();
         ++filled;
         if (++stage == kStages) {
@@ -397,7 +436,7 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
       }
       tc_fence_after();
       finish(a, t, tmem + ((uint32_t)(32 * g) << 16) + (uint32_t)(acc * kTileCols), half,
-             t.i0 + 128 * (int)rank + 32 * g, boxes);
+             t.i0 + 128 * (int)rank + 32 * g, (int)rank * kEpiWarps + warp - 2, boxes);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) arrive_leader(&sh.acc_empty[acc]);
@@ -480,12 +519,23 @@ int32_t gated_side(int64_t T, int64_t D, int64_t F, int32_t pairs) {
   return best;
 }
 
+int64_t gated_dx_tiles(int64_t T, int64_t D) { return ceil_div(T, kTileRows) * ceil_div(D, kTileCols); }
+
+int32_t gated_parts(int64_t T, int64_t D, int64_t F) {
+  constexpr int64_t kPairs = 76;
+  const int64_t tiles = gated_dx_tiles(T, D), stages = 2 * ceil_div(F, 64);
+  int32_t parts = 1;
+  while (2 * parts <= kGatedMaxParts && 2 * parts * tiles <= kPairs && 16 * parts <= stages) parts *= 2;
+  return parts;
+}
+
 void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs) {
   const int64_t cols = ceil_div(a->D, kTileCols);
-  a->n_dx = want_x ? (int32_t)(ceil_div(a->T, kTileRows) * cols) : 0;
+  a->parts = gated_parts(a->T, a->D, a->F);
+  a->n_dx = want_x ? (int32_t)(gated_dx_tiles(a->T, a->D) * a->parts) : 0;
   a->n_dw = want_w ? (int32_t)(2 * ceil_div(a->F, kTileRows) * cols) : 0;
   // stages of a tile, with what its beginning costs
-  const int64_t deep = 2 * ceil_div(a->F, 64) + 4, flat = ceil_div(a->T, 64) + 4;
+  const int64_t deep = 2 * ceil_div(a->F, 64) / a->parts + 4, flat = ceil_div(a->T, 64) + 4;
   const int64_t late = a->n_dx % pairs;
   a->skip = late == 0 ? 0 : (int32_t)std::min<int64_t>((deep + flat / 2) / flat, ceil_div(a->n_dw, pairs - late));
 }

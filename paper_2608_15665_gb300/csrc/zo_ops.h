@@ -177,7 +177,10 @@ struct GatedBackward {
   CUtensorMap d_cols[2], x_cols, dw[2];           // dW: dG, dU and X by rows of T
   int32_t T, D, F;
   int32_t box_rows;                 // tokens in a box of dG's and dU's rows
-  int32_t n_dx, n_dw;               // tiles of dX and of both dW (0: not wanted)
+  int32_t n_dx, n_dw;               // tiles of dX, times parts, and of both dW (0: not wanted)
+  int32_t parts;                    // of the K of a tile of dX
+  float* sums;                      // parts > 1: kGatedPartFloats of every part of every tile,
+  uint32_t* counters;               // and kGatedCounters of every tile, zero before the launch
   int32_t skip;                     // rounds of dW's tiles that take as long as a tile of dX
 };
 // columns and rows of a box of a result; tokens in a box of an operand: at most a CTA's 128
@@ -187,7 +190,14 @@ int32_t gated_box_rows(int64_t T);
 int32_t gated_side(int64_t T, int64_t D, int64_t F, int32_t pairs);
 // SM pairs that run at once, or 0
 int32_t gated_max_pairs();
-// fills n_dx, n_dw and skip
+// Parts of the K of dX's tiles: where the tiles leave half of a GB300's SM pairs or more without one,
+// as many as they have room for, each of eight stages at least.  By the sizes alone: the sums' order
+// does not depend on the device.
+constexpr int kGatedMaxParts = 8, kGatedCounters = 16;
+constexpr int64_t kGatedPartFloats = 256 * 256;
+int64_t gated_dx_tiles(int64_t T, int64_t D);
+int32_t gated_parts(int64_t T, int64_t D, int64_t F);
+// fills n_dx, n_dw, parts and skip
 void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs);
 cudaError_t launch_gated_forward(const GatedForward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
 cudaError_t launch_gated_backward(const GatedBackward& a, int32_t pairs, uint32_t* status, cudaStream_t s);

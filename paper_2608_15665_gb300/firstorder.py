@@ -532,7 +532,7 @@ def gated_linear_backward(dh, x, w_gate, w_up, gate, up, act="silu", want_x=True
     if want_weights:
         dwg, dwu = (_empty((F, D), dtype=_BF16, device=device) for _ in range(2))
         pdwg, pdwu = dwg.data_ptr(), dwu.data_ptr()
-    ws_bytes = zb.LIB.zo_gated_workspace(T, F)
+    ws_bytes = zb.LIB.zo_gated_workspace(T, D, F)
     ws = _empty(ws_bytes, dtype=torch.uint8, device=device)
     _call(zb.LIB.zo_gated_backward, dev, at, *ins[0], *px, T, D, *pg, *pu, F, code, *ins[1], *ins[2],
           pdx, D, pdwg, D, pdwu, D, ws.data_ptr(), ws_bytes)

@@ -93,7 +93,7 @@ def check_backward(got, dh, x, wg, wu, gate_, up, act):
 
 SHAPES = [(1, 8, 8), (1, 64, 64), (3, 72, 200), (2, 520, 1000), (16, 256, 264), (17, 128, 2056),
           (128, 264, 96), (129, 136, 512), (255, 64, 16), (256, 512, 128), (300, 200, 1000),
-          (1000, 1024, 2816), (2500, 72, 2000), (5000, 64, 520), (700, 8, 4104), (40, 4096, 304)]
+          (1000, 1024, 2816), (2500, 72, 2000), (5000, 64, 520), (700, 8, 4104), (40, 4096, 304), (77, 600, 3000)]
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
@@ -129,7 +129,7 @@ def test_results_in_rows_further_apart_leave_what_lies_between(lib, gpu):
     s = torch.cuda.current_stream()
     lib.zo_gated_forward(x, wg, wu, 0, v["H"], v["G"], v["U"], stream=s)
     dh = make(T, F, gpu, 4, 0.1, pad)
-    ws = torch.empty(lib.zo_gated_workspace(T, F), dtype=torch.uint8, device=gpu)
+    ws = torch.empty(lib.zo_gated_workspace(T, D, F), dtype=torch.uint8, device=gpu)
     lib.zo_gated_backward(dh, x, wg, wu, 0, v["G"], v["U"], v["dX"], v["dWg"], v["dWu"], ws, stream=s)
     check_backward((v["dX"], v["dWg"], v["dWu"]), dh, x, wg, wu, v["G"], v["U"], "silu")
     for n, t in outs.items():
