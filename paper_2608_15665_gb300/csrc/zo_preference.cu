@@ -35,7 +35,9 @@ constexpr int kMaxParts = 32, kPartCols = 4096;  // parts of a row, none narrowe
 // columns of a CTA's part in the backward pass (812 rows of 50257 fp32: 52 us; in whole rows 58, as 5.3
 // rows an SM are 6 for some)
 constexpr int kGradCols = 8192;
-constexpr float kLog2e = 1.4426950408889634f;
+// log2 e in two parts: rounded once it is off by 1.3e-8, which at the logits' usual distance from their
+// sum moves every row's lse by 1e-7 the same way, and a sequence's sum by that for each row
+constexpr float kLog2e = 1.4426950216293335f, kLog2eLo = 1.9259629e-8f;
 
 struct Rows {
   const void* x;
@@ -59,10 +61,12 @@ struct Sum {
   float c, s;
 };
 constexpr float kLowest = -3.402823466e38f;
-__device__ __forceinline__ float exp_of(float x) { return exp2_approx(x * kLog2e); }
+__device__ __forceinline__ float exp_of(float x) { return exp2_approx(fmaf(x, kLog2e, x * kLog2eLo)); }
+// (The hardware's exponential is 5e-8 low on average at negative arguments: once in a term, not again
+// at every change of base, or all rows' sums lean by 1.4e-7 the same way.)
 __device__ __forceinline__ Sum join(Sum a, Sum b) {
   const float c = fmaxf(a.c, b.c);
-  return Sum{c, a.s * exp_of(a.c - c) + b.s * exp_of(b.c - c)};
+  return Sum{c, a.s * expf(a.c - c) + b.s * expf(b.c - c)};
 }
 __device__ __forceinline__ float lse_of(Sum a) { return (float)((double)a.c + (double)logf(a.s)); }
 // x - lse, without lse's rounding
@@ -94,23 +98,25 @@ __device__ __forceinline__ void add(Sum& a, const Vec<T> (&v)[kUnroll]) {
 #pragma unroll
     for (int i = 0; i < Vec<T>::kN; ++i) top = fmaxf(top, v[u].get(i));
   const float c = fmaxf(a.c, top);
-  a.s *= exp_of(a.c - c);
+  a.s *= expf(a.c - c);
   a.c = c;
   // (two values an instruction, but for the exponentials)
   const float2 less = make_float2(-c, -c), scale = make_float2(kLog2e, kLog2e);
+  const float2 rest = make_float2(kLog2eLo, kLog2eLo);
   float2 s = make_float2(a.s, 0.0f);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
     for (int i = 0; i < Vec<T>::kN; i += 2) {
-      const float2 d = zo::mul2(zo::add2(make_float2(v[u].get(i), v[u].get(i + 1)), less), scale);
-      s = zo::add2(s, make_float2(exp2_approx(d.x), exp2_approx(d.y)));
+      const float2 d = zo::add2(make_float2(v[u].get(i), v[u].get(i + 1)), less);
+      const float2 e = zo::fma2(d, scale, zo::mul2(d, rest));
+      s = zo::add2(s, make_float2(exp2_approx(e.x), exp2_approx(e.y)));
     }
   a.s = s.x + s.y;
 }
 __device__ __forceinline__ void add(Sum& a, float x) {
   const float c = fmaxf(a.c, x);
-  a = Sum{c, a.s * exp_of(a.c - c) + exp_of(x - c)};
+  a = Sum{c, a.s * expf(a.c - c) + expf(x - c)};
 }
 
 // Elements in front of the first 16-byte boundary, at most n.
