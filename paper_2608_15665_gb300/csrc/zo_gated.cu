@@ -163,20 +163,38 @@ zo_status zo_gated_forward(const void* X, int64_t ldx, int64_t T, int64_t D, con
   const int32_t pairs = zo::gated_max_pairs();
   uint32_t* status = status_word();
   if (pairs <= 0 || !status) return refuse(ZO_ERR_CUDA, "zo_gated_forward: no usable CUDA device");
-  zo::GatedForward a{};
-  a.T = (int32_t)T;
-  a.D = (int32_t)D;
-  a.F = (int32_t)F;
-  a.act = act == ZO_GATED_SILU ? zo::kGatedSilu : zo::kGatedGelu;
-  a.save = G != nullptr;
-  a.side = zo::gated_side(T, D, F, pairs);
-  a.box_rows = zo::gated_box_rows(T);
-  if (!map_of(&a.x, X, D, T, ldx, 64, a.box_rows) || !map_of(&a.w[0], Wg, D, F, ldwg, 64, a.side) ||
-      !map_of(&a.w[1], Wu, D, F, ldwu, 64, a.side) || !out_map(&a.out[0], H, F, T, ldh) ||
-      (G && (!out_map(&a.out[1], G, F, T, ldg) || !out_map(&a.out[2], U, F, T, ldu))))
-    return refuse(ZO_ERR_CUDA, "zo_gated_forward: cuTensorMapEncodeTiled rejected a descriptor");
-  ZO_CUDA(zo::launch_gated_forward(a, pairs, status, reinterpret_cast<cudaStream_t>(stream)),
-          "gated forward kernel");
+  const zo::GatedPlan plan = zo::gated_plan(T, D, F, pairs);
+  const bool turned = plan.side == 0;
+  const auto fill = [&](auto& a, uint32_t x_rows, uint32_t w_rows) {
+    a.T = (int32_t)T;
+    a.D = (int32_t)D;
+    a.F = (int32_t)F;
+    a.act = act == ZO_GATED_SILU ? zo::kGatedSilu : zo::kGatedGelu;
+    a.save = G != nullptr;
+    void* out[3] = {H, G, U};
+    const int64_t ld[3] = {ldh, ldg, ldu};
+    bool ok = map_of(&a.x, X, D, T, ldx, 64, x_rows) && map_of(&a.w[0], Wg, D, F, ldwg, 64, w_rows) &&
+              map_of(&a.w[1], Wu, D, F, ldwu, 64, w_rows);
+    for (int k = 0; k < (G ? 3 : 1); ++k)
+      ok = ok && (turned ? map_of(&a.out[k], out[k], F, T, ld[k], zo::kGatedOutRows, zo::kGatedOutCols,
+                                  CU_TENSOR_MAP_SWIZZLE_64B)
+                         : out_map(&a.out[k], out[k], F, T, ld[k]));
+    return ok;
+  };
+  const auto s = reinterpret_cast<cudaStream_t>(stream);
+  const char* const no_map = "zo_gated_forward: cuTensorMapEncodeTiled rejected a descriptor";
+  if (turned) {
+    zo::GatedTurned a{};
+    a.tokens = plan.tokens;
+    if (!fill(a, plan.tokens / 2, 128)) return refuse(ZO_ERR_CUDA, no_map);
+    ZO_CUDA(zo::launch_gated_turned(a, pairs, status, s), "gated forward kernel");
+  } else {
+    zo::GatedForward a{};
+    a.side = plan.side;
+    a.box_rows = zo::gated_box_rows(T);
+    if (!fill(a, a.box_rows, a.side)) return refuse(ZO_ERR_CUDA, no_map);
+    ZO_CUDA(zo::launch_gated_forward(a, pairs, status, s), "gated forward kernel");
+  }
   return ZO_OK;
 }
 

@@ -5,6 +5,12 @@
 //             128 of the tokens, and its half of the B operand is `side` rows of Wg (c = 0) or of
 //             Wu (c = 1): accumulator columns 0 .. side - 1 are G's, the next `side` U's, in both
 //             CTAs, and the epilogue has both of an element in one thread.
+//   turned:   the forward pass with the tokens as the MMAs' columns: tile = 256 columns of G and the
+//             same of U x `tokens` tokens, a multiple of 16.  CTA c holds 128 rows of Wg and of Wu
+//             (two A operands, an accumulator each) and half of the tokens.  A tile of 256 tokens
+//             takes less from L2 than two of the above, and 777 tokens are four tiles of 208 rather
+//             than of 256; but the two accumulators leave room for no second pair beyond 128 tokens.
+//             gated_plan takes one or the other by what the busiest pair has to do.
 //   dX:       tile = 256 tokens x 256 columns; K runs over F twice, dG Wg and then dU Wu into one
 //             accumulator.  dG's and dU's rows lie along K, Wg and Wu are MN-major operands (the
 //             instruction descriptor's transpose bit), so no transposed copy is kept.
@@ -49,21 +55,31 @@ using ortho::elected;
 
 constexpr int kTileRows = 256, kTileCols = 256;
 constexpr int kHalfBytes = 128 * 128;                 // 128 rows x 64 bf16, or two MN-major blocks
-constexpr int kStageBytes = 2 * kHalfBytes;           // a CTA's A and B
-constexpr int kStages = 6;
-constexpr int kRing = kStages * kStageBytes;
+constexpr int kRing = 12 * kHalfBytes;
+// a CTA's stages: the A operands (128 rows each), then B
+template <typename Args>
+struct Ring {
+  static constexpr int kA = 1;
+  static constexpr int kStageBytes = (kA + 1) * kHalfBytes, kStages = kRing / kStageBytes;
+};
+template <>
+struct Ring<GatedTurned> {
+  static constexpr int kA = 2;
+  static constexpr int kStageBytes = (kA + 1) * kHalfBytes, kStages = kRing / kStageBytes;
+};
+constexpr int kMaxStages = 6;
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kBoxBytes = kGatedOutRows * kGatedOutCols * 2;
 constexpr int kBoxes = 3;                             // of an epilogue warp
-constexpr int kBufs = 2, kTmemCols = kBufs * kTileCols;
+constexpr int kBufs = 2, kTmemCols = 512;
 constexpr int kRoom = kRing + kEpiWarps * kBoxes * kBoxBytes;
 constexpr size_t kSmem = kRoom + 1024 /*barriers*/ + 1024 /*align*/;
 static_assert(kSmem <= 227 * 1024, "shared memory per CTA");
 constexpr long long kWait = 4000000000LL;             // ~2 s at 2 GHz
 
 struct Shared {
-  uint64_t full[kStages], empty[kStages];
+  uint64_t full[kMaxStages], empty[kMaxStages];
   uint64_t acc_full[kBufs], acc_empty[kBufs];
   uint64_t drain;                // one commit after the leader's last MMA
   uint32_t tmem_base;
@@ -152,6 +168,22 @@ __device__ __forceinline__ bool tile_at(const GatedBackward& a, int pair, int pa
   return true;
 }
 
+__device__ __forceinline__ bool tile_at(const GatedTurned& a, int pair, int pairs, int k, Tile* t) {
+  // the tokens first: the weights are read by pairs at work at the same time
+  const int blocks = (a.T + a.tokens - 1) / a.tokens, rows = (a.F + kTileRows - 1) / kTileRows;
+  const int64_t at = (int64_t)pair + (int64_t)k * pairs;
+  if (at >= (int64_t)rows * blocks) return false;
+  // (many tokens: in groups of 16 blocks of them, as above)
+  const int group = (int)(at / (16 * (int64_t)rows)), in = (int)(at - (int64_t)group * 16 * rows);
+  const int height = min(16, blocks - 16 * group);
+  t->j0 = (16 * group + in % height) * a.tokens;
+  t->i0 = in / height * kTileRows;
+  t->k0 = 0;
+  t->n0 = t->n = (a.D + 63) / 64;
+  t->dw = -1;
+  return true;
+}
+
 // One stage of a tile's operands for CTA `rank`.  Tokens past the last are not loaded where they
 // fill a CTA's half, or where there are fewer than a box's: what shared memory holds in their place
 // ends in accumulator lanes that nothing reads.
@@ -167,7 +199,7 @@ __device__ __forceinline__ void load_stage(const GatedBackward& a, const Tile& t
                                            uint8_t* dst, uint64_t* full, bool leader) {
   const bool second = t.dw >= 0 || t.i0 + 128 < a.T;
   if (leader)
-    mbar_arrive_expect_tx(full, t.dw >= 0 ? 2u * kStageBytes
+    mbar_arrive_expect_tx(full, t.dw >= 0 ? 4u * kHalfBytes
                                           : 2u * kHalfBytes + (second ? 2u : 1u) * (uint32_t)a.box_rows * 128u);
   const int i0 = t.i0 + 128 * (int)rank, j0 = t.j0 + 128 * (int)rank;
   const CUtensorMap* b;
@@ -185,9 +217,29 @@ __device__ __forceinline__ void load_stage(const GatedBackward& a, const Tile& t
   tma_load_2d_to_leader(dst + kHalfBytes + 8192, b, j0 + 64, 64 * k, full);
 }
 
+__device__ __forceinline__ void load_stage(const GatedTurned& a, const Tile& t, int k, uint32_t rank,
+                                           uint8_t* dst, uint64_t* full, bool leader) {
+  if (leader) mbar_arrive_expect_tx(full, 4u * kHalfBytes + (uint32_t)a.tokens * 128u);
+  tma_load_2d_to_leader(dst, &a.w[0], 64 * k, t.i0 + 128 * (int)rank, full);
+  tma_load_2d_to_leader(dst + kHalfBytes, &a.w[1], 64 * k, t.i0 + 128 * (int)rank, full);
+  tma_load_2d_to_leader(dst + 2 * kHalfBytes, &a.x, 64 * k, t.j0 + a.tokens / 2 * (int)rank, full);
+}
+
+// Accumulators, how many of them take turns, and where the next product's columns begin.
+template <typename Args>
+__device__ __forceinline__ int bufs_of(const Args&) { return kBufs; }
+__device__ __forceinline__ int bufs_of(const GatedTurned& a) { return a.tokens <= 128 ? kBufs : 1; }
+template <typename Args>
+__device__ __forceinline__ uint32_t acc_at(int acc) {
+  return (uint32_t)(acc * (Ring<Args>::kA == 2 ? 128 : kTileCols));
+}
+
 // Columns of a tile's accumulator, and how its operands are read.
 __device__ __forceinline__ uint32_t idesc_of(const GatedForward& a, const Tile&) {
   return idesc_bf16_f32(kTileRows, 16) - (2u << 17) + ((uint32_t)(2 * a.side) >> 3 << 17);
+}
+__device__ __forceinline__ uint32_t idesc_of(const GatedTurned& a, const Tile&) {
+  return idesc_bf16_f32(kTileRows, 16) - (2u << 17) + ((uint32_t)a.tokens >> 3 << 17);
 }
 __device__ __forceinline__ uint32_t idesc_of(const GatedBackward&, const Tile& t) {
   return idesc_bf16_f32(kTileRows, kTileCols) | kMnMajorB | (t.dw >= 0 ? kMnMajorA : 0u);
@@ -222,11 +274,46 @@ struct Boxes {
       bulk_commit();
     }
   }
+  // 16 tokens' values (from row0 on) of this lane's column col0 + lane, as a box of 16 rows of 32: two
+  // columns to a word, for which neighbouring lanes trade halves
+  __device__ __forceinline__ void store_turned(const float (&v)[16], const CUtensorMap* to, int col0,
+                                               int row0) {
+    const int lane = threadIdx.x & 31;
+    uint8_t* box = base + next * kBoxBytes;
+    next = next == kBoxes - 1 ? 0 : next + 1;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kBoxes - 1) : "memory");
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t w = pack2(v[2 * e], v[2 * e + 1]);
+      const uint32_t o = __shfl_xor_sync(0xffffffffu, w, 1);
+      const int row = 2 * e + (lane & 1);
+      *reinterpret_cast<uint32_t*>(box + row * 64 + (((lane >> 3) ^ ((row >> 1) & 3)) << 4) + (lane & 6) * 2) =
+          (lane & 1) ? (o >> 16) | (w & 0xFFFF0000u) : (w & 0xFFFFu) | (o << 16);
+    }
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_2d(to, col0, row0, box);
+      bulk_commit();
+    }
+  }
 };
 
 __device__ __forceinline__ void to_floats(const uint32_t (&r)[16], float (&v)[16]) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(r[e]);
+}
+
+__device__ __forceinline__ void activate(int32_t act, const float (&g)[16], const float (&u)[16],
+                                         float (&h)[16]) {
+  if (act == kGatedSilu) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) h[e] = g[e] * gated_gate(g[e], kGatedSilu) * u[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) h[e] = g[e] * gated_gate(g[e], kGatedGelu) * u[e];
+  }
 }
 
 // The accumulator at `tmem` (this warp's lanes) to the results: 32 rows from row0 on.
@@ -242,17 +329,31 @@ __device__ __forceinline__ void finish(const GatedForward& a, const Tile& t, uin
     float g[16], u[16], h[16];
     to_floats(gr, g);
     to_floats(ur, u);
-    if (a.act == kGatedSilu) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) h[e] = g[e] * gated_gate(g[e], kGatedSilu) * u[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) h[e] = g[e] * gated_gate(g[e], kGatedGelu) * u[e];
-    }
+    activate(a.act, g, u, h);
     boxes.store(h, &a.out[0], col, row0);
     if (a.save) {
       boxes.store(g, &a.out[1], col, row0);
       boxes.store(u, &a.out[2], col, row0);
+    }
+  }
+}
+__device__ __forceinline__ void finish(const GatedTurned& a, const Tile& t, uint32_t tmem, int half,
+                                       int row0, int, Boxes& boxes) {
+  for (int c = half; c < a.tokens / 16; c += 2) {
+    const int token = t.j0 + 16 * c;
+    if (row0 >= a.F || token >= a.T) break;
+    uint32_t gr[16], ur[16];
+    tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * c), gr);
+    tmem_ld_32x32b_x16(tmem + (uint32_t)(kTileCols + 16 * c), ur);
+    tmem_ld_wait();
+    float g[16], u[16], h[16];
+    to_floats(gr, g);
+    to_floats(ur, u);
+    activate(a.act, g, u, h);
+    boxes.store_turned(h, &a.out[0], row0, token);
+    if (a.save) {
+      boxes.store_turned(g, &a.out[1], row0, token);
+      boxes.store_turned(u, &a.out[2], row0, token);
     }
   }
 }
@@ -320,6 +421,9 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const volatile int* abort = &sh.abort_flag;
+  constexpr int kStages = Ring<Args>::kStages, kStageBytes = Ring<Args>::kStageBytes;
+  constexpr int kBAt = Ring<Args>::kA * kHalfBytes;
+  const int bufs = bufs_of(a);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -382,9 +486,9 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
       const uint32_t idesc = idesc_of(a, t);
       const bool a_mn = (idesc & kMnMajorA) != 0, b_mn = (idesc & kMnMajorB) != 0;
       const uint64_t a_first = a_mn ? sdesc_mn_sw128(ring) : sdesc_k_sw128(ring);
-      const uint64_t b_first = b_mn ? sdesc_mn_sw128(ring + kHalfBytes) : sdesc_k_sw128(ring + kHalfBytes);
+      const uint64_t b_first = b_mn ? sdesc_mn_sw128(ring + kBAt) : sdesc_k_sw128(ring + kBAt);
       const uint64_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
-      const uint32_t d = tmem + (uint32_t)(acc * kTileCols);
+      const uint32_t d = tmem + acc_at<Args>(acc);
       if (!warp_wait(&sh.acc_empty[acc], acc_parity, abort)) {
         ok = false;
         break;
@@ -399,8 +503,12 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
         const uint64_t bd = b_first + (uint64_t)stage * kStageStep;
         if (elected()) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int e = 0; e < 4; ++e) {
             mma_pair_ss(d, ad + a_step * e, bd + b_step * e, idesc, e != 0 || q != 0 ? 1u : 0u);
+            if constexpr (Ring<Args>::kA == 2)
+              mma_pair_ss(d + kTileCols, ad + (kHalfBytes >> 4) + a_step * e, bd + b_step * e, idesc,
+                          e != 0 || q != 0 ? 1u : 0u);
+          }
           commit_both(&sh.empty[stage]);
           if (q + 1 == t.n) commit_both(&sh.acc_full[acc]);
         }
@@ -410,7 +518,7 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
           parity ^= 1u;
         }
       }
-      if (++acc == kBufs) {
+      if (++acc == bufs) {
         acc = 0;
         acc_parity ^= 1u;
       }
@@ -435,12 +543,12 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
         break;
       }
       tc_fence_after();
-      finish(a, t, tmem + ((uint32_t)(32 * g) << 16) + (uint32_t)(acc * kTileCols), half,
+      finish(a, t, tmem + ((uint32_t)(32 * g) << 16) + acc_at<Args>(acc), half,
              t.i0 + 128 * (int)rank + 32 * g, (int)rank * kEpiWarps + warp - 2, boxes);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) arrive_leader(&sh.acc_empty[acc]);
-      if (++acc == kBufs) {
+      if (++acc == bufs) {
         acc = 0;
         parity ^= 1u;
       }
@@ -495,6 +603,7 @@ int32_t gated_max_pairs() {
     least = std::min(least, (int32_t)clusters);
   };
   ask(gated_kernel<GatedForward>);
+  ask(gated_kernel<GatedTurned>);
   ask(gated_kernel<GatedBackward>);
   return pairs[dev] = least;
 }
@@ -502,20 +611,31 @@ int32_t gated_max_pairs() {
 int32_t gated_box_rows(int64_t T) { return (int32_t)std::min<int64_t>(128, (T + 7) / 8 * 8); }
 
 // The busiest pair's cycles: rounds of tiles, each D / 64 stages that take the longer of their
-// MMAs (128 cycles for 16 of K and N = 256) and their operands' way from L2 (~54 bytes a cycle),
-// and one epilogue behind the last.
-int32_t gated_side(int64_t T, int64_t D, int64_t F, int32_t pairs) {
-  int32_t best = 128;
+// MMAs (128 cycles for 16 of K and N = 256, and not below 90) and their operands' way from L2 (~54
+// bytes a cycle), and epilogues of ~100 cycles a column, under the next tile's stages where there
+// are two accumulators.  Measured, the one kind of tile against the other (D = 4096, F = 11008): 1
+// token 38 us, turned 35; 128 tokens 40.5, 39; 256 41, 46; 300 58, 55; 512 60, 66; 4096 381, 414;
+// and 777 x 5120 x 13824 153, 134.
+GatedPlan gated_plan(int64_t T, int64_t D, int64_t F, int32_t pairs) {
+  GatedPlan best{128, 0};
   int64_t least = INT64_MAX;
-  for (int32_t side = 128; side >= 16; side -= 16) {
-    const int64_t tiles = ceil_div(T, kTileRows) * ceil_div(F, side);
-    const int64_t stage = std::max<int64_t>(std::max<int64_t>(4 * side, 360), (kHalfBytes + side * 128) / 54);
-    const int64_t cycles = ceil_div(tiles, pairs) * (ceil_div(D, 64) * stage + 600) + 40 * side;
+  const int64_t stages = ceil_div(D, 64);
+  const auto consider = [&](GatedPlan p, int64_t tiles, int64_t mma, int64_t bytes, int64_t epilogue, bool alone) {
+    const int64_t rounds = ceil_div(tiles, pairs);
+    const int64_t products = stages * std::max<int64_t>(mma, bytes / 54) + 600;
+    const int64_t cycles = alone ? rounds * (products + epilogue)
+                                 : rounds * std::max(products, epilogue) + std::min(products, epilogue);
     if (cycles < least) {
       least = cycles;
-      best = side;
+      best = p;
     }
-  }
+  };
+  for (int32_t side = 128; side >= 16; side -= 16)
+    consider({side, 0}, ceil_div(T, kTileRows) * ceil_div(F, side), std::max<int64_t>(4 * side, 360),
+             kHalfBytes + side * 128, 100 * side, false);
+  for (int32_t tokens = 256; tokens >= 32; tokens -= 16)
+    consider({0, tokens}, ceil_div(T, tokens) * ceil_div(F, kTileRows), std::max<int64_t>(4 * tokens, 720),
+             2 * kHalfBytes + tokens * 64, 100 * tokens, tokens > 128);
   return best;
 }
 
@@ -542,6 +662,11 @@ void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs) {
 
 cudaError_t launch_gated_forward(const GatedForward& a, int32_t pairs, uint32_t* status, cudaStream_t s) {
   const int64_t tiles = ceil_div(a.T, kTileRows) * ceil_div(a.F, a.side);
+  return launch(a, (int32_t)std::min<int64_t>(pairs, tiles), status, s);
+}
+
+cudaError_t launch_gated_turned(const GatedTurned& a, int32_t pairs, uint32_t* status, cudaStream_t s) {
+  const int64_t tiles = ceil_div(a.T, a.tokens) * ceil_div(a.F, kTileRows);
   return launch(a, (int32_t)std::min<int64_t>(pairs, tiles), status, s);
 }
 

@@ -172,6 +172,12 @@ struct GatedForward {
   int32_t side;                     // columns of Wg (and of Wu) to a tile
   int32_t box_rows;                 // tokens in a box of X
 };
+// the same with the tokens as the products' columns
+struct GatedTurned {
+  CUtensorMap x, w[2], out[3];
+  int32_t T, D, F, act, save;
+  int32_t tokens;                   // of a tile: a multiple of 16
+};
 struct GatedBackward {
   CUtensorMap d_rows[2], w_cols[2], dx;           // dX: dG, dU along F; Wg, Wu by rows of F
   CUtensorMap d_cols[2], x_cols, dw[2];           // dW: dG, dU and X by rows of T
@@ -183,11 +189,15 @@ struct GatedBackward {
   uint32_t* counters;               // and kGatedCounters of every tile, zero before the launch
   int32_t skip;                     // rounds of dW's tiles that take as long as a tile of dX
 };
-// columns and rows of a box of a result; tokens in a box of an operand: at most a CTA's 128
+// columns and rows of a box of a result (of turned tiles: the other way round); tokens in a box of an
+// operand: at most a CTA's 128
 constexpr int kGatedOutCols = 16, kGatedOutRows = 32;
 int32_t gated_box_rows(int64_t T);
-// columns of a tile's two halves for this call
-int32_t gated_side(int64_t T, int64_t D, int64_t F, int32_t pairs);
+// The tiles of a call: `side` columns of each half, or (side = 0) `tokens` tokens to a turned tile
+struct GatedPlan {
+  int32_t side, tokens;
+};
+GatedPlan gated_plan(int64_t T, int64_t D, int64_t F, int32_t pairs);
 // SM pairs that run at once, or 0
 int32_t gated_max_pairs();
 // Parts of the K of dX's tiles: where the tiles leave half of a GB300's SM pairs or more without one,
@@ -200,6 +210,7 @@ int32_t gated_parts(int64_t T, int64_t D, int64_t F);
 // fills n_dx, n_dw, parts and skip
 void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs);
 cudaError_t launch_gated_forward(const GatedForward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
+cudaError_t launch_gated_turned(const GatedTurned& a, int32_t pairs, uint32_t* status, cudaStream_t s);
 cudaError_t launch_gated_backward(const GatedBackward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
 
 }  // namespace zo
