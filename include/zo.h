@@ -595,7 +595,8 @@ ZO_API zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t
  *   16-byte aligned, for dG, dU and parts of sums; calls whose work overlaps need one each.
  * act: ZO_GATED_SILU g sig(g), or ZO_GATED_GELU_TANH g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))).
  * Every matrix is 16-byte aligned and its row stride (ldx, ... in elements) a multiple of 8; D and
- * F are multiples of 8, T is any number from 0 on (no tokens: dWg and dWu are zero).  Outputs must
+ * F are multiples of 8 below 2^24, T any number from 0 on below it (no tokens: dWg and dWu are zero),
+ * with T D, T F <= 2^34 and D F <= 2^37.  Outputs must
  * not overlap inputs.  No atomics: the same inputs give the same bits.  Asynchronous on `stream`
  * (void* cudaStream_t) of the current device.
  * zo_gated_sync_status -- synchronise the stream; ZO_ERR_TIMEOUT, once, where a wait of one of

@@ -51,7 +51,7 @@ constexpr int kCtas = 7;                         // of an SM
 // 8 bits: a warp's ring of blocks in shared memory (W and G in fp32 at most)
 constexpr int kStages = 2, kStageBytes = kBlock * 10;
 constexpr int kRingBytes = kThreads / 32 * kStages * kStageBytes;
-static_assert(kCtas * kRingBytes <= 227 * 1024, "shared memory per SM");
+static_assert(kRingBytes <= 48 * 1024 && kCtas * kRingBytes <= 227 * 1024, "shared memory");
 static_assert(kBlock == 256 && kRow % kBlock == 0 && kMaxUnits <= 32, "a chunk is whole blocks");
 
 struct Tensor {
@@ -726,10 +726,6 @@ zo_status zo_adamw_step(zo_adamw_ctx* c, int64_t t, int64_t* count, double lr, d
   if (c->plan.chunks == 0) return ZO_OK;
   const auto* ts = reinterpret_cast<const Tensor*>(c->ws + c->plan.tensors_at);
   const auto* chunks = reinterpret_cast<const int2*>(c->ws + c->plan.chunks_at);
-  if (c->bits == 8)
-    ZO_CUDA(cudaFuncSetAttribute(adamw_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kRingBytes),
-            "AdamW kernel's shared memory");
   ZO_CUDA(zo::launch_dependent(c->bits == 8 ? adamw_kernel<true> : adamw_kernel<false>,
                                (unsigned)c->plan.chunks, kThreads, c->bits == 8 ? kRingBytes : 0,
                                c->stream, 1, true, ts, chunks, c->plan.units, st, now, count ? counted : nullptr),

@@ -96,9 +96,9 @@ zo_status check_sizes(int64_t T, int64_t D, int64_t F, int32_t act) {
     return refuse(ZO_ERR_INVALID_ARG, "zo_gated: unknown activation");
   if (T < 0 || T >= kMaxExtent || D < 8 || D >= kMaxExtent || F < 8 || F >= kMaxExtent ||
       D % 8 != 0 || F % 8 != 0 || (T > 0 && F > (int64_t(1) << 34) / T) ||
-      (T > 0 && D > (int64_t(1) << 34) / T))
-    return refuse(ZO_ERR_SHAPE, "zo_gated: need 0 <= T < 2^24, D and F multiples of 8 below 2^24, and "
-                                "T D, T F <= 2^34");
+      (T > 0 && D > (int64_t(1) << 34) / T) || F > (int64_t(1) << 37) / D)
+    return refuse(ZO_ERR_SHAPE, "zo_gated: need 0 <= T < 2^24, D and F multiples of 8 below 2^24, "
+                                "T D, T F <= 2^34 and D F <= 2^37");
   return ZO_OK;
 }
 

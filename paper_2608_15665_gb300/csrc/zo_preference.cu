@@ -30,6 +30,7 @@ using namespace zo::host;
 // Small CTAs: one's first loads and last sums lie under the others' (16 pairs, 32000 wide: forward
 // 139 us with 128 threads, 148 with 256, 209 with 512).
 constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kPairThreads = 512;                // of a pair's two sequences
 constexpr int kUnroll = 4;                       // vectors of 16 bytes a thread has on their way
 constexpr int kMaxParts = 32, kPartCols = 4096;  // parts of a row, none narrower than this
 // columns of a CTA's part in the backward pass (812 rows of 50257 fp32: 52 us; in whole rows 58, as 5.3
@@ -220,41 +221,52 @@ __device__ __forceinline__ double warp_sum(double v) {
   return v;
 }
 
-// A CTA per pair: half of its warps sum the chosen sequence, half the rejected one.
+// A CTA per pair: half of its warps sum the chosen sequence, half the rejected one, four rows a
+// thread at a time.
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kPairThreads)
 pairs_kernel(const Rows a, const Loss f, const Sum* __restrict__ partial,
              const float* __restrict__ logp, const float* __restrict__ ref, float* __restrict__ lse,
              float* __restrict__ dlogp, float* __restrict__ logps, float* __restrict__ losses,
              float* __restrict__ loss, uint32_t* __restrict__ ticket) {
-  __shared__ double sums[kWarps], counts[kWarps];
+  constexpr int kPairWarps = kPairThreads / 32, kSide = kPairThreads / 2, kAtOnce = 4;
+  __shared__ double sums[kPairWarps], counts[kPairWarps];
   __shared__ float slopes[2];
   __shared__ bool last;
   const int64_t pair = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int side = warp / (kWarps / 2);                             // 0: chosen
+  const int side = warp / (kPairWarps / 2);                         // 0: chosen
   const int64_t seq = pair + side * a.pairs;
-  const int first = (int)threadIdx.x - side * (kThreads / 2);
+  const int first = (int)threadIdx.x - side * kSide;
   zo::pdl_wait();
   zo::pdl_trigger();
   // (offsets out of order or range: no row outside the matrix is touched)
   const int64_t begin = min(a.rows, max((int64_t)0, a.offsets[seq])), end = min(a.rows, a.offsets[seq + 1]);
   double sum = 0.0, count = 0.0;
-  for (int64_t r = begin + first; r < end; r += kThreads / 2) {
-    const int64_t label = a.labels[r];
-    if (label < 0) continue;
-    float lp;
-    if (a.parts > 1) {
-      Sum s = partial[r * a.parts];
-      for (int p = 1; p < a.parts; ++p) s = join(s, partial[r * a.parts + p]);
-      if (lse) lse[r] = lse_of(s);
-      lp = label < a.vocab ? logp_of(s, static_cast<float>(static_cast<const T*>(a.x)[r * a.ld + label]))
-                           : __int_as_float(0x7FC00000);
-    } else {
-      lp = logp[r];
+  for (int64_t r0 = begin + first; r0 < end; r0 += kAtOnce * kSide) {
+    int64_t label[kAtOnce];
+    float lp[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int64_t r = r0 + i * kSide;
+      label[i] = r < end ? a.labels[r] : -1;
+      lp[i] = r < end && a.parts == 1 ? logp[r] : 0.0f;
     }
-    sum += (double)lp;
-    count += 1.0;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (label[i] < 0) continue;
+      if (a.parts > 1) {
+        const int64_t r = r0 + i * kSide;
+        Sum s = partial[r * a.parts];
+        for (int p = 1; p < a.parts; ++p) s = join(s, partial[r * a.parts + p]);
+        if (lse) lse[r] = lse_of(s);
+        lp[i] = label[i] < a.vocab
+                    ? logp_of(s, static_cast<float>(static_cast<const T*>(a.x)[r * a.ld + label[i]]))
+                    : __int_as_float(0x7FC00000);
+      }
+      sum += (double)lp[i];
+      count += 1.0;
+    }
   }
   sum = warp_sum(sum);
   count = warp_sum(count);
@@ -268,9 +280,9 @@ pairs_kernel(const Rows a, const Loss f, const Sum* __restrict__ partial,
     for (int k = 0; k < 2; ++k) {
       double s = 0.0;
       n[k] = 0.0;
-      for (int w = 0; w < kWarps / 2; ++w) {
-        s += sums[k * (kWarps / 2) + w];
-        n[k] += counts[k * (kWarps / 2) + w];
+      for (int w = 0; w < kPairWarps / 2; ++w) {
+        s += sums[k * (kPairWarps / 2) + w];
+        n[k] += counts[k * (kPairWarps / 2) + w];
       }
       if (f.average && n[k] > 0.0) s /= n[k];
       logps[pair + k * a.pairs] = (float)s;
@@ -289,21 +301,27 @@ pairs_kernel(const Rows a, const Loss f, const Sum* __restrict__ partial,
   __syncthreads();
   if (dlogp) {
     const float d = slopes[side];
-    for (int64_t r = begin + first; r < end; r += kThreads / 2)
-      if (a.labels[r] >= 0) dlogp[r] = d;
+    for (int64_t r0 = begin + first; r0 < end; r0 += kAtOnce * kSide) {
+      bool counted[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        counted[i] = r0 + i * kSide < end && a.labels[r0 + i * kSide] >= 0;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (counted[i]) dlogp[r0 + i * kSide] = d;
+    }
   }
   if (!last) return;
   // the losses of all pairs, in an order of their own
   __threadfence();
   double total = 0.0;
-  for (int64_t p = threadIdx.x; p < a.pairs; p += kThreads) total += (double)__ldcg(losses + p);
+  for (int64_t p = threadIdx.x; p < a.pairs; p += kPairThreads) total += (double)__ldcg(losses + p);
   total = warp_sum(total);
-  __syncthreads();
   if (lane == 0) sums[warp] = total;
   __syncthreads();
   if (threadIdx.x == 0) {
     total = 0.0;
-    for (int w = 0; w < kWarps; ++w) total += sums[w];
+    for (int w = 0; w < kPairWarps; ++w) total += sums[w];
     *loss = (float)(total / (double)a.pairs);
   }
 }
@@ -467,7 +485,7 @@ zo_status zo_preference_forward(const void* logits, int64_t ldl, int64_t rows, i
                                0, s, 1, true, a, partial, logp, lse, dlogp, ticket),
           "preference: rows' kernel");
   ZO_CUDA(zo::launch_dependent(half ? pairs_kernel<__nv_bfloat16> : pairs_kernel<float>,
-                               (unsigned)pairs, kThreads, 0, s, 1, true, a, f, partial, logp,
+                               (unsigned)pairs, kPairThreads, 0, s, 1, true, a, f, partial, logp,
                                ref_logps, lse, dlogp, logps, losses, loss, ticket),
           "preference: pairs' kernel");
   return ZO_OK;

@@ -307,6 +307,8 @@ class AdamWState(NamedTuple):
 
 def adamw_state(weight, bits=32):
     """The states of a tensor before its first step: zero."""
+    if bits not in (8, 32):
+        raise zb.ZoError(zb.ZO_ERR_UNSUPPORTED, "adamw_state", "states are held in 8 or in 32 bits")
     n, dev = weight.numel(), weight.device
     if bits == 32:
         return AdamWState(torch.zeros(n, device=dev), torch.zeros(n, device=dev))
@@ -546,11 +548,18 @@ def gated_linear_sync(device=None):
         zb.zo_gated_sync_status(torch.cuda.current_stream())
 
 
+def _packed(t):
+    """A matrix as the kernels take it: rows without gaps, on a 16-byte boundary."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 class GatedLinear(torch.autograd.Function):
     """``GatedLinear.apply(x, w_gate, w_up, act)`` on a tokens x D matrix.  Differentiable once."""
 
     @staticmethod
     def forward(ctx, x, w_gate, w_up, act="silu"):
+        x = _packed(x)
         out = gated_linear(x, w_gate, w_up, act, save=any(ctx.needs_input_grad[:3]))
         ctx.save_for_backward(x, w_gate, w_up, out.gate, out.up)
         ctx.act = act
@@ -561,6 +570,6 @@ class GatedLinear(torch.autograd.Function):
     def backward(ctx, dh):
         x, w_gate, w_up, gate, up = ctx.saved_tensors
         need_x, need_g, need_u = ctx.needs_input_grad[:3]
-        dx, dwg, dwu = gated_linear_backward(dh.contiguous(), x, w_gate, w_up, gate, up, ctx.act,
+        dx, dwg, dwu = gated_linear_backward(_packed(dh), x, w_gate, w_up, gate, up, ctx.act,
                                              want_x=need_x, want_weights=need_g or need_u)
         return dx, dwg if need_g else None, dwu if need_u else None, None

@@ -102,3 +102,5 @@ def test_handle_refuses(lib):
             fo.AdamW(**args)
     with pytest.raises(ValueError):
         fo.AdamW(W, grads=[])
+    with pytest.raises(lib.ZoError):
+        fo.adamw_state(W[0], 16)

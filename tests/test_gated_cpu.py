@@ -21,7 +21,7 @@ def _call(fn, base, kw):
 COMMON = [(dict(act=2), 1), (dict(act=-1), 1), (dict(T=-1), 2), (dict(T=1 << 24), 2), (dict(D=0), 2),
           (dict(D=60), 2), (dict(F=12), 2), (dict(F=1 << 24), 2),
           (dict(T=1 << 20, F=1 << 16, ldh=1 << 16, lddh=1 << 16), 2),
-          (dict(ldx=63), 2), (dict(ldwg=56), 2), (dict(ldx=68), 3), (dict(Wg=0x2008), 3),
+          (dict(D=1 << 20, F=1 << 18, ldx=1 << 20), 2), (dict(ldx=63), 2), (dict(ldwg=56), 2), (dict(ldx=68), 3), (dict(Wg=0x2008), 3),
           (dict(Wu=0), 1), (dict(ldu=24), 2)]
 
 

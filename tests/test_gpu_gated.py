@@ -176,6 +176,13 @@ def test_autograd_gives_the_gradients_and_they_are_difference_quotients(lib, gpu
     out = fo.gated_linear(x, wg, wu, act, save=True)
     want = fo.gated_linear_backward(dh, x, wg, wu, out.gate, out.up, act)
     assert all(torch.equal(a.grad, b) for a, b in zip(leaves, want))
+    # inputs and gradients in other orders and places are taken as copies
+    base = torch.zeros(33 * 72 + 3, dtype=BF, device=gpu)
+    for odd in (x.t().contiguous().t(), base[3:].view(33, 72).copy_(x)):
+        leaf = odd.detach().requires_grad_()
+        h = fo.GatedLinear.apply(leaf, wg, wu, act)
+        h.backward(dh.t().contiguous().t())
+        assert torch.equal(h, out.h) and torch.equal(leaf.grad, want[0])
     # along a direction, in 64 bits: the sum of gradient times direction, to bf16's grade
     dirs = [make(*t.shape, gpu, 9 + i).double() for i, t in enumerate((x, wg, wu))]
 

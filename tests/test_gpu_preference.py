@@ -113,7 +113,7 @@ SHAPES = [
     ([0, 4], 130, 0, 0, 0, 0), ([5, 0, 3, 7], 1000, 8, 0, 4, 0), ([4, 4, 4, 4, 4, 4], 2049, 1, 2, 0, 3),
     ([1, 1], 32000, 0, 0, 0, 0), ([2, 3], 50257, 47, 0, 1, 0), ([1, 2], 160001, 0, 0, 0, 0),
     ([40, 25, 33, 61], 4096, 0, 0, 3, 0), ([90] * 8, 520, 0, 0, 0, 0), ([2] * 600, 40, 0, 0, 0, 0),
-    ([200, 301], 8200, 8, 0, 0, 8)]
+    ([200, 301], 8200, 8, 0, 0, 8), ([2500, 1300], 24, 0, 0, 0, 0)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

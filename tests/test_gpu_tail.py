@@ -61,7 +61,7 @@ def test_gradients_of_a_tail(lib, gpu):
     want.backward()
     # activations are rounded to bf16 (2^-9) five times on the way to logits of size ~2 and to sums
     # of ~8 of them: z is off by at most 0.2 x 16 rows x 2 x 5 x 2^-9
-    assert abs(float(loss) - float(want)) <= 0.2 * 16 * 2 * 5 * 2.0 ** -9
+    assert abs(float(loss.detach()) - float(want.detach())) <= 0.2 * 16 * 2 * 5 * 2.0 ** -9
     for k, leaf in leaves.items():
         g, w = leaf.grad.double(), wide[k].grad
         # a dozen roundings of 2^-9 on the way down and back, in random directions
@@ -87,7 +87,7 @@ def test_steps_of_a_tail_follow_64_bits(lib, gpu, bits):
     losses = []
     for t in range(1, 4):
         loss = tail.loss(p)
-        losses.append(float(loss))
+        losses.append(float(loss.detach()))
         grads = dict(zip(p, torch.autograd.grad(loss, list(p.values()))))
         before = {k: p[k].detach().double().clone() for k in names}
         for k, buf in zip(names, adamw.grads):
