@@ -503,8 +503,10 @@ ZO_API int64_t zo_muon_launches(const zo_muon_ctx* ctx);
  *     with x in steps of the codes around it.  r > 0 keeps a code above 0.  Infinity becomes NaN.
  * zo_adamw_step -- one step of every tensor: its number t >= 1 (count NULL), or t = 0 and a
  *   device count that the step raises by one and goes by, so that a captured step may be
- *   replayed.  The states' sums are formed from products that are each rounded to fp32.  A NaN
- *   or infinity in G gives NaN in its own element of W and m, no others.
+ *   replayed.  The states' sums are formed from products that are each rounded to fp32, and r is
+ *   rounded to nearest (from v = 2^-102 on): the codes are those of any fp32 evaluation.  A NaN or
+ *   infinity in G gives NaN in its own element of W and m (with 8 bits: so does a G whose square
+ *   leaves fp32's range), no others.
  */
 typedef struct zo_adamw_tensor {
   void* W;            /* device; m x n, row stride ldw elements, dtype below */
@@ -589,7 +591,8 @@ ZO_API zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t
  *   both NULL.
  * zo_gated_backward -- from dH (T x F) and the kept G and U:
  *     dG = rnd(dH U act'(G)),  dU = rnd(dH act(G)),
- *     dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X.
+ *     dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,
+ *   rnd to bf16, or for T <= 128 to sums of two bf16.
  *   NULL = not wanted: dX (then Wg and Wu are not read), or both of dWg and dWu (then X is not).
  *   workspace: caller-owned device memory of at least zo_gated_workspace(T, D, F) bytes,
  *   16-byte aligned, for dG, dU and parts of sums; calls whose work overlaps need one each.

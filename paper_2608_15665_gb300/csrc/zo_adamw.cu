@@ -301,19 +301,29 @@ __device__ __forceinline__ void encode(const float (&x)[kLane], uint32_t E, bool
                          __byte_perm(c[4 * q + 2], c[4 * q + 3], 0x0073), 0x5410);
 }
 
-// The largest finite |x| of the warp's block, as bits; odd: there are others.
+// The largest finite |x| of the warp's block, as bits; odd: there are others.  kSigned = false: x has
+// no negative values, and NaN and infinity are the largest bits.
+template <bool kSigned>
 __device__ __forceinline__ uint32_t largest(const float (&x)[kLane], bool* odd) {
-  // (a NaN is no maximum, but it and infinity spoil a sum of zeros)
-  float most = 0.0f;
-  float2 zeros = both(0.0f);
-#pragma unroll
-  for (int e = 0; e < kLane; e += 2) {
-    most = fmaxf(fmaxf(most, fabsf(x[e])), fabsf(x[e + 1]));
-    zeros = zo::fma2(make_float2(x[e], x[e + 1]), both(0.0f), zeros);
-  }
-  *odd = __any_sync(0xffffffffu, zeros.x + zeros.y != 0.0f);
   uint32_t top;
-  top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
+  if constexpr (kSigned) {
+    // (a NaN is no maximum, but it and infinity spoil a sum of zeros)
+    float most = 0.0f;
+    float2 zeros = both(0.0f);
+#pragma unroll
+    for (int e = 0; e < kLane; e += 2) {
+      most = fmaxf(fmaxf(most, fabsf(x[e])), fabsf(x[e + 1]));
+      zeros = zo::fma2(make_float2(x[e], x[e + 1]), both(0.0f), zeros);
+    }
+    *odd = __any_sync(0xffffffffu, zeros.x + zeros.y != 0.0f);
+    top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
+  } else {
+    top = __float_as_uint(x[0]);
+#pragma unroll
+    for (int e = 1; e < kLane; ++e) top = max(top, __float_as_uint(x[e]));
+    top = __reduce_max_sync(0xffffffffu, top);
+    *odd = top >= 0x7F800000u;
+  }
   if (*odd) {
     top = 0;
 #pragma unroll
@@ -330,6 +340,22 @@ __device__ __forceinline__ float root_of(float v) {
   float r;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
+}
+// Square roots rounded to nearest, of 2^-102 <= v < infinity (smaller ones to 2^-22 of them, or of
+// 2^-63): the hardware's reciprocal root y, s = v y, and
+// one Newton step by the residual, s + (v - s^2) y / 2 (Markstein, IBM J. Res. Dev. 34, 1990), with the
+// sign of s turned.  So a state's codes are those of any other fp32 evaluation.  (Infinity gives NaN,
+// which its code would be in any case.)
+__device__ __forceinline__ float2 rounded_roots(float2 v) {
+  const float2 u = zo::add2(v, both(0x1p-126f));      // (0 has no reciprocal root; others keep theirs)
+  float2 y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(u.x));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(u.y));
+  const float2 ny = make_float2(-y.x, -y.y), ns = zo::mul2(v, ny);
+  // v - s^2 as -(s s - v); then -(s + (v - s^2) y / 2)
+  const float2 rest = zo::fma2(ns, ns, make_float2(-v.x, -v.y));
+  const float2 nr = zo::fma2(rest, zo::mul2(y, both(0.5f)), ns);
+  return make_float2(-nr.x, -nr.y);
 }
 __device__ __forceinline__ float reciprocal(float v) {
   float r;
@@ -420,7 +446,7 @@ struct Unit {
       // know, or it would fuse the sum instead)
       m2 = zo::add2(zo::fma2(b1, m2, none), zo::fma2(c1, gr, none));
       v2 = zo::add2(zo::fma2(b2, v2, none), zo::fma2(c2, zo::mul2(gr, gr), none));
-      const float2 root = make_float2(root_of(v2.x), root_of(v2.y));
+      const float2 root = kEight ? rounded_roots(v2) : make_float2(root_of(v2.x), root_of(v2.y));
       const float2 den = zo::fma2(root, spread, both(st.eps));
       const float2 move = zo::mul2(zo::mul2(rate, m2), make_float2(reciprocal(den.x), reciprocal(den.y)));
       const float2 to = zo::fma2(keep, make_float2(x[e], x[e + 1]), move);
@@ -433,7 +459,7 @@ struct Unit {
     if constexpr (kEight) {
       const uint32_t first = __shfl_sync(0xffffffffu, (uint32_t)(count > 0), 0);
       bool odd_m, odd_v;
-      const uint32_t tm = largest(a, &odd_m), tv = largest(b, &odd_v);
+      const uint32_t tm = largest<true>(a, &odd_m), tv = largest<false>(b, &odd_v);
       // 2^k <= r < 2^(k + 1) where 2^2k <= v < 2^(2k + 2)
       em = tm >> 23;
       ev = tv >> 23 ? (uint32_t)((((int)(tv >> 23) - 127) >> 1) + 127) : 0u;
@@ -467,7 +493,7 @@ struct Unit {
 // as long as its loads, whole blocks of aligned tensors come through shared memory, the next one's
 // loads under this one's arithmetic: with loads into registers 24 warps an SM waited half of their
 // time (131M elements, bf16: 386 us; through shared memory 247 with three blocks ahead and 24 warps,
-// 229 with two and 28).
+// 229 with two and 28, 250 with roots rounded to nearest: 450 instructions a block, 3.0 a cycle).
 template <bool kEight, typename W, typename G>
 __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int units, uint32_t index,
                                           const Step& st, const Now& now) {

@@ -14,6 +14,8 @@
 //   dX:       tile = 256 tokens x 256 columns; K runs over F twice, dG Wg and then dU Wu into one
 //             accumulator.  dG's and dU's rows lie along K, Wg and Wu are MN-major operands (the
 //             instruction descriptor's transpose bit), so no transposed copy is kept.
+//             Up to 128 tokens dG and dU are sums of two bf16, in two rows a token that the tile has
+//             to spare: neighbouring accumulator lanes, which the epilogue adds up.
 //   dWg, dWu: tile = 256 rows of F x 256 columns of D, K = the tokens: both operands MN-major.
 //
 // dX's tiles are the deepest and few (where very few, K is split: gated_parts): they are dealt to the pairs first, round by round, and dW's
@@ -164,7 +166,8 @@ __device__ __forceinline__ bool tile_at(const GatedBackward& a, int pair, int pa
   t->i0 = in / cols * kTileRows;
   t->j0 = in % cols * kTileCols;
   t->k0 = 0;
-  t->n0 = t->n = (a.T + 63) / 64;
+  t->n0 = (a.T + 63) / 64;
+  t->n = a.twin ? 2 * t->n0 : t->n0;
   return true;
 }
 
@@ -197,7 +200,7 @@ __device__ __forceinline__ void load_stage(const GatedForward& a, const Tile& t,
 }
 __device__ __forceinline__ void load_stage(const GatedBackward& a, const Tile& t, int k, uint32_t rank,
                                            uint8_t* dst, uint64_t* full, bool leader) {
-  const bool second = t.dw >= 0 || t.i0 + 128 < a.T;
+  const bool second = t.dw >= 0 || t.i0 + 128 < (a.twin ? 2 * a.T : a.T);
   if (leader)
     mbar_arrive_expect_tx(full, t.dw >= 0 ? 4u * kHalfBytes
                                           : 2u * kHalfBytes + (second ? 2u : 1u) * (uint32_t)a.box_rows * 128u);
@@ -209,8 +212,11 @@ __device__ __forceinline__ void load_stage(const GatedBackward& a, const Tile& t
     if (rank == 0 || second) tma_load_2d_to_leader(dst, &a.d_rows[which], 64 * k, i0, full);
     b = &a.w_cols[which];
   } else {
-    tma_load_2d_to_leader(dst, &a.d_cols[t.dw], i0, 64 * k, full);
-    tma_load_2d_to_leader(dst + 8192, &a.d_cols[t.dw], i0 + 64, 64 * k, full);
+    const int which = k >= t.n0 ? 1 : 0;          // (twin: the second parts, with the same X)
+    k -= which * t.n0;
+    const CUtensorMap* d = &a.d_cols[t.dw][which];
+    tma_load_2d_to_leader(dst, d, i0, 64 * k, full);
+    tma_load_2d_to_leader(dst + 8192, d, i0 + 64, 64 * k, full);
     b = &a.x_cols;
   }
   tma_load_2d_to_leader(dst + kHalfBytes, b, j0, 64 * k, full);
@@ -363,7 +369,8 @@ __device__ __forceinline__ void finish(const GatedBackward& a, const Tile& t, ui
                                        int row0, int warp, Boxes& boxes) {
   constexpr int kChunks = kTileCols / 32;             // of a warp
   const CUtensorMap* to = t.dw < 0 ? &a.dx : &a.dw[t.dw];
-  const int rows = t.dw < 0 ? a.T : a.F, lane = threadIdx.x & 31;
+  const bool twin = t.dw < 0 && a.twin;
+  const int rows = t.dw >= 0 ? a.F : twin ? 2 * a.T : a.T, lane = threadIdx.x & 31;
   if (row0 >= rows) return;
   const bool split = t.dw < 0 && a.parts > 1;
   const float* from = nullptr;
@@ -405,7 +412,22 @@ __device__ __forceinline__ void finish(const GatedBackward& a, const Tile& t, ui
       tmem_ld_wait();
       to_floats(r, v);
     }
-    boxes.store(v, to, t.j0 + 16 * c, row0);
+    if (!twin) {
+      boxes.store(v, to, t.j0 + 16 * c, row0);
+      continue;
+    }
+    // the token's two rows are neighbouring lanes
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] += __shfl_xor_sync(0xffffffffu, v[e], 1);
+    const int token = (row0 + lane) / 2, col = t.j0 + 16 * c + 8 * (lane & 1);
+    if (token < a.T && col < a.D) {
+      const bool odd = lane & 1;                    // (each of the two stores eight columns)
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w[e] = odd ? pack2(v[2 * e + 8], v[2 * e + 9]) : pack2(v[2 * e], v[2 * e + 1]);
+      *reinterpret_cast<uint4*>(a.dx_rows + token * a.lddx + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
 }
 
@@ -655,7 +677,7 @@ void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs) {
   a->n_dx = want_x ? (int32_t)(gated_dx_tiles(a->T, a->D) * a->parts) : 0;
   a->n_dw = want_w ? (int32_t)(2 * ceil_div(a->F, kTileRows) * cols) : 0;
   // stages of a tile, with what its beginning costs
-  const int64_t deep = 2 * ceil_div(a->F, 64) / a->parts + 4, flat = ceil_div(a->T, 64) + 4;
+  const int64_t deep = 2 * ceil_div(a->F, 64) / a->parts + 4, flat = (a->twin ? 2 : 1) * ceil_div(a->T, 64) + 4;
   const int64_t late = a->n_dx % pairs;
   a->skip = late == 0 ? 0 : (int32_t)std::min<int64_t>((deep + flat / 2) / flat, ceil_div(a->n_dw, pairs - late));
 }

@@ -180,8 +180,12 @@ struct GatedTurned {
 };
 struct GatedBackward {
   CUtensorMap d_rows[2], w_cols[2], dx;           // dX: dG, dU along F; Wg, Wu by rows of F
-  CUtensorMap d_cols[2], x_cols, dw[2];           // dW: dG, dU and X by rows of T
+  CUtensorMap d_cols[2][2], x_cols, dw[2];        // dW: dG, dU and X by rows of T
   int32_t T, D, F;
+  int32_t twin;                     // dG and dU are sums of two bf16, in rows 2 t and 2 t + 1; their
+                                    // columns' maps: [0] of the first parts, [1] of the second
+  uint16_t* dx_rows;                // twin: dX, by plain stores
+  int64_t lddx;
   int32_t box_rows;                 // tokens in a box of dG's and dU's rows
   int32_t n_dx, n_dw;               // tiles of dX, times parts, and of both dW (0: not wanted)
   int32_t parts;                    // of the K of a tile of dX
@@ -206,6 +210,8 @@ int32_t gated_max_pairs();
 constexpr int kGatedMaxParts = 8, kGatedCounters = 16;
 constexpr int64_t kGatedPartFloats = 256 * 256;
 int64_t gated_dx_tiles(int64_t T, int64_t D);
+// Up to a CTA's 128 tokens a tile's other 128 rows are idle: dG and dU take two rows a token.
+inline bool gated_twin(int64_t T) { return T <= 128; }
 int32_t gated_parts(int64_t T, int64_t D, int64_t F);
 // fills n_dx, n_dw, parts and skip
 void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs);

@@ -34,7 +34,7 @@ def test_forward_refuses(lib, kw, status):
 
 @pytest.mark.parametrize("kw,status", [(k, s) for k, s in COMMON if "lddh" not in k] + [
     (dict(dH=0), 1), (dict(G=0), 1), (dict(X=0), 1), (dict(dWg=0), 1), (dict(dWu=0), 1),
-    (dict(ws=0), 1), (dict(ws_bytes=1023), 1), (dict(ws=0x10008), 3), (dict(dX=0x8008), 3),
+    (dict(ws=0), 1), (dict(ws_bytes=1535), 1), (dict(ws=0x10008), 3), (dict(dX=0x8008), 3),
     (dict(lddx=56), 2), (dict(lddwg=68), 3)])
 def test_backward_refuses(lib, kw, status):
     assert _call(lib.LIB.zo_gated_backward, BACKWARD, kw) == status and lib.zo_last_error()
@@ -48,11 +48,12 @@ def test_no_tokens_and_nothing_wanted_are_no_work(lib):
 
 def test_workspace(lib):
     ws = lib.LIB.zo_gated_workspace
-    assert ws(0, 64, 64) == 0 and ws(5, 64, 32) == 2 * 512
+    assert ws(0, 64, 64) == 0 and ws(5, 64, 32) == 2 * 768          # two rows a token
+    assert ws(200, 64, 32) == 2 * 12800
     assert ws(5, 64, 33) == 0 and ws(-1, 8, 8) == 0 and ws(5, 60, 32) == 0
     assert ws(4096, 4096, 11008) == 2 * 2 * 4096 * 11008
     # a tile of dX whose K of 2 x 16 stages is split in four, and its counters
-    assert ws(5, 64, 1024) == 2 * 5 * 1024 * 2 + 4 * 256 * 256 * 4 + 256
+    assert ws(5, 64, 1024) == 2 * 2 * 5 * 1024 * 2 + 4 * 256 * 256 * 4 + 256
 
 
 def test_binding_and_helpers_refuse_what_the_abi_cannot_see(lib):

@@ -352,3 +352,10 @@ def test_exponents_are_those_of_sums_of_rounded_products(lib, gpu, dtype):
     ev = np.frexp(v1.reshape(-1, 256).max(1))[1] - 1
     assert np.array_equal(state.m_exp.cpu().numpy(), em)
     assert np.array_equal(state.v_exp.cpu().numpy(), (ev >> 1) + 127)
+    # and so are the codes (those of normal numbers: below, products are rounded once more)
+    u = random_of(0, 0, 7, n)
+    for code, x, E in ((state.m, np.abs(m1), em), (state.v, np.sqrt(v1), (ev >> 1) + 127)):
+        y = x.astype(np.float64) * 2.0 ** np.repeat(134.0 - np.maximum(E, 40), 256)
+        step = 2.0 ** (np.floor(np.log2(np.maximum(y, 1e-30))) - 3)
+        normal = y >= 2.0 ** -6
+        assert np.array_equal(np.abs(f64(code))[normal], (np.floor(y / step + u) * step)[normal])

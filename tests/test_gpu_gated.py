@@ -6,7 +6,8 @@ pair; sixteen are added to the fp32 accumulator at a time, which rounds towards 
 (32 + |y|) 2^-22 of itself (the exponential's argument and the approximate functions).  H is off by its
 factors' errors (|act'| <= 1.13), dG = dH U s (1 + g y' (1 - s)) by the magnitudes of its terms.  dG
 and dU are rounded to bf16 (half a step, 2^-9): the reference rounds them too, and where their errors reach
-over a rounding's border the step between the two sides counts.  Every result is rounded once:
+over a rounding's border the step between the two sides counts; up to 128 tokens they are sums of two
+bf16, within 2^-17.  Every result is rounded once:
 2^-8 of it at most."""
 
 import numpy as np
@@ -78,7 +79,10 @@ def check_backward(got, dh, x, wg, wu, gate_, up, act):
     eU = dU.abs() * err
     parts = []
     for d, e in ((dG, eG), (dU, eU)):
-        parts.append((bf16(d), bf16(d + e) - bf16(d - e)))
+        if X.shape[0] <= 128:                            # sums of two bf16: 2^-9 of 2^-9
+            parts.append((d, e + 2.0 ** -17 * d.abs()))
+        else:
+            parts.append((bf16(d), bf16(d + e) - bf16(d - e)))
     (dGr, sG), (dUr, sU) = parts
     dx, dwg, dwu = got
     if dx is not None:
