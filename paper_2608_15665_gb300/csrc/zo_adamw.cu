@@ -396,8 +396,9 @@ struct Unit {
     }
     if constexpr (kEight) {
       const bool any = __shfl_sync(0xffffffffu, count, 0) > 0;
-      em = any ? t.Em[e0 / kBlock] : 0u;
-      ev = any ? t.Ev[e0 / kBlock] : 0u;
+      // (bytes of a line that other SMs write: from L2)
+      em = any ? __ldcg(t.Em + e0 / kBlock) : 0u;
+      ev = any ? __ldcg(t.Ev + e0 / kBlock) : 0u;
     }
   }
   // Through a warp's stage of shared memory: a lane takes what it has fetched itself.
@@ -511,8 +512,8 @@ __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int un
     uint32_t em = 0, ev = 0;                     // lane l: of block l
     if (lane < whole) {
       const int64_t block = begin / kBlock + (int64_t)lane * (kRow / kBlock);
-      em = t.Em[block];
-      ev = t.Ev[block];
+      em = __ldcg(t.Em + block);
+      ev = __ldcg(t.Ev + block);
     }
 #pragma unroll
     for (int q = 0; q < kStages - 1; ++q) {

@@ -333,9 +333,11 @@ gradient_kernel(const Rows a, const float* __restrict__ lse, const float* __rest
                 const float* __restrict__ dloss, T* out, int64_t ldo) {
   const int part = (int)(blockIdx.x % (unsigned)a.parts);
   const int64_t row = blockIdx.x / (unsigned)a.parts;
-  const int j0 = part * a.part_cols, n = min(a.part_cols, a.vocab - j0);
+  const int64_t j0 = (int64_t)part * a.part_cols;
+  const int n = (int)min((int64_t)a.part_cols, a.vocab - j0);
   zo::pdl_wait();
   zo::pdl_trigger();
+  if (n <= 0) return;                              // (many parts, each rounded up to eight columns)
   const int64_t label = a.labels[row];
   const float scale = label < 0 ? 0.0f : dlogp[row] * (dloss ? *dloss : 1.0f);
   const float base = lse[row];

@@ -366,6 +366,9 @@ class AdamW(_Handle):
                                  "the count on the device gives the step its number")
             self._call(zb.zo_adamw_step, 0, self.count, lr, betas[0], betas[1], eps, weight_decay)
             return
+        if torch.cuda.is_current_stream_capturing():
+            raise zb.ZoError(zb.ZO_ERR_INVALID_ARG, "AdamW.step", "a captured step would take the "
+                             "same number at every replay: give the handle a count on the device")
         t = self.steps + 1 if t is None else int(t)
         self._call(zb.zo_adamw_step, t, None, lr, betas[0], betas[1], eps, weight_decay)
         self.steps = t

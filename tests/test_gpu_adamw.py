@@ -259,6 +259,8 @@ def test_a_count_on_the_device_and_a_replayed_graph(lib, gpu):
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=s):
             opt.step(LR)
+            with pytest.raises(lib.ZoError):            # without a count: the same number every time
+                want.step(LR)
         want.step(LR)
         for k in range(3):
             for x in (G, G2):
