@@ -162,7 +162,10 @@ enum GatedAct : int32_t { kGatedSilu = 0, kGatedGelu = 1 };
 #ifdef __CUDACC__
 __device__ __forceinline__ float gated_gate(float g, int32_t act) {
   const float y = act == kGatedSilu ? g : 1.5957691216057308f * g * fmaf(0.044715f * g, g, 1.0f);
-  return __fdividef(1.0f, 1.0f + __expf(-y));
+  float e, s;                       // (without the library forms' care for subnormal numbers)
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950408889634f * y));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+  return s;
 }
 #endif
 
