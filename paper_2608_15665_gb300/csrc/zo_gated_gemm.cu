@@ -25,8 +25,10 @@
 // panels in use, 160 MB at 4096 tokens, came from HBM once for every tile: dWg and dWu of the 7B
 // shapes 525 us.)
 //
-// Bound by the operands' way from L2 to the SMs and the power cap's clock; few tokens by the
-// weights' way from HBM.  Accumulators are fp32 (the tensor cores' sums round towards zero: 2^-23
+// Bound by the power cap's clock and the operands' way from L2 to the SMs (4096 tokens on the 7B
+// shapes: 366 us forward in a short run, 1.65 PFLOP/s and 447 us in a long one, where cuBLAS takes 443
+// for the two products alone; tensor pipe 90% of active cycles forward, 95% backward); few tokens by
+// the weights' way from HBM (one token: 34 us, 5.3 TB/s).  Accumulators are fp32 (the tensor cores' sums round towards zero: 2^-23
 // of the sum's running size a step, far below bf16's 2^-9).
 //
 // Roles (320 threads per CTA, one CTA per SM):
@@ -636,8 +638,8 @@ int32_t gated_box_rows(int64_t T) { return (int32_t)std::min<int64_t>(128, (T + 
 // MMAs (128 cycles for 16 of K and N = 256, and not below 90) and their operands' way from L2 (~54
 // bytes a cycle), and epilogues of ~100 cycles a column, under the next tile's stages where there
 // are two accumulators.  Measured, the one kind of tile against the other (D = 4096, F = 11008): 1
-// token 38 us, turned 35; 128 tokens 40.5, 39; 256 41, 46; 300 58, 55; 512 60, 66; 4096 381, 414;
-// and 777 x 5120 x 13824 153, 134.
+// token 38 us, turned 35; 128 tokens 40, 39; 256 41, 46; 300 57, 56; 512 58, 65; 4096 366, 397; and
+// 777 x 5120 x 13824 149, 130.
 GatedPlan gated_plan(int64_t T, int64_t D, int64_t F, int32_t pairs) {
   GatedPlan best{128, 0};
   int64_t least = INT64_MAX;
