@@ -80,9 +80,11 @@ __global__ void __launch_bounds__(kThreads) gated_gradients_kernel(const Gradien
   for (int i = 0; i < 8; ++i) {
     const float x = value(g, i), d = value(dh, i);
     const float s = zo::gated_gate(x, a.act);
-    // the argument's derivative: 1, or 2 sqrt(2 / pi) (1 + 3 0.044715 x^2)
-    const float y1 = a.act == zo::kGatedSilu ? 1.0f : fmaf(0.2140644488f * x, x, 1.5957691216f);
-    const float slope = s * fmaf(x * y1, 1.0f - s, 1.0f);
+    // the argument's derivative: 1, or 2 sqrt(2 / pi) (1 + 3 0.044715 x^2), of which no more than
+    // |x| = 64 is needed: s is 0 or 1 there, and x's powers stay in range
+    const float z = a.act == zo::kGatedSilu ? x : fminf(fmaxf(x, -64.0f), 64.0f);
+    const float y1 = a.act == zo::kGatedSilu ? 1.0f : fmaf(0.2140644488f * z, z, 1.5957691216f);
+    const float slope = s * fmaf(z * y1, 1.0f - s, 1.0f) + (x - x);   // (NaN and infinity stay NaN)
     dg[i] = d * value(u, i) * slope;
     du[i] = d * x * s;
   }

@@ -152,6 +152,17 @@ def test_far_values_and_nan(lib, gpu):
         dh = make(64, 64, gpu, 4)
         got = fo.gated_linear_backward(dh, x, big, wu, out.gate, out.up, act)
         check_backward(got, dh, x, big, wu, out.gate, out.up, act)
+        # gates as far as bf16 goes: the slope is 0 or 1
+        g = torch.full((64, 64), 1e30, dtype=BF, device=gpu)
+        g[::2] = -1e30
+        g[1::4] = 100.0
+        one = torch.ones_like(g)
+        dx, dwg, dwu = fo.gated_linear_backward(one, x, wg, wu, g, one, act)
+        want = (g > 0).double().t() @ x.double()
+        assert float((dwg.double() - want).abs().max()) <= 2.0 ** -8 * float(want.abs().max()) + 1e-6
+        g[3, 4] = float("nan")
+        dwg = fo.gated_linear_backward(one, x, wg, wu, g, one, act, want_x=False)[1]
+        assert torch.isnan(dwg[4]).all() and torch.isfinite(dwg[:4]).all() and torch.isfinite(dwg[5:]).all()
     x2, wu2 = x.clone(), wu.clone()
     x2[5, 3], wu2[7, 2] = float("nan"), float("inf")
     h = fo.gated_linear(x2, wg, wu2).h

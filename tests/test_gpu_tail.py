@@ -116,3 +116,49 @@ def test_steps_of_a_tail_follow_64_bits(lib, gpu, bits):
     muon.sync()
     muon.close()
     assert all(l == l for l in losses)
+
+
+def test_calls_at_once_on_two_streams(lib, gpu):
+    """Blocks, losses and AdamW handles on two streams at the same time: the bits of calls alone."""
+    from paper_2608_15665_gb300 import firstorder as fo
+    g = torch.Generator().manual_seed(3)
+    x = [torch.randn(t, 128, generator=g).to(BF).to(gpu) for t in (100, 700)]
+    wg, wu = (torch.randn(1032, 128, generator=g).mul_(0.1).to(BF).to(gpu) for _ in range(2))
+    logits = [torch.randn(40, v, generator=g).to(gpu) for v in (900, 33000)]
+    labels = torch.randint(0, 900, (40,), generator=g).to(gpu)
+    offsets = torch.tensor([0, 9, 23, 34, 40], device=gpu)
+
+    def work(k, handle):
+        out = fo.gated_linear(x[k], wg, wu, save=True)
+        grads = fo.gated_linear_backward(out.h, x[k], wg, wu, out.gate, out.up)
+        got = fo.preference_loss(logits[k], labels, offsets)
+        d = fo.preference_loss_backward(logits[k], labels, got.lse, got.dlogp)
+        handle.step(lr=1e-2)
+        return [out.h, *grads, got.loss, got.logps, d]
+
+    def handles():
+        out = []
+        for k in range(2):
+            W = torch.arange(50000, device=gpu, dtype=torch.float32) * 1e-5 * (k + 1)
+            out.append(fo.AdamW([W], [torch.sin(W)], bits=8, seed=k))
+        torch.cuda.synchronize()
+        return out
+    alone = handles()
+    want = [work(k, alone[k]) for k in range(2)]
+    for _ in range(3):
+        for h in alone:
+            h.step(lr=1e-2)
+    torch.cuda.synchronize()
+    pair = handles()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for _ in range(4):
+        for k, s in enumerate(streams):
+            s.wait_stream(torch.cuda.default_stream())
+            with torch.cuda.stream(s):
+                got[k] = work(k, pair[k])
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(got[k], want[k]))
+        assert torch.equal(pair[k].weights[0], alone[k].weights[0])
+    fo.gated_linear_sync()
