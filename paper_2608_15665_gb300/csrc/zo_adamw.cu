@@ -5,7 +5,7 @@
 //   W <- rnd((1 - lr wd) W - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps))
 //
 // Bound by HBM with fp32 states (50M bf16 elements, 22 bytes each: 159 us, 103% of the copy rate), by
-// instruction issue with 8-bit ones (131M: 247 us, 79%): W is read and written, g read, the states
+// instruction issue with 8-bit ones (131M: 245 us, 79%): W is read and written, g read, the states
 // read and written, once each.  A warp
 // works on blocks of 256 neighbouring elements, eight to a lane; a CTA on a chunk of one tensor,
 // found in a table of the chunks.
@@ -344,20 +344,17 @@ __device__ __forceinline__ float root_of(float v) {
   return r;
 }
 // Square roots rounded to nearest, of 2^-102 <= v < infinity (smaller ones to 2^-22 of them, or of
-// 2^-63): the hardware's reciprocal root y, s = v y, and
-// one Newton step by the residual, s + (v - s^2) y / 2 (Markstein, IBM J. Res. Dev. 34, 1990), with the
-// sign of s turned.  So a state's codes are those of any other fp32 evaluation.  (Infinity gives NaN,
-// which its code would be in any case.)
+// 2^-63): the hardware's reciprocal root y, s = v y, and one Newton step by the residual,
+// s + (v - s^2) y / 2 (Markstein, IBM J. Res. Dev. 34, 1990).  So a state's codes are those of any
+// other fp32 evaluation.  (Infinity gives NaN, which its code would be in any case.)
 __device__ __forceinline__ float2 rounded_roots(float2 v) {
   const float2 u = zo::add2(v, both(0x1p-126f));      // (0 has no reciprocal root; others keep theirs)
   float2 y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(u.x));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(u.y));
-  const float2 ny = make_float2(-y.x, -y.y), ns = zo::mul2(v, ny);
-  // v - s^2 as -(s s - v); then -(s + (v - s^2) y / 2)
-  const float2 rest = zo::fma2(ns, ns, make_float2(-v.x, -v.y));
-  const float2 nr = zo::fma2(rest, zo::mul2(y, both(0.5f)), ns);
-  return make_float2(-nr.x, -nr.y);
+  const float2 s = zo::mul2(v, y);
+  const float2 rest = zo::fma2(zo::mul2(s, both(-1.0f)), s, v);
+  return zo::fma2(rest, zo::mul2(y, both(0.5f)), s);
 }
 __device__ __forceinline__ float reciprocal(float v) {
   float r;
@@ -406,18 +403,16 @@ struct Unit {
   // Through a warp's stage of shared memory: a lane takes what it has fetched itself.
   static constexpr int g_at() { return 32 * kLane * (int)sizeof(W); }
   static constexpr int m_at() { return g_at() + 32 * kLane * (int)sizeof(G); }
-  static __device__ __forceinline__ void fetch(const Tensor& t, int64_t e0, uint8_t* stage) {
+  static __device__ __forceinline__ void fetch(const W* pw, const G* pg, const S* pm, const S* pv,
+                                               uint8_t* stage) {
     const int lane = threadIdx.x & 31;
-    Raw<W>::fetch(stage + 16 * lane, static_cast<const W*>(t.W) + e0);
-    Raw<G>::fetch(stage + g_at() + 16 * lane, static_cast<const G*>(t.G) + e0);
-    Raw<S>::fetch(stage + m_at() + 8 * lane, static_cast<const S*>(t.M) + e0);
-    Raw<S>::fetch(stage + m_at() + 256 + 8 * lane, static_cast<const S*>(t.V) + e0);
+    Raw<W>::fetch(stage + 16 * lane, pw);
+    Raw<G>::fetch(stage + g_at() + 16 * lane, pg);
+    Raw<S>::fetch(stage + m_at() + 8 * lane, pm);
+    Raw<S>::fetch(stage + m_at() + 256 + 8 * lane, pv);
   }
-  __device__ __forceinline__ void take(const Tensor& t, int64_t first, const uint8_t* stage,
-                                       uint32_t e_m, uint32_t e_v) {
+  __device__ __forceinline__ void take(const uint8_t* stage, uint32_t e_m, uint32_t e_v) {
     const int lane = threadIdx.x & 31;
-    e0 = first;
-    count = kLane;
     w.take(stage + 16 * lane);
     g.take(stage + g_at() + 16 * lane);
     m.take(stage + m_at() + 8 * lane);
@@ -426,7 +421,8 @@ struct Unit {
     ev = e_v;
   }
 
-  __device__ __forceinline__ void finish(const Tensor& t, uint32_t index, const Step& st, const Now& now) {
+  // word: of the lane's eight elements in the stream of random words
+  __device__ __forceinline__ void compute(uint32_t word, uint32_t index, const Step& st, const Now& now) {
     float x[kLane], y[kLane], a[kLane], b[kLane];
     unpack(g, y);
     if constexpr (kEight) {
@@ -460,23 +456,29 @@ struct Unit {
     }
     pack(x, w);
     if constexpr (kEight) {
-      const uint32_t first = __shfl_sync(0xffffffffu, (uint32_t)(count > 0), 0);
       bool odd_m, odd_v;
       const uint32_t tm = largest<true>(a, &odd_m), tv = largest<false>(b, &odd_v);
       // 2^k <= r < 2^(k + 1) where 2^2k <= v < 2^(2k + 2)
       em = tm >> 23;
       ev = tv >> 23 ? (uint32_t)((((int)(tv >> 23) - 127) >> 1) + 127) : 0u;
       const uint4 random = random_words(
-          make_uint4((uint32_t)(e0 / kLane), index, now.t, kTagAdamW << 24), st.key);
+          make_uint4(word, index, now.t, kTagAdamW << 24), st.key);
       encode<true>(a, em, odd_m, random, m);
       encode<false>(y, ev, odd_v, random, v);
-      if (first && (threadIdx.x & 31) == 0) {
-        t.Em[e0 / kBlock] = (uint8_t)em;
-        t.Ev[e0 / kBlock] = (uint8_t)ev;
-      }
     } else {
       pack(a, m);
       pack(b, v);
+    }
+  }
+
+  __device__ __forceinline__ void finish(const Tensor& t, uint32_t index, const Step& st, const Now& now) {
+    compute((uint32_t)(e0 / kLane), index, st, now);
+    if constexpr (kEight) {
+      const bool any = __shfl_sync(0xffffffffu, count, 0) > 0;
+      if (any && (threadIdx.x & 31) == 0) {
+        t.Em[e0 / kBlock] = (uint8_t)em;
+        t.Ev[e0 / kBlock] = (uint8_t)ev;
+      }
     }
     W* pw = static_cast<W*>(t.W);
     S *pm = static_cast<S*>(t.M), *pv = static_cast<S*>(t.V);
@@ -496,7 +498,8 @@ struct Unit {
 // as long as its loads, whole blocks of aligned tensors come through shared memory, the next one's
 // loads under this one's arithmetic: with loads into registers 24 warps an SM waited half of their
 // time (131M elements, bf16: 386 us; through shared memory 247 with three blocks ahead and 24 warps,
-// 229 with two and 28, 247 with roots rounded to nearest: 450 instructions a block, 3.0 a cycle).
+// 229 with two and 28, 245 with roots rounded to nearest: 460 instructions a block, 2.9 a cycle,
+// the FMA and the ALU pipe each busy half of the time and in turn in the warps' way).
 template <bool kEight, typename W, typename G>
 __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int units, uint32_t index,
                                           const Step& st, const Now& now) {
@@ -512,25 +515,38 @@ __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int un
     const int whole = !t.wide || t.n < begin + kBlock ? 0
                       : (int)min((int64_t)units, (t.n - begin - kBlock) / kRow + 1);
     uint32_t em = 0, ev = 0;                     // lane l: of block l
+    const int64_t block = begin / kBlock + (int64_t)lane * (kRow / kBlock);
     if (lane < whole) {
-      const int64_t block = begin / kBlock + (int64_t)lane * (kRow / kBlock);
       em = __ldcg(t.Em + block);
       ev = __ldcg(t.Ev + block);
     }
+    using U = Unit<kEight, W, G>;
+    W* const pw = static_cast<W*>(t.W) + e0;
+    const G* const pg = static_cast<const G*>(t.G) + e0;
+    uint8_t *const pm = static_cast<uint8_t*>(t.M) + e0, *const pv = static_cast<uint8_t*>(t.V) + e0;
+    const uint32_t word = (uint32_t)(e0 / kLane);
+    const auto fetch = [&](int q) {
+      const int o = q * kRow;
+      if (q < whole) U::fetch(pw + o, pg + o, pm + o, pv + o, mine + q % kStages * kStageBytes);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
 #pragma unroll
-    for (int q = 0; q < kStages - 1; ++q) {
-      if (q < whole) Unit<kEight, W, G>::fetch(t, e0 + (int64_t)q * kRow, mine + q * kStageBytes);
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
+    for (int q = 0; q < kStages - 1; ++q) fetch(q);
     for (; k < whole; ++k) {
-      if (k + kStages - 1 < whole)
-        Unit<kEight, W, G>::fetch(t, e0 + (int64_t)(k + kStages - 1) * kRow,
-                                  mine + (k + kStages - 1) % kStages * kStageBytes);
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      fetch(k + kStages - 1);
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-      u.take(t, e0 + (int64_t)k * kRow, mine + k % kStages * kStageBytes,
-             __shfl_sync(0xffffffffu, em, k), __shfl_sync(0xffffffffu, ev, k));
-      u.finish(t, index, st, now);
+      u.take(mine + k % kStages * kStageBytes, __shfl_sync(0xffffffffu, em, k),
+             __shfl_sync(0xffffffffu, ev, k));
+      u.compute(word + (uint32_t)(k * (kRow / kLane)), index, st, now);
+      const int o = k * kRow;
+      u.w.store(pw + o);
+      u.m.store(pm + o);
+      u.v.store(pv + o);
+      if (lane == k) em = u.em, ev = u.ev;
+    }
+    if (lane < whole) {
+      t.Em[block] = (uint8_t)em;
+      t.Ev[block] = (uint8_t)ev;
     }
   }
   for (; k < units; ++k) {
