@@ -178,36 +178,52 @@ zo_status zo_gated_forward(const void* X, int64_t ldx, int64_t T, int64_t D, con
   const int32_t pairs = zo::gated_max_pairs();
   uint32_t* status = status_word();
   if (pairs <= 0 || !status) return refuse(ZO_ERR_CUDA, "zo_gated_forward: no usable CUDA device");
-  const zo::GatedPlan plan = zo::gated_plan(T, D, F, pairs);
-  const bool turned = plan.side == 0;
-  const auto fill = [&](auto& a, uint32_t x_rows, uint32_t w_rows) {
+  void* const out[3] = {H, G, U};
+  const int64_t ld[3] = {ldh, ldg, ldu};
+  const int outs = G ? 3 : 1;
+  const auto s = reinterpret_cast<cudaStream_t>(stream);
+  const char* const no_map = "zo_gated_forward: cuTensorMapEncodeTiled rejected a descriptor";
+  const auto sizes = [&](auto& a) {
     a.T = (int32_t)T;
     a.D = (int32_t)D;
     a.F = (int32_t)F;
     a.act = act == ZO_GATED_SILU ? zo::kGatedSilu : zo::kGatedGelu;
     a.save = G != nullptr;
-    void* out[3] = {H, G, U};
-    const int64_t ld[3] = {ldh, ldg, ldu};
-    bool ok = map_of(&a.x, X, D, T, ldx, 64, x_rows) && map_of(&a.w[0], Wg, D, F, ldwg, 64, w_rows) &&
-              map_of(&a.w[1], Wu, D, F, ldwu, 64, w_rows);
-    for (int k = 0; k < (G ? 3 : 1); ++k)
-      ok = ok && (turned ? map_of(&a.out[k], out[k], F, T, ld[k], zo::kGatedOutRows, zo::kGatedOutCols,
-                                  CU_TENSOR_MAP_SWIZZLE_64B)
-                         : out_map(&a.out[k], out[k], F, T, ld[k]));
-    return ok;
   };
-  const auto s = reinterpret_cast<cudaStream_t>(stream);
-  const char* const no_map = "zo_gated_forward: cuTensorMapEncodeTiled rejected a descriptor";
-  if (turned) {
+  const auto maps = [&](auto& a, uint32_t x_rows, uint32_t w_rows) {
+    return map_of(&a.x, X, D, T, ldx, 64, x_rows) && map_of(&a.w[0], Wg, D, F, ldwg, 64, w_rows) &&
+           map_of(&a.w[1], Wu, D, F, ldwu, 64, w_rows);
+  };
+  zo::GatedFew few{};
+  sizes(few);
+  if (zo::gated_few_plan(&few, 2 * pairs)) {
+    for (int k = 0; k < outs; ++k) {
+      few.out[k] = static_cast<uint16_t*>(out[k]);
+      few.ld[k] = ld[k];
+    }
+    if (!maps(few, few.box_rows, few.cols)) return refuse(ZO_ERR_CUDA, no_map);
+    ZO_CUDA(zo::launch_gated_few(few, status, s), "gated forward kernel");
+    return ZO_OK;
+  }
+  const zo::GatedPlan plan = zo::gated_plan(T, D, F, pairs);
+  if (plan.side == 0) {
     zo::GatedTurned a{};
+    sizes(a);
     a.tokens = plan.tokens;
-    if (!fill(a, plan.tokens / 2, 128)) return refuse(ZO_ERR_CUDA, no_map);
+    bool ok = maps(a, plan.tokens / 2, 128);
+    for (int k = 0; k < outs; ++k)
+      ok = ok && map_of(&a.out[k], out[k], F, T, ld[k], zo::kGatedOutRows, zo::kGatedOutCols,
+                        CU_TENSOR_MAP_SWIZZLE_64B);
+    if (!ok) return refuse(ZO_ERR_CUDA, no_map);
     ZO_CUDA(zo::launch_gated_turned(a, pairs, status, s), "gated forward kernel");
   } else {
     zo::GatedForward a{};
+    sizes(a);
     a.side = plan.side;
     a.box_rows = zo::gated_box_rows(T);
-    if (!fill(a, a.box_rows, a.side)) return refuse(ZO_ERR_CUDA, no_map);
+    bool ok = maps(a, a.box_rows, a.side);
+    for (int k = 0; k < outs; ++k) ok = ok && out_map(&a.out[k], out[k], F, T, ld[k]);
+    if (!ok) return refuse(ZO_ERR_CUDA, no_map);
     ZO_CUDA(zo::launch_gated_forward(a, pairs, status, s), "gated forward kernel");
   }
   return ZO_OK;

@@ -1,8 +1,8 @@
 // The products of the gated linear block on SM pairs: M = 256 tcgen05.mma.cta_group::2 across the
 // two SMs of a cluster, bf16 operands, fp32 accumulators in Tensor Memory.
 //
-//   forward:  tile = 256 tokens x `side` columns of G and the same of U.  CTA c of the pair holds
-//             128 of the tokens, and its half of the B operand is `side` rows of Wg (c = 0) or of
+//   forward:  (beyond 128 tokens; below, zo_gated_few.cu) tile = 256 tokens x `side` columns of G and
+//             the same of U.  CTA c of the pair holds 128 of the tokens, and its half of the B operand is `side` rows of Wg (c = 0) or of
 //             Wu (c = 1): accumulator columns 0 .. side - 1 are G's, the next `side` U's, in both
 //             CTAs, and the epilogue has both of an element in one thread.
 //   turned:   the forward pass with the tokens as the MMAs' columns: tile = 256 columns of G and the
@@ -27,9 +27,9 @@
 //
 // Bound by the power cap's clock and the operands' way from L2 to the SMs (4096 tokens on the 7B
 // shapes: 366 us forward in a short run, 1.65 PFLOP/s and 447 us in a long one, where cuBLAS takes 443
-// for the two products alone; tensor pipe 90% of active cycles forward, 95% backward); few tokens by
-// the weights' way from HBM (one token: 34 us, 5.3 TB/s).  Accumulators are fp32 (the tensor cores' sums round towards zero: 2^-23
-// of the sum's running size a step, far below bf16's 2^-9).
+// for the two products alone; tensor pipe 90% of active cycles forward, 95% backward).  Accumulators
+// are fp32 (the tensor cores' sums round towards zero: 2^-23 of the sum's running size a step, far
+// below bf16's 2^-9).
 //
 // Roles (320 threads per CTA, one CTA per SM):
 //   warp 0:     an elected lane is the TMA producer of this CTA's halves; both halves of a stage
@@ -637,9 +637,9 @@ int32_t gated_box_rows(int64_t T) { return (int32_t)std::min<int64_t>(128, (T + 
 // The busiest pair's cycles: rounds of tiles, each D / 64 stages that take the longer of their
 // MMAs (128 cycles for 16 of K and N = 256, and not below 90) and their operands' way from L2 (~54
 // bytes a cycle), and epilogues of ~100 cycles a column, under the next tile's stages where there
-// are two accumulators.  Measured, the one kind of tile against the other (D = 4096, F = 11008): 1
-// token 38 us, turned 35; 128 tokens 40, 39; 256 41, 46; 300 57, 56; 512 58, 65; 4096 366, 397; and
-// 777 x 5120 x 13824 149, 130.
+// are two accumulators.  Measured, the one kind of tile against the other (D = 4096, F = 11008): 256
+// tokens 41 us, turned 46; 300 57, 56; 512 58, 65; 4096 366, 397; and 777 x 5120 x 13824 149, 130.
+// (Up to 128 tokens zo_gated_few.cu is faster than either: 31 us at one token, 38 and 35 here.)
 GatedPlan gated_plan(int64_t T, int64_t D, int64_t F, int32_t pairs) {
   GatedPlan best{128, 0};
   int64_t least = INT64_MAX;

@@ -181,6 +181,15 @@ struct GatedTurned {
   int32_t T, D, F, act, save;
   int32_t tokens;                   // of a tile: a multiple of 16
 };
+// the same for at most 128 tokens (zo_gated_few.cu)
+struct GatedFew {
+  CUtensorMap x, w[2];
+  uint16_t* out[3];                 // H, G and U
+  int64_t ld[3];
+  int32_t T, D, F, act, save;
+  int32_t cols, box_rows;           // of a CTA: columns of H; tokens in a box of X
+  int32_t stages, tmem_cols;
+};
 struct GatedBackward {
   CUtensorMap d_rows[2], w_cols[2], dx;           // dX: dG, dU along F; Wg, Wu by rows of F
   CUtensorMap d_cols[2][2], x_cols, dw[2];        // dW: dG, dU and X by rows of T
@@ -219,6 +228,9 @@ int32_t gated_parts(int64_t T, int64_t D, int64_t F);
 // fills n_dx, n_dw, parts and skip
 void gated_deal(GatedBackward* a, bool want_x, bool want_w, int32_t pairs);
 cudaError_t launch_gated_forward(const GatedForward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
+// fills cols, box_rows, stages and tmem_cols; false: more than 128 tokens
+bool gated_few_plan(GatedFew* a, int32_t sms);
+cudaError_t launch_gated_few(const GatedFew& a, uint32_t* status, cudaStream_t s);
 cudaError_t launch_gated_turned(const GatedTurned& a, int32_t pairs, uint32_t* status, cudaStream_t s);
 cudaError_t launch_gated_backward(const GatedBackward& a, int32_t pairs, uint32_t* status, cudaStream_t s);
 

@@ -97,7 +97,8 @@ def check_backward(got, dh, x, wg, wu, gate_, up, act):
 
 SHAPES = [(1, 8, 8), (1, 64, 64), (3, 72, 200), (2, 520, 1000), (16, 256, 264), (17, 128, 2056),
           (128, 264, 96), (129, 136, 512), (255, 64, 16), (256, 512, 128), (300, 200, 1000),
-          (1000, 1024, 2816), (2500, 72, 2000), (5000, 64, 520), (700, 8, 4104), (40, 4096, 304), (77, 600, 3000)]
+          (1000, 1024, 2816), (2500, 72, 2000), (5000, 64, 520), (700, 8, 4104), (40, 4096, 304), (77, 600, 3000),
+          (30, 128, 21000), (128, 64, 20000), (130, 72, 4104)]
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
@@ -118,6 +119,29 @@ def test_both_passes_match_the_formulas(lib, gpu, T, D, F, pad, act):
     assert none is None and torch.equal(dx, got[0])
     none, dwg, dwu = fo.gated_linear_backward(dh, x, wg, wu, out.gate, out.up, act, want_x=False)
     assert none is None and torch.equal(dwg, got[1]) and torch.equal(dwu, got[2])
+    fo.gated_linear_sync()
+
+
+@pytest.mark.parametrize("T,D,F,act", [(513, 2048, 4000, "silu"), (290, 3000, 11008, "gelu"),
+                                       (777, 5120, 13824, "gelu"), (1100, 1024, 11008, "silu")])
+def test_forward_in_several_rounds_of_tiles(lib, gpu, T, D, F, act):
+    """Both kinds of tile, with one accumulator and with two, more tiles than SM pairs."""
+    from paper_2608_15665_gb300 import firstorder as fo
+    x, wg, wu = inputs(T, D, F, gpu)
+    check_forward(fo.gated_linear(x, wg, wu, act, save=True), x, wg, wu, act)
+    fo.gated_linear_sync()
+
+
+def test_backward_in_several_rounds_of_tiles(lib, gpu):
+    """More tiles of dX than SM pairs, and dW's dealt around the last ones; repeated, the same bits."""
+    from paper_2608_15665_gb300 import firstorder as fo
+    T, D, F = 2304, 4096, 1032
+    x, wg, wu = inputs(T, D, F, gpu)
+    out = fo.gated_linear(x, wg, wu, save=True)
+    dh = make(T, F, gpu, 4, 0.1)
+    runs = [fo.gated_linear_backward(dh, x, wg, wu, out.gate, out.up) for _ in range(6)]
+    check_backward(runs[0], dh, x, wg, wu, out.gate, out.up, "silu")
+    assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(r, runs[0]))
     fo.gated_linear_sync()
 
 
