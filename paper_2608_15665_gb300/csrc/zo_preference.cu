@@ -34,6 +34,9 @@ constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kPairThreads = 512;                // of a pair's two sequences
 constexpr int kUnroll = 4;                       // vectors of 16 bytes a thread has on their way
 constexpr int kMaxParts = 32, kPartCols = 4096;  // parts of a row, none narrower than this
+// Rows of up to so many bytes belong to a warp each (256M logits in bf16, forward: rows of 1000 487 us
+// by CTAs, 153 by warps; of 8000 104 and 93; backward of 1000 259 and 168, of 8000 152 and 158).
+constexpr int kShortForward = 16384, kShortBackward = 8192;
 // columns of a CTA's part in the backward pass (812 rows of 50257 fp32: 52 us; in whole rows 58, as 5.3
 // rows an SM are 6 for some)
 constexpr int kGradCols = 8192;
@@ -92,13 +95,16 @@ struct Vec {
   }
 };
 
+// live: how many of the vectors any thread of the team has (the same in all of them).  fp32's four
+// values are too few for a branch around them (rows of 1000: 216 us with it, 177 without).
 template <typename T>
-__device__ __forceinline__ void add(Sum& a, const Vec<T> (&v)[kUnroll]) {
+__device__ __forceinline__ void add(Sum& a, const Vec<T> (&v)[kUnroll], int live) {
   float top = v[0].get(0);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u)
+    if (sizeof(T) == 4 || u < live)
 #pragma unroll
-    for (int i = 0; i < Vec<T>::kN; ++i) top = fmaxf(top, v[u].get(i));
+      for (int i = 0; i < Vec<T>::kN; ++i) top = fmaxf(top, v[u].get(i));
   const float c = fmaxf(a.c, top);
   a.s *= expf(a.c - c);
   a.c = c;
@@ -108,12 +114,13 @@ __device__ __forceinline__ void add(Sum& a, const Vec<T> (&v)[kUnroll]) {
   float2 s = make_float2(a.s, 0.0f);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u)
+    if (sizeof(T) == 4 || u < live)
 #pragma unroll
-    for (int i = 0; i < Vec<T>::kN; i += 2) {
-      const float2 d = zo::add2(make_float2(v[u].get(i), v[u].get(i + 1)), less);
-      const float2 e = zo::fma2(d, scale, zo::mul2(d, rest));
-      s = zo::add2(s, make_float2(exp2_approx(e.x), exp2_approx(e.y)));
-    }
+      for (int i = 0; i < Vec<T>::kN; i += 2) {
+        const float2 d = zo::add2(make_float2(v[u].get(i), v[u].get(i + 1)), less);
+        const float2 e = zo::fma2(d, scale, zo::mul2(d, rest));
+        s = zo::add2(s, make_float2(exp2_approx(e.x), exp2_approx(e.y)));
+      }
   a.s = s.x + s.y;
 }
 __device__ __forceinline__ void add(Sum& a, float x) {
@@ -129,22 +136,23 @@ __device__ __forceinline__ int head_of(const T* p, int n) {
 }
 
 // The rows' sums.  parts > 1: every part's to partial; else lse and logp.  Rows that do not count
-// get zeros.  A CTA per row (part): rows that do not count lie together, and with a fixed number of
+// get zeros.  A team per row (part): a CTA, or a warp where a row is short.  Rows that do not count lie together, and with a fixed number of
 // rows to a CTA the busiest had a third more to read than the others (16 pairs: 190 us).
-template <typename T>
+template <typename T, int kTeam>
 __global__ void __launch_bounds__(kThreads)
 rows_kernel(const Rows a, Sum* __restrict__ partial, float* __restrict__ logp,
             float* __restrict__ lse, float* __restrict__ dlogp, uint32_t* __restrict__ ticket) {
   __shared__ Sum warp_sums[kWarps];
+  const int member = threadIdx.x % kTeam;
   const int part = (int)(blockIdx.x % (unsigned)a.parts);
-  const int64_t row = blockIdx.x / (unsigned)a.parts;
+  const int64_t row = blockIdx.x / (unsigned)a.parts * (int64_t)(kThreads / kTeam) + threadIdx.x / kTeam;
   zo::pdl_wait();
   zo::pdl_trigger();
   if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
   if (row >= a.rows) return;
   const int64_t label = a.labels[row];
   const bool counted = label >= 0 && row >= a.offsets[0] && row < a.offsets[2 * a.pairs];
-  if (threadIdx.x == 0 && part == 0) {
+  if (member == 0 && part == 0) {
     if (!counted) logp[row] = 0.0f;
     if (!counted && lse) lse[row] = 0.0f;
     if (dlogp) dlogp[row] = 0.0f;                // (of counted rows: until the pairs' kernel)
@@ -152,37 +160,47 @@ rows_kernel(const Rows a, Sum* __restrict__ partial, float* __restrict__ logp,
   if (!counted) return;
   const int j0 = part * a.part_cols, n = min(a.part_cols, a.vocab - j0);
   const T* x = static_cast<const T*>(a.x) + row * a.ld + j0;
+  const bool whole = a.parts == 1 && member == 0;
+  const float hit = whole && label < a.vocab ? static_cast<float>(x[label]) : __int_as_float(0x7FC00000);
   Sum sum{kLowest, 0.0f};
   const int head = head_of(x, n);
   const int vecs = (n - head) / Vec<T>::kN;
   const T* xv = x + head;
-  for (int i = threadIdx.x; i < vecs; i += kUnroll * kThreads) {
+  for (int i = member; i < vecs; i += kUnroll * kTeam) {
     Vec<T> v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       v[u].clear();
-      if (i + u * kThreads < vecs) v[u].load(xv + (int64_t)(i + u * kThreads) * Vec<T>::kN);
+      if (i + u * kTeam < vecs) v[u].load(xv + (int64_t)(i + u * kTeam) * Vec<T>::kN);
     }
-    add(sum, v);
+    add(sum, v, (vecs - (i - member) + kTeam - 1) / kTeam);
   }
   // what lies around the vectors
   const int around = head + (n - head) % Vec<T>::kN;
-  if ((int)threadIdx.x < around) {
-    const int k = (int)threadIdx.x < head ? (int)threadIdx.x : n - around + (int)threadIdx.x;
+  if (member < around) {
+    const int k = member < head ? member : n - around + member;
     add(sum, static_cast<float>(x[k]));
   }
+  // the warp's common base first, then its sum
+  float c = sum.c;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1)
-    sum = join(sum, Sum{__shfl_xor_sync(0xffffffffu, sum.c, d), __shfl_xor_sync(0xffffffffu, sum.s, d)});
-  if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kWarps; ++w) sum = join(sum, warp_sums[w]);
+  for (int d = 16; d > 0; d >>= 1) c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, d));
+  sum.s *= expf(sum.c - c);
+  sum.c = c;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum.s += __shfl_xor_sync(0xffffffffu, sum.s, d);
+  if constexpr (kTeam > 32) {
+    if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = sum;
+    __syncthreads();
+  }
+  if (member == 0) {
+    if constexpr (kTeam > 32)
+      for (int w = 1; w < kWarps; ++w) sum = join(sum, warp_sums[w]);
     if (a.parts > 1) {
       partial[row * a.parts + part] = sum;
     } else {
       if (lse) lse[row] = lse_of(sum);
-      logp[row] = label < a.vocab ? logp_of(sum, static_cast<float>(x[label])) : __int_as_float(0x7FC00000);
+      logp[row] = logp_of(sum, hit);               // (a label past the vocabulary: NaN)
     }
   }
 }
@@ -327,18 +345,19 @@ pairs_kernel(const Rows a, const Loss f, const Sum* __restrict__ partial,
   }
 }
 
-// The gradient of a part of a row.
-template <typename T>
+// The gradient of a part of a row, or of a short row by a warp.
+template <typename T, int kTeam>
 __global__ void __launch_bounds__(kThreads)
 gradient_kernel(const Rows a, const float* __restrict__ lse, const float* __restrict__ dlogp,
                 const float* __restrict__ dloss, T* out, int64_t ldo) {
   const int part = (int)(blockIdx.x % (unsigned)a.parts);
-  const int64_t row = blockIdx.x / (unsigned)a.parts;
+  const int member = threadIdx.x % kTeam;
+  const int64_t row = blockIdx.x / (unsigned)a.parts * (int64_t)(kThreads / kTeam) + threadIdx.x / kTeam;
   const int64_t j0 = (int64_t)part * a.part_cols;
   const int n = (int)min((int64_t)a.part_cols, a.vocab - j0);
   zo::pdl_wait();
   zo::pdl_trigger();
-  if (n <= 0) return;                              // (many parts, each rounded up to eight columns)
+  if (row >= a.rows || n <= 0) return;                              // (many parts, each rounded up to eight columns)
   const int64_t label = a.labels[row];
   const float scale = label < 0 ? 0.0f : dlogp[row] * (dloss ? *dloss : 1.0f);
   const float base = lse[row];
@@ -353,15 +372,15 @@ gradient_kernel(const Rows a, const float* __restrict__ lse, const float* __rest
   const int head = head_of(x, n);
   if (head == head_of(y, n)) {
     const int vecs = (n - head) / Vec<T>::kN;
-    for (int i = threadIdx.x; i < vecs; i += kUnroll * kThreads) {
+    for (int i = member; i < vecs; i += kUnroll * kTeam) {
       uint4 v[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
-        if (!zero && i + u * kThreads < vecs)
-          v[u] = __ldcs(reinterpret_cast<const uint4*>(x + head) + i + u * kThreads);
+        if (!zero && i + u * kTeam < vecs)
+          v[u] = __ldcs(reinterpret_cast<const uint4*>(x + head) + i + u * kTeam);
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const int at = i + u * kThreads;
+        const int at = i + u * kTeam;
         if (at >= vecs) break;
         uint4 r = make_uint4(0u, 0u, 0u, 0u);
         if (!zero) {
@@ -386,12 +405,12 @@ gradient_kernel(const Rows a, const float* __restrict__ lse, const float* __rest
       }
     }
     const int around = head + (n - head) % Vec<T>::kN;
-    if ((int)threadIdx.x < around) {
-      const int k = (int)threadIdx.x < head ? (int)threadIdx.x : n - around + (int)threadIdx.x;
+    if (member < around) {
+      const int k = member < head ? member : n - around + member;
       y[k] = static_cast<T>(zero ? 0.0f : grad(static_cast<float>(x[k]), k));
     }
   } else {
-    for (int k = threadIdx.x; k < n; k += kThreads)
+    for (int k = member; k < n; k += kTeam)
       y[k] = static_cast<T>(zero ? 0.0f : grad(static_cast<float>(x[k]), k));
   }
 }
@@ -404,6 +423,14 @@ int32_t parts_of(int64_t rows, int64_t vocab, int32_t sms) {
   while (parts < kMaxParts && rows * parts < 2 * (int64_t)sms && vocab >= 2 * (int64_t)parts * kPartCols)
     parts *= 2;
   return parts;
+}
+
+// Rows for a warp each: a CTA's joins and its beginning are too much for a short one.
+bool short_rows(int64_t vocab, int32_t dtype, int64_t bytes) {
+  return vocab * (dtype == ZO_BF16 ? 2 : 4) <= bytes;
+}
+unsigned teams(int64_t rows, int32_t parts, bool warps) {
+  return (unsigned)(warps ? (rows + kWarps - 1) / kWarps : rows * parts);
 }
 
 bool elem_aligned(const void* p, int32_t dtype) {
@@ -481,11 +508,14 @@ zo_status zo_preference_forward(const void* logits, int64_t ldl, int64_t rows, i
   auto* ticket = reinterpret_cast<uint32_t*>(ws);
   auto* logp = reinterpret_cast<float*>(ws + 256);
   auto* partial = reinterpret_cast<Sum*>(ws + 256 + (rows * 4 + 255) / 256 * 256);
-  const unsigned grid = rows > 0 ? (unsigned)(rows * a.parts) : 1u;
+  const bool warps = short_rows(vocab, dtype, kShortForward);
+  const unsigned grid = rows > 0 ? teams(rows, a.parts, warps) : 1u;
   const Loss f{kind, average != 0, beta, smoothing, margin};
   const bool half = dtype == ZO_BF16;
-  ZO_CUDA(zo::launch_dependent(half ? rows_kernel<__nv_bfloat16> : rows_kernel<float>, grid, kThreads,
-                               0, s, 1, true, a, partial, logp, lse, dlogp, ticket),
+  using B = __nv_bfloat16;
+  const auto rows_fn = half ? (warps ? rows_kernel<B, 32> : rows_kernel<B, kThreads>)
+                            : (warps ? rows_kernel<float, 32> : rows_kernel<float, kThreads>);
+  ZO_CUDA(zo::launch_dependent(rows_fn, grid, kThreads, 0, s, 1, true, a, partial, logp, lse, dlogp, ticket),
           "preference: rows' kernel");
   ZO_CUDA(zo::launch_dependent(half ? pairs_kernel<__nv_bfloat16> : pairs_kernel<float>,
                                (unsigned)pairs, kPairThreads, 0, s, 1, true, a, f, partial, logp,
@@ -522,14 +552,17 @@ zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t rows, 
   const auto s = reinterpret_cast<cudaStream_t>(stream);
   if (rows * a.parts > INT32_MAX)
     return refuse(ZO_ERR_SHAPE, "zo_preference_backward: too many logits for one call");
-  const unsigned grid = (unsigned)(rows * a.parts);
+  const bool warps = short_rows(vocab, dtype, kShortBackward);
+  const unsigned grid = teams(rows, a.parts, warps);
+  using B = __nv_bfloat16;
   if (dtype == ZO_BF16)
-    ZO_CUDA(zo::launch_dependent(gradient_kernel<__nv_bfloat16>, grid, kThreads, 0, s, 1, true, a, lse,
-                                 dlogp, dloss, static_cast<__nv_bfloat16*>(dlogits), ldd),
+    ZO_CUDA(zo::launch_dependent(warps ? gradient_kernel<B, 32> : gradient_kernel<B, kThreads>, grid,
+                                 kThreads, 0, s, 1, true, a, lse, dlogp, dloss, static_cast<B*>(dlogits), ldd),
             "preference: gradient kernel");
   else
-    ZO_CUDA(zo::launch_dependent(gradient_kernel<float>, grid, kThreads, 0, s, 1, true, a, lse, dlogp,
-                                 dloss, static_cast<float*>(dlogits), ldd),
+    ZO_CUDA(zo::launch_dependent(warps ? gradient_kernel<float, 32> : gradient_kernel<float, kThreads>,
+                                 grid, kThreads, 0, s, 1, true, a, lse, dlogp, dloss,
+                                 static_cast<float*>(dlogits), ldd),
             "preference: gradient kernel");
   return ZO_OK;
 }
