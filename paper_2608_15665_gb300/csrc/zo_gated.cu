@@ -220,8 +220,7 @@ zo_status zo_gated_forward(const void* X, int64_t ldx, int64_t T, int64_t D, con
     zo::GatedForward a{};
     sizes(a);
     a.side = plan.side;
-    a.box_rows = zo::gated_box_rows(T);
-    bool ok = maps(a, a.box_rows, a.side);
+    bool ok = maps(a, 128, a.side);
     for (int k = 0; k < outs; ++k) ok = ok && out_map(&a.out[k], out[k], F, T, ld[k]);
     if (!ok) return refuse(ZO_ERR_CUDA, no_map);
     ZO_CUDA(zo::launch_gated_forward(a, pairs, status, s), "gated forward kernel");

@@ -190,13 +190,13 @@ __device__ __forceinline__ bool tile_at(const GatedTurned& a, int pair, int pair
 }
 
 // One stage of a tile's operands for CTA `rank`.  Tokens past the last are not loaded where they
-// fill a CTA's half, or where there are fewer than a box's: what shared memory holds in their place
-// ends in accumulator lanes that nothing reads.
+// fill a CTA's half (in dX: or are beyond a call's only box): what shared memory holds in their
+// place ends in accumulator lanes that nothing reads.
 __device__ __forceinline__ void load_stage(const GatedForward& a, const Tile& t, int k, uint32_t rank,
                                            uint8_t* dst, uint64_t* full, bool leader) {
   const bool second = t.i0 + 128 < a.T;
   if (leader)
-    mbar_arrive_expect_tx(full, ((second ? 2u : 1u) * (uint32_t)a.box_rows + 2u * (uint32_t)a.side) * 128u);
+    mbar_arrive_expect_tx(full, (second ? 2u : 1u) * kHalfBytes + 2u * (uint32_t)a.side * 128u);
   if (rank == 0 || second) tma_load_2d_to_leader(dst, &a.x, 64 * k, t.i0 + 128 * (int)rank, full);
   tma_load_2d_to_leader(dst + kHalfBytes, &a.w[rank], 64 * k, t.j0, full);
 }

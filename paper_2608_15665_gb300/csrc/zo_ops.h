@@ -173,7 +173,6 @@ struct GatedForward {
   CUtensorMap x, w[2], out[3];      // X; Wg and Wu; H, G and U
   int32_t T, D, F, act, save;
   int32_t side;                     // columns of Wg (and of Wu) to a tile
-  int32_t box_rows;                 // tokens in a box of X
 };
 // the same with the tokens as the products' columns
 struct GatedTurned {
