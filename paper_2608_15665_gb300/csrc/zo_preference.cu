@@ -34,7 +34,7 @@ constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kPairThreads = 512;                // of a pair's two sequences
 constexpr int kUnroll = 4;                       // vectors of 16 bytes a thread has on their way
 constexpr int kMaxParts = 32, kPartCols = 4096;  // parts of a row, none narrower than this
-// Rows of up to so many bytes belong to a warp each (256M logits in bf16, forward: rows of 1000 487 us
+// Whole rows of up to so many bytes belong to a warp each (256M logits in bf16, forward: rows of 1000 487 us
 // by CTAs, 153 by warps; of 8000 104 and 93; backward of 1000 259 and 168, of 8000 152 and 158).
 constexpr int kShortForward = 16384, kShortBackward = 8192;
 // columns of a CTA's part in the backward pass (812 rows of 50257 fp32: 52 us; in whole rows 58, as 5.3
@@ -425,12 +425,16 @@ int32_t parts_of(int64_t rows, int64_t vocab, int32_t sms) {
   return parts;
 }
 
-// Rows for a warp each: a CTA's joins and its beginning are too much for a short one.
-bool short_rows(int64_t vocab, int32_t dtype, int64_t bytes) {
-  return vocab * (dtype == ZO_BF16 ? 2 : 4) <= bytes;
-}
-unsigned teams(int64_t rows, int32_t parts, bool warps) {
-  return (unsigned)(warps ? (rows + kWarps - 1) / kWarps : rows * parts);
+// The CTAs of a call, and whether each of their warps has a row of its own: a CTA's joins and its
+// beginning are too much for a short one.  (Rows in several parts are never short ones: a warp takes a
+// whole row.)
+struct Teams {
+  bool warps;
+  unsigned ctas;
+};
+Teams teams_of(const Rows& a, int32_t dtype, int64_t short_bytes) {
+  const bool warps = a.parts == 1 && a.vocab * (int64_t)(dtype == ZO_BF16 ? 2 : 4) <= short_bytes;
+  return Teams{warps, (unsigned)(warps ? (a.rows + kWarps - 1) / kWarps : a.rows * a.parts)};
 }
 
 bool elem_aligned(const void* p, int32_t dtype) {
@@ -508,8 +512,8 @@ zo_status zo_preference_forward(const void* logits, int64_t ldl, int64_t rows, i
   auto* ticket = reinterpret_cast<uint32_t*>(ws);
   auto* logp = reinterpret_cast<float*>(ws + 256);
   auto* partial = reinterpret_cast<Sum*>(ws + 256 + (rows * 4 + 255) / 256 * 256);
-  const bool warps = short_rows(vocab, dtype, kShortForward);
-  const unsigned grid = rows > 0 ? teams(rows, a.parts, warps) : 1u;
+  const auto [warps, ctas] = teams_of(a, dtype, kShortForward);
+  const unsigned grid = rows > 0 ? ctas : 1u;
   const Loss f{kind, average != 0, beta, smoothing, margin};
   const bool half = dtype == ZO_BF16;
   using B = __nv_bfloat16;
@@ -552,8 +556,7 @@ zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t rows, 
   const auto s = reinterpret_cast<cudaStream_t>(stream);
   if (rows * a.parts > INT32_MAX)
     return refuse(ZO_ERR_SHAPE, "zo_preference_backward: too many logits for one call");
-  const bool warps = short_rows(vocab, dtype, kShortBackward);
-  const unsigned grid = teams(rows, a.parts, warps);
+  const auto [warps, grid] = teams_of(a, dtype, kShortBackward);
   using B = __nv_bfloat16;
   if (dtype == ZO_BF16)
     ZO_CUDA(zo::launch_dependent(warps ? gradient_kernel<B, 32> : gradient_kernel<B, kThreads>, grid,
