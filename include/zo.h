@@ -494,7 +494,8 @@ ZO_API int64_t zo_muon_launches(const zo_muon_ctx* ctx);
  *   bits = 8:  M holds m, and V holds r = sqrt(v), as e4m3 codes (4 exponent bits of bias 7, 3
  *     mantissa bits, 0x7F = NaN) of which each stands for itself times 2^(max(E, 40) - 134) with
  *     the byte E of its block of 256 elements in Em (Ev), ceil(m n / 256) bytes each.  E is the
- *     biased fp32 exponent of the block's largest finite |m| (r).  A step computes in fp32, as
+ *     biased fp32 exponent of the block's largest finite |m| (r; 63 where the largest v is above 0
+ *     but subnormal).  A step computes in fp32, as
  *     above, and W takes the m and v from before their rounding.  That is up or down at random,
  *     by 16 bits of the counter contract's integer stream an element (a mean that moves by a
  *     thousandth a step would never leave a code if it went to the nearest): of the words of
@@ -504,7 +505,8 @@ ZO_API int64_t zo_muon_launches(const zo_muon_ctx* ctx);
  * zo_adamw_step -- one step of every tensor: its number t >= 1 (count NULL), or t = 0 and a
  *   device count that the step raises by one and goes by, so that a captured step may be
  *   replayed.  The states' sums are formed from products that are each rounded to fp32, and r is
- *   rounded to nearest (from v = 2^-102 on): the codes are those of any fp32 evaluation.  A NaN or
+ *   rounded to nearest (from v = 2^-102 on; smaller roots may be too small, by up to 2^-65): the
+ *   codes are those of any fp32 evaluation.  A NaN or
  *   infinity in G gives NaN in its own element of W and m (with 8 bits: so does a G whose square
  *   leaves fp32's range), no others.
  */

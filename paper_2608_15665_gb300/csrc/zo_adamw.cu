@@ -12,7 +12,7 @@
 //
 // States in 8 bits: m and r = sqrt(v) as e4m3 codes times 2^(E - 134), E = the biased fp32
 // exponent of the largest |m| (r) of the block of 256, in one byte; so the block's largest is in
-// [128, 256], and values down to 2^-17 of it keep a code.  r and not v: the codes reach over 17
+// [128, 256], and values down to 2^-17 of it keep a code (where the largest v is subnormal, E is 63).  r and not v: the codes reach over 17
 // binades, v's spread is twice that of r.  Codes are rounded up or down at random, by 16 bits of
 // the Philox stream an element, as v moves by a thousandth of itself a step and the codes are an
 // eighth apart: to nearest, a running mean would never move.  The expectation is the running
@@ -343,8 +343,8 @@ __device__ __forceinline__ float root_of(float v) {
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
-// Square roots rounded to nearest, of 2^-102 <= v < infinity (smaller ones to 2^-22 of them, or of
-// 2^-63): the hardware's reciprocal root y, s = v y, and one Newton step by the residual,
+// Square roots rounded to nearest, of 2^-102 <= v < infinity (smaller ones may come out too small, by
+// less than 2^-65): the hardware's reciprocal root y, s = v y, and one Newton step by the residual,
 // s + (v - s^2) y / 2 (Markstein, IBM J. Res. Dev. 34, 1990).  So a state's codes are those of any
 // other fp32 evaluation.  (Infinity gives NaN, which its code would be in any case.)
 __device__ __forceinline__ float2 rounded_roots(float2 v) {
@@ -458,9 +458,11 @@ struct Unit {
     if constexpr (kEight) {
       bool odd_m, odd_v;
       const uint32_t tm = largest<true>(a, &odd_m), tv = largest<false>(b, &odd_v);
-      // 2^k <= r < 2^(k + 1) where 2^2k <= v < 2^(2k + 2)
+      // 2^k <= r < 2^(k + 1) where 2^2k <= v < 2^(2k + 2); of a subnormal v, r < 2^-63 gets the power
+      // of two of the numbers above it, which leaves it 14 binades of codes (down to 2^-77, where v
+      // ends at 2^-149)
       em = tm >> 23;
-      ev = tv >> 23 ? (uint32_t)((((int)(tv >> 23) - 127) >> 1) + 127) : 0u;
+      ev = tv != 0u ? ((tv >> 23) + 127u) >> 1 : 0u;
       const uint4 random = random_words(
           make_uint4(word, index, now.t, kTagAdamW << 24), st.key);
       encode<true>(a, em, odd_m, random, m);
