@@ -505,8 +505,9 @@ ZO_API int64_t zo_muon_launches(const zo_muon_ctx* ctx);
  * zo_adamw_step -- one step of every tensor: its number t >= 1 (count NULL), or t = 0 and a
  *   device count that the step raises by one and goes by, so that a captured step may be
  *   replayed.  The states' sums are formed from products that are each rounded to fp32, and r is
- *   rounded to nearest (from v = 2^-102 on; smaller roots may be too small, by up to 2^-65): the
- *   codes are those of any fp32 evaluation.  A NaN or
+ *   rounded to nearest (from v = 2^-102 on; smaller roots may be too small, by up to 2^-65, where
+ *   that is nothing beside eps): the codes are those of any fp32 evaluation.  With eps = 0 an
+ *   element whose v is 0 gets m / 0.  A NaN or
  *   infinity in G gives NaN in its own element of W and m (with 8 bits: so does a G whose square
  *   leaves fp32's range), no others.
  */

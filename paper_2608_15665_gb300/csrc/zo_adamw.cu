@@ -356,6 +356,11 @@ __device__ __forceinline__ float2 rounded_roots(float2 v) {
   const float2 rest = zo::fma2(zo::mul2(s, both(-1.0f)), s, v);
   return zo::fma2(rest, zo::mul2(y, both(0.5f)), s);
 }
+// Roots of any v, subnormal ones too, rounded to nearest.  (Infinity gives NaN here as well.)
+template <bool kEight>
+__device__ __forceinline__ float exact_root(float v) {
+  return kEight ? __fsqrt_rn(v) + (v - v) : __fsqrt_rn(v);
+}
 __device__ __forceinline__ float reciprocal(float v) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -422,6 +427,7 @@ struct Unit {
   }
 
   // word: of the lane's eight elements in the stream of random words
+  template <bool kExact>
   __device__ __forceinline__ void compute(uint32_t word, uint32_t index, const Step& st, const Now& now) {
     float x[kLane], y[kLane], a[kLane], b[kLane];
     unpack(g, y);
@@ -445,7 +451,9 @@ struct Unit {
       // know, or it would fuse the sum instead)
       m2 = zo::add2(zo::fma2(b1, m2, none), zo::fma2(c1, gr, none));
       v2 = zo::add2(zo::fma2(b2, v2, none), zo::fma2(c2, zo::mul2(gr, gr), none));
-      const float2 root = kEight ? rounded_roots(v2) : make_float2(root_of(v2.x), root_of(v2.y));
+      const float2 root = kExact   ? make_float2(exact_root<kEight>(v2.x), exact_root<kEight>(v2.y))
+                          : kEight ? rounded_roots(v2)
+                                   : make_float2(root_of(v2.x), root_of(v2.y));
       const float2 den = zo::fma2(root, spread, both(st.eps));
       const float2 move = zo::mul2(zo::mul2(rate, m2), make_float2(reciprocal(den.x), reciprocal(den.y)));
       const float2 to = zo::fma2(keep, make_float2(x[e], x[e + 1]), move);
@@ -473,8 +481,9 @@ struct Unit {
     }
   }
 
+  template <bool kExact>
   __device__ __forceinline__ void finish(const Tensor& t, uint32_t index, const Step& st, const Now& now) {
-    compute((uint32_t)(e0 / kLane), index, st, now);
+    compute<kExact>((uint32_t)(e0 / kLane), index, st, now);
     if constexpr (kEight) {
       const bool any = __shfl_sync(0xffffffffu, count, 0) > 0;
       if (any && (threadIdx.x & 31) == 0) {
@@ -502,7 +511,7 @@ struct Unit {
 // time (131M elements, bf16: 386 us; through shared memory 247 with three blocks ahead and 24 warps,
 // 229 with two and 28, 245 with roots rounded to nearest: 460 instructions a block, 2.9 a cycle,
 // the FMA and the ALU pipe each busy half of the time and in turn in the warps' way).
-template <bool kEight, typename W, typename G>
+template <bool kEight, bool kExact, typename W, typename G>
 __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int units, uint32_t index,
                                           const Step& st, const Now& now) {
   int64_t e0 = first + (int64_t)threadIdx.x * kLane;
@@ -539,7 +548,7 @@ __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int un
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       u.take(mine + k % kStages * kStageBytes, __shfl_sync(0xffffffffu, em, k),
              __shfl_sync(0xffffffffu, ev, k));
-      u.compute(word + (uint32_t)(k * (kRow / kLane)), index, st, now);
+      u.template compute<kExact>(word + (uint32_t)(k * (kRow / kLane)), index, st, now);
       const int o = k * kRow;
       u.w.store(pw + o);
       u.m.store(pm + o);
@@ -553,12 +562,13 @@ __device__ __forceinline__ void run_chunk(const Tensor& t, int64_t first, int un
   }
   for (; k < units; ++k) {
     u.load(t, e0 + (int64_t)k * kRow);
-    u.finish(t, index, st, now);
+    u.template finish<kExact>(t, index, st, now);
   }
 }
 
-// chunks: (tensor, number of the chunk in it)
-template <bool kEight>
+// chunks: (tensor, number of the chunk in it).  kExact: for an eps so small that the hardware's roots of
+// small v would show beside it.
+template <bool kEight, bool kExact>
 __global__ void __launch_bounds__(kThreads, kEight ? kCtas : 8)
 adamw_kernel(const Tensor* __restrict__ tensors, const int2* __restrict__ chunks, int units,
              const __grid_constant__ Step st, Now now, const Now* __restrict__ counted) {
@@ -570,10 +580,10 @@ adamw_kernel(const Tensor* __restrict__ tensors, const int2* __restrict__ chunks
   const int64_t first = (int64_t)at.y * units * kRow;
   using B = __nv_bfloat16;
   switch (t.kind) {
-    case 0: run_chunk<kEight, float, float>(t, first, units, (uint32_t)at.x, st, now); break;
-    case 1: run_chunk<kEight, B, float>(t, first, units, (uint32_t)at.x, st, now); break;
-    case 2: run_chunk<kEight, float, B>(t, first, units, (uint32_t)at.x, st, now); break;
-    default: run_chunk<kEight, B, B>(t, first, units, (uint32_t)at.x, st, now); break;
+    case 0: run_chunk<kEight, kExact, float, float>(t, first, units, (uint32_t)at.x, st, now); break;
+    case 1: run_chunk<kEight, kExact, B, float>(t, first, units, (uint32_t)at.x, st, now); break;
+    case 2: run_chunk<kEight, kExact, float, B>(t, first, units, (uint32_t)at.x, st, now); break;
+    default: run_chunk<kEight, kExact, B, B>(t, first, units, (uint32_t)at.x, st, now); break;
   }
 }
 
@@ -773,9 +783,14 @@ zo_status zo_adamw_step(zo_adamw_ctx* c, int64_t t, int64_t* count, double lr, d
   if (c->plan.chunks == 0) return ZO_OK;
   const auto* ts = reinterpret_cast<const Tensor*>(c->ws + c->plan.tensors_at);
   const auto* chunks = reinterpret_cast<const int2*>(c->ws + c->plan.chunks_at);
-  ZO_CUDA(zo::launch_dependent(c->bits == 8 ? adamw_kernel<true> : adamw_kernel<false>,
-                               (unsigned)c->plan.chunks, kThreads, c->bits == 8 ? kRingBytes : 0,
-                               c->stream, 1, true, ts, chunks, c->plan.units, st, now, count ? counted : nullptr),
+  // The fast roots of subnormal v are off by up to 2^-63, which the bias correction multiplies by
+  // 1 / sqrt(1 - b2) at most: below 2^-25 of eps, else the exact ones.
+  const bool exact = eps < 0x1p-38 / std::sqrt(1.0 - beta2);
+  const auto kernel = c->bits == 8 ? (exact ? adamw_kernel<true, true> : adamw_kernel<true, false>)
+                                   : (exact ? adamw_kernel<false, true> : adamw_kernel<false, false>);
+  ZO_CUDA(zo::launch_dependent(kernel, (unsigned)c->plan.chunks, kThreads,
+                               c->bits == 8 ? kRingBytes : 0, c->stream, 1, true, ts, chunks,
+                               c->plan.units, st, now, count ? counted : nullptr),
           "AdamW kernel");
   ++c->launches;
   return ZO_OK;
