@@ -210,28 +210,32 @@ struct Loss {
   float beta, smoothing, margin;
 };
 
-// The loss of a pair and its derivative by D.
-__device__ __forceinline__ void pair_loss(const Loss& f, double D, float* loss, float* slope) {
+// The loss of a pair and its derivative by D.  D and z stay in 64 bits as the sums are, and so do the
+// parts that are linear in z; e = exp(-|z|) is fp32's, with the rest of z that fp32 drops (2^-24 of z, and
+// as much of e) put back.  (exp and log1p in 64 bits would make a call 1.7 us longer: one thread of a
+// pair works here, and the GPU's 64-bit units are few.)
+__device__ __forceinline__ void pair_loss(const Loss& f, double D, double* loss, double* slope) {
+  const double beta = f.beta;
   if (f.kind == ZO_PREFERENCE_SQUARE) {
-    const double d = D - 0.5 / (double)f.beta;
-    *loss = (float)(d * d);
-    *slope = (float)(2.0 * d);
+    const double d = D - 0.5 / beta;
+    *loss = d * d;
+    *slope = 2.0 * d;
     return;
   }
-  const float z = (float)((double)f.beta * D - (double)f.margin);
+  const double z = beta * D - (double)f.margin;
   if (f.kind == ZO_PREFERENCE_HINGE) {
-    *loss = z < 1.0f ? 1.0f - z : z >= 1.0f ? 0.0f : z;              // (NaN stays)
-    *slope = z < 1.0f ? -f.beta : z >= 1.0f ? 0.0f : z;
+    *loss = z < 1.0 ? 1.0 - z : z >= 1.0 ? 0.0 : z;                  // (NaN stays)
+    *slope = z < 1.0 ? -beta : z >= 1.0 ? 0.0 : z;
     return;
   }
-  // -log sig(z) = log(1 + exp(-|z|)) + max(-z, 0)
-  const float e = expf(-fabsf(z)), both = log1pf(e);
-  const float p = z >= 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);    // sig(z)
-  const float q = z >= 0.0f ? e / (1.0f + e) : 1.0f / (1.0f + e);    // 1 - sig(z)
-  const float a = f.smoothing;
+  // -log sig(z) = log(1 + e) + max(-z, 0), sig(-|z|) = e / (1 + e)
+  const float size = fabsf((float)z), near = expf(-size);
+  const float e = near > 0.0f ? fmaf(near, (float)((double)size - fabs(z)), near) : near;   // (0: so far that z may be infinite)
+  const double far = e / (1.0f + e);
+  const double a = f.smoothing;
   // (a product of zero with an infinite side is left out)
-  *loss = both + (z < 0.0f ? -z * (1.0f - a) : a > 0.0f ? z * a : z == z ? 0.0f : z);
-  *slope = f.beta * (a * p - (1.0f - a) * q);
+  *loss = (double)log1pf(e) + (z < 0.0 ? -z * (1.0 - a) : a > 0.0 ? z * a : z == z ? 0.0 : z);
+  *slope = beta * (a - (z < 0.0 ? 1.0 - far : far));                 // a sig(z) - (1 - a) (1 - sig(z))
 }
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -307,11 +311,11 @@ pairs_kernel(const Rows a, const Loss f, const Sum* __restrict__ partial,
       logps[pair + k * a.pairs] = (float)s;
       gain[k] = s - (ref ? (double)ref[pair + k * a.pairs] : 0.0);
     }
-    float value, slope;
+    double value, slope;
     pair_loss(f, gain[0] - gain[1], &value, &slope);
-    losses[pair] = value;
+    losses[pair] = (float)value;
     for (int k = 0; k < 2; ++k) {
-      const double by = (k ? -1.0 : 1.0) * (double)slope / (double)a.pairs;
+      const double by = (k ? -1.0 : 1.0) * slope / (double)a.pairs;
       slopes[k] = (float)(f.average && n[k] > 0.0 ? by / n[k] : by);
     }
     __threadfence();
