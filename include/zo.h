@@ -606,8 +606,8 @@ ZO_API zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t
  * not overlap inputs.  No atomics: the same inputs give the same bits.  Asynchronous on `stream`
  * (void* cudaStream_t) of the current device.
  * zo_gated_sync_status -- synchronise the stream; ZO_ERR_TIMEOUT, once, where a wait of one of
- *   these kernels on the current device has run out since it was last asked (its results are
- *   incomplete then); ZO_OK otherwise.
+ *   these kernels on the current device has run out since it was last asked (what it kept from
+ *   being formed is NaN then); ZO_OK otherwise.
  */
 enum { ZO_GATED_SILU = 0, ZO_GATED_GELU_TANH = 1 };
 

@@ -14,7 +14,7 @@
 // Bound by HBM (one token on the 7B shapes: 180 MB in 31 us).  Roles (256 threads): warp 0 loads by TMA, warp 1 issues the MMAs (an elected lane
 // each) and owns the Tensor Memory, then all eight warps empty the accumulator.  Every wait is
 // bounded; a give-up sets the status word, the producer waits for its copies in flight, the MMA warp
-// for its MMAs, and Tensor Memory is freed.
+// for its MMAs, NaN is stored where the sums are not known to be whole, and Tensor Memory is freed.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -157,24 +157,35 @@ gated_few_kernel(const __grid_constant__ GatedFew a, uint32_t* __restrict__ stat
       }
     }
     if (!ok) {
-      if (lane == 0) give_up(sh, status);
+      if (lane == 0) {
+        give_up(sh, status);
+        __threadfence_block();                  // (the flag is seen by whoever sees the commit)
+      }
+      __syncwarp();
       if (elected()) mma_commit(&sh.acc_full);  // every MMA has completed before Tensor Memory is freed
       __syncwarp();
     }
   }
   __syncwarp();
-  // (after a give-up acc_full says that the MMAs so far are done; nothing of them is stored)
+  // (after a give-up acc_full says that the MMAs so far are done; nothing of them is stored.  One
+  // answer for the whole warp, as its lanes read Tensor Memory together.)
   const bool done = warp_wait(&sh.acc_full, 0, nullptr);
   if (!done && lane == 0) give_up(sh, status);
+  const bool lost = __any_sync(0xffffffffu, !done || *abort);
   tc_fence_after();
   const int row = 32 * (warp & 3) + lane;
-  if (done && !*abort && 32 * (warp & 3) < a.T) {
+  if (32 * (warp & 3) < a.T) {
     const uint32_t from = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
     for (int c = warp >> 2; c < a.cols / 16 && col0 + 16 * c < a.F; c += 2) {
       uint32_t gr[16], ur[16];
-      tmem_ld_32x32b_x16(from + (uint32_t)(16 * c), gr);
-      tmem_ld_32x32b_x16(from + (uint32_t)(a.cols + 16 * c), ur);
-      tmem_ld_wait();
+      if (!lost) {
+        tmem_ld_32x32b_x16(from + (uint32_t)(16 * c), gr);
+        tmem_ld_32x32b_x16(from + (uint32_t)(a.cols + 16 * c), ur);
+        tmem_ld_wait();
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) gr[e] = ur[e] = 0x7FC00000u;
+      }
       float g[16], u[16], h[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {

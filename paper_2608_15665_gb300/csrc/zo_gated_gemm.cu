@@ -38,7 +38,8 @@
 //               accumulators.
 //   warps 2..9: epilogue: warp w reads TMEM lanes 32 (w % 4) .. + 31, every other 16 columns, and
 //               stores 32 x 16 boxes by TMA (32-byte swizzle), three of them in turn.
-// Every wait is bounded; a give-up sets the abort flag of both CTAs and the status word.
+// Every wait is bounded; a give-up sets the abort flag of both CTAs and the status word, and the
+// epilogue's warps store NaN for the tiles that they have not seen the end of.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -312,6 +313,34 @@ __device__ __forceinline__ void to_floats(const uint32_t (&r)[16], float (&v)[16
 #pragma unroll
   for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(r[e]);
 }
+__device__ __forceinline__ void to_nan(float (&v)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = __int_as_float(0x7FC00000);
+}
+// Sixteen columns of this warp's lanes of an accumulator, or of two; lost: there is none.
+__device__ __forceinline__ void columns(uint32_t tmem, bool lost, float (&v)[16]) {
+  if (lost) {
+    to_nan(v);
+    return;
+  }
+  uint32_t r[16];
+  tmem_ld_32x32b_x16(tmem, r);
+  tmem_ld_wait();
+  to_floats(r, v);
+}
+__device__ __forceinline__ void columns(uint32_t g_at, uint32_t u_at, bool lost, float (&g)[16], float (&u)[16]) {
+  if (lost) {
+    to_nan(g);
+    to_nan(u);
+    return;
+  }
+  uint32_t gr[16], ur[16];
+  tmem_ld_32x32b_x16(g_at, gr);
+  tmem_ld_32x32b_x16(u_at, ur);
+  tmem_ld_wait();
+  to_floats(gr, g);
+  to_floats(ur, u);
+}
 
 __device__ __forceinline__ void activate(int32_t act, const float (&g)[16], const float (&u)[16],
                                          float (&h)[16]) {
@@ -324,19 +353,14 @@ __device__ __forceinline__ void activate(int32_t act, const float (&g)[16], cons
   }
 }
 
-// The accumulator at `tmem` (this warp's lanes) to the results: 32 rows from row0 on.
+// The accumulator at `tmem` (this warp's lanes) to the results: 32 rows from row0 on, or NaN in their place.
 __device__ __forceinline__ void finish(const GatedForward& a, const Tile& t, uint32_t tmem, int half,
-                                       int row0, int, Boxes& boxes) {
+                                       int row0, int, bool lost, Boxes& boxes) {
   for (int c = half; c < a.side / 16; c += 2) {
     const int col = t.j0 + 16 * c;
     if (row0 >= a.T || col >= a.F) break;
-    uint32_t gr[16], ur[16];
-    tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * c), gr);
-    tmem_ld_32x32b_x16(tmem + (uint32_t)(a.side + 16 * c), ur);
-    tmem_ld_wait();
     float g[16], u[16], h[16];
-    to_floats(gr, g);
-    to_floats(ur, u);
+    columns(tmem + (uint32_t)(16 * c), tmem + (uint32_t)(a.side + 16 * c), lost, g, u);
     activate(a.act, g, u, h);
     boxes.store(h, &a.out[0], col, row0);
     if (a.save) {
@@ -346,17 +370,12 @@ __device__ __forceinline__ void finish(const GatedForward& a, const Tile& t, uin
   }
 }
 __device__ __forceinline__ void finish(const GatedTurned& a, const Tile& t, uint32_t tmem, int half,
-                                       int row0, int, Boxes& boxes) {
+                                       int row0, int, bool lost, Boxes& boxes) {
   for (int c = half; c < a.tokens / 16; c += 2) {
     const int token = t.j0 + 16 * c;
     if (row0 >= a.F || token >= a.T) break;
-    uint32_t gr[16], ur[16];
-    tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * c), gr);
-    tmem_ld_32x32b_x16(tmem + (uint32_t)(kTileCols + 16 * c), ur);
-    tmem_ld_wait();
     float g[16], u[16], h[16];
-    to_floats(gr, g);
-    to_floats(ur, u);
+    columns(tmem + (uint32_t)(16 * c), tmem + (uint32_t)(kTileCols + 16 * c), lost, g, u);
     activate(a.act, g, u, h);
     boxes.store_turned(h, &a.out[0], row0, token);
     if (a.save) {
@@ -368,7 +387,7 @@ __device__ __forceinline__ void finish(const GatedTurned& a, const Tile& t, uint
 // warp: of the pair's sixteen.  Of a tile whose K is split, each warp leaves its part's sums in
 // memory (32 lanes apart for coalescing), and the last part's adds them up in the parts' order.
 __device__ __forceinline__ void finish(const GatedBackward& a, const Tile& t, uint32_t tmem, int half,
-                                       int row0, int warp, Boxes& boxes) {
+                                       int row0, int warp, bool lost, Boxes& boxes) {
   constexpr int kChunks = kTileCols / 32;             // of a warp
   const CUtensorMap* to = t.dw < 0 ? &a.dx : &a.dw[t.dw];
   const bool twin = t.dw < 0 && a.twin;
@@ -383,11 +402,10 @@ __device__ __forceinline__ void finish(const GatedBackward& a, const Tile& t, ui
 #pragma unroll 1
     for (int i = 0; i < kChunks; ++i) {
       if (t.j0 + 16 * (half + 2 * i) >= a.D) break;
-      uint32_t r[16];
-      tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * (half + 2 * i)), r);
-      tmem_ld_wait();
+      float v[16];
+      columns(tmem + (uint32_t)(16 * (half + 2 * i)), lost, v);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) mine[(i * 16 + e) * 32] = __uint_as_float(r[e]);
+      for (int e = 0; e < 16; ++e) mine[(i * 16 + e) * 32] = v[e];
     }
     __threadfence();
     __syncwarp();
@@ -409,10 +427,7 @@ __device__ __forceinline__ void finish(const GatedBackward& a, const Tile& t, ui
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] += __ldcg(from + p * kGatedPartFloats + (i * 16 + e) * 32);
     } else {
-      uint32_t r[16];
-      tmem_ld_32x32b_x16(tmem + (uint32_t)(16 * c), r);
-      tmem_ld_wait();
-      to_floats(r, v);
+      columns(tmem + (uint32_t)(16 * c), lost, v);
     }
     if (!twin) {
       boxes.store(v, to, t.j0 + 16 * c, row0);
@@ -562,13 +577,14 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
     bool ok = true;
     Tile t;
     for (int k = 0; tile_at(a, pair, pairs, k, &t); ++k) {
-      if (!warp_wait(&sh.acc_full[acc], parity, abort)) {
-        ok = false;
-        break;
+      if (ok && !warp_wait(&sh.acc_full[acc], parity, abort)) {
+        ok = false;                            // this tile and the later ones: NaN, and no more waits
+        if (lane == 0) give_up(sh, status);
       }
       tc_fence_after();
       finish(a, t, tmem + ((uint32_t)(32 * g) << 16) + acc_at<Args>(acc), half,
-             t.i0 + 128 * (int)rank + 32 * g, (int)rank * kEpiWarps + warp - 2, boxes);
+             t.i0 + 128 * (int)rank + 32 * g, (int)rank * kEpiWarps + warp - 2, !ok, boxes);
+      if (!ok) continue;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) arrive_leader(&sh.acc_empty[acc]);
@@ -577,7 +593,6 @@ gated_kernel(const __grid_constant__ Args a, uint32_t* __restrict__ status) {
         parity ^= 1u;
       }
     }
-    if (!ok && lane == 0) give_up(sh, status);
     if (lane == 0) bulk_wait_all();
   }
 

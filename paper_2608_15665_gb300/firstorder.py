@@ -546,7 +546,7 @@ def gated_linear_backward(dh, x, w_gate, w_up, gate, up, act="silu", want_x=True
 
 def gated_linear_sync(device=None):
     """Waits for the current stream, and raises where a wait inside a gated linear block's kernel has
-    run out on this device since it was last asked (results of that call are incomplete then)."""
+    run out on this device since it was last asked (results of that call are NaN then, in part or whole)."""
     with torch.cuda.device(device):
         zb.zo_gated_sync_status(torch.cuda.current_stream())
 
