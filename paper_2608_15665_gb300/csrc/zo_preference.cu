@@ -363,7 +363,8 @@ gradient_kernel(const Rows a, const float* __restrict__ lse, const float* __rest
   zo::pdl_trigger();
   if (row >= a.rows || n <= 0) return;                              // (many parts, each rounded up to eight columns)
   const int64_t label = a.labels[row];
-  const float scale = label < 0 ? 0.0f : dlogp[row] * (dloss ? *dloss : 1.0f);
+  const float share = label < 0 ? 0.0f : dlogp[row];
+  const float scale = share == 0.0f ? 0.0f : share * (dloss ? *dloss : 1.0f);   // (dloss may be no number)
   const float base = lse[row];
   // (x and out may be the same memory: a thread writes what it has read itself)
   const T* x = static_cast<const T*>(a.x) + row * a.ld + j0;
