@@ -96,7 +96,8 @@ __global__ void __launch_bounds__(kThreads) gated_gradients_kernel(const Gradien
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float rest = v[i] - value(hi, i);
-      v[i] = rest == rest ? rest : 0.0f;          // (infinities stay in the first row)
+      // (infinities stay in the first row, those that the rounding makes as well)
+      v[i] = fabsf(rest) < __int_as_float(0x7F800000) ? rest : 0.0f;
     }
     *reinterpret_cast<uint4*>(to + out + F) = packed(v);
   };
