@@ -507,9 +507,9 @@ ZO_API int64_t zo_muon_launches(const zo_muon_ctx* ctx);
  *   replayed.  The states' sums are formed from products that are each rounded to fp32, and r is
  *   rounded to nearest (from v = 2^-102 on; smaller roots may be too small, by up to 2^-65, where
  *   that is nothing beside eps): the codes are those of any fp32 evaluation.  With eps = 0 an
- *   element whose v is 0 gets m / 0.  A NaN or
- *   infinity in G gives NaN in its own element of W and m (with 8 bits: so does a G whose square
- *   leaves fp32's range), no others.
+ *   element whose v is 0 gets m / 0.  What
+ *   is not finite in G makes W NaN in its own element and m and v not finite there (8 bits: NaN); with
+ *   8 bits a G whose square leaves fp32's range makes W and v NaN.  No other element sees it.
  */
 typedef struct zo_adamw_tensor {
   void* W;            /* device; m x n, row stride ldw elements, dtype below */
@@ -603,8 +603,9 @@ ZO_API zo_status zo_preference_backward(const void* logits, int64_t ldl, int64_t
  * Every matrix is 16-byte aligned and its row stride (ldx, ... in elements) a multiple of 8; D and
  * F are multiples of 8 below 2^24, T any number from 0 on below it (no tokens: dWg and dWu are zero),
  * with T D, T F <= 2^34 and D F <= 2^37.  Outputs must
- * not overlap inputs.  No atomics: the same inputs give the same bits.  Asynchronous on `stream`
- * (void* cudaStream_t) of the current device.
+ * not overlap inputs.  The same inputs give the same bits: no order of sums depends on timing (split sums
+ * are counted by atomics in the workspace and added in the order of their parts).  Asynchronous on
+ * `stream` (void* cudaStream_t) of the current device.
  * zo_gated_sync_status -- synchronise the stream; ZO_ERR_TIMEOUT, once, where a wait of one of
  *   these kernels on the current device has run out since it was last asked (what it kept from
  *   being formed is NaN then); ZO_OK otherwise.

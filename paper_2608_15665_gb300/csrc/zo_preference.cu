@@ -7,7 +7,7 @@
 //
 // Bound by HBM: the forward pass reads every counted row once (a running maximum c and the sum of
 // e^(l - c) in each thread, joined over the CTA), the backward pass reads and writes them once;
-// rows that do not count are not read (16 pairs of 600, 32000 bf16: 143 us, 93% of the copy rate;
+// rows that do not count are not read (16 pairs of 600, 32000 bf16: 144 us, 92% of the copy rate;
 // backward 8 of 1000: 341 us, 102%).  A CTA takes one row, or a part of one where the rows
 // alone do not fill the device.  (l - c first, then its product with log2 e: logits of the type's
 // lowest value, in one place or in all, overflow nowhere that matters.)
@@ -29,7 +29,7 @@ namespace {
 using namespace zo::host;
 
 // Small CTAs: one's first loads and last sums lie under the others' (16 pairs, 32000 wide: forward
-// 139 us with 128 threads, 148 with 256, 209 with 512).
+// 144 us with 128 threads, 151 with 256, 177 with 512).
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kPairThreads = 512;                // of a pair's two sequences
 constexpr int kUnroll = 4;                       // vectors of 16 bytes a thread has on their way

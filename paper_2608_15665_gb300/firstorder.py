@@ -321,7 +321,9 @@ def adamw_state(weight, bits=32):
 class AdamW(_Handle):
     """The AdamW optimiser over a list of tensors (bf16 or fp32, on one CUDA device) whose
     gradients live in ``grads`` (allocated beside the weights, zero, if not given) and whose
-    states, in 32 or 8 bits, in ``states``.  ``seed``: of the 8-bit states' random rounding.
+    states, in 32 or 8 bits, in ``states``.  ``seed``: of the 8-bit states' random rounding (handles
+    of the same seed take the same bits for their tensors of the same index: give each its own).  A
+    handle is made once and kept: making it uploads its tables and waits for them.
     ``steps``: the number of steps taken, kept on the host; a step is told its number by it.
     ``count``: a one-element int64 tensor on the device, which takes its place: then a step that
     was captured into a graph may be replayed."""
